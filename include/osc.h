@@ -53,8 +53,9 @@
  * Beyond the paper's main path, each in its own section below: the quantizers fused into their producers
  * (RMSNorm + Algorithm 2, SwiGLU + per-token FP8), the grouped form with the MoE dispatch fused behind the
  * quantizer, the MXFP8 form of the fallback, the NVFP4 / G = 16 form of the OSC path, the dynamic-protection
- * control group of Section 4.2 (a measured baseline), offline profiling (Algorithm 1), and osc_linear_static
- * (a deployment aid).
+ * control group of Section 4.2 (a measured baseline), offline profiling (Algorithm 1), osc_linear_static
+ * (a deployment aid), and what a served layer runs between its QKV projection and o_proj (pages and slots of a
+ * key/value cache, norm and rotation of the heads, attention with shared prefixes).
  *
  * Kernel selection is internal and depends only on the shape.  Few rows (M <= 32; <= 64 for layers with more
  * 128-feature tiles than SMs or a long K loop; <= 256 for long K loops with few tiles) run on a
@@ -535,6 +536,85 @@ osc_status osc_nvfp4_linear_grouped_gather(const osc_weights* w, const void* X, 
 osc_status osc_nvfp4_rmsnorm_linear_grouped_gather(const osc_weights* w, const void* H, int T, int64_t ldh, const void* gamma,
                                                    float eps, const int32_t* row_token, const int32_t* off, int M_total, int ex,
                                                    void* Y, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream);
+
+/* --------------------------------- between the QKV projection and o_proj: a paged key/value cache */
+
+/* Keys and values of one layer in pages of page_size tokens.  Dev bf16; channel d of head h of the token at place s
+ * of page p is element p * page_stride + s * token_stride + h * head_stride + d, for K and V alike (so both
+ * [page][token][head][channel] and [page][head][token][channel] buffers fit, and K and V may lie in one buffer).
+ * head_dim is 64 or 128; strides are elements, multiples of 8; n_pages * page_size < 2^31.  A "slot" is
+ * page * page_size + place.  The struct is host memory, read during the call. */
+typedef struct {
+    void* k;
+    void* v;
+    int32_t n_pages, page_size, n_heads, head_dim;
+    int64_t page_stride, token_stride, head_stride;
+} osc_kv_cache_t;
+
+/* Pages, slots and positions of a step's new tokens, from the lengths of R requests (once per step, for all layers).
+ *   cached, fresh: dev int32 [R]: tokens in the cache before the step, and new ones (0 allowed)
+ *   base:          dev int32 [R] or null (0): position of the request's first own token (a shared prefix's length)
+ *   free_pages:    dev int32 [n_free]: pages to hand out, in order
+ *   table:         dev int32 [R][ld_table], cols columns: the request's pages; entries of pages held already are read,
+ *                  those of new pages are written, the rest is left as it is
+ * Request r takes ceil((cached + fresh) / page_size) - ceil(cached / page_size) pages, requests in order.  Outputs:
+ *   row_off: int32 [R + 1]: first row of every request among the step's tokens, row_off[R] = number of tokens
+ *   kv_len:  int32 [R]: cached + fresh
+ *   slots, positions: int32 [T]: slot and position of every token; rows from row_off[R] on (a step filled up to a
+ *            captured size) get slot -1 and position 0
+ *   taken:   int32 [1]: pages taken.  More than n_free: the list ran out; table entries past it and the slots of
+ *            their tokens are -1.  Slots of tokens whose page lies past cols, or whose table entry is negative, are -1 too.
+ * More than T tokens: only the first T get slots and positions.  A second call with the same inputs gives the same
+ * outputs.  Negative lengths count as 0. */
+osc_status osc_kv_slots(const int32_t* cached, const int32_t* fresh, const int32_t* base, int R, int page_size,
+                        const int32_t* free_pages, int n_free, int32_t* table, int cols, int64_t ld_table, int T,
+                        int32_t* row_off, int32_t* kv_len, int32_t* slots, int32_t* positions, int32_t* taken, void* stream);
+
+/* Rotation by position.  Pair i of rot_dim / 2 turns by positions[axis[i]][t] * inv_freq[i] (the product is exact, also for
+ * far positions); its channels are (i, i + rot_dim / 2), or (2i, 2i + 1) when interleaved; channels from rot_dim on are
+ * not turned.  axes = 1: one position per token; 2 or 3: image and video positions (time, height, width), axis[i]
+ * (dev uint8 [rot_dim / 2], null = all 0) says by which of them pair i turns.  inv_freq: dev float [rot_dim / 2].  scale
+ * multiplies the turned channels (1 where the model has no such factor).  rot_dim: a multiple of 16, <= head_dim. */
+typedef struct {
+    const float* inv_freq;
+    const uint8_t* axis;
+    int32_t rot_dim, axes, interleaved;
+    float scale;
+} osc_rope_t;
+
+/* QKV [T, (n_q + 2 n_kv) * head_dim] (the QKV projection's output: query heads, key heads, value heads; n_kv and head_dim
+ * from the cache) in one pass: RMSNorm of every query and key head (gamma_q / gamma_k: dev bf16 [head_dim]; null = no
+ * norm), rotation, one rounding to bf16; queries to Q (dev bf16 [T, ldq]; may be QKV itself), keys and values (copied)
+ * to the tokens' slots of the cache.
+ *   positions: dev int32 [axes][ld_pos];  slots: dev int32 [T], or null: token t at slot t.
+ * Tokens with a slot outside 0 .. n_pages * page_size - 1 write nothing to the cache.  Two tokens must not share a
+ * slot.  Arithmetic in fp32, angles in double.  T == 0 is a no-op. */
+osc_status osc_qk_norm_rope(const void* QKV, int T, int64_t ld, int n_q, const osc_kv_cache_t* cache, const void* gamma_q,
+                            const void* gamma_k, float eps, const osc_rope_t* rope, const int32_t* positions, int64_t ld_pos,
+                            const int32_t* slots, void* Q, int64_t ldq, void* stream);
+
+/* Attention of a step's tokens over the cache.  Rows row_off[r] .. row_off[r + 1] - 1 of Q (dev bf16 [T, ldq], n_q heads,
+ * n_q a multiple of the cache's n_heads, at most 128 query heads per key/value head) are the n new tokens of request r,
+ * the last n of its kv_len[r] own keys, which lie in the pages of table row r; token i sees own keys j <= kv_len[r] - n + i.
+ * Optionally P groups of consecutive requests share a prefix each: requests group_off[g] .. group_off[g + 1] - 1 see, before
+ * their own keys, all prefix_len[g] keys in the pages of prefix_table row g, which lie in the cache once and are read
+ * once for the whole group.  Groups are in order and do not overlap; a request may be in none.
+ *   O = softmax(scale * Q K^T) V per head, dev bf16 [T, ldo]; lse (dev float [T][n_q], or null): natural logarithm of the
+ *   sum of exp(scale * q . k).  A row without any key gives 0 and -inf.  Rows from row_off[R] on are left as they are.
+ * Sums and the running maximum in fp32, weights in bf16.  page_size: a power of two of at least 16.  Lengths are read on
+ * the device: kv_len and prefix_len are cut to what the table's columns hold, a table entry outside 0 .. n_pages - 1 reads as a
+ * page of zeros, and nothing behind a length is used, whatever the cache holds there (NaN too).  A key that is masked for a row only by
+ * the order of the request's own new tokens still meets that row with weight 0, so an Inf or NaN in the VALUE of a new
+ * token reaches the rows of the tokens before it in the same request.
+ * max_new: most new tokens of any request if the caller knows (1 in a decoding step), 0 otherwise; a choice of kernel, the
+ * result holds whatever it says.  Workspace: osc_paged_attention_workspace_bytes with the same n_q, head_dim and with T, R, P at least the call's.
+ * P = 0: group_off, prefix_len and prefix_table are not read. */
+osc_status osc_paged_attention_workspace_bytes(int T, int n_q, int head_dim, int R, int P, size_t* bytes);
+osc_status osc_paged_attention(const void* Q, int T, int64_t ldq, int n_q, const osc_kv_cache_t* cache, int R,
+                               const int32_t* row_off, const int32_t* kv_len, const int32_t* table, int cols, int64_t ld_table,
+                               int P, const int32_t* group_off, const int32_t* prefix_len, const int32_t* prefix_table,
+                               int prefix_cols, int64_t ld_prefix, int max_new, float scale, void* O, int64_t ldo, float* lse,
+                               void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -61,6 +61,16 @@ class Mxfp8ActSizes(C.Structure):
                                           "sched_offset", "workspace_bytes")]
 
 
+class KvCacheStruct(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("n_pages", C.c_int32), ("page_size", C.c_int32), ("n_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("page_stride", C.c_int64), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class RopeStruct(C.Structure):
+    _fields_ = [("inv_freq", C.c_void_p), ("axis", C.c_void_p), ("rot_dim", C.c_int32), ("axes", C.c_int32),
+                ("interleaved", C.c_int32), ("scale", C.c_float)]
+
+
 _vp, _i, _i64, _sz = C.c_void_p, C.c_int, C.c_int64, C.c_size_t
 _SIGS = {
     "osc_status_string": (C.c_char_p, [_i]),
@@ -139,6 +149,12 @@ _SIGS = {
     "osc_mxfp8_quantize": (_i, [_vp, _i, _i, _i64, _vp, _vp, _vp]),
     "osc_mxfp8_gemm": (_i, [_vp, _vp, _vp, _i, _vp, _i64, _vp]),
     "osc_mxfp8_linear": (_i, [_vp, _vp, _i, _i64, _vp, _i64, _vp, _sz, _vp]),
+    "osc_kv_slots": (_i, [_vp, _vp, _vp, _i, _i, _vp, _i, _vp, _i, _i64, _i, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "osc_qk_norm_rope": (_i, [_vp, _i, _i64, _i, C.POINTER(KvCacheStruct), _vp, _vp, C.c_float, C.POINTER(RopeStruct), _vp, _i64,
+                              _vp, _vp, _i64, _vp]),
+    "osc_paged_attention_workspace_bytes": (_i, [_i, _i, _i, _i, _i, C.POINTER(_sz)]),
+    "osc_paged_attention": (_i, [_vp, _i, _i64, _i, C.POINTER(KvCacheStruct), _i, _vp, _vp, _vp, _i, _i64, _i, _vp, _vp, _vp, _i,
+                                 _i64, _i, C.c_float, _vp, _i64, _vp, _vp, _sz, _vp]),
 }
 for _name, (_res, _args) in _SIGS.items():
     _f = getattr(_lib, _name)
@@ -795,3 +811,117 @@ def osc_rmsnorm_linear_swiglu_grouped_gather(w: OscWeights, Hin: torch.Tensor, g
                                                          float(eps), _ptr(row_token), _ptr(off), M, _ptr(H),
                                                          H.stride(0) if M else w.N // 2, _ptr(workspace),
                                                          workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+# ------------------------------- between the QKV projection and o_proj: a paged key/value cache
+
+def _want(name, t, dtype, ndim=None):
+    """The calls below read lengths and tables on the device, where a wrong type would go unnoticed: checked here."""
+    if t is None:
+        return
+    if t.dtype != dtype or (ndim is not None and t.dim() != ndim):
+        raise ValueError(f"{name}: {ndim if ndim is not None else 'any'}-d {dtype} expected, got {t.dim()}-d {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name}: cuda tensor expected")
+    if _raw_device is not None and t.device.index != _raw_device():
+        raise ValueError(f"{name}: lies on {t.device}, the current device is cuda:{_raw_device()}")
+    if t.dim() and t.numel() and t.stride(-1) != 1 and t.shape[-1] != 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+
+
+class KvCache:
+    """Keys and values of one layer: cuda bf16 [n_pages, page_size, n_heads, head_dim] views, any strides that leave the
+    channels contiguous (a permuted [n_pages, n_heads, page_size, head_dim] buffer too), the same for k and v."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor):
+        _want("k", k, torch.bfloat16, 4)
+        _want("v", v, torch.bfloat16, 4)
+        if k.shape != v.shape or any(a != b for n, a, b in zip(k.shape, k.stride(), v.stride()) if n > 1):
+            raise ValueError("k and v must have the same shape and strides")
+        self.k, self.v = k, v
+        n_pages, page_size, n_heads, head_dim = k.shape
+        st = [s if n > 1 else 8 * ((head_dim + 7) // 8) for n, s in zip(k.shape[:3], k.stride()[:3])]
+        self.n_pages, self.page_size, self.n_heads, self.head_dim = n_pages, page_size, n_heads, head_dim
+        self.c = KvCacheStruct(_ptr(k), _ptr(v), n_pages, page_size, n_heads, head_dim, *st)
+
+
+class Rope:
+    """Rotation by position: inv_freq cuda float32 [rot_dim / 2]; axis cuda uint8 [rot_dim / 2] (which of the position
+    axes turns a pair) or None."""
+
+    def __init__(self, inv_freq: torch.Tensor, axis: torch.Tensor = None, interleaved: bool = False, scale: float = 1.0):
+        _want("inv_freq", inv_freq, torch.float32, 1)
+        _want("axis", axis, torch.uint8, 1)
+        if axis is not None and axis.shape != inv_freq.shape:
+            raise ValueError("axis and inv_freq must have the same length")
+        self.inv_freq, self.axis, self.interleaved, self.scale = inv_freq, axis, interleaved, scale
+        self.c = {n: RopeStruct(_ptr(inv_freq), _ptr(axis), 2 * inv_freq.shape[0], n, int(interleaved), scale) for n in (1, 2, 3)}
+
+
+def osc_kv_slots(cached, fresh, base, page_size: int, free_pages, table, row_off, kv_len, slots, positions, taken, stream=None):
+    """Pages, slots and positions of a step's new tokens from the requests' lengths (all int32; table [R, cols] is
+    updated in place, row_off [R + 1], kv_len [R], slots [T], positions [T] and taken [1] are written)."""
+    R, T = cached.shape[0], slots.shape[0]
+    for n, t, d in (("cached", cached, 1), ("fresh", fresh, 1), ("base", base, 1), ("free_pages", free_pages, 1), ("table", table, 2),
+                    ("row_off", row_off, 1), ("kv_len", kv_len, 1), ("slots", slots, 1), ("positions", positions, 1), ("taken", taken, 1)):
+        _want(n, t, torch.int32, d)
+    if (fresh.shape[0] != R or table.shape[0] != R or kv_len.shape[0] < R or row_off.shape[0] < R + 1 or positions.shape[0] < T or
+            taken.shape[0] < 1 or (base is not None and base.shape[0] != R)):
+        raise ValueError("osc_kv_slots: lengths do not belong together")
+    _check(_lib.osc_kv_slots(_ptr(cached), _ptr(fresh), _ptr(base), R, page_size, _ptr(free_pages), free_pages.shape[0], _ptr(table),
+                             table.shape[1], table.stride(0), T, _ptr(row_off), _ptr(kv_len), _ptr(slots), _ptr(positions),
+                             _ptr(taken), _stream(stream)))
+
+
+def osc_qk_norm_rope(QKV: torch.Tensor, n_q: int, cache: KvCache, Q: torch.Tensor, positions: torch.Tensor, rope: Rope, gamma_q=None,
+                     gamma_k=None, eps: float = 1e-6, slots=None, stream=None):
+    """Norm and rotation of the query and key heads of QKV [T, (n_q + 2 n_kv) head_dim]; queries to Q [T, n_q head_dim],
+    keys and values to their slots of the cache.  positions: int32 [T] or [axes, T]."""
+    T = QKV.shape[0]
+    _want("QKV", QKV, torch.bfloat16, 2)
+    _want("Q", Q, torch.bfloat16, 2)
+    _want("gamma_q", gamma_q, torch.bfloat16, 1)
+    _want("gamma_k", gamma_k, torch.bfloat16, 1)
+    _want("slots", slots, torch.int32, 1)
+    _want("positions", positions, torch.int32)
+    axes = positions.shape[0] if positions.dim() == 2 else 1
+    if not 1 <= axes <= 3 or positions.dim() not in (1, 2):
+        raise ValueError("positions: [T] or [axes, T] with at most three axes")
+    if (positions.shape[-1] < T or Q.shape[0] != T or (slots is not None and slots.shape[0] < T) or
+            QKV.shape[1] != (n_q + 2 * cache.n_heads) * cache.head_dim or Q.shape[1] < n_q * cache.head_dim or
+            any(g is not None and g.shape[0] != cache.head_dim for g in (gamma_q, gamma_k))):
+        raise ValueError("osc_qk_norm_rope: shapes do not belong together")
+    _check(_lib.osc_qk_norm_rope(_ptr(QKV), T, QKV.stride(0) if T > 1 else QKV.shape[1], n_q, cache.c, _ptr(gamma_q), _ptr(gamma_k),
+                                 float(eps), rope.c[axes], _ptr(positions), positions.stride(0) if axes > 1 else T, _ptr(slots),
+                                 _ptr(Q), Q.stride(0) if T > 1 else Q.shape[1], _stream(stream)))
+
+
+def osc_paged_attention_workspace_bytes(T: int, n_q: int, head_dim: int, R: int, P: int = 0) -> int:
+    out = _sz()
+    _check(_lib.osc_paged_attention_workspace_bytes(T, n_q, head_dim, R, P, C.byref(out)))
+    return int(out.value)
+
+
+def osc_paged_attention(Q: torch.Tensor, cache: KvCache, row_off, kv_len, table, O: torch.Tensor, workspace: torch.Tensor, scale: float,
+                        lse=None, group_off=None, prefix_len=None, prefix_table=None, max_new: int = 0, stream=None):
+    """Attention of the new tokens Q [T, n_q head_dim] over the cache; O [T, n_q head_dim], lse float32 [T, n_q] or None.
+    With group_off [P + 1], prefix_len [P] and prefix_table [P, cols], groups of requests share prefixes."""
+    T, R = Q.shape[0], kv_len.shape[0]
+    P = prefix_len.shape[0] if prefix_len is not None else 0
+    _want("Q", Q, torch.bfloat16, 2)
+    _want("O", O, torch.bfloat16, 2)
+    _want("lse", lse, torch.float32, 2)
+    for n, t, d in (("row_off", row_off, 1), ("kv_len", kv_len, 1), ("table", table, 2), ("group_off", group_off, 1),
+                    ("prefix_len", prefix_len, 1), ("prefix_table", prefix_table, 2)):
+        _want(n, t, torch.int32, d)
+    n_q = Q.shape[1] // cache.head_dim
+    if (Q.shape[1] % cache.head_dim or O.shape != Q.shape or row_off.shape[0] < R + 1 or table.shape[0] < R or
+            (P and (group_off is None or prefix_table is None or group_off.shape[0] < P + 1 or prefix_table.shape[0] < P)) or
+            (lse is not None and (lse.shape != (T, n_q) or not lse.is_contiguous()))):
+        raise ValueError("osc_paged_attention: shapes do not belong together")
+    _check(_lib.osc_paged_attention(_ptr(Q), T, Q.stride(0) if T > 1 else Q.shape[1], n_q, cache.c, R, _ptr(row_off), _ptr(kv_len), _ptr(table),
+                                    table.shape[1], table.stride(0), P, _ptr(group_off) if P else None, _ptr(prefix_len) if P else None,
+                                    _ptr(prefix_table) if P else None, prefix_table.shape[1] if P else 0,
+                                    prefix_table.stride(0) if P else 0, max_new, float(scale), _ptr(O),
+                                    O.stride(0) if T > 1 else O.shape[1], _ptr(lse), _ptr(workspace),
+                                    workspace.numel() * workspace.element_size(), _stream(stream)))

@@ -1,0 +1,182 @@
+// Host side of the calls around the paged key/value cache: validation, workspace layout, launches.
+#include <math.h>
+
+#include "../../include/osc.h"
+#include "common.cuh"
+
+namespace osc {
+
+static osc_status check_cache(const osc_kv_cache_t* c) {
+    if (!c) return fail(OSC_ERR_INVALID_ARG, "cache is null");
+    if (c->n_pages < 0 || c->page_size < 1 || c->n_heads < 1)
+        return fail(OSC_ERR_INVALID_ARG, "cache: n_pages = %d, page_size = %d, n_heads = %d", c->n_pages, c->page_size, c->n_heads);
+    if (c->head_dim != 64 && c->head_dim != 128) return fail(OSC_ERR_SHAPE, "cache: head_dim = %d, must be 64 or 128", c->head_dim);
+    if ((int64_t)c->n_pages * c->page_size > 0x7FFFFFFFll)
+        return fail(OSC_ERR_SHAPE, "cache: n_pages * page_size = %lld passes 2^31 - 1", (long long)c->n_pages * c->page_size);
+    if (c->n_pages > 0 && (!c->k || !c->v)) return fail(OSC_ERR_INVALID_ARG, "cache: null device pointer");
+    if ((c->n_pages > 1 && c->page_stride < c->head_dim) || (c->page_size > 1 && c->token_stride < c->head_dim) ||
+        (c->n_heads > 1 && c->head_stride < c->head_dim))
+        return fail(OSC_ERR_SHAPE, "cache: a stride is smaller than head_dim = %d", c->head_dim);
+    if (c->page_stride % 8 || c->token_stride % 8 || c->head_stride % 8 || !aligned16(c->k) || !aligned16(c->v))
+        return fail(OSC_ERR_ALIGN, "cache: k and v must be 16-byte aligned, strides multiples of 8");
+    return OSC_OK;
+}
+
+struct AttnLayout {
+    size_t few_start, wide_start, group, dense[2], dense_ml[2], few_part, few_ml, wide_part, wide_ml, total;
+};
+static AttnLayout attn_layout(int T, int n_q, int D, int R, int P) {
+    AttnLayout l;
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t o = at; at += align256(bytes); return o; };
+    const size_t S = (size_t)R + P + 1, rows = (size_t)T * n_q;
+    l.few_start = take(S * 8);
+    l.wide_start = take(S * 8);
+    l.group = take((size_t)R * 4);
+    for (int i = 0; i < 2; ++i) {   // rows with two sources exist only where there are prefixes
+        l.dense[i] = take(P ? rows * D * 4 : 0);
+        l.dense_ml[i] = take(P ? rows * 8 : 0);
+    }
+    l.few_part = take((size_t)AT_FEW_CTAS * 2 * AT_FEW_ROWS * D * 4);
+    l.few_ml = take((size_t)AT_FEW_CTAS * 2 * AT_FEW_ROWS * 8);
+    l.wide_part = take((size_t)AT_WIDE_CTAS * 4 * AT_WIDE_TILE * D * 4);
+    l.wide_ml = take((size_t)AT_WIDE_CTAS * 4 * AT_WIDE_TILE * 8);
+    l.total = at;
+    return l;
+}
+
+}  // namespace osc
+
+using namespace osc;
+
+extern "C" {
+
+osc_status osc_kv_slots(const int32_t* cached, const int32_t* fresh, const int32_t* base, int R, int page_size,
+                        const int32_t* free_pages, int n_free, int32_t* table, int cols, int64_t ld_table, int T,
+                        int32_t* row_off, int32_t* kv_len, int32_t* slots, int32_t* positions, int32_t* taken, void* stream) {
+    if (R < 0 || T < 0 || n_free < 0 || cols < 0) return fail(OSC_ERR_INVALID_ARG, "R = %d, T = %d, n_free = %d, cols = %d", R, T, n_free, cols);
+    if (page_size < 1) return fail(OSC_ERR_SHAPE, "page_size = %d", page_size);
+    if (!row_off || !taken || (T > 0 && (!slots || !positions)) || (n_free > 0 && !free_pages) ||
+        (R > 0 && (!cached || !fresh || !kv_len)) || (R > 0 && cols > 0 && !table))
+        return fail(OSC_ERR_INVALID_ARG, "null device pointer");
+    if (R > 1 && ld_table < cols) return fail(OSC_ERR_SHAPE, "ld_table = %lld < cols = %d", (long long)ld_table, cols);
+    DeviceInfo di;
+    if (osc_status s = device_info(&di)) return s;
+    KvSlotsArgs a = {};
+    a.cached = cached; a.fresh = fresh; a.base = base; a.free_pages = free_pages; a.table = table; a.ld_table = ld_table;
+    a.row_off = row_off; a.kv_len = kv_len; a.slots = slots; a.positions = positions; a.taken = taken;
+    a.R = R; a.page = page_size; a.n_free = n_free; a.cols = cols; a.T = T;
+    cudaError_t e = launch_kv_slots(a, di.num_sms, static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail(e, "kv_slots_kernel");
+    return OSC_OK;
+}
+
+osc_status osc_qk_norm_rope(const void* QKV, int T, int64_t ld, int n_q, const osc_kv_cache_t* cache, const void* gamma_q,
+                            const void* gamma_k, float eps, const osc_rope_t* rope, const int32_t* positions, int64_t ld_pos,
+                            const int32_t* slots, void* Q, int64_t ldq, void* stream) {
+    if (T < 0 || n_q < 1) return fail(OSC_ERR_INVALID_ARG, "T = %d, n_q = %d", T, n_q);
+    if (osc_status s = check_cache(cache)) return s;
+    if (!rope) return fail(OSC_ERR_INVALID_ARG, "rope is null");
+    const int D = cache->head_dim;
+    if (rope->rot_dim < 16 || rope->rot_dim % 16 || rope->rot_dim > D)
+        return fail(OSC_ERR_SHAPE, "rot_dim = %d must be a multiple of 16 within head_dim = %d", rope->rot_dim, D);
+    if (rope->axes < 1 || rope->axes > 3) return fail(OSC_ERR_INVALID_ARG, "axes = %d outside 1..3", rope->axes);
+    if ((int64_t)n_q + 2ll * cache->n_heads > 65536) return fail(OSC_ERR_SHAPE, "n_q = %d, n_heads = %d: too many heads", n_q, cache->n_heads);
+    if (T == 0) return OSC_OK;
+    if (!QKV || !Q || !positions || !rope->inv_freq) return fail(OSC_ERR_INVALID_ARG, "null device pointer");
+    const int64_t width = ((int64_t)n_q + 2 * cache->n_heads) * D;
+    if (ld < width || ldq < (int64_t)n_q * D || (rope->axes > 1 && ld_pos < T))
+        return fail(OSC_ERR_SHAPE, "ld = %lld < %lld, ldq = %lld < %lld or ld_pos = %lld < T", (long long)ld, (long long)width, (long long)ldq,
+                    (long long)n_q * D, (long long)ld_pos);
+    if (ld % 8 || ldq % 8 || !aligned16(QKV) || !aligned16(Q))
+        return fail(OSC_ERR_ALIGN, "QKV and Q must be 16-byte aligned, ld and ldq multiples of 8");
+    DeviceInfo di;
+    if (osc_status s = device_info(&di)) return s;
+    QkNormRopeArgs a = {};
+    a.qkv = static_cast<const uint16_t*>(QKV); a.ld = ld;
+    a.gamma_q = static_cast<const uint16_t*>(gamma_q); a.gamma_k = static_cast<const uint16_t*>(gamma_k);
+    a.inv_freq = rope->inv_freq; a.axis = rope->axis; a.positions = positions; a.ld_pos = ld_pos;
+    a.q = static_cast<uint16_t*>(Q); a.ldq = ldq;
+    a.k = static_cast<uint16_t*>(cache->k); a.v = static_cast<uint16_t*>(cache->v);
+    a.page_stride = cache->page_stride; a.token_stride = cache->token_stride; a.head_stride = cache->head_stride;
+    a.slots = slots; a.eps = eps; a.scale = rope->scale;
+    a.T = T; a.Hq = n_q; a.Hk = cache->n_heads; a.rot = rope->rot_dim; a.axes = rope->axes; a.page = cache->page_size; a.n_pages = cache->n_pages;
+    cudaError_t e = launch_qk_norm_rope(a, D, rope->interleaved != 0, di.num_sms, static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail(e, "qk_norm_rope_kernel");
+    return OSC_OK;
+}
+
+static osc_status check_attention_sizes(int T, int n_q, int D, int R, int P) {
+    if (T < 0 || n_q < 1 || R < 0 || P < 0) return fail(OSC_ERR_INVALID_ARG, "T = %d, n_q = %d, R = %d, P = %d", T, n_q, R, P);
+    if (D != 64 && D != 128) return fail(OSC_ERR_SHAPE, "head_dim = %d, must be 64 or 128", D);
+    if (n_q > 65536 || (int64_t)R + P > 0x3FFFFFFF) return fail(OSC_ERR_SHAPE, "n_q = %d, R = %d, P = %d: too many", n_q, R, P);
+    return OSC_OK;
+}
+
+osc_status osc_paged_attention_workspace_bytes(int T, int n_q, int head_dim, int R, int P, size_t* bytes) {
+    if (!bytes) return fail(OSC_ERR_INVALID_ARG, "bytes is null");
+    if (osc_status s = check_attention_sizes(T, n_q, head_dim, R, P)) return s;
+    *bytes = attn_layout(T, n_q, head_dim, R, P).total;
+    return OSC_OK;
+}
+
+osc_status osc_paged_attention(const void* Q, int T, int64_t ldq, int n_q, const osc_kv_cache_t* cache, int R,
+                               const int32_t* row_off, const int32_t* kv_len, const int32_t* table, int cols, int64_t ld_table,
+                               int P, const int32_t* group_off, const int32_t* prefix_len, const int32_t* prefix_table,
+                               int prefix_cols, int64_t ld_prefix, int max_new, float scale, void* O, int64_t ldo, float* lse,
+                               void* workspace, size_t workspace_bytes, void* stream) {
+    if (osc_status s = check_cache(cache)) return s;
+    const int D = cache->head_dim;
+    if (osc_status s = check_attention_sizes(T, n_q, D, R, P)) return s;
+    if (n_q % cache->n_heads || n_q / cache->n_heads > 128)
+        return fail(OSC_ERR_SHAPE, "n_q = %d must be a multiple of n_heads = %d, at most 128 times it", n_q, cache->n_heads);
+    if (cache->page_size < 16 || (cache->page_size & (cache->page_size - 1)))
+        return fail(OSC_ERR_SHAPE, "page_size = %d must be a power of two of at least 16", cache->page_size);
+    if (cols < 0 || (P > 0 && prefix_cols < 0) || max_new < 0)
+        return fail(OSC_ERR_INVALID_ARG, "cols = %d, prefix_cols = %d, max_new = %d", cols, prefix_cols, max_new);
+    if (!(scale > 0.0f) || !(scale < INFINITY)) return fail(OSC_ERR_INVALID_ARG, "scale = %g must be positive and finite", (double)scale);
+    if (T == 0 || R == 0) return OSC_OK;
+    if (!Q || !O || !row_off || !kv_len || (cols > 0 && !table) || !workspace) return fail(OSC_ERR_INVALID_ARG, "null device pointer");
+    if (P > 0 && (!group_off || !prefix_len || (prefix_cols > 0 && !prefix_table)))
+        return fail(OSC_ERR_INVALID_ARG, "null device pointer of a shared prefix");
+    if ((R > 1 && ld_table < cols) || (P > 1 && ld_prefix < prefix_cols))
+        return fail(OSC_ERR_SHAPE, "ld_table = %lld < cols = %d or ld_prefix = %lld < prefix_cols = %d", (long long)ld_table, cols,
+                    (long long)ld_prefix, prefix_cols);
+    if (ldq < (int64_t)n_q * D || ldo < (int64_t)n_q * D)
+        return fail(OSC_ERR_SHAPE, "ldq = %lld, ldo = %lld < n_q * head_dim = %lld", (long long)ldq, (long long)ldo, (long long)n_q * D);
+    if (ldq % 8 || ldo % 8 || !aligned16(Q) || !aligned16(O) || !aligned16(workspace))
+        return fail(OSC_ERR_ALIGN, "Q, O and workspace must be 16-byte aligned, ldq and ldo multiples of 8");
+    const AttnLayout l = attn_layout(T, n_q, D, R, P);
+    if (workspace_bytes < l.total) return fail(OSC_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, l.total);
+    DeviceInfo di;
+    if (osc_status s = device_info(&di)) return s;
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    AttnArgs a = {};
+    a.q = static_cast<const uint16_t*>(Q); a.ldq = ldq; a.o = static_cast<uint16_t*>(O); a.ldo = ldo; a.lse = lse;
+    a.k = static_cast<const uint16_t*>(cache->k); a.v = static_cast<const uint16_t*>(cache->v);
+    a.page_stride = cache->page_stride; a.token_stride = cache->token_stride; a.head_stride = cache->head_stride;
+    a.row_off = row_off; a.kv_len = kv_len; a.table = table; a.ld_table = ld_table; a.cols = cols;
+    a.group_off = group_off; a.prefix_len = prefix_len; a.ptable = prefix_table; a.ld_ptable = ld_prefix; a.pcols = P ? prefix_cols : 0;
+    a.T = T; a.Hq = n_q; a.Hk = cache->n_heads; a.G = n_q / cache->n_heads; a.R = R; a.P = P; a.n_pages = cache->n_pages;
+    while ((1 << a.page_shift) < cache->page_size) ++a.page_shift;
+    a.scale_log2 = scale * 1.44269504088896341f;
+    a.few_ctas = di.num_sms * 2 < AT_FEW_CTAS ? di.num_sms * 2 : AT_FEW_CTAS;
+    a.wide_ctas = di.num_sms < AT_WIDE_CTAS ? di.num_sms : AT_WIDE_CTAS;
+    a.wide_min_rows = 0x7FFFFFFF;
+    a.plan.few_start = reinterpret_cast<int64_t*>(ws + l.few_start);
+    a.plan.wide_start = reinterpret_cast<int64_t*>(ws + l.wide_start);
+    a.plan.req_group = reinterpret_cast<int32_t*>(ws + l.group);
+    for (int i = 0; i < 2; ++i) {
+        a.dense[i] = reinterpret_cast<float*>(ws + l.dense[i]);
+        a.dense_ml[i] = reinterpret_cast<float2*>(ws + l.dense_ml[i]);
+    }
+    a.few_part = reinterpret_cast<float*>(ws + l.few_part);
+    a.few_ml = reinterpret_cast<float2*>(ws + l.few_ml);
+    a.wide_part = reinterpret_cast<float*>(ws + l.wide_part);
+    a.wide_ml = reinterpret_cast<float2*>(ws + l.wide_ml);
+    cudaError_t e = launch_attn(a, D, static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail(e, "attention kernels");
+    return OSC_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,357 @@
+// Kernels around a paged key/value cache, between the QKV projection and the attention:
+//   kv_slots_kernel     pages for the new tokens of every request, slots and positions of the tokens
+//   qk_norm_rope_kernel RMSNorm of the query and key heads, rotation by position, keys and values into the cache
+#include "common.cuh"
+
+namespace osc {
+
+// ---------------------------------------------------------------------------------------------- kv_slots
+// Request r holds `cached` tokens and gets `fresh` new ones.  With have = ceil(cached / p) and
+// want = ceil((cached + fresh) / p) pages, it takes want - have pages from the free list, in request order:
+//   first_r      = sum over r' < r of (want - have)
+//   table[r][have + j] = free[first_r + j]
+//   row_off      = exclusive sum of fresh
+//   token i of r : at = cached + i, slot = table[r][at / p] * p + at % p, position = base + at
+// Both sums run over the requests only, so every CTA does them for itself (32-bit halves of one 64-bit value, two
+// shuffle scans) instead of a second launch; tokens and pages are then shared out over the grid, each finding its
+// request by binary search in shared memory.  A page that this call hands out is read from the free list, not
+// from the table, so nothing written by another CTA is read.  What bounds it is latency: lengths -> scan ->
+// search -> page -> store, one after the other.
+constexpr int KS_THREADS = 512;
+
+struct KvSlotsArgs {
+    const int32_t* cached;
+    const int32_t* fresh;
+    const int32_t* base;    // may be null: 0
+    const int32_t* free_pages;
+    int32_t* table;
+    int64_t ld_table;
+    int32_t* row_off;
+    int32_t* kv_len;
+    int32_t* slots;
+    int32_t* positions;
+    int32_t* taken;
+    int R, page, n_free, cols, T;
+};
+
+// largest i in [0, n) with start[i] <= x (start ascending, start[0] <= x)
+__device__ __forceinline__ int search_last(const int* start, int n, int x) {
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (start[mid] <= x) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+__global__ void __launch_bounds__(KS_THREADS) kv_slots_kernel(const KvSlotsArgs a) {
+    __shared__ int s_row[KS_THREADS + 1], s_first[KS_THREADS + 1], s_cached[KS_THREADS], s_base[KS_THREADS];
+    __shared__ unsigned long long s_warp[KS_THREADS / 32];
+    grid_launch_dependents();
+    grid_dependency_wait();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    unsigned long long carry = 0;   // tokens in the low half, pages in the high half, of the requests before the chunk
+    for (int r0 = 0; r0 < a.R; r0 += KS_THREADS) {
+        const int nr = min(KS_THREADS, a.R - r0);
+        int cached = 0, fresh = 0, need = 0;
+        if (tid < nr) {
+            cached = max(a.cached[r0 + tid], 0);
+            fresh = max(a.fresh[r0 + tid], 0);
+            need = (int)(((long long)cached + fresh + a.page - 1) / a.page - ((long long)cached + a.page - 1) / a.page);
+            s_cached[tid] = cached;
+            s_base[tid] = a.base ? a.base[r0 + tid] : 0;
+        }
+        const unsigned long long own = (unsigned long long)(unsigned)fresh | (unsigned long long)(unsigned)need << 32;
+        unsigned long long inc = own;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const unsigned long long up = __shfl_up_sync(0xFFFFFFFFu, inc, o);
+            if (lane >= o) inc += up;
+        }
+        if (lane == 31) s_warp[warp] = inc;
+        __syncthreads();
+        unsigned long long before = carry, total = carry;
+        for (int w = 0; w < KS_THREADS / 32; ++w) {
+            if (w < warp) before += s_warp[w];
+            total += s_warp[w];
+        }
+        const unsigned long long exc = before + inc - own;
+        s_row[tid] = (int)(unsigned)exc;
+        s_first[tid] = (int)(exc >> 32);
+        if (tid == 0) {
+            s_row[KS_THREADS] = (int)(unsigned)total;
+            s_first[KS_THREADS] = (int)(total >> 32);
+        }
+        if (blockIdx.x == 0 && tid < nr) {
+            a.row_off[r0 + tid] = (int)(unsigned)exc;
+            a.kv_len[r0 + tid] = (int)min((long long)cached + fresh, 0x7FFFFFFFll);
+        }
+        __syncthreads();
+        // the chunk's tokens
+        const int t_end = min((int)(unsigned)total, a.T);
+        for (int t = (int)(unsigned)carry + blockIdx.x * KS_THREADS + tid; t >= 0 && t < t_end; t += gridDim.x * KS_THREADS) {
+            const int i = search_last(s_row, nr, t);
+            const int at = s_cached[i] + (t - s_row[i]);
+            const int col = at / a.page, have = (s_cached[i] + a.page - 1) / a.page;
+            int page = -1;
+            if (at >= 0 && col < a.cols) {
+                const int f = s_first[i] + (col - have);
+                if (col < have) page = a.table[(int64_t)(r0 + i) * a.ld_table + col];
+                else if (f >= 0 && f < a.n_free) page = a.free_pages[f];
+            }
+            const long long slot = (long long)page * a.page + (at - col * a.page);
+            a.slots[t] = (page >= 0 && slot <= 0x7FFFFFFFll) ? (int)slot : -1;
+            a.positions[t] = s_base[i] + at;
+        }
+        // the chunk's new pages
+        const int p_begin = (int)(carry >> 32), p_end = (int)(total >> 32);
+        for (int f = p_begin + blockIdx.x * KS_THREADS + tid; f >= 0 && f < p_end; f += gridDim.x * KS_THREADS) {
+            const int i = search_last(s_first, nr, f);
+            const int col = (s_cached[i] + a.page - 1) / a.page + (f - s_first[i]);
+            if (col >= 0 && col < a.cols) a.table[(int64_t)(r0 + i) * a.ld_table + col] = f < a.n_free ? a.free_pages[f] : -1;
+        }
+        carry = total;
+        __syncthreads();   // the shared arrays are filled again for the next chunk
+    }
+    // rows that only fill the step up have no slot: whatever writes the cache leaves them out
+    for (int t = max((int)(unsigned)carry, 0) + blockIdx.x * KS_THREADS + tid; t < a.T; t += gridDim.x * KS_THREADS) {
+        a.slots[t] = -1;
+        a.positions[t] = 0;
+    }
+    if (blockIdx.x == 0 && tid == 0) {
+        a.row_off[a.R] = (int)(unsigned)carry;
+        a.taken[0] = (int)(carry >> 32);
+    }
+}
+
+cudaError_t launch_kv_slots(const KvSlotsArgs& a, int num_sms, cudaStream_t st) {
+    const int grid = max(1, min(num_sms, (a.T + KS_THREADS - 1) / KS_THREADS));
+    return launch_pdl(kv_slots_kernel, dim3(grid), dim3(KS_THREADS), 0, st, a);
+}
+
+// ------------------------------------------------------------------------------------------ qk_norm_rope
+// Per token t and head h of the queries and keys, with one rounding to bf16 at the end:
+//   y     = x * rsqrt(mean(x^2) + eps) * gamma                       (fp32; left out where gamma is null)
+//   a_i   = position[axis_i][t] * inv_freq_i                         (exact in double)
+//   (y_i, y_i') -> scale * (y_i cos a_i - y_i' sin a_i, y_i' cos a_i + y_i sin a_i)
+// with i' = i + rot/2 (halves) or the pair (2i, 2i+1) (interleaved); channels from rot on are not turned.  Values
+// are copied.  Queries go to Q, keys and values to the token's slot of the cache.
+//
+// Every byte is read and written once, so HBM bounds it from a few hundred tokens on, and instruction issue is not
+// far behind.  A head is D/8 lanes of eight channels, a warp takes 32/(D/8) heads at a time and walks over the heads of ONE token,
+// so that the token's cosines and sines are worked out once (two angles per lane, then through shared memory
+// into registers) and serve all heads.  For rot == D in halves a lane holds four channels of each half, so that both
+// members of a pair are in one lane and the rotation needs no shuffle.  With few tokens a token's heads are
+// shared out over several warps instead.
+// The angle is reduced in double (position * frequency passes 2^24 for far positions, where fp32 would lose the
+// turn entirely) to half turns in [-1, 1], whose sine and cosine are taken in fp32: an error of 2^-23 against a
+// rounding step of 2^-8.
+constexpr int QR_WARPS = 8;
+constexpr int QR_UNROLL = 4;    // steps whose loads are issued before the first is worked on
+
+struct QkNormRopeArgs {
+    const uint16_t* qkv;
+    int64_t ld;
+    const uint16_t* gamma_q;   // null: no norm
+    const uint16_t* gamma_k;
+    const float* inv_freq;
+    const uint8_t* axis;       // null: axis 0 for every pair
+    const int32_t* positions;
+    int64_t ld_pos;
+    uint16_t* q;
+    int64_t ldq;
+    uint16_t* k;
+    uint16_t* v;
+    int64_t page_stride, token_stride, head_stride;
+    const int32_t* slots;      // null: token t at slot t
+    float eps, scale;
+    int T, Hq, Hk, rot, axes, page, n_pages;
+    int warps_per_token;
+};
+
+constexpr int ROPE_SPLIT = 0;        // halves, rot == D: a lane holds four channels of each half
+constexpr int ROPE_INTERLEAVED = 1;  // pairs (2i, 2i+1)
+constexpr int ROPE_PARTIAL = 2;      // halves, rot < D: the partner channel comes by shuffle
+
+template <int D, int MODE>
+__global__ void __launch_bounds__(QR_WARPS * 32) qk_norm_rope_kernel(const QkNormRopeArgs a) {
+    constexpr int LPH = D / 8;       // lanes per head
+    constexpr int HPS = 32 / LPH;    // heads per step of a warp
+    __shared__ float2 s_cs[QR_WARPS][D / 2];
+    __shared__ float s_gamma[2][D];
+    grid_launch_dependents();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int sub = lane / LPH, hl = lane % LPH;
+    grid_dependency_wait();
+    for (int i = threadIdx.x; i < 2 * D; i += QR_WARPS * 32) {
+        const uint16_t* g = i < D ? a.gamma_q : a.gamma_k;
+        s_gamma[i / D][i % D] = g ? __uint_as_float((uint32_t)g[i % D] << 16) : 1.0f;
+    }
+    __syncthreads();
+    const int64_t job = (int64_t)blockIdx.x * QR_WARPS + warp;
+    const int64_t t64 = job / a.warps_per_token;
+    if (t64 >= a.T) return;
+    const int t = (int)t64, part = (int)(job % a.warps_per_token);
+
+    // cosines and sines of the token
+    for (int i = lane; i < a.rot / 2; i += 32) {
+        int ax = a.axis ? a.axis[i] : 0;
+        ax = min(ax, a.axes - 1);
+        const double ang = (double)a.positions[(int64_t)ax * a.ld_pos + t] * (double)a.inv_freq[i];
+        double u = ang * 0.31830988618379067154;      // half turns
+        u -= 2.0 * rint(u * 0.5);
+        float s, c;
+        sincospif((float)u, &s, &c);
+        s_cs[warp][i] = make_float2(c * a.scale, s * a.scale);
+    }
+    __syncwarp();
+    // first channel of the lane's two groups of four, and the pair index of its channels
+    const int e0 = MODE == ROPE_SPLIT ? 4 * hl : 8 * hl;
+    const int e1 = MODE == ROPE_SPLIT ? D / 2 + 4 * hl : 8 * hl + 4;
+    float c[8], s[8];
+    bool turned = true;
+    if (MODE == ROPE_SPLIT || MODE == ROPE_INTERLEAVED) {
+        turned = MODE == ROPE_SPLIT || e0 < a.rot;    // rot is a multiple of 16: a lane's eight channels turn together
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int i = 4 * hl + j;                 // both layouts: pairs 4 hl .. 4 hl + 3
+            const float2 v = turned ? s_cs[warp][i] : make_float2(1.0f, 0.0f);
+            c[j] = v.x;
+            s[j] = v.y;
+        }
+    } else {
+        turned = e0 < a.rot;
+        const bool upper = e0 >= a.rot / 2;           // rot / 2 is a multiple of 8
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int i = upper ? e0 + j - a.rot / 2 : e0 + j;
+            const float2 v = turned ? s_cs[warp][i] : make_float2(1.0f, 0.0f);
+            c[j] = v.x;
+            s[j] = upper ? v.y : -v.y;                // y = x cos + (partner) (-sin, +sin)
+        }
+    }
+    const int half_lanes = a.rot / 16;
+    const int partner = !turned ? lane : (e0 < a.rot / 2 ? lane + half_lanes : lane - half_lanes);
+
+    const int slot = a.slots ? a.slots[t] : t;
+    const int page = slot >= 0 ? slot / a.page : -1;
+    const bool cached = slot >= 0 && page < a.n_pages;
+    const int64_t cache_row = cached ? (int64_t)page * a.page_stride + (int64_t)(slot - page * a.page) * a.token_stride : 0;
+
+    const int nq = (a.Hq + HPS - 1) / HPS, nk = (a.Hk + HPS - 1) / HPS;
+    const int steps = nq + 2 * nk;
+    const int st0 = (int)((int64_t)steps * part / a.warps_per_token), st1 = (int)((int64_t)steps * (part + 1) / a.warps_per_token);
+    const uint16_t* row = a.qkv + (int64_t)t * a.ld;
+    for (int b = st0; b < st1; b += QR_UNROLL) {
+        uint2 raw[QR_UNROLL][2];
+#pragma unroll
+        for (int j = 0; j < QR_UNROLL; ++j) {
+            const int i = b + j;
+            const int kind = i < nq ? 0 : i < nq + nk ? 1 : 2;
+            const int h = (i - (kind == 0 ? 0 : kind == 1 ? nq : nq + nk)) * HPS + sub;
+            const int hs = kind == 0 ? h : a.Hq + (kind - 1) * a.Hk + h;
+            raw[j][0] = raw[j][1] = make_uint2(0u, 0u);
+            if (i < st1 && h < (kind == 0 ? a.Hq : a.Hk)) {
+                const uint16_t* x = row + (int64_t)hs * D;
+                if (MODE == ROPE_SPLIT) {
+                    raw[j][0] = *reinterpret_cast<const uint2*>(x + e0);
+                    raw[j][1] = *reinterpret_cast<const uint2*>(x + e1);
+                } else {
+                    const uint4 v = *reinterpret_cast<const uint4*>(x + e0);
+                    raw[j][0] = make_uint2(v.x, v.y);
+                    raw[j][1] = make_uint2(v.z, v.w);
+                }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < QR_UNROLL; ++j) {
+            const int i = b + j;
+            if (i >= st1) break;
+            const int kind = i < nq ? 0 : i < nq + nk ? 1 : 2;
+            const int h = (i - (kind == 0 ? 0 : kind == 1 ? nq : nq + nk)) * HPS + sub;
+            uint32_t w[4] = {raw[j][0].x, raw[j][0].y, raw[j][1].x, raw[j][1].y};
+            if (kind < 2) {
+                float x[8];
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                    x[2 * m] = __uint_as_float(w[m] << 16);
+                    x[2 * m + 1] = __uint_as_float(w[m] & 0xFFFF0000u);
+                }
+                if ((kind == 0 ? a.gamma_q : a.gamma_k) != nullptr) {
+                    float ss = 0.0f, ss2 = 0.0f;
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) {
+                        ss = fmaf(x[m], x[m], ss);
+                        ss2 = fmaf(x[m + 4], x[m + 4], ss2);
+                    }
+                    ss += ss2;
+#pragma unroll
+                    for (int o = LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xFFFFFFFFu, ss, o);
+                    const float r = rsqrtf(ss * (1.0f / D) + a.eps);
+                    const float4 g0 = *reinterpret_cast<const float4*>(&s_gamma[kind][e0]);
+                    const float4 g1 = *reinterpret_cast<const float4*>(&s_gamma[kind][e1]);
+                    x[0] *= r * g0.x; x[1] *= r * g0.y; x[2] *= r * g0.z; x[3] *= r * g0.w;
+                    x[4] *= r * g1.x; x[5] *= r * g1.y; x[6] *= r * g1.z; x[7] *= r * g1.w;
+                }
+                float y[8];
+                if (MODE == ROPE_SPLIT) {
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) {
+                        y[m] = x[m] * c[m] - x[m + 4] * s[m];
+                        y[m + 4] = x[m + 4] * c[m] + x[m] * s[m];
+                    }
+                } else if (MODE == ROPE_INTERLEAVED) {
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) {
+                        y[2 * m] = x[2 * m] * c[m] - x[2 * m + 1] * s[m];
+                        y[2 * m + 1] = x[2 * m + 1] * c[m] + x[2 * m] * s[m];
+                    }
+                } else {
+#pragma unroll
+                    for (int m = 0; m < 8; ++m) {
+                        const float o = __shfl_sync(0xFFFFFFFFu, x[m], partner);
+                        y[m] = turned ? x[m] * c[m] + o * s[m] : x[m];
+                    }
+                }
+#pragma unroll
+                for (int m = 0; m < 4; ++m) w[m] = bf162_bits(__floats2bfloat162_rn(y[2 * m], y[2 * m + 1]));
+            }
+            uint16_t* dst = nullptr;
+            if (kind == 0) {
+                if (h < a.Hq) dst = a.q + (int64_t)t * a.ldq + (int64_t)h * D;
+            } else if (cached && h < a.Hk) {
+                dst = (kind == 1 ? a.k : a.v) + cache_row + (int64_t)h * a.head_stride;
+            }
+            if (dst) {
+                if (MODE == ROPE_SPLIT) {
+                    *reinterpret_cast<uint2*>(dst + e0) = make_uint2(w[0], w[1]);
+                    *reinterpret_cast<uint2*>(dst + e1) = make_uint2(w[2], w[3]);
+                } else {
+                    *reinterpret_cast<uint4*>(dst + e0) = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+            }
+        }
+    }
+}
+
+template <int D>
+static cudaError_t launch_qk_norm_rope_d(const QkNormRopeArgs& a, int mode, dim3 grid, cudaStream_t st) {
+    const dim3 block(QR_WARPS * 32);
+    if (mode == ROPE_SPLIT) return launch_pdl(qk_norm_rope_kernel<D, ROPE_SPLIT>, grid, block, 0, st, a);
+    if (mode == ROPE_INTERLEAVED) return launch_pdl(qk_norm_rope_kernel<D, ROPE_INTERLEAVED>, grid, block, 0, st, a);
+    return launch_pdl(qk_norm_rope_kernel<D, ROPE_PARTIAL>, grid, block, 0, st, a);
+}
+
+cudaError_t launch_qk_norm_rope(QkNormRopeArgs a, int D, bool interleaved, int num_sms, cudaStream_t st) {
+    const int hps = 32 / (D / 8);
+    const int steps = (a.Hq + hps - 1) / hps + 2 * ((a.Hk + hps - 1) / hps);
+    // one warp per token once that gives every SM its 32 warps; below it, a token's steps are spread over more warps
+    int wpt = (int)(((int64_t)num_sms * 32 + a.T - 1) / a.T);
+    a.warps_per_token = max(1, min(wpt, steps));
+    const int64_t jobs = (int64_t)a.T * a.warps_per_token;
+    const dim3 grid((unsigned)((jobs + QR_WARPS - 1) / QR_WARPS));
+    const int mode = interleaved ? ROPE_INTERLEAVED : a.rot == D ? ROPE_SPLIT : ROPE_PARTIAL;
+    return D == 128 ? launch_qk_norm_rope_d<128>(a, mode, grid, st) : launch_qk_norm_rope_d<64>(a, mode, grid, st);
+}
+
+}  // namespace osc

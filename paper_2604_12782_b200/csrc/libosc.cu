@@ -6,5 +6,8 @@
 #include "gemm2_kernels.cu"
 #include "gemm3_kernels.cu"
 #include "profile_kernels.cu"
+#include "kv_kernels.cu"
+#include "attn_kernels.cu"
 #include "api.cu"
 #include "static_scratch.cu"
+#include "attn_api.cu"

@@ -1,0 +1,212 @@
+"""Attention over the paged cache, with and without shared prefixes, against the 64-bit definition.  What no row may use
+holds NaN (see AttnCase), so a key too many shows."""
+import numpy as np
+import pytest
+import torch
+
+from serving_inputs import AttnCase
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def B():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    from paper_2604_12782_b200 import binding
+    return binding
+
+
+def go(B, what="", max_new=0, pad=0, **kw):
+    c = AttnCase(**kw)
+    o, lse = c.run(B, max_new=max_new, pad=pad)
+    B.osc_sync_check()
+    c.check(o, lse, what or str({k: v for k, v in kw.items()})[:200])
+    if pad:
+        assert (c.obig[:, c.Hk * c.G * c.D:].float() == 7.0).all()
+    return c
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("kv", [1, 2, 15, 16, 17, 63, 64, 65, 127, 128, 129, 200, 1000])
+def test_one_token(B, D, kv):
+    go(B, seed=kv, Hk=2, G=4, D=D, page=16, new=[1], kv=[kv], max_new=1)
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
+@pytest.mark.parametrize("layout", ["nhd", "hnd", "pair"])
+def test_pages_and_layouts(B, page, layout):
+    go(B, seed=page, Hk=2, G=2, D=128, page=page, new=[1, 1, 1], kv=[300, 5, 77], layout=layout, pad=16)
+    go(B, seed=page + 1, Hk=3, G=1, D=64, page=page, new=[2, 40, 1], kv=[300, 41, 77], prefix=[page + 9], layout=layout)
+    go(B, seed=page + 2, Hk=2, G=8, D=128, page=page, new=[30, 1], kv=[300, 77], prefix=[3 * page], layout=layout, pad=8)
+
+
+@pytest.mark.parametrize("G", [1, 2, 3, 4, 5, 7, 8, 12, 16, 20, 33, 64, 100, 128])
+def test_group_sizes(B, G):
+    go(B, seed=G, Hk=1 if G > 16 else 2, G=G, D=128 if G % 2 else 64, page=16, new=[1, 3, 1], kv=[40, 130, 9], prefix=[70])
+
+
+@pytest.mark.parametrize("max_new", [0, 1, 50])
+def test_ragged_steps(B, max_new):
+    """The hint is a choice of kernel, the result holds whatever it says."""
+    go(B, seed=1, Hk=2, G=4, D=128, page=32, new=[1, 0, 50, 1, 7, 0, 33, 1], kv=[5, 80, 50, 400, 20, 0, 200, 1], max_new=max_new, tail_rows=3)
+
+
+def test_long_prompts(B):
+    go(B, seed=2, Hk=1, G=4, D=128, page=64, new=[300, 129], kv=[300, 500])
+    go(B, seed=3, Hk=1, G=1, D=64, page=16, new=[520], kv=[1111])
+    go(B, seed=4, Hk=2, G=6, D=128, page=16, new=[65, 64, 63], kv=[65, 200, 63], prefix=[257, 128], groups=[0, 2, 3])
+
+
+def test_rows_without_keys(B):
+    # no own keys and no prefix; fewer own keys than new tokens; an empty prefix; requests outside every group
+    go(B, seed=5, Hk=2, G=4, D=128, page=16, new=[1, 1, 3, 1], kv=[0, 4, 1, 0], tail_rows=2)
+    go(B, seed=6, Hk=2, G=4, D=64, page=16, new=[1, 1, 40, 2], kv=[0, 4, 9, 1], prefix=[0, 33], groups=[0, 2, 3])
+    go(B, seed=7, Hk=1, G=8, D=128, page=16, new=[0, 0], kv=[0, 0], tail_rows=4)
+    go(B, seed=8, Hk=1, G=8, D=128, page=16, new=[200], kv=[3])
+    go(B, seed=9, Hk=1, G=8, D=128, page=16, new=[1, 1, 1], kv=[0, 0, 0], prefix=[100], groups=[0, 2])
+
+
+@pytest.mark.parametrize("R,prefix", [(1, 1), (1, 300), (4, 128), (9, 700), (33, 129), (70, 1000)])
+def test_shared_prefix(B, R, prefix):
+    rng = np.random.default_rng(R)
+    go(B, seed=R, Hk=2, G=4, D=128, page=16, new=[1] * R, kv=list(rng.integers(0, 90, R)), prefix=[prefix], max_new=1)
+
+
+def test_groups(B):
+    go(B, seed=10, Hk=2, G=8, D=64, page=16, new=[1] * 12, kv=[3, 0, 40, 7, 100, 1, 1, 64, 65, 2, 0, 9], prefix=[64, 0, 300, 17],
+       groups=[1, 4, 4, 9, 10])
+    go(B, seed=11, Hk=1, G=2, D=128, page=32, new=[5, 1, 0, 30, 2, 2], kv=[5, 10, 12, 31, 64, 3], prefix=[90, 200, 5], groups=[0, 2, 3, 6],
+       tail_rows=1)
+
+
+def test_large_scores_and_one_peak(B):
+    """Scores of +-100 and more: the running maximum moves, weights underflow."""
+    go(B, seed=12, Hk=2, G=4, D=128, page=16, new=[1, 20], kv=[700, 300], prefix=[200], q_mul=20.0)
+    c = AttnCase(13, 1, 4, 128, 16, [1], [600], q_mul=1.0)
+    c.k[:] = torch.nan_to_num(c.k, nan=0.0)
+    o, lse = c.run(B)
+    c.check(o, lse, "finite garbage behind the end")
+
+
+def test_absent_pages_read_as_zero(B):
+    """A table entry outside the cache stands for keys and values of 0; nothing outside the cache is touched."""
+    for new in (1, 40):
+        c = AttnCase(14, 2, 4, 128, 16, [new], [100], prefix=[64])
+        c.table[0, 2] = -1
+        c.table[0, 4] = 2 ** 30
+        c.ptable[0, 1] = c.k.shape[0]
+        K, V = c.own[0]
+        for lo in (32, 64):
+            K[lo:lo + 16] = 0
+            V[lo:lo + 16] = 0
+        c.pre[0][0][16:32] = 0
+        c.pre[0][1][16:32] = 0
+        o, lse = c.run(B)
+        B.osc_sync_check()
+        c.check(o, lse, f"absent pages, {new} tokens")
+
+
+def test_lengths_past_the_table_are_cut(B):
+    c = AttnCase(15, 1, 4, 64, 16, [1], [48], prefix=[32])
+    o1, l1 = c.run(B)
+    c.kv_len.fill_(100000)
+    c.prefix_len.fill_(2 ** 31 - 1)
+    c.table, c.ptable = c.table[:, :3].contiguous(), c.ptable[:, :2].contiguous()
+    o2, l2 = c.run(B)
+    B.osc_sync_check()
+    assert torch.equal(o1, o2) and torch.equal(l1, l2)
+
+
+def test_unusual_offsets_stay_in_bounds(B):
+    """Row offsets that fall, pass T or are negative, and groups past R: nothing outside the buffers, no fault."""
+    c = AttnCase(16, 2, 4, 128, 16, [2, 2, 30], [20, 20, 40], prefix=[50])
+    for rows, groups in (([0, 10, 4, 1000], [0, 3]), ([-5, 2, 2, 34], [-2, 9]), ([40, 30, 20, 10], [2, 1]), ([0, 2, 4, 34], [3, 3])):
+        c.row_off.copy_(torch.tensor(rows, dtype=torch.int32))
+        c.group_off.copy_(torch.tensor(groups, dtype=torch.int32))
+        c.run(B)
+        B.osc_sync_check()
+
+
+def test_same_bits_every_time_and_without_lse(B):
+    c = AttnCase(17, 2, 4, 128, 16, [1] * 20 + [70], [300 + 17 * i for i in range(20)] + [400], prefix=[900])
+    o1, l1 = c.run(B)
+    for _ in range(5):
+        o2, l2 = c.run(B)
+        assert torch.equal(o1, o2) and torch.equal(l1, l2)
+    o3, _ = c.run(B, with_lse=False)
+    assert torch.equal(o1, o3)
+
+
+def test_streams_and_captured_step(B):
+    """A captured step replayed with other lengths, two graphs on one workspace one after the other, and a side stream."""
+    c = AttnCase(18, 2, 4, 128, 16, [1] * 6, [200, 5, 90, 64, 0, 33], prefix=[150], groups=[0, 6])
+    d = AttnCase(19, 2, 4, 128, 16, [1] * 6, [60, 45, 199, 1, 20, 7], prefix=[150], groups=[0, 6])
+    Hq, D, T = 8, 128, 6
+    ws = torch.empty(B.osc_paged_attention_workspace_bytes(T, Hq, D, 6, 1), dtype=torch.uint8, device="cuda")
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graphs = []
+    with torch.cuda.stream(st):
+        for x in (c, d):
+            x.o = torch.full((T, Hq * D), 7.0, dtype=torch.bfloat16, device="cuda")
+            x.lse = torch.full((T, Hq), 7.0, device="cuda")
+            cache = B.KvCache(x.k, x.v)
+            args = (x.q, cache, x.row_off, x.kv_len, x.table, x.o, ws, x.scale, x.lse, x.group_off, x.prefix_len, x.ptable, 1)
+            B.osc_paged_attention(*args)
+            st.synchronize()
+            x.check(x.o, x.lse, "side stream")
+            x.o.fill_(7.0)
+            g = torch.cuda.CUDAGraph()
+            st.synchronize()
+            with torch.cuda.graph(g, stream=st):
+                B.osc_paged_attention(*args)
+            graphs.append(g)
+        for _ in range(3):
+            for g in graphs:
+                g.replay()
+        st.synchronize()
+        c.check(c.o, c.lse, "graph 1")
+        d.check(d.o, d.lse, "graph 2")
+        kv = [100, 5, 30, 64, 0, 1]                    # shorter than the pages hold: the keys are the first ones
+        c.kv_len.copy_(torch.tensor(kv, dtype=torch.int32))
+        c.prefix_len.fill_(70)
+        graphs[0].replay()
+        st.synchronize()
+    c.kv, c.prefix = kv, [70]
+    c.own = [(K[:n], V[:n]) for (K, V), n in zip(c.own, kv)]
+    c.pre = [(K[:70], V[:70]) for K, V in c.pre]
+    c.check(c.o, c.lse, "graph 1 with other lengths")
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_random_steps(B, seed):
+    rng = np.random.default_rng(100 + seed)
+    R = int(rng.integers(1, 12))
+    new = [int(rng.integers(0, 3)) if rng.random() < 0.7 else int(rng.integers(0, 90)) for _ in range(R)]
+    kv = [n + int(rng.integers(0, 400)) if rng.random() < 0.8 else int(rng.integers(0, n + 1)) for n in new]
+    P = int(rng.integers(0, 3))
+    cuts = sorted(int(x) for x in rng.integers(0, R + 1, P + 1)) if P else None
+    go(B, seed=seed, Hk=int(rng.integers(1, 4)), G=int(rng.choice([1, 2, 4, 5, 8])), D=int(rng.choice([64, 128])), page=int(rng.choice([16, 32, 64])),
+       new=new, kv=kv, prefix=[int(x) for x in rng.integers(0, 500, P)], groups=cuts, tail_rows=int(rng.integers(0, 3)),
+       max_new=int(rng.choice([0, 1, max(new + [1])])), pad=8 * int(rng.integers(0, 3)))
+
+
+def test_offsets_past_32_bits(B):
+    """A cache whose last pages lie more than 2^32 elements behind its first."""
+    n_pages, page, Hk, D = 2_200_000, 16, 1, 128
+    if torch.cuda.mem_get_info()[0] < 24e9:
+        pytest.skip("needs 24 GB")
+    c = AttnCase(20, Hk, 4, D, page, [1, 40], [500, 300], prefix=[333])
+    for name in ("k", "v"):
+        small = getattr(c, name)
+        big = torch.empty((n_pages, page, Hk, D), dtype=torch.bfloat16, device="cuda")
+        big[-small.shape[0]:] = small
+        setattr(c, name, big)
+    shift = n_pages - small.shape[0]
+    for t in (c.table, c.ptable):
+        t.copy_(torch.where((t >= 0) & (t < small.shape[0]), t + shift, t))
+        t.copy_(torch.where(t < n_pages, t, n_pages + 5))
+    o, lse = c.run(B)
+    B.osc_sync_check()
+    c.check(o, lse, "far pages")

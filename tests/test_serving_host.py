@@ -1,0 +1,140 @@
+"""The calls around the paged key/value cache on a host without a GPU: refusals before any device work, and the 64-bit
+definitions against hand-worked values."""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+
+from oracle import serving
+
+
+@pytest.fixture(scope="module")
+def B():
+    import __graft_entry__ as g
+    g.build()
+    from paper_2604_12782_b200 import binding
+    return binding
+
+
+def cache(B, **kw):
+    a = dict(k=0x1000, v=0x2000, n_pages=4, page_size=16, n_heads=2, head_dim=128, page_stride=16 * 256, token_stride=256, head_stride=128)
+    a.update(kw)
+    return B.KvCacheStruct(*a.values())
+
+
+def test_kv_slots_refusals(B):
+    ok = dict(cached=0x1000, fresh=0x2000, base=None, R=2, page=16, free=0x3000, n_free=4, table=0x4000, cols=3, ld=3, T=5, row=0x5000, kv=0x6000,
+              slots=0x7000, pos=0x8000, taken=0x9000)
+
+    def call(**kw):
+        return B._lib.osc_kv_slots(*{**ok, **kw}.values(), None)
+    for k in ("cached", "fresh", "free", "table", "row", "kv", "slots", "pos", "taken"):
+        assert call(**{k: None}) == -1, k
+    assert call(R=-1) == -1 and call(T=-1) == -1 and call(n_free=-1) == -1 and call(cols=-1) == -1
+    assert call(page=0) == -2 and call(ld=2) == -2
+
+
+def test_qk_norm_rope_refusals(B):
+    def call(T=4, ld=8 * 128, n_q=4, c=None, rot=128, axes=1, pos=0x5000, Q=0x6000, ldq=512, qkv=0x7000, inv=0x8000, ld_pos=4, null_rope=False):
+        r = B.RopeStruct(inv, None, rot, axes, 0, 1.0)
+        return B._lib.osc_qk_norm_rope(qkv, T, ld, n_q, c or cache(B), None, None, 1e-6, None if null_rope else r, pos, ld_pos, None, Q, ldq, None)
+    assert call(T=0) == 0 and call(T=0, qkv=None, Q=None, pos=None) == 0
+    assert call(T=-1) == -1 and call(n_q=0) == -1 and call(null_rope=True) == -1
+    assert call(qkv=None) == -1 and call(Q=None) == -1 and call(pos=None) == -1 and call(inv=None) == -1
+    assert call(rot=8) == -2 and call(rot=20) == -2 and call(rot=144) == -2 and call(axes=0) == -1 and call(axes=4) == -1
+    assert call(ld=1016) == -2 and call(ldq=504) == -2 and call(axes=2, ld_pos=3) == -2
+    assert call(ld=1028) == -4 and call(ldq=516) == -4 and call(Q=0x6008) == -4 and call(qkv=0x7002) == -4
+    assert call(c=cache(B, head_dim=96)) == -2 and call(c=cache(B, n_heads=0)) == -1 and call(c=cache(B, page_size=0)) == -1
+    assert call(c=cache(B, k=None)) == -1 and call(c=cache(B, k=0x1008)) == -4 and call(c=cache(B, token_stride=252)) == -4
+    assert call(c=cache(B, head_stride=64)) == -2 and call(c=cache(B, n_pages=2 ** 28)) == -2 and call(c=cache(B, n_pages=-1)) == -1
+
+
+def test_paged_attention_refusals(B):
+    ok = dict(Q=0x1000, T=4, ldq=512, n_q=4, c=cache(B), R=2, row=0x2000, kv=0x3000, table=0x4000, cols=3, ld=3, P=0, goff=None, plen=None, ptab=None,
+              pcols=0, ldp=0, max_new=0, scale=0.1, O=0x5000, ldo=512, lse=None, ws=0x10000, n=1 << 40)
+
+    def call(**kw):
+        return B._lib.osc_paged_attention(*{**ok, **kw}.values(), None)
+    assert call(T=0) == 0 and call(R=0) == 0
+    for k in ("Q", "row", "kv", "table", "O", "ws"):
+        assert call(**{k: None}) == -1, k
+    pre = dict(P=2, goff=0x6000, plen=0x7000, ptab=0x8000, pcols=2, ldp=2)
+    for k in ("goff", "plen", "ptab"):
+        assert call(**{**pre, k: None}) == -1, k
+    assert call(**{**pre, "ldp": 1}) == -2 and call(ld=2) == -2 and call(**{**pre, "pcols": -1}) == -1
+    assert call(T=-1) == -1 and call(R=-1) == -1 and call(P=-1) == -1 and call(cols=-1) == -1 and call(max_new=-1) == -1
+    assert call(n_q=5) == -2 and call(n_q=258, ldq=258 * 128, ldo=258 * 128) == -2 and call(n_q=0) == -1
+    assert call(c=cache(B, page_size=24)) == -2 and call(c=cache(B, page_size=8)) == -2
+    for s in (0.0, -1.0, math.inf, math.nan):
+        assert call(scale=s) == -1, s
+    assert call(ldq=504) == -2 and call(ldo=504) == -2 and call(ldq=516) == -4 and call(O=0x5004) == -4 and call(ws=0x10008) == -4
+    assert call(n=1000) == -5
+    sz = C.c_size_t()
+    f = B._lib.osc_paged_attention_workspace_bytes
+    assert f(1, 4, 128, 1, 0, C.byref(sz)) == 0 and sz.value > 0
+    assert call(n=B.osc_paged_attention_workspace_bytes(4, 4, 128, 2, 0) - 1) == -5
+    assert f(1, 4, 96, 1, 0, C.byref(sz)) == -2 and f(-1, 4, 128, 1, 0, C.byref(sz)) == -1 and f(1, 4, 128, 1, 0, None) == -1
+    assert B.osc_paged_attention_workspace_bytes(300, 32, 128, 9, 2) > B.osc_paged_attention_workspace_bytes(200, 32, 128, 9, 2)
+
+
+def test_binding_refuses_wrong_tensors(B):
+    import torch
+    i, b = torch.zeros(4, dtype=torch.int32), torch.zeros(2, 16, 2, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="cuda"):
+        B.osc_kv_slots(i, i, None, 16, i, i.view(2, 2), i, i, i, i, i)
+    with pytest.raises(ValueError, match="int32"):
+        B.osc_kv_slots(i.long(), i, None, 16, i, i.view(2, 2), i, i, i, i, i)
+    with pytest.raises(ValueError, match="cuda"):
+        B.KvCache(b, b)
+    with pytest.raises(ValueError, match="bfloat16"):
+        B.KvCache(b.half(), b.half())
+    with pytest.raises(ValueError, match="float32"):
+        B.Rope(torch.zeros(4, dtype=torch.float64))
+
+
+def test_definition_of_slots_by_hand():
+    # pages of 4; request 0 holds 3 tokens on page 7 and gets 2 (one on the old page, one on a new one), request 1 gets none,
+    # request 2 starts with 5
+    row, kv, table, slots, pos, taken = serving.kv_slots([3, 8, 0], [2, 0, 5], [10, 0, 100], 4, [20, 21, 22, 23],
+                                                         [[7, -1], [1, 2], [-1, -1]], 8)
+    assert row.tolist() == [0, 2, 2, 7] and kv.tolist() == [5, 8, 5] and taken == 3
+    assert table.tolist() == [[7, 20], [1, 2], [21, 22]]
+    assert slots.tolist() == [31, 80, 84, 85, 86, 87, 88, -1]
+    assert pos.tolist() == [13, 14, 100, 101, 102, 103, 104, 0]
+
+
+def test_definition_of_norm_and_rotation():
+    rng = np.random.default_rng(0)
+    x = rng.standard_normal((3, 2, 16))
+    g = rng.uniform(0.5, 1.5, 16)
+    inv = np.array([1.0, 0.25, 0.125, 0.5, 0.0625, 0.75, 0.375, 0.03125], np.float32)
+    pos = np.array([[0, 7, 100000]])
+    y, size = serving.qk_norm_rope(x, g, 1e-6, inv, None, pos, False)
+    n = x / np.sqrt((x * x).mean(-1, keepdims=True) + 1e-6) * g
+    assert np.allclose(y[0], n[0], atol=1e-15)                                   # position 0 turns nothing
+    assert np.allclose((y ** 2).sum(-1), (n ** 2).sum(-1), rtol=1e-13)           # a rotation keeps lengths
+    z = (n[:, :, :8] + 1j * n[:, :, 8:]) * np.exp(1j * pos[0][:, None, None] * inv)
+    assert np.allclose(y[:, :, :8], z.real, atol=1e-10) and np.allclose(y[:, :, 8:], z.imag, atol=1e-10)
+    yi, _ = serving.qk_norm_rope(x, g, 1e-6, inv, None, pos, True)
+    zi = (n[:, :, 0::2] + 1j * n[:, :, 1::2]) * np.exp(1j * pos[0][:, None, None] * inv)
+    assert np.allclose(yi[:, :, 0::2], zi.real, atol=1e-10) and np.allclose(yi[:, :, 1::2], zi.imag, atol=1e-10)
+    # two axes: pairs of axis 1 turn by the second row; the same position on both axes is the one-axis rotation
+    ax = np.array([0, 1] * 4)
+    two, _ = serving.qk_norm_rope(x, g, 1e-6, inv, ax, np.concatenate([pos, pos]), False)
+    assert np.array_equal(two, y)
+    two, _ = serving.qk_norm_rope(x, g, 1e-6, inv, ax, np.concatenate([pos, 0 * pos]), False)
+    assert np.allclose(two[:, :, 1], n[:, :, 1]) and np.allclose(two[:, :, 0], y[:, :, 0])
+
+
+def test_definition_of_attention():
+    rng = np.random.default_rng(1)
+    q, k, v = rng.standard_normal((3, 2, 4, 8)), rng.standard_normal((9, 2, 8)), rng.standard_normal((9, 2, 8))
+    o, lse, absv, _ = serving.attention(q, k, v, [0, 1, 9], 0.5)
+    assert (o[0] == 0).all() and np.isneginf(lse[0]).all()
+    assert np.allclose(o[1], np.broadcast_to(v[0][:, None], (2, 4, 8)))
+    for h in range(2):
+        s = 0.5 * q[2, h] @ k[:, h].T
+        w = np.exp(s) / np.exp(s).sum(-1, keepdims=True)
+        assert np.allclose(o[2, h], w @ v[:, h]) and np.allclose(lse[2, h], np.log(np.exp(s).sum(-1)))
+        assert (absv[2, h] >= np.abs(o[2, h])).all()
