@@ -22,6 +22,24 @@ static osc_status check_cache(const osc_kv_cache_t* c) {
     return OSC_OK;
 }
 
+// bf16 tensor map of 3 or 4 dimensions, boxes of 64 channels, 128-byte swizzle, zeros outside.  strides in elements.
+static osc_status encode_heads(CUtensorMap* tm, const void* base, int rank, const int64_t* dims, const int64_t* strides, const int* box,
+                               const char* what) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return fail(OSC_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
+    cuuint64_t gdim[4], gstr[3];
+    cuuint32_t gbox[4], estr[4] = {1, 1, 1, 1};
+    for (int i = 0; i < rank; ++i) {
+        gdim[i] = (cuuint64_t)dims[i];
+        gbox[i] = (cuuint32_t)box[i];
+        if (i) gstr[i - 1] = (cuuint64_t)(dims[i] > 1 ? strides[i] : dims[0]) * 2;
+    }
+    CUresult r = fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), gdim, gstr, gbox, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return fail(OSC_ERR_CUDA, "cuTensorMapEncodeTiled(%s) failed with code %d", what, (int)r);
+    return OSC_OK;
+}
+
 struct AttnLayout {
     size_t few_start, wide_start, group, dense[2], dense_ml[2], few_part, few_ml, wide_part, wide_ml, total;
 };
@@ -151,7 +169,8 @@ osc_status osc_paged_attention(const void* Q, int T, int64_t ldq, int n_q, const
     DeviceInfo di;
     if (osc_status s = device_info(&di)) return s;
     uint8_t* ws = static_cast<uint8_t*>(workspace);
-    AttnArgs a = {};
+    AttnWideArgs w = {};
+    AttnArgs& a = w.a;
     a.q = static_cast<const uint16_t*>(Q); a.ldq = ldq; a.o = static_cast<uint16_t*>(O); a.ldo = ldo; a.lse = lse;
     a.k = static_cast<const uint16_t*>(cache->k); a.v = static_cast<const uint16_t*>(cache->v);
     a.page_stride = cache->page_stride; a.token_stride = cache->token_stride; a.head_stride = cache->head_stride;
@@ -162,7 +181,20 @@ osc_status osc_paged_attention(const void* Q, int T, int64_t ldq, int n_q, const
     a.scale_log2 = scale * 1.44269504088896341f;
     a.few_ctas = di.num_sms * 2 < AT_FEW_CTAS ? di.num_sms * 2 : AT_FEW_CTAS;
     a.wide_ctas = di.num_sms < AT_WIDE_CTAS ? di.num_sms : AT_WIDE_CTAS;
-    a.wide_min_rows = 0x7FFFFFFF;
+    // Up to 16 rows per key/value head a request is one unit of the few-row kernel, whatever the rest of the step is.  The tcgen05
+    // kernel is launched where a segment may have more: a shared prefix, or requests with more new tokens than that.
+    const bool wide = a.n_pages > 0 && (P > 0 || max_new == 0 || (int64_t)max_new * a.G > AT_FEW_ROWS);
+    a.wide_min_rows = wide ? AT_FEW_ROWS + 1 : 0x7FFFFFFF;
+    if (wide) {
+        const int64_t qd[3] = {D, n_q, T}, qs[3] = {1, D, ldq};
+        const int qb[3] = {64, a.G, AT_WIDE_TILE / a.G};
+        const int64_t kd[4] = {D, cache->page_size, cache->n_heads, cache->n_pages};
+        const int64_t ks[4] = {1, cache->token_stride, cache->head_stride, cache->page_stride};
+        const int kb[4] = {64, cache->page_size < AT_WIDE_KEYS ? cache->page_size : AT_WIDE_KEYS, 1, 1};
+        if (osc_status s = encode_heads(&w.tm_q, Q, 3, qd, qs, qb, "Q")) return s;
+        if (osc_status s = encode_heads(&w.tm_k, cache->k, 4, kd, ks, kb, "K")) return s;
+        if (osc_status s = encode_heads(&w.tm_v, cache->v, 4, kd, ks, kb, "V")) return s;
+    }
     a.plan.few_start = reinterpret_cast<int64_t*>(ws + l.few_start);
     a.plan.wide_start = reinterpret_cast<int64_t*>(ws + l.wide_start);
     a.plan.req_group = reinterpret_cast<int32_t*>(ws + l.group);
@@ -174,7 +206,7 @@ osc_status osc_paged_attention(const void* Q, int T, int64_t ldq, int n_q, const
     a.few_ml = reinterpret_cast<float2*>(ws + l.few_ml);
     a.wide_part = reinterpret_cast<float*>(ws + l.wide_part);
     a.wide_ml = reinterpret_cast<float2*>(ws + l.wide_ml);
-    cudaError_t e = launch_attn(a, D, static_cast<cudaStream_t>(stream));
+    cudaError_t e = launch_attn(w, D, wide, static_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) return cuda_fail(e, "attention kernels");
     return OSC_OK;
 }

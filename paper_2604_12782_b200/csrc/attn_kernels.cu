@@ -692,19 +692,4 @@ __global__ void __launch_bounds__(AT_JOIN_THREADS) attn_join_kernel(const AttnAr
     }
 }
 
-// ---------------------------------------------------------------------------------------------- launch
-template <int D>
-static cudaError_t launch_attn_d(const AttnArgs& a, cudaStream_t st) {
-    static PerDevice pd;
-    cudaError_t e = opt_in_shared_memory(pd, attn_few_kernel<D>, FewCfg<D>::SMEM);
-    if (e != cudaSuccess) return e;
-    if ((e = launch_pdl(attn_plan_kernel, dim3(1), dim3(AT_PLAN_THREADS), 0, st, a)) != cudaSuccess) return e;
-    if ((e = launch_pdl(attn_few_kernel<D>, dim3(a.few_ctas), dim3(AT_FEW_THREADS), FewCfg<D>::SMEM, st, a)) != cudaSuccess) return e;
-    return launch_pdl(attn_join_kernel<D>, dim3(a.T, a.Hk), dim3(AT_JOIN_THREADS), 0, st, a);
-}
-
-cudaError_t launch_attn(const AttnArgs& a, int D, cudaStream_t st) {
-    return D == 128 ? launch_attn_d<128>(a, st) : launch_attn_d<64>(a, st);
-}
-
 }  // namespace osc

@@ -8,6 +8,7 @@
 #include "profile_kernels.cu"
 #include "kv_kernels.cu"
 #include "attn_kernels.cu"
+#include "attn2_kernels.cu"
 #include "api.cu"
 #include "static_scratch.cu"
 #include "attn_api.cu"
