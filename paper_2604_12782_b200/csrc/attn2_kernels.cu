@@ -13,10 +13,14 @@
 //   warps 0-3, 4-7 : softmax of stream 0, 1, and their epilogue
 //   warp 8         : TMA (a key tile is loaded page by page; a page that is not there reads as zeros)
 //   warp 9         : MMA issue, TMEM owner
+//   warp 10        : the units of the CTA's share, for everyone else
+//   warp 11        : idle; the third warpgroup gives registers to the softmax
 //
 // P V with the weights of the running maximum as it stands: O is rescaled in TMEM only when the maximum has moved by
 // more than 2^8 (see AT_SLACK), by the softmax threads themselves.  That needs no wait of its own: the S tile that moved
 // the maximum was issued behind the previous P V, so S complete means O complete.
+#include <algorithm>
+
 #include "common.cuh"
 
 namespace osc {
@@ -28,7 +32,37 @@ struct AttnWideArgs {
     AttnArgs a;
 };
 
-constexpr int AW_THREADS = 320;
+constexpr int AW_THREADS = 384;
+// Registers: launched with 168 a thread (12 warps); the softmax warpgroups hold a row of 128 scores each thread and take
+// 208, the third warpgroup (TMA, MMA, two idle warps) gives down to 80: 256 x 208 + 128 x 80 <= 384 x 168.
+constexpr int AW_REGS_SOFTMAX = 208, AW_REGS_OTHER = 80;
+template <int R>
+__device__ __forceinline__ void regs_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(R)); }
+template <int R>
+__device__ __forceinline__ void regs_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(R)); }
+
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ uint64_t pack2(float x, float y) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t r, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(r)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
 
 template <int D>
 struct WideCfg {
@@ -36,8 +70,8 @@ struct WideCfg {
     static constexpr int HALF_BYTES = 128 * 128;
     static constexpr int TILE_BYTES = HALVES * HALF_BYTES;       // 128 rows (or keys) x D
     static constexpr int STAGES = D == 128 ? 5 : 8;
-    static constexpr int BAR_BYTES = 256;
-    static constexpr int SMEM = (2 + STAGES) * TILE_BYTES + BAR_BYTES + 128 * 8 + 1024;
+    static constexpr int BAR_BYTES = 384;
+    static constexpr int SMEM = (2 + STAGES) * TILE_BYTES + BAR_BYTES + 128 * 8 + 2 * 64 + 1024;
     static constexpr int TM_S = 0;         // TMEM columns: S0, S1, O0, O1
     static constexpr int TM_O = 256;
     static_assert(SMEM <= 232448, "shared memory");
@@ -65,6 +99,11 @@ __device__ __forceinline__ void tmem_st_32x32(uint32_t taddr, const uint32_t* r)
                  "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]),
                  "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
 }
+__device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t* r) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+                 "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // Descriptor of a V tile as the B operand of P V: B is [channel][key], stored with the channels contiguous (64 to a
@@ -81,29 +120,27 @@ __device__ __forceinline__ uint64_t smem_desc_sw128_mn(uint32_t saddr, uint32_t 
 }
 constexpr uint32_t IDESC_B_MN = 1u << 16;   // B operand with its N extent contiguous
 
-// The part of a unit that a CTA's share has: key tiles [ka, kb); stream s takes cnt[s] of them.
-struct WideUnit {
-    int ka, kb, cnt[2];
-    bool pair;
-    __device__ int tile(int s, int i) const { return pair ? ka + i : ka + 2 * i + s; }
-    __device__ int load(int s, int i) const { return pair ? i : 2 * i + s; }      // which of the unit's K (or V) loads
+// What the roles need to know of a unit, or of the part of it that the CTA's share has: key tiles [ka, ka + n).  Warp 10
+// walks over the line and keeps two of these ahead in shared memory.
+struct __align__(16) WideUnit {
+    int ka, n;          // n = 0: the share is done
+    int cnt[2];         // key tiles of stream 0 and 1
+    int pair;           // both row tiles filled: stream s has row tile s and all its key tiles; else every other key tile
+    int nf;             // key tiles in front (the group's prefix), before the own keys'
+    int plen, klen;     // keys in front, own keys
+    int front, seg;     // segments that name the pages of the keys in front and of the own keys
+    int h, row0;        // head, first row of the unit (token index in Q)
+    int tok0, tokens;   // first token of the unit and number of tokens, inside the segment
+    int causal;
+    int out;            // bits: OUT_*
 };
-__device__ __forceinline__ WideUnit wide_unit(const AttnArgs& a, const Cursor<WideUnits>& c, int64_t x, int64_t x1) {
-    WideUnit w;
-    w.ka = c.kt;
-    w.kb = (int)min((int64_t)c.nt, c.kt + (x1 - x));
-    const int tpt = AT_WIDE_TILE / a.G, tok0 = c.u * 2 * tpt;
-    const int n = w.kb - w.ka;
-    w.pair = c.g.n > tok0 + tpt;
-    if (w.pair) {
-        const int nt0 = (seg_sees(c.g, tok0 + tpt - 1) + AT_WIDE_KEYS - 1) / AT_WIDE_KEYS;
-        w.cnt[0] = max(min(w.kb, nt0) - w.ka, 0);
-        w.cnt[1] = n;
-    } else {
-        w.cnt[0] = (n + 1) / 2;
-        w.cnt[1] = n / 2;
-    }
-    return w;
+constexpr int OUT_SPLIT = 1, OUT_TWO = 2, OUT_OWN = 4, OUT_LATER = 8;   // OUT_LATER: the share has tiles before this unit
+
+__device__ __forceinline__ int unit_tile(const WideUnit& w, int s, int i) { return w.pair ? w.ka + i : w.ka + 2 * i + s; }
+__device__ __forceinline__ int unit_load(const WideUnit& w, int s, int i) { return w.pair ? i : 2 * i + s; }   // which of the unit's K (or V) loads
+// keys of key tile kt before any mask
+__device__ __forceinline__ int unit_left(const WideUnit& w, int kt) {
+    return kt < w.nf ? w.plen - kt * AT_WIDE_KEYS : w.klen - (kt - w.nf) * AT_WIDE_KEYS;
 }
 
 template <int D>
@@ -125,10 +162,13 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
     uint64_t* o_empty = q_full + 8;
     uint64_t* j_full = q_full + 10;
     uint64_t* j_empty = q_full + 11;
-    uint64_t* drain_bar = q_full + 12;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(q_full + 13);
+    uint64_t* u_full = q_full + 12;      // [2]
+    uint64_t* u_empty = q_full + 14;     // [2]
+    uint64_t* drain_bar = q_full + 16;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(q_full + 17);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     float2* s_ml = reinterpret_cast<float2*>(reinterpret_cast<uint8_t*>(bars) + C::BAR_BYTES);   // [128]: stream 1's (m, l)
+    WideUnit* units = reinterpret_cast<WideUnit*>(s_ml + 128);                                   // [2]
 
     const int warp = __shfl_sync(0xFFFFFFFFu, (int)(threadIdx.x >> 5), 0);
     const int lane = threadIdx.x & 31;
@@ -141,6 +181,8 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
             mbar_init(&p_full[i], 4);
             mbar_init(&o_full[i], 1);
             mbar_init(&o_empty[i], 4);
+            mbar_init(&u_full[i], 1);
+            mbar_init(&u_empty[i], 10);
         }
         mbar_init(j_full, 4);
         mbar_init(j_empty, 4);
@@ -161,231 +203,293 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
     const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, *tmem_slot, 0);
     grid_launch_dependents();
     grid_dependency_wait();
-
-    const int S = a.P + a.R;
-    const int64_t N = a.plan.wide_start[S];
-    const int nc = line_ctas(N, a.wide_ctas, AT_WIDE_MIN_TILES);
-    int64_t x0 = 0, x1 = 0;
-    if (N > 0 && (int)blockIdx.x < nc) {
-        x0 = share_begin(N, nc, blockIdx.x);
-        x1 = share_begin(N, nc, blockIdx.x + 1);
-    }
-    Cursor<WideUnits> cur;
-    if (x0 < x1) cur.seek(a, a.plan.wide_start, S, x0);
     const int tpt = AT_WIDE_TILE / a.G;
 
-    if (x0 >= x1) {
-        // nothing on this share
-    } else if (warp == 8) {
-        // ------------------------------------------------------------------------------------------ TMA
-        const int bt = min(1 << a.page_shift, AT_WIDE_KEYS);     // tokens of a box
-        const int boxes = AT_WIDE_KEYS / bt * C::HALVES;         // of a K or V tile: at most 16, one lane each
-        const int mine = lane / C::HALVES, half = lane % C::HALVES;
-        const uint32_t ring0 = smem_u32(ring);
-        uint32_t n_load = 0;            // loads so far: stage n % STAGES, phase n / STAGES
-        int st = 0;
-        uint32_t ph = 0, q_ph = 0;
-        for (int64_t x = x0; x < x1;) {
-            const WideUnit w = wide_unit(a, cur, x, x1);
-            if (!wait_bounded(q_empty, q_ph ^ 1u, abort_flag, 61)) goto stop_loads;
-            q_ph ^= 1u;
-            if (elect_one()) {
-                const int tiles = w.pair ? 2 : 1;
-                mbar_arrive_expect_tx(q_full, (uint32_t)(tiles * C::HALVES * tpt * a.G * 128));
-                for (int t = 0; t < tiles; ++t)
-                    for (int hf = 0; hf < C::HALVES; ++hf)
-                        tma_load_3d(smem_u32(smem + t * C::TILE_BYTES + hf * C::HALF_BYTES), &args.tm_q, q_full, hf * 64, cur.h * a.G,
-                                    cur.g.t0 + (cur.u * 2 + t) * tpt);
-            }
-            __syncwarp();
-            for (int kt = w.ka; kt < w.kb; ++kt) {
-                int page = a.n_pages, place = 0;      // a box past the last page is filled with zeros
-                if (lane < boxes) {
-                    const int key = kt * AT_WIDE_KEYS + mine * bt;
-                    if (key < cur.g.klen) {
-                        const int col = key >> a.page_shift;
-                        const int p = col < cur.g.npages ? cur.g.pages[col] : -1;
-                        if (p >= 0 && p < a.n_pages) page = p;
-                        place = key & ((1 << a.page_shift) - 1);
+    if (warp >= 8) {
+        regs_dec<AW_REGS_OTHER>();
+        if (warp == 10) {
+            // ------------------------------------------------------------------------------------- units
+            const int S = a.P + a.R;
+            const int64_t N = a.plan.wide_start[S], q = a.plan.share[1];
+            const int64_t x0 = min(q * blockIdx.x, N), x1 = min(x0 + q, N);
+            Cursor<WideUnits> cur;
+            if (x0 < x1) cur.seek(a, a.plan.wide_start, S, x0);
+            else if (lane == 0) a.plan.cut[1][blockIdx.x].tiles = 0;
+            int b = 0;
+            uint32_t ph = 0;
+            for (int64_t x = x0;;) {
+                WideUnit w = {};
+                if (x < x1) {
+                    w.ka = cur.kt;
+                    w.n = (int)min((int64_t)(cur.nt - cur.kt), x1 - x);
+                    w.tok0 = cur.u * 2 * tpt;
+                    w.tokens = min(cur.g.n - w.tok0, 2 * tpt);
+                    w.pair = w.tokens > tpt;
+                    w.nf = front_tiles<WideUnits>(a, cur.g);
+                    if (w.pair) {
+                        const int nt0 = w.nf + (seg_sees(cur.g, w.tok0 + tpt - 1) + AT_WIDE_KEYS - 1) / AT_WIDE_KEYS;
+                        w.cnt[0] = max(min(w.ka + w.n, nt0) - w.ka, 0);
+                        w.cnt[1] = w.n;
+                    } else {
+                        w.cnt[0] = (w.n + 1) / 2;
+                        w.cnt[1] = w.n / 2;
                     }
+                    w.plen = cur.g.plen;
+                    w.klen = cur.g.klen;
+                    w.front = cur.g.group;
+                    w.seg = cur.s;
+                    w.h = cur.h;
+                    w.row0 = cur.g.t0 + w.tok0;
+                    w.causal = cur.g.causal ? cur.g.n : 0;
+                    w.out = (w.n < cur.nt ? OUT_SPLIT : 0) | (cur.g.flags & SEG_TWO ? OUT_TWO : 0) | (cur.s >= a.P ? OUT_OWN : 0) | (x > x0 ? OUT_LATER : 0);
                 }
-#pragma unroll
-                for (int kv = 0; kv < 2; ++kv) {
-                    if (!wait_bounded(&empty[st], ph ^ 1u, abort_flag, 62)) goto stop_loads;
-                    if (lane == 0) mbar_arrive_expect_tx(&full[st], C::TILE_BYTES);
-                    __syncwarp();
-                    if (lane < boxes)
-                        tma_load_4d(ring0 + st * C::TILE_BYTES + half * C::HALF_BYTES + mine * bt * 128, kv ? &args.tm_v : &args.tm_k, &full[st],
-                                    half * 64, place, cur.h, page);
-                    ++n_load;
-                    if (++st == STAGES) { st = 0; ph ^= 1u; }
+                if (!wait_bounded(&u_empty[b], ph ^ 1u, abort_flag, 76)) break;
+                if (lane == 0) {
+                    units[b] = w;
+                    mbar_arrive(&u_full[b]);
                 }
+                if (++b == 2) { b = 0; ph ^= 1u; }
+                if (w.n == 0) break;
+                if (x + w.n == x1 && lane == 0)
+                    tell_cut(a.plan.cut[1][blockIdx.x], x - w.ka, x - w.ka + cur.nt, x0, x1, cur.s, cur.h, cur.u, cur.g.flags);
+                x += w.n;
+                if (x < x1) cur.next_unit(a, SEG_WIDE);
             }
-            x += w.kb - w.ka;
-            if (x < x1) cur.next_unit(a, a.plan.wide_start);
-        }
-    stop_loads:
-        __syncwarp();
-        if (*abort_flag) {      // gave up somewhere: the copies under way land before the CTA's memory goes away
-            int dummy = 0;
-            volatile int* never = &dummy;
-            for (uint32_t i = n_load > STAGES ? n_load - STAGES : 0; i < n_load; ++i)
-                wait_bounded(&full[i % STAGES], (i / STAGES) & 1u, never, 63);
-            if (q_ph) wait_bounded(q_full, 0u, never, 64); else wait_bounded(q_full, 1u, never, 64);
-        }
-    } else if (warp == 9) {
-        // ------------------------------------------------------------------------------------------ MMA
-        const uint32_t ring0 = smem_u32(ring), q0 = smem_u32(smem);
-        const uint64_t k_hi = smem_desc_sw128(0), v_hi = smem_desc_sw128_mn(0, C::HALVES > 1 ? C::HALF_BYTES : 1024);
-        constexpr uint32_t IDESC_S = idesc_bf16(128, 128), IDESC_O = idesc_bf16(128, D) | IDESC_B_MN;
-        uint32_t base = 0;                 // loads of the units before
-        uint32_t q_ph = 0, p_ph[2] = {0, 0}, oe_ph[2] = {1, 1};
-        for (int64_t x = x0; x < x1;) {
-            const WideUnit w = wide_unit(a, cur, x, x1);
-            if (!wait_bounded(q_full, q_ph, abort_flag, 65)) goto done;
-            q_ph ^= 1u;
-            // S_s(i): product of the stream's rows with its i-th key tile
-            auto issue_s = [&](int s, int i) -> bool {
-                const uint32_t n = base + 2 * w.load(s, i), stg = n % STAGES;
-                if (!wait_bounded(&full[stg], (n / STAGES) & 1u, abort_flag, 66)) return false;
-                tc_fence_after();
+        } else if (warp == 8) {
+            // --------------------------------------------------------------------------------------- TMA
+            const int bt = min(1 << a.page_shift, AT_WIDE_KEYS);     // tokens of a box
+            const int boxes = AT_WIDE_KEYS / bt * C::HALVES;         // of a K or V tile: at most 16, one lane each
+            const int mine = lane / C::HALVES, half = lane % C::HALVES;
+            const uint32_t ring0 = smem_u32(ring);
+            uint32_t n_load = 0;            // loads so far: stage n % STAGES, phase n / STAGES
+            int st = 0, b = 0;
+            uint32_t ph = 0, q_ph = 0, u_ph = 0;
+            while (true) {
+                if (!wait_bounded(&u_full[b], u_ph, abort_flag, 60)) goto stop_loads;
+                const WideUnit& w = units[b];
+                const int ka = w.ka, kb = ka + w.n, nf = w.nf, h = w.h;
+                if (kb == ka) break;
+                if (!wait_bounded(q_empty, q_ph ^ 1u, abort_flag, 61)) goto stop_loads;
+                q_ph ^= 1u;
                 if (elect_one()) {
-                    const uint32_t qa = q0 + (w.pair && s ? C::TILE_BYTES : 0), kb = ring0 + stg * C::TILE_BYTES;
-#pragma unroll
-                    for (int k = 0; k < D / 16; ++k) {
-                        const uint32_t off = (k / 4) * C::HALF_BYTES + (k % 4) * 32;
-                        mma_f16(tmem + C::TM_S + s * 128, k_hi | (uint64_t)((qa + off) >> 4), k_hi | (uint64_t)((kb + off) >> 4), IDESC_S, k ? 1u : 0u);
-                    }
-                    tc_commit(&s_full[s]);
-                    if (!w.pair || s == 1) tc_commit(&empty[stg]);
+                    const int tiles = w.pair ? 2 : 1;
+                    mbar_arrive_expect_tx(q_full, (uint32_t)(tiles * C::HALVES * tpt * a.G * 128));
+                    for (int t = 0; t < tiles; ++t)
+                        for (int hf = 0; hf < C::HALVES; ++hf)
+                            tma_load_3d(smem_u32(smem + t * C::TILE_BYTES + hf * C::HALF_BYTES), &args.tm_q, q_full, hf * 64, h * a.G, w.row0 + t * tpt);
                 }
                 __syncwarp();
-                return true;
-            };
-            for (int s = 0; s < 2; ++s)
-                if (w.cnt[s] > 0 && !issue_s(s, 0)) goto done;
-            const int most = max(w.cnt[0], w.cnt[1]);
-            for (int i = 0; i < most; ++i) {
-                for (int s = 0; s < 2; ++s) {
-                    if (i >= w.cnt[s]) continue;
-                    if (i == 0) {      // the epilogue of the unit before has read O
-                        if (!wait_bounded(&o_empty[s], oe_ph[s], abort_flag, 67)) goto done;
-                        oe_ph[s] ^= 1u;
+                const int32_t* own_pages = seg_pages(a, w.seg);
+                const int32_t* front_pages = nf ? seg_pages(a, w.front) : own_pages;
+                for (int kt = ka; kt < kb; ++kt) {
+                    int page = a.n_pages, place = 0;      // a box past the last page is filled with zeros
+                    if (lane < boxes) {
+                        const int key = (kt < nf ? kt : kt - nf) * AT_WIDE_KEYS + mine * bt;
+                        if (mine * bt < unit_left(w, kt)) {          // a length is within the list's columns
+                            const int p = (kt < nf ? front_pages : own_pages)[key >> a.page_shift];
+                            if (p >= 0 && p < a.n_pages) page = p;
+                            place = key & ((1 << a.page_shift) - 1);
+                        }
                     }
-                    const uint32_t n = base + 2 * w.load(s, i) + 1, stg = n % STAGES;
-                    if (!wait_bounded(&full[stg], (n / STAGES) & 1u, abort_flag, 68)) goto done;
-                    const int left = cur.g.klen - w.tile(s, i) * AT_WIDE_KEYS;
-                    if (left < AT_WIDE_KEYS && (s == 0 || !w.pair || i >= w.cnt[0])) {
-                        // Behind the last key the page holds whatever was there before: a NaN or Inf would survive its weight of 0.
-                        uint8_t* v = ring + stg * C::TILE_BYTES;
-                        for (int c = left * 8 + lane; c < AT_WIDE_KEYS * 8; c += 32)
 #pragma unroll
-                            for (int hf = 0; hf < C::HALVES; ++hf)
-                                *reinterpret_cast<uint4*>(v + hf * C::HALF_BYTES + c * 16) = make_uint4(0u, 0u, 0u, 0u);
-                        fence_proxy_async_smem();
+                    for (int kv = 0; kv < 2; ++kv) {
+                        if (!wait_bounded(&empty[st], ph ^ 1u, abort_flag, 62)) goto stop_loads;
+                        if (lane == 0) mbar_arrive_expect_tx(&full[st], C::TILE_BYTES);
                         __syncwarp();
+                        if (lane < boxes)
+                            tma_load_4d(ring0 + st * C::TILE_BYTES + half * C::HALF_BYTES + mine * bt * 128, kv ? &args.tm_v : &args.tm_k, &full[st],
+                                        half * 64, place, h, page);
+                        ++n_load;
+                        if (++st == STAGES) { st = 0; ph ^= 1u; }
                     }
-                    if (!wait_bounded(&p_full[s], p_ph[s], abort_flag, 69)) goto done;
-                    p_ph[s] ^= 1u;
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&u_empty[b]);
+                if (++b == 2) { b = 0; u_ph ^= 1u; }
+            }
+        stop_loads:
+            __syncwarp();
+            if (*abort_flag) {      // gave up somewhere: the copies under way land before the CTA's memory goes away
+                int dummy = 0;
+                volatile int* never = &dummy;
+                for (uint32_t i = n_load > STAGES ? n_load - STAGES : 0; i < n_load; ++i)
+                    wait_bounded(&full[i % STAGES], (i / STAGES) & 1u, never, 63);
+                wait_bounded(q_full, q_ph ^ 1u, never, 64);
+            }
+        } else if (warp == 9) {
+            // --------------------------------------------------------------------------------------- MMA
+            const uint32_t ring0 = smem_u32(ring), q0 = smem_u32(smem);
+            const uint64_t k_hi = smem_desc_sw128(0), v_hi = smem_desc_sw128_mn(0, C::HALVES > 1 ? C::HALF_BYTES : 1024);
+            constexpr uint32_t IDESC_S = idesc_bf16(128, 128), IDESC_O = idesc_bf16(128, D) | IDESC_B_MN;
+            uint32_t base = 0;                 // loads of the units before
+            uint32_t q_ph = 0, p_ph[2] = {0, 0}, oe_ph[2] = {1, 1}, u_ph = 0;
+            int b = 0;
+            while (true) {
+                if (!wait_bounded(&u_full[b], u_ph, abort_flag, 77)) goto done;
+                const WideUnit& w = units[b];
+                const int n = w.n, pair = w.pair, cnt[2] = {w.cnt[0], w.cnt[1]};
+                if (n == 0) break;
+                if (!wait_bounded(q_full, q_ph, abort_flag, 65)) goto done;
+                q_ph ^= 1u;
+                // S_s(i): product of the stream's rows with its i-th key tile
+                auto issue_s = [&](int s, int i) -> bool {
+                    const uint32_t ld = base + 2 * unit_load(w, s, i), stg = ld % STAGES;
+                    if (!wait_bounded(&full[stg], (ld / STAGES) & 1u, abort_flag, 66)) return false;
                     tc_fence_after();
                     if (elect_one()) {
-                        const uint32_t vb = ring0 + stg * C::TILE_BYTES;
+                        const uint32_t qa = q0 + (pair && s ? C::TILE_BYTES : 0), kb = ring0 + stg * C::TILE_BYTES;
 #pragma unroll
-                        for (int k = 0; k < 8; ++k)
-                            mma_f16_ts(tmem + C::TM_O + s * D, tmem + C::TM_S + s * 128 + k * 8, v_hi | (uint64_t)((vb + k * 2048) >> 4), IDESC_O,
-                                       (i | k) ? 1u : 0u);
-                        if (!w.pair || s == 1) tc_commit(&empty[stg]);
-                        if (i == w.cnt[s] - 1) tc_commit(&o_full[s]);
+                        for (int k = 0; k < D / 16; ++k) {
+                            const uint32_t off = (k / 4) * C::HALF_BYTES + (k % 4) * 32;
+                            mma_f16(tmem + C::TM_S + s * 128, k_hi | (uint64_t)((qa + off) >> 4), k_hi | (uint64_t)((kb + off) >> 4), IDESC_S, k ? 1u : 0u);
+                        }
+                        tc_commit(&s_full[s]);
+                        if (!pair || s == 1) tc_commit(&empty[stg]);
                     }
                     __syncwarp();
-                    if (i + 1 < w.cnt[s] && !issue_s(s, i + 1)) goto done;
+                    return true;
+                };
+                for (int s = 0; s < 2; ++s)
+                    if (cnt[s] > 0 && !issue_s(s, 0)) goto done;
+                const int most = max(cnt[0], cnt[1]);
+                for (int i = 0; i < most; ++i) {
+                    for (int s = 0; s < 2; ++s) {
+                        if (i >= cnt[s]) continue;
+                        if (i == 0) {      // the epilogue of the unit before has read O
+                            if (!wait_bounded(&o_empty[s], oe_ph[s], abort_flag, 67)) goto done;
+                            oe_ph[s] ^= 1u;
+                        }
+                        const uint32_t ld = base + 2 * unit_load(w, s, i) + 1, stg = ld % STAGES;
+                        if (!wait_bounded(&full[stg], (ld / STAGES) & 1u, abort_flag, 68)) goto done;
+                        const int left = unit_left(w, unit_tile(w, s, i));
+                        if (left < AT_WIDE_KEYS && (s == 0 || !pair || i >= cnt[0])) {
+                            // Behind the last key the page holds whatever was there before: a NaN or Inf would survive its weight of 0.
+                            uint8_t* v = ring + stg * C::TILE_BYTES;
+                            for (int c = left * 8 + lane; c < AT_WIDE_KEYS * 8; c += 32)
+#pragma unroll
+                                for (int hf = 0; hf < C::HALVES; ++hf)
+                                    *reinterpret_cast<uint4*>(v + hf * C::HALF_BYTES + c * 16) = make_uint4(0u, 0u, 0u, 0u);
+                            fence_proxy_async_smem();
+                            __syncwarp();
+                        }
+                        if (!wait_bounded(&p_full[s], p_ph[s], abort_flag, 69)) goto done;
+                        p_ph[s] ^= 1u;
+                        tc_fence_after();
+                        if (elect_one()) {
+                            const uint32_t vb = ring0 + stg * C::TILE_BYTES;
+#pragma unroll
+                            for (int k = 0; k < 8; ++k)
+                                mma_f16_ts(tmem + C::TM_O + s * D, tmem + C::TM_S + s * 128 + k * 8, v_hi | (uint64_t)((vb + k * 2048) >> 4), IDESC_O,
+                                           (i | k) ? 1u : 0u);
+                            if (!pair || s == 1) tc_commit(&empty[stg]);
+                            if (i == cnt[s] - 1) tc_commit(&o_full[s]);
+                        }
+                        __syncwarp();
+                        if (i + 1 < cnt[s] && !issue_s(s, i + 1)) goto done;
+                    }
                 }
+                if (elect_one()) tc_commit(q_empty);
+                __syncwarp();
+                base += 2 * (uint32_t)n;
+                if (lane == 0) mbar_arrive(&u_empty[b]);
+                if (++b == 2) { b = 0; u_ph ^= 1u; }
             }
-            if (elect_one()) tc_commit(q_empty);
-            __syncwarp();
-            base += 2 * (uint32_t)(w.kb - w.ka);
-            x += w.kb - w.ka;
-            if (x < x1) cur.next_unit(a, a.plan.wide_start);
         }
     } else {
-        // -------------------------------------------------------------------------------------- softmax
+        // ------------------------------------------------------------------------------------------ softmax
+        regs_inc<AW_REGS_SOFTMAX>();
         const int s = warp >> 2;
         const int r = threadIdx.x & 127;                                 // row of the tile = TMEM lane
+        const int my_tok = r / a.G, my_head = r % a.G;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t t_s = tmem + lanes + C::TM_S + s * 128, t_o = tmem + lanes + C::TM_O;
-        uint32_t s_ph = 0, o_ph[2] = {0, 0};
-        uint32_t j_ph = 0;
-        for (int64_t x = x0; x < x1;) {
-            const WideUnit w = wide_unit(a, cur, x, x1);
-            const int tile = w.pair ? s : 0;
-            const int tok = (cur.u * 2 + tile) * tpt + r / a.G;          // token inside the segment
-            const bool valid = r < tpt * a.G && tok < cur.g.n;
-            const int sees = valid ? seg_sees(cur.g, tok) : cur.g.klen;
+        uint32_t s_ph = 0, o_ph[2] = {0, 0}, j_ph = 0, u_ph = 0;
+        int b = 0;
+        while (true) {
+            if (!wait_bounded(&u_full[b], u_ph, abort_flag, 78)) goto done;
+            const WideUnit& w = units[b];
+            if (w.n == 0) break;
             float m = -INFINITY, l = 0.0f;
-            for (int i = 0; i < w.cnt[s]; ++i) {
-                if (!wait_bounded(&s_full[s], s_ph, abort_flag, 70)) goto done;
-                s_ph ^= 1u;
-                tc_fence_after();
-                uint32_t v[4][32];
+            {
+                const int tok = (w.pair ? s * tpt : 0) + my_tok;         // token inside the unit
+                const bool valid = my_tok < tpt && tok < w.tokens;
+                const int nf = w.nf, step = w.pair ? 1 : 2;
+                // keys that the row sees from the first key of the own tile 0 on; a row that is not there sees all
+                const int sees = valid && w.causal ? max(w.klen - w.causal + w.tok0 + tok + 1, 0) : w.klen;
+                int kt = w.pair ? w.ka : w.ka + s;
+                for (int i = 0, cnt = w.cnt[s]; i < cnt; ++i, kt += step) {
+                    if (!wait_bounded(&s_full[s], s_ph, abort_flag, 70)) goto done;
+                    s_ph ^= 1u;
+                    tc_fence_after();
+                    uint32_t v[4][32];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) tmem_ld_32x32(t_s + j * 32, v[j]);
-                tmem_ld_wait();
-                const int left = sees - w.tile(s, i) * AT_WIDE_KEYS;     // keys of the tile that the row sees
-                if (!__all_sync(0xFFFFFFFFu, left >= AT_WIDE_KEYS)) {
+                    for (int j = 0; j < 4; ++j) tmem_ld_32x32(t_s + j * 32, v[j]);
+                    tmem_ld_wait();
+                    const int left = kt < nf ? w.plen - kt * AT_WIDE_KEYS : sees - (kt - nf) * AT_WIDE_KEYS;   // keys of the tile that the row sees
+                    if (!__all_sync(0xFFFFFFFFu, left >= AT_WIDE_KEYS)) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
+                        for (int j = 0; j < 4; ++j)
 #pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (j * 32 + e >= left) v[j][e] = 0xFF800000u;
-                }
-                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) mx[e & 3] = fmaxf(mx[e & 3], __uint_as_float(v[j][e]));
-                const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2;
-                float f = 1.0f;
-                const bool move = top > m + AT_SLACK;
-                if (move) {
-                    f = exp2_approx(m - top);
-                    m = top;
-                    l *= f;
-                }
-                const float ref = m == -INFINITY ? 0.0f : -m;
-                float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                uint32_t pk[64];
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-#pragma unroll
-                    for (int e = 0; e < 32; e += 2) {
-                        const float p0 = exp2_approx(fmaf(__uint_as_float(v[j][e]), a.scale_log2, ref));
-                        const float p1 = exp2_approx(fmaf(__uint_as_float(v[j][e + 1]), a.scale_log2, ref));
-                        sum[e & 2] += p0;
-                        sum[(e & 2) + 1] += p1;
-                        pk[(j * 32 + e) / 2] = bf162_bits(__floats2bfloat162_rn(p0, p1));
+                            for (int e = 0; e < 32; ++e)
+                                if (j * 32 + e >= left) v[j][e] = 0xFF800000u;
                     }
-                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-                tmem_st_32x32(t_s, pk);
-                tmem_st_32x32(t_s + 32, pk + 32);
-                if (__any_sync(0xFFFFFFFFu, move) && i > 0) {
+                    float mx[4];
 #pragma unroll
-                    for (int c = 0; c < D; c += 32) {
-                        uint32_t o[32];
-                        tmem_ld_32x32(t_o + s * D + c, o);
-                        tmem_ld_wait();
+                    for (int j = 0; j < 4; ++j) {
+                        mx[j] = __uint_as_float(v[j][0]);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                        tmem_st_32x32(t_o + s * D + c, o);
+                        for (int e = 1; e < 31; e += 2) mx[j] = max3(mx[j], __uint_as_float(v[j][e]), __uint_as_float(v[j][e + 1]));
+                        mx[j] = fmaxf(mx[j], __uint_as_float(v[j][31]));
                     }
+                    const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2;
+                    float f = 1.0f;
+                    const bool move = top > m + AT_SLACK;
+                    if (move) {
+                        f = exp2_approx(m - top);
+                        m = top;
+                        l *= f;
+                    }
+                    const float ref = m == -INFINITY ? 0.0f : -m;
+                    const uint64_t scale2 = pack2(a.scale_log2, a.scale_log2), ref2 = pack2(ref, ref);
+                    uint64_t sum[2] = {0, 0};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        uint32_t pk[16];
+#pragma unroll
+                        for (int e = 0; e < 32; e += 2) {
+                            float p0, p1;
+                            unpack2(fma2(pack2(__uint_as_float(v[j][e]), __uint_as_float(v[j][e + 1])), scale2, ref2), p0, p1);
+                            p0 = exp2_approx(p0);
+                            p1 = exp2_approx(p1);
+                            sum[(e >> 1) & 1] = add2(sum[(e >> 1) & 1], pack2(p0, p1));
+                            pk[e / 2] = bf162_bits(__floats2bfloat162_rn(p0, p1));
+                        }
+                        tmem_st_32x16(t_s + j * 16, pk);
+                    }
+                    float s0, s1;
+                    unpack2(add2(sum[0], sum[1]), s0, s1);
+                    l += s0 + s1;
+                    if (__any_sync(0xFFFFFFFFu, move) && i > 0) {
+#pragma unroll
+                        for (int c = 0; c < D; c += 32) {
+                            uint32_t o[32];
+                            tmem_ld_32x32(t_o + s * D + c, o);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                            tmem_st_32x32(t_o + s * D + c, o);
+                        }
+                    }
+                    tmem_st_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&p_full[s]);
                 }
-                tmem_st_wait();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&p_full[s]);
             }
             // ---- the unit's rows: into O, or as (m, l, O) into the workspace
+            const bool pair = w.pair, have0 = w.cnt[0] > 0, have1 = w.cnt[1] > 0, have = s ? have1 : have0;
             float m1 = -INFINITY, l1 = 0.0f;
-            if (!w.pair) {
+            if (!pair) {
                 if (s == 1) {
                     if (!wait_bounded(j_empty, j_ph ^ 1u, abort_flag, 74)) goto done;
                     s_ml[r] = make_float2(m, l);
@@ -400,48 +504,48 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                 }
                 j_ph ^= 1u;
             }
-            if (w.pair ? true : s == 0) {
-                const bool two = !w.pair && w.cnt[1] > 0;
-                if (w.cnt[s] > 0 && !wait_bounded(&o_full[s], o_ph[s], abort_flag, 71)) goto done;
+            if (pair || s == 0) {
+                const bool two = !pair && have1;
+                if (have && !wait_bounded(&o_full[s], o_ph[s], abort_flag, 71)) goto done;
                 if (two && !wait_bounded(&o_full[1], o_ph[1], abort_flag, 72)) goto done;
                 tc_fence_after();
+                const int tok = (pair ? s * tpt : 0) + my_tok, hq = w.h * a.G + my_head, out = w.out;
+                const bool valid = my_tok < tpt && tok < w.tokens;
                 const float mn = fmaxf(m, m1);
                 const float f0 = mn == -INFINITY ? 0.0f : exp2_approx(m - mn), f1 = mn == -INFINITY ? 0.0f : exp2_approx(m1 - mn);
                 const float lt = l * f0 + l1 * f1;
-                const bool split = w.ka > 0 || w.kb < cur.nt;
-                const bool more = cur.s < a.P || a.plan.req_group[cur.s - a.P] >= 0;     // the rows have (or may have) another source
-                const bool direct = !split && !more;
+                const bool direct = !(out & (OUT_SPLIT | OUT_TWO));
                 const float inv = !direct ? 1.0f : lt > 0.0f || lt != lt ? 1.0f / lt : 0.0f;
                 const float c0 = f0 * inv, c1 = f1 * inv;
-                const int64_t token = cur.g.t0 + tok, hq = cur.h * a.G + r % a.G, row = token * a.Hq + hq;
-                const int64_t at = split ? ((int64_t)blockIdx.x * 2 + (x > x0 ? 1 : 0)) * (2 * AT_WIDE_TILE) + tile * AT_WIDE_TILE + r : row;
-                float* part = (split ? a.wide_part : a.dense[cur.s >= a.P]) + at * D;
-                uint16_t* op = a.o + token * a.ldo + hq * D;
+                const int64_t token = w.row0 + tok, row = token * a.Hq + hq;
+                const int64_t at = out & OUT_SPLIT ? ((int64_t)blockIdx.x * 2 + (out & OUT_LATER ? 1 : 0)) * (2 * AT_WIDE_TILE) + (pair ? s * AT_WIDE_TILE : 0) + r : row;
+                float* part = (out & OUT_SPLIT ? a.wide_part : a.dense[out & OUT_OWN ? 1 : 0]) + at * D;
+                uint16_t* op = a.o + token * a.ldo + (int64_t)hq * D;
 #pragma unroll
                 for (int c = 0; c < D; c += 32) {
                     uint32_t o[32];
-                    if (w.cnt[s] > 0) {
+                    if (have) {
                         tmem_ld_32x32(t_o + s * D + c, o);
                         tmem_ld_wait();
                     }
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) o[e] = w.cnt[s] > 0 && c0 != 0.0f ? __float_as_uint(__uint_as_float(o[e]) * c0) : 0u;
+                    for (int e = 0; e < 32; ++e) o[e] = have && c0 != 0.0f ? __float_as_uint(__uint_as_float(o[e]) * c0) : 0u;
                     if (two) {
-                        uint32_t q[32];
-                        tmem_ld_32x32(t_o + D + c, q);
+                        uint32_t o1[32];
+                        tmem_ld_32x32(t_o + D + c, o1);
                         tmem_ld_wait();
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(fmaf(__uint_as_float(q[e]), c1, __uint_as_float(o[e])));
+                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(fmaf(__uint_as_float(o1[e]), c1, __uint_as_float(o[e])));
                     }
                     if (valid) {
                         if (direct) {
 #pragma unroll
                             for (int e = 0; e < 32; e += 8) {
-                                uint32_t b[4];
+                                uint32_t h[4];
 #pragma unroll
                                 for (int y = 0; y < 4; ++y)
-                                    b[y] = bf162_bits(__floats2bfloat162_rn(__uint_as_float(o[e + 2 * y]), __uint_as_float(o[e + 2 * y + 1])));
-                                *reinterpret_cast<uint4*>(op + c + e) = make_uint4(b[0], b[1], b[2], b[3]);
+                                    h[y] = bf162_bits(__floats2bfloat162_rn(__uint_as_float(o[e + 2 * y]), __uint_as_float(o[e + 2 * y + 1])));
+                                *reinterpret_cast<uint4*>(op + c + e) = make_uint4(h[0], h[1], h[2], h[3]);
                             }
                         } else {
 #pragma unroll
@@ -451,20 +555,21 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                     }
                 }
                 if (valid) {
-                    if (!direct) (split ? a.wide_ml : a.dense_ml[cur.s >= a.P])[at] = make_float2(mn, lt);
+                    if (!direct) (out & OUT_SPLIT ? a.wide_ml : a.dense_ml[out & OUT_OWN ? 1 : 0])[at] = make_float2(mn, lt);
                     else if (a.lse) a.lse[row] = lt == 0.0f ? -INFINITY : (mn + log2f(lt)) * 0.69314718055994531f;
                 }
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) {
-                    if (w.cnt[s] > 0) mbar_arrive(&o_empty[s]);
+                    if (have) mbar_arrive(&o_empty[s]);
                     if (two) mbar_arrive(&o_empty[1]);
                 }
             }
-            for (int j = 0; j < 2; ++j)
-                if (w.cnt[j] > 0) o_ph[j] ^= 1u;
-            x += w.kb - w.ka;
-            if (x < x1) cur.next_unit(a, a.plan.wide_start);
+            o_ph[0] ^= have0;
+            o_ph[1] ^= have1;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&u_empty[b]);
+            if (++b == 2) { b = 0; u_ph ^= 1u; }
         }
     }
 
@@ -488,17 +593,31 @@ done:
 
 // ---------------------------------------------------------------------------------------------- launch
 // plan -> tcgen05 kernel (if any segment can be wide) -> few-row kernel -> join, one behind the other on the stream
+template <int D, int HW>
+static cudaError_t launch_attn_few(const AttnArgs& a, cudaStream_t st) {
+    static PerDevice pd;
+    cudaError_t e = opt_in_shared_memory(pd, attn_few_kernel<D, HW>, FewCfg<D, HW>::SMEM);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(attn_few_kernel<D, HW>, dim3(a.few_ctas), dim3(AT_FEW_THREADS), FewCfg<D, HW>::SMEM, st, a);
+}
 template <int D>
 static cudaError_t launch_attn_d(const AttnWideArgs& w, bool wide, cudaStream_t st) {
-    static PerDevice pd_few, pd_wide;
+    static PerDevice pd_wide;
     const AttnArgs& a = w.a;
-    cudaError_t e = opt_in_shared_memory(pd_few, attn_few_kernel<D>, FewCfg<D>::SMEM);
-    if (e == cudaSuccess && wide) e = opt_in_shared_memory(pd_wide, attn_wide_kernel<D>, WideCfg<D>::SMEM);
+    cudaError_t e = wide ? opt_in_shared_memory(pd_wide, attn_wide_kernel<D>, WideCfg<D>::SMEM) : cudaSuccess;
     if (e != cudaSuccess) return e;
     if ((e = launch_pdl(attn_plan_kernel, dim3(1), dim3(AT_PLAN_THREADS), 0, st, a)) != cudaSuccess) return e;
     if (wide && (e = launch_pdl(attn_wide_kernel<D>, dim3(a.wide_ctas), dim3(AW_THREADS), WideCfg<D>::SMEM, st, w)) != cudaSuccess) return e;
-    if ((e = launch_pdl(attn_few_kernel<D>, dim3(a.few_ctas), dim3(AT_FEW_THREADS), FewCfg<D>::SMEM, st, a)) != cudaSuccess) return e;
-    return launch_pdl(attn_join_kernel<D>, dim3(a.T, a.Hk), dim3(AT_JOIN_THREADS), 0, st, a);
+    e = a.few_hw == 4 ? launch_attn_few<D, 4>(a, st) : a.few_hw == 2 ? launch_attn_few<D, 2>(a, st) : launch_attn_few<D, 1>(a, st);
+    if (e != cudaSuccess) return e;
+    // Where rows have two sources anyway (prefixes), few units are left to the first two kinds of blocks.
+    const int wide_split = a.P ? 2 : 8, few_split = a.P ? 1 : a.few_hw;
+    const int wide_blocks = wide ? a.wide_ctas * wide_split : 0, few_blocks = a.few_ctas * few_split;
+    const int tokens = (int)std::min<int64_t>(32, std::max<int64_t>(1, (int64_t)a.T * a.Hk / (4 * AT_MAX_SMS)));
+    const int64_t token_blocks = a.P ? ((int64_t)a.T + tokens - 1) / tokens * a.Hk : 0;
+    if (wide_blocks + few_blocks + token_blocks > 0x7FFFFFFF) return cudaErrorInvalidConfiguration;
+    return launch_pdl(attn_join_kernel<D>, dim3((unsigned)(wide_blocks + few_blocks + token_blocks)), dim3(AT_JOIN_THREADS), 0, st, a, wide_blocks,
+                      wide_split, few_blocks, few_split, tokens);
 }
 
 cudaError_t launch_attn(const AttnWideArgs& w, int D, bool wide, cudaStream_t st) {

@@ -8,10 +8,12 @@
 //
 // The work is a list of segments: every group's prefix with the rows (tokens x query heads of one key/value head)
 // of ALL its requests, then every request's own keys with its own rows.  So a prefix is read once per row tile, not
-// once per request.  A segment is cut into units (row tile, key/value head), a unit into key tiles.  All key tiles
-// of all units form one line that is cut into equal shares, one per CTA, whatever the lengths are: a CTA's share
-// begins and ends inside a unit at most twice, so it leaves at most two pieces (m, l, O) in the workspace, joined
-// by a last kernel.  The line is laid out by a one-CTA kernel from the lengths on the device; the host knows none.
+// once per request.  Where every request of a group fills row tiles by itself (prompts), nothing is gained by
+// packing their rows together, and a request's keys are one list instead: prefix, then own keys.
+// A segment is cut into units (row tile, key/value heads), a unit into key tiles.  All key tiles of all units form
+// one line that is cut into equal shares, one per CTA, whatever the lengths are: a CTA's share begins and ends
+// inside a unit at most twice, so it leaves at most two pieces (m, l, O) in the workspace, joined by a last
+// kernel.  The line is laid out by a one-CTA kernel from the lengths on the device; the host knows none.
 //
 // Segments with few rows run on the kernel of this file (16-row tiles, warp-level MMA: with 16 rows a key byte
 // meets 16 multiply-adds, so HBM bounds it whatever the tensor path), segments with many rows on the
@@ -23,17 +25,41 @@
 namespace osc {
 
 constexpr int AT_FEW_ROWS = 16;              // rows of a few-row unit
-constexpr int AT_FEW_KEYS = 64;              // keys of its tiles
 constexpr int AT_WIDE_TILE = 128;            // rows of one tcgen05 tile; a wide unit has two of them
-constexpr int AT_WIDE_KEYS = 128;
+constexpr int AT_WIDE_KEYS = 128;            // keys of its tiles
+constexpr int AT_MERGE_ROWS = 2 * AT_WIDE_TILE;  // a group whose requests all have at least this many rows has no prefix segment
 constexpr int AT_MAX_SMS = 148;
 constexpr int AT_FEW_CTAS = 2 * AT_MAX_SMS;  // most CTAs of the few-row kernel (two per SM)
+constexpr int AT_FEW_HEADS = 4;              // most key/value heads of a few-row unit
 constexpr int AT_WIDE_CTAS = AT_MAX_SMS;
+
+// A segment as the plan leaves it in the workspace (two 16-byte loads).
+struct __align__(16) Segment {
+    int t0, n;               // first row and number of tokens
+    int klen;                // keys: the prefix, or the request's own
+    int plen;                // keys of the group's prefix in front of the own keys (merged groups), else 0
+    int tiles;               // key tiles of all units of one head (of one head group on the few-row line)
+    int group;               // of a request: its group, -1: none (or one with an empty prefix)
+    int causal;              // 1: own keys, token i sees klen - n + i + 1 of them; 0: prefix, every token sees klen
+    int flags;
+};
+constexpr int SEG_WIDE = 1;  // on the tcgen05 line
+constexpr int SEG_TWO = 2;   // the rows have another source: O goes to the workspace
+
+// A unit that the end of a CTA's share cuts, told by the first CTA that meets it; the join finds its pieces by it.
+struct __align__(16) CutUnit {
+    int64_t begin;           // its first tile
+    int s, h, u, tiles;      // tiles 0: the share ends with a unit, or the unit's rows have two sources, or it was cut before
+    int pad[2];
+};
 
 struct AttnPlan {            // filled by attn_plan_kernel
     int64_t* few_start;      // [S + 1] first tile of every segment on the few-row line
     int64_t* wide_start;     // [S + 1] ... on the tcgen05 line
-    int32_t* req_group;      // [R] group of every request, -1: none (or a group whose prefix is empty)
+    Segment* seg;            // [S]
+    int32_t* mixed;          // [P]: the group has requests with few rows
+    int64_t* share;          // [3]: tiles of a share on the few-row line, on the tcgen05 line; whether any row has two sources
+    CutUnit* cut[2];         // [AT_FEW_CTAS], [AT_WIDE_CTAS]: filled by the attention kernels
 };
 
 struct AttnArgs {
@@ -52,84 +78,57 @@ struct AttnArgs {
     const int32_t* prefix_len;   // [P]
     const int32_t* ptable;       // [P][ld_ptable]
     int64_t ld_table, ld_ptable;
-    int T, Hq, Hk, G, R, P, cols, pcols, page_shift, n_pages;
+    int T, Hq, Hk, G, head_dim, R, P, cols, pcols, page_shift, n_pages;
     int wide_min_rows;       // segments with at least this many rows per head go to the tcgen05 kernel
+    int few_hw;              // heads of a few-row unit: 4, 2 or 1
     int few_ctas, wide_ctas;
     float scale_log2;        // scale * log2(e)
     AttnPlan plan;
     float* dense[2];         // [T * Hq][D]: whole-unit results where a row has two sources (0: prefix, 1: own keys)
     float2* dense_ml[2];     // (m, l)
-    float* few_part;         // [AT_FEW_CTAS][2][16][D]: first and last piece of every CTA
+    float* few_part;         // [AT_FEW_CTAS][2][few_hw][16][D]: first and last piece of every CTA
     float2* few_ml;
     float* wide_part;        // [AT_WIDE_CTAS][2][256][D]
     float2* wide_ml;
 };
 
 // ------------------------------------------------------------------------------------------------ segments
-struct Segment {
-    int t0, n;               // first row and number of tokens
-    int klen;                // keys
-    int causal;              // 1: own keys, token i sees klen - n + i + 1 of them; 0: prefix, every token sees klen
-    const int32_t* pages;
-    int npages;              // columns of the page list
-};
-
 // Lengths come from the device unchecked: rows are clamped to [0, T], keys to what the page list can name.
 __device__ __forceinline__ int attn_row(const AttnArgs& a, int r) { return min(max(a.row_off[r], 0), a.T); }
 __device__ __forceinline__ int attn_group(const AttnArgs& a, int g) { return min(max(a.group_off[g], 0), a.R); }
 __device__ __forceinline__ int attn_keys(int len, int cols, int page_shift) {
     const int64_t room = (int64_t)cols << page_shift;
-    return (int)min((int64_t)max(len, 0), min(room, (int64_t)0x40000000));
+    return (int)min((int64_t)max(len, 0), min(room, (int64_t)0x20000000));
 }
-__device__ __forceinline__ Segment attn_segment(const AttnArgs& a, int s) {
-    Segment g;
-    int t1;
-    if (s < a.P) {
-        const int r0 = attn_group(a, s), r1 = max(attn_group(a, s + 1), r0);
-        g.t0 = attn_row(a, r0);
-        t1 = attn_row(a, r1);
-        g.klen = attn_keys(a.prefix_len[s], a.pcols, a.page_shift);
-        g.causal = 0;
-        g.pages = a.ptable + (int64_t)s * a.ld_ptable;
-        g.npages = a.pcols;
-    } else {
-        const int r = s - a.P;
-        g.t0 = attn_row(a, r);
-        t1 = attn_row(a, r + 1);
-        g.klen = attn_keys(a.kv_len[r], a.cols, a.page_shift);
-        g.causal = 1;
-        g.pages = a.table + (int64_t)r * a.ld_table;
-        g.npages = a.cols;
-    }
-    g.n = max(t1 - g.t0, 0);
-    return g;
+// page list of the segment's own keys, and of the prefix in front of them
+__device__ __forceinline__ const int32_t* seg_pages(const AttnArgs& a, int s) {
+    return s < a.P ? a.ptable + (int64_t)s * a.ld_ptable : a.table + (int64_t)(s - a.P) * a.ld_table;
 }
-// keys that token i of the segment sees
+// keys that token i of the segment sees, without the prefix in front
 __device__ __forceinline__ int seg_sees(const Segment& g, int i) { return g.causal ? max(g.klen - g.n + i + 1, 0) : g.klen; }
-__device__ __forceinline__ bool seg_is_wide(const AttnArgs& a, const Segment& g) {
-    return (int64_t)g.n * a.G >= a.wide_min_rows;
-}
 
-// The two kinds of units.  Few-row: 16 consecutive (token, head) rows.  Wide: two tiles of as many whole tokens as
-// fit 128 rows.
+// The two kinds of units.  Few-row: 16 consecutive (token, head) rows of one token list, few_hw heads side by side, tiles
+// of 64 / few_hw keys.  Wide: two tiles of as many whole tokens as fit 128 rows, one head.
 struct FewUnits {
-    static constexpr int KEYS = AT_FEW_KEYS;
+    __device__ static int key_shift(const AttnArgs& a) { return a.few_hw == 4 ? 4 : a.few_hw == 2 ? 5 : 6; }
+    __device__ static int heads(const AttnArgs& a) { return a.Hk / a.few_hw; }
     __device__ static int count(const AttnArgs& a, const Segment& g) { return (int)(((int64_t)g.n * a.G + AT_FEW_ROWS - 1) / AT_FEW_ROWS); }
     __device__ static int last_token(const AttnArgs& a, const Segment& g, int u) {
         return (int)min((int64_t)(g.n - 1), ((int64_t)u * AT_FEW_ROWS + AT_FEW_ROWS - 1) / a.G);
     }
-    // own keys, all units but the last: ceil((klen - n + 1 + floor((16 u + 15) / G)) / 64)
+    // own keys, all units but the last: ceil((klen - n + 1 + floor((16 u + 15) / G)) / KEYS)
     __device__ static void line(const AttnArgs& a, const Segment& g, int64_t& A, int64_t& B, int64_t& M, int64_t& u0) {
-        const int64_t before = (int64_t)g.klen - g.n;
+        const int64_t before = (int64_t)g.klen - g.n, keys = 1 << key_shift(a);
         A = AT_FEW_ROWS;
-        B = a.G * (before + KEYS) + AT_FEW_ROWS - 1;
-        M = (int64_t)KEYS * a.G;
+        B = a.G * (before + keys) + AT_FEW_ROWS - 1;
+        M = keys * a.G;
         const int64_t need = -before * a.G - (AT_FEW_ROWS - 1);
         u0 = need > 0 ? (need + AT_FEW_ROWS - 1) / AT_FEW_ROWS : 0;
     }
 };
 struct WideUnits {
-    static constexpr int KEYS = AT_WIDE_KEYS;
+    __device__ static constexpr int key_shift(const AttnArgs&) { return 7; }
+    __device__ static int heads(const AttnArgs& a) { return a.Hk; }
     __device__ static int tokens(const AttnArgs& a) { return 2 * (AT_WIDE_TILE / a.G); }
     __device__ static int count(const AttnArgs& a, const Segment& g) { return (int)(((int64_t)g.n + tokens(a) - 1) / tokens(a)); }
     __device__ static int last_token(const AttnArgs& a, const Segment& g, int u) {
@@ -139,14 +138,19 @@ struct WideUnits {
     __device__ static void line(const AttnArgs& a, const Segment& g, int64_t& A, int64_t& B, int64_t& M, int64_t& u0) {
         const int64_t before = (int64_t)g.klen - g.n;
         A = tokens(a);
-        B = before + A + KEYS - 1;
-        M = KEYS;
+        B = before + A + AT_WIDE_KEYS - 1;
+        M = AT_WIDE_KEYS;
         u0 = before < 0 ? -before / A : 0;
     }
 };
+// tiles of the prefix in front, and of the whole unit
+template <class U>
+__device__ __forceinline__ int front_tiles(const AttnArgs& a, const Segment& g) {
+    return (g.plen + (1 << U::key_shift(a)) - 1) >> U::key_shift(a);
+}
 template <class U>
 __device__ __forceinline__ int unit_tiles(const AttnArgs& a, const Segment& g, int u) {
-    return (seg_sees(g, U::last_token(a, g, u)) + U::KEYS - 1) / U::KEYS;
+    return front_tiles<U>(a, g) + ((seg_sees(g, U::last_token(a, g, u)) + (1 << U::key_shift(a)) - 1) >> U::key_shift(a));
 }
 // sum over i < n of floor((a i + b) / m), for a, b >= 0 and m > 0, as in Euclid's algorithm
 __device__ __forceinline__ int64_t floor_sum(int64_t n, int64_t m, int64_t a, int64_t b) {
@@ -165,62 +169,67 @@ __device__ __forceinline__ int64_t floor_sum(int64_t n, int64_t m, int64_t a, in
     }
     return sum;
 }
-// key tiles of the units before unit u (u <= count) of one key/value head
+// key tiles of the units before unit u (u <= count) of one head
 template <class U>
 __device__ __forceinline__ int64_t tiles_before(const AttnArgs& a, const Segment& g, int nu, int u) {
-    if (u == 0 || g.klen == 0) return 0;
+    if (u == 0) return 0;
     if (!g.causal) return (int64_t)u * unit_tiles<U>(a, g, 0);
-    int64_t sum = 0;
+    int64_t sum = (int64_t)u * front_tiles<U>(a, g);
+    if (g.klen == 0) return sum;
     if (u == nu) {                       // the last unit may be short
-        sum = unit_tiles<U>(a, g, nu - 1);
         --u;
+        sum += (seg_sees(g, U::last_token(a, g, u)) + (1 << U::key_shift(a)) - 1) >> U::key_shift(a);
     }
-    int64_t A, B, M, u0;
-    U::line(a, g, A, B, M, u0);          // tiles(i) = floor((A i + B) / M) from unit u0 on, none before it
-    if (u > u0) sum += floor_sum(u - u0, M, A, B + A * u0);
+    if (u > 0) {
+        int64_t A, B, M, u0;
+        U::line(a, g, A, B, M, u0);      // own tiles(i) = floor((A i + B) / M) from unit u0 on, none before it
+        if (u > u0) sum += floor_sum(u - u0, M, A, B + A * u0);
+    }
     return sum;
 }
-// key tiles of all units of one key/value head
+// key tiles of all units of one head
 template <class U>
 __device__ __forceinline__ int64_t head_tiles(const AttnArgs& a, const Segment& g) {
-    if (g.n == 0 || g.klen == 0) return 0;
+    if (g.n == 0) return 0;
     const int nu = U::count(a, g);
     return tiles_before<U>(a, g, nu, nu);
 }
 
-// Shares of the line of N tiles among C CTAs: CTA c has [floor(c N / C), floor((c + 1) N / C)).  Where the line is
-// short, fewer CTAs share it, so that a share is at least MIN tiles: a piece costs its prologue and a join.
-__device__ __forceinline__ int line_ctas(int64_t N, int ctas, int min_tiles) {
-    const int64_t c = (N + min_tiles - 1) / min_tiles;
-    return (int)(c < ctas ? (c < 1 ? 1 : c) : ctas);
+// A line of N tiles is cut into shares of q = max(ceil(N / CTAs), least) tiles; CTA c has [c q, (c + 1) q).  A least
+// share, because a piece costs its prologue and a join.
+__device__ __forceinline__ int64_t share_tiles(int64_t N, int ctas, int least) { return max((N + ctas - 1) / ctas, (int64_t)least); }
+__device__ __forceinline__ int64_t div_fast(int64_t x, int64_t q) {
+    return ((x | q) >> 32) == 0 ? (int64_t)((uint32_t)x / (uint32_t)q) : x / q;
 }
-__device__ __forceinline__ int64_t share_begin(int64_t N, int C, int c) { return N * c / C; }
-// CTA whose share has tile x: the largest c with c N / C < x + 1
-__device__ __forceinline__ int share_of(int64_t N, int C, int64_t x) { return (int)(((x + 1) * C - 1) / N); }
-constexpr int AT_FEW_MIN_TILES = 1;
+// least share: 64 keys of few_hw heads
+__device__ __forceinline__ int few_min_tiles(const AttnArgs& a) { return a.few_hw; }
 constexpr int AT_WIDE_MIN_TILES = 2;
 
-// A position on a line: key tile kt of unit u of key/value head h of segment s.
+// A position on a line: key tile kt of unit u of head (group) h of segment s.
 template <class U>
 struct Cursor {
     int s, h, u, kt, nu, nt;
     Segment g;
+    // all lanes of a warp together
     __device__ void seek(const AttnArgs& a, const int64_t* start, int S, int64_t x) {
-        int lo = 0, hi = S;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (start[mid] <= x) lo = mid; else hi = mid;
+        const int lane = threadIdx.x & 31;
+        int lo = 0, len = S;
+        while (len > 1) {                // the last segment that begins at or before x, 32 candidates at a time
+            const int step = (len + 31) / 32, i = lane * step;
+            const uint32_t b = __ballot_sync(0xFFFFFFFFu, i < len && start[lo + i] <= x);
+            const int k = 31 - __clz(b);
+            lo += k * step;
+            len = min(step, len - k * step);
         }
         s = lo;
-        g = attn_segment(a, s);
+        g = a.plan.seg[s];
         nu = U::count(a, g);
-        const int64_t per_head = head_tiles<U>(a, g);
         int64_t y = x - start[s];
-        h = (int)(y / per_head);
-        y -= (int64_t)h * per_head;
+        h = (int)div_fast(y, g.tiles);
+        y -= (int64_t)h * g.tiles;
         if (!g.causal) {
             nt = unit_tiles<U>(a, g, 0);
-            u = (int)(y / nt);
+            u = (int)div_fast(y, nt);
             kt = (int)(y - (int64_t)u * nt);
         } else {
             int b = 0, e = nu;           // the last unit with at most y tiles before it
@@ -234,15 +243,14 @@ struct Cursor {
         }
     }
     // to the first tile of the next unit that has any; the caller knows that one exists
-    __device__ void next_unit(const AttnArgs& a, const int64_t* start) {
+    __device__ void next_unit(const AttnArgs& a, int line) {
         kt = 0;
         do {
             if (++u == nu) {
                 u = 0;
-                if (++h == a.Hk) {
+                if (++h == U::heads(a)) {
                     h = 0;
-                    do ++s; while (start[s + 1] == start[s]);
-                    g = attn_segment(a, s);
+                    do g = a.plan.seg[++s]; while (g.tiles == 0 || (g.flags & SEG_WIDE) != line);
                     nu = U::count(a, g);
                 }
             }
@@ -254,7 +262,15 @@ struct Cursor {
 // first tile of unit u of head h of a segment
 template <class U>
 __device__ __forceinline__ int64_t unit_begin(const AttnArgs& a, const Segment& g, int64_t seg_start, int h, int u) {
-    return seg_start + h * head_tiles<U>(a, g) + tiles_before<U>(a, g, U::count(a, g), u);
+    return seg_start + (int64_t)h * g.tiles + tiles_before<U>(a, g, U::count(a, g), u);
+}
+
+__device__ __forceinline__ void tell_cut(CutUnit& c, int64_t unit_x0, int64_t unit_x1, int64_t x0, int64_t x1, int s, int h, int u, int flags) {
+    c.begin = unit_x0;
+    c.s = s;
+    c.h = h;
+    c.u = u;
+    c.tiles = unit_x1 > x1 && unit_x0 >= x0 && !(flags & SEG_TWO) ? (int)(unit_x1 - unit_x0) : 0;
 }
 
 // ------------------------------------------------------------------------------------------------ the plan
@@ -265,26 +281,70 @@ __global__ void __launch_bounds__(AT_PLAN_THREADS) attn_plan_kernel(const AttnAr
     grid_launch_dependents();
     grid_dependency_wait();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, S = a.P + a.R;
+    // the last group that begins at or before request r, if the request is in it and its prefix is not empty
+    auto group_of = [&](int r) -> int {
+        if (a.P == 0 || a.pcols == 0) return -1;
+        int lo = 0, hi = a.P;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (attn_group(a, mid) <= r) lo = mid; else hi = mid;
+        }
+        return attn_group(a, lo) <= r && r < attn_group(a, lo + 1) && a.prefix_len[lo] > 0 ? lo : -1;
+    };
+    // groups that have requests with few rows need a prefix segment
+    if (a.P > 0) {
+        for (int g = tid; g < a.P; g += AT_PLAN_THREADS) a.plan.mixed[g] = 0;
+        __syncthreads();
+        for (int r = tid; r < a.R; r += AT_PLAN_THREADS) {
+            const int64_t rows = (int64_t)(attn_row(a, r + 1) - attn_row(a, r)) * a.G;
+            if (rows > 0 && (rows < AT_MERGE_ROWS || rows < a.wide_min_rows)) {
+                const int g = group_of(r);
+                if (g >= 0) a.plan.mixed[g] = 1;
+            }
+        }
+        __syncthreads();
+    }
     int64_t carry[2] = {0, 0};
+    bool two = false;
     for (int s0 = 0; s0 < S; s0 += AT_PLAN_THREADS) {
         const int s = s0 + tid;
         int64_t own[2] = {0, 0}, inc[2];
         if (s < S) {
-            const Segment g = attn_segment(a, s);
-            if (seg_is_wide(a, g)) own[1] = head_tiles<WideUnits>(a, g) * a.Hk;
-            else own[0] = head_tiles<FewUnits>(a, g) * a.Hk;
-            if (s >= a.P) {
-                int gr = -1;
-                if (a.P > 0 && a.pcols > 0) {
-                    int lo = 0, hi = a.P;          // the last group that begins at or before the request
-                    while (hi - lo > 1) {
-                        const int mid = (lo + hi) >> 1;
-                        if (attn_group(a, mid) <= s - a.P) lo = mid; else hi = mid;
-                    }
-                    if (attn_group(a, lo) <= s - a.P && s - a.P < attn_group(a, lo + 1) && a.prefix_len[lo] > 0) gr = lo;
+            Segment g;
+            g.plen = 0;
+            g.flags = 0;
+            g.causal = s >= a.P;
+            if (s < a.P) {
+                const int r0 = attn_group(a, s), r1 = max(attn_group(a, s + 1), r0);
+                g.t0 = attn_row(a, r0);
+                g.n = a.plan.mixed[s] ? max(attn_row(a, r1) - g.t0, 0) : 0;
+                g.klen = attn_keys(a.prefix_len[s], a.pcols, a.page_shift);
+                g.group = s;
+                g.flags = SEG_TWO;
+                if (g.klen == 0) g.n = 0;
+            } else {
+                const int r = s - a.P;
+                g.t0 = attn_row(a, r);
+                g.n = max(attn_row(a, r + 1) - g.t0, 0);
+                g.klen = attn_keys(a.kv_len[r], a.cols, a.page_shift);
+                g.group = group_of(r);
+                if (g.group >= 0) {
+                    if (a.plan.mixed[g.group]) g.flags = SEG_TWO;
+                    else g.plen = attn_keys(a.prefix_len[g.group], a.pcols, a.page_shift);
                 }
-                a.plan.req_group[s - a.P] = gr;
             }
+            if ((int64_t)g.n * a.G >= a.wide_min_rows) {
+                g.flags |= SEG_WIDE;
+                const int64_t t = head_tiles<WideUnits>(a, g);
+                g.tiles = (int)t;
+                own[1] = t * WideUnits::heads(a);
+            } else {
+                const int64_t t = head_tiles<FewUnits>(a, g);
+                g.tiles = (int)t;
+                own[0] = t * FewUnits::heads(a);
+            }
+            a.plan.seg[s] = g;
+            two |= g.n > 0 && (g.flags & SEG_TWO);
         }
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -308,9 +368,24 @@ __global__ void __launch_bounds__(AT_PLAN_THREADS) attn_plan_kernel(const AttnAr
         }
         __syncthreads();
     }
+    two = __syncthreads_or(two);
     if (tid == 0) {
+        a.plan.share[2] = two;
         a.plan.few_start[S] = carry[0];
         a.plan.wide_start[S] = carry[1];
+        a.plan.share[0] = share_tiles(carry[0], a.few_ctas, few_min_tiles(a));
+        a.plan.share[1] = share_tiles(carry[1], a.wide_ctas, AT_WIDE_MIN_TILES);
+    }
+    // Rows without any key (fewer own keys than new tokens, and no prefix) are in no unit, or in one that has other rows: 0, -inf
+    for (int r = warp; r < a.R; r += AT_PLAN_THREADS / 32) {
+        const int t0 = attn_row(a, r), n = attn_row(a, r + 1) - t0;
+        const int none = n - attn_keys(a.kv_len[r], a.cols, a.page_shift);
+        if (none <= 0 || group_of(r) >= 0) continue;
+        for (int t = t0; t < t0 + min(none, n); ++t) {
+            for (int c = lane; c < a.Hq * a.head_dim / 8; c += 32) *reinterpret_cast<uint4*>(a.o + (int64_t)t * a.ldo + c * 8) = make_uint4(0u, 0u, 0u, 0u);
+            if (a.lse)
+                for (int c = lane; c < a.Hq; c += 32) a.lse[(int64_t)t * a.Hq + c] = -INFINITY;
+        }
     }
 }
 
@@ -345,37 +420,40 @@ __device__ __forceinline__ float exp2_approx(float x) {
 constexpr float AT_SLACK = 8.0f;
 constexpr int AT_FEW_THREADS = 128;
 
-template <int D>
+template <int D, int HW>
 struct FewCfg {
     static constexpr int KV_BYTES = 16 * D * 2;                  // one warp's 16 keys (or values) of a tile
     static constexpr int SLOT_BYTES = 2 * KV_BYTES;
     static constexpr int STAGES = D == 128 ? 3 : 6;
     static constexpr int RING = 4 * STAGES * SLOT_BYTES;         // every warp has its own ring
-    static constexpr int JOIN = 2 * (16 * D * 4 + 16 * 8);       // two warps' (O, m, l) on the way to two others
-    static constexpr int SMEM = RING + JOIN;
+    static constexpr int JOIN_FLOATS = 16 * D + 32;              // one warp's O, m and l
+    static constexpr int SMEM = RING + (HW < 4 ? 2 * JOIN_FLOATS * 4 : 0);
 };
 
-// One CTA: four warps, each on its own 16 keys of every 64-key tile with its own ring of cp.async slots and its own
-// (m, l, O), so that no barrier runs inside the key loop; the four results are joined through shared memory at the
-// end of a unit.  The loads run on over the ends of units.  A page number is fetched one tile ahead of the
-// loads that need it.
-template <int D>
+// One CTA: four warps, each with its own ring of cp.async slots and its own (m, l, O), so that no barrier runs inside the
+// key loop.  With four heads to a unit a warp has a head and no barrier runs at all; the four heads of a token lie side by side
+// in the cache, so the CTA still reads whole 1 KB rows.  Where the number of heads is not a multiple of four, two or four warps
+// take different keys of a head and are joined through shared memory at the end of a unit.  (All warps on one head
+// whatever the head count cost 129 us instead of the figure in the table on 256 requests of ~512 keys: the join, three barriers a unit.)
+// The loads run on over the ends of units.  A page number is fetched one tile ahead of the loads that need it.
+template <int D, int HW>
 __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnArgs a) {
-    using C = FewCfg<D>;
+    using C = FewCfg<D, HW>;
     constexpr int NJ = D / 8;          // 8-channel column blocks of O
     constexpr int KS = D / 16;         // k steps of Q K^T
     constexpr int CHUNKS = D / 8;      // 16-byte chunks of a key
+    constexpr int KEYS = 64 / HW;      // keys of a tile
     extern __shared__ __align__(128) uint8_t at_smem[];
     grid_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     grid_dependency_wait();
     const int S = a.P + a.R;
-    const int64_t N = a.plan.few_start[S];
-    if (N == 0) return;
-    const int nc = line_ctas(N, a.few_ctas, AT_FEW_MIN_TILES);
-    if ((int)blockIdx.x >= nc) return;
-    const int64_t x0 = share_begin(N, nc, blockIdx.x), x1 = share_begin(N, nc, blockIdx.x + 1);
-    if (x0 >= x1) return;
+    const int64_t N = a.plan.few_start[S], q = a.plan.share[0];
+    const int64_t x0 = min(q * blockIdx.x, N), x1 = min(x0 + q, N);
+    if (x0 >= x1) {
+        if (threadIdx.x == 0) a.plan.cut[0][blockIdx.x].tiles = 0;
+        return;
+    }
 
     const uint32_t ring = smem_u32(at_smem) + warp * C::STAGES * C::SLOT_BYTES;
     float* join = reinterpret_cast<float*>(at_smem + C::RING);
@@ -384,21 +462,22 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
     cur.seek(a, a.plan.few_start, S, x0);
     ld = cur;
     const int page_mask = (1 << a.page_shift) - 1;
-    const int kw = warp * 16;          // first key of the warp inside a tile
+    const int hw = warp % HW;          // head of the warp inside the unit
+    const int kw = warp / HW * 16;     // first key of the warp inside a tile
     // page that holds the warp's 16 keys of the loader's tile (a page has at least 16 tokens)
     auto page_of = [&]() -> int {
-        const int key = ld.kt * AT_FEW_KEYS + kw;
+        const int key = ld.kt * KEYS + kw;
         if (key >= ld.g.klen) return -1;
-        const int c = key >> a.page_shift;
-        const int p = c < ld.g.npages ? ld.g.pages[c] : -1;
+        const int p = seg_pages(a, ld.s)[key >> a.page_shift];     // klen is within the list's columns
         return (p >= 0 && p < a.n_pages) ? p : -1;
     };
     int64_t xl = x0;                   // loader's position
     int page = page_of();
     auto load = [&](int slot) {
         if (xl < x1) {
-            const int key = ld.kt * AT_FEW_KEYS + kw;
-            const int64_t base = (int64_t)max(page, 0) * a.page_stride + (int64_t)(key & page_mask) * a.token_stride + (int64_t)ld.h * a.head_stride;
+            const int key = ld.kt * KEYS + kw;
+            const int64_t base = (int64_t)max(page, 0) * a.page_stride + (int64_t)(key & page_mask) * a.token_stride +
+                                 (int64_t)(ld.h * HW + hw) * a.head_stride;
             const uint32_t dst = ring + slot * C::SLOT_BYTES;
             const int nvalid = page >= 0 ? ld.g.klen - key : 0;   // keys past the end (and absent pages) read as zero
 #pragma unroll
@@ -410,7 +489,7 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
                 cp_async_16(d + C::KV_BYTES, a.v + off, r < nvalid);
             }
             if (++xl < x1) {
-                if (++ld.kt == ld.nt) ld.next_unit(a, a.plan.few_start);
+                if (++ld.kt == ld.nt) ld.next_unit(a, 0);
                 page = page_of();
             }
         }
@@ -426,6 +505,7 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
         // ---- a unit (or the share's part of it)
         const int row0 = cur.u * AT_FEW_ROWS;
         const int nrows = (int)min((int64_t)AT_FEW_ROWS, (int64_t)cur.g.n * a.G - row0);
+        const int head = cur.h * HW + hw;
         uint32_t qf[KS][4];
         int sees[2];
 #pragma unroll
@@ -434,7 +514,7 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
             const int tok = (row0 + r) / a.G, hd = (row0 + r) % a.G;
             const bool ok = r < nrows;
             sees[hlf] = ok ? seg_sees(cur.g, tok) : 0;
-            const uint16_t* qp = a.q + (ok ? (int64_t)(cur.g.t0 + tok) * a.ldq + (int64_t)(cur.h * a.G + hd) * D : 0) + cq * 2;
+            const uint16_t* qp = a.q + (ok ? (int64_t)(cur.g.t0 + tok) * a.ldq + (int64_t)(head * a.G + hd) * D : 0) + cq * 2;
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
                 qf[ks][hlf] = ok ? *reinterpret_cast<const uint32_t*>(qp + ks * 16) : 0u;
@@ -453,7 +533,7 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
             cp_async_wait<C::STAGES - 1>();
             __syncwarp();
             const uint32_t kb = ring + slot * C::SLOT_BYTES, vb = kb + C::KV_BYTES;
-            const int key0 = cur.kt * AT_FEW_KEYS + kw;
+            const int key0 = cur.kt * KEYS + kw;
             if (key0 < cur.g.klen) {
                 float sc[2][4] = {};
                 {
@@ -520,16 +600,16 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
             __syncwarp();              // the slot is filled again by the next load
             if (++slot == C::STAGES) slot = 0;
         }
-        // ---- join the four warps: 2, 3 -> 0, 1, then 1 -> 0
 #pragma unroll
         for (int hlf = 0; hlf < 2; ++hlf) {
             l[hlf] += __shfl_xor_sync(0xFFFFFFFFu, l[hlf], 1);
             l[hlf] += __shfl_xor_sync(0xFFFFFFFFu, l[hlf], 2);
         }
+        // ---- join the warps of a head: 2, 3 -> 0, 1, then (one head) 1 -> 0
 #pragma unroll
-        for (int step = 2; step >= 1; step >>= 1) {
+        for (int step = 2; step >= HW; step >>= 1) {
             if (warp >= step && warp < 2 * step) {
-                float* buf = join + (warp - step) * (16 * D + 32);
+                float* buf = join + (warp - step) * C::JOIN_FLOATS;
 #pragma unroll
                 for (int j = 0; j < NJ; ++j) {
                     *reinterpret_cast<float2*>(buf + r0 * D + j * 8 + cq * 2) = make_float2(o[j][0], o[j][1]);
@@ -542,7 +622,7 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
             }
             __syncthreads();
             if (warp < step) {
-                const float* buf = join + warp * (16 * D + 32);
+                const float* buf = join + warp * C::JOIN_FLOATS;
 #pragma unroll
                 for (int hlf = 0; hlf < 2; ++hlf) {
                     const int r = r0 + hlf * 8;
@@ -561,23 +641,25 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
             }
             __syncthreads();
         }
-        if (warp == 0) {
+        if (warp < HW) {
             const bool split = unit_x0 < x0 || unit_x1 > x1;
-            const bool two = cur.s < a.P || a.plan.req_group[cur.s - a.P] >= 0;   // the rows have (or may have) another source
+            const bool two = cur.g.flags & SEG_TWO;
 #pragma unroll
             for (int hlf = 0; hlf < 2; ++hlf) {
                 const int r = r0 + hlf * 8;
                 if (r >= nrows) continue;
-                const int64_t row = (int64_t)(cur.g.t0 + (row0 + r) / a.G) * a.Hq + cur.h * a.G + (row0 + r) % a.G;
+                const int64_t token = cur.g.t0 + (row0 + r) / a.G;
+                const int hq = head * a.G + (row0 + r) % a.G;
+                const int64_t row = token * a.Hq + hq;
                 if (!split && !two) {
                     const float inv = l[hlf] > 0.0f || l[hlf] != l[hlf] ? 1.0f / l[hlf] : 0.0f;
-                    uint16_t* op = a.o + (int64_t)(row / a.Hq) * a.ldo + (row % a.Hq) * D + cq * 2;
+                    uint16_t* op = a.o + token * a.ldo + (int64_t)hq * D + cq * 2;
 #pragma unroll
                     for (int j = 0; j < NJ; ++j)
                         *reinterpret_cast<uint32_t*>(op + j * 8) = bf162_bits(__floats2bfloat162_rn(o[j][2 * hlf] * inv, o[j][2 * hlf + 1] * inv));
                     if (a.lse && cq == 0) a.lse[row] = l[hlf] == 0.0f ? -INFINITY : (m[hlf] + log2f(l[hlf])) * 0.69314718055994531f;
                 } else {
-                    const int64_t at = split ? ((int64_t)blockIdx.x * 2 + (unit_x0 > x0 ? 1 : 0)) * AT_FEW_ROWS + r : row;
+                    const int64_t at = split ? (((int64_t)blockIdx.x * 2 + (unit_x0 > x0 ? 1 : 0)) * HW + hw) * AT_FEW_ROWS + r : row;
                     float* part = split ? a.few_part : a.dense[cur.s >= a.P];
                     float2* ml = split ? a.few_ml : a.dense_ml[cur.s >= a.P];
 #pragma unroll
@@ -587,108 +669,206 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
                 }
             }
         }
-        if (x < x1) cur.next_unit(a, a.plan.few_start);
+        if (x < x1) cur.next_unit(a, 0);
+        else if (threadIdx.x == 0) tell_cut(a.plan.cut[0][blockIdx.x], unit_x0, unit_x1, x0, x1, cur.s, cur.h, cur.u, cur.g.flags);
     }
     cp_async_wait<0>();
 }
 
 // ------------------------------------------------------------------------------------------------- join
-// One CTA per (token, key/value head): finds the token's request, walks over the pieces of its rows in the order of
-// the line (so the result does not depend on which CTA was first) and writes o and lse.  Rows that a unit wrote
-// itself (all their keys in one unit) are left alone; rows without any key become 0 and -inf.
-constexpr int AT_JOIN_THREADS = 128;
+// Joins the pieces of rows whose keys were not all in one unit of one share, one warp per row, in the order of the
+// lines (so the result does not depend on which CTA was first).  Three kinds of blocks, because the rows to be joined are not
+// known on the host and looking at every row costs more than the joining (262 us for 8001 tokens of prompts
+// against 1 ms of attention, when it was done that way):
+//   units that the end of a share cuts, as the attention kernels told them: blocks for every share of either line;
+//   rows with two sources (prefix and own keys): blocks over the tokens, only launched where there are prefixes.
+// Pieces are taken 32 at a time, one per lane for m and l, eight rows of O under way at a time.
+constexpr int AT_JOIN_THREADS = 256;
+constexpr int AT_JOIN_WARPS = AT_JOIN_THREADS / 32;
 
-// Adds the pieces of one row from one segment.  `which` 0: prefix, 1: own keys.
-template <int D, class U, class F>
-__device__ __forceinline__ void join_pieces(const AttnArgs& a, const Segment& g, int64_t N, int ctas, int min_tiles, int64_t seg_start,
-                                            int h, int u, int row_in_unit, int unit_rows, const float* part, const float2* ml,
-                                            const float* dense, const float2* dense_ml, int64_t dense_row, F add) {
-    const int nt = unit_tiles<U>(a, g, u);
-    if (nt == 0) return;
-    const int C = line_ctas(N, ctas, min_tiles);
-    const int64_t b = unit_begin<U>(a, g, seg_start, h, u), e = b + nt;
-    const int c0 = share_of(N, C, b), c1 = share_of(N, C, e - 1);
-    if (c0 == c1) { add(dense + dense_row * D, dense_ml[dense_row]); return; }
-    for (int c = c0; c <= c1; ++c) {
-        const int64_t at = ((int64_t)c * 2 + (b > share_begin(N, C, c) ? 1 : 0)) * unit_rows + row_in_unit;
-        add(part + at * D, ml[at]);
-    }
+struct PieceList {           // pieces of one row from one segment
+    int count;               // 0: none; 1: the whole unit, in the dense buffer
+    int cta, which;          // share of the first piece, and whether it is that CTA's last piece
+    int stride;              // rows between two slots
+    int64_t row;             // row in a slot, or in the dense buffer
+    const float* part;
+    const float2* ml;
+    __device__ int64_t at(int i) const { return count == 1 ? row : ((int64_t)(cta + i) * 2 + (i ? 0 : which)) * stride + row; }
+};
+__device__ __forceinline__ void list_pieces(PieceList& p, int64_t begin, int tiles, int64_t q) {
+    const int64_t c0 = div_fast(begin, q), c1 = div_fast(begin + tiles - 1, q);
+    p.cta = (int)c0;
+    p.which = begin > c0 * q;
+    p.count = (int)(c1 - c0) + 1;
 }
 
 template <int D>
-__global__ void __launch_bounds__(AT_JOIN_THREADS) attn_join_kernel(const AttnArgs a) {
+__device__ __forceinline__ void join_row(const AttnArgs& a, const PieceList& p0, const PieceList& p1, int64_t token, int hq) {
     constexpr int V = D / 32;          // channels per lane
-    __shared__ int s_req;
+    const int lane = threadIdx.x & 31;
+    float m = -INFINITY, l = 0.0f, o[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) o[j] = 0.0f;
+    const int n = p0.count + p1.count;
+    for (int i0 = 0; i0 < n; i0 += 32) {
+        const int i = i0 + lane;
+        float2 ml = make_float2(-INFINITY, 0.0f);
+        const float* src = nullptr;
+        if (i < n) {
+            const bool first = i < p0.count;
+            const int64_t at = first ? p0.at(i) : p1.at(i - p0.count);
+            ml = (first ? p0.ml : p1.ml)[at];
+            src = (first ? p0.part : p1.part) + at * D;
+        }
+        float mx = ml.x;
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, d));
+        mx = fmaxf(mx, m);
+        const float f0 = mx == -INFINITY ? 0.0f : exp2_approx(m - mx);
+        const float w = mx == -INFINITY ? 0.0f : exp2_approx(ml.x - mx);
+        float lw = ml.y * w;
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) lw += __shfl_xor_sync(0xFFFFFFFFu, lw, d);
+        m = mx;
+        l = l * f0 + lw;
+#pragma unroll
+        for (int j = 0; j < V; ++j) o[j] *= f0;
+        const int k = min(32, n - i0);
+        for (int b = 0; b < k; b += 8) {
+            float v[8][V], wb[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int from = min(b + j, k - 1);
+                const float* sp = reinterpret_cast<const float*>(__shfl_sync(0xFFFFFFFFu, (unsigned long long)src, from));
+                wb[j] = __shfl_sync(0xFFFFFFFFu, w, from);
+                if (b + j >= k) wb[j] = 0.0f;
+                if (V == 4) {
+                    const float4 x = *reinterpret_cast<const float4*>(sp + lane * 4);
+                    v[j][0] = x.x; v[j][1] = x.y; v[j][V - 2] = x.z; v[j][V - 1] = x.w;
+                } else {
+                    const float2 x = *reinterpret_cast<const float2*>(sp + lane * 2);
+                    v[j][0] = x.x; v[j][1] = x.y;
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (wb[j] != 0.0f)     // a piece without weight may hold anything
+#pragma unroll
+                    for (int y = 0; y < V; ++y) o[y] = fmaf(v[j][y], wb[j], o[y]);
+        }
+    }
+    const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+    uint16_t* op = a.o + token * a.ldo + (int64_t)hq * D + lane * V;
+    if (V == 4) {
+        *reinterpret_cast<uint2*>(op) = make_uint2(bf162_bits(__floats2bfloat162_rn(o[0] * inv, o[1] * inv)),
+                                                   bf162_bits(__floats2bfloat162_rn(o[V - 2] * inv, o[V - 1] * inv)));
+    } else {
+        *reinterpret_cast<uint32_t*>(op) = bf162_bits(__floats2bfloat162_rn(o[0] * inv, o[1] * inv));
+    }
+    if (a.lse && lane == 0) a.lse[token * a.Hq + hq] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+}
+
+template <int D>
+__global__ void __launch_bounds__(AT_JOIN_THREADS, 3) attn_join_kernel(const AttnArgs a, int wide_blocks, int wide_split, int few_blocks, int few_split,
+                                                                    int tokens) {
     grid_launch_dependents();
     grid_dependency_wait();
-    const int t = blockIdx.x, h = blockIdx.y, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    if (tid == 0) s_req = -1;
-    __syncthreads();
-    for (int r = tid; r < a.R; r += AT_JOIN_THREADS)
-        if (attn_row(a, r) <= t && t < attn_row(a, r + 1)) s_req = r;
-    __syncthreads();
-    const int r = s_req;
-    if (r < 0) return;                 // behind the last request: left as it is
-    const int S = a.P + a.R;
-    const int grp = a.plan.req_group[r];
-    const int64_t nf = a.plan.few_start[S], nw = a.plan.wide_start[S];
-    const Segment own = attn_segment(a, a.P + r);
-    Segment pre = own;
-    if (grp >= 0) pre = attn_segment(a, grp);
-    for (int g = warp; g < a.G; g += AT_JOIN_THREADS / 32) {
-        const int hq = h * a.G + g;
-        const int64_t row = (int64_t)t * a.Hq + hq;
-        float m = -INFINITY, l = 0.0f, o[V];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    int b = blockIdx.x;
+    PieceList none, p;
+    none.count = 0;
+    if (b < wide_blocks) {
+        const CutUnit cut = a.plan.cut[1][b / wide_split];
+        if (cut.tiles == 0) return;
+        const Segment sg = a.plan.seg[cut.s];
+        list_pieces(p, cut.begin, cut.tiles, a.plan.share[1]);
+        p.stride = 2 * AT_WIDE_TILE;
+        p.part = a.wide_part;
+        p.ml = a.wide_ml;
+        const int tpt = AT_WIDE_TILE / a.G, rows = 2 * AT_WIDE_TILE / wide_split, part = b % wide_split;
+        for (int i = part * rows + warp; i < (part + 1) * rows; i += AT_JOIN_WARPS) {
+            const int r = i % AT_WIDE_TILE, tok = (cut.u * 2 + i / AT_WIDE_TILE) * tpt + r / a.G;
+            if (r >= tpt * a.G || tok >= sg.n) continue;
+            p.row = i;
+            join_row<D>(a, none, p, sg.t0 + tok, cut.h * a.G + r % a.G);
+        }
+        return;
+    }
+    b -= wide_blocks;
+    if (b < few_blocks) {
+        const CutUnit cut = a.plan.cut[0][b / few_split];
+        if (cut.tiles == 0) return;
+        const Segment sg = a.plan.seg[cut.s];
+        list_pieces(p, cut.begin, cut.tiles, a.plan.share[0]);
+        p.stride = a.few_hw * AT_FEW_ROWS;
+        p.part = a.few_part;
+        p.ml = a.few_ml;
+        const int rows = p.stride / few_split, part = b % few_split;
+        for (int i = part * rows + warp; i < (part + 1) * rows; i += AT_JOIN_WARPS) {
+            const int fr = cut.u * AT_FEW_ROWS + i % AT_FEW_ROWS, tok = fr / a.G;
+            if (tok >= sg.n) continue;
+            p.row = i;
+            join_row<D>(a, none, p, sg.t0 + tok, (cut.h * a.few_hw + i / AT_FEW_ROWS) * a.G + fr % a.G);
+        }
+        return;
+    }
+    b -= few_blocks;
+    // `tokens` tokens of one head: the rows that have a prefix and own keys
+    if (a.plan.share[2] == 0) return;
+    const int h = b % a.Hk;
+    const int64_t nf = a.plan.share[0], nw = a.plan.share[1];
+    for (int i = warp; i < tokens * a.G; i += AT_JOIN_WARPS) {
+        const int64_t t64 = (int64_t)(b / a.Hk) * tokens + i / a.G;
+        if (t64 >= a.T) return;
+        const int t = (int)t64, g = i % a.G;
+        int r = 0, len = a.R;            // the last request that begins at or before t
+        while (len > 1) {
+            const int step = (len + 31) / 32, j = lane * step;
+            const uint32_t f = __ballot_sync(0xFFFFFFFFu, j < len && attn_row(a, r + j) <= t);
+            const int k = max(31 - __clz(f), 0);
+            r += k * step;
+            len = min(step, len - k * step);
+        }
+        const Segment own = a.plan.seg[a.P + r];
+        if (t < own.t0 || t >= own.t0 + own.n || !(own.flags & SEG_TWO)) continue;
+        const Segment pre = a.plan.seg[own.group];
+        {
+            const int hq = h * a.G + g;
+            PieceList list[2];
 #pragma unroll
-        for (int j = 0; j < V; ++j) o[j] = 0.0f;
-        auto add = [&](const float* part, float2 ml) {
-            const float mn = fmaxf(m, ml.x);
-            if (mn == -INFINITY) return;
-            const float f0 = exp2_approx(m - mn), f1 = exp2_approx(ml.x - mn);
-            m = mn;
-            l = l * f0 + ml.y * f1;
-#pragma unroll
-            for (int j = 0; j < V; ++j) o[j] = o[j] * f0 + part[lane * V + j] * f1;
-        };
-        bool direct = false;
-        for (int which = grp >= 0 ? 0 : 1; which < 2; ++which) {
-            const Segment& sg = which ? own : pre;
-            const int s = which ? a.P + r : grp;
-            const int tok = t - sg.t0;
-            if (sg.klen == 0 || tok < 0 || tok >= sg.n) continue;
-            if (seg_is_wide(a, sg)) {
-                const int tpt = AT_WIDE_TILE / a.G, u = tok / (2 * tpt), in = tok % (2 * tpt);
-                if (which && grp < 0) {
+            for (int which = 0; which < 2; ++which) {
+                const Segment& sg = which ? own : pre;
+                const int s = which ? a.P + r : own.group, tok = t - sg.t0;
+                PieceList& pl = list[which];
+                pl.count = 0;
+                if (tok < 0 || tok >= sg.n) continue;
+                if (sg.flags & SEG_WIDE) {
+                    const int tpt = AT_WIDE_TILE / a.G, u = tok / (2 * tpt), in = tok % (2 * tpt);
                     const int nt = unit_tiles<WideUnits>(a, sg, u);
-                    const int C = line_ctas(nw, a.wide_ctas, AT_WIDE_MIN_TILES);
-                    const int64_t b = nt ? unit_begin<WideUnits>(a, sg, a.plan.wide_start[s], h, u) : 0;
-                    if (nt && share_of(nw, C, b) == share_of(nw, C, b + nt - 1)) { direct = true; continue; }
-                }
-                const int rin = (in / tpt) * AT_WIDE_TILE + (in % tpt) * a.G + g;
-                join_pieces<D, WideUnits>(a, sg, nw, a.wide_ctas, AT_WIDE_MIN_TILES, a.plan.wide_start[s], h, u, rin, 2 * AT_WIDE_TILE,
-                                          a.wide_part, a.wide_ml, a.dense[which], a.dense_ml[which], row, add);
-            } else {
-                const int fr = tok * a.G + g, u = fr / AT_FEW_ROWS;
-                if (which && grp < 0) {
+                    if (nt == 0) continue;
+                    list_pieces(pl, unit_begin<WideUnits>(a, sg, a.plan.wide_start[s], h, u), nt, nw);
+                    pl.stride = 2 * AT_WIDE_TILE;
+                    pl.row = (in / tpt) * AT_WIDE_TILE + (in % tpt) * a.G + g;
+                    pl.part = a.wide_part;
+                    pl.ml = a.wide_ml;
+                } else {
+                    const int fr = tok * a.G + g, u = fr / AT_FEW_ROWS;
                     const int nt = unit_tiles<FewUnits>(a, sg, u);
-                    const int C = line_ctas(nf, a.few_ctas, AT_FEW_MIN_TILES);
-                    const int64_t b = nt ? unit_begin<FewUnits>(a, sg, a.plan.few_start[s], h, u) : 0;
-                    if (nt && share_of(nf, C, b) == share_of(nf, C, b + nt - 1)) { direct = true; continue; }
+                    if (nt == 0) continue;
+                    list_pieces(pl, unit_begin<FewUnits>(a, sg, a.plan.few_start[s], h / a.few_hw, u), nt, nf);
+                    pl.stride = a.few_hw * AT_FEW_ROWS;
+                    pl.row = (h % a.few_hw) * AT_FEW_ROWS + fr % AT_FEW_ROWS;
+                    pl.part = a.few_part;
+                    pl.ml = a.few_ml;
                 }
-                join_pieces<D, FewUnits>(a, sg, nf, a.few_ctas, AT_FEW_MIN_TILES, a.plan.few_start[s], h, u, fr % AT_FEW_ROWS, AT_FEW_ROWS,
-                                         a.few_part, a.few_ml, a.dense[which], a.dense_ml[which], row, add);
+                if (pl.count == 1) {
+                    pl.row = (int64_t)t * a.Hq + hq;
+                    pl.part = a.dense[which];
+                    pl.ml = a.dense_ml[which];
+                }
             }
+            join_row<D>(a, list[0], list[1], t, hq);
         }
-        if (direct) continue;
-        const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-        uint16_t* op = a.o + (int64_t)t * a.ldo + (int64_t)hq * D + lane * V;
-        if (V == 4) {
-            *reinterpret_cast<uint2*>(op) = make_uint2(bf162_bits(__floats2bfloat162_rn(o[0] * inv, o[1] * inv)),
-                                                       bf162_bits(__floats2bfloat162_rn(o[V - 2] * inv, o[V - 1] * inv)));
-        } else {
-            *reinterpret_cast<uint32_t*>(op) = bf162_bits(__floats2bfloat162_rn(o[0] * inv, o[1] * inv));
-        }
-        if (a.lse && lane == 0) a.lse[row] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
     }
 }
 
