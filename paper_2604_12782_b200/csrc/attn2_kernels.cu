@@ -201,8 +201,8 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, *tmem_slot, 0);
-    grid_launch_dependents();
     grid_dependency_wait();
+    grid_launch_dependents();   // not before: the few-row kernel counts on the plan being there when it begins
     const int tpt = AT_WIDE_TILE / a.G;
 
     if (warp >= 8) {
@@ -213,7 +213,8 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
             const int64_t N = a.plan.wide_start[S], q = a.plan.share[1];
             const int64_t x0 = min(q * blockIdx.x, N), x1 = min(x0 + q, N);
             Cursor<WideUnits> cur;
-            if (x0 < x1) cur.seek(a, a.plan.wide_start, S, x0);
+            const LineSource<false> src = {a.plan.seg, a.plan.wide_start};
+            if (x0 < x1) cur.seek(a, src, S, x0);
             else if (lane == 0) a.plan.cut[1][blockIdx.x].tiles = 0;
             int b = 0;
             uint32_t ph = 0;
@@ -251,9 +252,9 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                 if (++b == 2) { b = 0; ph ^= 1u; }
                 if (w.n == 0) break;
                 if (x + w.n == x1 && lane == 0)
-                    tell_cut(a.plan.cut[1][blockIdx.x], x - w.ka, x - w.ka + cur.nt, x0, x1, cur.s, cur.h, cur.u, cur.g.flags);
+                    tell_cut(a.plan.cut[1] + blockIdx.x, x - w.ka, x - w.ka + cur.nt, x0, x1, q, cur.h, cur.u, cur.g);
                 x += w.n;
-                if (x < x1) cur.next_unit(a, SEG_WIDE);
+                if (x < x1) cur.next_unit(a, src, SEG_WIDE);
             }
         } else if (warp == 8) {
             // --------------------------------------------------------------------------------------- TMA
@@ -593,12 +594,13 @@ done:
 
 // ---------------------------------------------------------------------------------------------- launch
 // plan -> tcgen05 kernel (if any segment can be wide) -> few-row kernel -> join, one behind the other on the stream
-template <int D, int HW>
-static cudaError_t launch_attn_few(const AttnArgs& a, cudaStream_t st) {
+template <int D, int HW, bool SELF>
+static cudaError_t launch_attn_few(const AttnArgs& a, bool early, cudaStream_t st) {
     static PerDevice pd;
-    cudaError_t e = opt_in_shared_memory(pd, attn_few_kernel<D, HW>, FewCfg<D, HW>::SMEM);
+    constexpr int smem = FewCfg<D, HW, SELF>::SMEM;
+    cudaError_t e = opt_in_shared_memory(pd, attn_few_kernel<D, HW, SELF>, smem);
     if (e != cudaSuccess) return e;
-    return launch_pdl(attn_few_kernel<D, HW>, dim3(a.few_ctas), dim3(AT_FEW_THREADS), FewCfg<D, HW>::SMEM, st, a);
+    return launch_pdl(attn_few_kernel<D, HW, SELF>, dim3(a.few_ctas), dim3(AT_FEW_THREADS), smem, st, a, early);
 }
 template <int D>
 static cudaError_t launch_attn_d(const AttnWideArgs& w, bool wide, cudaStream_t st) {
@@ -606,12 +608,17 @@ static cudaError_t launch_attn_d(const AttnWideArgs& w, bool wide, cudaStream_t 
     const AttnArgs& a = w.a;
     cudaError_t e = wide ? opt_in_shared_memory(pd_wide, attn_wide_kernel<D>, WideCfg<D>::SMEM) : cudaSuccess;
     if (e != cudaSuccess) return e;
-    if ((e = launch_pdl(attn_plan_kernel, dim3(1), dim3(AT_PLAN_THREADS), 0, st, a)) != cudaSuccess) return e;
-    if (wide && (e = launch_pdl(attn_wide_kernel<D>, dim3(a.wide_ctas), dim3(AW_THREADS), WideCfg<D>::SMEM, st, w)) != cudaSuccess) return e;
-    e = a.few_hw == 4 ? launch_attn_few<D, 4>(a, st) : a.few_hw == 2 ? launch_attn_few<D, 2>(a, st) : launch_attn_few<D, 1>(a, st);
-    if (e != cudaSuccess) return e;
-    // Where rows have two sources anyway (prefixes), few units are left to the first two kinds of blocks.
-    const int wide_split = a.P ? 2 : 8, few_split = a.P ? 1 : a.few_hw;
+    if (!wide && a.P == 0 && a.R <= FEW_SELF && a.few_hw == 4) {
+        if ((e = launch_attn_few<D, 4, true>(a, false, st)) != cudaSuccess) return e;
+    } else {
+        const int threads = std::min(1024, std::max(128, (a.P + a.R + 127) / 128 * 128));
+        if ((e = launch_pdl(attn_plan_kernel, dim3(1), dim3(threads), 0, st, a)) != cudaSuccess) return e;
+        if (wide && (e = launch_pdl(attn_wide_kernel<D>, dim3(a.wide_ctas), dim3(AW_THREADS), WideCfg<D>::SMEM, st, w)) != cudaSuccess) return e;
+        e = a.few_hw == 4 ? launch_attn_few<D, 4, false>(a, wide, st)
+            : a.few_hw == 2 ? launch_attn_few<D, 2, false>(a, wide, st) : launch_attn_few<D, 1, false>(a, wide, st);
+        if (e != cudaSuccess) return e;
+    }
+    const int wide_split = 8, few_split = a.few_hw;
     const int wide_blocks = wide ? a.wide_ctas * wide_split : 0, few_blocks = a.few_ctas * few_split;
     const int tokens = (int)std::min<int64_t>(32, std::max<int64_t>(1, (int64_t)a.T * a.Hk / (4 * AT_MAX_SMS)));
     const int64_t token_blocks = a.P ? ((int64_t)a.T + tokens - 1) / tokens * a.Hk : 0;

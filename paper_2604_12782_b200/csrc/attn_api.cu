@@ -41,7 +41,7 @@ static osc_status encode_heads(CUtensorMap* tm, const void* base, int rank, cons
 }
 
 struct AttnLayout {
-    size_t few_start, wide_start, share, cut[2], seg, mixed, dense[2], dense_ml[2], few_part, few_ml, wide_part, wide_ml, total;
+    size_t few_start, wide_start, share, cut[2], seg, tok_req, dense[2], dense_ml[2], few_part, few_ml, wide_part, wide_ml, total;
 };
 static AttnLayout attn_layout(int T, int n_q, int D, int R, int P) {
     AttnLayout l;
@@ -54,7 +54,7 @@ static AttnLayout attn_layout(int T, int n_q, int D, int R, int P) {
     l.cut[0] = take((size_t)AT_FEW_CTAS * sizeof(CutUnit));
     l.cut[1] = take((size_t)AT_WIDE_CTAS * sizeof(CutUnit));
     l.seg = take((S - 1) * sizeof(Segment));
-    l.mixed = take((size_t)P * 4);
+    l.tok_req = take(P ? (size_t)T * 4 : 0);
     for (int i = 0; i < 2; ++i) {   // rows with two sources exist only where there are prefixes
         l.dense[i] = take(P ? rows * D * 4 : 0);
         l.dense_ml[i] = take(P ? rows * 8 : 0);
@@ -212,7 +212,7 @@ osc_status osc_paged_attention(const void* Q, int T, int64_t ldq, int n_q, const
     a.plan.wide_start = reinterpret_cast<int64_t*>(ws + l.wide_start);
     a.plan.share = reinterpret_cast<int64_t*>(ws + l.share);
     a.plan.seg = reinterpret_cast<Segment*>(ws + l.seg);
-    a.plan.mixed = reinterpret_cast<int32_t*>(ws + l.mixed);
+    a.plan.tok_req = reinterpret_cast<int32_t*>(ws + l.tok_req);
     for (int i = 0; i < 2; ++i) {
         a.plan.cut[i] = reinterpret_cast<CutUnit*>(ws + l.cut[i]);
         a.dense[i] = reinterpret_cast<float*>(ws + l.dense[i]);

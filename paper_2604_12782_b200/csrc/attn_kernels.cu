@@ -44,20 +44,22 @@ struct __align__(16) Segment {
     int flags;
 };
 constexpr int SEG_WIDE = 1;  // on the tcgen05 line
-constexpr int SEG_TWO = 2;   // the rows have another source: O goes to the workspace
+constexpr int SEG_TWO = 2;   // the rows have another source: O goes to the workspace, and the join looks at every row
 
 // A unit that the end of a CTA's share cuts, told by the first CTA that meets it; the join finds its pieces by it.
 struct __align__(16) CutUnit {
-    int64_t begin;           // its first tile
-    int s, h, u, tiles;      // tiles 0: the share ends with a unit, or the unit's rows have two sources, or it was cut before
-    int pad[2];
+    int64_t begin, share;    // its first tile, and the tiles of a share
+    int tiles;               // 0: the share ends with a unit, or the unit's rows have two sources, or it was cut before
+    int h, u;                // head (group) and row unit
+    int t0, n;               // rows of the segment
+    int pad[3];
 };
 
 struct AttnPlan {            // filled by attn_plan_kernel
     int64_t* few_start;      // [S + 1] first tile of every segment on the few-row line
     int64_t* wide_start;     // [S + 1] ... on the tcgen05 line
     Segment* seg;            // [S]
-    int32_t* mixed;          // [P]: the group has requests with few rows
+    int32_t* tok_req;        // [T], where there are prefixes: the request of every token whose rows have two sources, else -1
     int64_t* share;          // [3]: tiles of a share on the few-row line, on the tcgen05 line; whether any row has two sources
     CutUnit* cut[2];         // [AT_FEW_CTAS], [AT_WIDE_CTAS]: filled by the attention kernels
 };
@@ -93,6 +95,9 @@ struct AttnArgs {
 };
 
 // ------------------------------------------------------------------------------------------------ segments
+// What the plan wrote is read past L1: the few-row kernel may begin before the kernel behind the plan has ended.
+__device__ __forceinline__ int64_t load_plan(const int64_t* p) { return __ldcg(reinterpret_cast<const long long*>(p)); }
+
 // Lengths come from the device unchecked: rows are clamped to [0, T], keys to what the page list can name.
 __device__ __forceinline__ int attn_row(const AttnArgs& a, int r) { return min(max(a.row_off[r], 0), a.T); }
 __device__ __forceinline__ int attn_group(const AttnArgs& a, int g) { return min(max(a.group_off[g], 0), a.R); }
@@ -205,26 +210,42 @@ __device__ __forceinline__ int64_t div_fast(int64_t x, int64_t q) {
 __device__ __forceinline__ int few_min_tiles(const AttnArgs& a) { return a.few_hw; }
 constexpr int AT_WIDE_MIN_TILES = 2;
 
+// Where a cursor finds segments and their first tiles: what the plan kernel left in the workspace, or (SELF) shared memory.
+template <bool SELF>
+struct LineSource {
+    const Segment* seg;
+    const int64_t* start;
+    __device__ __forceinline__ int64_t begin(int s) const { return SELF ? start[s] : load_plan(start + s); }
+    __device__ __forceinline__ Segment load(int s) const {
+        if (SELF) return seg[s];
+        Segment g;
+        const int4* src = reinterpret_cast<const int4*>(seg + s);
+        reinterpret_cast<int4*>(&g)[0] = __ldcg(src);
+        reinterpret_cast<int4*>(&g)[1] = __ldcg(src + 1);
+        return g;
+    }
+};
+
 // A position on a line: key tile kt of unit u of head (group) h of segment s.
-template <class U>
+template <class U, bool SELF = false>
 struct Cursor {
     int s, h, u, kt, nu, nt;
     Segment g;
     // all lanes of a warp together
-    __device__ void seek(const AttnArgs& a, const int64_t* start, int S, int64_t x) {
+    __device__ void seek(const AttnArgs& a, const LineSource<SELF>& src, int S, int64_t x) {
         const int lane = threadIdx.x & 31;
         int lo = 0, len = S;
         while (len > 1) {                // the last segment that begins at or before x, 32 candidates at a time
             const int step = (len + 31) / 32, i = lane * step;
-            const uint32_t b = __ballot_sync(0xFFFFFFFFu, i < len && start[lo + i] <= x);
+            const uint32_t b = __ballot_sync(0xFFFFFFFFu, i < len && src.begin(lo + i) <= x);
             const int k = 31 - __clz(b);
             lo += k * step;
             len = min(step, len - k * step);
         }
         s = lo;
-        g = a.plan.seg[s];
+        g = src.load(s);
         nu = U::count(a, g);
-        int64_t y = x - start[s];
+        int64_t y = x - src.begin(s);
         h = (int)div_fast(y, g.tiles);
         y -= (int64_t)h * g.tiles;
         if (!g.causal) {
@@ -243,14 +264,14 @@ struct Cursor {
         }
     }
     // to the first tile of the next unit that has any; the caller knows that one exists
-    __device__ void next_unit(const AttnArgs& a, int line) {
+    __device__ void next_unit(const AttnArgs& a, const LineSource<SELF>& src, int line) {
         kt = 0;
         do {
             if (++u == nu) {
                 u = 0;
                 if (++h == U::heads(a)) {
                     h = 0;
-                    do g = a.plan.seg[++s]; while (g.tiles == 0 || (g.flags & SEG_WIDE) != line);
+                    do g = src.load(++s); while (g.tiles == 0 || (g.flags & SEG_WIDE) != line);
                     nu = U::count(a, g);
                 }
             }
@@ -265,63 +286,117 @@ __device__ __forceinline__ int64_t unit_begin(const AttnArgs& a, const Segment& 
     return seg_start + (int64_t)h * g.tiles + tiles_before<U>(a, g, U::count(a, g), u);
 }
 
-__device__ __forceinline__ void tell_cut(CutUnit& c, int64_t unit_x0, int64_t unit_x1, int64_t x0, int64_t x1, int s, int h, int u, int flags) {
-    c.begin = unit_x0;
-    c.s = s;
-    c.h = h;
-    c.u = u;
-    c.tiles = unit_x1 > x1 && unit_x0 >= x0 && !(flags & SEG_TWO) ? (int)(unit_x1 - unit_x0) : 0;
+__device__ __forceinline__ void tell_cut(CutUnit* c, int64_t unit_x0, int64_t unit_x1, int64_t x0, int64_t x1, int64_t q, int h, int u,
+                                         const Segment& g) {
+    c->begin = unit_x0;
+    c->share = q;
+    c->h = h;
+    c->u = u;
+    c->t0 = g.t0;
+    c->n = g.n;
+    c->tiles = unit_x1 > x1 && unit_x0 >= x0 && !(g.flags & SEG_TWO) ? (int)(unit_x1 - unit_x0) : 0;
 }
 
 // ------------------------------------------------------------------------------------------------ the plan
-constexpr int AT_PLAN_THREADS = 1024;
+// Inclusive sum over the block of one pair of values per thread; s_warp: [2][32] in shared memory.  Returns the block's totals in `total`.
+__device__ __forceinline__ void block_scan2(int64_t (&v)[2], int64_t (&total)[2], int64_t (*s_warp)[32], int warps) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t up = __shfl_up_sync(0xFFFFFFFFu, v[j], o);
+            if (lane >= o) v[j] += up;
+        }
+        if (lane == 31) s_warp[j][warp] = v[j];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        int64_t x = lane < warps ? s_warp[j][lane] : 0, inc = x;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t up = __shfl_up_sync(0xFFFFFFFFu, inc, o);
+            if (lane >= o) inc += up;
+        }
+        total[j] = __shfl_sync(0xFFFFFFFFu, inc, 31);
+        v[j] += __shfl_sync(0xFFFFFFFFu, inc - x, warp);
+    }
+    __syncthreads();
+}
 
-__global__ void __launch_bounds__(AT_PLAN_THREADS) attn_plan_kernel(const AttnArgs a) {
-    __shared__ int64_t s_warp[2][AT_PLAN_THREADS / 32];
+// Rows without any key (fewer own keys than new tokens, and no prefix) are in no unit, or in one that has other rows: 0, -inf.
+// One warp, for tokens [t0, t0 + n).
+__device__ __forceinline__ void clear_rows(const AttnArgs& a, int t0, int n) {
+    const int lane = threadIdx.x & 31;
+    for (int t = t0; t < t0 + n; ++t) {
+        for (int c = lane; c < a.Hq * a.head_dim / 8; c += 32) *reinterpret_cast<uint4*>(a.o + (int64_t)t * a.ldo + c * 8) = make_uint4(0u, 0u, 0u, 0u);
+        if (a.lse)
+            for (int c = lane; c < a.Hq; c += 32) a.lse[(int64_t)t * a.Hq + c] = -INFINITY;
+    }
+}
+
+// One CTA of up to 1024 threads, a thread per segment; lengths are read once, groups are searched in shared memory.
+constexpr int AT_PLAN_GROUPS = 512;    // groups of a step that fit there; more are looked up in global memory
+
+__global__ void __launch_bounds__(1024) attn_plan_kernel(const AttnArgs a) {
+    __shared__ int64_t s_warp[2][32];
+    __shared__ int s_off[AT_PLAN_GROUPS + 1], s_len[AT_PLAN_GROUPS], s_mixed[AT_PLAN_GROUPS];
     grid_launch_dependents();
     grid_dependency_wait();
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, S = a.P + a.R;
+    const int tid = threadIdx.x, threads = blockDim.x, S = a.P + a.R;
+    const bool in_smem = a.P <= AT_PLAN_GROUPS;
+    auto off = [&](int g) { return in_smem ? s_off[g] : attn_group(a, g); };
+    auto len = [&](int g) { return in_smem ? s_len[g] : attn_keys(a.prefix_len[g], a.pcols, a.page_shift); };
     // the last group that begins at or before request r, if the request is in it and its prefix is not empty
     auto group_of = [&](int r) -> int {
-        if (a.P == 0 || a.pcols == 0) return -1;
+        if (a.P == 0) return -1;
         int lo = 0, hi = a.P;
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
-            if (attn_group(a, mid) <= r) lo = mid; else hi = mid;
+            if (off(mid) <= r) lo = mid; else hi = mid;
         }
-        return attn_group(a, lo) <= r && r < attn_group(a, lo + 1) && a.prefix_len[lo] > 0 ? lo : -1;
+        return off(lo) <= r && r < off(lo + 1) && len(lo) > 0 ? lo : -1;
     };
-    // groups that have requests with few rows need a prefix segment
     if (a.P > 0) {
-        for (int g = tid; g < a.P; g += AT_PLAN_THREADS) a.plan.mixed[g] = 0;
-        __syncthreads();
-        for (int r = tid; r < a.R; r += AT_PLAN_THREADS) {
-            const int64_t rows = (int64_t)(attn_row(a, r + 1) - attn_row(a, r)) * a.G;
-            if (rows > 0 && (rows < AT_MERGE_ROWS || rows < a.wide_min_rows)) {
-                const int g = group_of(r);
-                if (g >= 0) a.plan.mixed[g] = 1;
+        if (in_smem) {
+            for (int g = tid; g <= a.P; g += threads) {
+                s_off[g] = attn_group(a, g);
+                if (g < a.P) {
+                    s_len[g] = attn_keys(a.prefix_len[g], a.pcols, a.page_shift);
+                    s_mixed[g] = 0;
+                }
             }
+            __syncthreads();
+            // groups that have requests with few rows need a prefix segment (with more groups than fit here all have one)
+            for (int r = tid; r < a.R; r += threads) {
+                const int64_t rows = (int64_t)(attn_row(a, r + 1) - attn_row(a, r)) * a.G;
+                if (rows > 0 && (rows < AT_MERGE_ROWS || rows < a.wide_min_rows)) {
+                    const int g = group_of(r);
+                    if (g >= 0) s_mixed[g] = 1;
+                }
+            }
+            __syncthreads();
         }
-        __syncthreads();
     }
+    auto mixed = [&](int g) { return in_smem ? s_mixed[g] != 0 : true; };
     int64_t carry[2] = {0, 0};
-    bool two = false;
-    for (int s0 = 0; s0 < S; s0 += AT_PLAN_THREADS) {
+    bool two = false, empty = false;
+    for (int s0 = 0; s0 < S; s0 += threads) {
         const int s = s0 + tid;
-        int64_t own[2] = {0, 0}, inc[2];
+        int64_t own[2] = {0, 0}, inc[2], total[2];
         if (s < S) {
             Segment g;
             g.plen = 0;
             g.flags = 0;
             g.causal = s >= a.P;
             if (s < a.P) {
-                const int r0 = attn_group(a, s), r1 = max(attn_group(a, s + 1), r0);
+                const int r0 = off(s), r1 = max(off(s + 1), r0);
+                g.klen = len(s);
                 g.t0 = attn_row(a, r0);
-                g.n = a.plan.mixed[s] ? max(attn_row(a, r1) - g.t0, 0) : 0;
-                g.klen = attn_keys(a.prefix_len[s], a.pcols, a.page_shift);
+                g.n = g.klen > 0 && mixed(s) ? max(attn_row(a, r1) - g.t0, 0) : 0;
                 g.group = s;
                 g.flags = SEG_TWO;
-                if (g.klen == 0) g.n = 0;
             } else {
                 const int r = s - a.P;
                 g.t0 = attn_row(a, r);
@@ -329,9 +404,11 @@ __global__ void __launch_bounds__(AT_PLAN_THREADS) attn_plan_kernel(const AttnAr
                 g.klen = attn_keys(a.kv_len[r], a.cols, a.page_shift);
                 g.group = group_of(r);
                 if (g.group >= 0) {
-                    if (a.plan.mixed[g.group]) g.flags = SEG_TWO;
-                    else g.plen = attn_keys(a.prefix_len[g.group], a.pcols, a.page_shift);
+                    if (mixed(g.group)) g.flags = SEG_TWO;
+                    else g.plen = len(g.group);
                 }
+                two |= g.n > 0 && (g.flags & SEG_TWO);
+                empty |= g.n > g.klen && g.group < 0;
             }
             if ((int64_t)g.n * a.G >= a.wide_min_rows) {
                 g.flags |= SEG_WIDE;
@@ -344,31 +421,19 @@ __global__ void __launch_bounds__(AT_PLAN_THREADS) attn_plan_kernel(const AttnAr
                 own[0] = t * FewUnits::heads(a);
             }
             a.plan.seg[s] = g;
-            two |= g.n > 0 && (g.flags & SEG_TWO);
         }
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            inc[j] = own[j];
-            for (int o = 1; o < 32; o <<= 1) {
-                const int64_t up = __shfl_up_sync(0xFFFFFFFFu, inc[j], o);
-                if (lane >= o) inc[j] += up;
-            }
-            if (lane == 31) s_warp[j][warp] = inc[j];
+        inc[0] = own[0];
+        inc[1] = own[1];
+        block_scan2(inc, total, s_warp, threads / 32);
+        if (s < S) {
+            a.plan.few_start[s] = carry[0] + inc[0] - own[0];
+            a.plan.wide_start[s] = carry[1] + inc[1] - own[1];
         }
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            int64_t before = carry[j], total = carry[j];
-            for (int w = 0; w < AT_PLAN_THREADS / 32; ++w) {
-                if (w < warp) before += s_warp[j][w];
-                total += s_warp[j][w];
-            }
-            if (s < S) (j ? a.plan.wide_start : a.plan.few_start)[s] = before + inc[j] - own[j];
-            carry[j] = total;
-        }
-        __syncthreads();
+        carry[0] += total[0];
+        carry[1] += total[1];
     }
     two = __syncthreads_or(two);
+    empty = __syncthreads_or(empty);
     if (tid == 0) {
         a.plan.share[2] = two;
         a.plan.few_start[S] = carry[0];
@@ -376,16 +441,56 @@ __global__ void __launch_bounds__(AT_PLAN_THREADS) attn_plan_kernel(const AttnAr
         a.plan.share[0] = share_tiles(carry[0], a.few_ctas, few_min_tiles(a));
         a.plan.share[1] = share_tiles(carry[1], a.wide_ctas, AT_WIDE_MIN_TILES);
     }
-    // Rows without any key (fewer own keys than new tokens, and no prefix) are in no unit, or in one that has other rows: 0, -inf
-    for (int r = warp; r < a.R; r += AT_PLAN_THREADS / 32) {
-        const int t0 = attn_row(a, r), n = attn_row(a, r + 1) - t0;
-        const int none = n - attn_keys(a.kv_len[r], a.cols, a.page_shift);
-        if (none <= 0 || group_of(r) >= 0) continue;
-        for (int t = t0; t < t0 + min(none, n); ++t) {
-            for (int c = lane; c < a.Hq * a.head_dim / 8; c += 32) *reinterpret_cast<uint4*>(a.o + (int64_t)t * a.ldo + c * 8) = make_uint4(0u, 0u, 0u, 0u);
-            if (a.lse)
-                for (int c = lane; c < a.Hq; c += 32) a.lse[(int64_t)t * a.Hq + c] = -INFINITY;
+    if (two) {
+        for (int t = tid; t < a.T; t += threads) a.plan.tok_req[t] = -1;
+        __syncthreads();
+        for (int r = tid >> 5; r < a.R; r += threads / 32) {
+            const Segment& g = a.plan.seg[a.P + r];
+            if (g.flags & SEG_TWO)
+                for (int t = g.t0 + (tid & 31); t < g.t0 + g.n; t += 32) a.plan.tok_req[t] = r;
         }
+    }
+    if (empty) {
+        for (int r = tid >> 5; r < a.R; r += threads / 32) {
+            const Segment& g = a.plan.seg[a.P + r];
+            if (g.group < 0 && g.n > g.klen) clear_rows(a, g.t0, g.n - g.klen);
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ pieces
+struct PieceList {           // pieces of one row from one segment
+    int count;               // 0: none; 1: the whole unit, in the dense buffer
+    int cta, which;          // share of the first piece, and whether it is that CTA's last piece
+    int stride;              // rows between two slots
+    int64_t row;             // row in a slot, or in the dense buffer
+    const float* part;
+    const float2* ml;
+    __device__ int64_t at(int i) const { return count == 1 ? row : ((int64_t)(cta + i) * 2 + (i ? 0 : which)) * stride + row; }
+};
+__device__ __forceinline__ void list_pieces(PieceList& p, int64_t begin, int tiles, int64_t q) {
+    const int64_t c0 = div_fast(begin, q), c1 = div_fast(begin + tiles - 1, q);
+    p.cta = (int)c0;
+    p.which = begin > c0 * q;
+    p.count = (int)(c1 - c0) + 1;
+}
+
+// pieces of row g of token t's head h from a segment on the tcgen05 line
+__device__ __forceinline__ void wide_pieces(const AttnArgs& a, PieceList& p, const Segment& sg, int64_t seg_start, int64_t q, int t, int h, int g, int dense) {
+    const int tok = t - sg.t0, tpt = AT_WIDE_TILE / a.G, u = tok / (2 * tpt), in = tok % (2 * tpt);
+    p.count = 0;
+    if (tok < 0 || tok >= sg.n) return;
+    const int nt = unit_tiles<WideUnits>(a, sg, u);
+    if (nt == 0) return;
+    list_pieces(p, unit_begin<WideUnits>(a, sg, seg_start, h, u), nt, q);
+    p.stride = 2 * AT_WIDE_TILE;
+    p.row = (in / tpt) * AT_WIDE_TILE + (in % tpt) * a.G + g;
+    p.part = a.wide_part;
+    p.ml = a.wide_ml;
+    if (p.count == 1) {
+        p.row = (int64_t)t * a.Hq + h * a.G + g;
+        p.part = a.dense[dense];
+        p.ml = a.dense_ml[dense];
     }
 }
 
@@ -420,14 +525,18 @@ __device__ __forceinline__ float exp2_approx(float x) {
 constexpr float AT_SLACK = 8.0f;
 constexpr int AT_FEW_THREADS = 128;
 
-template <int D, int HW>
+constexpr int FEW_SELF = 256;          // requests whose line every CTA lays out for itself
+
+template <int D, int HW, bool SELF>
 struct FewCfg {
     static constexpr int KV_BYTES = 16 * D * 2;                  // one warp's 16 keys (or values) of a tile
     static constexpr int SLOT_BYTES = 2 * KV_BYTES;
     static constexpr int STAGES = D == 128 ? 3 : 6;
     static constexpr int RING = 4 * STAGES * SLOT_BYTES;         // every warp has its own ring
     static constexpr int JOIN_FLOATS = 16 * D + 32;              // one warp's O, m and l
-    static constexpr int SMEM = RING + (HW < 4 ? 2 * JOIN_FLOATS * 4 : 0);
+    static constexpr int JOIN = HW < 4 ? 2 * JOIN_FLOATS * 4 : 0;
+    static constexpr int PLAN = SELF ? FEW_SELF * (int)sizeof(Segment) + (FEW_SELF + 1) * 8 : 0;
+    static constexpr int SMEM = RING + JOIN + PLAN;
 };
 
 // One CTA: four warps, each with its own ring of cp.async slots and its own (m, l, O), so that no barrier runs inside the
@@ -435,10 +544,14 @@ struct FewCfg {
 // in the cache, so the CTA still reads whole 1 KB rows.  Where the number of heads is not a multiple of four, two or four warps
 // take different keys of a head and are joined through shared memory at the end of a unit.  (All warps on one head
 // whatever the head count cost 129 us instead of the figure in the table on 256 requests of ~512 keys: the join, three barriers a unit.)
+// It needs nothing of the tcgen05 kernel that may be launched in front of it, so it begins (`early`) on every SM that has no
+// tcgen05 CTA or whose CTA has ended, and only waits for that kernel before it ends itself: whatever comes behind waits for both.
+// Without prefixes and prompts, up to FEW_SELF requests, every CTA lays out the line for itself in shared memory (SELF) and
+// no plan kernel runs: the launch and its two trips through L2 would be a third of the smallest calls.
 // The loads run on over the ends of units.  A page number is fetched one tile ahead of the loads that need it.
-template <int D, int HW>
-__global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnArgs a) {
-    using C = FewCfg<D, HW>;
+template <int D, int HW, bool SELF>
+__global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnArgs a, bool early) {
+    using C = FewCfg<D, HW, SELF>;
     constexpr int NJ = D / 8;          // 8-channel column blocks of O
     constexpr int KS = D / 16;         // k steps of Q K^T
     constexpr int CHUNKS = D / 8;      // 16-byte chunks of a key
@@ -446,20 +559,62 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
     extern __shared__ __align__(128) uint8_t at_smem[];
     grid_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    grid_dependency_wait();
+    if (!early) grid_dependency_wait();
     const int S = a.P + a.R;
-    const int64_t N = a.plan.few_start[S], q = a.plan.share[0];
+    LineSource<SELF> src = {a.plan.seg, a.plan.few_start};
+    int64_t N, q;
+    if (SELF) {
+        __shared__ int64_t s_warp[2][32];
+        Segment* seg = reinterpret_cast<Segment*>(at_smem + C::RING + C::JOIN);
+        int64_t* start = reinterpret_cast<int64_t*>(seg + FEW_SELF);
+        int64_t carry = 0;
+        bool empty = false;
+        for (int s0 = 0; s0 < S; s0 += AT_FEW_THREADS) {
+            const int s = s0 + threadIdx.x;
+            int64_t inc[2] = {0, 0}, total[2], own = 0;
+            if (s < S) {
+                Segment g;
+                g.plen = 0;
+                g.flags = 0;
+                g.causal = 1;
+                g.group = -1;
+                g.t0 = attn_row(a, s);
+                g.n = max(attn_row(a, s + 1) - g.t0, 0);
+                g.klen = attn_keys(a.kv_len[s], a.cols, a.page_shift);
+                g.tiles = (int)head_tiles<FewUnits>(a, g);
+                own = (int64_t)g.tiles * FewUnits::heads(a);
+                inc[0] = own;
+                seg[s] = g;
+                empty |= g.n > g.klen;
+            }
+            block_scan2(inc, total, s_warp, AT_FEW_THREADS / 32);
+            if (s < S) start[s] = carry + inc[0] - own;
+            carry += total[0];
+        }
+        empty = __syncthreads_or(empty);
+        N = carry;
+        q = share_tiles(N, a.few_ctas, few_min_tiles(a));
+        src.seg = seg;
+        src.start = start;
+        if (empty)
+            for (int r = blockIdx.x * 4 + warp; r < S; r += gridDim.x * 4)
+                if (seg[r].n > seg[r].klen) clear_rows(a, seg[r].t0, seg[r].n - seg[r].klen);
+    } else {
+        N = load_plan(a.plan.few_start + S);
+        q = load_plan(a.plan.share);
+    }
     const int64_t x0 = min(q * blockIdx.x, N), x1 = min(x0 + q, N);
     if (x0 >= x1) {
         if (threadIdx.x == 0) a.plan.cut[0][blockIdx.x].tiles = 0;
+        if (early) grid_dependency_wait();
         return;
     }
 
     const uint32_t ring = smem_u32(at_smem) + warp * C::STAGES * C::SLOT_BYTES;
     float* join = reinterpret_cast<float*>(at_smem + C::RING);
 
-    Cursor<FewUnits> cur, ld;
-    cur.seek(a, a.plan.few_start, S, x0);
+    Cursor<FewUnits, SELF> cur, ld;
+    cur.seek(a, src, S, x0);
     ld = cur;
     const int page_mask = (1 << a.page_shift) - 1;
     const int hw = warp % HW;          // head of the warp inside the unit
@@ -489,7 +644,7 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
                 cp_async_16(d + C::KV_BYTES, a.v + off, r < nvalid);
             }
             if (++xl < x1) {
-                if (++ld.kt == ld.nt) ld.next_unit(a, 0);
+                if (++ld.kt == ld.nt) ld.next_unit(a, src, 0);
                 page = page_of();
             }
         }
@@ -669,10 +824,11 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
                 }
             }
         }
-        if (x < x1) cur.next_unit(a, 0);
-        else if (threadIdx.x == 0) tell_cut(a.plan.cut[0][blockIdx.x], unit_x0, unit_x1, x0, x1, cur.s, cur.h, cur.u, cur.g.flags);
+        if (x < x1) cur.next_unit(a, src, 0);
+        else if (threadIdx.x == 0) tell_cut(a.plan.cut[0] + blockIdx.x, unit_x0, unit_x1, x0, x1, q, cur.h, cur.u, cur.g);
     }
     cp_async_wait<0>();
+    if (early) grid_dependency_wait();
 }
 
 // ------------------------------------------------------------------------------------------------- join
@@ -682,29 +838,14 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
 // against 1 ms of attention, when it was done that way):
 //   units that the end of a share cuts, as the attention kernels told them: blocks for every share of either line;
 //   rows with two sources (prefix and own keys): blocks over the tokens, only launched where there are prefixes.
-// Pieces are taken 32 at a time, one per lane for m and l, eight rows of O under way at a time.
+// Pieces are taken 32 at a time, one per lane for m and l, twelve rows of O under way at a time.
 constexpr int AT_JOIN_THREADS = 256;
 constexpr int AT_JOIN_WARPS = AT_JOIN_THREADS / 32;
-
-struct PieceList {           // pieces of one row from one segment
-    int count;               // 0: none; 1: the whole unit, in the dense buffer
-    int cta, which;          // share of the first piece, and whether it is that CTA's last piece
-    int stride;              // rows between two slots
-    int64_t row;             // row in a slot, or in the dense buffer
-    const float* part;
-    const float2* ml;
-    __device__ int64_t at(int i) const { return count == 1 ? row : ((int64_t)(cta + i) * 2 + (i ? 0 : which)) * stride + row; }
-};
-__device__ __forceinline__ void list_pieces(PieceList& p, int64_t begin, int tiles, int64_t q) {
-    const int64_t c0 = div_fast(begin, q), c1 = div_fast(begin + tiles - 1, q);
-    p.cta = (int)c0;
-    p.which = begin > c0 * q;
-    p.count = (int)(c1 - c0) + 1;
-}
 
 template <int D>
 __device__ __forceinline__ void join_row(const AttnArgs& a, const PieceList& p0, const PieceList& p1, int64_t token, int hq) {
     constexpr int V = D / 32;          // channels per lane
+    constexpr int FLIGHT = 12;         // rows of O under way at a time
     const int lane = threadIdx.x & 31;
     float m = -INFINITY, l = 0.0f, o[V];
 #pragma unroll
@@ -734,10 +875,10 @@ __device__ __forceinline__ void join_row(const AttnArgs& a, const PieceList& p0,
 #pragma unroll
         for (int j = 0; j < V; ++j) o[j] *= f0;
         const int k = min(32, n - i0);
-        for (int b = 0; b < k; b += 8) {
-            float v[8][V], wb[8];
+        for (int b = 0; b < k; b += FLIGHT) {
+            float v[FLIGHT][V], wb[FLIGHT];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
+            for (int j = 0; j < FLIGHT; ++j) {
                 const int from = min(b + j, k - 1);
                 const float* sp = reinterpret_cast<const float*>(__shfl_sync(0xFFFFFFFFu, (unsigned long long)src, from));
                 wb[j] = __shfl_sync(0xFFFFFFFFu, w, from);
@@ -751,7 +892,7 @@ __device__ __forceinline__ void join_row(const AttnArgs& a, const PieceList& p0,
                 }
             }
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
+            for (int j = 0; j < FLIGHT; ++j)
                 if (wb[j] != 0.0f)     // a piece without weight may hold anything
 #pragma unroll
                     for (int y = 0; y < V; ++y) o[y] = fmaf(v[j][y], wb[j], o[y]);
@@ -769,28 +910,27 @@ __device__ __forceinline__ void join_row(const AttnArgs& a, const PieceList& p0,
 }
 
 template <int D>
-__global__ void __launch_bounds__(AT_JOIN_THREADS, 3) attn_join_kernel(const AttnArgs a, int wide_blocks, int wide_split, int few_blocks, int few_split,
+__global__ void __launch_bounds__(AT_JOIN_THREADS, 2) attn_join_kernel(const AttnArgs a, int wide_blocks, int wide_split, int few_blocks, int few_split,
                                                                     int tokens) {
     grid_launch_dependents();
     grid_dependency_wait();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = threadIdx.x >> 5;
     int b = blockIdx.x;
     PieceList none, p;
     none.count = 0;
     if (b < wide_blocks) {
         const CutUnit cut = a.plan.cut[1][b / wide_split];
         if (cut.tiles == 0) return;
-        const Segment sg = a.plan.seg[cut.s];
-        list_pieces(p, cut.begin, cut.tiles, a.plan.share[1]);
+        list_pieces(p, cut.begin, cut.tiles, cut.share);
         p.stride = 2 * AT_WIDE_TILE;
         p.part = a.wide_part;
         p.ml = a.wide_ml;
         const int tpt = AT_WIDE_TILE / a.G, rows = 2 * AT_WIDE_TILE / wide_split, part = b % wide_split;
         for (int i = part * rows + warp; i < (part + 1) * rows; i += AT_JOIN_WARPS) {
             const int r = i % AT_WIDE_TILE, tok = (cut.u * 2 + i / AT_WIDE_TILE) * tpt + r / a.G;
-            if (r >= tpt * a.G || tok >= sg.n) continue;
+            if (r >= tpt * a.G || tok >= cut.n) continue;
             p.row = i;
-            join_row<D>(a, none, p, sg.t0 + tok, cut.h * a.G + r % a.G);
+            join_row<D>(a, none, p, cut.t0 + tok, cut.h * a.G + r % a.G);
         }
         return;
     }
@@ -798,17 +938,16 @@ __global__ void __launch_bounds__(AT_JOIN_THREADS, 3) attn_join_kernel(const Att
     if (b < few_blocks) {
         const CutUnit cut = a.plan.cut[0][b / few_split];
         if (cut.tiles == 0) return;
-        const Segment sg = a.plan.seg[cut.s];
-        list_pieces(p, cut.begin, cut.tiles, a.plan.share[0]);
+        list_pieces(p, cut.begin, cut.tiles, cut.share);
         p.stride = a.few_hw * AT_FEW_ROWS;
         p.part = a.few_part;
         p.ml = a.few_ml;
         const int rows = p.stride / few_split, part = b % few_split;
         for (int i = part * rows + warp; i < (part + 1) * rows; i += AT_JOIN_WARPS) {
             const int fr = cut.u * AT_FEW_ROWS + i % AT_FEW_ROWS, tok = fr / a.G;
-            if (tok >= sg.n) continue;
+            if (tok >= cut.n) continue;
             p.row = i;
-            join_row<D>(a, none, p, sg.t0 + tok, (cut.h * a.few_hw + i / AT_FEW_ROWS) * a.G + fr % a.G);
+            join_row<D>(a, none, p, cut.t0 + tok, (cut.h * a.few_hw + i / AT_FEW_ROWS) * a.G + fr % a.G);
         }
         return;
     }
@@ -821,17 +960,9 @@ __global__ void __launch_bounds__(AT_JOIN_THREADS, 3) attn_join_kernel(const Att
         const int64_t t64 = (int64_t)(b / a.Hk) * tokens + i / a.G;
         if (t64 >= a.T) return;
         const int t = (int)t64, g = i % a.G;
-        int r = 0, len = a.R;            // the last request that begins at or before t
-        while (len > 1) {
-            const int step = (len + 31) / 32, j = lane * step;
-            const uint32_t f = __ballot_sync(0xFFFFFFFFu, j < len && attn_row(a, r + j) <= t);
-            const int k = max(31 - __clz(f), 0);
-            r += k * step;
-            len = min(step, len - k * step);
-        }
-        const Segment own = a.plan.seg[a.P + r];
-        if (t < own.t0 || t >= own.t0 + own.n || !(own.flags & SEG_TWO)) continue;
-        const Segment pre = a.plan.seg[own.group];
+        const int r = a.plan.tok_req[t];
+        if (r < 0) continue;
+        const Segment own = a.plan.seg[a.P + r], pre = a.plan.seg[own.group];
         {
             const int hq = h * a.G + g;
             PieceList list[2];
@@ -843,14 +974,7 @@ __global__ void __launch_bounds__(AT_JOIN_THREADS, 3) attn_join_kernel(const Att
                 pl.count = 0;
                 if (tok < 0 || tok >= sg.n) continue;
                 if (sg.flags & SEG_WIDE) {
-                    const int tpt = AT_WIDE_TILE / a.G, u = tok / (2 * tpt), in = tok % (2 * tpt);
-                    const int nt = unit_tiles<WideUnits>(a, sg, u);
-                    if (nt == 0) continue;
-                    list_pieces(pl, unit_begin<WideUnits>(a, sg, a.plan.wide_start[s], h, u), nt, nw);
-                    pl.stride = 2 * AT_WIDE_TILE;
-                    pl.row = (in / tpt) * AT_WIDE_TILE + (in % tpt) * a.G + g;
-                    pl.part = a.wide_part;
-                    pl.ml = a.wide_ml;
+                    wide_pieces(a, pl, sg, a.plan.wide_start[s], nw, t, h, g, which);
                 } else {
                     const int fr = tok * a.G + g, u = fr / AT_FEW_ROWS;
                     const int nt = unit_tiles<FewUnits>(a, sg, u);
@@ -860,11 +984,11 @@ __global__ void __launch_bounds__(AT_JOIN_THREADS, 3) attn_join_kernel(const Att
                     pl.row = (h % a.few_hw) * AT_FEW_ROWS + fr % AT_FEW_ROWS;
                     pl.part = a.few_part;
                     pl.ml = a.few_ml;
-                }
-                if (pl.count == 1) {
-                    pl.row = (int64_t)t * a.Hq + hq;
-                    pl.part = a.dense[which];
-                    pl.ml = a.dense_ml[which];
+                    if (pl.count == 1) {
+                        pl.row = (int64_t)t * a.Hq + hq;
+                        pl.part = a.dense[which];
+                        pl.ml = a.dense_ml[which];
+                    }
                 }
             }
             join_row<D>(a, list[0], list[1], t, hq);
