@@ -2,23 +2,24 @@
 // tcgen05 kernel on the tile line of attn_kernels.cu.
 //
 // A unit is two tiles of up to 128 rows (tokens x query heads of one key/value head).  S = Q K^T and O += P V
-// both run on the fifth-generation tensor cores: Q, K and V tiles come by TMA into shared memory, S and O live in TMEM, P goes
-// back into the columns of its S and is read from there as the A operand.  With D = 128 a 128 x 128 tile costs the tensor
-// pipe 2 x 512 cycles and the exponential units (16 a cycle) 1024, so two streams run in counterphase, each with its
-// own S, O and warpgroup (one row per thread): while one stream's softmax runs, the other's products do.
+// both run on the fifth-generation tensor cores: Q, K and V tiles come by TMA into shared memory, S, P and O live in TMEM (P, the weights
+// in bf16, is read from there as the A operand).  Two streams run in counterphase, each with its own S, P, O and warpgroup (one
+// row per thread): while one stream's softmax runs, the other's products do.
 //   both row tiles filled: stream s is row tile s; they share every K and V tile.
 //   one row tile:          both streams take the same rows and every other key tile; the results are joined
-//                          at the end of the unit (a thread of warpgroup 0 can read both O rows: they lie in its lanes).
+//                          at the end of the unit (a thread can read both O rows: they lie in its lanes).
+// Key tiles of 64: with 128 keys S and O fill TMEM and P has to go into the columns of its S, so that a stream's steps run strictly
+// one after the other (S, softmax, P V, next S: 3800 cycles for 128 keys of both row tiles, tensor pipe half idle).  With 64 there is room for
+// P, and the next S is worked out while the softmax of this one runs.
 //
 //   warps 0-3, 4-7 : softmax of stream 0, 1, and their epilogue
 //   warp 8         : TMA (a key tile is loaded page by page; a page that is not there reads as zeros)
 //   warp 9         : MMA issue, TMEM owner
 //   warp 10        : the units of the CTA's share, for everyone else
-//   warp 11        : idle; the third warpgroup gives registers to the softmax
+//   warp 11        : zeros behind the last key of a V tile
 //
 // P V with the weights of the running maximum as it stands: O is rescaled in TMEM only when the maximum has moved by
-// more than 2^8 (see AT_SLACK), by the softmax threads themselves.  That needs no wait of its own: the S tile that moved
-// the maximum was issued behind the previous P V, so S complete means O complete.
+// more than 2^8 (see AT_SLACK), by the softmax threads themselves, between the P V before and the one to come.
 #include <algorithm>
 
 #include "common.cuh"
@@ -32,14 +33,8 @@ struct AttnWideArgs {
     AttnArgs a;
 };
 
-constexpr int AW_THREADS = 384;
-// Registers: launched with 168 a thread (12 warps); the softmax warpgroups hold a row of 128 scores each thread and take
-// 208, the third warpgroup (TMA, MMA, two idle warps) gives down to 80: 256 x 208 + 128 x 80 <= 384 x 168.
-constexpr int AW_REGS_SOFTMAX = 208, AW_REGS_OTHER = 80;
-template <int R>
-__device__ __forceinline__ void regs_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(R)); }
-template <int R>
-__device__ __forceinline__ void regs_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(R)); }
+constexpr int AW_SOFTMAX_WARPS = 8;
+constexpr int AW_THREADS = (AW_SOFTMAX_WARPS + 4) * 32;
 
 // Two fp32 operations in one instruction.
 __device__ __forceinline__ uint64_t pack2(float x, float y) {
@@ -67,13 +62,18 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 template <int D>
 struct WideCfg {
     static constexpr int HALVES = D / 64;                        // 128-byte swizzle rows hold 64 channels
-    static constexpr int HALF_BYTES = 128 * 128;
-    static constexpr int TILE_BYTES = HALVES * HALF_BYTES;       // 128 rows (or keys) x D
-    static constexpr int STAGES = D == 128 ? 5 : 8;
-    static constexpr int BAR_BYTES = 384;
-    static constexpr int SMEM = (2 + STAGES) * TILE_BYTES + BAR_BYTES + 128 * 8 + 2 * 64 + 1024;
-    static constexpr int TM_S = 0;         // TMEM columns: S0, S1, O0, O1
-    static constexpr int TM_O = 256;
+    static constexpr int QHALF_BYTES = 128 * 128;                // 128 rows of 64 channels
+    static constexpr int QTILE_BYTES = HALVES * QHALF_BYTES;
+    static constexpr int HALF_BYTES = AT_WIDE_KEYS * 128;        // 64 keys of 64 channels
+    static constexpr int TILE_BYTES = HALVES * HALF_BYTES;
+    static constexpr int STAGES = 8;
+    static constexpr int OUT_BYTES = AW_SOFTMAX_WARPS * 2048;    // every softmax warp's 32 rows x 16 columns of O on the way out
+    static constexpr int ROW_FLOATS = 2 * 2 * 2 * 128;           // [parity][stream][128] maxima and sums of a unit
+    static constexpr int BAR_BYTES = 288;
+    static constexpr int SMEM = 2 * QTILE_BYTES + STAGES * TILE_BYTES + OUT_BYTES + ROW_FLOATS * 4 + BAR_BYTES + 2 * 64 + 1024;
+    static constexpr int TM_S = 0;         // TMEM columns: S0, S1 (64 each), P0, P1 (32 each), O0, O1 (D each)
+    static constexpr int TM_P = 128;
+    static constexpr int TM_O = 192;
     static_assert(SMEM <= 232448, "shared memory");
 };
 
@@ -91,13 +91,10 @@ __device__ __forceinline__ void mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uin
                  "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
                  ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
 }
-__device__ __forceinline__ void tmem_st_32x32(uint32_t taddr, const uint32_t* r) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-                 "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
-                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
-                 "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]),
-                 "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]),
-                 "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
+__device__ __forceinline__ void tmem_ld_x16(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+                   "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(taddr) : "memory");
 }
 __device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t* r) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
@@ -120,8 +117,8 @@ __device__ __forceinline__ uint64_t smem_desc_sw128_mn(uint32_t saddr, uint32_t 
 }
 constexpr uint32_t IDESC_B_MN = 1u << 16;   // B operand with its N extent contiguous
 
-// What the roles need to know of a unit, or of the part of it that the CTA's share has: key tiles [ka, ka + n).  Warp 10
-// walks over the line and keeps two of these ahead in shared memory.
+// What the roles need to know of a unit, or of the part of it that the CTA's share has: key tiles [ka, ka + n).  The units
+// warp walks over the line and keeps two of these ahead in shared memory.
 struct __align__(16) WideUnit {
     int ka, n;          // n = 0: the share is done
     int cnt[2];         // key tiles of stream 0 and 1
@@ -146,54 +143,48 @@ __device__ __forceinline__ int unit_left(const WideUnit& w, int kt) {
 template <int D>
 __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_constant__ AttnWideArgs args) {
     using C = WideCfg<D>;
-    constexpr int STAGES = C::STAGES;
+    constexpr int STAGES = C::STAGES, NSW = AW_SOFTMAX_WARPS;
     const AttnArgs& a = args.a;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    uint8_t* ring = smem + 2 * C::TILE_BYTES;
-    uint64_t* bars = reinterpret_cast<uint64_t*>(ring + STAGES * C::TILE_BYTES);
+    uint8_t* ring = smem + 2 * C::QTILE_BYTES;
+    uint8_t* out_tiles = ring + STAGES * C::TILE_BYTES;
+    float2* unit_ml = reinterpret_cast<float2*>(out_tiles + C::OUT_BYTES);  // [parity][stream][128]
+    uint64_t* bars = reinterpret_cast<uint64_t*>(unit_ml + 4 * 128);
     uint64_t* full = bars;
     uint64_t* empty = bars + STAGES;
     uint64_t* q_full = bars + 2 * STAGES;
     uint64_t* q_empty = q_full + 1;
-    uint64_t* s_full = q_full + 2;
-    uint64_t* p_full = q_full + 4;
-    uint64_t* o_full = q_full + 6;
-    uint64_t* o_empty = q_full + 8;
-    uint64_t* j_full = q_full + 10;
-    uint64_t* j_empty = q_full + 11;
-    uint64_t* u_full = q_full + 12;      // [2]
-    uint64_t* u_empty = q_full + 14;     // [2]
+    uint64_t* s_full = q_full + 2;       // [2]
+    uint64_t* p_full = q_full + 4;       // [2]
+    uint64_t* s_empty = q_full + 6;      // [2]
+    uint64_t* pv_done = q_full + 8;      // [2]
+    uint64_t* u_full = q_full + 10;      // [2]
+    uint64_t* u_empty = q_full + 12;     // [2]
+    uint64_t* o_empty = q_full + 14;
+    uint64_t* e_full = q_full + 15;
     uint64_t* drain_bar = q_full + 16;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(q_full + 17);
+    uint64_t* v_clean = q_full + 17;
+    uint64_t* v_end = q_full + 18;
+    WideUnit* units = reinterpret_cast<WideUnit*>(reinterpret_cast<uint8_t*>(bars) + C::BAR_BYTES);   // [2]
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(q_full + 19);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-    float2* s_ml = reinterpret_cast<float2*>(reinterpret_cast<uint8_t*>(bars) + C::BAR_BYTES);   // [128]: stream 1's (m, l)
-    WideUnit* units = reinterpret_cast<WideUnit*>(s_ml + 128);                                   // [2]
+    static_assert((2 * STAGES + 19) * 8 + 8 <= C::BAR_BYTES, "barriers");
 
     const int warp = __shfl_sync(0xFFFFFFFFu, (int)(threadIdx.x >> 5), 0);
     const int lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < STAGES; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
-        mbar_init(q_full, 1);
-        mbar_init(q_empty, 1);
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(&s_full[i], 1);
-            mbar_init(&p_full[i], 4);
-            mbar_init(&o_full[i], 1);
-            mbar_init(&o_empty[i], 4);
-            mbar_init(&u_full[i], 1);
-            mbar_init(&u_empty[i], 10);
+        for (int i = 0; i < 2 * STAGES + 19; ++i) {
+            const int b = i - 2 * STAGES;      // all barriers take one arrival but these
+            mbar_init(&bars[i], b == 4 || b == 5 || b == 6 || b == 7 ? NSW / 2 : b == 12 || b == 13 ? NSW + 3 : b == 14 || b == 15 ? NSW : 1);
         }
-        mbar_init(j_full, 4);
-        mbar_init(j_empty, 4);
-        mbar_init(drain_bar, 1);
         *abort_flag = 0;
         fence_barrier_init();
         prefetch_tmap(&args.tm_q);
         prefetch_tmap(&args.tm_k);
         prefetch_tmap(&args.tm_v);
     }
-    if (warp == 9) {
+    if (warp == NSW + 1) {
         tmem_alloc(tmem_slot, 512);
         tmem_relinquish();
     }
@@ -204,25 +195,25 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
     grid_dependency_wait();
     grid_launch_dependents();   // not before: the few-row kernel counts on the plan being there when it begins
     const int tpt = AT_WIDE_TILE / a.G;
+    const uint32_t ring0 = smem_u32(ring);
 
-    if (warp >= 8) {
-        regs_dec<AW_REGS_OTHER>();
-        if (warp == 10) {
+    if (warp >= NSW) {
+        if (warp == NSW + 2) {
             // ------------------------------------------------------------------------------------- units
             const int S = a.P + a.R;
-            const int64_t N = a.plan.wide_start[S], q = a.plan.share[1];
-            const int64_t x0 = min(q * blockIdx.x, N), x1 = min(x0 + q, N);
+            const int N = a.plan.wide_start[S], q = a.plan.share[1];
+            const int x0 = (int)min((int64_t)q * blockIdx.x, (int64_t)N), x1 = (int)min((int64_t)x0 + q, (int64_t)N);
             Cursor<WideUnits> cur;
             const LineSource<false> src = {a.plan.seg, a.plan.wide_start};
             if (x0 < x1) cur.seek(a, src, S, x0);
             else if (lane == 0) a.plan.cut[1][blockIdx.x].tiles = 0;
             int b = 0;
             uint32_t ph = 0;
-            for (int64_t x = x0;;) {
+            for (int x = x0;;) {
                 WideUnit w = {};
                 if (x < x1) {
                     w.ka = cur.kt;
-                    w.n = (int)min((int64_t)(cur.nt - cur.kt), x1 - x);
+                    w.n = min(cur.nt - cur.kt, x1 - x);
                     w.tok0 = cur.u * 2 * tpt;
                     w.tokens = min(cur.g.n - w.tok0, 2 * tpt);
                     w.pair = w.tokens > tpt;
@@ -241,7 +232,7 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                     w.seg = cur.s;
                     w.h = cur.h;
                     w.row0 = cur.g.t0 + w.tok0;
-                    w.causal = cur.g.causal ? cur.g.n : 0;
+                    w.causal = cur.g.flags & SEG_OWN ? cur.g.n : 0;
                     w.out = (w.n < cur.nt ? OUT_SPLIT : 0) | (cur.g.flags & SEG_TWO ? OUT_TWO : 0) | (cur.s >= a.P ? OUT_OWN : 0) | (x > x0 ? OUT_LATER : 0);
                 }
                 if (!wait_bounded(&u_empty[b], ph ^ 1u, abort_flag, 76)) break;
@@ -256,12 +247,11 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                 x += w.n;
                 if (x < x1) cur.next_unit(a, src, SEG_WIDE);
             }
-        } else if (warp == 8) {
+        } else if (warp == NSW) {
             // --------------------------------------------------------------------------------------- TMA
             const int bt = min(1 << a.page_shift, AT_WIDE_KEYS);     // tokens of a box
             const int boxes = AT_WIDE_KEYS / bt * C::HALVES;         // of a K or V tile: at most 16, one lane each
             const int mine = lane / C::HALVES, half = lane % C::HALVES;
-            const uint32_t ring0 = smem_u32(ring);
             uint32_t n_load = 0;            // loads so far: stage n % STAGES, phase n / STAGES
             int st = 0, b = 0;
             uint32_t ph = 0, q_ph = 0, u_ph = 0;
@@ -270,16 +260,6 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                 const WideUnit& w = units[b];
                 const int ka = w.ka, kb = ka + w.n, nf = w.nf, h = w.h;
                 if (kb == ka) break;
-                if (!wait_bounded(q_empty, q_ph ^ 1u, abort_flag, 61)) goto stop_loads;
-                q_ph ^= 1u;
-                if (elect_one()) {
-                    const int tiles = w.pair ? 2 : 1;
-                    mbar_arrive_expect_tx(q_full, (uint32_t)(tiles * C::HALVES * tpt * a.G * 128));
-                    for (int t = 0; t < tiles; ++t)
-                        for (int hf = 0; hf < C::HALVES; ++hf)
-                            tma_load_3d(smem_u32(smem + t * C::TILE_BYTES + hf * C::HALF_BYTES), &args.tm_q, q_full, hf * 64, h * a.G, w.row0 + t * tpt);
-                }
-                __syncwarp();
                 const int32_t* own_pages = seg_pages(a, w.seg);
                 const int32_t* front_pages = nf ? seg_pages(a, w.front) : own_pages;
                 for (int kt = ka; kt < kb; ++kt) {
@@ -292,7 +272,6 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                             place = key & ((1 << a.page_shift) - 1);
                         }
                     }
-#pragma unroll
                     for (int kv = 0; kv < 2; ++kv) {
                         if (!wait_bounded(&empty[st], ph ^ 1u, abort_flag, 62)) goto stop_loads;
                         if (lane == 0) mbar_arrive_expect_tx(&full[st], C::TILE_BYTES);
@@ -302,6 +281,16 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                                         half * 64, place, h, page);
                         ++n_load;
                         if (++st == STAGES) { st = 0; ph ^= 1u; }
+                        if (kt > ka || kv) continue;
+                        // behind the first K: Q, whose place is free when the unit before has no more S to come
+                        if (!wait_bounded(q_empty, q_ph ^ 1u, abort_flag, 61)) goto stop_loads;
+                        q_ph ^= 1u;
+                        const int tiles = w.pair ? 2 : 1;
+                        if (lane == 0) mbar_arrive_expect_tx(q_full, (uint32_t)(tiles * C::HALVES * tpt * a.G * 128));
+                        __syncwarp();
+                        if (lane < tiles * C::HALVES)
+                            tma_load_3d(smem_u32(smem + mine * C::QTILE_BYTES + half * C::QHALF_BYTES), &args.tm_q, q_full, half * 64, h * a.G,
+                                        w.row0 + mine * tpt);
                     }
                 }
                 __syncwarp();
@@ -317,80 +306,114 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                     wait_bounded(&full[i % STAGES], (i / STAGES) & 1u, never, 63);
                 wait_bounded(q_full, q_ph ^ 1u, never, 64);
             }
-        } else if (warp == 9) {
-            // --------------------------------------------------------------------------------------- MMA
-            const uint32_t ring0 = smem_u32(ring), q0 = smem_u32(smem);
-            const uint64_t k_hi = smem_desc_sw128(0), v_hi = smem_desc_sw128_mn(0, C::HALVES > 1 ? C::HALF_BYTES : 1024);
-            constexpr uint32_t IDESC_S = idesc_bf16(128, 128), IDESC_O = idesc_bf16(128, D) | IDESC_B_MN;
-            uint32_t base = 0;                 // loads of the units before
-            uint32_t q_ph = 0, p_ph[2] = {0, 0}, oe_ph[2] = {1, 1}, u_ph = 0;
+        } else if (warp == NSW + 3) {
+            // ----------------------------------------------------------------------------- ends of V lists
+            // Behind the last key of a list the page holds whatever was there before: a NaN or Inf would survive its weight of 0.  The
+            // MMA thread says when such a tile is there and waits for it to be cleaned.
+            uint32_t base = 0, u_ph = 0, ve_ph = 0;
             int b = 0;
             while (true) {
                 if (!wait_bounded(&u_full[b], u_ph, abort_flag, 77)) goto done;
                 const WideUnit& w = units[b];
-                const int n = w.n, pair = w.pair, cnt[2] = {w.cnt[0], w.cnt[1]};
+                const int n = w.n;
                 if (n == 0) break;
+                for (int kt = w.nf > w.ka ? w.nf - 1 : w.ka + n - 1; kt < w.ka + n; kt = w.ka + n - 1 > kt ? w.ka + n - 1 : w.ka + n) {
+                    const int left = unit_left(w, kt);
+                    if (left >= AT_WIDE_KEYS) continue;
+                    const uint32_t ld = base + 2 * (kt - w.ka) + 1, stg = ld % STAGES;
+                    if (!wait_bounded(v_end, ve_ph, abort_flag, 80)) goto done;
+                    ve_ph ^= 1u;
+                    uint8_t* v = ring + stg * C::TILE_BYTES;
+                    for (int c = left * 8 + lane; c < AT_WIDE_KEYS * 8; c += 32)
+                        for (int hf = 0; hf < C::HALVES; ++hf) *reinterpret_cast<uint4*>(v + hf * C::HALF_BYTES + c * 16) = make_uint4(0u, 0u, 0u, 0u);
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(v_clean);
+                }
+                base += 2 * (uint32_t)n;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&u_empty[b]);
+                if (++b == 2) { b = 0; u_ph ^= 1u; }
+            }
+        } else {
+            // --------------------------------------------------------------------------------------- MMA
+            // The whole warp walks through this (one elected lane issues), and what it reads from shared memory goes through a shuffle: only
+            // then do the descriptors stay in uniform registers.  Run by one thread, every MMA took two to three times as long to issue.
+            auto uni = [](int x) { return __shfl_sync(0xFFFFFFFFu, x, 0); };
+            const uint64_t q_desc = smem_desc_sw128(smem_u32(smem)), k_desc = smem_desc_sw128(ring0);
+            const uint64_t v_desc = smem_desc_sw128_mn(ring0, C::HALVES > 1 ? C::HALF_BYTES : 1024);
+            constexpr uint32_t IDESC_S = idesc_bf16(128, AT_WIDE_KEYS), IDESC_O = idesc_bf16(128, D) | IDESC_B_MN;
+            uint32_t base = 0;                 // loads of the units before
+            uint32_t q_ph = 0, p_ph = 0, se_ph = 3, oe_ph = 1, u_ph = 0, vc_ph = 0;
+            int b = 0;
+            while (true) {
+                if (!wait_bounded(&u_full[b], u_ph, abort_flag, 78)) goto done;
+                const WideUnit& w = units[b];
+                const int n = uni(w.n), cnt0 = uni(w.cnt[0]), cnt1 = uni(w.cnt[1]), pair = uni(w.pair), ka = uni(w.ka);
+                const int nf = uni(w.nf), plen = uni(w.plen), klen = uni(w.klen);
+                const uint32_t two = pair ? 2 : 4;       // loads from one key tile of a stream to the next
+                if (n == 0) break;
+                const int end_front = plen % AT_WIDE_KEYS ? nf - 1 : -1, end_own = klen % AT_WIDE_KEYS ? nf + klen / AT_WIDE_KEYS : -1;
                 if (!wait_bounded(q_full, q_ph, abort_flag, 65)) goto done;
                 q_ph ^= 1u;
-                // S_s(i): product of the stream's rows with its i-th key tile
-                auto issue_s = [&](int s, int i) -> bool {
-                    const uint32_t ld = base + 2 * unit_load(w, s, i), stg = ld % STAGES;
-                    if (!wait_bounded(&full[stg], (ld / STAGES) & 1u, abort_flag, 66)) return false;
-                    tc_fence_after();
-                    if (elect_one()) {
-                        const uint32_t qa = q0 + (pair && s ? C::TILE_BYTES : 0), kb = ring0 + stg * C::TILE_BYTES;
+                const int most = max(cnt0, cnt1);
+                // Step j: S0(j), P V of stream 1's tile j - 2, S1(j), P V of stream 0's tile j - 1: the order in which their inputs come when the
+                // streams are half a period apart.
+                for (int j = 0; j <= most + 1; ++j) {
 #pragma unroll
-                        for (int k = 0; k < D / 16; ++k) {
-                            const uint32_t off = (k / 4) * C::HALF_BYTES + (k % 4) * 32;
-                            mma_f16(tmem + C::TM_S + s * 128, k_hi | (uint64_t)((qa + off) >> 4), k_hi | (uint64_t)((kb + off) >> 4), IDESC_S, k ? 1u : 0u);
-                        }
-                        tc_commit(&s_full[s]);
-                        if (!pair || s == 1) tc_commit(&empty[stg]);
-                    }
-                    __syncwarp();
-                    return true;
-                };
-                for (int s = 0; s < 2; ++s)
-                    if (cnt[s] > 0 && !issue_s(s, 0)) goto done;
-                const int most = max(cnt[0], cnt[1]);
-                for (int i = 0; i < most; ++i) {
                     for (int s = 0; s < 2; ++s) {
-                        if (i >= cnt[s]) continue;
-                        if (i == 0) {      // the epilogue of the unit before has read O
-                            if (!wait_bounded(&o_empty[s], oe_ph[s], abort_flag, 67)) goto done;
-                            oe_ph[s] ^= 1u;
-                        }
-                        const uint32_t ld = base + 2 * unit_load(w, s, i) + 1, stg = ld % STAGES;
-                        if (!wait_bounded(&full[stg], (ld / STAGES) & 1u, abort_flag, 68)) goto done;
-                        const int left = unit_left(w, unit_tile(w, s, i));
-                        if (left < AT_WIDE_KEYS && (s == 0 || !pair || i >= cnt[0])) {
-                            // Behind the last key the page holds whatever was there before: a NaN or Inf would survive its weight of 0.
-                            uint8_t* v = ring + stg * C::TILE_BYTES;
-                            for (int c = left * 8 + lane; c < AT_WIDE_KEYS * 8; c += 32)
+                        const int cnt = s ? cnt1 : cnt0;
+                        const uint32_t first = base + (pair ? 0 : 2 * s);                 // the stream's first K; V is the load behind it
+                        if (j < cnt) {
+                            const uint32_t ld = first + j * two, stg = ld % STAGES;
+                            if (!wait_bounded(&full[stg], (ld / STAGES) & 1u, abort_flag, 66)) goto done;
+                            if (!wait_bounded(&s_empty[s], (se_ph >> s) & 1u, abort_flag, 84)) goto done;     // the S before has been read
+                            se_ph ^= 1u << s;
+                            tc_fence_after();
+                            const uint64_t qd = q_desc + (pair ? s * (C::QTILE_BYTES >> 4) : 0), kd = k_desc + stg * (C::TILE_BYTES >> 4);
+                            if (elect_one()) {
 #pragma unroll
-                                for (int hf = 0; hf < C::HALVES; ++hf)
-                                    *reinterpret_cast<uint4*>(v + hf * C::HALF_BYTES + c * 16) = make_uint4(0u, 0u, 0u, 0u);
-                            fence_proxy_async_smem();
+                                for (int k = 0; k < D / 16; ++k)
+                                    mma_f16(tmem + C::TM_S + s * AT_WIDE_KEYS, qd + (((k / 4) * C::QHALF_BYTES + (k % 4) * 32) >> 4),
+                                            kd + (((k / 4) * C::HALF_BYTES + (k % 4) * 32) >> 4), IDESC_S, k ? 1u : 0u);
+                                tc_commit(&s_full[s]);
+                                if (!pair || s == 1) tc_commit(&empty[stg]);
+                                if (j == cnt - 1 && (s ? cnt1 >= cnt0 : cnt0 > cnt1)) tc_commit(q_empty);      // no more S of this unit
+                            }
                             __syncwarp();
                         }
-                        if (!wait_bounded(&p_full[s], p_ph[s], abort_flag, 69)) goto done;
-                        p_ph[s] ^= 1u;
-                        tc_fence_after();
-                        if (elect_one()) {
-                            const uint32_t vb = ring0 + stg * C::TILE_BYTES;
+                        // between the two S: stream 1's P V; behind them: stream 0's
+                        const int t = s ^ 1, i = j - 1 - t, pcnt = t ? cnt1 : cnt0;
+                        if (i >= 0 && i < pcnt) {
+                            const uint32_t ld = base + (pair ? 0 : 2 * t) + i * two + 1, stg = ld % STAGES;
+                            if (i == 0 && (t == 0 || cnt0 == 0)) {      // the epilogue of the unit before has read O
+                                if (!wait_bounded(o_empty, oe_ph, abort_flag, 67)) goto done;
+                                oe_ph ^= 1u;
+                            }
+                            if (!wait_bounded(&full[stg], (ld / STAGES) & 1u, abort_flag, 68)) goto done;
+                            const int kt = ka + (int)(ld - base) / 2;
+                            if ((kt == end_front || kt == end_own) && (t == 0 || !pair || i >= cnt0)) {
+                                if (lane == 0) mbar_arrive(v_end);
+                                __syncwarp();
+                                if (!wait_bounded(v_clean, vc_ph, abort_flag, 81)) goto done;
+                                vc_ph ^= 1u;
+                            }
+                            if (!wait_bounded(&p_full[t], (p_ph >> t) & 1u, abort_flag, 69)) goto done;
+                            p_ph ^= 1u << t;
+                            tc_fence_after();
+                            const uint64_t vd = v_desc + stg * (C::TILE_BYTES >> 4);
+                            if (elect_one()) {
 #pragma unroll
-                            for (int k = 0; k < 8; ++k)
-                                mma_f16_ts(tmem + C::TM_O + s * D, tmem + C::TM_S + s * 128 + k * 8, v_hi | (uint64_t)((vb + k * 2048) >> 4), IDESC_O,
-                                           (i | k) ? 1u : 0u);
-                            if (!pair || s == 1) tc_commit(&empty[stg]);
-                            if (i == cnt[s] - 1) tc_commit(&o_full[s]);
+                                for (int k = 0; k < AT_WIDE_KEYS / 16; ++k)
+                                    mma_f16_ts(tmem + C::TM_O + t * D, tmem + C::TM_P + t * (AT_WIDE_KEYS / 2) + k * 8, vd + k * 128, IDESC_O,
+                                               (i | k) ? 1u : 0u);
+                                tc_commit(&pv_done[t]);
+                                if (!pair || t == 1) tc_commit(&empty[stg]);
+                            }
+                            __syncwarp();
                         }
-                        __syncwarp();
-                        if (i + 1 < cnt[s] && !issue_s(s, i + 1)) goto done;
                     }
                 }
-                if (elect_one()) tc_commit(q_empty);
-                __syncwarp();
                 base += 2 * (uint32_t)n;
                 if (lane == 0) mbar_arrive(&u_empty[b]);
                 if (++b == 2) { b = 0; u_ph ^= 1u; }
@@ -398,38 +421,43 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
         }
     } else {
         // ------------------------------------------------------------------------------------------ softmax
-        regs_inc<AW_REGS_SOFTMAX>();
-        const int s = warp >> 2;
+        const int s = warp >> 2;                                         // stream
         const int r = threadIdx.x & 127;                                 // row of the tile = TMEM lane
-        const int my_tok = r / a.G, my_head = r % a.G;
+        const int my_tok = r / a.G;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t t_s = tmem + lanes + C::TM_S + s * 128, t_o = tmem + lanes + C::TM_O;
-        uint32_t s_ph = 0, o_ph[2] = {0, 0}, j_ph = 0, u_ph = 0;
+        const uint32_t t_s = tmem + lanes + C::TM_S + s * AT_WIDE_KEYS, t_p = tmem + lanes + C::TM_P + s * (AT_WIDE_KEYS / 2), t_o = tmem + lanes + C::TM_O;
+        const float scale = a.scale_log2;
+        uint32_t s_ph = 0, pv_ph = 0, e_ph = 0, u_ph = 0;
         int b = 0;
         while (true) {
-            if (!wait_bounded(&u_full[b], u_ph, abort_flag, 78)) goto done;
+            if (!wait_bounded(&u_full[b], u_ph, abort_flag, 79)) goto done;
             const WideUnit& w = units[b];
             if (w.n == 0) break;
             float m = -INFINITY, l = 0.0f;
+            const int cnt = w.cnt[s];
             {
                 const int tok = (w.pair ? s * tpt : 0) + my_tok;         // token inside the unit
                 const bool valid = my_tok < tpt && tok < w.tokens;
                 const int nf = w.nf, step = w.pair ? 1 : 2;
-                // keys that the row sees from the first key of the own tile 0 on; a row that is not there sees all
+                // own keys that the row sees; a row that is not there sees all
                 const int sees = valid && w.causal ? max(w.klen - w.causal + w.tok0 + tok + 1, 0) : w.klen;
                 int kt = w.pair ? w.ka : w.ka + s;
-                for (int i = 0, cnt = w.cnt[s]; i < cnt; ++i, kt += step) {
+                for (int i = 0; i < cnt; ++i, kt += step) {
                     if (!wait_bounded(&s_full[s], s_ph, abort_flag, 70)) goto done;
                     s_ph ^= 1u;
                     tc_fence_after();
-                    uint32_t v[4][32];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) tmem_ld_32x32(t_s + j * 32, v[j]);
+                    uint32_t v[2][32];
+                    tmem_ld_32x32(t_s, v[0]);
+                    tmem_ld_32x32(t_s + 32, v[1]);
+                    const int left = kt < nf ? w.plen - kt * AT_WIDE_KEYS : sees - (kt - nf) * AT_WIDE_KEYS;      // keys of the tile that the row sees
+                    const bool whole = __all_sync(0xFFFFFFFFu, left >= AT_WIDE_KEYS);
                     tmem_ld_wait();
-                    const int left = kt < nf ? w.plen - kt * AT_WIDE_KEYS : sees - (kt - nf) * AT_WIDE_KEYS;   // keys of the tile that the row sees
-                    if (!__all_sync(0xFFFFFFFFu, left >= AT_WIDE_KEYS)) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&s_empty[s]);
+                    if (!whole) {
 #pragma unroll
-                        for (int j = 0; j < 4; ++j)
+                        for (int j = 0; j < 2; ++j)
 #pragma unroll
                             for (int e = 0; e < 32; ++e)
                                 if (j * 32 + e >= left) v[j][e] = 0xFF800000u;
@@ -437,139 +465,163 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                     float mx[4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        mx[j] = __uint_as_float(v[j][0]);
+                        mx[j] = fmaxf(__uint_as_float(v[0][j]), __uint_as_float(v[1][j]));
 #pragma unroll
-                        for (int e = 1; e < 31; e += 2) mx[j] = max3(mx[j], __uint_as_float(v[j][e]), __uint_as_float(v[j][e + 1]));
-                        mx[j] = fmaxf(mx[j], __uint_as_float(v[j][31]));
+                        for (int e = j + 4; e < 32; e += 4) mx[j] = max3(mx[j], __uint_as_float(v[0][e]), __uint_as_float(v[1][e]));
                     }
-                    const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2;
-                    float f = 1.0f;
+                    const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
                     const bool move = top > m + AT_SLACK;
-                    if (move) {
-                        f = exp2_approx(m - top);
-                        m = top;
-                        l *= f;
-                    }
+                    const float f = move ? exp2_approx(m - top) : 1.0f;
+                    if (move) m = top;
                     const float ref = m == -INFINITY ? 0.0f : -m;
-                    const uint64_t scale2 = pack2(a.scale_log2, a.scale_log2), ref2 = pack2(ref, ref);
+                    const uint64_t scale2 = pack2(scale, scale), ref2 = pack2(ref, ref);
                     uint64_t sum[2] = {0, 0};
+                    uint32_t pk[2][16];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        uint32_t pk[16];
+                    for (int j = 0; j < 2; ++j)
 #pragma unroll
                         for (int e = 0; e < 32; e += 2) {
                             float p0, p1;
                             unpack2(fma2(pack2(__uint_as_float(v[j][e]), __uint_as_float(v[j][e + 1])), scale2, ref2), p0, p1);
                             p0 = exp2_approx(p0);
                             p1 = exp2_approx(p1);
-                            sum[(e >> 1) & 1] = add2(sum[(e >> 1) & 1], pack2(p0, p1));
-                            pk[e / 2] = bf162_bits(__floats2bfloat162_rn(p0, p1));
+                            sum[(e / 2) & 1] = add2(sum[(e / 2) & 1], pack2(p0, p1));
+                            pk[j][e / 2] = bf162_bits(__floats2bfloat162_rn(p0, p1));
                         }
-                        tmem_st_32x16(t_s + j * 16, pk);
-                    }
-                    float s0, s1;
-                    unpack2(add2(sum[0], sum[1]), s0, s1);
-                    l += s0 + s1;
-                    if (__any_sync(0xFFFFFFFFu, move) && i > 0) {
+                    if (i > 0) {      // the P V before has read P, and O is not being written
+                        if (!wait_bounded(&pv_done[s], pv_ph, abort_flag, 82)) goto done;
+                        pv_ph ^= 1u;
+                        if (__any_sync(0xFFFFFFFFu, move)) {
+                            tc_fence_after();
+#pragma unroll 1
+                            for (int c = 0; c < D; c += 16) {
+                                uint32_t o[16];
+                                tmem_ld_x16(t_o + s * D + c, o);
+                                tmem_ld_wait();
 #pragma unroll
-                        for (int c = 0; c < D; c += 32) {
-                            uint32_t o[32];
-                            tmem_ld_32x32(t_o + s * D + c, o);
-                            tmem_ld_wait();
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                            tmem_st_32x32(t_o + s * D + c, o);
+                                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                                tmem_st_32x16(t_o + s * D + c, o);
+                            }
                         }
                     }
+                    tmem_st_32x16(t_p, pk[0]);
+                    tmem_st_32x16(t_p + 16, pk[1]);
                     tmem_st_wait();
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&p_full[s]);
+                    float s0, s1;
+                    unpack2(add2(sum[0], sum[1]), s0, s1);
+                    l = l * f + (s0 + s1);
                 }
             }
             // ---- the unit's rows: into O, or as (m, l, O) into the workspace
-            const bool pair = w.pair, have0 = w.cnt[0] > 0, have1 = w.cnt[1] > 0, have = s ? have1 : have0;
-            float m1 = -INFINITY, l1 = 0.0f;
-            if (!pair) {
-                if (s == 1) {
-                    if (!wait_bounded(j_empty, j_ph ^ 1u, abort_flag, 74)) goto done;
-                    s_ml[r] = make_float2(m, l);
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(j_full);
-                } else {
-                    if (!wait_bounded(j_full, j_ph, abort_flag, 75)) goto done;
-                    m1 = s_ml[r].x;
-                    l1 = s_ml[r].y;
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(j_empty);
-                }
-                j_ph ^= 1u;
+            const bool pair = w.pair, have0 = w.cnt[0] > 0, have1 = w.cnt[1] > 0;
+            if (cnt > 0) {
+                if (!wait_bounded(&pv_done[s], pv_ph, abort_flag, 71)) goto done;
+                pv_ph ^= 1u;
             }
-            if (pair || s == 0) {
-                const bool two = !pair && have1;
-                if (have && !wait_bounded(&o_full[s], o_ph[s], abort_flag, 71)) goto done;
-                if (two && !wait_bounded(&o_full[1], o_ph[1], abort_flag, 72)) goto done;
-                tc_fence_after();
-                const int tok = (pair ? s * tpt : 0) + my_tok, hq = w.h * a.G + my_head, out = w.out;
-                const bool valid = my_tok < tpt && tok < w.tokens;
-                const float mn = fmaxf(m, m1);
-                const float f0 = mn == -INFINITY ? 0.0f : exp2_approx(m - mn), f1 = mn == -INFINITY ? 0.0f : exp2_approx(m1 - mn);
-                const float lt = l * f0 + l1 * f1;
-                const bool direct = !(out & (OUT_SPLIT | OUT_TWO));
-                const float inv = !direct ? 1.0f : lt > 0.0f || lt != lt ? 1.0f / lt : 0.0f;
-                const float c0 = f0 * inv, c1 = f1 * inv;
-                const int64_t token = w.row0 + tok, row = token * a.Hq + hq;
-                const int64_t at = out & OUT_SPLIT ? ((int64_t)blockIdx.x * 2 + (out & OUT_LATER ? 1 : 0)) * (2 * AT_WIDE_TILE) + (pair ? s * AT_WIDE_TILE : 0) + r : row;
-                float* part = (out & OUT_SPLIT ? a.wide_part : a.dense[out & OUT_OWN ? 1 : 0]) + at * D;
-                uint16_t* op = a.o + token * a.ldo + (int64_t)hq * D;
-#pragma unroll
-                for (int c = 0; c < D; c += 32) {
-                    uint32_t o[32];
-                    if (have) {
-                        tmem_ld_32x32(t_o + s * D + c, o);
-                        tmem_ld_wait();
-                    }
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) o[e] = have && c0 != 0.0f ? __float_as_uint(__uint_as_float(o[e]) * c0) : 0u;
-                    if (two) {
-                        uint32_t o1[32];
-                        tmem_ld_32x32(t_o + D + c, o1);
-                        tmem_ld_wait();
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(fmaf(__uint_as_float(o1[e]), c1, __uint_as_float(o[e])));
-                    }
-                    if (valid) {
-                        if (direct) {
-#pragma unroll
-                            for (int e = 0; e < 32; e += 8) {
-                                uint32_t h[4];
-#pragma unroll
-                                for (int y = 0; y < 4; ++y)
-                                    h[y] = bf162_bits(__floats2bfloat162_rn(__uint_as_float(o[e + 2 * y]), __uint_as_float(o[e + 2 * y + 1])));
-                                *reinterpret_cast<uint4*>(op + c + e) = make_uint4(h[0], h[1], h[2], h[3]);
-                            }
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 32; e += 4)
-                                *reinterpret_cast<uint4*>(part + c + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
-                        }
-                    }
-                }
-                if (valid) {
-                    if (!direct) (out & OUT_SPLIT ? a.wide_ml : a.dense_ml[out & OUT_OWN ? 1 : 0])[at] = make_float2(mn, lt);
-                    else if (a.lse) a.lse[row] = lt == 0.0f ? -INFINITY : (mn + log2f(lt)) * 0.69314718055994531f;
-                }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) {
-                    if (have) mbar_arrive(&o_empty[s]);
-                    if (two) mbar_arrive(&o_empty[1]);
-                }
-            }
-            o_ph[0] ^= have0;
-            o_ph[1] ^= have1;
+            float2* ml = unit_ml + (e_ph & 1) * 256;
+            ml[s * 128 + r] = make_float2(m, l);
             __syncwarp();
-            if (lane == 0) mbar_arrive(&u_empty[b]);
+            if (lane == 0) mbar_arrive(e_full);
+            if (!wait_bounded(e_full, e_ph & 1, abort_flag, 83)) goto done;
+            e_ph ^= 1u;
+            tc_fence_after();
+            // both row tiles filled: a stream's own rows; else the two warpgroups share out the columns of the one tile, O being the two
+            // streams' joined
+            const int first = pair ? s : 0;
+            const bool joined = !pair && have1, have = first ? have1 : have0;
+            m = ml[first * 128 + r].x;
+            l = ml[first * 128 + r].y;
+            float c0 = m == -INFINITY ? 0.0f : 1.0f, c1 = 0.0f;
+            if (joined) {
+                const float m1 = ml[128 + r].x, l1 = ml[128 + r].y, mn = fmaxf(m, m1);
+                c0 = mn == -INFINITY ? 0.0f : exp2_approx(m - mn);
+                c1 = mn == -INFINITY ? 0.0f : exp2_approx(m1 - mn);
+                m = mn;
+                l = l * c0 + l1 * c1;
+            }
+            const int out = w.out, tok0 = pair ? s * tpt : 0, tokens = w.tokens, hq0 = w.h * a.G, row0 = w.row0;
+            const bool direct = !(out & (OUT_SPLIT | OUT_TWO));
+            if (direct) {
+                const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+                c0 *= inv;
+                c1 *= inv;
+            }
+            const int slot0 = AT_FEW_SLOTS + (blockIdx.x * 2 + (out & OUT_LATER ? 1 : 0)) * (2 * AT_WIDE_TILE) + (pair ? s * AT_WIDE_TILE : 0);
+            // row of the partial results (or of lse) that tile row x goes to, -1: none
+            auto place = [&](int x) -> int {
+                const int t = x / a.G;
+                if (t >= tpt || tok0 + t >= tokens) return -1;
+                if (out & OUT_SPLIT) return slot0 + x;
+                const int row = (row0 + tok0 + t) * a.Hq + hq0 + x - t * a.G;
+                return direct ? row : dense_row(a, out & OUT_OWN ? 1 : 0, row);
+            };
+            if (pair || s == 0) {
+                const int at = place(r);
+                if (at >= 0) {
+                    if (!direct) a.ml[at] = make_float2(m, l);
+                    else if (a.lse) a.lse[at] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+                }
+            }
+            // A thread holds a row; through shared memory (16-byte units swizzled by the row) four lanes write 64 bytes of one row side by side,
+            // eight rows at a time.  (Written by the rows' own threads, 16 bytes of 32 rows in one store, a unit took 7000 to 10000
+            // cycles to get out.)  The loop is kept rolled: code that runs once comes out of L2 line by line, slower than the data.
+            int64_t to[4];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                const int at = place((warp & 3) * 32 + y * 8 + lane / 4);
+                to[y] = at < 0 ? -1 : direct ? (int64_t)(at / a.Hq) * a.ldo + (int64_t)(at % a.Hq) * D : (int64_t)at * D;
+            }
+            uint8_t* tile = out_tiles + warp * 2048;
+            const int cols = pair ? D : D / 2, col0 = pair ? 0 : s * cols;
+            const int e = lane & 3, wsw = (lane >> 1) & 3, rsw = (lane >> 3) & 3;
+#pragma unroll 1
+            for (int c = col0; c < col0 + cols; c += 16) {
+                float o[16];
+#pragma unroll
+                for (int y = 0; y < 16; ++y) o[y] = 0.0f;
+                uint32_t x[16];
+                if (have) {
+                    tmem_ld_x16(t_o + first * D + c, x);
+                    tmem_ld_wait();
+                    if (c0 != 0.0f) {
+#pragma unroll
+                        for (int y = 0; y < 16; ++y) o[y] = __uint_as_float(x[y]) * c0;
+                    }
+                }
+                if (joined) {
+                    tmem_ld_x16(t_o + D + c, x);
+                    tmem_ld_wait();
+                    if (c1 != 0.0f) {
+#pragma unroll
+                        for (int y = 0; y < 16; ++y) o[y] = fmaf(__uint_as_float(x[y]), c1, o[y]);
+                    }
+                }
+#pragma unroll
+                for (int y = 0; y < 4; ++y)
+                    *reinterpret_cast<float4*>(tile + lane * 64 + ((y ^ wsw) * 16)) = make_float4(o[4 * y], o[4 * y + 1], o[4 * y + 2], o[4 * y + 3]);
+                __syncwarp();
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    const float4 q = *reinterpret_cast<const float4*>(tile + (y * 8 + lane / 4) * 64 + ((e ^ rsw) * 16));
+                    if (to[y] >= 0) {
+                        if (direct)
+                            *reinterpret_cast<uint2*>(a.o + to[y] + c + e * 4) =
+                                make_uint2(bf162_bits(__floats2bfloat162_rn(q.x, q.y)), bf162_bits(__floats2bfloat162_rn(q.z, q.w)));
+                        else
+                            *reinterpret_cast<float4*>(a.part + to[y] + c + e * 4) = q;
+                    }
+                }
+                __syncwarp();
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(o_empty);
+                mbar_arrive(&u_empty[b]);
+            }
             if (++b == 2) { b = 0; u_ph ^= 1u; }
         }
     }
@@ -578,7 +630,7 @@ done:
     __syncwarp();
     tc_fence_before();
     __syncthreads();
-    if (warp == 9) {
+    if (warp == NSW + 1) {
         if (*abort_flag && lane == 0) {
             // gave up somewhere: let outstanding tensor-core work retire before TMEM goes away
             tc_commit(drain_bar);
@@ -618,13 +670,12 @@ static cudaError_t launch_attn_d(const AttnWideArgs& w, bool wide, cudaStream_t 
             : a.few_hw == 2 ? launch_attn_few<D, 2, false>(a, wide, st) : launch_attn_few<D, 1, false>(a, wide, st);
         if (e != cudaSuccess) return e;
     }
-    const int wide_split = 8, few_split = a.few_hw;
+    // Blocks with nothing to do cost a wave of the grid too: few-row units are cut small only where there is nothing else.
+    const int wide_split = (int64_t)a.T * a.G >= 2048 ? 8 : 2, few_split = wide ? 1 : a.few_hw;
     const int wide_blocks = wide ? a.wide_ctas * wide_split : 0, few_blocks = a.few_ctas * few_split;
-    const int tokens = (int)std::min<int64_t>(32, std::max<int64_t>(1, (int64_t)a.T * a.Hk / (4 * AT_MAX_SMS)));
-    const int64_t token_blocks = a.P ? ((int64_t)a.T + tokens - 1) / tokens * a.Hk : 0;
-    if (wide_blocks + few_blocks + token_blocks > 0x7FFFFFFF) return cudaErrorInvalidConfiguration;
-    return launch_pdl(attn_join_kernel<D>, dim3((unsigned)(wide_blocks + few_blocks + token_blocks)), dim3(AT_JOIN_THREADS), 0, st, a, wide_blocks,
-                      wide_split, few_blocks, few_split, tokens);
+    const int token_blocks = a.P ? (int)std::min<int64_t>(3 * AT_MAX_SMS, ((int64_t)a.T * a.Hq + AT_JOIN_WARPS - 1) / AT_JOIN_WARPS) : 0;
+    return launch_pdl(attn_join_kernel<D>, dim3(wide_blocks + few_blocks + token_blocks), dim3(AT_JOIN_THREADS), 0, st, a, wide_blocks, wide_split,
+                      few_blocks, few_split);
 }
 
 cudaError_t launch_attn(const AttnWideArgs& w, int D, bool wide, cudaStream_t st) {

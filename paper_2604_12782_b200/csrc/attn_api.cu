@@ -1,6 +1,8 @@
 // Host side of the calls around the paged key/value cache: validation, workspace layout, launches.
 #include <math.h>
 
+#include <algorithm>
+
 #include "../../include/osc.h"
 #include "common.cuh"
 
@@ -41,28 +43,24 @@ static osc_status encode_heads(CUtensorMap* tm, const void* base, int rank, cons
 }
 
 struct AttnLayout {
-    size_t few_start, wide_start, share, cut[2], seg, tok_req, dense[2], dense_ml[2], few_part, few_ml, wide_part, wide_ml, total;
+    size_t few_start, wide_start, share, cut[2], seg, tok_req, part, ml, total;
 };
 static AttnLayout attn_layout(int T, int n_q, int D, int R, int P) {
     AttnLayout l;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t o = at; at += align256(bytes); return o; };
-    const size_t S = (size_t)R + P + 1, rows = (size_t)T * n_q;
-    l.few_start = take(S * 8);
-    l.wide_start = take(S * 8);
-    l.share = take(24);
+    const size_t S = (size_t)R + P;
+    // rows of partial results; rows with two sources exist only where there are prefixes
+    const size_t rows = AT_FEW_SLOTS + AT_WIDE_SLOTS + (P ? 2 * (size_t)T * n_q : 0);
+    l.few_start = take((S + 1) * 4);
+    l.wide_start = take((S + 1) * 4);
+    l.share = take(12);
     l.cut[0] = take((size_t)AT_FEW_CTAS * sizeof(CutUnit));
     l.cut[1] = take((size_t)AT_WIDE_CTAS * sizeof(CutUnit));
-    l.seg = take((S - 1) * sizeof(Segment));
+    l.seg = take(S * sizeof(Segment));
     l.tok_req = take(P ? (size_t)T * 4 : 0);
-    for (int i = 0; i < 2; ++i) {   // rows with two sources exist only where there are prefixes
-        l.dense[i] = take(P ? rows * D * 4 : 0);
-        l.dense_ml[i] = take(P ? rows * 8 : 0);
-    }
-    l.few_part = take((size_t)AT_FEW_CTAS * 2 * AT_FEW_HEADS * AT_FEW_ROWS * D * 4);
-    l.few_ml = take((size_t)AT_FEW_CTAS * 2 * AT_FEW_HEADS * AT_FEW_ROWS * 8);
-    l.wide_part = take((size_t)AT_WIDE_CTAS * 4 * AT_WIDE_TILE * D * 4);
-    l.wide_ml = take((size_t)AT_WIDE_CTAS * 4 * AT_WIDE_TILE * 8);
+    l.part = take(rows * D * 4);
+    l.ml = take(rows * 8);
     l.total = at;
     return l;
 }
@@ -168,13 +166,19 @@ osc_status osc_paged_attention(const void* Q, int T, int64_t ldq, int n_q, const
         return fail(OSC_ERR_SHAPE, "ldq = %lld, ldo = %lld < n_q * head_dim = %lld", (long long)ldq, (long long)ldo, (long long)n_q * D);
     if (ldq % 8 || ldo % 8 || !aligned16(Q) || !aligned16(O) || !aligned16(workspace))
         return fail(OSC_ERR_ALIGN, "Q, O and workspace must be 16-byte aligned, ldq and ldo multiples of 8");
-    // tile counts of a segment are ints
+    // Counts of tiles and of rows are ints on the device.  The line cannot hold more than every request's units over all the keys its
+    // table names (16 keys and 16 rows to a tile at the least), nor more than that of all rows over the prefix tables.
     const int64_t own_keys = (int64_t)cols * cache->page_size, front_keys = P ? (int64_t)prefix_cols * cache->page_size : 0;
-    const int64_t few_units = ((int64_t)T * (n_q / cache->n_heads)) / 16 + 1;
+    const int64_t few_units = ((int64_t)T * (n_q / cache->n_heads)) / AT_FEW_ROWS + (int64_t)R + P;
+    const int64_t wide_units = few_units / 8 + (int64_t)R + P;
+    const int hw = cache->n_heads % 4 == 0 ? 4 : cache->n_heads % 2 == 0 ? 2 : 1;
+    const double most_few = (double)few_units * (cache->n_heads / hw) * (std::max(own_keys, front_keys) / (64.0 / hw) + 1.0);
+    const double most_wide = (double)wide_units * cache->n_heads * ((own_keys + front_keys) / 64.0 + 2.0);
+    const double most_request = ((double)R + P) * (cache->n_heads / hw) * (std::max(own_keys, front_keys) / (64.0 / hw) + 1.0);
     if (own_keys > 0x20000000 || front_keys > 0x20000000)
         return fail(OSC_ERR_SHAPE, "table columns hold %lld / %lld keys, at most 2^29 are supported", (long long)own_keys, (long long)front_keys);
-    if ((few_units / 4 + 1) * ((own_keys + front_keys) / 128 + 2) > 0x7FFFFFFFll)
-        return fail(OSC_ERR_SHAPE, "T = %d rows over up to %lld keys: too many tiles", T, (long long)(own_keys + front_keys));
+    if (most_wide >= 2147483648.0 || most_request >= 2147483648.0 || (cache->n_pages == 0 && most_few >= 2147483648.0) || (int64_t)T * n_q > 0x20000000)
+        return fail(OSC_ERR_SHAPE, "T = %d, R = %d, P = %d over up to %lld keys: too many tiles", T, R, P, (long long)(own_keys + front_keys));
     const AttnLayout l = attn_layout(T, n_q, D, R, P);
     if (workspace_bytes < l.total) return fail(OSC_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, l.total);
     DeviceInfo di;
@@ -190,13 +194,13 @@ osc_status osc_paged_attention(const void* Q, int T, int64_t ldq, int n_q, const
     a.T = T; a.Hq = n_q; a.Hk = cache->n_heads; a.G = n_q / cache->n_heads; a.head_dim = D; a.R = R; a.P = P; a.n_pages = cache->n_pages;
     while ((1 << a.page_shift) < cache->page_size) ++a.page_shift;
     a.scale_log2 = scale * 1.44269504088896341f;
-    a.few_hw = a.Hk % 4 == 0 ? 4 : a.Hk % 2 == 0 ? 2 : 1;
+    a.few_hw = hw;
     a.few_ctas = di.num_sms * 2 < AT_FEW_CTAS ? di.num_sms * 2 : AT_FEW_CTAS;
     a.wide_ctas = di.num_sms < AT_WIDE_CTAS ? di.num_sms : AT_WIDE_CTAS;
     // Up to 16 rows per key/value head a request is one unit of the few-row kernel, whatever the rest of the step is.  The tcgen05
     // kernel is launched where a segment may have more: a shared prefix, or requests with more new tokens than that.
     // (Nor may the 16-row units of a step whose max_new is wrong be too many to count.)
-    const bool wide = a.n_pages > 0 && (P > 0 || max_new == 0 || (int64_t)max_new * a.G > AT_FEW_ROWS || few_units * (own_keys / 16 + 1) > 0x7FFFFFFFll);
+    const bool wide = a.n_pages > 0 && (P > 0 || max_new == 0 || (int64_t)max_new * a.G > AT_FEW_ROWS || most_few >= 2147483648.0);
     a.wide_min_rows = wide ? AT_FEW_ROWS + 1 : 0x7FFFFFFF;
     if (wide) {
         const int64_t qd[3] = {D, n_q, T}, qs[3] = {1, D, ldq};
@@ -208,20 +212,14 @@ osc_status osc_paged_attention(const void* Q, int T, int64_t ldq, int n_q, const
         if (osc_status s = encode_heads(&w.tm_k, cache->k, 4, kd, ks, kb, "K")) return s;
         if (osc_status s = encode_heads(&w.tm_v, cache->v, 4, kd, ks, kb, "V")) return s;
     }
-    a.plan.few_start = reinterpret_cast<int64_t*>(ws + l.few_start);
-    a.plan.wide_start = reinterpret_cast<int64_t*>(ws + l.wide_start);
-    a.plan.share = reinterpret_cast<int64_t*>(ws + l.share);
+    a.plan.few_start = reinterpret_cast<int32_t*>(ws + l.few_start);
+    a.plan.wide_start = reinterpret_cast<int32_t*>(ws + l.wide_start);
+    a.plan.share = reinterpret_cast<int32_t*>(ws + l.share);
+    for (int i = 0; i < 2; ++i) a.plan.cut[i] = reinterpret_cast<CutUnit*>(ws + l.cut[i]);
     a.plan.seg = reinterpret_cast<Segment*>(ws + l.seg);
     a.plan.tok_req = reinterpret_cast<int32_t*>(ws + l.tok_req);
-    for (int i = 0; i < 2; ++i) {
-        a.plan.cut[i] = reinterpret_cast<CutUnit*>(ws + l.cut[i]);
-        a.dense[i] = reinterpret_cast<float*>(ws + l.dense[i]);
-        a.dense_ml[i] = reinterpret_cast<float2*>(ws + l.dense_ml[i]);
-    }
-    a.few_part = reinterpret_cast<float*>(ws + l.few_part);
-    a.few_ml = reinterpret_cast<float2*>(ws + l.few_ml);
-    a.wide_part = reinterpret_cast<float*>(ws + l.wide_part);
-    a.wide_ml = reinterpret_cast<float2*>(ws + l.wide_ml);
+    a.part = reinterpret_cast<float*>(ws + l.part);
+    a.ml = reinterpret_cast<float2*>(ws + l.ml);
     cudaError_t e = launch_attn(w, D, wide, static_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) return cuda_fail(e, "attention kernels");
     return OSC_OK;

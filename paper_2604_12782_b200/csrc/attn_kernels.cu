@@ -26,7 +26,7 @@ namespace osc {
 
 constexpr int AT_FEW_ROWS = 16;              // rows of a few-row unit
 constexpr int AT_WIDE_TILE = 128;            // rows of one tcgen05 tile; a wide unit has two of them
-constexpr int AT_WIDE_KEYS = 128;            // keys of its tiles
+constexpr int AT_WIDE_KEYS = 64;             // keys of its tiles
 constexpr int AT_MERGE_ROWS = 2 * AT_WIDE_TILE;  // a group whose requests all have at least this many rows has no prefix segment
 constexpr int AT_MAX_SMS = 148;
 constexpr int AT_FEW_CTAS = 2 * AT_MAX_SMS;  // most CTAs of the few-row kernel (two per SM)
@@ -39,28 +39,29 @@ struct __align__(16) Segment {
     int klen;                // keys: the prefix, or the request's own
     int plen;                // keys of the group's prefix in front of the own keys (merged groups), else 0
     int tiles;               // key tiles of all units of one head (of one head group on the few-row line)
+    int start;               // its first tile on its line
     int group;               // of a request: its group, -1: none (or one with an empty prefix)
-    int causal;              // 1: own keys, token i sees klen - n + i + 1 of them; 0: prefix, every token sees klen
     int flags;
 };
 constexpr int SEG_WIDE = 1;  // on the tcgen05 line
+constexpr int SEG_OWN = 4;   // own keys: token i sees klen - n + i + 1 of them; else a prefix: every token sees klen
 constexpr int SEG_TWO = 2;   // the rows have another source: O goes to the workspace, and the join looks at every row
 
 // A unit that the end of a CTA's share cuts, told by the first CTA that meets it; the join finds its pieces by it.
 struct __align__(16) CutUnit {
-    int64_t begin, share;    // its first tile, and the tiles of a share
+    int begin, share;        // its first tile, and the tiles of a share
     int tiles;               // 0: the share ends with a unit, or the unit's rows have two sources, or it was cut before
     int h, u;                // head (group) and row unit
     int t0, n;               // rows of the segment
-    int pad[3];
+    int pad;
 };
 
 struct AttnPlan {            // filled by attn_plan_kernel
-    int64_t* few_start;      // [S + 1] first tile of every segment on the few-row line
-    int64_t* wide_start;     // [S + 1] ... on the tcgen05 line
+    int32_t* few_start;      // [S + 1] first tile of every segment on the few-row line
+    int32_t* wide_start;     // [S + 1] ... on the tcgen05 line
     Segment* seg;            // [S]
     int32_t* tok_req;        // [T], where there are prefixes: the request of every token whose rows have two sources, else -1
-    int64_t* share;          // [3]: tiles of a share on the few-row line, on the tcgen05 line; whether any row has two sources
+    int32_t* share;          // [3]: tiles of a share on the few-row line, on the tcgen05 line; whether any row has two sources
     CutUnit* cut[2];         // [AT_FEW_CTAS], [AT_WIDE_CTAS]: filled by the attention kernels
 };
 
@@ -86,17 +87,19 @@ struct AttnArgs {
     int few_ctas, wide_ctas;
     float scale_log2;        // scale * log2(e)
     AttnPlan plan;
-    float* dense[2];         // [T * Hq][D]: whole-unit results where a row has two sources (0: prefix, 1: own keys)
-    float2* dense_ml[2];     // (m, l)
-    float* few_part;         // [AT_FEW_CTAS][2][few_hw][16][D]: first and last piece of every CTA
-    float2* few_ml;
-    float* wide_part;        // [AT_WIDE_CTAS][2][256][D]
-    float2* wide_ml;
+    // Partial results, row by row: O [D] in part, (m, l) in ml.  Rows [0, AT_FEW_SLOTS): the first and the last piece of every few-row
+    // CTA ([CTA][2][few_hw][16]); then those of the tcgen05 CTAs ([CTA][2][256]); then, where there are prefixes, twice T * Hq rows
+    // for whole units of rows with two sources (prefix, own keys).
+    float* part;
+    float2* ml;
 };
+constexpr int AT_FEW_SLOTS = AT_FEW_CTAS * 2 * AT_FEW_HEADS * AT_FEW_ROWS;
+constexpr int AT_WIDE_SLOTS = AT_WIDE_CTAS * 2 * 2 * AT_WIDE_TILE;
+__device__ __forceinline__ int dense_row(const AttnArgs& a, int own, int row) { return AT_FEW_SLOTS + AT_WIDE_SLOTS + own * a.T * a.Hq + row; }
 
 // ------------------------------------------------------------------------------------------------ segments
 // What the plan wrote is read past L1: the few-row kernel may begin before the kernel behind the plan has ended.
-__device__ __forceinline__ int64_t load_plan(const int64_t* p) { return __ldcg(reinterpret_cast<const long long*>(p)); }
+__device__ __forceinline__ int load_plan(const int32_t* p) { return __ldcg(p); }
 
 // Lengths come from the device unchecked: rows are clamped to [0, T], keys to what the page list can name.
 __device__ __forceinline__ int attn_row(const AttnArgs& a, int r) { return min(max(a.row_off[r], 0), a.T); }
@@ -110,7 +113,7 @@ __device__ __forceinline__ const int32_t* seg_pages(const AttnArgs& a, int s) {
     return s < a.P ? a.ptable + (int64_t)s * a.ld_ptable : a.table + (int64_t)(s - a.P) * a.ld_table;
 }
 // keys that token i of the segment sees, without the prefix in front
-__device__ __forceinline__ int seg_sees(const Segment& g, int i) { return g.causal ? max(g.klen - g.n + i + 1, 0) : g.klen; }
+__device__ __forceinline__ int seg_sees(const Segment& g, int i) { return g.flags & SEG_OWN ? max(g.klen - g.n + i + 1, 0) : g.klen; }
 
 // The two kinds of units.  Few-row: 16 consecutive (token, head) rows of one token list, few_hw heads side by side, tiles
 // of 64 / few_hw keys.  Wide: two tiles of as many whole tokens as fit 128 rows, one head.
@@ -132,14 +135,14 @@ struct FewUnits {
     }
 };
 struct WideUnits {
-    __device__ static constexpr int key_shift(const AttnArgs&) { return 7; }
+    __device__ static constexpr int key_shift(const AttnArgs&) { return 6; }
     __device__ static int heads(const AttnArgs& a) { return a.Hk; }
     __device__ static int tokens(const AttnArgs& a) { return 2 * (AT_WIDE_TILE / a.G); }
     __device__ static int count(const AttnArgs& a, const Segment& g) { return (int)(((int64_t)g.n + tokens(a) - 1) / tokens(a)); }
     __device__ static int last_token(const AttnArgs& a, const Segment& g, int u) {
         return (int)min((int64_t)g.n, ((int64_t)u + 1) * tokens(a)) - 1;
     }
-    // own keys, all units but the last: ceil((klen - n + (u + 1) tokens) / 128)
+    // own keys, all units but the last: ceil((klen - n + (u + 1) tokens) / 64)
     __device__ static void line(const AttnArgs& a, const Segment& g, int64_t& A, int64_t& B, int64_t& M, int64_t& u0) {
         const int64_t before = (int64_t)g.klen - g.n;
         A = tokens(a);
@@ -174,12 +177,12 @@ __device__ __forceinline__ int64_t floor_sum(int64_t n, int64_t m, int64_t a, in
     }
     return sum;
 }
-// key tiles of the units before unit u (u <= count) of one head
+// key tiles of the units before unit u (u <= count) of one head; the host has seen to it that counts of tiles are ints
 template <class U>
-__device__ __forceinline__ int64_t tiles_before(const AttnArgs& a, const Segment& g, int nu, int u) {
+__device__ __forceinline__ int tiles_before(const AttnArgs& a, const Segment& g, int nu, int u) {
     if (u == 0) return 0;
-    if (!g.causal) return (int64_t)u * unit_tiles<U>(a, g, 0);
-    int64_t sum = (int64_t)u * front_tiles<U>(a, g);
+    if (!(g.flags & SEG_OWN)) return u * unit_tiles<U>(a, g, 0);
+    int sum = u * front_tiles<U>(a, g);
     if (g.klen == 0) return sum;
     if (u == nu) {                       // the last unit may be short
         --u;
@@ -188,13 +191,13 @@ __device__ __forceinline__ int64_t tiles_before(const AttnArgs& a, const Segment
     if (u > 0) {
         int64_t A, B, M, u0;
         U::line(a, g, A, B, M, u0);      // own tiles(i) = floor((A i + B) / M) from unit u0 on, none before it
-        if (u > u0) sum += floor_sum(u - u0, M, A, B + A * u0);
+        if (u > u0) sum += (int)floor_sum(u - u0, M, A, B + A * u0);
     }
     return sum;
 }
 // key tiles of all units of one head
 template <class U>
-__device__ __forceinline__ int64_t head_tiles(const AttnArgs& a, const Segment& g) {
+__device__ __forceinline__ int head_tiles(const AttnArgs& a, const Segment& g) {
     if (g.n == 0) return 0;
     const int nu = U::count(a, g);
     return tiles_before<U>(a, g, nu, nu);
@@ -202,20 +205,17 @@ __device__ __forceinline__ int64_t head_tiles(const AttnArgs& a, const Segment& 
 
 // A line of N tiles is cut into shares of q = max(ceil(N / CTAs), least) tiles; CTA c has [c q, (c + 1) q).  A least
 // share, because a piece costs its prologue and a join.
-__device__ __forceinline__ int64_t share_tiles(int64_t N, int ctas, int least) { return max((N + ctas - 1) / ctas, (int64_t)least); }
-__device__ __forceinline__ int64_t div_fast(int64_t x, int64_t q) {
-    return ((x | q) >> 32) == 0 ? (int64_t)((uint32_t)x / (uint32_t)q) : x / q;
-}
+__device__ __forceinline__ int share_tiles(int N, int ctas, int least) { return max((int)(((int64_t)N + ctas - 1) / ctas), least); }
 // least share: 64 keys of few_hw heads
 __device__ __forceinline__ int few_min_tiles(const AttnArgs& a) { return a.few_hw; }
-constexpr int AT_WIDE_MIN_TILES = 2;
+constexpr int AT_WIDE_MIN_TILES = 4;
 
 // Where a cursor finds segments and their first tiles: what the plan kernel left in the workspace, or (SELF) shared memory.
 template <bool SELF>
 struct LineSource {
     const Segment* seg;
-    const int64_t* start;
-    __device__ __forceinline__ int64_t begin(int s) const { return SELF ? start[s] : load_plan(start + s); }
+    const int32_t* start;
+    __device__ __forceinline__ int begin(int s) const { return SELF ? start[s] : load_plan(start + s); }
     __device__ __forceinline__ Segment load(int s) const {
         if (SELF) return seg[s];
         Segment g;
@@ -232,7 +232,7 @@ struct Cursor {
     int s, h, u, kt, nu, nt;
     Segment g;
     // all lanes of a warp together
-    __device__ void seek(const AttnArgs& a, const LineSource<SELF>& src, int S, int64_t x) {
+    __device__ void seek(const AttnArgs& a, const LineSource<SELF>& src, int S, int x) {
         const int lane = threadIdx.x & 31;
         int lo = 0, len = S;
         while (len > 1) {                // the last segment that begins at or before x, 32 candidates at a time
@@ -245,13 +245,13 @@ struct Cursor {
         s = lo;
         g = src.load(s);
         nu = U::count(a, g);
-        int64_t y = x - src.begin(s);
-        h = (int)div_fast(y, g.tiles);
-        y -= (int64_t)h * g.tiles;
-        if (!g.causal) {
+        int y = x - g.start;
+        h = y / g.tiles;
+        y -= h * g.tiles;
+        if (!(g.flags & SEG_OWN)) {
             nt = unit_tiles<U>(a, g, 0);
-            u = (int)div_fast(y, nt);
-            kt = (int)(y - (int64_t)u * nt);
+            u = y / nt;
+            kt = y - u * nt;
         } else {
             int b = 0, e = nu;           // the last unit with at most y tiles before it
             while (e - b > 1) {
@@ -260,7 +260,7 @@ struct Cursor {
             }
             u = b;
             nt = unit_tiles<U>(a, g, u);
-            kt = (int)(y - tiles_before<U>(a, g, nu, u));
+            kt = y - tiles_before<U>(a, g, nu, u);
         }
     }
     // to the first tile of the next unit that has any; the caller knows that one exists
@@ -282,11 +282,11 @@ struct Cursor {
 
 // first tile of unit u of head h of a segment
 template <class U>
-__device__ __forceinline__ int64_t unit_begin(const AttnArgs& a, const Segment& g, int64_t seg_start, int h, int u) {
-    return seg_start + (int64_t)h * g.tiles + tiles_before<U>(a, g, U::count(a, g), u);
+__device__ __forceinline__ int unit_begin(const AttnArgs& a, const Segment& g, int h, int u) {
+    return g.start + h * g.tiles + tiles_before<U>(a, g, U::count(a, g), u);
 }
 
-__device__ __forceinline__ void tell_cut(CutUnit* c, int64_t unit_x0, int64_t unit_x1, int64_t x0, int64_t x1, int64_t q, int h, int u,
+__device__ __forceinline__ void tell_cut(CutUnit* c, int unit_x0, int unit_x1, int x0, int x1, int q, int h, int u,
                                          const Segment& g) {
     c->begin = unit_x0;
     c->share = q;
@@ -294,18 +294,18 @@ __device__ __forceinline__ void tell_cut(CutUnit* c, int64_t unit_x0, int64_t un
     c->u = u;
     c->t0 = g.t0;
     c->n = g.n;
-    c->tiles = unit_x1 > x1 && unit_x0 >= x0 && !(g.flags & SEG_TWO) ? (int)(unit_x1 - unit_x0) : 0;
+    c->tiles = unit_x1 > x1 && unit_x0 >= x0 && !(g.flags & SEG_TWO) ? unit_x1 - unit_x0 : 0;
 }
 
 // ------------------------------------------------------------------------------------------------ the plan
 // Inclusive sum over the block of one pair of values per thread; s_warp: [2][32] in shared memory.  Returns the block's totals in `total`.
-__device__ __forceinline__ void block_scan2(int64_t (&v)[2], int64_t (&total)[2], int64_t (*s_warp)[32], int warps) {
+__device__ __forceinline__ void block_scan2(int (&v)[2], int (&total)[2], int (*s_warp)[32], int warps) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const int64_t up = __shfl_up_sync(0xFFFFFFFFu, v[j], o);
+            const int up = __shfl_up_sync(0xFFFFFFFFu, v[j], o);
             if (lane >= o) v[j] += up;
         }
         if (lane == 31) s_warp[j][warp] = v[j];
@@ -313,10 +313,11 @@ __device__ __forceinline__ void block_scan2(int64_t (&v)[2], int64_t (&total)[2]
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-        int64_t x = lane < warps ? s_warp[j][lane] : 0, inc = x;
+        const int x = lane < warps ? s_warp[j][lane] : 0;
+        int inc = x;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const int64_t up = __shfl_up_sync(0xFFFFFFFFu, inc, o);
+            const int up = __shfl_up_sync(0xFFFFFFFFu, inc, o);
             if (lane >= o) inc += up;
         }
         total[j] = __shfl_sync(0xFFFFFFFFu, inc, 31);
@@ -340,7 +341,7 @@ __device__ __forceinline__ void clear_rows(const AttnArgs& a, int t0, int n) {
 constexpr int AT_PLAN_GROUPS = 512;    // groups of a step that fit there; more are looked up in global memory
 
 __global__ void __launch_bounds__(1024) attn_plan_kernel(const AttnArgs a) {
-    __shared__ int64_t s_warp[2][32];
+    __shared__ int s_warp[2][32];
     __shared__ int s_off[AT_PLAN_GROUPS + 1], s_len[AT_PLAN_GROUPS], s_mixed[AT_PLAN_GROUPS];
     grid_launch_dependents();
     grid_dependency_wait();
@@ -380,16 +381,15 @@ __global__ void __launch_bounds__(1024) attn_plan_kernel(const AttnArgs a) {
         }
     }
     auto mixed = [&](int g) { return in_smem ? s_mixed[g] != 0 : true; };
-    int64_t carry[2] = {0, 0};
+    int carry[2] = {0, 0};
     bool two = false, empty = false;
     for (int s0 = 0; s0 < S; s0 += threads) {
         const int s = s0 + tid;
-        int64_t own[2] = {0, 0}, inc[2], total[2];
+        int own[2] = {0, 0}, inc[2], total[2];
+        Segment g;
         if (s < S) {
-            Segment g;
             g.plen = 0;
-            g.flags = 0;
-            g.causal = s >= a.P;
+            g.flags = s >= a.P ? SEG_OWN : 0;
             if (s < a.P) {
                 const int r0 = off(s), r1 = max(off(s + 1), r0);
                 g.klen = len(s);
@@ -404,7 +404,7 @@ __global__ void __launch_bounds__(1024) attn_plan_kernel(const AttnArgs a) {
                 g.klen = attn_keys(a.kv_len[r], a.cols, a.page_shift);
                 g.group = group_of(r);
                 if (g.group >= 0) {
-                    if (mixed(g.group)) g.flags = SEG_TWO;
+                    if (mixed(g.group)) g.flags |= SEG_TWO;
                     else g.plen = len(g.group);
                 }
                 two |= g.n > 0 && (g.flags & SEG_TWO);
@@ -412,22 +412,22 @@ __global__ void __launch_bounds__(1024) attn_plan_kernel(const AttnArgs a) {
             }
             if ((int64_t)g.n * a.G >= a.wide_min_rows) {
                 g.flags |= SEG_WIDE;
-                const int64_t t = head_tiles<WideUnits>(a, g);
-                g.tiles = (int)t;
-                own[1] = t * WideUnits::heads(a);
+                g.tiles = head_tiles<WideUnits>(a, g);
+                own[1] = g.tiles * WideUnits::heads(a);
             } else {
-                const int64_t t = head_tiles<FewUnits>(a, g);
-                g.tiles = (int)t;
-                own[0] = t * FewUnits::heads(a);
+                g.tiles = head_tiles<FewUnits>(a, g);
+                own[0] = g.tiles * FewUnits::heads(a);
             }
-            a.plan.seg[s] = g;
         }
         inc[0] = own[0];
         inc[1] = own[1];
         block_scan2(inc, total, s_warp, threads / 32);
         if (s < S) {
-            a.plan.few_start[s] = carry[0] + inc[0] - own[0];
-            a.plan.wide_start[s] = carry[1] + inc[1] - own[1];
+            const int few = carry[0] + inc[0] - own[0], wide = carry[1] + inc[1] - own[1];
+            a.plan.few_start[s] = few;
+            a.plan.wide_start[s] = wide;
+            g.start = g.flags & SEG_WIDE ? wide : few;
+            a.plan.seg[s] = g;
         }
         carry[0] += total[0];
         carry[1] += total[1];
@@ -441,6 +441,7 @@ __global__ void __launch_bounds__(1024) attn_plan_kernel(const AttnArgs a) {
         a.plan.share[0] = share_tiles(carry[0], a.few_ctas, few_min_tiles(a));
         a.plan.share[1] = share_tiles(carry[1], a.wide_ctas, AT_WIDE_MIN_TILES);
     }
+    __syncthreads();
     if (two) {
         for (int t = tid; t < a.T; t += threads) a.plan.tok_req[t] = -1;
         __syncthreads();
@@ -459,39 +460,21 @@ __global__ void __launch_bounds__(1024) attn_plan_kernel(const AttnArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------------ pieces
-struct PieceList {           // pieces of one row from one segment
-    int count;               // 0: none; 1: the whole unit, in the dense buffer
-    int cta, which;          // share of the first piece, and whether it is that CTA's last piece
-    int stride;              // rows between two slots
-    int64_t row;             // row in a slot, or in the dense buffer
-    const float* part;
-    const float2* ml;
-    __device__ int64_t at(int i) const { return count == 1 ? row : ((int64_t)(cta + i) * 2 + (i ? 0 : which)) * stride + row; }
+struct PieceList {           // pieces of one row from one unit
+    int count;               // 0: none; 1: the whole unit
+    int first, rest, stride; // rows of the partial results: `first` for piece 0, rest + i * stride for the others
+    __device__ int at(int i) const { return i ? rest + i * stride : first; }
 };
-__device__ __forceinline__ void list_pieces(PieceList& p, int64_t begin, int tiles, int64_t q) {
-    const int64_t c0 = div_fast(begin, q), c1 = div_fast(begin + tiles - 1, q);
-    p.cta = (int)c0;
-    p.which = begin > c0 * q;
-    p.count = (int)(c1 - c0) + 1;
-}
-
-// pieces of row g of token t's head h from a segment on the tcgen05 line
-__device__ __forceinline__ void wide_pieces(const AttnArgs& a, PieceList& p, const Segment& sg, int64_t seg_start, int64_t q, int t, int h, int g, int dense) {
-    const int tok = t - sg.t0, tpt = AT_WIDE_TILE / a.G, u = tok / (2 * tpt), in = tok % (2 * tpt);
-    p.count = 0;
-    if (tok < 0 || tok >= sg.n) return;
-    const int nt = unit_tiles<WideUnits>(a, sg, u);
-    if (nt == 0) return;
-    list_pieces(p, unit_begin<WideUnits>(a, sg, seg_start, h, u), nt, q);
-    p.stride = 2 * AT_WIDE_TILE;
-    p.row = (in / tpt) * AT_WIDE_TILE + (in % tpt) * a.G + g;
-    p.part = a.wide_part;
-    p.ml = a.wide_ml;
-    if (p.count == 1) {
-        p.row = (int64_t)t * a.Hq + h * a.G + g;
-        p.part = a.dense[dense];
-        p.ml = a.dense_ml[dense];
-    }
+// A unit of `tiles` tiles from `begin` on, cut into shares of q; `base`: row of the line's slots; stride: rows between two
+// slots of a CTA; row: row in a slot; whole: row of the dense results
+__device__ __forceinline__ PieceList list_pieces(int begin, int tiles, int q, int base, int stride, int row, int whole) {
+    PieceList p;
+    const int c0 = begin / q, c1 = (begin + tiles - 1) / q;
+    p.count = c1 - c0 + 1;
+    p.stride = 2 * stride;
+    p.rest = base + c0 * 2 * stride + row;
+    p.first = p.count == 1 ? whole : p.rest + (begin > c0 * q ? stride : 0);
+    return p;
 }
 
 // --------------------------------------------------------------------------------------------- few rows
@@ -535,7 +518,7 @@ struct FewCfg {
     static constexpr int RING = 4 * STAGES * SLOT_BYTES;         // every warp has its own ring
     static constexpr int JOIN_FLOATS = 16 * D + 32;              // one warp's O, m and l
     static constexpr int JOIN = HW < 4 ? 2 * JOIN_FLOATS * 4 : 0;
-    static constexpr int PLAN = SELF ? FEW_SELF * (int)sizeof(Segment) + (FEW_SELF + 1) * 8 : 0;
+    static constexpr int PLAN = SELF ? FEW_SELF * (int)sizeof(Segment) + FEW_SELF * 4 : 0;
     static constexpr int SMEM = RING + JOIN + PLAN;
 };
 
@@ -562,33 +545,32 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
     if (!early) grid_dependency_wait();
     const int S = a.P + a.R;
     LineSource<SELF> src = {a.plan.seg, a.plan.few_start};
-    int64_t N, q;
+    int N, q;
     if (SELF) {
-        __shared__ int64_t s_warp[2][32];
+        __shared__ int s_warp[2][32];
         Segment* seg = reinterpret_cast<Segment*>(at_smem + C::RING + C::JOIN);
-        int64_t* start = reinterpret_cast<int64_t*>(seg + FEW_SELF);
-        int64_t carry = 0;
+        int* start = reinterpret_cast<int*>(seg + FEW_SELF);
+        int carry = 0;
         bool empty = false;
         for (int s0 = 0; s0 < S; s0 += AT_FEW_THREADS) {
             const int s = s0 + threadIdx.x;
-            int64_t inc[2] = {0, 0}, total[2], own = 0;
+            int inc[2] = {0, 0}, total[2], own = 0;
             if (s < S) {
                 Segment g;
                 g.plen = 0;
-                g.flags = 0;
-                g.causal = 1;
+                g.flags = SEG_OWN;
                 g.group = -1;
                 g.t0 = attn_row(a, s);
                 g.n = max(attn_row(a, s + 1) - g.t0, 0);
                 g.klen = attn_keys(a.kv_len[s], a.cols, a.page_shift);
-                g.tiles = (int)head_tiles<FewUnits>(a, g);
-                own = (int64_t)g.tiles * FewUnits::heads(a);
+                g.tiles = head_tiles<FewUnits>(a, g);
+                own = g.tiles * FewUnits::heads(a);
                 inc[0] = own;
                 seg[s] = g;
                 empty |= g.n > g.klen;
             }
             block_scan2(inc, total, s_warp, AT_FEW_THREADS / 32);
-            if (s < S) start[s] = carry + inc[0] - own;
+            if (s < S) start[s] = seg[s].start = carry + inc[0] - own;
             carry += total[0];
         }
         empty = __syncthreads_or(empty);
@@ -603,7 +585,7 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
         N = load_plan(a.plan.few_start + S);
         q = load_plan(a.plan.share);
     }
-    const int64_t x0 = min(q * blockIdx.x, N), x1 = min(x0 + q, N);
+    const int x0 = (int)min((int64_t)q * blockIdx.x, (int64_t)N), x1 = (int)min((int64_t)x0 + q, (int64_t)N);
     if (x0 >= x1) {
         if (threadIdx.x == 0) a.plan.cut[0][blockIdx.x].tiles = 0;
         if (early) grid_dependency_wait();
@@ -626,7 +608,7 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
         const int p = seg_pages(a, ld.s)[key >> a.page_shift];     // klen is within the list's columns
         return (p >= 0 && p < a.n_pages) ? p : -1;
     };
-    int64_t xl = x0;                   // loader's position
+    int xl = x0;                       // loader's position
     int page = page_of();
     auto load = [&](int slot) {
         if (xl < x1) {
@@ -655,7 +637,7 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
 
     const int r0 = lane >> 2, cq = lane & 3;       // the thread's rows r0, r0 + 8 and column pair of an MMA fragment
     int slot = 0, fill = C::STAGES - 1;
-    int64_t x = x0;
+    int x = x0;
     while (x < x1) {
         // ---- a unit (or the share's part of it)
         const int row0 = cur.u * AT_FEW_ROWS;
@@ -680,8 +662,8 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
 #pragma unroll
         for (int j = 0; j < NJ; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.0f;
         float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
-        const int64_t unit_x0 = x - cur.kt, unit_x1 = unit_x0 + cur.nt;
-        const int64_t xe = min(unit_x1, x1);
+        const int unit_x0 = x - cur.kt, unit_x1 = unit_x0 + cur.nt;
+        const int xe = min(unit_x1, x1);
         for (; x < xe; ++x, ++cur.kt) {
             load(fill);
             if (++fill == C::STAGES) fill = 0;
@@ -814,13 +796,13 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
                         *reinterpret_cast<uint32_t*>(op + j * 8) = bf162_bits(__floats2bfloat162_rn(o[j][2 * hlf] * inv, o[j][2 * hlf + 1] * inv));
                     if (a.lse && cq == 0) a.lse[row] = l[hlf] == 0.0f ? -INFINITY : (m[hlf] + log2f(l[hlf])) * 0.69314718055994531f;
                 } else {
-                    const int64_t at = split ? (((int64_t)blockIdx.x * 2 + (unit_x0 > x0 ? 1 : 0)) * HW + hw) * AT_FEW_ROWS + r : row;
-                    float* part = split ? a.few_part : a.dense[cur.s >= a.P];
-                    float2* ml = split ? a.few_ml : a.dense_ml[cur.s >= a.P];
+                    const int at = split ? ((blockIdx.x * 2 + (unit_x0 > x0 ? 1 : 0)) * HW + hw) * AT_FEW_ROWS + r
+                                         : dense_row(a, cur.s >= a.P, (int)row);
+                    float* part = a.part + (int64_t)at * D + cq * 2;
 #pragma unroll
                     for (int j = 0; j < NJ; ++j)
-                        *reinterpret_cast<float2*>(part + at * D + j * 8 + cq * 2) = make_float2(o[j][2 * hlf], o[j][2 * hlf + 1]);
-                    if (cq == 0) ml[at] = make_float2(m[hlf], l[hlf]);
+                        *reinterpret_cast<float2*>(part + j * 8) = make_float2(o[j][2 * hlf], o[j][2 * hlf + 1]);
+                    if (cq == 0) a.ml[at] = make_float2(m[hlf], l[hlf]);
                 }
             }
         }
@@ -838,64 +820,64 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
 // against 1 ms of attention, when it was done that way):
 //   units that the end of a share cuts, as the attention kernels told them: blocks for every share of either line;
 //   rows with two sources (prefix and own keys): blocks over the tokens, only launched where there are prefixes.
-// Pieces are taken 32 at a time, one per lane for m and l, twelve rows of O under way at a time.
 constexpr int AT_JOIN_THREADS = 256;
 constexpr int AT_JOIN_WARPS = AT_JOIN_THREADS / 32;
 
+// Pieces are taken 32 at a time: a lane finds the place, m and l of one; eight rows of O are under way at a time.
 template <int D>
 __device__ __forceinline__ void join_row(const AttnArgs& a, const PieceList& p0, const PieceList& p1, int64_t token, int hq) {
     constexpr int V = D / 32;          // channels per lane
-    constexpr int FLIGHT = 12;         // rows of O under way at a time
+    constexpr int FLIGHT = 8;
     const int lane = threadIdx.x & 31;
     float m = -INFINITY, l = 0.0f, o[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) o[j] = 0.0f;
     const int n = p0.count + p1.count;
     for (int i0 = 0; i0 < n; i0 += 32) {
-        const int i = i0 + lane;
-        float2 ml = make_float2(-INFINITY, 0.0f);
-        const float* src = nullptr;
-        if (i < n) {
-            const bool first = i < p0.count;
-            const int64_t at = first ? p0.at(i) : p1.at(i - p0.count);
-            ml = (first ? p0.ml : p1.ml)[at];
-            src = (first ? p0.part : p1.part) + at * D;
-        }
-        float mx = ml.x;
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, d));
-        mx = fmaxf(mx, m);
-        const float f0 = mx == -INFINITY ? 0.0f : exp2_approx(m - mx);
-        const float w = mx == -INFINITY ? 0.0f : exp2_approx(ml.x - mx);
-        float lw = ml.y * w;
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) lw += __shfl_xor_sync(0xFFFFFFFFu, lw, d);
-        m = mx;
-        l = l * f0 + lw;
-#pragma unroll
-        for (int j = 0; j < V; ++j) o[j] *= f0;
-        const int k = min(32, n - i0);
+        const int i = min(i0 + lane, n - 1), k = min(32, n - i0);
+        const int at = i < p0.count ? p0.at(i) : p1.at(i - p0.count);
+        float2 ml = a.ml[at];
+        if (i0 + lane >= n) ml = make_float2(-INFINITY, 0.0f);
+        float w = 0.0f;
         for (int b = 0; b < k; b += FLIGHT) {
-            float v[FLIGHT][V], wb[FLIGHT];
+            float v[FLIGHT][V];
 #pragma unroll
             for (int j = 0; j < FLIGHT; ++j) {
-                const int from = min(b + j, k - 1);
-                const float* sp = reinterpret_cast<const float*>(__shfl_sync(0xFFFFFFFFu, (unsigned long long)src, from));
-                wb[j] = __shfl_sync(0xFFFFFFFFu, w, from);
-                if (b + j >= k) wb[j] = 0.0f;
-                if (V == 4) {
-                    const float4 x = *reinterpret_cast<const float4*>(sp + lane * 4);
-                    v[j][0] = x.x; v[j][1] = x.y; v[j][V - 2] = x.z; v[j][V - 1] = x.w;
-                } else {
-                    const float2 x = *reinterpret_cast<const float2*>(sp + lane * 2);
-                    v[j][0] = x.x; v[j][1] = x.y;
+                if (b + j < k) {
+                    const float* src = a.part + (int64_t)__shfl_sync(0xFFFFFFFFu, at, b + j) * D + lane * V;
+                    if (V == 4) {
+                        const float4 x = *reinterpret_cast<const float4*>(src);
+                        v[j][0] = x.x; v[j][1] = x.y; v[j][V - 2] = x.z; v[j][V - 1] = x.w;
+                    } else {
+                        const float2 x = *reinterpret_cast<const float2*>(src);
+                        v[j][0] = x.x; v[j][1] = x.y;
+                    }
                 }
             }
+            if (b == 0) {
+                float mx = ml.x;
 #pragma unroll
-            for (int j = 0; j < FLIGHT; ++j)
-                if (wb[j] != 0.0f)     // a piece without weight may hold anything
+                for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, d));
+                mx = fmaxf(mx, m);
+                const float f0 = mx == -INFINITY ? 0.0f : exp2_approx(m - mx);
+                w = mx == -INFINITY ? 0.0f : exp2_approx(ml.x - mx);
+                float lw = ml.y * w;
 #pragma unroll
-                    for (int y = 0; y < V; ++y) o[y] = fmaf(v[j][y], wb[j], o[y]);
+                for (int d = 16; d > 0; d >>= 1) lw += __shfl_xor_sync(0xFFFFFFFFu, lw, d);
+                m = mx;
+                l = l * f0 + lw;
+#pragma unroll
+                for (int j = 0; j < V; ++j) o[j] *= f0;
+            }
+#pragma unroll
+            for (int j = 0; j < FLIGHT; ++j) {
+                if (b + j < k) {
+                    const float wj = __shfl_sync(0xFFFFFFFFu, w, b + j);
+                    if (wj != 0.0f)    // a piece without weight may hold anything
+#pragma unroll
+                        for (int y = 0; y < V; ++y) o[y] = fmaf(v[j][y], wj, o[y]);
+                }
+            }
         }
     }
     const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
@@ -910,27 +892,21 @@ __device__ __forceinline__ void join_row(const AttnArgs& a, const PieceList& p0,
 }
 
 template <int D>
-__global__ void __launch_bounds__(AT_JOIN_THREADS, 2) attn_join_kernel(const AttnArgs a, int wide_blocks, int wide_split, int few_blocks, int few_split,
-                                                                    int tokens) {
+__global__ void __launch_bounds__(AT_JOIN_THREADS, 3) attn_join_kernel(const AttnArgs a, int wide_blocks, int wide_split, int few_blocks, int few_split) {
     grid_launch_dependents();
     grid_dependency_wait();
     const int warp = threadIdx.x >> 5;
     int b = blockIdx.x;
-    PieceList none, p;
-    none.count = 0;
+    PieceList none;
+    none.count = none.first = none.rest = none.stride = 0;
     if (b < wide_blocks) {
         const CutUnit cut = a.plan.cut[1][b / wide_split];
         if (cut.tiles == 0) return;
-        list_pieces(p, cut.begin, cut.tiles, cut.share);
-        p.stride = 2 * AT_WIDE_TILE;
-        p.part = a.wide_part;
-        p.ml = a.wide_ml;
         const int tpt = AT_WIDE_TILE / a.G, rows = 2 * AT_WIDE_TILE / wide_split, part = b % wide_split;
         for (int i = part * rows + warp; i < (part + 1) * rows; i += AT_JOIN_WARPS) {
             const int r = i % AT_WIDE_TILE, tok = (cut.u * 2 + i / AT_WIDE_TILE) * tpt + r / a.G;
             if (r >= tpt * a.G || tok >= cut.n) continue;
-            p.row = i;
-            join_row<D>(a, none, p, cut.t0 + tok, cut.h * a.G + r % a.G);
+            join_row<D>(a, none, list_pieces(cut.begin, cut.tiles, cut.share, AT_FEW_SLOTS, 2 * AT_WIDE_TILE, i, 0), cut.t0 + tok, cut.h * a.G + r % a.G);
         }
         return;
     }
@@ -938,61 +914,47 @@ __global__ void __launch_bounds__(AT_JOIN_THREADS, 2) attn_join_kernel(const Att
     if (b < few_blocks) {
         const CutUnit cut = a.plan.cut[0][b / few_split];
         if (cut.tiles == 0) return;
-        list_pieces(p, cut.begin, cut.tiles, cut.share);
-        p.stride = a.few_hw * AT_FEW_ROWS;
-        p.part = a.few_part;
-        p.ml = a.few_ml;
-        const int rows = p.stride / few_split, part = b % few_split;
+        const int stride = a.few_hw * AT_FEW_ROWS, rows = stride / few_split, part = b % few_split;
         for (int i = part * rows + warp; i < (part + 1) * rows; i += AT_JOIN_WARPS) {
             const int fr = cut.u * AT_FEW_ROWS + i % AT_FEW_ROWS, tok = fr / a.G;
             if (tok >= cut.n) continue;
-            p.row = i;
-            join_row<D>(a, none, p, cut.t0 + tok, (cut.h * a.few_hw + i / AT_FEW_ROWS) * a.G + fr % a.G);
+            join_row<D>(a, none, list_pieces(cut.begin, cut.tiles, cut.share, 0, stride, i, 0), cut.t0 + tok,
+                        (cut.h * a.few_hw + i / AT_FEW_ROWS) * a.G + fr % a.G);
         }
         return;
     }
+    // rows that have a prefix and own keys: the rest of the grid strides over all rows
     b -= few_blocks;
-    // `tokens` tokens of one head: the rows that have a prefix and own keys
-    if (a.plan.share[2] == 0) return;
-    const int h = b % a.Hk;
-    const int64_t nf = a.plan.share[0], nw = a.plan.share[1];
-    for (int i = warp; i < tokens * a.G; i += AT_JOIN_WARPS) {
-        const int64_t t64 = (int64_t)(b / a.Hk) * tokens + i / a.G;
-        if (t64 >= a.T) return;
-        const int t = (int)t64, g = i % a.G;
+    const int two = a.plan.share[2], nf = a.plan.share[0], nw = a.plan.share[1], rows = a.T * a.Hq;
+    if (two == 0) return;
+    const int step = ((int)gridDim.x - wide_blocks - few_blocks) * AT_JOIN_WARPS;
+    for (int i = b * AT_JOIN_WARPS + warp; i < rows; i += step) {
+        const int t = i / a.Hq, hq = i - t * a.Hq, h = hq / a.G, g = hq - h * a.G;
         const int r = a.plan.tok_req[t];
         if (r < 0) continue;
-        const Segment own = a.plan.seg[a.P + r], pre = a.plan.seg[own.group];
-        {
-            const int hq = h * a.G + g;
-            PieceList list[2];
+        const Segment own = a.plan.seg[a.P + r];
+        PieceList list[2];
 #pragma unroll
-            for (int which = 0; which < 2; ++which) {
-                const Segment& sg = which ? own : pre;
-                const int s = which ? a.P + r : own.group, tok = t - sg.t0;
-                PieceList& pl = list[which];
-                pl.count = 0;
-                if (tok < 0 || tok >= sg.n) continue;
+        for (int which = 0; which < 2; ++which) {
+            const Segment sg = which ? own : a.plan.seg[own.group];
+            const int tok = t - sg.t0;
+            PieceList p = none;
+            if (tok >= 0 && tok < sg.n) {
                 if (sg.flags & SEG_WIDE) {
-                    wide_pieces(a, pl, sg, a.plan.wide_start[s], nw, t, h, g, which);
+                    const int tpt = AT_WIDE_TILE / a.G, u = tok / (2 * tpt), in = tok - u * 2 * tpt, second = in >= tpt;
+                    const int nt = unit_tiles<WideUnits>(a, sg, u);
+                    if (nt) p = list_pieces(unit_begin<WideUnits>(a, sg, h, u), nt, nw, AT_FEW_SLOTS, 2 * AT_WIDE_TILE,
+                                            second * AT_WIDE_TILE + (in - second * tpt) * a.G + g, dense_row(a, which, i));
                 } else {
                     const int fr = tok * a.G + g, u = fr / AT_FEW_ROWS;
                     const int nt = unit_tiles<FewUnits>(a, sg, u);
-                    if (nt == 0) continue;
-                    list_pieces(pl, unit_begin<FewUnits>(a, sg, a.plan.few_start[s], h / a.few_hw, u), nt, nf);
-                    pl.stride = a.few_hw * AT_FEW_ROWS;
-                    pl.row = (h % a.few_hw) * AT_FEW_ROWS + fr % AT_FEW_ROWS;
-                    pl.part = a.few_part;
-                    pl.ml = a.few_ml;
-                    if (pl.count == 1) {
-                        pl.row = (int64_t)t * a.Hq + hq;
-                        pl.part = a.dense[which];
-                        pl.ml = a.dense_ml[which];
-                    }
+                    if (nt) p = list_pieces(unit_begin<FewUnits>(a, sg, h / a.few_hw, u), nt, nf, 0, a.few_hw * AT_FEW_ROWS,
+                                            h % a.few_hw * AT_FEW_ROWS + fr % AT_FEW_ROWS, dense_row(a, which, i));
                 }
             }
-            join_row<D>(a, list[0], list[1], t, hq);
+            list[which] = p;
         }
+        join_row<D>(a, list[0], list[1], t, hq);
     }
 }
 

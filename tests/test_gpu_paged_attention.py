@@ -210,3 +210,10 @@ def test_offsets_past_32_bits(B):
     o, lse = c.run(B)
     B.osc_sync_check()
     c.check(o, lse, "far pages")
+
+
+def test_many_units_to_a_share(B):
+    """Prompts long enough that every CTA of the kernel for many rows runs through several units, with lists that end inside tiles
+    of all kinds, one after the other."""
+    go(B, seed=21, Hk=8, G=4, D=128, page=64, new=[700, 3, 650, 900], kv=[1000, 900, 650, 1111], prefix=[391])
+    go(B, seed=22, Hk=8, G=8, D=64, page=16, new=[500, 333, 420], kv=[777, 640, 421], prefix=[129, 70], groups=[0, 2, 3])
