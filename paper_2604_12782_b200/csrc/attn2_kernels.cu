@@ -3,14 +3,15 @@
 //
 // A unit is two tiles of up to 128 rows (tokens x query heads of one key/value head).  S = Q K^T and O += P V
 // both run on the fifth-generation tensor cores: Q, K and V tiles come by TMA into shared memory, S, P and O live in TMEM (P, the weights
-// in bf16, is read from there as the A operand).  Two streams run in counterphase, each with its own S, P, O and warpgroup (one
+// in bf16, is read from there as the A operand).  Two streams run in counterphase, each with its own P, O and warpgroup (one
 // row per thread): while one stream's softmax runs, the other's products do.
 //   both row tiles filled: stream s is row tile s; they share every K and V tile.
 //   one row tile:          both streams take the same rows and every other key tile; the results are joined
 //                          at the end of the unit (a thread can read both O rows: they lie in its lanes).
-// Key tiles of 64: with 128 keys S and O fill TMEM and P has to go into the columns of its S, so that a stream's steps run strictly
-// one after the other (S, softmax, P V, next S: 3800 cycles for 128 keys of both row tiles, tensor pipe half idle).  With 64 there is room for
-// P, and the next S is worked out while the softmax of this one runs.
+// With D = 128 two S (128 x 128), two P and two O do not fit TMEM.  The streams share ONE S: a softmax thread takes its whole row of scores
+// into registers at once, and the other stream's product can go there a few hundred cycles later.  (Each stream with its own S and P in the
+// columns of that S made a stream's steps run strictly one after the other - S, softmax, P V, next S: 3700 cycles for 128 keys of both tiles,
+// tensor pipe 47 % busy; own S and P with 64-key tiles: 5500, twice the MMA warp's steps, whose 500 cycles each were then what counted.)
 //
 //   warps 0-3, 4-7 : softmax of stream 0, 1, and their epilogue
 //   warp 8         : TMA (a key tile is loaded page by page; a page that is not there reads as zeros)
@@ -35,6 +36,14 @@ struct AttnWideArgs {
 
 constexpr int AW_SOFTMAX_WARPS = 8;
 constexpr int AW_THREADS = (AW_SOFTMAX_WARPS + 4) * 32;
+// Registers: launched with 168 a thread (12 warps).  The softmax warpgroups hold a row of 128 scores each thread and take
+// 208, the last one gives down to 80.
+constexpr int AW_REGS_LAUNCH = 168, AW_REGS_SOFTMAX = 208, AW_REGS_OTHER = 80;
+static_assert(AW_SOFTMAX_WARPS * AW_REGS_SOFTMAX + 4 * AW_REGS_OTHER <= (AW_SOFTMAX_WARPS + 4) * AW_REGS_LAUNCH, "register split");
+template <int R>
+__device__ __forceinline__ void regs_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(R)); }
+template <int R>
+__device__ __forceinline__ void regs_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(R)); }
 
 // Two fp32 operations in one instruction.
 __device__ __forceinline__ uint64_t pack2(float x, float y) {
@@ -64,16 +73,16 @@ struct WideCfg {
     static constexpr int HALVES = D / 64;                        // 128-byte swizzle rows hold 64 channels
     static constexpr int QHALF_BYTES = 128 * 128;                // 128 rows of 64 channels
     static constexpr int QTILE_BYTES = HALVES * QHALF_BYTES;
-    static constexpr int HALF_BYTES = AT_WIDE_KEYS * 128;        // 64 keys of 64 channels
+    static constexpr int HALF_BYTES = AT_WIDE_KEYS * 128;        // 128 keys of 64 channels
     static constexpr int TILE_BYTES = HALVES * HALF_BYTES;
-    static constexpr int STAGES = 8;
+    static constexpr int STAGES = D == 128 ? 2 : 4;              // K tiles, and as many V tiles
     static constexpr int OUT_BYTES = AW_SOFTMAX_WARPS * 2048;    // every softmax warp's 32 rows x 16 columns of O on the way out
     static constexpr int ROW_FLOATS = 2 * 2 * 2 * 128;           // [parity][stream][128] maxima and sums of a unit
-    static constexpr int BAR_BYTES = 288;
-    static constexpr int SMEM = 2 * QTILE_BYTES + STAGES * TILE_BYTES + OUT_BYTES + ROW_FLOATS * 4 + BAR_BYTES + 2 * 64 + 1024;
-    static constexpr int TM_S = 0;         // TMEM columns: S0, S1 (64 each), P0, P1 (32 each), O0, O1 (D each)
+    static constexpr int BAR_BYTES = 320;
+    static constexpr int SMEM = 2 * QTILE_BYTES + 2 * STAGES * TILE_BYTES + OUT_BYTES + ROW_FLOATS * 4 + BAR_BYTES + 2 * 64 + 1024;
+    static constexpr int TM_S = 0;         // TMEM columns: S (128), P0, P1 (64 each), O0, O1 (D each)
     static constexpr int TM_P = 128;
-    static constexpr int TM_O = 192;
+    static constexpr int TM_O = 256;
     static_assert(SMEM <= 232448, "shared memory");
 };
 
@@ -148,35 +157,36 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t* ring = smem + 2 * C::QTILE_BYTES;
-    uint8_t* out_tiles = ring + STAGES * C::TILE_BYTES;
+    uint8_t* out_tiles = ring + 2 * STAGES * C::TILE_BYTES;
     float2* unit_ml = reinterpret_cast<float2*>(out_tiles + C::OUT_BYTES);  // [parity][stream][128]
     uint64_t* bars = reinterpret_cast<uint64_t*>(unit_ml + 4 * 128);
-    uint64_t* full = bars;
-    uint64_t* empty = bars + STAGES;
-    uint64_t* q_full = bars + 2 * STAGES;
+    uint64_t* full = bars;               // [2][STAGES]: K, V
+    uint64_t* empty = bars + 2 * STAGES; // [2][STAGES]
+    uint64_t* q_full = bars + 4 * STAGES;
     uint64_t* q_empty = q_full + 1;
     uint64_t* s_full = q_full + 2;       // [2]
     uint64_t* p_full = q_full + 4;       // [2]
-    uint64_t* s_empty = q_full + 6;      // [2]
-    uint64_t* pv_done = q_full + 8;      // [2]
-    uint64_t* u_full = q_full + 10;      // [2]
-    uint64_t* u_empty = q_full + 12;     // [2]
-    uint64_t* o_empty = q_full + 14;
-    uint64_t* e_full = q_full + 15;
-    uint64_t* drain_bar = q_full + 16;
-    uint64_t* v_clean = q_full + 17;
-    uint64_t* v_end = q_full + 18;
+    uint64_t* pv_done = q_full + 6;      // [2]
+    uint64_t* u_full = q_full + 8;       // [2]
+    uint64_t* u_empty = q_full + 10;     // [2]
+    uint64_t* s_empty = q_full + 12;
+    uint64_t* o_empty = q_full + 13;
+    uint64_t* e_full = q_full + 14;
+    uint64_t* drain_bar = q_full + 15;
+    uint64_t* v_clean = q_full + 16;
+    uint64_t* v_end = q_full + 17;
+    constexpr int BARS = 4 * STAGES + 18;
     WideUnit* units = reinterpret_cast<WideUnit*>(reinterpret_cast<uint8_t*>(bars) + C::BAR_BYTES);   // [2]
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(q_full + 19);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + BARS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-    static_assert((2 * STAGES + 19) * 8 + 8 <= C::BAR_BYTES, "barriers");
+    static_assert(BARS * 8 + 8 <= C::BAR_BYTES, "barriers");
 
     const int warp = __shfl_sync(0xFFFFFFFFu, (int)(threadIdx.x >> 5), 0);
     const int lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < 2 * STAGES + 19; ++i) {
-            const int b = i - 2 * STAGES;      // all barriers take one arrival but these
-            mbar_init(&bars[i], b == 4 || b == 5 || b == 6 || b == 7 ? NSW / 2 : b == 12 || b == 13 ? NSW + 3 : b == 14 || b == 15 ? NSW : 1);
+        for (int i = 0; i < BARS; ++i) {
+            const int b = i - 4 * STAGES;      // all barriers take one arrival but these
+            mbar_init(&bars[i], b == 4 || b == 5 || b == 12 ? NSW / 2 : b == 10 || b == 11 ? NSW + 3 : b == 13 || b == 14 ? NSW : 1);
         }
         *abort_flag = 0;
         fence_barrier_init();
@@ -198,6 +208,7 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
     const uint32_t ring0 = smem_u32(ring);
 
     if (warp >= NSW) {
+        regs_dec<AW_REGS_OTHER>();
         if (warp == NSW + 2) {
             // ------------------------------------------------------------------------------------- units
             const int S = a.P + a.R;
@@ -252,37 +263,46 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
             const int bt = min(1 << a.page_shift, AT_WIDE_KEYS);     // tokens of a box
             const int boxes = AT_WIDE_KEYS / bt * C::HALVES;         // of a K or V tile: at most 16, one lane each
             const int mine = lane / C::HALVES, half = lane % C::HALVES;
-            uint32_t n_load = 0;            // loads so far: stage n % STAGES, phase n / STAGES
-            int st = 0, b = 0;
-            uint32_t ph = 0, q_ph = 0, u_ph = 0;
+            uint32_t n_k = 0, n_v = 0;      // K and V loads so far: tile n in slot n % STAGES, phase n / STAGES
+            int b = 0;
+            uint32_t q_ph = 0, u_ph = 0;
             while (true) {
                 if (!wait_bounded(&u_full[b], u_ph, abort_flag, 60)) goto stop_loads;
                 const WideUnit& w = units[b];
-                const int ka = w.ka, kb = ka + w.n, nf = w.nf, h = w.h;
-                if (kb == ka) break;
+                const int ka = w.ka, n = w.n, nf = w.nf, h = w.h;
+                if (n == 0) break;
                 const int32_t* own_pages = seg_pages(a, w.seg);
                 const int32_t* front_pages = nf ? seg_pages(a, w.front) : own_pages;
-                for (int kt = ka; kt < kb; ++kt) {
-                    int page = a.n_pages, place = 0;      // a box past the last page is filled with zeros
-                    if (lane < boxes) {
-                        const int key = (kt < nf ? kt : kt - nf) * AT_WIDE_KEYS + mine * bt;
-                        if (mine * bt < unit_left(w, kt)) {          // a length is within the list's columns
-                            const int p = (kt < nf ? front_pages : own_pages)[key >> a.page_shift];
-                            if (p >= 0 && p < a.n_pages) page = p;
-                            place = key & ((1 << a.page_shift) - 1);
+                int page = 0, place = 0;
+                // K one tile ahead of V: a K slot is free again long before the V slot of the same tile
+                for (int i = 0; i <= n; ++i) {
+                    const int v_page = page, v_place = place;
+                    if (i < n) {
+                        const int kt = ka + i;
+                        page = a.n_pages;      // a box past the last page is filled with zeros
+                        place = 0;
+                        if (lane < boxes) {
+                            const int key = (kt < nf ? kt : kt - nf) * AT_WIDE_KEYS + mine * bt;
+                            if (mine * bt < unit_left(w, kt)) {          // a length is within the list's columns
+                                const int p = (kt < nf ? front_pages : own_pages)[key >> a.page_shift];
+                                if (p >= 0 && p < a.n_pages) page = p;
+                                place = key & ((1 << a.page_shift) - 1);
+                            }
                         }
                     }
-                    for (int kv = 0; kv < 2; ++kv) {
-                        if (!wait_bounded(&empty[st], ph ^ 1u, abort_flag, 62)) goto stop_loads;
+#pragma unroll 1
+                    for (int v = 0; v < 2; ++v) {
+                        if (v ? i == 0 : i == n) continue;
+                        const uint32_t t = v ? n_v : n_k, st = v * STAGES + t % STAGES;
+                        if (!wait_bounded(&empty[st], (t / STAGES + 1) & 1u, abort_flag, 62)) goto stop_loads;
                         if (lane == 0) mbar_arrive_expect_tx(&full[st], C::TILE_BYTES);
                         __syncwarp();
                         if (lane < boxes)
-                            tma_load_4d(ring0 + st * C::TILE_BYTES + half * C::HALF_BYTES + mine * bt * 128, kv ? &args.tm_v : &args.tm_k, &full[st],
-                                        half * 64, place, h, page);
-                        ++n_load;
-                        if (++st == STAGES) { st = 0; ph ^= 1u; }
-                        if (kt > ka || kv) continue;
-                        // behind the first K: Q, whose place is free when the unit before has no more S to come
+                            tma_load_4d(ring0 + st * C::TILE_BYTES + half * C::HALF_BYTES + mine * bt * 128, v ? &args.tm_v : &args.tm_k, &full[st],
+                                        half * 64, v ? v_place : place, h, v ? v_page : page);
+                        if (v) ++n_v; else ++n_k;
+                    }
+                    if (i == 0) {      // behind the first K: Q, whose place is free when the unit before has no more S to come
                         if (!wait_bounded(q_empty, q_ph ^ 1u, abort_flag, 61)) goto stop_loads;
                         q_ph ^= 1u;
                         const int tiles = w.pair ? 2 : 1;
@@ -302,8 +322,10 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
             if (*abort_flag) {      // gave up somewhere: the copies under way land before the CTA's memory goes away
                 int dummy = 0;
                 volatile int* never = &dummy;
-                for (uint32_t i = n_load > STAGES ? n_load - STAGES : 0; i < n_load; ++i)
-                    wait_bounded(&full[i % STAGES], (i / STAGES) & 1u, never, 63);
+                for (int v = 0; v < 2; ++v) {
+                    const uint32_t t = v ? n_v : n_k;
+                    for (uint32_t i = t > STAGES ? t - STAGES : 0; i < t; ++i) wait_bounded(&full[v * STAGES + i % STAGES], (i / STAGES) & 1u, never, 63);
+                }
                 wait_bounded(q_full, q_ph ^ 1u, never, 64);
             }
         } else if (warp == NSW + 3) {
@@ -320,7 +342,7 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                 for (int kt = w.nf > w.ka ? w.nf - 1 : w.ka + n - 1; kt < w.ka + n; kt = w.ka + n - 1 > kt ? w.ka + n - 1 : w.ka + n) {
                     const int left = unit_left(w, kt);
                     if (left >= AT_WIDE_KEYS) continue;
-                    const uint32_t ld = base + 2 * (kt - w.ka) + 1, stg = ld % STAGES;
+                    const uint32_t stg = STAGES + (base + kt - w.ka) % STAGES;
                     if (!wait_bounded(v_end, ve_ph, abort_flag, 80)) goto done;
                     ve_ph ^= 1u;
                     uint8_t* v = ring + stg * C::TILE_BYTES;
@@ -330,7 +352,7 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                     __syncwarp();
                     if (lane == 0) mbar_arrive(v_clean);
                 }
-                base += 2 * (uint32_t)n;
+                base += n;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&u_empty[b]);
                 if (++b == 2) { b = 0; u_ph ^= 1u; }
@@ -343,17 +365,17 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
             const uint64_t q_desc = smem_desc_sw128(smem_u32(smem)), k_desc = smem_desc_sw128(ring0);
             const uint64_t v_desc = smem_desc_sw128_mn(ring0, C::HALVES > 1 ? C::HALF_BYTES : 1024);
             constexpr uint32_t IDESC_S = idesc_bf16(128, AT_WIDE_KEYS), IDESC_O = idesc_bf16(128, D) | IDESC_B_MN;
-            uint32_t base = 0;                 // loads of the units before
-            uint32_t q_ph = 0, p_ph = 0, se_ph = 3, oe_ph = 1, u_ph = 0, vc_ph = 0;
+            uint32_t base = 0;                 // tiles of the units before
+            uint32_t q_ph = 0, p_ph = 0, se_ph = 1, oe_ph = 1, u_ph = 0, vc_ph = 0;
             int b = 0;
             while (true) {
                 if (!wait_bounded(&u_full[b], u_ph, abort_flag, 78)) goto done;
                 const WideUnit& w = units[b];
                 const int n = uni(w.n), cnt0 = uni(w.cnt[0]), cnt1 = uni(w.cnt[1]), pair = uni(w.pair), ka = uni(w.ka);
                 const int nf = uni(w.nf), plen = uni(w.plen), klen = uni(w.klen);
-                const uint32_t two = pair ? 2 : 4;       // loads from one key tile of a stream to the next
                 if (n == 0) break;
-                const int end_front = plen % AT_WIDE_KEYS ? nf - 1 : -1, end_own = klen % AT_WIDE_KEYS ? nf + klen / AT_WIDE_KEYS : -1;
+                // tiles of the unit's part that end inside (V to be cleaned), counted from its first
+                const int end_front = plen % AT_WIDE_KEYS ? nf - 1 - ka : -1, end_own = klen % AT_WIDE_KEYS ? nf + klen / AT_WIDE_KEYS - ka : -1;
                 if (!wait_bounded(q_full, q_ph, abort_flag, 65)) goto done;
                 q_ph ^= 1u;
                 const int most = max(cnt0, cnt1);
@@ -363,18 +385,17 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
 #pragma unroll
                     for (int s = 0; s < 2; ++s) {
                         const int cnt = s ? cnt1 : cnt0;
-                        const uint32_t first = base + (pair ? 0 : 2 * s);                 // the stream's first K; V is the load behind it
                         if (j < cnt) {
-                            const uint32_t ld = first + j * two, stg = ld % STAGES;
-                            if (!wait_bounded(&full[stg], (ld / STAGES) & 1u, abort_flag, 66)) goto done;
-                            if (!wait_bounded(&s_empty[s], (se_ph >> s) & 1u, abort_flag, 84)) goto done;     // the S before has been read
-                            se_ph ^= 1u << s;
+                            const uint32_t t = base + (pair ? j : 2 * j + s), stg = t % STAGES;
+                            if (!wait_bounded(&full[stg], (t / STAGES) & 1u, abort_flag, 66)) goto done;
+                            if (!wait_bounded(s_empty, se_ph, abort_flag, 84)) goto done;     // the S before has been read
+                            se_ph ^= 1u;
                             tc_fence_after();
                             const uint64_t qd = q_desc + (pair ? s * (C::QTILE_BYTES >> 4) : 0), kd = k_desc + stg * (C::TILE_BYTES >> 4);
                             if (elect_one()) {
 #pragma unroll
                                 for (int k = 0; k < D / 16; ++k)
-                                    mma_f16(tmem + C::TM_S + s * AT_WIDE_KEYS, qd + (((k / 4) * C::QHALF_BYTES + (k % 4) * 32) >> 4),
+                                    mma_f16(tmem + C::TM_S, qd + (((k / 4) * C::QHALF_BYTES + (k % 4) * 32) >> 4),
                                             kd + (((k / 4) * C::HALF_BYTES + (k % 4) * 32) >> 4), IDESC_S, k ? 1u : 0u);
                                 tc_commit(&s_full[s]);
                                 if (!pair || s == 1) tc_commit(&empty[stg]);
@@ -383,49 +404,50 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                             __syncwarp();
                         }
                         // between the two S: stream 1's P V; behind them: stream 0's
-                        const int t = s ^ 1, i = j - 1 - t, pcnt = t ? cnt1 : cnt0;
-                        if (i >= 0 && i < pcnt) {
-                            const uint32_t ld = base + (pair ? 0 : 2 * t) + i * two + 1, stg = ld % STAGES;
-                            if (i == 0 && (t == 0 || cnt0 == 0)) {      // the epilogue of the unit before has read O
+                        const int x = s ^ 1, i = j - 1 - x;
+                        if (i >= 0 && i < (x ? cnt1 : cnt0)) {
+                            const int tile = pair ? i : 2 * i + x;
+                            const uint32_t t = base + tile, stg = STAGES + t % STAGES;
+                            if (i == 0 && (x == 0 || cnt0 == 0)) {      // the epilogue of the unit before has read O
                                 if (!wait_bounded(o_empty, oe_ph, abort_flag, 67)) goto done;
                                 oe_ph ^= 1u;
                             }
-                            if (!wait_bounded(&full[stg], (ld / STAGES) & 1u, abort_flag, 68)) goto done;
-                            const int kt = ka + (int)(ld - base) / 2;
-                            if ((kt == end_front || kt == end_own) && (t == 0 || !pair || i >= cnt0)) {
+                            if (!wait_bounded(&full[stg], (t / STAGES) & 1u, abort_flag, 68)) goto done;
+                            if ((tile == end_front || tile == end_own) && (x == 0 || !pair || i >= cnt0)) {
                                 if (lane == 0) mbar_arrive(v_end);
                                 __syncwarp();
                                 if (!wait_bounded(v_clean, vc_ph, abort_flag, 81)) goto done;
                                 vc_ph ^= 1u;
                             }
-                            if (!wait_bounded(&p_full[t], (p_ph >> t) & 1u, abort_flag, 69)) goto done;
-                            p_ph ^= 1u << t;
+                            if (!wait_bounded(&p_full[x], (p_ph >> x) & 1u, abort_flag, 69)) goto done;
+                            p_ph ^= 1u << x;
                             tc_fence_after();
                             const uint64_t vd = v_desc + stg * (C::TILE_BYTES >> 4);
                             if (elect_one()) {
 #pragma unroll
                                 for (int k = 0; k < AT_WIDE_KEYS / 16; ++k)
-                                    mma_f16_ts(tmem + C::TM_O + t * D, tmem + C::TM_P + t * (AT_WIDE_KEYS / 2) + k * 8, vd + k * 128, IDESC_O,
+                                    mma_f16_ts(tmem + C::TM_O + x * D, tmem + C::TM_P + x * (AT_WIDE_KEYS / 2) + k * 8, vd + k * 128, IDESC_O,
                                                (i | k) ? 1u : 0u);
-                                tc_commit(&pv_done[t]);
-                                if (!pair || t == 1) tc_commit(&empty[stg]);
+                                tc_commit(&pv_done[x]);
+                                if (!pair || x == 1) tc_commit(&empty[stg]);
                             }
                             __syncwarp();
                         }
                     }
                 }
-                base += 2 * (uint32_t)n;
+                base += n;
                 if (lane == 0) mbar_arrive(&u_empty[b]);
                 if (++b == 2) { b = 0; u_ph ^= 1u; }
             }
         }
     } else {
         // ------------------------------------------------------------------------------------------ softmax
+        regs_inc<AW_REGS_SOFTMAX>();
         const int s = warp >> 2;                                         // stream
         const int r = threadIdx.x & 127;                                 // row of the tile = TMEM lane
         const int my_tok = r / a.G;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t t_s = tmem + lanes + C::TM_S + s * AT_WIDE_KEYS, t_p = tmem + lanes + C::TM_P + s * (AT_WIDE_KEYS / 2), t_o = tmem + lanes + C::TM_O;
+        const uint32_t t_s = tmem + lanes + C::TM_S, t_p = tmem + lanes + C::TM_P + s * (AT_WIDE_KEYS / 2), t_o = tmem + lanes + C::TM_O;
         const float scale = a.scale_log2;
         uint32_t s_ph = 0, pv_ph = 0, e_ph = 0, u_ph = 0;
         int b = 0;
@@ -446,18 +468,18 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                     if (!wait_bounded(&s_full[s], s_ph, abort_flag, 70)) goto done;
                     s_ph ^= 1u;
                     tc_fence_after();
-                    uint32_t v[2][32];
-                    tmem_ld_32x32(t_s, v[0]);
-                    tmem_ld_32x32(t_s + 32, v[1]);
+                    uint32_t v[4][32];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) tmem_ld_32x32(t_s + j * 32, v[j]);
                     const int left = kt < nf ? w.plen - kt * AT_WIDE_KEYS : sees - (kt - nf) * AT_WIDE_KEYS;      // keys of the tile that the row sees
                     const bool whole = __all_sync(0xFFFFFFFFu, left >= AT_WIDE_KEYS);
                     tmem_ld_wait();
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(&s_empty[s]);
+                    if (lane == 0) mbar_arrive(s_empty);
                     if (!whole) {
 #pragma unroll
-                        for (int j = 0; j < 2; ++j)
+                        for (int j = 0; j < 4; ++j)
 #pragma unroll
                             for (int e = 0; e < 32; ++e)
                                 if (j * 32 + e >= left) v[j][e] = 0xFF800000u;
@@ -465,9 +487,10 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                     float mx[4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        mx[j] = fmaxf(__uint_as_float(v[0][j]), __uint_as_float(v[1][j]));
+                        mx[j] = __uint_as_float(v[j][0]);
 #pragma unroll
-                        for (int e = j + 4; e < 32; e += 4) mx[j] = max3(mx[j], __uint_as_float(v[0][e]), __uint_as_float(v[1][e]));
+                        for (int e = 1; e < 31; e += 2) mx[j] = max3(mx[j], __uint_as_float(v[j][e]), __uint_as_float(v[j][e + 1]));
+                        mx[j] = fmaxf(mx[j], __uint_as_float(v[j][31]));
                     }
                     const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
                     const bool move = top > m + AT_SLACK;
@@ -476,9 +499,9 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                     const float ref = m == -INFINITY ? 0.0f : -m;
                     const uint64_t scale2 = pack2(scale, scale), ref2 = pack2(ref, ref);
                     uint64_t sum[2] = {0, 0};
-                    uint32_t pk[2][16];
+                    uint32_t pk[4][16];
 #pragma unroll
-                    for (int j = 0; j < 2; ++j)
+                    for (int j = 0; j < 4; ++j)
 #pragma unroll
                         for (int e = 0; e < 32; e += 2) {
                             float p0, p1;
@@ -504,8 +527,8 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                             }
                         }
                     }
-                    tmem_st_32x16(t_p, pk[0]);
-                    tmem_st_32x16(t_p + 16, pk[1]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) tmem_st_32x16(t_p + j * 16, pk[j]);
                     tmem_st_wait();
                     tc_fence_before();
                     __syncwarp();
@@ -654,11 +677,22 @@ static cudaError_t launch_attn_few(const AttnArgs& a, bool early, cudaStream_t s
     if (e != cudaSuccess) return e;
     return launch_pdl(attn_few_kernel<D, HW, SELF>, dim3(a.few_ctas), dim3(AT_FEW_THREADS), smem, st, a, early);
 }
+// The kernel's register split only works out if it was compiled to be launched with AW_REGS_LAUNCH registers a thread.
+template <int D>
+static cudaError_t prepare_attn_wide() {
+    static PerDevice pd;
+    const int slot = per_device_slot();
+    if (slot >= 0 && pd.done[slot]) return cudaSuccess;
+    cudaFuncAttributes fa;
+    cudaError_t e = cudaFuncGetAttributes(&fa, attn_wide_kernel<D>);
+    if (e != cudaSuccess) return e;
+    if (fa.numRegs != AW_REGS_LAUNCH) return cudaErrorInvalidKernelImage;
+    return opt_in_shared_memory(pd, attn_wide_kernel<D>, WideCfg<D>::SMEM);
+}
 template <int D>
 static cudaError_t launch_attn_d(const AttnWideArgs& w, bool wide, cudaStream_t st) {
-    static PerDevice pd_wide;
     const AttnArgs& a = w.a;
-    cudaError_t e = wide ? opt_in_shared_memory(pd_wide, attn_wide_kernel<D>, WideCfg<D>::SMEM) : cudaSuccess;
+    cudaError_t e = wide ? prepare_attn_wide<D>() : cudaSuccess;
     if (e != cudaSuccess) return e;
     if (!wide && a.P == 0 && a.R <= FEW_SELF && a.few_hw == 4) {
         if ((e = launch_attn_few<D, 4, true>(a, false, st)) != cudaSuccess) return e;

@@ -26,7 +26,7 @@ namespace osc {
 
 constexpr int AT_FEW_ROWS = 16;              // rows of a few-row unit
 constexpr int AT_WIDE_TILE = 128;            // rows of one tcgen05 tile; a wide unit has two of them
-constexpr int AT_WIDE_KEYS = 64;             // keys of its tiles
+constexpr int AT_WIDE_KEYS = 128;            // keys of its tiles
 constexpr int AT_MERGE_ROWS = 2 * AT_WIDE_TILE;  // a group whose requests all have at least this many rows has no prefix segment
 constexpr int AT_MAX_SMS = 148;
 constexpr int AT_FEW_CTAS = 2 * AT_MAX_SMS;  // most CTAs of the few-row kernel (two per SM)
@@ -135,14 +135,14 @@ struct FewUnits {
     }
 };
 struct WideUnits {
-    __device__ static constexpr int key_shift(const AttnArgs&) { return 6; }
+    __device__ static constexpr int key_shift(const AttnArgs&) { return 7; }
     __device__ static int heads(const AttnArgs& a) { return a.Hk; }
     __device__ static int tokens(const AttnArgs& a) { return 2 * (AT_WIDE_TILE / a.G); }
     __device__ static int count(const AttnArgs& a, const Segment& g) { return (int)(((int64_t)g.n + tokens(a) - 1) / tokens(a)); }
     __device__ static int last_token(const AttnArgs& a, const Segment& g, int u) {
         return (int)min((int64_t)g.n, ((int64_t)u + 1) * tokens(a)) - 1;
     }
-    // own keys, all units but the last: ceil((klen - n + (u + 1) tokens) / 64)
+    // own keys, all units but the last: ceil((klen - n + (u + 1) tokens) / 128)
     __device__ static void line(const AttnArgs& a, const Segment& g, int64_t& A, int64_t& B, int64_t& M, int64_t& u0) {
         const int64_t before = (int64_t)g.klen - g.n;
         A = tokens(a);
@@ -208,7 +208,7 @@ __device__ __forceinline__ int head_tiles(const AttnArgs& a, const Segment& g) {
 __device__ __forceinline__ int share_tiles(int N, int ctas, int least) { return max((int)(((int64_t)N + ctas - 1) / ctas), least); }
 // least share: 64 keys of few_hw heads
 __device__ __forceinline__ int few_min_tiles(const AttnArgs& a) { return a.few_hw; }
-constexpr int AT_WIDE_MIN_TILES = 4;
+constexpr int AT_WIDE_MIN_TILES = 2;
 
 // Where a cursor finds segments and their first tiles: what the plan kernel left in the workspace, or (SELF) shared memory.
 template <bool SELF>
