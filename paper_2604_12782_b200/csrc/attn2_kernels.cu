@@ -11,13 +11,12 @@
 // With D = 128 two S (128 x 128), two P and two O do not fit TMEM.  The streams share ONE S: a softmax thread takes its whole row of scores
 // into registers at once, and the other stream's product can go there a few hundred cycles later.  (Each stream with its own S and P in the
 // columns of that S made a stream's steps run strictly one after the other - S, softmax, P V, next S: 3700 cycles for 128 keys of both tiles,
-// tensor pipe 47 % busy; own S and P with 64-key tiles: 5500, twice the MMA warp's steps, whose 500 cycles each were then what counted.)
+// tensor pipe 47 % busy; own S and P with 64-key tiles: 5500, twice the MMA warp's steps, whose overhead was then what counted.)
 //
 //   warps 0-3, 4-7 : softmax of stream 0, 1, and their epilogue
 //   warp 8         : TMA (a key tile is loaded page by page; a page that is not there reads as zeros)
-//   warp 9         : MMA issue, TMEM owner
+//   warps 9, 11    : MMA issue of S, of P V (warp 9 owns TMEM)
 //   warp 10        : the units of the CTA's share, for everyone else
-//   warp 11        : zeros behind the last key of a V tile
 //
 // P V with the weights of the running maximum as it stands: O is rescaled in TMEM only when the maximum has moved by
 // more than 2^8 (see AT_SLACK), by the softmax threads themselves, between the P V before and the one to come.
@@ -173,9 +172,7 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
     uint64_t* o_empty = q_full + 13;
     uint64_t* e_full = q_full + 14;
     uint64_t* drain_bar = q_full + 15;
-    uint64_t* v_clean = q_full + 16;
-    uint64_t* v_end = q_full + 17;
-    constexpr int BARS = 4 * STAGES + 18;
+    constexpr int BARS = 4 * STAGES + 16;
     WideUnit* units = reinterpret_cast<WideUnit*>(reinterpret_cast<uint8_t*>(bars) + C::BAR_BYTES);   // [2]
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + BARS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
@@ -186,7 +183,7 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
     if (threadIdx.x == 0) {
         for (int i = 0; i < BARS; ++i) {
             const int b = i - 4 * STAGES;      // all barriers take one arrival but these
-            mbar_init(&bars[i], b == 4 || b == 5 || b == 12 ? NSW / 2 : b == 10 || b == 11 ? NSW + 3 : b == 13 || b == 14 ? NSW : 1);
+            mbar_init(&bars[i], b == 4 || b == 5 || b == 12 ? NSW / 2 : b == 10 || b == 11 ? NSW + 3 : b == 13 || b == 14 ? NSW : b == 15 ? 2 : 1);
         }
         *abort_flag = 0;
         fence_barrier_init();
@@ -328,64 +325,33 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                 }
                 wait_bounded(q_full, q_ph ^ 1u, never, 64);
             }
-        } else if (warp == NSW + 3) {
-            // ----------------------------------------------------------------------------- ends of V lists
-            // Behind the last key of a list the page holds whatever was there before: a NaN or Inf would survive its weight of 0.  The
-            // MMA thread says when such a tile is there and waits for it to be cleaned.
-            uint32_t base = 0, u_ph = 0, ve_ph = 0;
-            int b = 0;
-            while (true) {
-                if (!wait_bounded(&u_full[b], u_ph, abort_flag, 77)) goto done;
-                const WideUnit& w = units[b];
-                const int n = w.n;
-                if (n == 0) break;
-                for (int kt = w.nf > w.ka ? w.nf - 1 : w.ka + n - 1; kt < w.ka + n; kt = w.ka + n - 1 > kt ? w.ka + n - 1 : w.ka + n) {
-                    const int left = unit_left(w, kt);
-                    if (left >= AT_WIDE_KEYS) continue;
-                    const uint32_t stg = STAGES + (base + kt - w.ka) % STAGES;
-                    if (!wait_bounded(v_end, ve_ph, abort_flag, 80)) goto done;
-                    ve_ph ^= 1u;
-                    uint8_t* v = ring + stg * C::TILE_BYTES;
-                    for (int c = left * 8 + lane; c < AT_WIDE_KEYS * 8; c += 32)
-                        for (int hf = 0; hf < C::HALVES; ++hf) *reinterpret_cast<uint4*>(v + hf * C::HALF_BYTES + c * 16) = make_uint4(0u, 0u, 0u, 0u);
-                    fence_proxy_async_smem();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(v_clean);
-                }
-                base += n;
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&u_empty[b]);
-                if (++b == 2) { b = 0; u_ph ^= 1u; }
-            }
         } else {
-            // --------------------------------------------------------------------------------------- MMA
-            // The whole warp walks through this (one elected lane issues), and what it reads from shared memory goes through a shuffle: only
-            // then do the descriptors stay in uniform registers.  Run by one thread, every MMA took two to three times as long to issue.
+            // --------------------------------------------------------------------------------- MMA: S, and P V
+            // Two warps, because the products are independent of each other (S and P have columns of their own) and an issuing warp is
+            // held up until its MMAs are nearly through: with one warp for all four products of a step, its waits and address
+            // arithmetic (370 cycles each) came on top of the 520 cycles of each product.
+            // The whole warp walks through the loops (one elected lane issues), and what it reads from shared memory goes through a shuffle:
+            // only then do the descriptors stay in uniform registers.
             auto uni = [](int x) { return __shfl_sync(0xFFFFFFFFu, x, 0); };
+            const bool s_warp = warp == NSW + 1;
             const uint64_t q_desc = smem_desc_sw128(smem_u32(smem)), k_desc = smem_desc_sw128(ring0);
             const uint64_t v_desc = smem_desc_sw128_mn(ring0, C::HALVES > 1 ? C::HALF_BYTES : 1024);
             constexpr uint32_t IDESC_S = idesc_bf16(128, AT_WIDE_KEYS), IDESC_O = idesc_bf16(128, D) | IDESC_B_MN;
             uint32_t base = 0;                 // tiles of the units before
-            uint32_t q_ph = 0, p_ph = 0, se_ph = 1, oe_ph = 1, u_ph = 0, vc_ph = 0;
+            uint32_t q_ph = 0, p_ph = 0, se_ph = 1, oe_ph = 1, u_ph = 0;
             int b = 0;
             while (true) {
                 if (!wait_bounded(&u_full[b], u_ph, abort_flag, 78)) goto done;
                 const WideUnit& w = units[b];
-                const int n = uni(w.n), cnt0 = uni(w.cnt[0]), cnt1 = uni(w.cnt[1]), pair = uni(w.pair), ka = uni(w.ka);
-                const int nf = uni(w.nf), plen = uni(w.plen), klen = uni(w.klen);
+                const int n = uni(w.n), cnt0 = uni(w.cnt[0]), cnt1 = uni(w.cnt[1]), pair = uni(w.pair), most = max(cnt0, cnt1);
                 if (n == 0) break;
-                // tiles of the unit's part that end inside (V to be cleaned), counted from its first
-                const int end_front = plen % AT_WIDE_KEYS ? nf - 1 - ka : -1, end_own = klen % AT_WIDE_KEYS ? nf + klen / AT_WIDE_KEYS - ka : -1;
-                if (!wait_bounded(q_full, q_ph, abort_flag, 65)) goto done;
-                q_ph ^= 1u;
-                const int most = max(cnt0, cnt1);
-                // Step j: S0(j), P V of stream 1's tile j - 2, S1(j), P V of stream 0's tile j - 1: the order in which their inputs come when the
-                // streams are half a period apart.
-                for (int j = 0; j <= most + 1; ++j) {
+                if (s_warp) {
+                    if (!wait_bounded(q_full, q_ph, abort_flag, 65)) goto done;
+                    q_ph ^= 1u;
+                    for (int j = 0; j < most; ++j) {
 #pragma unroll
-                    for (int s = 0; s < 2; ++s) {
-                        const int cnt = s ? cnt1 : cnt0;
-                        if (j < cnt) {
+                        for (int s = 0; s < 2; ++s) {
+                            if (j >= (s ? cnt1 : cnt0)) continue;
                             const uint32_t t = base + (pair ? j : 2 * j + s), stg = t % STAGES;
                             if (!wait_bounded(&full[stg], (t / STAGES) & 1u, abort_flag, 66)) goto done;
                             if (!wait_bounded(s_empty, se_ph, abort_flag, 84)) goto done;     // the S before has been read
@@ -399,25 +365,34 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                                             kd + (((k / 4) * C::HALF_BYTES + (k % 4) * 32) >> 4), IDESC_S, k ? 1u : 0u);
                                 tc_commit(&s_full[s]);
                                 if (!pair || s == 1) tc_commit(&empty[stg]);
-                                if (j == cnt - 1 && (s ? cnt1 >= cnt0 : cnt0 > cnt1)) tc_commit(q_empty);      // no more S of this unit
                             }
                             __syncwarp();
                         }
-                        // between the two S: stream 1's P V; behind them: stream 0's
-                        const int x = s ^ 1, i = j - 1 - x;
-                        if (i >= 0 && i < (x ? cnt1 : cnt0)) {
+                    }
+                    if (elect_one()) tc_commit(q_empty);      // no more S of this unit
+                    __syncwarp();
+                } else {
+                    // tiles of the unit's part that end inside, counted from its first
+                    const int ka = uni(w.ka), nf = uni(w.nf), plen = uni(w.plen), klen = uni(w.klen);
+                    const int end_front = plen % AT_WIDE_KEYS ? nf - 1 - ka : -1, end_own = klen % AT_WIDE_KEYS ? nf + klen / AT_WIDE_KEYS - ka : -1;
+                    if (!wait_bounded(o_empty, oe_ph, abort_flag, 67)) goto done;      // the epilogue of the unit before has read O
+                    oe_ph ^= 1u;
+                    for (int i = 0; i < most; ++i) {
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            if (i >= (x ? cnt1 : cnt0)) continue;
                             const int tile = pair ? i : 2 * i + x;
                             const uint32_t t = base + tile, stg = STAGES + t % STAGES;
-                            if (i == 0 && (x == 0 || cnt0 == 0)) {      // the epilogue of the unit before has read O
-                                if (!wait_bounded(o_empty, oe_ph, abort_flag, 67)) goto done;
-                                oe_ph ^= 1u;
-                            }
                             if (!wait_bounded(&full[stg], (t / STAGES) & 1u, abort_flag, 68)) goto done;
                             if ((tile == end_front || tile == end_own) && (x == 0 || !pair || i >= cnt0)) {
-                                if (lane == 0) mbar_arrive(v_end);
+                                // Behind the last key of a list the page holds whatever was there before: a NaN or Inf would survive its weight of 0.
+                                const int left = unit_left(w, ka + tile);
+                                uint8_t* v = smem + 2 * C::QTILE_BYTES + stg * C::TILE_BYTES;
+                                for (int c = left * 8 + lane; c < AT_WIDE_KEYS * 8; c += 32)
+                                    for (int hf = 0; hf < C::HALVES; ++hf)
+                                        *reinterpret_cast<uint4*>(v + hf * C::HALF_BYTES + c * 16) = make_uint4(0u, 0u, 0u, 0u);
+                                fence_proxy_async_smem();
                                 __syncwarp();
-                                if (!wait_bounded(v_clean, vc_ph, abort_flag, 81)) goto done;
-                                vc_ph ^= 1u;
                             }
                             if (!wait_bounded(&p_full[x], (p_ph >> x) & 1u, abort_flag, 69)) goto done;
                             p_ph ^= 1u << x;
@@ -653,10 +628,10 @@ done:
     __syncwarp();
     tc_fence_before();
     __syncthreads();
+    if (*abort_flag && (warp == NSW + 1 || warp == NSW + 3) && lane == 0) tc_commit(drain_bar);
     if (warp == NSW + 1) {
         if (*abort_flag && lane == 0) {
             // gave up somewhere: let outstanding tensor-core work retire before TMEM goes away
-            tc_commit(drain_bar);
             int dummy = 0;
             volatile int* never = &dummy;
             wait_bounded(drain_bar, 0, never, 73);
