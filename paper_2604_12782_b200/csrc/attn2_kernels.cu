@@ -201,7 +201,7 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
     const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, *tmem_slot, 0);
     grid_dependency_wait();
     grid_launch_dependents();   // not before: the few-row kernel counts on the plan being there when it begins
-    const int tpt = AT_WIDE_TILE / a.G;
+    const int tpt = a.tpt;
     const uint32_t ring0 = smem_u32(ring);
 
     if (warp >= NSW) {
@@ -679,12 +679,12 @@ static cudaError_t launch_attn_d(const AttnWideArgs& w, bool wide, cudaStream_t 
             : a.few_hw == 2 ? launch_attn_few<D, 2, false>(a, wide, st) : launch_attn_few<D, 1, false>(a, wide, st);
         if (e != cudaSuccess) return e;
     }
-    // Blocks with nothing to do cost a wave of the grid too: few-row units are cut small only where there is nothing else.
-    const int wide_split = (int64_t)a.T * a.G >= 2048 ? 8 : 2, few_split = wide ? 1 : a.few_hw;
-    const int wide_blocks = wide ? a.wide_ctas * wide_split : 0, few_blocks = a.few_ctas * few_split;
-    const int token_blocks = a.P ? (int)std::min<int64_t>(3 * AT_MAX_SMS, ((int64_t)a.T * a.Hq + AT_JOIN_WARPS - 1) / AT_JOIN_WARPS) : 0;
-    return launch_pdl(attn_join_kernel<D>, dim3(wide_blocks + few_blocks + token_blocks), dim3(AT_JOIN_THREADS), 0, st, a, wide_blocks, wide_split,
-                      few_blocks, few_split);
+    JoinGrid g;
+    g.wide_split = (int64_t)a.T * a.G >= 2048 ? 8 : 1;      // with few rows nearly all of them have two sources
+    g.wide_blocks = wide ? a.wide_ctas * g.wide_split : 0;
+    g.few_blocks = a.few_ctas * a.few_hw;
+    g.row_blocks = a.P ? (int)std::min<int64_t>(3 * AT_MAX_SMS, ((int64_t)a.T * a.Hq + AT_JOIN_WARPS - 1) / AT_JOIN_WARPS) : 0;
+    return launch_pdl(attn_join_kernel<D>, dim3(g.wide_blocks + g.few_blocks + g.row_blocks), dim3(AT_JOIN_THREADS), 0, st, a, g);
 }
 
 cudaError_t launch_attn(const AttnWideArgs& w, int D, bool wide, cudaStream_t st) {

@@ -191,7 +191,7 @@ osc_status osc_paged_attention(const void* Q, int T, int64_t ldq, int n_q, const
     a.page_stride = cache->page_stride; a.token_stride = cache->token_stride; a.head_stride = cache->head_stride;
     a.row_off = row_off; a.kv_len = kv_len; a.table = table; a.ld_table = ld_table; a.cols = cols;
     a.group_off = group_off; a.prefix_len = prefix_len; a.ptable = prefix_table; a.ld_ptable = ld_prefix; a.pcols = P ? prefix_cols : 0;
-    a.T = T; a.Hq = n_q; a.Hk = cache->n_heads; a.G = n_q / cache->n_heads; a.head_dim = D; a.R = R; a.P = P; a.n_pages = cache->n_pages;
+    a.T = T; a.Hq = n_q; a.Hk = cache->n_heads; a.G = n_q / cache->n_heads; a.tpt = AT_WIDE_TILE / a.G; a.head_dim = D; a.R = R; a.P = P; a.n_pages = cache->n_pages;
     while ((1 << a.page_shift) < cache->page_size) ++a.page_shift;
     a.scale_log2 = scale * 1.44269504088896341f;
     a.few_hw = hw;
@@ -204,7 +204,7 @@ osc_status osc_paged_attention(const void* Q, int T, int64_t ldq, int n_q, const
     a.wide_min_rows = wide ? AT_FEW_ROWS + 1 : 0x7FFFFFFF;
     if (wide) {
         const int64_t qd[3] = {D, n_q, T}, qs[3] = {1, D, ldq};
-        const int qb[3] = {64, a.G, AT_WIDE_TILE / a.G};
+        const int qb[3] = {64, a.G, a.tpt};
         const int64_t kd[4] = {D, cache->page_size, cache->n_heads, cache->n_pages};
         const int64_t ks[4] = {1, cache->token_stride, cache->head_stride, cache->page_stride};
         const int kb[4] = {64, cache->page_size < AT_WIDE_KEYS ? cache->page_size : AT_WIDE_KEYS, 1, 1};

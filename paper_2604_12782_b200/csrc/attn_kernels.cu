@@ -83,6 +83,7 @@ struct AttnArgs {
     int64_t ld_table, ld_ptable;
     int T, Hq, Hk, G, head_dim, R, P, cols, pcols, page_shift, n_pages;
     int wide_min_rows;       // segments with at least this many rows per head go to the tcgen05 kernel
+    int tpt;                 // whole tokens that fit the 128 rows of a tcgen05 tile
     int few_hw;              // heads of a few-row unit: 4, 2 or 1
     int few_ctas, wide_ctas;
     float scale_log2;        // scale * log2(e)
@@ -115,14 +116,15 @@ __device__ __forceinline__ const int32_t* seg_pages(const AttnArgs& a, int s) {
 // keys that token i of the segment sees, without the prefix in front
 __device__ __forceinline__ int seg_sees(const Segment& g, int i) { return g.flags & SEG_OWN ? max(g.klen - g.n + i + 1, 0) : g.klen; }
 
+// Rows of a segment (tokens x heads of one key/value head) and of all segments are ints: the host has seen to T * n_q <= 2^29.
 // The two kinds of units.  Few-row: 16 consecutive (token, head) rows of one token list, few_hw heads side by side, tiles
 // of 64 / few_hw keys.  Wide: two tiles of as many whole tokens as fit 128 rows, one head.
 struct FewUnits {
     __device__ static int key_shift(const AttnArgs& a) { return a.few_hw == 4 ? 4 : a.few_hw == 2 ? 5 : 6; }
     __device__ static int heads(const AttnArgs& a) { return a.Hk / a.few_hw; }
-    __device__ static int count(const AttnArgs& a, const Segment& g) { return (int)(((int64_t)g.n * a.G + AT_FEW_ROWS - 1) / AT_FEW_ROWS); }
+    __device__ static int count(const AttnArgs& a, const Segment& g) { return (g.n * a.G + AT_FEW_ROWS - 1) / AT_FEW_ROWS; }
     __device__ static int last_token(const AttnArgs& a, const Segment& g, int u) {
-        return (int)min((int64_t)(g.n - 1), ((int64_t)u * AT_FEW_ROWS + AT_FEW_ROWS - 1) / a.G);
+        return min(g.n - 1, (u * AT_FEW_ROWS + AT_FEW_ROWS - 1) / a.G);
     }
     // own keys, all units but the last: ceil((klen - n + 1 + floor((16 u + 15) / G)) / KEYS)
     __device__ static void line(const AttnArgs& a, const Segment& g, int64_t& A, int64_t& B, int64_t& M, int64_t& u0) {
@@ -137,10 +139,10 @@ struct FewUnits {
 struct WideUnits {
     __device__ static constexpr int key_shift(const AttnArgs&) { return 7; }
     __device__ static int heads(const AttnArgs& a) { return a.Hk; }
-    __device__ static int tokens(const AttnArgs& a) { return 2 * (AT_WIDE_TILE / a.G); }
-    __device__ static int count(const AttnArgs& a, const Segment& g) { return (int)(((int64_t)g.n + tokens(a) - 1) / tokens(a)); }
+    __device__ static int tokens(const AttnArgs& a) { return 2 * a.tpt; }
+    __device__ static int count(const AttnArgs& a, const Segment& g) { return (g.n + tokens(a) - 1) / tokens(a); }
     __device__ static int last_token(const AttnArgs& a, const Segment& g, int u) {
-        return (int)min((int64_t)g.n, ((int64_t)u + 1) * tokens(a)) - 1;
+        return min(g.n, (u + 1) * tokens(a)) - 1;
     }
     // own keys, all units but the last: ceil((klen - n + (u + 1) tokens) / 128)
     __device__ static void line(const AttnArgs& a, const Segment& g, int64_t& A, int64_t& B, int64_t& M, int64_t& u0) {
@@ -410,7 +412,7 @@ __global__ void __launch_bounds__(1024) attn_plan_kernel(const AttnArgs a) {
                 two |= g.n > 0 && (g.flags & SEG_TWO);
                 empty |= g.n > g.klen && g.group < 0;
             }
-            if ((int64_t)g.n * a.G >= a.wide_min_rows) {
+            if (g.n * a.G >= a.wide_min_rows) {
                 g.flags |= SEG_WIDE;
                 g.tiles = head_tiles<WideUnits>(a, g);
                 own[1] = g.tiles * WideUnits::heads(a);
@@ -478,8 +480,8 @@ __device__ __forceinline__ PieceList list_pieces(int begin, int tiles, int q, in
 }
 
 // --------------------------------------------------------------------------------------------- few rows
-__device__ __forceinline__ void cp_async_16(uint32_t dst, const void* src, bool valid) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0) : "memory");
+__device__ __forceinline__ void cp_async_16(uint32_t dst, const void* src, bool valid, uint64_t policy) {
+    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0), "l"(policy) : "memory");
 }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -610,6 +612,7 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
     };
     int xl = x0;                       // loader's position
     int page = page_of();
+    const uint64_t policy = l2_policy_evict_first();   // read once: must not push code, plan and partial results out of L2
     auto load = [&](int slot) {
         if (xl < x1) {
             const int key = ld.kt * KEYS + kw;
@@ -622,8 +625,8 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
                 const int r = (i * 32 + lane) / CHUNKS, c = (i * 32 + lane) % CHUNKS;
                 const int64_t off = r < nvalid ? base + (int64_t)r * a.token_stride + c * 8 : 0;
                 const uint32_t d = dst + r * (D * 2) + ((c ^ (r & 7)) * 16);
-                cp_async_16(d, a.k + off, r < nvalid);
-                cp_async_16(d + C::KV_BYTES, a.v + off, r < nvalid);
+                cp_async_16(d, a.k + off, r < nvalid, policy);
+                cp_async_16(d + C::KV_BYTES, a.v + off, r < nvalid, policy);
             }
             if (++xl < x1) {
                 if (++ld.kt == ld.nt) ld.next_unit(a, src, 0);
@@ -632,7 +635,7 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
         }
         cp_async_commit();
     };
-#pragma unroll
+#pragma unroll 1
     for (int i = 0; i < C::STAGES - 1; ++i) load(i);
 
     const int r0 = lane >> 2, cq = lane & 3;       // the thread's rows r0, r0 + 8 and column pair of an MMA fragment
@@ -641,7 +644,7 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
     while (x < x1) {
         // ---- a unit (or the share's part of it)
         const int row0 = cur.u * AT_FEW_ROWS;
-        const int nrows = (int)min((int64_t)AT_FEW_ROWS, (int64_t)cur.g.n * a.G - row0);
+        const int nrows = min(AT_FEW_ROWS, cur.g.n * a.G - row0);
         const int head = cur.h * HW + hw;
         uint32_t qf[KS][4];
         int sees[2];
@@ -814,147 +817,129 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
 }
 
 // ------------------------------------------------------------------------------------------------- join
-// Joins the pieces of rows whose keys were not all in one unit of one share, one warp per row, in the order of the
-// lines (so the result does not depend on which CTA was first).  Three kinds of blocks, because the rows to be joined are not
-// known on the host and looking at every row costs more than the joining (262 us for 8001 tokens of prompts
-// against 1 ms of attention, when it was done that way):
+// Joins the pieces of rows whose keys were not all in one unit of one share, in the order of the lines (so the result does not depend on
+// which CTA was first), one warp to a row.  Three kinds of blocks, because the rows to be joined are not known on the host and looking at
+// every row costs more than the joining (262 us for 8001 tokens of prompts against 1 ms of attention, when it was done that way):
 //   units that the end of a share cuts, as the attention kernels told them: blocks for every share of either line;
 //   rows with two sources (prefix and own keys): blocks over the tokens, only launched where there are prefixes.
+// The code is kept short and mostly rolled: behind a kernel that has streamed hundreds of MB through L2 it comes from HBM line by
+// line, and a version with four rows to a warp and pieces shared out over warps, though it had more loads under way, took longer.
 constexpr int AT_JOIN_THREADS = 256;
 constexpr int AT_JOIN_WARPS = AT_JOIN_THREADS / 32;
 
-// Pieces are taken 32 at a time: a lane finds the place, m and l of one; eight rows of O are under way at a time.
 template <int D>
-__device__ __forceinline__ void join_row(const AttnArgs& a, const PieceList& p0, const PieceList& p1, int64_t token, int hq) {
+__device__ __forceinline__ void join_row(const AttnArgs& a, const PieceList& p0, const PieceList& p1, int token, int hq) {
     constexpr int V = D / 32;          // channels per lane
-    constexpr int FLIGHT = 8;
-    const int lane = threadIdx.x & 31;
+    constexpr int FLIGHT = 8;          // pieces under way at a time
+    const int lane = threadIdx.x & 31, n = p0.count + p1.count;
     float m = -INFINITY, l = 0.0f, o[V];
 #pragma unroll
-    for (int j = 0; j < V; ++j) o[j] = 0.0f;
-    const int n = p0.count + p1.count;
-    for (int i0 = 0; i0 < n; i0 += 32) {
-        const int i = min(i0 + lane, n - 1), k = min(32, n - i0);
-        const int at = i < p0.count ? p0.at(i) : p1.at(i - p0.count);
-        float2 ml = a.ml[at];
-        if (i0 + lane >= n) ml = make_float2(-INFINITY, 0.0f);
-        float w = 0.0f;
-        for (int b = 0; b < k; b += FLIGHT) {
-            float v[FLIGHT][V];
+    for (int y = 0; y < V; ++y) o[y] = 0.0f;
+#pragma unroll 1
+    for (int i = 0; i < n; i += FLIGHT) {
+        float2 ml[FLIGHT];
+        float v[FLIGHT][V];
 #pragma unroll
-            for (int j = 0; j < FLIGHT; ++j) {
-                if (b + j < k) {
-                    const float* src = a.part + (int64_t)__shfl_sync(0xFFFFFFFFu, at, b + j) * D + lane * V;
-                    if (V == 4) {
-                        const float4 x = *reinterpret_cast<const float4*>(src);
-                        v[j][0] = x.x; v[j][1] = x.y; v[j][V - 2] = x.z; v[j][V - 1] = x.w;
-                    } else {
-                        const float2 x = *reinterpret_cast<const float2*>(src);
-                        v[j][0] = x.x; v[j][1] = x.y;
-                    }
-                }
-            }
-            if (b == 0) {
-                float mx = ml.x;
-#pragma unroll
-                for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, d));
-                mx = fmaxf(mx, m);
-                const float f0 = mx == -INFINITY ? 0.0f : exp2_approx(m - mx);
-                w = mx == -INFINITY ? 0.0f : exp2_approx(ml.x - mx);
-                float lw = ml.y * w;
-#pragma unroll
-                for (int d = 16; d > 0; d >>= 1) lw += __shfl_xor_sync(0xFFFFFFFFu, lw, d);
-                m = mx;
-                l = l * f0 + lw;
-#pragma unroll
-                for (int j = 0; j < V; ++j) o[j] *= f0;
-            }
-#pragma unroll
-            for (int j = 0; j < FLIGHT; ++j) {
-                if (b + j < k) {
-                    const float wj = __shfl_sync(0xFFFFFFFFu, w, b + j);
-                    if (wj != 0.0f)    // a piece without weight may hold anything
-#pragma unroll
-                        for (int y = 0; y < V; ++y) o[y] = fmaf(v[j][y], wj, o[y]);
-                }
+        for (int j = 0; j < FLIGHT; ++j) {
+            const int x = min(i + j, n - 1), at = x < p0.count ? p0.at(x) : p1.at(x - p0.count);
+            ml[j] = a.ml[at];
+            if (i + j >= n) ml[j].x = -INFINITY;
+            const float* src = a.part + (int64_t)at * D + lane * V;
+            if (V == 4) {
+                const float4 q = *reinterpret_cast<const float4*>(src);
+                v[j][0] = q.x; v[j][1] = q.y; v[j][V - 2] = q.z; v[j][V - 1] = q.w;
+            } else {
+                const float2 q = *reinterpret_cast<const float2*>(src);
+                v[j][0] = q.x; v[j][1] = q.y;
             }
         }
+        float mn = m;
+#pragma unroll
+        for (int j = 0; j < FLIGHT; ++j) mn = fmaxf(mn, ml[j].x);
+        if (mn == -INFINITY) continue;
+        const float f = exp2_approx(m - mn);
+        m = mn;
+        l *= f;
+#pragma unroll
+        for (int y = 0; y < V; ++y) o[y] *= f;
+#pragma unroll
+        for (int j = 0; j < FLIGHT; ++j)
+            if (ml[j].x != -INFINITY) {        // a piece without weight may hold anything
+                const float w = exp2_approx(ml[j].x - mn);
+                l = fmaf(ml[j].y, w, l);
+#pragma unroll
+                for (int y = 0; y < V; ++y) o[y] = fmaf(v[j][y], w, o[y]);
+            }
     }
     const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-    uint16_t* op = a.o + token * a.ldo + (int64_t)hq * D + lane * V;
-    if (V == 4) {
+    uint16_t* op = a.o + (int64_t)token * a.ldo + (int64_t)hq * D + lane * V;
+    if (V == 4)
         *reinterpret_cast<uint2*>(op) = make_uint2(bf162_bits(__floats2bfloat162_rn(o[0] * inv, o[1] * inv)),
                                                    bf162_bits(__floats2bfloat162_rn(o[V - 2] * inv, o[V - 1] * inv)));
-    } else {
+    else
         *reinterpret_cast<uint32_t*>(op) = bf162_bits(__floats2bfloat162_rn(o[0] * inv, o[1] * inv));
-    }
-    if (a.lse && lane == 0) a.lse[token * a.Hq + hq] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+    if (a.lse && lane == 0) a.lse[(int64_t)token * a.Hq + hq] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
 }
 
+struct JoinGrid {
+    int wide_blocks;         // wide_ctas x wide_split: a part of the 256 rows of a cut wide unit each
+    int wide_split;
+    int few_blocks;          // few_ctas x few_hw: one head of a cut few-row unit each
+    int row_blocks;          // over the tokens' rows
+};
+
 template <int D>
-__global__ void __launch_bounds__(AT_JOIN_THREADS, 3) attn_join_kernel(const AttnArgs a, int wide_blocks, int wide_split, int few_blocks, int few_split) {
+__global__ void __launch_bounds__(AT_JOIN_THREADS, 3) attn_join_kernel(const AttnArgs a, const JoinGrid grid) {
     grid_launch_dependents();
     grid_dependency_wait();
     const int warp = threadIdx.x >> 5;
     int b = blockIdx.x;
-    PieceList none;
-    none.count = none.first = none.rest = none.stride = 0;
-    if (b < wide_blocks) {
-        const CutUnit cut = a.plan.cut[1][b / wide_split];
+    PieceList p[2];
+    p[0].count = p[0].first = p[0].rest = p[0].stride = 0;
+    const bool wide = b < grid.wide_blocks;
+    if (!wide) b -= grid.wide_blocks;
+    if (wide || b < grid.few_blocks) {
+        const int split = wide ? grid.wide_split : a.few_hw;
+        const CutUnit cut = a.plan.cut[wide][b / split];
         if (cut.tiles == 0) return;
-        const int tpt = AT_WIDE_TILE / a.G, rows = 2 * AT_WIDE_TILE / wide_split, part = b % wide_split;
-        for (int i = part * rows + warp; i < (part + 1) * rows; i += AT_JOIN_WARPS) {
-            const int r = i % AT_WIDE_TILE, tok = (cut.u * 2 + i / AT_WIDE_TILE) * tpt + r / a.G;
-            if (r >= tpt * a.G || tok >= cut.n) continue;
-            join_row<D>(a, none, list_pieces(cut.begin, cut.tiles, cut.share, AT_FEW_SLOTS, 2 * AT_WIDE_TILE, i, 0), cut.t0 + tok, cut.h * a.G + r % a.G);
-        }
-        return;
-    }
-    b -= wide_blocks;
-    if (b < few_blocks) {
-        const CutUnit cut = a.plan.cut[0][b / few_split];
-        if (cut.tiles == 0) return;
-        const int stride = a.few_hw * AT_FEW_ROWS, rows = stride / few_split, part = b % few_split;
-        for (int i = part * rows + warp; i < (part + 1) * rows; i += AT_JOIN_WARPS) {
-            const int fr = cut.u * AT_FEW_ROWS + i % AT_FEW_ROWS, tok = fr / a.G;
-            if (tok >= cut.n) continue;
-            join_row<D>(a, none, list_pieces(cut.begin, cut.tiles, cut.share, 0, stride, i, 0), cut.t0 + tok,
-                        (cut.h * a.few_hw + i / AT_FEW_ROWS) * a.G + fr % a.G);
+        const int tpt = a.tpt, part = b % split, rows = wide ? 2 * AT_WIDE_TILE / split : AT_FEW_ROWS;
+#pragma unroll 1
+        for (int i = warp; i < rows; i += AT_JOIN_WARPS) {
+            const int row = part * rows + i, r = wide ? row % AT_WIDE_TILE : cut.u * AT_FEW_ROWS + i;
+            const int tok = r / a.G + (wide ? (cut.u * 2 + row / AT_WIDE_TILE) * tpt : 0);
+            if ((wide && r >= tpt * a.G) || tok >= cut.n) continue;
+            p[1] = list_pieces(cut.begin, cut.tiles, cut.share, wide ? AT_FEW_SLOTS : 0, wide ? 2 * AT_WIDE_TILE : a.few_hw * AT_FEW_ROWS, row, 0);
+            join_row<D>(a, p[0], p[1], cut.t0 + tok, (wide ? cut.h : cut.h * a.few_hw + part) * a.G + r % a.G);
         }
         return;
     }
     // rows that have a prefix and own keys: the rest of the grid strides over all rows
-    b -= few_blocks;
+    b -= grid.few_blocks;
     const int two = a.plan.share[2], nf = a.plan.share[0], nw = a.plan.share[1], rows = a.T * a.Hq;
     if (two == 0) return;
-    const int step = ((int)gridDim.x - wide_blocks - few_blocks) * AT_JOIN_WARPS;
-    for (int i = b * AT_JOIN_WARPS + warp; i < rows; i += step) {
+#pragma unroll 1
+    for (int i = b * AT_JOIN_WARPS + warp; i < rows; i += grid.row_blocks * AT_JOIN_WARPS) {
         const int t = i / a.Hq, hq = i - t * a.Hq, h = hq / a.G, g = hq - h * a.G;
         const int r = a.plan.tok_req[t];
         if (r < 0) continue;
         const Segment own = a.plan.seg[a.P + r];
-        PieceList list[2];
-#pragma unroll
+#pragma unroll 1
         for (int which = 0; which < 2; ++which) {
             const Segment sg = which ? own : a.plan.seg[own.group];
-            const int tok = t - sg.t0;
-            PieceList p = none;
+            const int tok = t - sg.t0, fr = tok * a.G + g;
+            PieceList x;
+            x.count = x.first = x.rest = x.stride = 0;
             if (tok >= 0 && tok < sg.n) {
-                if (sg.flags & SEG_WIDE) {
-                    const int tpt = AT_WIDE_TILE / a.G, u = tok / (2 * tpt), in = tok - u * 2 * tpt, second = in >= tpt;
-                    const int nt = unit_tiles<WideUnits>(a, sg, u);
-                    if (nt) p = list_pieces(unit_begin<WideUnits>(a, sg, h, u), nt, nw, AT_FEW_SLOTS, 2 * AT_WIDE_TILE,
-                                            second * AT_WIDE_TILE + (in - second * tpt) * a.G + g, dense_row(a, which, i));
-                } else {
-                    const int fr = tok * a.G + g, u = fr / AT_FEW_ROWS;
-                    const int nt = unit_tiles<FewUnits>(a, sg, u);
-                    if (nt) p = list_pieces(unit_begin<FewUnits>(a, sg, h / a.few_hw, u), nt, nf, 0, a.few_hw * AT_FEW_ROWS,
-                                            h % a.few_hw * AT_FEW_ROWS + fr % AT_FEW_ROWS, dense_row(a, which, i));
-                }
+                const bool w = sg.flags & SEG_WIDE;
+                const int tpt = a.tpt, u = w ? tok / (2 * tpt) : fr / AT_FEW_ROWS, in = tok - u * 2 * tpt;
+                const int row = w ? (in >= tpt ? AT_WIDE_TILE + (in - tpt) * a.G : in * a.G) + g : h % a.few_hw * AT_FEW_ROWS + fr % AT_FEW_ROWS;
+                const int nt = w ? unit_tiles<WideUnits>(a, sg, u) : unit_tiles<FewUnits>(a, sg, u);
+                const int begin = w ? unit_begin<WideUnits>(a, sg, h, u) : unit_begin<FewUnits>(a, sg, h / a.few_hw, u);
+                if (nt) x = list_pieces(begin, nt, w ? nw : nf, w ? AT_FEW_SLOTS : 0, w ? 2 * AT_WIDE_TILE : a.few_hw * AT_FEW_ROWS, row, dense_row(a, which, i));
             }
-            list[which] = p;
+            if (which) p[1] = x; else p[0] = x;
         }
-        join_row<D>(a, list[0], list[1], t, hq);
+        join_row<D>(a, p[0], p[1], t, hq);
     }
 }
 
