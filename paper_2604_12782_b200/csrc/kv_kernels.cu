@@ -137,17 +137,19 @@ cudaError_t launch_kv_slots(const KvSlotsArgs& a, int num_sms, cudaStream_t st) 
 // with i' = i + rot/2 (halves) or the pair (2i, 2i+1) (interleaved); channels from rot on are not turned.  Values
 // are copied.  Queries go to Q, keys and values to the token's slot of the cache.
 //
-// Every byte is read and written once, so HBM bounds it from a few hundred tokens on, and instruction issue is not
-// far behind.  A head is D/8 lanes of eight channels, a warp takes 32/(D/8) heads at a time and walks over the heads of ONE token,
-// so that the token's cosines and sines are worked out once (two angles per lane, then through shared memory
-// into registers) and serve all heads.  For rot == D in halves a lane holds four channels of each half, so that both
-// members of a pair are in one lane and the rotation needs no shuffle.  With few tokens a token's heads are
+// Every byte is read and written once, so HBM bounds it from a few hundred tokens on, if enough loads are under way and
+// instruction issue stays below.  A head is D/8 lanes of eight channels, a warp takes 32/(D/8) heads at a time (a step) and walks over the
+// heads of ONE token, so that the token's cosines and sines are worked out once (two angles per lane, then through shared memory
+// into registers) and serve all heads.  A lane's four pairs take four factors each, gamma times cosine or sine, worked out once for the query
+// heads and once for the key heads; the norm's factor, known last, multiplies the turned pair.  For rot == D in halves a
+// lane holds four channels of each half, so that both members of a pair are in one lane and the rotation needs no shuffle.  The loads of the next
+// four steps are issued before this four are worked on, the first ones before the angles.  With few tokens a token's heads are
 // shared out over several warps instead.
 // The angle is reduced in double (position * frequency passes 2^24 for far positions, where fp32 would lose the
 // turn entirely) to half turns in [-1, 1], whose sine and cosine are taken in fp32: an error of 2^-23 against a
 // rounding step of 2^-8.
-constexpr int QR_WARPS = 8;
-constexpr int QR_UNROLL = 4;    // steps whose loads are issued before the first is worked on
+constexpr int QR_WARPS = 4;
+constexpr int QR_UNROLL = 4;    // steps whose loads are issued together
 
 struct QkNormRopeArgs {
     const uint16_t* qkv;
@@ -174,85 +176,35 @@ constexpr int ROPE_INTERLEAVED = 1;  // pairs (2i, 2i+1)
 constexpr int ROPE_PARTIAL = 2;      // halves, rot < D: the partner channel comes by shuffle
 
 template <int D, int MODE>
-__global__ void __launch_bounds__(QR_WARPS * 32) qk_norm_rope_kernel(const QkNormRopeArgs a) {
+__global__ void __launch_bounds__(QR_WARPS * 32, 5) qk_norm_rope_kernel(const QkNormRopeArgs a) {
     constexpr int LPH = D / 8;       // lanes per head
     constexpr int HPS = 32 / LPH;    // heads per step of a warp
     __shared__ float2 s_cs[QR_WARPS][D / 2];
-    __shared__ float s_gamma[2][D];
     grid_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int sub = lane / LPH, hl = lane % LPH;
-    grid_dependency_wait();
-    for (int i = threadIdx.x; i < 2 * D; i += QR_WARPS * 32) {
-        const uint16_t* g = i < D ? a.gamma_q : a.gamma_k;
-        s_gamma[i / D][i % D] = g ? __uint_as_float((uint32_t)g[i % D] << 16) : 1.0f;
-    }
-    __syncthreads();
     const int64_t job = (int64_t)blockIdx.x * QR_WARPS + warp;
-    const int64_t t64 = job / a.warps_per_token;
-    if (t64 >= a.T) return;
-    const int t = (int)t64, part = (int)(job % a.warps_per_token);
+    const int t = (int)(job / a.warps_per_token), part = (int)(job - (int64_t)t * a.warps_per_token);
+    grid_dependency_wait();
+    if (t >= a.T) return;
 
-    // cosines and sines of the token
-    for (int i = lane; i < a.rot / 2; i += 32) {
-        int ax = a.axis ? a.axis[i] : 0;
-        ax = min(ax, a.axes - 1);
-        const double ang = (double)a.positions[(int64_t)ax * a.ld_pos + t] * (double)a.inv_freq[i];
-        double u = ang * 0.31830988618379067154;      // half turns
-        u -= 2.0 * rint(u * 0.5);
-        float s, c;
-        sincospif((float)u, &s, &c);
-        s_cs[warp][i] = make_float2(c * a.scale, s * a.scale);
-    }
-    __syncwarp();
-    // first channel of the lane's two groups of four, and the pair index of its channels
+    // first channel of the lane's two groups of four
     const int e0 = MODE == ROPE_SPLIT ? 4 * hl : 8 * hl;
     const int e1 = MODE == ROPE_SPLIT ? D / 2 + 4 * hl : 8 * hl + 4;
-    float c[8], s[8];
-    bool turned = true;
-    if (MODE == ROPE_SPLIT || MODE == ROPE_INTERLEAVED) {
-        turned = MODE == ROPE_SPLIT || e0 < a.rot;    // rot is a multiple of 16: a lane's eight channels turn together
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int i = 4 * hl + j;                 // both layouts: pairs 4 hl .. 4 hl + 3
-            const float2 v = turned ? s_cs[warp][i] : make_float2(1.0f, 0.0f);
-            c[j] = v.x;
-            s[j] = v.y;
-        }
-    } else {
-        turned = e0 < a.rot;
-        const bool upper = e0 >= a.rot / 2;           // rot / 2 is a multiple of 8
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int i = upper ? e0 + j - a.rot / 2 : e0 + j;
-            const float2 v = turned ? s_cs[warp][i] : make_float2(1.0f, 0.0f);
-            c[j] = v.x;
-            s[j] = upper ? v.y : -v.y;                // y = x cos + (partner) (-sin, +sin)
-        }
-    }
-    const int half_lanes = a.rot / 16;
-    const int partner = !turned ? lane : (e0 < a.rot / 2 ? lane + half_lanes : lane - half_lanes);
-
-    const int slot = a.slots ? a.slots[t] : t;
-    const int page = slot >= 0 ? slot / a.page : -1;
-    const bool cached = slot >= 0 && page < a.n_pages;
-    const int64_t cache_row = cached ? (int64_t)page * a.page_stride + (int64_t)(slot - page * a.page) * a.token_stride : 0;
-
     const int nq = (a.Hq + HPS - 1) / HPS, nk = (a.Hk + HPS - 1) / HPS;
     const int steps = nq + 2 * nk;
-    const int st0 = (int)((int64_t)steps * part / a.warps_per_token), st1 = (int)((int64_t)steps * (part + 1) / a.warps_per_token);
+    const int st0 = steps * part / a.warps_per_token, st1 = steps * (part + 1) / a.warps_per_token;
     const uint16_t* row = a.qkv + (int64_t)t * a.ld;
-    for (int b = st0; b < st1; b += QR_UNROLL) {
-        uint2 raw[QR_UNROLL][2];
+    uint2 raw[QR_UNROLL][2];
+    auto fetch = [&](int b) {
 #pragma unroll
         for (int j = 0; j < QR_UNROLL; ++j) {
-            const int i = b + j;
-            const int kind = i < nq ? 0 : i < nq + nk ? 1 : 2;
+            const int i = b + j, kind = i < nq ? 0 : i < nq + nk ? 1 : 2;
             const int h = (i - (kind == 0 ? 0 : kind == 1 ? nq : nq + nk)) * HPS + sub;
             const int hs = kind == 0 ? h : a.Hq + (kind - 1) * a.Hk + h;
             raw[j][0] = raw[j][1] = make_uint2(0u, 0u);
             if (i < st1 && h < (kind == 0 ? a.Hq : a.Hk)) {
-                const uint16_t* x = row + (int64_t)hs * D;
+                const uint16_t* x = row + hs * D;
                 if (MODE == ROPE_SPLIT) {
                     raw[j][0] = *reinterpret_cast<const uint2*>(x + e0);
                     raw[j][1] = *reinterpret_cast<const uint2*>(x + e1);
@@ -263,62 +215,151 @@ __global__ void __launch_bounds__(QR_WARPS * 32) qk_norm_rope_kernel(const QkNor
                 }
             }
         }
+    };
+    fetch(st0);
+    const int slot = a.slots ? a.slots[t] : t;
+
+    // cosines and sines of the token
+#pragma unroll 1
+    for (int i = lane; i < a.rot / 2; i += 32) {
+        const int ax = a.axis ? min((int)a.axis[i], a.axes - 1) : 0;
+        const double ang = (double)a.positions[(int64_t)ax * a.ld_pos + t] * (double)a.inv_freq[i];
+        double u = ang * 0.31830988618379067154;      // half turns
+        u -= 2.0 * rint(u * 0.5);
+        float s, c;
+        sincospif((float)u, &s, &c);
+        s_cs[warp][i] = make_float2(c * a.scale, s * a.scale);
+    }
+    __syncwarp();
+    const int page = slot >= 0 ? slot / a.page : -1;
+    const bool cached = slot >= 0 && page < a.n_pages;
+    const int64_t cache_row = cached ? (int64_t)page * a.page_stride + (int64_t)(slot - page * a.page) * a.token_stride : 0;
+    const int half_lanes = a.rot / 16;
+    const bool turned = MODE == ROPE_SPLIT || e0 < a.rot;         // rot is a multiple of 16: a lane's eight channels turn together
+    const bool upper = MODE == ROPE_PARTIAL && e0 >= a.rot / 2;   // rot / 2 is a multiple of 8
+    const int partner = !turned ? lane : upper ? lane - half_lanes : lane + half_lanes;
+
+    // Factors of the lane's channels for heads of one kind: SPLIT, INTERLEAVED: y_a = r (x_a ac - x_b bs), y_b = r (x_b bc + x_a as);
+    // PARTIAL: y = r x gamma cos + r' x' gamma' (-+ sin), with the partner lane's x' gamma' by shuffle: ac, bc hold gamma, as, bs unused.
+    uint64_t ac[2], as[2], bc[2], bs[2];
+    float cs[8], sn[8];
+    if (MODE == ROPE_PARTIAL) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float2 v = turned ? s_cs[warp][upper ? e0 + j - a.rot / 2 : e0 + j] : make_float2(1.0f, 0.0f);
+            cs[j] = v.x;
+            sn[j] = upper ? v.y : -v.y;
+        }
+    }
+    auto factors = [&](const uint16_t* gamma) {
+        float g[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) g[j] = 1.0f;
+        if (gamma) {
+            const uint2 w0 = *reinterpret_cast<const uint2*>(gamma + e0), w1 = *reinterpret_cast<const uint2*>(gamma + e1);
+            const uint32_t w[4] = {w0.x, w0.y, w1.x, w1.y};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                g[2 * j] = __uint_as_float(w[j] << 16);
+                g[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
+            }
+        }
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            if (MODE == ROPE_PARTIAL) {
+                ac[m] = pack2(g[2 * m], g[2 * m + 1]);
+                bc[m] = pack2(g[4 + 2 * m], g[5 + 2 * m]);
+                as[m] = bs[m] = 0;
+                continue;
+            }
+            const float2 v0 = turned ? s_cs[warp][4 * hl + 2 * m] : make_float2(1.0f, 0.0f);
+            const float2 v1 = turned ? s_cs[warp][4 * hl + 2 * m + 1] : make_float2(1.0f, 0.0f);
+            const float ga0 = MODE == ROPE_SPLIT ? g[2 * m] : g[4 * m], ga1 = MODE == ROPE_SPLIT ? g[2 * m + 1] : g[4 * m + 2];
+            const float gb0 = MODE == ROPE_SPLIT ? g[4 + 2 * m] : g[4 * m + 1], gb1 = MODE == ROPE_SPLIT ? g[5 + 2 * m] : g[4 * m + 3];
+            ac[m] = pack2(ga0 * v0.x, ga1 * v1.x);
+            as[m] = pack2(ga0 * v0.y, ga1 * v1.y);
+            bc[m] = pack2(gb0 * v0.x, gb1 * v1.x);
+            bs[m] = pack2(-gb0 * v0.y, -gb1 * v1.y);
+        }
+    };
+    int have = -1;                   // kind of head that the factors are for
+#pragma unroll 1
+    for (int b = st0; b < st1; b += QR_UNROLL) {
+        uint2 now[QR_UNROLL][2];
+#pragma unroll
+        for (int j = 0; j < QR_UNROLL; ++j) {
+            now[j][0] = raw[j][0];
+            now[j][1] = raw[j][1];
+        }
+        if (b + QR_UNROLL < st1) fetch(b + QR_UNROLL);
 #pragma unroll
         for (int j = 0; j < QR_UNROLL; ++j) {
             const int i = b + j;
             if (i >= st1) break;
             const int kind = i < nq ? 0 : i < nq + nk ? 1 : 2;
             const int h = (i - (kind == 0 ? 0 : kind == 1 ? nq : nq + nk)) * HPS + sub;
-            uint32_t w[4] = {raw[j][0].x, raw[j][0].y, raw[j][1].x, raw[j][1].y};
+            uint32_t w[4] = {now[j][0].x, now[j][0].y, now[j][1].x, now[j][1].y};
             if (kind < 2) {
-                float x[8];
-#pragma unroll
-                for (int m = 0; m < 4; ++m) {
-                    x[2 * m] = __uint_as_float(w[m] << 16);
-                    x[2 * m + 1] = __uint_as_float(w[m] & 0xFFFF0000u);
+                const uint16_t* gamma = kind == 0 ? a.gamma_q : a.gamma_k;
+                if (kind != have) {
+                    factors(gamma);
+                    have = kind;
                 }
-                if ((kind == 0 ? a.gamma_q : a.gamma_k) != nullptr) {
-                    float ss = 0.0f, ss2 = 0.0f;
+                uint64_t x[4];           // SPLIT: (a0 a1) (a2 a3) (b0 b1) (b2 b3); INTERLEAVED, PARTIAL: channels in order
 #pragma unroll
-                    for (int m = 0; m < 4; ++m) {
-                        ss = fmaf(x[m], x[m], ss);
-                        ss2 = fmaf(x[m + 4], x[m + 4], ss2);
-                    }
-                    ss += ss2;
+                for (int m = 0; m < 4; ++m) x[m] = pack2(__uint_as_float(w[m] << 16), __uint_as_float(w[m] & 0xFFFF0000u));
+                float r = 1.0f;
+                if (gamma) {
+                    float s0, s1;
+                    unpack2(add2(fma2(x[0], x[0], mul2(x[1], x[1])), fma2(x[2], x[2], mul2(x[3], x[3]))), s0, s1);
+                    float ss = s0 + s1;
 #pragma unroll
                     for (int o = LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xFFFFFFFFu, ss, o);
-                    const float r = rsqrtf(ss * (1.0f / D) + a.eps);
-                    const float4 g0 = *reinterpret_cast<const float4*>(&s_gamma[kind][e0]);
-                    const float4 g1 = *reinterpret_cast<const float4*>(&s_gamma[kind][e1]);
-                    x[0] *= r * g0.x; x[1] *= r * g0.y; x[2] *= r * g0.z; x[3] *= r * g0.w;
-                    x[4] *= r * g1.x; x[5] *= r * g1.y; x[6] *= r * g1.z; x[7] *= r * g1.w;
+                    r = rsqrtf(ss * (1.0f / D) + a.eps);
                 }
-                float y[8];
-                if (MODE == ROPE_SPLIT) {
-#pragma unroll
-                    for (int m = 0; m < 4; ++m) {
-                        y[m] = x[m] * c[m] - x[m + 4] * s[m];
-                        y[m + 4] = x[m + 4] * c[m] + x[m] * s[m];
-                    }
-                } else if (MODE == ROPE_INTERLEAVED) {
-#pragma unroll
-                    for (int m = 0; m < 4; ++m) {
-                        y[2 * m] = x[2 * m] * c[m] - x[2 * m + 1] * s[m];
-                        y[2 * m + 1] = x[2 * m + 1] * c[m] + x[2 * m] * s[m];
-                    }
-                } else {
+                const uint64_t r2 = pack2(r, r);
+                if (MODE == ROPE_PARTIAL) {
+                    float v[8];
+                    unpack2(mul2(x[0], mul2(ac[0], r2)), v[0], v[1]);
+                    unpack2(mul2(x[1], mul2(ac[1], r2)), v[2], v[3]);
+                    unpack2(mul2(x[2], mul2(bc[0], r2)), v[4], v[5]);
+                    unpack2(mul2(x[3], mul2(bc[1], r2)), v[6], v[7]);
+                    float y[8];
 #pragma unroll
                     for (int m = 0; m < 8; ++m) {
-                        const float o = __shfl_sync(0xFFFFFFFFu, x[m], partner);
-                        y[m] = turned ? x[m] * c[m] + o * s[m] : x[m];
+                        const float o = __shfl_sync(0xFFFFFFFFu, v[m], partner);
+                        y[m] = turned ? v[m] * cs[m] + o * sn[m] : v[m];
                     }
-                }
 #pragma unroll
-                for (int m = 0; m < 4; ++m) w[m] = bf162_bits(__floats2bfloat162_rn(y[2 * m], y[2 * m + 1]));
+                    for (int m = 0; m < 4; ++m) w[m] = bf162_bits(__floats2bfloat162_rn(y[2 * m], y[2 * m + 1]));
+                } else {
+                    uint64_t xa[2] = {x[0], x[1]}, xb[2] = {x[2], x[3]};
+                    if (MODE == ROPE_INTERLEAVED) {
+#pragma unroll
+                        for (int m = 0; m < 2; ++m) {
+                            float p, q, u, z;
+                            unpack2(x[2 * m], p, q);
+                            unpack2(x[2 * m + 1], u, z);
+                            xa[m] = pack2(p, u);
+                            xb[m] = pack2(q, z);
+                        }
+                    }
+                    float ya[4], yb[4];
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) {
+                        unpack2(mul2(r2, fma2(xa[m], ac[m], mul2(xb[m], bs[m]))), ya[2 * m], ya[2 * m + 1]);
+                        unpack2(mul2(r2, fma2(xb[m], bc[m], mul2(xa[m], as[m]))), yb[2 * m], yb[2 * m + 1]);
+                    }
+#pragma unroll
+                    for (int m = 0; m < 4; ++m)
+                        w[m] = MODE == ROPE_SPLIT ? bf162_bits(m < 2 ? __floats2bfloat162_rn(ya[2 * m], ya[2 * m + 1])
+                                                                     : __floats2bfloat162_rn(yb[2 * m - 4], yb[2 * m - 3]))
+                                                  : bf162_bits(__floats2bfloat162_rn(ya[m], yb[m]));
+                }
             }
             uint16_t* dst = nullptr;
             if (kind == 0) {
-                if (h < a.Hq) dst = a.q + (int64_t)t * a.ldq + (int64_t)h * D;
+                if (h < a.Hq) dst = a.q + (int64_t)t * a.ldq + h * D;
             } else if (cached && h < a.Hk) {
                 dst = (kind == 1 ? a.k : a.v) + cache_row + (int64_t)h * a.head_stride;
             }
@@ -345,8 +386,8 @@ static cudaError_t launch_qk_norm_rope_d(const QkNormRopeArgs& a, int mode, dim3
 cudaError_t launch_qk_norm_rope(QkNormRopeArgs a, int D, bool interleaved, int num_sms, cudaStream_t st) {
     const int hps = 32 / (D / 8);
     const int steps = (a.Hq + hps - 1) / hps + 2 * ((a.Hk + hps - 1) / hps);
-    // one warp per token once that gives every SM its 32 warps; below it, a token's steps are spread over more warps
-    int wpt = (int)(((int64_t)num_sms * 32 + a.T - 1) / a.T);
+    // a warp per token once that fills the machine's 20 warps an SM; below it, a token's steps are spread over as many as fit
+    const int wpt = (int)((int64_t)num_sms * QR_WARPS * 5 / a.T);
     a.warps_per_token = max(1, min(wpt, steps));
     const int64_t jobs = (int64_t)a.T * a.warps_per_token;
     const dim3 grid((unsigned)((jobs + QR_WARPS - 1) / QR_WARPS));
