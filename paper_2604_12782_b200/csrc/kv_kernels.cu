@@ -1,6 +1,8 @@
 // Kernels around a paged key/value cache, between the QKV projection and the attention:
 //   kv_slots_kernel     pages for the new tokens of every request, slots and positions of the tokens
 //   qk_norm_rope_kernel RMSNorm of the query and key heads, rotation by position, keys and values into the cache
+#include <algorithm>
+
 #include "common.cuh"
 
 namespace osc {
@@ -142,13 +144,18 @@ cudaError_t launch_kv_slots(const KvSlotsArgs& a, int num_sms, cudaStream_t st) 
 // heads of ONE token, so that the token's cosines and sines are worked out once (two angles per lane, then through shared memory
 // into registers) and serve all heads.  A lane's four pairs take four factors each, gamma times cosine or sine, worked out once for the query
 // heads and once for the key heads; the norm's factor, known last, multiplies the turned pair.  For rot == D in halves a
-// lane holds four channels of each half, so that both members of a pair are in one lane and the rotation needs no shuffle.  The loads of the next
-// four steps are issued before this four are worked on, the first ones before the angles.  With few tokens a token's heads are
-// shared out over several warps instead.
+// lane holds four channels of each half, so that both members of a pair are in one lane and the rotation needs no shuffle.  The loads of
+// four steps are issued together; pointers advance by constants, and the three kinds of heads have loops of their own (with one loop that
+// worked out kind, head and addresses for every step it took 150 instructions a step, and 8192 tokens were bound by their issue:
+// 44 us, issue slots 64 % used).  With few tokens a token's heads are shared out over several warps instead.
+// (Batches of eight, or the whole token on its way into shared memory by one bulk copy with eight warps an SM, were
+// slower: 42 and 57 us for 8192 tokens, because the chains of a step want many warps.  Calling a warp's whole part into L2 first changed
+// nothing: HBM, reading and writing, is 85 % busy.)
 // The angle is reduced in double (position * frequency passes 2^24 for far positions, where fp32 would lose the
 // turn entirely) to half turns in [-1, 1], whose sine and cosine are taken in fp32: an error of 2^-23 against a
 // rounding step of 2^-8.
 constexpr int QR_WARPS = 4;
+constexpr int QR_CTAS = 8;      // per SM
 constexpr int QR_UNROLL = 4;    // steps whose loads are issued together
 
 struct QkNormRopeArgs {
@@ -176,54 +183,40 @@ constexpr int ROPE_INTERLEAVED = 1;  // pairs (2i, 2i+1)
 constexpr int ROPE_PARTIAL = 2;      // halves, rot < D: the partner channel comes by shuffle
 
 template <int D, int MODE>
-__global__ void __launch_bounds__(QR_WARPS * 32, 5) qk_norm_rope_kernel(const QkNormRopeArgs a) {
+__global__ void __launch_bounds__(QR_WARPS * 32, MODE == ROPE_SPLIT ? QR_CTAS : QR_CTAS - 2) qk_norm_rope_kernel(const QkNormRopeArgs a) {
     constexpr int LPH = D / 8;       // lanes per head
     constexpr int HPS = 32 / LPH;    // heads per step of a warp
     __shared__ float2 s_cs[QR_WARPS][D / 2];
     grid_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int sub = lane / LPH, hl = lane % LPH;
-    const int64_t job = (int64_t)blockIdx.x * QR_WARPS + warp;
-    const int t = (int)(job / a.warps_per_token), part = (int)(job - (int64_t)t * a.warps_per_token);
+    const int nq = (a.Hq + HPS - 1) / HPS, nk = (a.Hk + HPS - 1) / HPS;
+    const int steps = nq + 2 * nk;
+    const uint32_t job = blockIdx.x * QR_WARPS + warp;      // the host has seen to T * warps_per_token < 2^31
+    const int t = (int)(job / (uint32_t)a.warps_per_token), part = (int)(job - (uint32_t)t * a.warps_per_token);
     grid_dependency_wait();
     if (t >= a.T) return;
-
+    const int st0 = steps * part / a.warps_per_token, st1 = steps * (part + 1) / a.warps_per_token;
+    const uint16_t* row = a.qkv + (int64_t)t * a.ld;
     // first channel of the lane's two groups of four
     const int e0 = MODE == ROPE_SPLIT ? 4 * hl : 8 * hl;
     const int e1 = MODE == ROPE_SPLIT ? D / 2 + 4 * hl : 8 * hl + 4;
-    const int nq = (a.Hq + HPS - 1) / HPS, nk = (a.Hk + HPS - 1) / HPS;
-    const int steps = nq + 2 * nk;
-    const int st0 = steps * part / a.warps_per_token, st1 = steps * (part + 1) / a.warps_per_token;
-    const uint16_t* row = a.qkv + (int64_t)t * a.ld;
-    uint2 raw[QR_UNROLL][2];
-    auto fetch = [&](int b) {
-#pragma unroll
-        for (int j = 0; j < QR_UNROLL; ++j) {
-            const int i = b + j, kind = i < nq ? 0 : i < nq + nk ? 1 : 2;
-            const int h = (i - (kind == 0 ? 0 : kind == 1 ? nq : nq + nk)) * HPS + sub;
-            const int hs = kind == 0 ? h : a.Hq + (kind - 1) * a.Hk + h;
-            raw[j][0] = raw[j][1] = make_uint2(0u, 0u);
-            if (i < st1 && h < (kind == 0 ? a.Hq : a.Hk)) {
-                const uint16_t* x = row + hs * D;
-                if (MODE == ROPE_SPLIT) {
-                    raw[j][0] = *reinterpret_cast<const uint2*>(x + e0);
-                    raw[j][1] = *reinterpret_cast<const uint2*>(x + e1);
-                } else {
-                    const uint4 v = *reinterpret_cast<const uint4*>(x + e0);
-                    raw[j][0] = make_uint2(v.x, v.y);
-                    raw[j][1] = make_uint2(v.z, v.w);
-                }
-            }
-        }
-    };
-    fetch(st0);
+    const int half_lanes = a.rot / 16;
+    const bool turned = MODE == ROPE_SPLIT || e0 < a.rot;         // rot is a multiple of 16: a lane's eight channels turn together
+    const bool upper = MODE == ROPE_PARTIAL && e0 >= a.rot / 2;   // rot / 2 is a multiple of 8
+    const int partner = !turned ? lane : upper ? lane - half_lanes : lane + half_lanes;
     const int slot = a.slots ? a.slots[t] : t;
 
-    // cosines and sines of the token
-#pragma unroll 1
-    for (int i = lane; i < a.rot / 2; i += 32) {
+    // cosines and sines of the token; all its positions are fetched beside the pairs' axes
+    int pos[3];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) pos[i] = i < a.axes ? a.positions[(int64_t)i * a.ld_pos + t] : 0;
+#pragma unroll
+    for (int k = 0; k < D / 64; ++k) {
+        const int i = k * 32 + lane;
+        if (i >= a.rot / 2) break;
         const int ax = a.axis ? min((int)a.axis[i], a.axes - 1) : 0;
-        const double ang = (double)a.positions[(int64_t)ax * a.ld_pos + t] * (double)a.inv_freq[i];
+        const double ang = (double)(ax == 0 ? pos[0] : ax == 1 ? pos[1] : pos[2]) * (double)a.inv_freq[i];
         double u = ang * 0.31830988618379067154;      // half turns
         u -= 2.0 * rint(u * 0.5);
         float s, c;
@@ -234,10 +227,6 @@ __global__ void __launch_bounds__(QR_WARPS * 32, 5) qk_norm_rope_kernel(const Qk
     const int page = slot >= 0 ? slot / a.page : -1;
     const bool cached = slot >= 0 && page < a.n_pages;
     const int64_t cache_row = cached ? (int64_t)page * a.page_stride + (int64_t)(slot - page * a.page) * a.token_stride : 0;
-    const int half_lanes = a.rot / 16;
-    const bool turned = MODE == ROPE_SPLIT || e0 < a.rot;         // rot is a multiple of 16: a lane's eight channels turn together
-    const bool upper = MODE == ROPE_PARTIAL && e0 >= a.rot / 2;   // rot / 2 is a multiple of 8
-    const int partner = !turned ? lane : upper ? lane - half_lanes : lane + half_lanes;
 
     // Factors of the lane's channels for heads of one kind: SPLIT, INTERLEAVED: y_a = r (x_a ac - x_b bs), y_b = r (x_b bc + x_a as);
     // PARTIAL: y = r x gamma cos + r' x' gamma' (-+ sin), with the partner lane's x' gamma' by shuffle: ac, bc hold gamma, as, bs unused.
@@ -282,117 +271,131 @@ __global__ void __launch_bounds__(QR_WARPS * 32, 5) qk_norm_rope_kernel(const Qk
             bs[m] = pack2(-gb0 * v0.y, -gb1 * v1.y);
         }
     };
-    int have = -1;                   // kind of head that the factors are for
 #pragma unroll 1
-    for (int b = st0; b < st1; b += QR_UNROLL) {
-        uint2 now[QR_UNROLL][2];
+    for (int kind = 0; kind < 3; ++kind) {
+        // steps of this kind that are the warp's, and how many of them are heads for this lane
+        const int H = kind ? a.Hk : a.Hq, first = kind == 0 ? 0 : kind == 1 ? nq : nq + nk;
+        const int i0 = max(st0 - first, 0), n = min(st1 - first, kind ? nk : nq) - i0;
+        if (n <= 0) continue;
+        const int h0 = i0 * HPS + sub, mine = min(n, (H - h0 + HPS - 1) / HPS);
+        const uint16_t* src = row + ((kind == 0 ? 0 : kind == 1 ? a.Hq : a.Hq + a.Hk) + h0) * D;
+        uint16_t* dst = kind == 0 ? a.q + (int64_t)t * a.ldq + h0 * D : (kind == 1 ? a.k : a.v) + cache_row + (int64_t)h0 * a.head_stride;
+        const int64_t dst_step = kind == 0 ? HPS * D : HPS * a.head_stride;
+        const int writes = kind == 0 || cached ? mine : 0;
+        const uint16_t* gamma = kind == 0 ? a.gamma_q : a.gamma_k;
+        if (kind < 2) factors(gamma);
+#pragma unroll 1
+        for (int b = 0; b < n; b += QR_UNROLL) {
+            uint32_t w[QR_UNROLL][4];
 #pragma unroll
-        for (int j = 0; j < QR_UNROLL; ++j) {
-            now[j][0] = raw[j][0];
-            now[j][1] = raw[j][1];
-        }
-        if (b + QR_UNROLL < st1) fetch(b + QR_UNROLL);
-#pragma unroll
-        for (int j = 0; j < QR_UNROLL; ++j) {
-            const int i = b + j;
-            if (i >= st1) break;
-            const int kind = i < nq ? 0 : i < nq + nk ? 1 : 2;
-            const int h = (i - (kind == 0 ? 0 : kind == 1 ? nq : nq + nk)) * HPS + sub;
-            uint32_t w[4] = {now[j][0].x, now[j][0].y, now[j][1].x, now[j][1].y};
-            if (kind < 2) {
-                const uint16_t* gamma = kind == 0 ? a.gamma_q : a.gamma_k;
-                if (kind != have) {
-                    factors(gamma);
-                    have = kind;
-                }
-                uint64_t x[4];           // SPLIT: (a0 a1) (a2 a3) (b0 b1) (b2 b3); INTERLEAVED, PARTIAL: channels in order
-#pragma unroll
-                for (int m = 0; m < 4; ++m) x[m] = pack2(__uint_as_float(w[m] << 16), __uint_as_float(w[m] & 0xFFFF0000u));
-                float r = 1.0f;
-                if (gamma) {
-                    float s0, s1;
-                    unpack2(add2(fma2(x[0], x[0], mul2(x[1], x[1])), fma2(x[2], x[2], mul2(x[3], x[3]))), s0, s1);
-                    float ss = s0 + s1;
-#pragma unroll
-                    for (int o = LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xFFFFFFFFu, ss, o);
-                    r = rsqrtf(ss * (1.0f / D) + a.eps);
-                }
-                const uint64_t r2 = pack2(r, r);
-                if (MODE == ROPE_PARTIAL) {
-                    float v[8];
-                    unpack2(mul2(x[0], mul2(ac[0], r2)), v[0], v[1]);
-                    unpack2(mul2(x[1], mul2(ac[1], r2)), v[2], v[3]);
-                    unpack2(mul2(x[2], mul2(bc[0], r2)), v[4], v[5]);
-                    unpack2(mul2(x[3], mul2(bc[1], r2)), v[6], v[7]);
-                    float y[8];
-#pragma unroll
-                    for (int m = 0; m < 8; ++m) {
-                        const float o = __shfl_sync(0xFFFFFFFFu, v[m], partner);
-                        y[m] = turned ? v[m] * cs[m] + o * sn[m] : v[m];
+            for (int j = 0; j < QR_UNROLL; ++j) {
+                w[j][0] = w[j][1] = w[j][2] = w[j][3] = 0u;
+                if (b + j < mine) {
+                    if (MODE == ROPE_SPLIT) {
+                        const uint2 x0 = *reinterpret_cast<const uint2*>(src + j * HPS * D + e0), x1 = *reinterpret_cast<const uint2*>(src + j * HPS * D + e1);
+                        w[j][0] = x0.x; w[j][1] = x0.y; w[j][2] = x1.x; w[j][3] = x1.y;
+                    } else {
+                        const uint4 x0 = *reinterpret_cast<const uint4*>(src + j * HPS * D + e0);
+                        w[j][0] = x0.x; w[j][1] = x0.y; w[j][2] = x0.z; w[j][3] = x0.w;
                     }
+                }
+            }
+            src += QR_UNROLL * HPS * D;
+            // Four independent chains (sum of squares, shuffles, rsqrt, rotation) side by side: no branch between them, so the last batch
+            // may turn heads that are not there.
+            if (kind < 2) {
 #pragma unroll
-                    for (int m = 0; m < 4; ++m) w[m] = bf162_bits(__floats2bfloat162_rn(y[2 * m], y[2 * m + 1]));
-                } else {
-                    uint64_t xa[2] = {x[0], x[1]}, xb[2] = {x[2], x[3]};
-                    if (MODE == ROPE_INTERLEAVED) {
+                for (int j = 0; j < QR_UNROLL; ++j) {
+                    uint64_t x[4];           // SPLIT: (a0 a1) (a2 a3) (b0 b1) (b2 b3); INTERLEAVED, PARTIAL: channels in order
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) x[m] = pack2(__uint_as_float(w[j][m] << 16), __uint_as_float(w[j][m] & 0xFFFF0000u));
+                    float r = 1.0f;
+                    if (gamma) {
+                        float s0, s1;
+                        unpack2(add2(fma2(x[0], x[0], mul2(x[1], x[1])), fma2(x[2], x[2], mul2(x[3], x[3]))), s0, s1);
+                        float ss = s0 + s1;
+#pragma unroll
+                        for (int o = LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xFFFFFFFFu, ss, o);
+                        r = rsqrtf(ss * (1.0f / D) + a.eps);
+                    }
+                    const uint64_t r2 = pack2(r, r);
+                    if (MODE == ROPE_PARTIAL) {
+                        float v[8], y[8];
+                        unpack2(mul2(x[0], mul2(ac[0], r2)), v[0], v[1]);
+                        unpack2(mul2(x[1], mul2(ac[1], r2)), v[2], v[3]);
+                        unpack2(mul2(x[2], mul2(bc[0], r2)), v[4], v[5]);
+                        unpack2(mul2(x[3], mul2(bc[1], r2)), v[6], v[7]);
+#pragma unroll
+                        for (int m = 0; m < 8; ++m) {
+                            const float o = __shfl_sync(0xFFFFFFFFu, v[m], partner);
+                            y[m] = turned ? v[m] * cs[m] + o * sn[m] : v[m];
+                        }
+#pragma unroll
+                        for (int m = 0; m < 4; ++m) w[j][m] = bf162_bits(__floats2bfloat162_rn(y[2 * m], y[2 * m + 1]));
+                    } else {
+                        uint64_t xa[2] = {x[0], x[1]}, xb[2] = {x[2], x[3]};
+                        if (MODE == ROPE_INTERLEAVED) {
+#pragma unroll
+                            for (int m = 0; m < 2; ++m) {
+                                float p, q, u, z;
+                                unpack2(x[2 * m], p, q);
+                                unpack2(x[2 * m + 1], u, z);
+                                xa[m] = pack2(p, u);
+                                xb[m] = pack2(q, z);
+                            }
+                        }
+                        float ya[4], yb[4];
 #pragma unroll
                         for (int m = 0; m < 2; ++m) {
-                            float p, q, u, z;
-                            unpack2(x[2 * m], p, q);
-                            unpack2(x[2 * m + 1], u, z);
-                            xa[m] = pack2(p, u);
-                            xb[m] = pack2(q, z);
+                            unpack2(mul2(r2, fma2(xa[m], ac[m], mul2(xb[m], bs[m]))), ya[2 * m], ya[2 * m + 1]);
+                            unpack2(mul2(r2, fma2(xb[m], bc[m], mul2(xa[m], as[m]))), yb[2 * m], yb[2 * m + 1]);
                         }
-                    }
-                    float ya[4], yb[4];
 #pragma unroll
-                    for (int m = 0; m < 2; ++m) {
-                        unpack2(mul2(r2, fma2(xa[m], ac[m], mul2(xb[m], bs[m]))), ya[2 * m], ya[2 * m + 1]);
-                        unpack2(mul2(r2, fma2(xb[m], bc[m], mul2(xa[m], as[m]))), yb[2 * m], yb[2 * m + 1]);
+                        for (int m = 0; m < 4; ++m)
+                            w[j][m] = MODE == ROPE_SPLIT ? bf162_bits(m < 2 ? __floats2bfloat162_rn(ya[2 * m], ya[2 * m + 1])
+                                                                            : __floats2bfloat162_rn(yb[2 * m - 4], yb[2 * m - 3]))
+                                                         : bf162_bits(__floats2bfloat162_rn(ya[m], yb[m]));
                     }
-#pragma unroll
-                    for (int m = 0; m < 4; ++m)
-                        w[m] = MODE == ROPE_SPLIT ? bf162_bits(m < 2 ? __floats2bfloat162_rn(ya[2 * m], ya[2 * m + 1])
-                                                                     : __floats2bfloat162_rn(yb[2 * m - 4], yb[2 * m - 3]))
-                                                  : bf162_bits(__floats2bfloat162_rn(ya[m], yb[m]));
                 }
             }
-            uint16_t* dst = nullptr;
-            if (kind == 0) {
-                if (h < a.Hq) dst = a.q + (int64_t)t * a.ldq + h * D;
-            } else if (cached && h < a.Hk) {
-                dst = (kind == 1 ? a.k : a.v) + cache_row + (int64_t)h * a.head_stride;
-            }
-            if (dst) {
-                if (MODE == ROPE_SPLIT) {
-                    *reinterpret_cast<uint2*>(dst + e0) = make_uint2(w[0], w[1]);
-                    *reinterpret_cast<uint2*>(dst + e1) = make_uint2(w[2], w[3]);
-                } else {
-                    *reinterpret_cast<uint4*>(dst + e0) = make_uint4(w[0], w[1], w[2], w[3]);
+#pragma unroll
+            for (int j = 0; j < QR_UNROLL; ++j) {
+                if (b + j < writes) {
+                    if (MODE == ROPE_SPLIT) {
+                        *reinterpret_cast<uint2*>(dst + e0) = make_uint2(w[j][0], w[j][1]);
+                        *reinterpret_cast<uint2*>(dst + e1) = make_uint2(w[j][2], w[j][3]);
+                    } else {
+                        *reinterpret_cast<uint4*>(dst + e0) = make_uint4(w[j][0], w[j][1], w[j][2], w[j][3]);
+                    }
                 }
+                dst += dst_step;
             }
         }
     }
 }
 
-template <int D>
-static cudaError_t launch_qk_norm_rope_d(const QkNormRopeArgs& a, int mode, dim3 grid, cudaStream_t st) {
-    const dim3 block(QR_WARPS * 32);
-    if (mode == ROPE_SPLIT) return launch_pdl(qk_norm_rope_kernel<D, ROPE_SPLIT>, grid, block, 0, st, a);
-    if (mode == ROPE_INTERLEAVED) return launch_pdl(qk_norm_rope_kernel<D, ROPE_INTERLEAVED>, grid, block, 0, st, a);
-    return launch_pdl(qk_norm_rope_kernel<D, ROPE_PARTIAL>, grid, block, 0, st, a);
-}
-
-cudaError_t launch_qk_norm_rope(QkNormRopeArgs a, int D, bool interleaved, int num_sms, cudaStream_t st) {
+template <int D, int MODE>
+static cudaError_t launch_qk_norm_rope_mode(QkNormRopeArgs a, int num_sms, cudaStream_t st) {
     const int hps = 32 / (D / 8);
     const int steps = (a.Hq + hps - 1) / hps + 2 * ((a.Hk + hps - 1) / hps);
-    // a warp per token once that fills the machine's 20 warps an SM; below it, a token's steps are spread over as many as fit
-    const int wpt = (int)((int64_t)num_sms * QR_WARPS * 5 / a.T);
-    a.warps_per_token = max(1, min(wpt, steps));
+    // A warp per token once that fills half of the machine's resident warps; below it, a token's steps are spread over as many as fit.
+    // More is worse, every warp works out the angles again: 8192 tokens in 1 / 2 / 4 / 8 warps each 39.4 / 37.0 / 46.4 / 66.5 us,
+    // 5001 tokens 27.8 / 29.9 / 35.8 / 46.8, 256 tokens 10.4 / 6.3 / 6.3 / 6.3.
+    const int64_t resident = (int64_t)num_sms * QR_WARPS * QR_CTAS;
+    a.warps_per_token = (int)std::max<int64_t>(1, std::min<int64_t>(resident / 2 / a.T, std::min(steps, 32)));
     const int64_t jobs = (int64_t)a.T * a.warps_per_token;
-    const dim3 grid((unsigned)((jobs + QR_WARPS - 1) / QR_WARPS));
-    const int mode = interleaved ? ROPE_INTERLEAVED : a.rot == D ? ROPE_SPLIT : ROPE_PARTIAL;
-    return D == 128 ? launch_qk_norm_rope_d<128>(a, mode, grid, st) : launch_qk_norm_rope_d<64>(a, mode, grid, st);
+    return launch_pdl(qk_norm_rope_kernel<D, MODE>, dim3((unsigned)((jobs + QR_WARPS - 1) / QR_WARPS)), dim3(QR_WARPS * 32), 0, st, a);
+}
+
+template <int D>
+static cudaError_t launch_qk_norm_rope_d(const QkNormRopeArgs& a, bool interleaved, int num_sms, cudaStream_t st) {
+    if (interleaved) return launch_qk_norm_rope_mode<D, ROPE_INTERLEAVED>(a, num_sms, st);
+    if (a.rot == D) return launch_qk_norm_rope_mode<D, ROPE_SPLIT>(a, num_sms, st);
+    return launch_qk_norm_rope_mode<D, ROPE_PARTIAL>(a, num_sms, st);
+}
+
+cudaError_t launch_qk_norm_rope(const QkNormRopeArgs& a, int D, bool interleaved, int num_sms, cudaStream_t st) {
+    return D == 128 ? launch_qk_norm_rope_d<128>(a, interleaved, num_sms, st) : launch_qk_norm_rope_d<64>(a, interleaved, num_sms, st);
 }
 
 }  // namespace osc
