@@ -815,18 +815,47 @@ def osc_rmsnorm_linear_swiglu_grouped_gather(w: OscWeights, Hin: torch.Tensor, g
 
 # ------------------------------- between the QKV projection and o_proj: a paged key/value cache
 
-def _want(name, t, dtype, ndim=None):
-    """The calls below read lengths and tables on the device, where a wrong type would go unnoticed: checked here."""
-    if t is None:
-        return
-    if t.dtype != dtype or (ndim is not None and t.dim() != ndim):
-        raise ValueError(f"{name}: {ndim if ndim is not None else 'any'}-d {dtype} expected, got {t.dim()}-d {t.dtype}")
-    if not t.is_cuda:
-        raise ValueError(f"{name}: cuda tensor expected")
-    if _raw_device is not None and t.device.index != _raw_device():
-        raise ValueError(f"{name}: lies on {t.device}, the current device is cuda:{_raw_device()}")
-    if t.dim() and t.numel() and t.stride(-1) != 1 and t.shape[-1] != 1:
-        raise ValueError(f"{name}: the last dimension must be contiguous")
+# Lengths, tables and slots are read on the device, where a tensor of another type or on another device would go unnoticed, so the calls
+# below look at every tensor.  They run once per step or layer in front of kernels of a few microseconds: the look is one pass with three
+# attribute reads a tensor, and only a refusal works out what was wrong.
+def _device_of(t):
+    """Device of a call: that of its first tensor, which has to be the current one; -1 otherwise."""
+    d = t.get_device()
+    return d if d >= 0 and d == (_raw_device() if _raw_device is not None else torch.cuda.current_device()) else -1
+
+
+def _refuse(dtype, ndim, dev, **tensors):
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        if t.dtype != dtype or (ndim and t.dim() != ndim):
+            raise ValueError(f"{name}: {ndim if ndim else 'any'}-d {dtype} expected, got {t.dim()}-d {t.dtype}")
+        if not t.is_cuda:
+            raise ValueError(f"{name}: cuda tensor expected")
+        if dev < 0 or t.get_device() != dev:
+            raise ValueError(f"{name}: lies on {t.device}, not on the current device")
+        if t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1:
+            raise ValueError(f"{name}: the last dimension must be contiguous")
+
+
+def _bad(dtype, dev, *tensors):
+    """Whether a call must not take one of these (one-dimensional or wholly contiguous) tensors."""
+    for t in tensors:
+        if t is not None and (t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous()):
+            return True
+    return dev < 0
+
+
+def _bad_rows(dtype, dev, *tensors):
+    """The same for matrices whose rows may be further apart than they are long."""
+    for t in tensors:
+        if t is not None and (t.dtype is not dtype or t.get_device() != dev or t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1)):
+            return True
+    return dev < 0
+
+
+def _addr(t):
+    return t.data_ptr() if t is not None else None
 
 
 class KvCache:
@@ -834,11 +863,10 @@ class KvCache:
     channels contiguous (a permuted [n_pages, n_heads, page_size, head_dim] buffer too), the same for k and v."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor):
-        _want("k", k, torch.bfloat16, 4)
-        _want("v", v, torch.bfloat16, 4)
+        _refuse(torch.bfloat16, 4, k.get_device(), k=k, v=v)
         if k.shape != v.shape or any(a != b for n, a, b in zip(k.shape, k.stride(), v.stride()) if n > 1):
             raise ValueError("k and v must have the same shape and strides")
-        self.k, self.v = k, v
+        self.k, self.v, self.device = k, v, k.get_device()
         n_pages, page_size, n_heads, head_dim = k.shape
         st = [s if n > 1 else 8 * ((head_dim + 7) // 8) for n, s in zip(k.shape[:3], k.stride()[:3])]
         self.n_pages, self.page_size, self.n_heads, self.head_dim = n_pages, page_size, n_heads, head_dim
@@ -850,50 +878,57 @@ class Rope:
     axes turns a pair) or None."""
 
     def __init__(self, inv_freq: torch.Tensor, axis: torch.Tensor = None, interleaved: bool = False, scale: float = 1.0):
-        _want("inv_freq", inv_freq, torch.float32, 1)
-        _want("axis", axis, torch.uint8, 1)
+        _refuse(torch.float32, 1, inv_freq.get_device(), inv_freq=inv_freq)
+        _refuse(torch.uint8, 1, inv_freq.get_device(), axis=axis)
         if axis is not None and axis.shape != inv_freq.shape:
             raise ValueError("axis and inv_freq must have the same length")
-        self.inv_freq, self.axis, self.interleaved, self.scale = inv_freq, axis, interleaved, scale
+        self.inv_freq, self.axis, self.interleaved, self.scale, self.device = inv_freq, axis, interleaved, scale, inv_freq.get_device()
         self.c = {n: RopeStruct(_ptr(inv_freq), _ptr(axis), 2 * inv_freq.shape[0], n, int(interleaved), scale) for n in (1, 2, 3)}
 
 
 def osc_kv_slots(cached, fresh, base, page_size: int, free_pages, table, row_off, kv_len, slots, positions, taken, stream=None):
     """Pages, slots and positions of a step's new tokens from the requests' lengths (all int32; table [R, cols] is
     updated in place, row_off [R + 1], kv_len [R], slots [T], positions [T] and taken [1] are written)."""
-    R, T = cached.shape[0], slots.shape[0]
-    for n, t, d in (("cached", cached, 1), ("fresh", fresh, 1), ("base", base, 1), ("free_pages", free_pages, 1), ("table", table, 2),
-                    ("row_off", row_off, 1), ("kv_len", kv_len, 1), ("slots", slots, 1), ("positions", positions, 1), ("taken", taken, 1)):
-        _want(n, t, torch.int32, d)
-    if (fresh.shape[0] != R or table.shape[0] != R or kv_len.shape[0] < R or row_off.shape[0] < R + 1 or positions.shape[0] < T or
-            taken.shape[0] < 1 or (base is not None and base.shape[0] != R)):
+    dev, i32 = _device_of(cached), torch.int32
+    if _bad(i32, dev, cached, fresh, base, free_pages, row_off, kv_len, slots, positions, taken) or _bad_rows(i32, dev, table):
+        _refuse(i32, 1, dev, cached=cached, fresh=fresh, base=base, free_pages=free_pages, row_off=row_off, kv_len=kv_len, slots=slots,
+                positions=positions, taken=taken)
+        _refuse(i32, 2, dev, table=table)
+    R, T = cached.numel(), slots.numel()
+    rows, cols = table.shape
+    if (fresh.numel() != R or rows != R or kv_len.numel() < R or row_off.numel() < R + 1 or positions.numel() < T or taken.numel() < 1 or
+            (base is not None and base.numel() != R)):
         raise ValueError("osc_kv_slots: lengths do not belong together")
-    _check(_lib.osc_kv_slots(_ptr(cached), _ptr(fresh), _ptr(base), R, page_size, _ptr(free_pages), free_pages.shape[0], _ptr(table),
-                             table.shape[1], table.stride(0), T, _ptr(row_off), _ptr(kv_len), _ptr(slots), _ptr(positions),
-                             _ptr(taken), _stream(stream)))
+    _check(_lib.osc_kv_slots(cached.data_ptr(), fresh.data_ptr(), _addr(base), R, page_size, free_pages.data_ptr(), free_pages.numel(),
+                             table.data_ptr(), cols, table.stride(0), T, row_off.data_ptr(), kv_len.data_ptr(), slots.data_ptr(),
+                             positions.data_ptr(), taken.data_ptr(), _stream(stream)))
 
 
 def osc_qk_norm_rope(QKV: torch.Tensor, n_q: int, cache: KvCache, Q: torch.Tensor, positions: torch.Tensor, rope: Rope, gamma_q=None,
                      gamma_k=None, eps: float = 1e-6, slots=None, stream=None):
     """Norm and rotation of the query and key heads of QKV [T, (n_q + 2 n_kv) head_dim]; queries to Q [T, n_q head_dim],
     keys and values to their slots of the cache.  positions: int32 [T] or [axes, T]."""
-    T = QKV.shape[0]
-    _want("QKV", QKV, torch.bfloat16, 2)
-    _want("Q", Q, torch.bfloat16, 2)
-    _want("gamma_q", gamma_q, torch.bfloat16, 1)
-    _want("gamma_k", gamma_k, torch.bfloat16, 1)
-    _want("slots", slots, torch.int32, 1)
-    _want("positions", positions, torch.int32)
-    axes = positions.shape[0] if positions.dim() == 2 else 1
-    if not 1 <= axes <= 3 or positions.dim() not in (1, 2):
+    dev, i32, bf16 = _device_of(QKV), torch.int32, torch.bfloat16
+    two = positions.dim() == 2
+    if (_bad_rows(bf16, dev, QKV, Q) or _bad(bf16, dev, gamma_q, gamma_k) or _bad(i32, dev, slots) or
+            (_bad_rows if two else _bad)(i32, dev, positions) or cache.device != dev or rope.device != dev):
+        _refuse(bf16, 2, dev, QKV=QKV, Q=Q)
+        _refuse(bf16, 1, dev, gamma_q=gamma_q, gamma_k=gamma_k)
+        _refuse(i32, 1, dev, slots=slots)
+        _refuse(i32, 2 if two else 1, dev, positions=positions)
+        raise ValueError(f"osc_qk_norm_rope: cache on cuda:{cache.device}, rope on cuda:{rope.device}, QKV on cuda:{dev}; vectors must be contiguous")
+    T, width = QKV.shape
+    qT, qw = Q.shape
+    axes = positions.shape[0] if two else 1
+    if not 1 <= axes <= 3:
         raise ValueError("positions: [T] or [axes, T] with at most three axes")
-    if (positions.shape[-1] < T or Q.shape[0] != T or (slots is not None and slots.shape[0] < T) or
-            QKV.shape[1] != (n_q + 2 * cache.n_heads) * cache.head_dim or Q.shape[1] < n_q * cache.head_dim or
-            any(g is not None and g.shape[0] != cache.head_dim for g in (gamma_q, gamma_k))):
+    if (positions.shape[-1] < T or qT != T or (slots is not None and slots.numel() < T) or
+            width != (n_q + 2 * cache.n_heads) * cache.head_dim or qw < n_q * cache.head_dim or
+            (gamma_q is not None and gamma_q.numel() != cache.head_dim) or (gamma_k is not None and gamma_k.numel() != cache.head_dim)):
         raise ValueError("osc_qk_norm_rope: shapes do not belong together")
-    _check(_lib.osc_qk_norm_rope(_ptr(QKV), T, QKV.stride(0) if T > 1 else QKV.shape[1], n_q, cache.c, _ptr(gamma_q), _ptr(gamma_k),
-                                 float(eps), rope.c[axes], _ptr(positions), positions.stride(0) if axes > 1 else T, _ptr(slots),
-                                 _ptr(Q), Q.stride(0) if T > 1 else Q.shape[1], _stream(stream)))
+    _check(_lib.osc_qk_norm_rope(QKV.data_ptr(), T, QKV.stride(0) if T > 1 else width, n_q, cache.c, _addr(gamma_q), _addr(gamma_k), eps,
+                                 rope.c[axes], positions.data_ptr(), positions.stride(0) if axes > 1 else T, _addr(slots), Q.data_ptr(),
+                                 Q.stride(0) if T > 1 else qw, _stream(stream)))
 
 
 def osc_paged_attention_workspace_bytes(T: int, n_q: int, head_dim: int, R: int, P: int = 0) -> int:
@@ -906,22 +941,29 @@ def osc_paged_attention(Q: torch.Tensor, cache: KvCache, row_off, kv_len, table,
                         lse=None, group_off=None, prefix_len=None, prefix_table=None, max_new: int = 0, stream=None):
     """Attention of the new tokens Q [T, n_q head_dim] over the cache; O [T, n_q head_dim], lse float32 [T, n_q] or None.
     With group_off [P + 1], prefix_len [P] and prefix_table [P, cols], groups of requests share prefixes."""
-    T, R = Q.shape[0], kv_len.shape[0]
-    P = prefix_len.shape[0] if prefix_len is not None else 0
-    _want("Q", Q, torch.bfloat16, 2)
-    _want("O", O, torch.bfloat16, 2)
-    _want("lse", lse, torch.float32, 2)
-    for n, t, d in (("row_off", row_off, 1), ("kv_len", kv_len, 1), ("table", table, 2), ("group_off", group_off, 1),
-                    ("prefix_len", prefix_len, 1), ("prefix_table", prefix_table, 2)):
-        _want(n, t, torch.int32, d)
-    n_q = Q.shape[1] // cache.head_dim
-    if (Q.shape[1] % cache.head_dim or O.shape != Q.shape or row_off.shape[0] < R + 1 or table.shape[0] < R or
-            (P and (group_off is None or prefix_table is None or group_off.shape[0] < P + 1 or prefix_table.shape[0] < P)) or
-            (lse is not None and (lse.shape != (T, n_q) or not lse.is_contiguous()))):
+    dev, i32, bf16 = _device_of(Q), torch.int32, torch.bfloat16
+    if (_bad_rows(bf16, dev, Q, O) or _bad(i32, dev, row_off, kv_len, prefix_len, group_off) or _bad_rows(i32, dev, table, prefix_table) or
+            _bad(torch.float32, dev, lse) or _bad(torch.uint8, dev, workspace) or cache.device != dev):
+        _refuse(bf16, 2, dev, Q=Q, O=O)
+        _refuse(i32, 1, dev, row_off=row_off, kv_len=kv_len, prefix_len=prefix_len, group_off=group_off)
+        _refuse(i32, 2, dev, table=table, prefix_table=prefix_table)
+        _refuse(torch.float32, 2, dev, lse=lse)
+        _refuse(torch.uint8, 1, dev, workspace=workspace)
+        raise ValueError(f"osc_paged_attention: vectors and lse must be contiguous, the cache (cuda:{cache.device}) on the device of Q, cuda:{dev}")
+    T, width = Q.shape
+    R, (rows, cols), n_q = kv_len.numel(), table.shape, width // cache.head_dim
+    P = prefix_len.numel() if prefix_len is not None else 0
+    if (width % cache.head_dim or O.shape != Q.shape or row_off.numel() < R + 1 or rows < R or
+            (P and (group_off is None or prefix_table is None or group_off.numel() < P + 1 or prefix_table.shape[0] < P)) or
+            (lse is not None and lse.numel() != T * n_q)):
         raise ValueError("osc_paged_attention: shapes do not belong together")
-    _check(_lib.osc_paged_attention(_ptr(Q), T, Q.stride(0) if T > 1 else Q.shape[1], n_q, cache.c, R, _ptr(row_off), _ptr(kv_len), _ptr(table),
-                                    table.shape[1], table.stride(0), P, _ptr(group_off) if P else None, _ptr(prefix_len) if P else None,
-                                    _ptr(prefix_table) if P else None, prefix_table.shape[1] if P else 0,
-                                    prefix_table.stride(0) if P else 0, max_new, float(scale), _ptr(O),
-                                    O.stride(0) if T > 1 else O.shape[1], _ptr(lse), _ptr(workspace),
-                                    workspace.numel() * workspace.element_size(), _stream(stream)))
+    ldq, ldo = (Q.stride(0), O.stride(0)) if T > 1 else (width, width)
+    if P:
+        _check(_lib.osc_paged_attention(Q.data_ptr(), T, ldq, n_q, cache.c, R, row_off.data_ptr(), kv_len.data_ptr(), table.data_ptr(), cols,
+                                        table.stride(0), P, group_off.data_ptr(), prefix_len.data_ptr(), prefix_table.data_ptr(),
+                                        prefix_table.shape[1], prefix_table.stride(0), max_new, scale, O.data_ptr(), ldo, _addr(lse),
+                                        workspace.data_ptr(), workspace.numel(), _stream(stream)))
+    else:
+        _check(_lib.osc_paged_attention(Q.data_ptr(), T, ldq, n_q, cache.c, R, row_off.data_ptr(), kv_len.data_ptr(), table.data_ptr(), cols,
+                                        table.stride(0), 0, None, None, None, 0, 0, max_new, scale, O.data_ptr(), ldo, _addr(lse),
+                                        workspace.data_ptr(), workspace.numel(), _stream(stream)))
