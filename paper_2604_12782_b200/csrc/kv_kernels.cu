@@ -19,7 +19,6 @@ namespace osc {
 // request by binary search in shared memory.  A page that this call hands out is read from the free list, not
 // from the table, so nothing written by another CTA is read.  What bounds it is latency: lengths -> scan ->
 // search -> page -> store, one after the other.
-constexpr int KS_THREADS = 512;
 
 struct KvSlotsArgs {
     const int32_t* cached;
@@ -46,6 +45,8 @@ __device__ __forceinline__ int search_last(const int* start, int n, int x) {
     return lo;
 }
 
+// KS_THREADS: 256, or 1024 for more requests than that, so that nearly every step is one chunk of requests
+template <int KS_THREADS>
 __global__ void __launch_bounds__(KS_THREADS) kv_slots_kernel(const KvSlotsArgs a) {
     __shared__ int s_row[KS_THREADS + 1], s_first[KS_THREADS + 1], s_cached[KS_THREADS], s_base[KS_THREADS];
     __shared__ unsigned long long s_warp[KS_THREADS / 32];
@@ -73,6 +74,7 @@ __global__ void __launch_bounds__(KS_THREADS) kv_slots_kernel(const KvSlotsArgs 
         if (lane == 31) s_warp[warp] = inc;
         __syncthreads();
         unsigned long long before = carry, total = carry;
+#pragma unroll 1
         for (int w = 0; w < KS_THREADS / 32; ++w) {
             if (w < warp) before += s_warp[w];
             total += s_warp[w];
@@ -126,9 +128,13 @@ __global__ void __launch_bounds__(KS_THREADS) kv_slots_kernel(const KvSlotsArgs 
     }
 }
 
+template <int KS_THREADS>
+static cudaError_t launch_kv_slots_n(const KvSlotsArgs& a, int num_sms, cudaStream_t st) {
+    const int grid = std::max(1, std::min(num_sms, a.T / KS_THREADS + (a.T % KS_THREADS != 0)));
+    return launch_pdl(kv_slots_kernel<KS_THREADS>, dim3(grid), dim3(KS_THREADS), 0, st, a);
+}
 cudaError_t launch_kv_slots(const KvSlotsArgs& a, int num_sms, cudaStream_t st) {
-    const int grid = max(1, min(num_sms, (a.T + KS_THREADS - 1) / KS_THREADS));
-    return launch_pdl(kv_slots_kernel, dim3(grid), dim3(KS_THREADS), 0, st, a);
+    return a.R <= 256 ? launch_kv_slots_n<256>(a, num_sms, st) : launch_kv_slots_n<1024>(a, num_sms, st);
 }
 
 // ------------------------------------------------------------------------------------------ qk_norm_rope
