@@ -403,7 +403,7 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
         regs_inc<AW_REGS_SOFTMAX>();
         const int s = warp >> 2;                                         // stream
         const int r = threadIdx.x & 127;                                 // row of the tile = TMEM lane
-        const int my_tok = r / a.G;
+        const int my_tok = r * a.inv_g >> 16;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t t_s = tmem + lanes + C::TM_S, t_p = tmem + lanes + C::TM_P + s * (AT_WIDE_KEYS / 2), t_o = tmem + lanes + C::TM_O;
         const float scale = a.scale_log2;
@@ -533,7 +533,7 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
             const int slot0 = AT_FEW_SLOTS + (blockIdx.x * 2 + (out & OUT_LATER ? 1 : 0)) * (2 * AT_WIDE_TILE) + (pair ? s * AT_WIDE_TILE : 0);
             // row of the partial results (or of lse) that tile row x goes to, -1: none
             auto place = [&](int x) -> int {
-                const int t = x / a.G;
+                const int t = x * a.inv_g >> 16;
                 if (t >= tpt || tok0 + t >= tokens) return -1;
                 if (out & OUT_SPLIT) return slot0 + x;
                 const int row = (row0 + tok0 + t) * a.Hq + hq0 + x - t * a.G;
@@ -655,7 +655,7 @@ static cudaError_t launch_attn_d(const AttnWideArgs& w, bool wide, cudaStream_t 
     if (!wide && a.P == 0 && a.R <= FEW_SELF && a.few_hw == 4) {
         if ((e = launch_attn_few<D, 4, true>(a, false, st)) != cudaSuccess) return e;
     } else {
-        const int threads = std::min(1024, std::max(128, (a.P + a.R + 127) / 128 * 128));
+        const int threads = std::min(1024, std::max(128, (a.P + a.R + 31) / 32 * 32));
         if ((e = launch_pdl(attn_plan_kernel, dim3(1), dim3(threads), 0, st, a)) != cudaSuccess) return e;
         if (wide && (e = launch_pdl(attn_wide_kernel<D>, dim3(a.wide_ctas), dim3(AW_THREADS), WideCfg<D>::SMEM, st, w)) != cudaSuccess) return e;
         e = a.few_hw == 4 ? launch_attn_few<D, 4, false>(a, wide, st)
@@ -664,10 +664,10 @@ static cudaError_t launch_attn_d(const AttnWideArgs& w, bool wide, cudaStream_t 
     }
     JoinGrid g;
     g.wide_split = (int64_t)a.T * a.G >= 2048 ? 8 : 1;      // with few rows nearly all of them have two sources
+    g.few_split = a.P ? 1 : a.few_hw;
     g.wide_blocks = wide ? a.wide_ctas * g.wide_split : 0;
-    g.few_blocks = a.few_ctas * a.few_hw;
     g.row_blocks = a.P ? (int)std::min<int64_t>(3 * AT_MAX_SMS, ((int64_t)a.T * a.Hq + AT_JOIN_WARPS - 1) / AT_JOIN_WARPS) : 0;
-    return launch_pdl(attn_join_kernel<D>, dim3(g.wide_blocks + g.few_blocks + g.row_blocks), dim3(AT_JOIN_THREADS), 0, st, a, g);
+    return launch_pdl(attn_join_kernel<D>, dim3(g.row_blocks + g.wide_blocks + a.few_ctas * g.few_split), dim3(AT_JOIN_THREADS), 0, st, a, g);
 }
 
 cudaError_t launch_attn(const AttnWideArgs& w, int D, bool wide, cudaStream_t st) {

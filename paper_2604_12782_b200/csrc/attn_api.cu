@@ -191,7 +191,7 @@ osc_status osc_paged_attention(const void* Q, int T, int64_t ldq, int n_q, const
     a.page_stride = cache->page_stride; a.token_stride = cache->token_stride; a.head_stride = cache->head_stride;
     a.row_off = row_off; a.kv_len = kv_len; a.table = table; a.ld_table = ld_table; a.cols = cols;
     a.group_off = group_off; a.prefix_len = prefix_len; a.ptable = prefix_table; a.ld_ptable = ld_prefix; a.pcols = P ? prefix_cols : 0;
-    a.T = T; a.Hq = n_q; a.Hk = cache->n_heads; a.G = n_q / cache->n_heads; a.tpt = AT_WIDE_TILE / a.G; a.head_dim = D; a.R = R; a.P = P; a.n_pages = cache->n_pages;
+    a.T = T; a.Hq = n_q; a.Hk = cache->n_heads; a.G = n_q / cache->n_heads; a.tpt = AT_WIDE_TILE / a.G; a.inv_g = (65536 + a.G - 1) / a.G; a.head_dim = D; a.R = R; a.P = P; a.n_pages = cache->n_pages;
     while ((1 << a.page_shift) < cache->page_size) ++a.page_shift;
     a.scale_log2 = scale * 1.44269504088896341f;
     a.few_hw = hw;

@@ -60,7 +60,8 @@ struct AttnPlan {            // filled by attn_plan_kernel
     int32_t* few_start;      // [S + 1] first tile of every segment on the few-row line
     int32_t* wide_start;     // [S + 1] ... on the tcgen05 line
     Segment* seg;            // [S]
-    int32_t* tok_req;        // [T], where there are prefixes: the request of every token whose rows have two sources, else -1
+    int32_t* tok_req;        // [T], where there are prefixes: the request of every token whose rows have two sources, else -1;
+                             // not written where no request covers the token
     int32_t* share;          // [3]: tiles of a share on the few-row line, on the tcgen05 line; whether any row has two sources
     CutUnit* cut[2];         // [AT_FEW_CTAS], [AT_WIDE_CTAS]: filled by the attention kernels
 };
@@ -83,6 +84,7 @@ struct AttnArgs {
     int64_t ld_table, ld_ptable;
     int T, Hq, Hk, G, head_dim, R, P, cols, pcols, page_shift, n_pages;
     int wide_min_rows;       // segments with at least this many rows per head go to the tcgen05 kernel
+    int inv_g;               // ceil(2^16 / G): x / G = x * inv_g >> 16 for x < 128
     int tpt;                 // whole tokens that fit the 128 rows of a tcgen05 tile
     int few_hw;              // heads of a few-row unit: 4, 2 or 1
     int few_ctas, wide_ctas;
@@ -179,6 +181,7 @@ __device__ __forceinline__ int64_t floor_sum(int64_t n, int64_t m, int64_t a, in
     }
     return sum;
 }
+constexpr int AT_LOOP_UNITS = 64;
 // key tiles of the units before unit u (u <= count) of one head; the host has seen to it that counts of tiles are ints
 template <class U>
 __device__ __forceinline__ int tiles_before(const AttnArgs& a, const Segment& g, int nu, int u) {
@@ -193,7 +196,12 @@ __device__ __forceinline__ int tiles_before(const AttnArgs& a, const Segment& g,
     if (u > 0) {
         int64_t A, B, M, u0;
         U::line(a, g, A, B, M, u0);      // own tiles(i) = floor((A i + B) / M) from unit u0 on, none before it
-        if (u > u0) sum += (int)floor_sum(u - u0, M, A, B + A * u0);
+        if (u - u0 <= AT_LOOP_UNITS) {   // nearly always: a short loop, where the closed form's 64-bit divisions take longer
+#pragma unroll 1
+            for (int i = (int)u0; i < u; ++i) sum += unit_tiles<U>(a, g, i) - front_tiles<U>(a, g);
+        } else {
+            sum += (int)floor_sum(u - u0, M, A, B + A * u0);
+        }
     }
     return sum;
 }
@@ -210,7 +218,7 @@ __device__ __forceinline__ int head_tiles(const AttnArgs& a, const Segment& g) {
 __device__ __forceinline__ int share_tiles(int N, int ctas, int least) { return max((int)(((int64_t)N + ctas - 1) / ctas), least); }
 // least share: 64 keys of few_hw heads
 __device__ __forceinline__ int few_min_tiles(const AttnArgs& a) { return a.few_hw; }
-constexpr int AT_WIDE_MIN_TILES = 2;
+constexpr int AT_WIDE_MIN_TILES = 4;
 
 // Where a cursor finds segments and their first tiles: what the plan kernel left in the workspace, or (SELF) shared memory.
 template <bool SELF>
@@ -254,6 +262,14 @@ struct Cursor {
             nt = unit_tiles<U>(a, g, 0);
             u = y / nt;
             kt = y - u * nt;
+        } else if (nu <= AT_LOOP_UNITS) {
+            u = 0;
+            nt = unit_tiles<U>(a, g, 0);
+            while (y >= nt) {
+                y -= nt;
+                nt = unit_tiles<U>(a, g, ++u);
+            }
+            kt = y;
         } else {
             int b = 0, e = nu;           // the last unit with at most y tiles before it
             while (e - b > 1) {
@@ -372,8 +388,10 @@ __global__ void __launch_bounds__(1024) attn_plan_kernel(const AttnArgs a) {
             }
             __syncthreads();
             // groups that have requests with few rows need a prefix segment (with more groups than fit here all have one)
-            for (int r = tid; r < a.R; r += threads) {
-                const int64_t rows = (int64_t)(attn_row(a, r + 1) - attn_row(a, r)) * a.G;
+            for (int s = tid; s < S; s += threads) {
+                const int r = s - a.P;
+                if (r < 0) continue;
+                const int rows = (attn_row(a, r + 1) - attn_row(a, r)) * a.G;
                 if (rows > 0 && (rows < AT_MERGE_ROWS || rows < a.wide_min_rows)) {
                     const int g = group_of(r);
                     if (g >= 0) s_mixed[g] = 1;
@@ -384,7 +402,7 @@ __global__ void __launch_bounds__(1024) attn_plan_kernel(const AttnArgs a) {
     }
     auto mixed = [&](int g) { return in_smem ? s_mixed[g] != 0 : true; };
     int carry[2] = {0, 0};
-    bool two = false, empty = false;
+    bool two = false, empty = false, longer = false;
     for (int s0 = 0; s0 < S; s0 += threads) {
         const int s = s0 + tid;
         int own[2] = {0, 0}, inc[2], total[2];
@@ -411,6 +429,9 @@ __global__ void __launch_bounds__(1024) attn_plan_kernel(const AttnArgs a) {
                 }
                 two |= g.n > 0 && (g.flags & SEG_TWO);
                 empty |= g.n > g.klen && g.group < 0;
+                if (a.P > 0 && g.n <= 32)          // the tokens' requests; of longer ones and behind the last token further down
+                    for (int t = g.t0; t < g.t0 + g.n; ++t) a.plan.tok_req[t] = g.flags & SEG_TWO ? r : -1;
+                longer |= a.P > 0 && g.n > 32;
             }
             if (g.n * a.G >= a.wide_min_rows) {
                 g.flags |= SEG_WIDE;
@@ -435,7 +456,7 @@ __global__ void __launch_bounds__(1024) attn_plan_kernel(const AttnArgs a) {
         carry[1] += total[1];
     }
     two = __syncthreads_or(two);
-    empty = __syncthreads_or(empty);
+    empty = __syncthreads_or(empty || longer);
     if (tid == 0) {
         a.plan.share[2] = two;
         a.plan.few_start[S] = carry[0];
@@ -443,20 +464,14 @@ __global__ void __launch_bounds__(1024) attn_plan_kernel(const AttnArgs a) {
         a.plan.share[0] = share_tiles(carry[0], a.few_ctas, few_min_tiles(a));
         a.plan.share[1] = share_tiles(carry[1], a.wide_ctas, AT_WIDE_MIN_TILES);
     }
-    __syncthreads();
-    if (two) {
-        for (int t = tid; t < a.T; t += threads) a.plan.tok_req[t] = -1;
-        __syncthreads();
-        for (int r = tid >> 5; r < a.R; r += threads / 32) {
-            const Segment& g = a.plan.seg[a.P + r];
-            if (g.flags & SEG_TWO)
-                for (int t = g.t0 + (tid & 31); t < g.t0 + g.n; t += 32) a.plan.tok_req[t] = r;
-        }
-    }
+    if (two)
+        for (int t = attn_row(a, a.R) + tid; t < a.T; t += threads) a.plan.tok_req[t] = -1;
     if (empty) {
         for (int r = tid >> 5; r < a.R; r += threads / 32) {
             const Segment& g = a.plan.seg[a.P + r];
             if (g.group < 0 && g.n > g.klen) clear_rows(a, g.t0, g.n - g.klen);
+            if (two && g.n > 32)
+                for (int t = g.t0 + (tid & 31); t < g.t0 + g.n; t += 32) a.plan.tok_req[t] = g.flags & SEG_TWO ? r : -1;
         }
     }
 }
@@ -465,7 +480,6 @@ __global__ void __launch_bounds__(1024) attn_plan_kernel(const AttnArgs a) {
 struct PieceList {           // pieces of one row from one unit
     int count;               // 0: none; 1: the whole unit
     int first, rest, stride; // rows of the partial results: `first` for piece 0, rest + i * stride for the others
-    __device__ int at(int i) const { return i ? rest + i * stride : first; }
 };
 // A unit of `tiles` tiles from `begin` on, cut into shares of q; `base`: row of the line's slots; stride: rows between two
 // slots of a CTA; row: row in a slot; whole: row of the dense results
@@ -828,48 +842,57 @@ constexpr int AT_JOIN_THREADS = 256;
 constexpr int AT_JOIN_WARPS = AT_JOIN_THREADS / 32;
 
 template <int D>
-__device__ __forceinline__ void join_row(const AttnArgs& a, const PieceList& p0, const PieceList& p1, int token, int hq) {
+__device__ __forceinline__ void join_row(const AttnArgs& a, const PieceList (&p)[2], int token, int hq) {
     constexpr int V = D / 32;          // channels per lane
     constexpr int FLIGHT = 8;          // pieces under way at a time
-    const int lane = threadIdx.x & 31, n = p0.count + p1.count;
+    const int lane = threadIdx.x & 31;
+    const float* part = a.part + lane * V;
     float m = -INFINITY, l = 0.0f, o[V];
 #pragma unroll
     for (int y = 0; y < V; ++y) o[y] = 0.0f;
 #pragma unroll 1
-    for (int i = 0; i < n; i += FLIGHT) {
-        float2 ml[FLIGHT];
-        float v[FLIGHT][V];
+    for (int which = 0; which < 2; ++which) {
+        const int n = which ? p[1].count : p[0].count, first = which ? p[1].first : p[0].first;
+        const int rest = which ? p[1].rest : p[0].rest, stride = which ? p[1].stride : p[0].stride;
+#pragma unroll 1
+        for (int i = 0; i < n; i += FLIGHT) {
+            float2 ml[FLIGHT];
+            float v[FLIGHT][V];
 #pragma unroll
-        for (int j = 0; j < FLIGHT; ++j) {
-            const int x = min(i + j, n - 1), at = x < p0.count ? p0.at(x) : p1.at(x - p0.count);
-            ml[j] = a.ml[at];
-            if (i + j >= n) ml[j].x = -INFINITY;
-            const float* src = a.part + (int64_t)at * D + lane * V;
-            if (V == 4) {
-                const float4 q = *reinterpret_cast<const float4*>(src);
-                v[j][0] = q.x; v[j][1] = q.y; v[j][V - 2] = q.z; v[j][V - 1] = q.w;
-            } else {
-                const float2 q = *reinterpret_cast<const float2*>(src);
-                v[j][0] = q.x; v[j][1] = q.y;
+            for (int j = 0; j < FLIGHT; ++j) {
+                ml[j] = make_float2(-INFINITY, 0.0f);
+                if (i + j < n) {
+                    const int at = i + j ? rest + (i + j) * stride : first;
+                    ml[j] = a.ml[at];
+                    const float* src = part + (int64_t)at * D;
+                    if (V == 4) {
+                        const float4 q = *reinterpret_cast<const float4*>(src);
+                        v[j][0] = q.x; v[j][1] = q.y; v[j][V - 2] = q.z; v[j][V - 1] = q.w;
+                    } else {
+                        const float2 q = *reinterpret_cast<const float2*>(src);
+                        v[j][0] = q.x; v[j][1] = q.y;
+                    }
+                }
+            }
+            float mn = m;
+#pragma unroll
+            for (int j = 0; j < FLIGHT; ++j) mn = fmaxf(mn, ml[j].x);
+            if (mn == -INFINITY) continue;
+            const float f = exp2_approx(m - mn);
+            m = mn;
+            l *= f;
+#pragma unroll
+            for (int y = 0; y < V; ++y) o[y] *= f;
+#pragma unroll
+            for (int j = 0; j < FLIGHT; ++j) {
+                const float w = exp2_approx(ml[j].x - mn);
+                if (w != 0.0f) {           // a piece without weight may hold anything
+                    l = fmaf(ml[j].y, w, l);
+#pragma unroll
+                    for (int y = 0; y < V; ++y) o[y] = fmaf(v[j][y], w, o[y]);
+                }
             }
         }
-        float mn = m;
-#pragma unroll
-        for (int j = 0; j < FLIGHT; ++j) mn = fmaxf(mn, ml[j].x);
-        if (mn == -INFINITY) continue;
-        const float f = exp2_approx(m - mn);
-        m = mn;
-        l *= f;
-#pragma unroll
-        for (int y = 0; y < V; ++y) o[y] *= f;
-#pragma unroll
-        for (int j = 0; j < FLIGHT; ++j)
-            if (ml[j].x != -INFINITY) {        // a piece without weight may hold anything
-                const float w = exp2_approx(ml[j].x - mn);
-                l = fmaf(ml[j].y, w, l);
-#pragma unroll
-                for (int y = 0; y < V; ++y) o[y] = fmaf(v[j][y], w, o[y]);
-            }
     }
     const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
     uint16_t* op = a.o + (int64_t)token * a.ldo + (int64_t)hq * D + lane * V;
@@ -881,11 +904,12 @@ __device__ __forceinline__ void join_row(const AttnArgs& a, const PieceList& p0,
     if (a.lse && lane == 0) a.lse[(int64_t)token * a.Hq + hq] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
 }
 
+// Blocks in this order: those with the longest chains come first, the many that mostly find nothing to do last.
 struct JoinGrid {
+    int row_blocks;          // over the tokens' rows
     int wide_blocks;         // wide_ctas x wide_split: a part of the 256 rows of a cut wide unit each
     int wide_split;
-    int few_blocks;          // few_ctas x few_hw: one head of a cut few-row unit each
-    int row_blocks;          // over the tokens' rows
+    int few_split;           // few_ctas x few_split: a part of the rows of a cut few-row unit each
 };
 
 template <int D>
@@ -896,50 +920,58 @@ __global__ void __launch_bounds__(AT_JOIN_THREADS, 3) attn_join_kernel(const Att
     int b = blockIdx.x;
     PieceList p[2];
     p[0].count = p[0].first = p[0].rest = p[0].stride = 0;
-    const bool wide = b < grid.wide_blocks;
-    if (!wide) b -= grid.wide_blocks;
-    if (wide || b < grid.few_blocks) {
-        const int split = wide ? grid.wide_split : a.few_hw;
+    if (b >= grid.row_blocks) {
+        b -= grid.row_blocks;
+        const bool wide = b < grid.wide_blocks;
+        if (!wide) b -= grid.wide_blocks;
+        const int split = wide ? grid.wide_split : grid.few_split;
         const CutUnit cut = a.plan.cut[wide][b / split];
         if (cut.tiles == 0) return;
-        const int tpt = a.tpt, part = b % split, rows = wide ? 2 * AT_WIDE_TILE / split : AT_FEW_ROWS;
+        const int slot_rows = wide ? 2 * AT_WIDE_TILE : a.few_hw * AT_FEW_ROWS, rows = slot_rows / split, part = b % split;
 #pragma unroll 1
         for (int i = warp; i < rows; i += AT_JOIN_WARPS) {
-            const int row = part * rows + i, r = wide ? row % AT_WIDE_TILE : cut.u * AT_FEW_ROWS + i;
-            const int tok = r / a.G + (wide ? (cut.u * 2 + row / AT_WIDE_TILE) * tpt : 0);
-            if ((wide && r >= tpt * a.G) || tok >= cut.n) continue;
-            p[1] = list_pieces(cut.begin, cut.tiles, cut.share, wide ? AT_FEW_SLOTS : 0, wide ? 2 * AT_WIDE_TILE : a.few_hw * AT_FEW_ROWS, row, 0);
-            join_row<D>(a, p[0], p[1], cut.t0 + tok, (wide ? cut.h : cut.h * a.few_hw + part) * a.G + r % a.G);
+            const int row = part * rows + i, r = wide ? row % AT_WIDE_TILE : cut.u * AT_FEW_ROWS + row % AT_FEW_ROWS;
+            const int tok = r / a.G + (wide ? (cut.u * 2 + row / AT_WIDE_TILE) * a.tpt : 0);
+            if ((wide && r >= a.tpt * a.G) || tok >= cut.n) continue;
+            p[1] = list_pieces(cut.begin, cut.tiles, cut.share, wide ? AT_FEW_SLOTS : 0, slot_rows, row, 0);
+            join_row<D>(a, p, cut.t0 + tok, (wide ? cut.h : cut.h * a.few_hw + row / AT_FEW_ROWS) * a.G + r % a.G);
         }
         return;
     }
-    // rows that have a prefix and own keys: the rest of the grid strides over all rows
-    b -= grid.few_blocks;
+    // rows that have a prefix and own keys
     const int two = a.plan.share[2], nf = a.plan.share[0], nw = a.plan.share[1], rows = a.T * a.Hq;
     if (two == 0) return;
 #pragma unroll 1
     for (int i = b * AT_JOIN_WARPS + warp; i < rows; i += grid.row_blocks * AT_JOIN_WARPS) {
         const int t = i / a.Hq, hq = i - t * a.Hq, h = hq / a.G, g = hq - h * a.G;
         const int r = a.plan.tok_req[t];
-        if (r < 0) continue;
+        if ((unsigned)r >= (unsigned)a.R) continue;
+        // a token that no request covers holds what the workspace held before: it counts only inside its request
         const Segment own = a.plan.seg[a.P + r];
-#pragma unroll 1
-        for (int which = 0; which < 2; ++which) {
-            const Segment sg = which ? own : a.plan.seg[own.group];
-            const int tok = t - sg.t0, fr = tok * a.G + g;
-            PieceList x;
-            x.count = x.first = x.rest = x.stride = 0;
-            if (tok >= 0 && tok < sg.n) {
-                const bool w = sg.flags & SEG_WIDE;
-                const int tpt = a.tpt, u = w ? tok / (2 * tpt) : fr / AT_FEW_ROWS, in = tok - u * 2 * tpt;
-                const int row = w ? (in >= tpt ? AT_WIDE_TILE + (in - tpt) * a.G : in * a.G) + g : h % a.few_hw * AT_FEW_ROWS + fr % AT_FEW_ROWS;
-                const int nt = w ? unit_tiles<WideUnits>(a, sg, u) : unit_tiles<FewUnits>(a, sg, u);
-                const int begin = w ? unit_begin<WideUnits>(a, sg, h, u) : unit_begin<FewUnits>(a, sg, h / a.few_hw, u);
-                if (nt) x = list_pieces(begin, nt, w ? nw : nf, w ? AT_FEW_SLOTS : 0, w ? 2 * AT_WIDE_TILE : a.few_hw * AT_FEW_ROWS, row, dense_row(a, which, i));
-            }
-            if (which) p[1] = x; else p[0] = x;
+        if (t < own.t0 || t >= own.t0 + own.n || !(own.flags & SEG_TWO)) continue;
+        // even lanes work out the pieces of the prefix, odd lanes those of the own keys
+        const int which = threadIdx.x & 1;
+        const Segment sg = which ? own : a.plan.seg[own.group];
+        const int tok = t - sg.t0, fr = tok * a.G + g;
+        PieceList x;
+        x.count = x.first = x.rest = x.stride = 0;
+        if (tok >= 0 && tok < sg.n) {
+            const bool w = sg.flags & SEG_WIDE;
+            const int tpt = a.tpt, u = w ? tok / (2 * tpt) : fr / AT_FEW_ROWS, in = tok - u * 2 * tpt, hs = a.few_hw == 4 ? 2 : a.few_hw == 2 ? 1 : 0;
+            const int row = w ? (in >= tpt ? AT_WIDE_TILE + (in - tpt) * a.G : in * a.G) + g : (h & (a.few_hw - 1)) * AT_FEW_ROWS + fr % AT_FEW_ROWS;
+            const int nt = w ? unit_tiles<WideUnits>(a, sg, u) : unit_tiles<FewUnits>(a, sg, u);
+            const int begin = w ? unit_begin<WideUnits>(a, sg, h, u) : unit_begin<FewUnits>(a, sg, h >> hs, u);
+            if (nt) x = list_pieces(begin, nt, w ? nw : nf, w ? AT_FEW_SLOTS : 0, w ? 2 * AT_WIDE_TILE : a.few_hw * AT_FEW_ROWS, row, dense_row(a, which, i));
         }
-        join_row<D>(a, p[0], p[1], t, hq);
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            p[k].count = __shfl_sync(0xFFFFFFFFu, x.count, k);
+            p[k].first = __shfl_sync(0xFFFFFFFFu, x.first, k);
+            p[k].rest = __shfl_sync(0xFFFFFFFFu, x.rest, k);
+            p[k].stride = __shfl_sync(0xFFFFFFFFu, x.stride, k);
+        }
+        join_row<D>(a, p, t, hq);
     }
 }
 

@@ -217,3 +217,69 @@ def test_many_units_to_a_share(B):
     of all kinds, one after the other."""
     go(B, seed=21, Hk=8, G=4, D=128, page=64, new=[700, 3, 650, 900], kv=[1000, 900, 650, 1111], prefix=[391])
     go(B, seed=22, Hk=8, G=8, D=64, page=16, new=[500, 333, 420], kv=[777, 640, 421], prefix=[129, 70], groups=[0, 2, 3])
+
+
+@pytest.mark.parametrize("R,P,G", [(257, 0, 4), (300, 3, 4), (1100, 2, 2), (1300, 0, 1), (700, 600, 1)])
+def test_many_requests(B, R, P, G):
+    """More requests and groups than the plan handles in one go."""
+    rng = np.random.default_rng(R)
+    new = list(rng.choice([0, 1, 2], R, p=[0.1, 0.8, 0.1]))
+    kv = [int(n + rng.integers(0, 40)) for n in new]
+    go(B, seed=R, Hk=1, G=G, D=64, page=16, new=new, kv=kv, prefix=[int(x) for x in rng.integers(0, 60, P)], tail_rows=1)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_long_and_short_requests_of_one_group(B, D):
+    """Prompts and single tokens behind the same prefix; a second group of prompts only."""
+    go(B, seed=21, Hk=2, G=4, D=D, page=16, new=[70, 1, 300, 0, 33, 1], kv=[90, 40, 300, 7, 500, 0], prefix=[200])
+    go(B, seed=22, Hk=1, G=8, D=D, page=32, new=[100, 1, 64, 40, 130], kv=[100, 300, 64, 300, 131], prefix=[333, 90], groups=[0, 2, 5], tail_rows=2)
+
+
+def test_tokens_in_front_of_the_first_request(B):
+    """Rows in front of row_off[0] are left as they were, whatever the workspace held."""
+    for fill in (0, 1, 0x7F):
+        c = AttnCase(23, 2, 4, 128, 16, [1, 1, 40, 1], [30, 4, 60, 9], prefix=[100, 50], groups=[0, 2, 4])
+        front, Hq, D = 5, 8, 128
+        q = torch.full((c.T + front, Hq * D), float("nan"), dtype=torch.bfloat16, device="cuda")
+        q[front:] = c.q
+        o = torch.full_like(q, 7.0)
+        lse = torch.full((c.T + front, Hq), 7.0, device="cuda")
+        ws = torch.full((B.osc_paged_attention_workspace_bytes(c.T + front, Hq, D, 4, 2) // 4,), fill, dtype=torch.int32, device="cuda")
+        ws = ws.view(torch.uint8)
+        B.osc_paged_attention(q, B.KvCache(c.k, c.v), c.row_off + front, c.kv_len, c.table, o, ws, c.scale, lse=lse, group_off=c.group_off,
+                              prefix_len=c.prefix_len, prefix_table=c.ptable)
+        B.osc_sync_check()
+        c.check(o[front:], lse[front:], f"front rows, workspace of {fill}")
+        assert (o[:front].float() == 7.0).all() and (lse[:front] == 7.0).all()
+
+
+def test_no_requests_and_no_tokens(B):
+    c = AttnCase(24, 2, 4, 64, 16, [0, 0], [5, 0], prefix=[20])
+    o, lse = c.run(B)
+    B.osc_sync_check()
+    c.check(o, lse, "no tokens")
+    d = AttnCase(25, 2, 4, 64, 16, [1], [5], tail_rows=2)
+    o, lse = torch.full((3, 512), 7.0, dtype=torch.bfloat16, device="cuda"), torch.full((3, 8), 7.0, device="cuda")
+    ws = torch.zeros(B.osc_paged_attention_workspace_bytes(3, 8, 64, 0, 0), dtype=torch.uint8, device="cuda")
+    B.osc_paged_attention(d.q, B.KvCache(d.k, d.v), d.row_off[:1], d.kv_len[:0], d.table[:0], o, ws, d.scale, lse=lse)
+    B.osc_sync_check()
+    assert (o.float() == 7.0).all() and (lse == 7.0).all()
+
+
+def test_two_streams_at_once(B):
+    """Two steps under way at once, each with its own workspace."""
+    cases = [AttnCase(26, 2, 4, 128, 16, [1] * 40 + [90], [700] * 41, prefix=[1500]), AttnCase(27, 4, 8, 128, 16, [1] * 9, [5000] * 9)]
+    streams, bufs = [torch.cuda.Stream() for _ in cases], []
+    for c in cases:
+        Hq, R, P = c.Hk * c.G, len(c.new), len(c.prefix)
+        bufs.append((torch.full((c.T, Hq * c.D), 7.0, dtype=torch.bfloat16, device="cuda"), torch.full((c.T, Hq), 7.0, device="cuda"),
+                     torch.zeros(B.osc_paged_attention_workspace_bytes(c.T, Hq, c.D, R, P), dtype=torch.uint8, device="cuda")))
+    torch.cuda.synchronize()
+    for _ in range(8):
+        for c, (o, lse, ws), st in zip(cases, bufs, streams):
+            P = len(c.prefix)
+            B.osc_paged_attention(c.q, B.KvCache(c.k, c.v), c.row_off, c.kv_len, c.table, o, ws, c.scale, lse=lse, group_off=c.group_off,
+                                  prefix_len=c.prefix_len, prefix_table=c.ptable if P else None, stream=st)
+    torch.cuda.synchronize()
+    for c, (o, lse, _) in zip(cases, bufs):
+        c.check(o, lse, "two streams")
