@@ -607,8 +607,13 @@ osc_status osc_qk_norm_rope(const void* QKV, int T, int64_t ld, int n_q, const o
  * the order of the request's own new tokens still meets that row with weight 0, so an Inf or NaN in the VALUE of a new
  * token reaches the rows of the tokens before it in the same request.
  * max_new: most new tokens of any request if the caller knows (1 in a decoding step), 0 otherwise; a choice of kernel, the
- * result holds whatever it says.  Workspace: osc_paged_attention_workspace_bytes with the same n_q, head_dim and with T, R, P at least the call's.
- * P = 0: group_off, prefix_len and prefix_table are not read. */
+ * result holds whatever it says.  P = 0: group_off, prefix_len and prefix_table are not read.
+ * Workspace: osc_paged_attention_workspace_bytes with the same n_q and head_dim and with T, R, P at least the call's; what it
+ * holds does not matter.  Two calls under way at once need one each.
+ * Limits (OSC_ERR_SHAPE): T * n_q <= 2^29; the columns of a table hold at most 2^29 keys; R, P and the tables' widths together
+ * stay below 2^31 tiles (a tile is at the least 64 keys of one key/value head, or 16 of four, by 16 rows).
+ * The cache's, the offsets' and the tables' contents are the caller's: rows that two requests claim, or a row_off that falls, give
+ * unspecified rows of O and lse, never an access outside the buffers. */
 osc_status osc_paged_attention_workspace_bytes(int T, int n_q, int head_dim, int R, int P, size_t* bytes);
 osc_status osc_paged_attention(const void* Q, int T, int64_t ldq, int n_q, const osc_kv_cache_t* cache, int R,
                                const int32_t* row_off, const int32_t* kv_len, const int32_t* table, int cols, int64_t ld_table,
