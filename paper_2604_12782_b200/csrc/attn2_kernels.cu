@@ -664,7 +664,7 @@ static cudaError_t launch_attn_d(const AttnWideArgs& w, bool wide, cudaStream_t 
     }
     JoinGrid g;
     g.wide_split = (int64_t)a.T * a.G >= 2048 ? 8 : 1;      // with few rows nearly all of them have two sources
-    g.few_split = a.P ? 1 : a.few_hw;
+    g.few_split = wide ? 1 : a.few_hw;
     g.wide_blocks = wide ? a.wide_ctas * g.wide_split : 0;
     g.row_blocks = a.P ? (int)std::min<int64_t>(3 * AT_MAX_SMS, ((int64_t)a.T * a.Hq + AT_JOIN_WARPS - 1) / AT_JOIN_WARPS) : 0;
     return launch_pdl(attn_join_kernel<D>, dim3(g.row_blocks + g.wide_blocks + a.few_ctas * g.few_split), dim3(AT_JOIN_THREADS), 0, st, a, g);

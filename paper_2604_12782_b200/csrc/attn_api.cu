@@ -195,12 +195,12 @@ osc_status osc_paged_attention(const void* Q, int T, int64_t ldq, int n_q, const
     while ((1 << a.page_shift) < cache->page_size) ++a.page_shift;
     a.scale_log2 = scale * 1.44269504088896341f;
     a.few_hw = hw;
-    a.few_ctas = di.num_sms * 2 < AT_FEW_CTAS ? di.num_sms * 2 : AT_FEW_CTAS;
     a.wide_ctas = di.num_sms < AT_WIDE_CTAS ? di.num_sms : AT_WIDE_CTAS;
     // Up to 16 rows per key/value head a request is one unit of the few-row kernel, whatever the rest of the step is.  The tcgen05
     // kernel is launched where a segment may have more: a shared prefix, or requests with more new tokens than that.
     // (Nor may the 16-row units of a step whose max_new is wrong be too many to count.)
     const bool wide = a.n_pages > 0 && (P > 0 || max_new == 0 || (int64_t)max_new * a.G > AT_FEW_ROWS || most_few >= 2147483648.0);
+    a.few_ctas = std::min(di.num_sms * (wide ? 4 : 2), AT_FEW_CTAS);
     a.wide_min_rows = wide ? AT_FEW_ROWS + 1 : 0x7FFFFFFF;
     if (wide) {
         const int64_t qd[3] = {D, n_q, T}, qs[3] = {1, D, ldq};

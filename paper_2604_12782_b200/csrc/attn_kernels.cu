@@ -29,7 +29,7 @@ constexpr int AT_WIDE_TILE = 128;            // rows of one tcgen05 tile; a wide
 constexpr int AT_WIDE_KEYS = 128;            // keys of its tiles
 constexpr int AT_MERGE_ROWS = 2 * AT_WIDE_TILE;  // a group whose requests all have at least this many rows has no prefix segment
 constexpr int AT_MAX_SMS = 148;
-constexpr int AT_FEW_CTAS = 2 * AT_MAX_SMS;  // most CTAs of the few-row kernel (two per SM)
+constexpr int AT_FEW_CTAS = 4 * AT_MAX_SMS;  // most CTAs of the few-row kernel (two per SM at a time)
 constexpr int AT_FEW_HEADS = 4;              // most key/value heads of a few-row unit
 constexpr int AT_WIDE_CTAS = AT_MAX_SMS;
 
@@ -219,6 +219,21 @@ __device__ __forceinline__ int share_tiles(int N, int ctas, int least) { return 
 // least share: 64 keys of few_hw heads
 __device__ __forceinline__ int few_min_tiles(const AttnArgs& a) { return a.few_hw; }
 constexpr int AT_WIDE_MIN_TILES = 4;
+// Shares of the two lines of a step that has both (nf, nw tiles).  The tcgen05 kernel is bound by arithmetic, the few-row kernel by
+// memory, and both are resident at once: the first gets as many CTAs as its part of the SMs' time, the second runs on the other
+// SMs.  A tcgen05 tile takes an SM about 1.9 us, a few-row tile 0.65 us (256 requests behind 16384 keys: 150 us like this, 170 us with
+// all SMs on one kernel after the other; 66 tcgen05 CTAs 150, 50 181, 84 157).  How long either takes is only known that roughly, so the
+// few-row shares are several rounds of the SMs left over: those that the tcgen05 kernel leaves early take from the last round.
+__device__ __forceinline__ void share_lines(const AttnArgs& a, int nf, int nw, int32_t* share) {
+    const int sms = a.wide_ctas;
+    int wide = sms, few = min(a.few_ctas, 2 * sms);
+    if (nf > 0 && nw > 0) wide = max((int)(sms * (3.0f * nw) / (3.0f * nw + nf) + 0.5f), 1);
+    const int q = share_tiles(nw, wide, AT_WIDE_MIN_TILES);
+    const int left = 2 * (sms - (nw + q - 1) / q);
+    if (nw > 0 && left > 0 && left <= a.few_ctas) few = a.few_ctas / left * left;
+    share[0] = share_tiles(nf, few, few_min_tiles(a));
+    share[1] = q;
+}
 
 // Where a cursor finds segments and their first tiles: what the plan kernel left in the workspace, or (SELF) shared memory.
 template <bool SELF>
@@ -461,8 +476,7 @@ __global__ void __launch_bounds__(1024) attn_plan_kernel(const AttnArgs a) {
         a.plan.share[2] = two;
         a.plan.few_start[S] = carry[0];
         a.plan.wide_start[S] = carry[1];
-        a.plan.share[0] = share_tiles(carry[0], a.few_ctas, few_min_tiles(a));
-        a.plan.share[1] = share_tiles(carry[1], a.wide_ctas, AT_WIDE_MIN_TILES);
+        share_lines(a, carry[0], carry[1], a.plan.share);
     }
     if (two)
         for (int t = attn_row(a, a.R) + tid; t < a.T; t += threads) a.plan.tok_req[t] = -1;
@@ -544,7 +558,8 @@ struct FewCfg {
 // take different keys of a head and are joined through shared memory at the end of a unit.  (All warps on one head
 // whatever the head count cost 129 us instead of the figure in the table on 256 requests of ~512 keys: the join, three barriers a unit.)
 // It needs nothing of the tcgen05 kernel that may be launched in front of it, so it begins (`early`) on every SM that has no
-// tcgen05 CTA or whose CTA has ended, and only waits for that kernel before it ends itself: whatever comes behind waits for both.
+// tcgen05 CTA or whose CTA has ended.  Its last CTA alone waits for that kernel before it ends: whatever comes behind waits for both,
+// and no SM is held by CTAs that have nothing left to do (32 requests behind 4096 keys: 43 -> 38 us).
 // Without prefixes and prompts, up to FEW_SELF requests, every CTA lays out the line for itself in shared memory (SELF) and
 // no plan kernel runs: the launch and its two trips through L2 would be a third of the smallest calls.
 // The loads run on over the ends of units.  A page number is fetched one tile ahead of the loads that need it.
@@ -604,7 +619,7 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
     const int x0 = (int)min((int64_t)q * blockIdx.x, (int64_t)N), x1 = (int)min((int64_t)x0 + q, (int64_t)N);
     if (x0 >= x1) {
         if (threadIdx.x == 0) a.plan.cut[0][blockIdx.x].tiles = 0;
-        if (early) grid_dependency_wait();
+        if (early && blockIdx.x == gridDim.x - 1) grid_dependency_wait();
         return;
     }
 
@@ -827,7 +842,7 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
         else if (threadIdx.x == 0) tell_cut(a.plan.cut[0] + blockIdx.x, unit_x0, unit_x1, x0, x1, q, cur.h, cur.u, cur.g);
     }
     cp_async_wait<0>();
-    if (early) grid_dependency_wait();
+    if (early && blockIdx.x == gridDim.x - 1) grid_dependency_wait();
 }
 
 // ------------------------------------------------------------------------------------------------- join
