@@ -667,7 +667,8 @@ static cudaError_t launch_attn_d(const AttnWideArgs& w, bool wide, cudaStream_t 
     g.few_split = wide ? 1 : a.few_hw;
     g.wide_blocks = wide ? a.wide_ctas * g.wide_split : 0;
     g.row_blocks = a.P ? (int)std::min<int64_t>(3 * AT_MAX_SMS, ((int64_t)a.T * a.Hq + AT_JOIN_WARPS - 1) / AT_JOIN_WARPS) : 0;
-    return launch_pdl(attn_join_kernel<D>, dim3(g.row_blocks + g.wide_blocks + a.few_ctas * g.few_split), dim3(AT_JOIN_THREADS), 0, st, a, g);
+    return launch_pdl((int64_t)a.T * a.Hq <= AT_JOIN_FEW_ROWS ? attn_join_kernel<D, 16> : attn_join_kernel<D, 8>,
+                      dim3(g.row_blocks + g.wide_blocks + a.few_ctas * g.few_split), dim3(AT_JOIN_THREADS), 0, st, a, g);
 }
 
 cudaError_t launch_attn(const AttnWideArgs& w, int D, bool wide, cudaStream_t st) {
