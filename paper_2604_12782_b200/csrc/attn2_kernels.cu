@@ -196,11 +196,14 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
             const int x0 = (int)min((int64_t)q * blockIdx.x, (int64_t)N), x1 = (int)min((int64_t)x0 + q, (int64_t)N);
             Cursor<WideUnits> cur;
             const LineSource<false> src = {a.plan.seg, a.plan.wide_start};
-            if (x0 < x1) cur.seek(a, src, S, x0);
-            else if (lane == 0) a.plan.cut[1][blockIdx.x].tiles = 0;
-            int b = 0;
+            if (lane == 0) a.plan.cut[1][blockIdx.x].tiles = 0;
+            int b = 0, x = x0;
             uint32_t ph = 0;
-            for (int x = x0;;) {
+            if (x0 < x1) {
+                cur.seek(a, src, S, x0);
+                if (cur.kt < 0) { x -= cur.kt; cur.kt = 0; }         // in front of the unit's tiles
+            }
+            while (true) {
                 WideUnit w = {};
                 if (x < x1) {
                     w.ka = cur.kt;
@@ -236,7 +239,10 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                 if (x + w.n == x1 && lane == 0)
                     tell_cut(a.plan.cut[1] + blockIdx.x, x - w.ka, x - w.ka + cur.nt, x0, x1, q, cur.h, cur.u, cur.g);
                 x += w.n;
-                if (x < x1) cur.next_unit(a, src, SEG_WIDE);
+                if (x < x1) {
+                    cur.next_unit(a, src, SEG_WIDE);
+                    x += WideUnits::LEAD;
+                }
             }
         } else if (warp == NSW) {
             // --------------------------------------------------------------------------------------- TMA

@@ -173,7 +173,7 @@ osc_status osc_paged_attention(const void* Q, int T, int64_t ldq, int n_q, const
     const int64_t wide_units = few_units / 8 + (int64_t)R + P;
     const int hw = cache->n_heads % 4 == 0 ? 4 : cache->n_heads % 2 == 0 ? 2 : 1;
     const double most_few = (double)few_units * (cache->n_heads / hw) * (std::max(own_keys, front_keys) / (64.0 / hw) + 1.0);
-    const double most_wide = (double)wide_units * cache->n_heads * ((own_keys + front_keys) / 128.0 + 2.0);
+    const double most_wide = (double)wide_units * cache->n_heads * ((own_keys + front_keys) / 128.0 + 2.0 + WideUnits::LEAD);
     const double most_request = ((double)R + P) * (cache->n_heads / hw) * (std::max(own_keys, front_keys) / (64.0 / hw) + 1.0);
     if (own_keys > 0x20000000 || front_keys > 0x20000000)
         return fail(OSC_ERR_SHAPE, "table columns hold %lld / %lld keys, at most 2^29 are supported", (long long)own_keys, (long long)front_keys);

@@ -38,8 +38,8 @@ struct __align__(16) Segment {
     int t0, n;               // first row and number of tokens
     int klen;                // keys: the prefix, or the request's own
     int plen;                // keys of the group's prefix in front of the own keys (merged groups), else 0
-    int tiles;               // key tiles of all units of one head (of one head group on the few-row line)
-    int start;               // its first tile on its line
+    int tiles;               // places of all units of one head (of one head group on the few-row line): key tiles, and LEAD a unit
+    int start;               // its first place on its line
     int group;               // of a request: its group, -1: none (or one with an empty prefix)
     int flags;
 };
@@ -122,6 +122,7 @@ __device__ __forceinline__ int seg_sees(const Segment& g, int i) { return g.flag
 // The two kinds of units.  Few-row: 16 consecutive (token, head) rows of one token list, few_hw heads side by side, tiles
 // of 64 / few_hw keys.  Wide: two tiles of as many whole tokens as fit 128 rows, one head.
 struct FewUnits {
+    static constexpr int LEAD = 0;     // places on the line in front of a unit's tiles
     __device__ static int key_shift(const AttnArgs& a) { return a.few_hw == 4 ? 4 : a.few_hw == 2 ? 5 : 6; }
     __device__ static int heads(const AttnArgs& a) { return a.Hk / a.few_hw; }
     __device__ static int count(const AttnArgs& a, const Segment& g) { return (g.n * a.G + AT_FEW_ROWS - 1) / AT_FEW_ROWS; }
@@ -139,6 +140,7 @@ struct FewUnits {
     }
 };
 struct WideUnits {
+    static constexpr int LEAD = 4;     // a unit costs about that many tiles beside its own: Q, an empty and a filling pipeline, O
     __device__ static constexpr int key_shift(const AttnArgs&) { return 7; }
     __device__ static int heads(const AttnArgs& a) { return a.Hk; }
     __device__ static int tokens(const AttnArgs& a) { return 2 * a.tpt; }
@@ -164,6 +166,8 @@ template <class U>
 __device__ __forceinline__ int unit_tiles(const AttnArgs& a, const Segment& g, int u) {
     return front_tiles<U>(a, g) + ((seg_sees(g, U::last_token(a, g, u)) + (1 << U::key_shift(a)) - 1) >> U::key_shift(a));
 }
+template <class U>
+__device__ __forceinline__ int unit_span(int tiles) { return tiles ? tiles + U::LEAD : 0; }
 // sum over i < n of floor((a i + b) / m), for a, b >= 0 and m > 0, as in Euclid's algorithm
 __device__ __forceinline__ int64_t floor_sum(int64_t n, int64_t m, int64_t a, int64_t b) {
     int64_t sum = 0;
@@ -182,39 +186,46 @@ __device__ __forceinline__ int64_t floor_sum(int64_t n, int64_t m, int64_t a, in
     return sum;
 }
 constexpr int AT_LOOP_UNITS = 64;
-// key tiles of the units before unit u (u <= count) of one head; the host has seen to it that counts of tiles are ints
+// places on the line of the units before unit u (u <= count) of one head; the host has seen to it that they are ints
 template <class U>
-__device__ __forceinline__ int tiles_before(const AttnArgs& a, const Segment& g, int nu, int u) {
+__device__ __forceinline__ int span_before(const AttnArgs& a, const Segment& g, int nu, int u) {
     if (u == 0) return 0;
-    if (!(g.flags & SEG_OWN)) return u * unit_tiles<U>(a, g, 0);
-    int sum = u * front_tiles<U>(a, g);
-    if (g.klen == 0) return sum;
-    if (u == nu) {                       // the last unit may be short
-        --u;
-        sum += (seg_sees(g, U::last_token(a, g, u)) + (1 << U::key_shift(a)) - 1) >> U::key_shift(a);
-    }
-    if (u > 0) {
+    if (!(g.flags & SEG_OWN)) return u * unit_span<U>(unit_tiles<U>(a, g, 0));
+    const int front = front_tiles<U>(a, g);
+    int sum = u * front, some = front ? u : 0;   // tiles, and units that have any
+    if (g.klen > 0) {
+        if (u == nu) {                   // the last unit may be short
+            --u;
+            const int last = (seg_sees(g, U::last_token(a, g, u)) + (1 << U::key_shift(a)) - 1) >> U::key_shift(a);
+            sum += last;
+            if (!front && last) ++some;
+        }
         int64_t A, B, M, u0;
-        U::line(a, g, A, B, M, u0);      // own tiles(i) = floor((A i + B) / M) from unit u0 on, none before it
-        if (u - u0 <= AT_LOOP_UNITS) {   // nearly always: a short loop, where the closed form's 64-bit divisions take longer
+        U::line(a, g, A, B, M, u0);      // own tiles(i) = floor((A i + B) / M) >= 1 from unit u0 on, none before it
+        if (u > u0) {
+            if (!front) some += (int)(u - u0);
+            if (u - u0 <= AT_LOOP_UNITS) {   // nearly always: a short loop, where the closed form's 64-bit divisions take longer
 #pragma unroll 1
-            for (int i = (int)u0; i < u; ++i) sum += unit_tiles<U>(a, g, i) - front_tiles<U>(a, g);
-        } else {
-            sum += (int)floor_sum(u - u0, M, A, B + A * u0);
+                for (int i = (int)u0; i < u; ++i) sum += unit_tiles<U>(a, g, i) - front;
+            } else {
+                sum += (int)floor_sum(u - u0, M, A, B + A * u0);
+            }
         }
     }
-    return sum;
+    return sum + U::LEAD * some;
 }
-// key tiles of all units of one head
+// places of all units of one head
 template <class U>
-__device__ __forceinline__ int head_tiles(const AttnArgs& a, const Segment& g) {
+__device__ __forceinline__ int head_span(const AttnArgs& a, const Segment& g) {
     if (g.n == 0) return 0;
     const int nu = U::count(a, g);
-    return tiles_before<U>(a, g, nu, nu);
+    return span_before<U>(a, g, nu, nu);
 }
 
-// A line of N tiles is cut into shares of q = max(ceil(N / CTAs), least) tiles; CTA c has [c q, (c + 1) q).  A least
-// share, because a piece costs its prologue and a join.
+// A line of N places is cut into shares of q = max(ceil(N / CTAs), least); CTA c has [c q, (c + 1) q).  A least
+// share, because a piece costs its prologue and a join.  On the tcgen05 line every unit has LEAD empty places in front of its tiles, so
+// that a share of many short units is no longer than one of few long ones (prompts of 8001 tokens: shares of 210 tiles in 5 to 12
+// units ended between 360 and 405 us).
 __device__ __forceinline__ int share_tiles(int N, int ctas, int least) { return max((int)(((int64_t)N + ctas - 1) / ctas), least); }
 // least share: 64 keys of few_hw heads
 __device__ __forceinline__ int few_min_tiles(const AttnArgs& a) { return a.few_hw; }
@@ -251,7 +262,7 @@ struct LineSource {
     }
 };
 
-// A position on a line: key tile kt of unit u of head (group) h of segment s.
+// A position on a line: key tile kt of unit u of head (group) h of segment s; after seek, kt < 0 where it lies in front of the unit's tiles.
 template <class U, bool SELF = false>
 struct Cursor {
     int s, h, u, kt, nu, nt;
@@ -275,25 +286,25 @@ struct Cursor {
         y -= h * g.tiles;
         if (!(g.flags & SEG_OWN)) {
             nt = unit_tiles<U>(a, g, 0);
-            u = y / nt;
-            kt = y - u * nt;
+            u = y / unit_span<U>(nt);
+            kt = y - u * unit_span<U>(nt) - U::LEAD;
         } else if (nu <= AT_LOOP_UNITS) {
             u = 0;
             nt = unit_tiles<U>(a, g, 0);
-            while (y >= nt) {
-                y -= nt;
+            while (y >= unit_span<U>(nt)) {
+                y -= unit_span<U>(nt);
                 nt = unit_tiles<U>(a, g, ++u);
             }
-            kt = y;
+            kt = y - U::LEAD;
         } else {
-            int b = 0, e = nu;           // the last unit with at most y tiles before it
+            int b = 0, e = nu;           // the last unit with at most y places before it
             while (e - b > 1) {
                 const int mid = (b + e) >> 1;
-                if (tiles_before<U>(a, g, nu, mid) <= y) b = mid; else e = mid;
+                if (span_before<U>(a, g, nu, mid) <= y) b = mid; else e = mid;
             }
             u = b;
             nt = unit_tiles<U>(a, g, u);
-            kt = y - tiles_before<U>(a, g, nu, u);
+            kt = y - span_before<U>(a, g, nu, u) - U::LEAD;
         }
     }
     // to the first tile of the next unit that has any; the caller knows that one exists
@@ -316,7 +327,7 @@ struct Cursor {
 // first tile of unit u of head h of a segment
 template <class U>
 __device__ __forceinline__ int unit_begin(const AttnArgs& a, const Segment& g, int h, int u) {
-    return g.start + h * g.tiles + tiles_before<U>(a, g, U::count(a, g), u);
+    return g.start + h * g.tiles + span_before<U>(a, g, U::count(a, g), u) + U::LEAD;
 }
 
 __device__ __forceinline__ void tell_cut(CutUnit* c, int unit_x0, int unit_x1, int x0, int x1, int q, int h, int u,
@@ -450,10 +461,10 @@ __global__ void __launch_bounds__(1024) attn_plan_kernel(const AttnArgs a) {
             }
             if (g.n * a.G >= a.wide_min_rows) {
                 g.flags |= SEG_WIDE;
-                g.tiles = head_tiles<WideUnits>(a, g);
+                g.tiles = head_span<WideUnits>(a, g);
                 own[1] = g.tiles * WideUnits::heads(a);
             } else {
-                g.tiles = head_tiles<FewUnits>(a, g);
+                g.tiles = head_span<FewUnits>(a, g);
                 own[0] = g.tiles * FewUnits::heads(a);
             }
         }
@@ -594,7 +605,7 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
                 g.t0 = attn_row(a, s);
                 g.n = max(attn_row(a, s + 1) - g.t0, 0);
                 g.klen = attn_keys(a.kv_len[s], a.cols, a.page_shift);
-                g.tiles = head_tiles<FewUnits>(a, g);
+                g.tiles = head_span<FewUnits>(a, g);
                 own = g.tiles * FewUnits::heads(a);
                 inc[0] = own;
                 seg[s] = g;

@@ -283,3 +283,11 @@ def test_two_streams_at_once(B):
     torch.cuda.synchronize()
     for c, (o, lse, _) in zip(cases, bufs):
         c.check(o, lse, "two streams")
+
+
+@pytest.mark.parametrize("kv", [50, 300, 700])
+def test_many_units(B, kv):
+    """More row units in one request than the line is laid out for in a loop: some without keys, some short, some behind a prefix."""
+    go(B, seed=28, Hk=1, G=64, D=64, page=16, new=[300, 1], kv=[kv, 40])
+    go(B, seed=29, Hk=1, G=128, D=64, page=16, new=[150, 150], kv=[kv, 160], prefix=[130])
+    go(B, seed=30, Hk=2, G=8, D=64, page=16, new=[200, 3], kv=[kv, 40], max_new=1)
