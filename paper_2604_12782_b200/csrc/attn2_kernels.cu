@@ -537,71 +537,103 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                 c1 *= inv;
             }
             const int slot0 = AT_FEW_SLOTS + (blockIdx.x * 2 + (out & OUT_LATER ? 1 : 0)) * (2 * AT_WIDE_TILE) + (pair ? s * AT_WIDE_TILE : 0);
-            // row of the partial results (or of lse) that tile row x goes to, -1: none
-            auto place = [&](int x) -> int {
+            // token and head of tile row x; whether there is one
+            auto row_of = [&](int x, int& tok, int& hq) -> bool {
                 const int t = x * a.inv_g >> 16;
-                if (t >= tpt || tok0 + t >= tokens) return -1;
-                if (out & OUT_SPLIT) return slot0 + x;
-                const int row = (row0 + tok0 + t) * a.Hq + hq0 + x - t * a.G;
-                return direct ? row : dense_row(a, out & OUT_OWN ? 1 : 0, row);
+                tok = row0 + tok0 + t;
+                hq = hq0 + x - t * a.G;
+                return t < tpt && tok0 + t < tokens;
             };
+            // its row of the partial results
+            auto part_row = [&](int x, int tok, int hq) -> int { return out & OUT_SPLIT ? slot0 + x : dense_row(a, out & OUT_OWN ? 1 : 0, tok * a.Hq + hq); };
             if (pair || s == 0) {
-                const int at = place(r);
-                if (at >= 0) {
-                    if (!direct) a.ml[at] = make_float2(m, l);
-                    else if (a.lse) a.lse[at] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+                int tok, hq;
+                if (row_of(r, tok, hq)) {
+                    if (!direct) a.ml[part_row(r, tok, hq)] = make_float2(m, l);
+                    else if (a.lse) a.lse[tok * a.Hq + hq] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
                 }
             }
             // A thread holds a row; through shared memory (16-byte units swizzled by the row) four lanes write 64 bytes of one row side by side,
-            // eight rows at a time.  (Written by the rows' own threads, 16 bytes of 32 rows in one store, a unit took 7000 to 10000
-            // cycles to get out.)  The loop is kept rolled: code that runs once comes out of L2 line by line, slower than the data.
+            // eight rows at a time: 32 channels in bf16, or 16 of a partial result.  (Written by the rows' own threads, 16 bytes of 32 rows in one
+            // store, a unit took 7000 to 10000 cycles to get out; 16 channels at a time for bf16 too, and with two divisions a row, 8200.)
             int64_t to[4];
 #pragma unroll
             for (int y = 0; y < 4; ++y) {
-                const int at = place((warp & 3) * 32 + y * 8 + lane / 4);
-                to[y] = at < 0 ? -1 : direct ? (int64_t)(at / a.Hq) * a.ldo + (int64_t)(at % a.Hq) * D : (int64_t)at * D;
+                const int x = (warp & 3) * 32 + y * 8 + lane / 4;
+                int tok, hq;
+                to[y] = !row_of(x, tok, hq) ? -1 : direct ? tok * a.ldo + hq * D : (int64_t)part_row(x, tok, hq) * D;
             }
             uint8_t* tile = out_tiles + warp * 2048;
             const int cols = pair ? D : D / 2, col0 = pair ? 0 : s * cols;
             const int e = lane & 3, wsw = (lane >> 1) & 3, rsw = (lane >> 3) & 3;
+            if (direct) {
 #pragma unroll 1
-            for (int c = col0; c < col0 + cols; c += 16) {
-                float o[16];
+                for (int c = col0; c < col0 + cols; c += 32) {
+                    uint32_t x[32], pk[16];
 #pragma unroll
-                for (int y = 0; y < 16; ++y) o[y] = 0.0f;
-                uint32_t x[16];
-                if (have) {
-                    tmem_ld_x16(t_o + first * D + c, x);
-                    tmem_ld_wait();
-                    if (c0 != 0.0f) {
-#pragma unroll
-                        for (int y = 0; y < 16; ++y) o[y] = __uint_as_float(x[y]) * c0;
+                    for (int y = 0; y < 32; ++y) x[y] = 0u;
+                    if (have) {
+                        tmem_ld_32x32(t_o + first * D + c, x);
+                        tmem_ld_wait();
                     }
-                }
-                if (joined) {
-                    tmem_ld_x16(t_o + D + c, x);
-                    tmem_ld_wait();
-                    if (c1 != 0.0f) {
+                    float o[32];
 #pragma unroll
-                        for (int y = 0; y < 16; ++y) o[y] = fmaf(__uint_as_float(x[y]), c1, o[y]);
+                    for (int y = 0; y < 32; ++y) o[y] = c0 != 0.0f ? __uint_as_float(x[y]) * c0 : 0.0f;
+                    if (joined) {
+                        tmem_ld_32x32(t_o + D + c, x);
+                        tmem_ld_wait();
+                        if (c1 != 0.0f) {
+#pragma unroll
+                            for (int y = 0; y < 32; ++y) o[y] = fmaf(__uint_as_float(x[y]), c1, o[y]);
+                        }
                     }
-                }
 #pragma unroll
-                for (int y = 0; y < 4; ++y)
-                    *reinterpret_cast<float4*>(tile + lane * 64 + ((y ^ wsw) * 16)) = make_float4(o[4 * y], o[4 * y + 1], o[4 * y + 2], o[4 * y + 3]);
-                __syncwarp();
+                    for (int y = 0; y < 16; ++y) pk[y] = bf162_bits(__floats2bfloat162_rn(o[2 * y], o[2 * y + 1]));
 #pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    const float4 q = *reinterpret_cast<const float4*>(tile + (y * 8 + lane / 4) * 64 + ((e ^ rsw) * 16));
-                    if (to[y] >= 0) {
-                        if (direct)
-                            *reinterpret_cast<uint2*>(a.o + to[y] + c + e * 4) =
-                                make_uint2(bf162_bits(__floats2bfloat162_rn(q.x, q.y)), bf162_bits(__floats2bfloat162_rn(q.z, q.w)));
-                        else
-                            *reinterpret_cast<float4*>(a.part + to[y] + c + e * 4) = q;
+                    for (int y = 0; y < 4; ++y)
+                        *reinterpret_cast<uint4*>(tile + lane * 64 + ((y ^ wsw) * 16)) = make_uint4(pk[4 * y], pk[4 * y + 1], pk[4 * y + 2], pk[4 * y + 3]);
+                    __syncwarp();
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) {
+                        const uint4 q = *reinterpret_cast<const uint4*>(tile + (y * 8 + lane / 4) * 64 + ((e ^ rsw) * 16));
+                        if (to[y] >= 0) *reinterpret_cast<uint4*>(a.o + to[y] + c + e * 8) = q;
                     }
+                    __syncwarp();
                 }
-                __syncwarp();
+            } else {
+#pragma unroll 1
+                for (int c = col0; c < col0 + cols; c += 16) {
+                    float o[16];
+#pragma unroll
+                    for (int y = 0; y < 16; ++y) o[y] = 0.0f;
+                    uint32_t x[16];
+                    if (have) {
+                        tmem_ld_x16(t_o + first * D + c, x);
+                        tmem_ld_wait();
+                        if (c0 != 0.0f) {
+#pragma unroll
+                            for (int y = 0; y < 16; ++y) o[y] = __uint_as_float(x[y]) * c0;
+                        }
+                    }
+                    if (joined) {
+                        tmem_ld_x16(t_o + D + c, x);
+                        tmem_ld_wait();
+                        if (c1 != 0.0f) {
+#pragma unroll
+                            for (int y = 0; y < 16; ++y) o[y] = fmaf(__uint_as_float(x[y]), c1, o[y]);
+                        }
+                    }
+#pragma unroll
+                    for (int y = 0; y < 4; ++y)
+                        *reinterpret_cast<float4*>(tile + lane * 64 + ((y ^ wsw) * 16)) = make_float4(o[4 * y], o[4 * y + 1], o[4 * y + 2], o[4 * y + 3]);
+                    __syncwarp();
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) {
+                        const float4 q = *reinterpret_cast<const float4*>(tile + (y * 8 + lane / 4) * 64 + ((e ^ rsw) * 16));
+                        if (to[y] >= 0) *reinterpret_cast<float4*>(a.part + to[y] + c + e * 4) = q;
+                    }
+                    __syncwarp();
+                }
             }
             tc_fence_before();
             __syncwarp();
