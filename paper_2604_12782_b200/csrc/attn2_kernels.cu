@@ -125,7 +125,6 @@ struct __align__(16) WideUnit {
 constexpr int OUT_SPLIT = 1, OUT_TWO = 2, OUT_OWN = 4, OUT_LATER = 8;   // OUT_LATER: the share has tiles before this unit
 
 __device__ __forceinline__ int unit_tile(const WideUnit& w, int s, int i) { return w.pair ? w.ka + i : w.ka + 2 * i + s; }
-__device__ __forceinline__ int unit_load(const WideUnit& w, int s, int i) { return w.pair ? i : 2 * i + s; }   // which of the unit's K (or V) loads
 // keys of key tile kt before any mask
 __device__ __forceinline__ int unit_left(const WideUnit& w, int kt) {
     return kt < w.nf ? w.plen - kt * AT_WIDE_KEYS : w.klen - (kt - w.nf) * AT_WIDE_KEYS;
@@ -508,22 +507,27 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                 if (!wait_bounded(&pv_done[s], pv_ph, abort_flag, 71)) goto done;
                 pv_ph ^= 1u;
             }
-            float2* ml = unit_ml + (e_ph & 1) * 256;
-            ml[s * 128 + r] = make_float2(m, l);
-            __syncwarp();
-            if (lane == 0) mbar_arrive(e_full);
-            if (!wait_bounded(e_full, e_ph & 1, abort_flag, 83)) goto done;
-            e_ph ^= 1u;
-            tc_fence_after();
             // both row tiles filled: a stream's own rows; else the two warpgroups share out the columns of the one tile, O being the two
             // streams' joined
             const int first = pair ? s : 0;
             const bool joined = !pair && have1, have = first ? have1 : have0;
-            m = ml[first * 128 + r].x;
-            l = ml[first * 128 + r].y;
+            float m1 = -INFINITY, l1 = 0.0f;
+            if (!pair) {
+                float2* ml = unit_ml + (e_ph & 1) * 256;
+                ml[s * 128 + r] = make_float2(m, l);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(e_full);
+                if (!wait_bounded(e_full, e_ph & 1, abort_flag, 83)) goto done;
+                e_ph ^= 1u;
+                m = ml[r].x;
+                l = ml[r].y;
+                m1 = ml[128 + r].x;
+                l1 = ml[128 + r].y;
+            }
+            tc_fence_after();
             float c0 = m == -INFINITY ? 0.0f : 1.0f, c1 = 0.0f;
             if (joined) {
-                const float m1 = ml[128 + r].x, l1 = ml[128 + r].y, mn = fmaxf(m, m1);
+                const float mn = fmaxf(m, m1);
                 c0 = mn == -INFINITY ? 0.0f : exp2_approx(m - mn);
                 c1 = mn == -INFINITY ? 0.0f : exp2_approx(m1 - mn);
                 m = mn;
