@@ -58,7 +58,7 @@ struct WideCfg {
     static constexpr int HALF_BYTES = AT_WIDE_KEYS * 128;        // 128 keys of 64 channels
     static constexpr int TILE_BYTES = HALVES * HALF_BYTES;
     static constexpr int STAGES = D == 128 ? 2 : 4;              // K tiles, and as many V tiles
-    static constexpr int OUT_BYTES = AW_SOFTMAX_WARPS * 2048;    // every softmax warp's 32 rows x 16 columns of O on the way out
+    static constexpr int OUT_BYTES = AW_SOFTMAX_WARPS * 2048;    // every softmax warp's 32 rows x 64 bytes of O on the way out
     static constexpr int ROW_FLOATS = 2 * 2 * 2 * 128;           // [parity][stream][128] maxima and sums of a unit
     static constexpr int BAR_BYTES = 320;
     static constexpr int SMEM = 2 * QTILE_BYTES + 2 * STAGES * TILE_BYTES + OUT_BYTES + ROW_FLOATS * 4 + BAR_BYTES + 2 * 64 + 1024;
@@ -124,7 +124,6 @@ struct __align__(16) WideUnit {
 };
 constexpr int OUT_SPLIT = 1, OUT_TWO = 2, OUT_OWN = 4, OUT_LATER = 8;   // OUT_LATER: the share has tiles before this unit
 
-__device__ __forceinline__ int unit_tile(const WideUnit& w, int s, int i) { return w.pair ? w.ka + i : w.ka + 2 * i + s; }
 // keys of key tile kt before any mask
 __device__ __forceinline__ int unit_left(const WideUnit& w, int kt) {
     return kt < w.nf ? w.plen - kt * AT_WIDE_KEYS : w.klen - (kt - w.nf) * AT_WIDE_KEYS;
