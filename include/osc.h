@@ -570,8 +570,8 @@ osc_status osc_kv_slots(const int32_t* cached, const int32_t* fresh, const int32
                         const int32_t* free_pages, int n_free, int32_t* table, int cols, int64_t ld_table, int T,
                         int32_t* row_off, int32_t* kv_len, int32_t* slots, int32_t* positions, int32_t* taken, void* stream);
 
-/* Rotation by position.  Pair i of rot_dim / 2 turns by positions[axis[i]][t] * inv_freq[i] (the product is exact, also for
- * far positions); its channels are (i, i + rot_dim / 2), or (2i, 2i + 1) when interleaved; channels from rot_dim on are
+/* Rotation by position.  Pair i of rot_dim / 2 turns by positions[axis[i]][t] * inv_freq[i] (in double: exact for positions
+ * below 2^29); its channels are (i, i + rot_dim / 2), or (2i, 2i + 1) when interleaved; channels from rot_dim on are
  * not turned.  axes = 1: one position per token; 2 or 3: image and video positions (time, height, width), axis[i]
  * (dev uint8 [rot_dim / 2], null = all 0) says by which of them pair i turns.  inv_freq: dev float [rot_dim / 2].  scale
  * multiplies the turned channels (1 where the model has no such factor).  rot_dim: a multiple of 16, <= head_dim. */
@@ -588,7 +588,8 @@ typedef struct {
  * to the tokens' slots of the cache.
  *   positions: dev int32 [axes][ld_pos];  slots: dev int32 [T], or null: token t at slot t.
  * Tokens with a slot outside 0 .. n_pages * page_size - 1 write nothing to the cache.  Two tokens must not share a
- * slot.  Arithmetic in fp32, angles in double.  T == 0 is a no-op. */
+ * slot.  Arithmetic in fp32 (so a head whose sum of squares passes its range, |x| from about 10^18 on, gives zeros where there is
+ * a norm), angles in double.  T == 0 is a no-op. */
 osc_status osc_qk_norm_rope(const void* QKV, int T, int64_t ld, int n_q, const osc_kv_cache_t* cache, const void* gamma_q,
                             const void* gamma_k, float eps, const osc_rope_t* rope, const int32_t* positions, int64_t ld_pos,
                             const int32_t* slots, void* Q, int64_t ldq, void* stream);

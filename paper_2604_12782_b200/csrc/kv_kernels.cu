@@ -118,7 +118,7 @@ __global__ void __launch_bounds__(KS_THREADS) kv_slots_kernel(const KvSlotsArgs 
         __syncthreads();   // the shared arrays are filled again for the next chunk
     }
     // rows that only fill the step up have no slot: whatever writes the cache leaves them out
-    for (int t = max((int)(unsigned)carry, 0) + blockIdx.x * KS_THREADS + tid; t < a.T; t += gridDim.x * KS_THREADS) {
+    for (int t = max((int)(unsigned)carry, 0) + blockIdx.x * KS_THREADS + tid; t >= 0 && t < a.T; t += gridDim.x * KS_THREADS) {
         a.slots[t] = -1;
         a.positions[t] = 0;
     }
@@ -140,7 +140,7 @@ cudaError_t launch_kv_slots(const KvSlotsArgs& a, int num_sms, cudaStream_t st) 
 // ------------------------------------------------------------------------------------------ qk_norm_rope
 // Per token t and head h of the queries and keys, with one rounding to bf16 at the end:
 //   y     = x * rsqrt(mean(x^2) + eps) * gamma                       (fp32; left out where gamma is null)
-//   a_i   = position[axis_i][t] * inv_freq_i                         (exact in double)
+//   a_i   = position[axis_i][t] * inv_freq_i                         (in double)
 //   (y_i, y_i') -> scale * (y_i cos a_i - y_i' sin a_i, y_i' cos a_i + y_i sin a_i)
 // with i' = i + rot/2 (halves) or the pair (2i, 2i+1) (interleaved); channels from rot on are not turned.  Values
 // are copied.  Queries go to Q, keys and values to the token's slot of the cache.
