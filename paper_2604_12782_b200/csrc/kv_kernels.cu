@@ -181,6 +181,7 @@ struct QkNormRopeArgs {
     const int32_t* slots;      // null: token t at slot t
     float eps, scale;
     int T, Hq, Hk, rot, axes, page, n_pages;
+    int whole;               // tokens with one warp each; those behind them have warps_per_token
     int warps_per_token;
 };
 
@@ -198,11 +199,15 @@ __global__ void __launch_bounds__(QR_WARPS * 32, MODE == ROPE_SPLIT ? QR_CTAS : 
     const int sub = lane / LPH, hl = lane % LPH;
     const int nq = (a.Hq + HPS - 1) / HPS, nk = (a.Hk + HPS - 1) / HPS;
     const int steps = nq + 2 * nk;
-    const uint32_t job = blockIdx.x * QR_WARPS + warp;      // the host has seen to T * warps_per_token < 2^31
-    const int t = (int)(job / (uint32_t)a.warps_per_token), part = (int)(job - (uint32_t)t * a.warps_per_token);
+    const uint32_t job = blockIdx.x * QR_WARPS + warp;      // fewer than 2^31 + QR_WARPS
+    const bool shared = job >= (uint32_t)a.whole;
+    const uint32_t rest = job - a.whole, w_t = rest / (uint32_t)a.warps_per_token;
+    const uint32_t t_u = shared ? a.whole + w_t : job;
+    const int part = shared ? (int)(rest - w_t * a.warps_per_token) : 0, parts = shared ? a.warps_per_token : 1;
     grid_dependency_wait();
-    if (t >= a.T) return;
-    const int st0 = steps * part / a.warps_per_token, st1 = steps * (part + 1) / a.warps_per_token;
+    if (t_u >= (uint32_t)a.T) return;
+    const int t = (int)t_u;
+    const int st0 = steps * part / parts, st1 = steps * (part + 1) / parts;
     const uint16_t* row = a.qkv + (int64_t)t * a.ld;
     // first channel of the lane's two groups of four
     const int e0 = MODE == ROPE_SPLIT ? 4 * hl : 8 * hl;
@@ -384,12 +389,15 @@ template <int D, int MODE>
 static cudaError_t launch_qk_norm_rope_mode(QkNormRopeArgs a, int num_sms, cudaStream_t st) {
     const int hps = 32 / (D / 8);
     const int steps = (a.Hq + hps - 1) / hps + 2 * ((a.Hk + hps - 1) / hps);
-    // A warp per token once that fills half of the machine's resident warps; below it, a token's steps are spread over as many as fit.
-    // More is worse, every warp works out the angles again: 8192 tokens in 1 / 2 / 4 / 8 warps each 39.4 / 37.0 / 46.4 / 66.5 us,
-    // 5001 tokens 27.8 / 29.9 / 35.8 / 46.8, 256 tokens 10.4 / 6.3 / 6.3 / 6.3.
-    const int64_t resident = (int64_t)num_sms * QR_WARPS * QR_CTAS;
-    a.warps_per_token = (int)std::max<int64_t>(1, std::min<int64_t>(resident / 2 / a.T, std::min(steps, 32)));
-    const int64_t jobs = (int64_t)a.T * a.warps_per_token;
+    // A warp per token for as many rounds of the machine's resident warps as are full.  The tokens behind them (all, where there are few) are spread
+    // over more warps while those fill half of the machine: the last round is then as short as its work (5001 tokens, 1.06 rounds: 23.4 us,
+    // 27.0 with a warp per token).  More is worse, every warp works out the angles again: 8192 tokens in 1 / 2 / 4 / 8 warps each
+    // 39.4 / 37.0 / 46.4 / 66.5 us, 5001 tokens 27.8 / 29.9 / 35.8 / 46.8, 256 tokens 10.4 / 6.3 / 6.3 / 6.3.
+    const int resident = num_sms * QR_WARPS * (MODE == ROPE_SPLIT ? QR_CTAS : QR_CTAS - 2);
+    a.whole = a.T / resident * resident;
+    const int rest = a.T - a.whole;
+    a.warps_per_token = rest ? std::max(1, std::min(resident / 2 / rest, std::min(steps, 32))) : 1;
+    const int64_t jobs = (int64_t)a.whole + (int64_t)rest * a.warps_per_token;
     return launch_pdl(qk_norm_rope_kernel<D, MODE>, dim3((unsigned)((jobs + QR_WARPS - 1) / QR_WARPS)), dim3(QR_WARPS * 32), 0, st, a);
 }
 

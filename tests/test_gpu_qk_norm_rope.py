@@ -133,3 +133,10 @@ def test_no_tokens_and_zero_rows(B):
     assert (k == 7).all() and (q == 7).all()
     B.osc_qk_norm_rope(x, 4, B.KvCache(k, v), q, pos, rope, gamma_q=g, gamma_k=g)      # x = 0: the norm's eps keeps it 0
     assert (q == 0).all() and (k[0, :3] == 0).all() and (k[0, 3:] == 7).all() and (k[1] == 7).all()
+
+
+@pytest.mark.parametrize("T,inter", [(4735, False), (4736, False), (4741, False), (9473, False), (3600, True), (7104, True)])
+def test_more_tokens_than_warps(B, T, inter):
+    """About the numbers of tokens (warps on 148 SMs) behind which the rest is spread over several warps a token."""
+    run_case(B, T, T, 3, 1, 64, 64, inter=inter)
+    run_case(B, T + 1, T, 1, 1, 128, 128 if inter else 48, inter=inter)
