@@ -187,7 +187,8 @@ osc_status osc_paged_attention(const void* Q, int T, int64_t ldq, int n_q, const
     AttnWideArgs w = {};
     AttnArgs& a = w.a;
     a.q = static_cast<const uint16_t*>(Q); a.ldq = ldq; a.o = static_cast<uint16_t*>(O); a.ldo = ldo; a.lse = lse;
-    a.k = static_cast<const uint16_t*>(cache->k); a.v = static_cast<const uint16_t*>(cache->v);
+    // copies of absent pages read nothing, but are given an address: that of Q where there is no cache
+    a.k = static_cast<const uint16_t*>(cache->n_pages ? cache->k : Q); a.v = static_cast<const uint16_t*>(cache->n_pages ? cache->v : Q);
     a.page_stride = cache->page_stride; a.token_stride = cache->token_stride; a.head_stride = cache->head_stride;
     a.row_off = row_off; a.kv_len = kv_len; a.table = table; a.ld_table = ld_table; a.cols = cols;
     a.group_off = group_off; a.prefix_len = prefix_len; a.ptable = prefix_table; a.ld_ptable = ld_prefix; a.pcols = P ? prefix_cols : 0;

@@ -291,3 +291,41 @@ def test_many_units(B, kv):
     go(B, seed=28, Hk=1, G=64, D=64, page=16, new=[300, 1], kv=[kv, 40])
     go(B, seed=29, Hk=1, G=128, D=64, page=16, new=[150, 150], kv=[kv, 160], prefix=[130])
     go(B, seed=30, Hk=2, G=8, D=64, page=16, new=[200, 3], kv=[kv, 40], max_new=1)
+
+
+def test_a_cache_without_pages(B):
+    """Every table entry is outside the cache: keys and values of 0, so a row that sees any key gives 0 and ln(number of keys)."""
+    for new, kv, P in (([1, 1], [5, 70], 0), ([1, 40], [5, 70], 1), ([3], [0], 0)):
+        T, R, Hq, D = sum(new), len(new), 8, 128
+        q = torch.randn(T, Hq * D, device="cuda").to(torch.bfloat16)
+        k = torch.empty(0, 16, 2, D, dtype=torch.bfloat16, device="cuda")
+        i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")     # noqa: E731
+        o, lse = torch.full((T, Hq * D), 7.0, dtype=torch.bfloat16, device="cuda"), torch.full((T, Hq), 7.0, device="cuda")
+        ws = torch.zeros(B.osc_paged_attention_workspace_bytes(T, Hq, D, R, P), dtype=torch.uint8, device="cuda")
+        rows = np.concatenate([[0], np.cumsum(new)])
+        B.osc_paged_attention(q, B.KvCache(k, k.clone()), i32(rows.tolist()), i32(kv), torch.zeros(R, 8, dtype=torch.int32, device="cuda"), o, ws, 0.1, lse=lse,
+                              group_off=i32([0, R]) if P else None, prefix_len=i32([30]) if P else None,
+                              prefix_table=torch.zeros(1, 2, dtype=torch.int32, device="cuda") if P else None)
+        B.osc_sync_check()
+        assert (o == 0).all()
+        sees = np.concatenate([np.maximum(m - n + np.arange(n) + 1, 0) for n, m in zip(new, kv)]) + 30 * P
+        with np.errstate(divide="ignore"):
+            want = np.log(sees)
+        got = lse.cpu().numpy().astype(np.float64)
+        # ex2, lg2 and the sums are off by a few 2^-22 of ln(n) + 1
+        assert (np.abs(np.where(sees[:, None] > 0, got - np.where(sees > 0, want, 0)[:, None], 0)) <= 2.0 ** -18 * 6).all()
+        assert (got[sees == 0] == -np.inf).all()
+
+
+@pytest.mark.parametrize("page", [512, 4096])
+def test_large_pages_and_tables_with_a_stride(B, page):
+    c = AttnCase(31, 2, 4, 128, page, [1, 60, 1], [700, 1300, 9], prefix=[600, 20], groups=[0, 2, 3])
+    wide = torch.full((3, c.table.shape[1] + 5), 2 ** 31 - 1, dtype=torch.int32, device="cuda")
+    wide[:, :c.table.shape[1]] = c.table
+    c.table = wide[:, :c.table.shape[1]]
+    pwide = torch.full((2, c.ptable.shape[1] + 3), -2 ** 31, dtype=torch.int32, device="cuda")
+    pwide[:, :c.ptable.shape[1]] = c.ptable
+    c.ptable = pwide[:, :c.ptable.shape[1]]
+    o, lse = c.run(B)
+    B.osc_sync_check()
+    c.check(o, lse, f"pages of {page}")
