@@ -565,7 +565,7 @@ typedef struct {
  *   taken:   int32 [1]: pages taken.  More than n_free: the list ran out; table entries past it and the slots of
  *            their tokens are -1.  Slots of tokens whose page lies past cols, or whose table entry is negative, are -1 too.
  * More than T tokens: only the first T get slots and positions.  A second call with the same inputs gives the same
- * outputs.  Negative lengths count as 0. */
+ * outputs.  Negative lengths count as 0.  What is written (table included) must not overlap anything else (OSC_ERR_INVALID_ARG). */
 osc_status osc_kv_slots(const int32_t* cached, const int32_t* fresh, const int32_t* base, int R, int page_size,
                         const int32_t* free_pages, int n_free, int32_t* table, int cols, int64_t ld_table, int T,
                         int32_t* row_off, int32_t* kv_len, int32_t* slots, int32_t* positions, int32_t* taken, void* stream);
@@ -584,7 +584,7 @@ typedef struct {
 
 /* QKV [T, (n_q + 2 n_kv) * head_dim] (the QKV projection's output: query heads, key heads, value heads; n_kv and head_dim
  * from the cache) in one pass: RMSNorm of every query and key head (gamma_q / gamma_k: dev bf16 [head_dim]; null = no
- * norm), rotation, one rounding to bf16; queries to Q (dev bf16 [T, ldq]; may be QKV itself), keys and values (copied)
+ * norm), rotation, one rounding to bf16; queries to Q (dev bf16 [T, ldq]; may be QKV itself, with ldq = ld), keys and values (copied)
  * to the tokens' slots of the cache.
  *   positions: dev int32 [axes][ld_pos];  slots: dev int32 [T], or null: token t at slot t.
  * Tokens with a slot outside 0 .. n_pages * page_size - 1 write nothing to the cache.  Two tokens must not share a
@@ -602,6 +602,7 @@ osc_status osc_qk_norm_rope(const void* QKV, int T, int64_t ld, int n_q, const o
  * once for the whole group.  Groups are in order and do not overlap; a request may be in none.
  *   O = softmax(scale * Q K^T) V per head, dev bf16 [T, ldo]; lse (dev float [T][n_q], or null): natural logarithm of the
  *   sum of exp(scale * q . k).  A row without any key gives 0 and -inf.  Rows from row_off[R] on are left as they are.
+ * O must not overlap Q.
  * Sums and the running maximum in fp32, weights in bf16.  page_size: a power of two of at least 16.  Lengths are read on
  * the device: kv_len and prefix_len are cut to what the table's columns hold, a table entry outside 0 .. n_pages - 1 reads as a
  * page of zeros, and nothing behind a length is used, whatever the cache holds there (NaN too).  A key that is masked for a row only by

@@ -817,7 +817,7 @@ def osc_rmsnorm_linear_swiglu_grouped_gather(w: OscWeights, Hin: torch.Tensor, g
 
 # Lengths, tables and slots are read on the device, where a tensor of another type or on another device would go unnoticed, so the calls
 # below look at every tensor.  They run once per step or layer in front of kernels of a few microseconds: the look is one pass with three
-# attribute reads a tensor, and only a refusal works out what was wrong.
+# attribute reads a tensor, and only a refusal works out what was wrong.  (t.stride()[0]: half the time of t.stride(0).)
 def _device_of(t):
     """Device of a call: that of its first tensor, which has to be the current one; -1 otherwise."""
     d = t.get_device()
@@ -849,7 +849,7 @@ def _bad(dtype, dev, *tensors):
 def _bad_rows(dtype, dev, *tensors):
     """The same for matrices whose rows may be further apart than they are long."""
     for t in tensors:
-        if t is not None and (t.dtype is not dtype or t.get_device() != dev or t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1)):
+        if t is not None and (t.dtype is not dtype or t.get_device() != dev or t.dim() != 2 or (t.stride()[1] != 1 and t.shape[1] > 1)):
             return True
     return dev < 0
 
@@ -900,7 +900,7 @@ def osc_kv_slots(cached, fresh, base, page_size: int, free_pages, table, row_off
             (base is not None and base.numel() != R)):
         raise ValueError("osc_kv_slots: lengths do not belong together")
     _check(_lib.osc_kv_slots(cached.data_ptr(), fresh.data_ptr(), _addr(base), R, page_size, free_pages.data_ptr(), free_pages.numel(),
-                             table.data_ptr(), cols, table.stride(0), T, row_off.data_ptr(), kv_len.data_ptr(), slots.data_ptr(),
+                             table.data_ptr(), cols, table.stride()[0], T, row_off.data_ptr(), kv_len.data_ptr(), slots.data_ptr(),
                              positions.data_ptr(), taken.data_ptr(), _stream(stream)))
 
 
@@ -926,9 +926,9 @@ def osc_qk_norm_rope(QKV: torch.Tensor, n_q: int, cache: KvCache, Q: torch.Tenso
             width != (n_q + 2 * cache.n_heads) * cache.head_dim or qw < n_q * cache.head_dim or
             (gamma_q is not None and gamma_q.numel() != cache.head_dim) or (gamma_k is not None and gamma_k.numel() != cache.head_dim)):
         raise ValueError("osc_qk_norm_rope: shapes do not belong together")
-    _check(_lib.osc_qk_norm_rope(QKV.data_ptr(), T, QKV.stride(0) if T > 1 else width, n_q, cache.c, _addr(gamma_q), _addr(gamma_k), eps,
-                                 rope.c[axes], positions.data_ptr(), positions.stride(0) if axes > 1 else T, _addr(slots), Q.data_ptr(),
-                                 Q.stride(0) if T > 1 else qw, _stream(stream)))
+    _check(_lib.osc_qk_norm_rope(QKV.data_ptr(), T, QKV.stride()[0] if T > 1 else width, n_q, cache.c, _addr(gamma_q), _addr(gamma_k), eps,
+                                 rope.c[axes], positions.data_ptr(), positions.stride()[0] if axes > 1 else T, _addr(slots), Q.data_ptr(),
+                                 Q.stride()[0] if T > 1 else qw, _stream(stream)))
 
 
 def osc_paged_attention_workspace_bytes(T: int, n_q: int, head_dim: int, R: int, P: int = 0) -> int:
@@ -957,13 +957,13 @@ def osc_paged_attention(Q: torch.Tensor, cache: KvCache, row_off, kv_len, table,
             (P and (group_off is None or prefix_table is None or group_off.numel() < P + 1 or prefix_table.shape[0] < P)) or
             (lse is not None and lse.numel() != T * n_q)):
         raise ValueError("osc_paged_attention: shapes do not belong together")
-    ldq, ldo = (Q.stride(0), O.stride(0)) if T > 1 else (width, width)
+    ldq, ldo = (Q.stride()[0], O.stride()[0]) if T > 1 else (width, width)
     if P:
         _check(_lib.osc_paged_attention(Q.data_ptr(), T, ldq, n_q, cache.c, R, row_off.data_ptr(), kv_len.data_ptr(), table.data_ptr(), cols,
-                                        table.stride(0), P, group_off.data_ptr(), prefix_len.data_ptr(), prefix_table.data_ptr(),
-                                        prefix_table.shape[1], prefix_table.stride(0), max_new, scale, O.data_ptr(), ldo, _addr(lse),
+                                        table.stride()[0], P, group_off.data_ptr(), prefix_len.data_ptr(), prefix_table.data_ptr(),
+                                        prefix_table.shape[1], prefix_table.stride()[0], max_new, scale, O.data_ptr(), ldo, _addr(lse),
                                         workspace.data_ptr(), workspace.numel(), _stream(stream)))
     else:
         _check(_lib.osc_paged_attention(Q.data_ptr(), T, ldq, n_q, cache.c, R, row_off.data_ptr(), kv_len.data_ptr(), table.data_ptr(), cols,
-                                        table.stride(0), 0, None, None, None, 0, 0, max_new, scale, O.data_ptr(), ldo, _addr(lse),
+                                        table.stride()[0], 0, None, None, None, 0, 0, max_new, scale, O.data_ptr(), ldo, _addr(lse),
                                         workspace.data_ptr(), workspace.numel(), _stream(stream)))

@@ -80,6 +80,15 @@ osc_status osc_kv_slots(const int32_t* cached, const int32_t* fresh, const int32
         (R > 0 && (!cached || !fresh || !kv_len)) || (R > 0 && cols > 0 && !table))
         return fail(OSC_ERR_INVALID_ARG, "null device pointer");
     if (R > 1 && ld_table < cols) return fail(OSC_ERR_SHAPE, "ld_table = %lld < cols = %d", (long long)ld_table, cols);
+    // Every CTA reads all lengths for itself, so nothing that is written may lie on them, nor on one another.
+    const struct { const int32_t* p; int64_t n; const char* name; } buf[10] = {
+        {row_off, (int64_t)R + 1, "row_off"}, {kv_len, R, "kv_len"}, {slots, T, "slots"}, {positions, T, "positions"}, {taken, 1, "taken"},
+        {table, R > 0 ? (R - 1) * ld_table + cols : 0, "table"}, {cached, R, "cached"}, {fresh, R, "fresh"}, {base, base ? R : 0, "base"},
+        {free_pages, n_free, "free_pages"}};
+    for (int i = 0; i < 6; ++i)
+        for (int j = i + 1; j < 10; ++j)
+            if (buf[i].n > 0 && buf[j].n > 0 && buf[i].p < buf[j].p + buf[j].n && buf[j].p < buf[i].p + buf[i].n)
+                return fail(OSC_ERR_INVALID_ARG, "%s overlaps %s", buf[i].name, buf[j].name);
     DeviceInfo di;
     if (osc_status s = device_info(&di)) return s;
     KvSlotsArgs a = {};
@@ -110,6 +119,7 @@ osc_status osc_qk_norm_rope(const void* QKV, int T, int64_t ld, int n_q, const o
                     (long long)n_q * D, (long long)ld_pos);
     if (ld % 8 || ldq % 8 || !aligned16(QKV) || !aligned16(Q))
         return fail(OSC_ERR_ALIGN, "QKV and Q must be 16-byte aligned, ld and ldq multiples of 8");
+    if (Q == QKV && T > 1 && ldq != ld) return fail(OSC_ERR_INVALID_ARG, "Q is QKV, but ldq = %lld is not ld = %lld", (long long)ldq, (long long)ld);
     DeviceInfo di;
     if (osc_status s = device_info(&di)) return s;
     QkNormRopeArgs a = {};
@@ -166,6 +176,7 @@ osc_status osc_paged_attention(const void* Q, int T, int64_t ldq, int n_q, const
         return fail(OSC_ERR_SHAPE, "ldq = %lld, ldo = %lld < n_q * head_dim = %lld", (long long)ldq, (long long)ldo, (long long)n_q * D);
     if (ldq % 8 || ldo % 8 || !aligned16(Q) || !aligned16(O) || !aligned16(workspace))
         return fail(OSC_ERR_ALIGN, "Q, O and workspace must be 16-byte aligned, ldq and ldo multiples of 8");
+    if (O == Q) return fail(OSC_ERR_INVALID_ARG, "O is Q");
     // Counts of tiles and of rows are ints on the device.  The line cannot hold more than every request's units over all the keys its
     // table names (16 keys and 16 rows to a tile at the least), nor more than that of all rows over the prefix tables.
     const int64_t own_keys = (int64_t)cols * cache->page_size, front_keys = P ? (int64_t)prefix_cols * cache->page_size : 0;

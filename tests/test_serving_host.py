@@ -78,6 +78,25 @@ def test_paged_attention_refusals(B):
     assert B.osc_paged_attention_workspace_bytes(300, 32, 128, 9, 2) > B.osc_paged_attention_workspace_bytes(200, 32, 128, 9, 2)
 
 
+def test_overlapping_buffers_are_refused(B):
+    """What one CTA reads another must not have written: every CTA of osc_kv_slots reads all lengths, a row of Q is read by several."""
+    ok = dict(cached=0x1000, fresh=0x2000, base=0xA000, R=2, page=16, free=0x3000, n_free=4, table=0x4000, cols=3, ld=3, T=5, row=0x5000, kv=0x6000,
+              slots=0x7000, pos=0x8000, taken=0x9000)
+
+    def call(**kw):
+        return B._lib.osc_kv_slots(*{**ok, **kw}.values(), None)
+    for out in ("row", "kv", "slots", "pos", "taken", "table"):
+        for other in ("cached", "fresh", "base", "free", "row", "kv", "slots", "pos", "taken", "table"):
+            if out != other:
+                assert call(**{out: ok[other]}) == -1, (out, other)
+    assert call(kv=0x1004) == -1 and call(kv=0x1000 - 4) == -1 and call(taken=0x4000 + 5 * 4) == -1 and call(table=0x1000 - 5 * 4) == -1
+    r = B.RopeStruct(0x8000, None, 128, 1, 0, 1.0)
+    assert B._lib.osc_qk_norm_rope(0x7000, 4, 8 * 128, 4, cache(B), None, None, 1e-6, r, 0x5000, 4, None, 0x7000, 512, None) == -1
+    sz = 1 << 40
+    assert B._lib.osc_paged_attention(0x1000, 4, 512, 4, cache(B), 2, 0x2000, 0x3000, 0x4000, 3, 3, 0, None, None, None, 0, 0, 0, 0.1, 0x1000, 512, None,
+                                      0x10000, sz, None) == -1
+
+
 def test_binding_refuses_wrong_tensors(B):
     import torch
     i, b = torch.zeros(4, dtype=torch.int32), torch.zeros(2, 16, 2, 64, dtype=torch.bfloat16)
