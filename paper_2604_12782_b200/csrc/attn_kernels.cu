@@ -227,8 +227,13 @@ __device__ __forceinline__ int head_span(const AttnArgs& a, const Segment& g) {
 // that a share of many short units is no longer than one of few long ones (prompts of 8001 tokens: shares of 210 tiles in 5 to 12
 // units ended between 360 and 405 us).
 __device__ __forceinline__ int share_tiles(int N, int ctas, int least) { return max((int)(((int64_t)N + ctas - 1) / ctas), least); }
-// least share: 64 keys of few_hw heads
-__device__ __forceinline__ int few_min_tiles(const AttnArgs& a) { return a.few_hw; }
+// Least share of the few-row line.  Where there is less work than CTAs, q tiles to a share take about 0.62 q us, and the t / q pieces of a
+// row whose keys are t tiles 0.85 us for every 16 in the join: the sum is least at q = sqrt(0.086 t).  t is taken as the mean over the
+// segments.  One request of 100 / 300 / 600 / 1500 / 4000 keys, 8 heads: 7.6 / 8.2 / 8.9 / 11.1 / 13.5 us; with four tiles for all
+// 10.7 / 10.9 / 10.9 / 11.5 / 13.7, with one for all 7.6 / 8.1 / 9.1 / 12.3 / 15.4.
+__device__ __forceinline__ int few_min_tiles(const AttnArgs& a, int n) {
+    return max((int)(sqrtf(0.086f * (float)n / ((float)(a.P + a.R) * (float)FewUnits::heads(a))) + 0.5f), 1);
+}
 constexpr int AT_WIDE_MIN_TILES = 4;
 // Shares of the two lines of a step that has both (nf, nw tiles).  The tcgen05 kernel is bound by arithmetic, the few-row kernel by
 // memory, and both are resident at once: the first gets as many CTAs as its part of the SMs' time, the second runs on the other
@@ -242,7 +247,7 @@ __device__ __forceinline__ void share_lines(const AttnArgs& a, int nf, int nw, i
     const int q = share_tiles(nw, wide, AT_WIDE_MIN_TILES);
     const int left = 2 * (sms - (nw + q - 1) / q);
     if (nw > 0 && left > 0 && left <= a.few_ctas) few = a.few_ctas / left * left;
-    share[0] = share_tiles(nf, few, few_min_tiles(a));
+    share[0] = share_tiles(nf, few, few_min_tiles(a, nf));
     share[1] = q;
 }
 
@@ -618,7 +623,7 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
         }
         empty = __syncthreads_or(empty);
         N = carry;
-        q = share_tiles(N, a.few_ctas, few_min_tiles(a));
+        q = share_tiles(N, a.few_ctas, few_min_tiles(a, N));
         src.seg = seg;
         src.start = start;
         if (empty)
