@@ -614,8 +614,8 @@ osc_status osc_qk_norm_rope(const void* QKV, int T, int64_t ld, int n_q, const o
  * holds does not matter.  Two calls under way at once need one each.
  * Limits (OSC_ERR_SHAPE): T * n_q <= 2^29; the columns of a table hold at most 2^29 keys; R, P and the tables' widths together
  * stay below 2^31 tiles (a tile is at the least 64 keys of one key/value head, or 16 of four, by 16 rows).
- * The cache's, the offsets' and the tables' contents are the caller's: rows that two requests claim, or a row_off that falls, give
- * unspecified rows of O and lse, never an access outside the buffers. */
+ * The cache's, the offsets' and the tables' contents are the caller's: where row_off or group_off falls, no row is written; whatever they hold,
+ * nothing outside the buffers is touched. */
 osc_status osc_paged_attention_workspace_bytes(int T, int n_q, int head_dim, int R, int P, size_t* bytes);
 osc_status osc_paged_attention(const void* Q, int T, int64_t ldq, int n_q, const osc_kv_cache_t* cache, int R,
                                const int32_t* row_off, const int32_t* kv_len, const int32_t* table, int cols, int64_t ld_table,

@@ -433,7 +433,7 @@ __global__ void __launch_bounds__(1024) attn_plan_kernel(const AttnArgs a) {
     }
     auto mixed = [&](int g) { return in_smem ? s_mixed[g] != 0 : true; };
     int carry[2] = {0, 0};
-    bool two = false, empty = false, longer = false;
+    bool two = false, empty = false, longer = false, falls = false;
     for (int s0 = 0; s0 < S; s0 += threads) {
         const int s = s0 + tid;
         int own[2] = {0, 0}, inc[2], total[2];
@@ -443,6 +443,7 @@ __global__ void __launch_bounds__(1024) attn_plan_kernel(const AttnArgs a) {
             g.flags = s >= a.P ? SEG_OWN : 0;
             if (s < a.P) {
                 const int r0 = off(s), r1 = max(off(s + 1), r0);
+                falls |= off(s + 1) < r0;
                 g.klen = len(s);
                 g.t0 = attn_row(a, r0);
                 g.n = g.klen > 0 && mixed(s) ? max(attn_row(a, r1) - g.t0, 0) : 0;
@@ -451,7 +452,9 @@ __global__ void __launch_bounds__(1024) attn_plan_kernel(const AttnArgs a) {
             } else {
                 const int r = s - a.P;
                 g.t0 = attn_row(a, r);
-                g.n = max(attn_row(a, r + 1) - g.t0, 0);
+                g.n = attn_row(a, r + 1) - g.t0;
+                falls |= g.n < 0;
+                g.n = max(g.n, 0);
                 g.klen = attn_keys(a.kv_len[r], a.cols, a.page_shift);
                 g.group = group_of(r);
                 if (g.group >= 0) {
@@ -487,7 +490,12 @@ __global__ void __launch_bounds__(1024) attn_plan_kernel(const AttnArgs a) {
         carry[1] += total[1];
     }
     two = __syncthreads_or(two);
-    empty = __syncthreads_or(empty || longer);
+    empty = __syncthreads_or(empty || longer || falls);
+    // Offsets that fall: requests or groups may hold the same rows, and all their tiles together pass what the host has counted.
+    if (empty && __syncthreads_or(falls)) {
+        two = empty = false;
+        carry[0] = carry[1] = 0;
+    }
     if (tid == 0) {
         a.plan.share[2] = two;
         a.plan.few_start[S] = carry[0];
@@ -599,7 +607,7 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
         Segment* seg = reinterpret_cast<Segment*>(at_smem + C::RING + C::JOIN);
         int* start = reinterpret_cast<int*>(seg + FEW_SELF);
         int carry = 0;
-        bool empty = false;
+        bool empty = false, falls = false;
         for (int s0 = 0; s0 < S; s0 += AT_FEW_THREADS) {
             const int s = s0 + threadIdx.x;
             int inc[2] = {0, 0}, total[2], own = 0;
@@ -609,7 +617,9 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
                 g.flags = SEG_OWN;
                 g.group = -1;
                 g.t0 = attn_row(a, s);
-                g.n = max(attn_row(a, s + 1) - g.t0, 0);
+                g.n = attn_row(a, s + 1) - g.t0;
+                falls |= g.n < 0;
+                g.n = max(g.n, 0);
                 g.klen = attn_keys(a.kv_len[s], a.cols, a.page_shift);
                 g.tiles = head_span<FewUnits>(a, g);
                 own = g.tiles * FewUnits::heads(a);
@@ -621,8 +631,12 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
             if (s < S) start[s] = seg[s].start = carry + inc[0] - own;
             carry += total[0];
         }
-        empty = __syncthreads_or(empty);
+        empty = __syncthreads_or(empty || falls);
         N = carry;
+        if (empty && __syncthreads_or(falls)) {    // as in the plan kernel
+            empty = false;
+            N = 0;
+        }
         q = share_tiles(N, a.few_ctas, few_min_tiles(a, N));
         src.seg = seg;
         src.start = start;

@@ -329,3 +329,21 @@ def test_large_pages_and_tables_with_a_stride(B, page):
     o, lse = c.run(B)
     B.osc_sync_check()
     c.check(o, lse, f"pages of {page}")
+
+
+@pytest.mark.parametrize("max_new", [0, 1])
+def test_falling_offsets_compute_nothing(B, max_new):
+    """Requests or groups that would share rows: no row is written (with and without prefixes, so by either way of planning)."""
+    c = AttnCase(32, 4, 4, 128, 16, [2, 2, 30], [20, 20, 40], prefix=[50])
+    for rows, groups in (([0, 10, 4, 34], [0, 3]), ([0, 34, 0, 34], [0, 3]), ([40, 30, 20, 10], [0, 3]), ([0, 2, 4, 34], [3, 0])):
+        c.row_off.copy_(torch.tensor(rows, dtype=torch.int32))
+        c.group_off.copy_(torch.tensor(groups, dtype=torch.int32))
+        o, lse = c.run(B, max_new=max_new)
+        B.osc_sync_check()
+        assert (o.float() == 7.0).all() and (lse == 7.0).all()
+    d = AttnCase(33, 4, 4, 128, 16, [2, 2, 30], [20, 20, 1])
+    for rows in ([0, 10, 4, 34], [0, 34, 0, 34], [40, 30, 20, 10]):
+        d.row_off.copy_(torch.tensor(rows, dtype=torch.int32))
+        o, lse = d.run(B, max_new=max_new)
+        B.osc_sync_check()
+        assert (o.float() == 7.0).all() and (lse == 7.0).all()
