@@ -117,8 +117,8 @@ osc_status osc_qk_norm_rope(const void* QKV, int T, int64_t ld, int n_q, const o
     if (ld < width || ldq < (int64_t)n_q * D || (rope->axes > 1 && ld_pos < T))
         return fail(OSC_ERR_SHAPE, "ld = %lld < %lld, ldq = %lld < %lld or ld_pos = %lld < T", (long long)ld, (long long)width, (long long)ldq,
                     (long long)n_q * D, (long long)ld_pos);
-    if (ld % 8 || ldq % 8 || !aligned16(QKV) || !aligned16(Q))
-        return fail(OSC_ERR_ALIGN, "QKV and Q must be 16-byte aligned, ld and ldq multiples of 8");
+    if (ld % 8 || ldq % 8 || !aligned16(QKV) || !aligned16(Q) || !aligned16(gamma_q) || !aligned16(gamma_k))
+        return fail(OSC_ERR_ALIGN, "QKV, Q, gamma_q and gamma_k must be 16-byte aligned, ld and ldq multiples of 8");
     if (Q == QKV && T > 1 && ldq != ld) return fail(OSC_ERR_INVALID_ARG, "Q is QKV, but ldq = %lld is not ld = %lld", (long long)ldq, (long long)ld);
     DeviceInfo di;
     if (osc_status s = device_info(&di)) return s;

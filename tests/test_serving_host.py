@@ -157,3 +157,14 @@ def test_definition_of_attention():
         w = np.exp(s) / np.exp(s).sum(-1, keepdims=True)
         assert np.allclose(o[2, h], w @ v[:, h]) and np.allclose(lse[2, h], np.log(np.exp(s).sum(-1)))
         assert (absv[2, h] >= np.abs(o[2, h])).all()
+
+
+def test_qk_norm_rope_refuses_unaligned_gamma(B):
+    """The norm's weights are read several channels at a time, so a view that begins inside such a group must not reach the kernel."""
+    r = B.RopeStruct(0x8000, None, 128, 1, 0, 1.0)
+
+    def call(gq, gk):
+        return B._lib.osc_qk_norm_rope(0x70000, 4, 8 * 128, 4, cache(B), gq, gk, 1e-6, r, 0x5000, 4, None, 0x60000, 512, None)
+    for off in (2, 4, 6, 8, 10, 14):
+        assert call(0x9000 + off, None) == -4 and call(None, 0x9000 + off) == -4, off
+        assert call(0x9000 + off, 0xA000) == -4 and call(0xA000, 0x9000 + off) == -4, off
