@@ -556,7 +556,7 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
             if (pair || s == 0) {
                 int tok, hq;
                 if (row_of(r, tok, hq)) {
-                    if (!direct) a.ml[part_row(r, tok, hq)] = make_float2(m, l);
+                    if (!direct) a.ml[part_row(r, tok, hq)] = piece_ml(m, l);
                     else if (a.lse) a.lse[tok * a.Hq + hq] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
                 }
             }

@@ -531,6 +531,10 @@ __device__ __forceinline__ PieceList list_pieces(int begin, int tiles, int q, in
     return p;
 }
 
+// (m, l) of a piece as the join reads it.  NaN scores leave the maximum alone (a maximum drops NaN), but not the sum.  Such a piece says
+// m = +inf: the join then weighs it with NaN and all others with 0, where a maximum of -inf, or far below the others', would drop it.
+__device__ __forceinline__ float2 piece_ml(float m, float l) { return make_float2(l != l ? INFINITY : m, l); }
+
 // --------------------------------------------------------------------------------------------- few rows
 __device__ __forceinline__ void cp_async_16(uint32_t dst, const void* src, bool valid, uint64_t policy) {
     asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0), "l"(policy) : "memory");
@@ -865,7 +869,7 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
 #pragma unroll
                     for (int j = 0; j < NJ; ++j)
                         *reinterpret_cast<float2*>(part + j * 8) = make_float2(o[j][2 * hlf], o[j][2 * hlf + 1]);
-                    if (cq == 0) a.ml[at] = make_float2(m[hlf], l[hlf]);
+                    if (cq == 0) a.ml[at] = piece_ml(m[hlf], l[hlf]);
                 }
             }
         }

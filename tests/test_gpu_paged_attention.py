@@ -347,3 +347,63 @@ def test_falling_offsets_compute_nothing(B, max_new):
         o, lse = d.run(B, max_new=max_new)
         B.osc_sync_check()
         assert (o.float() == 7.0).all() and (lse == 7.0).all()
+
+
+def same_bits(a, b):
+    return torch.equal(a.contiguous().view(torch.int16), b.contiguous().view(torch.int16))
+
+
+NAN_STEPS = {
+    # name: (case, maximum of new tokens, tokens of which one head's query is NaN)
+    "whole units, few rows": (dict(seed=34, Hk=4, G=4, D=128, page=16, new=[1, 1, 1], kv=[16, 9, 3]), 1, [1]),
+    "cut units, few rows": (dict(seed=35, Hk=4, G=4, D=128, page=16, new=[1, 1], kv=[600, 700]), 1, [0]),
+    "cut units, few rows, joined warps": (dict(seed=36, Hk=1, G=4, D=64, page=16, new=[1, 1], kv=[3000, 2500]), 1, [0]),
+    "whole units, many rows": (dict(seed=37, Hk=2, G=4, D=128, page=16, new=[60, 64], kv=[100, 64]), 0, [3, 70]),
+    "cut units, many rows": (dict(seed=38, Hk=1, G=4, D=128, page=64, new=[20, 70], kv=[2500, 4000]), 0, [5, 40]),
+    "cut units of 64 channels": (dict(seed=39, Hk=1, G=8, D=64, page=16, new=[9, 40], kv=[2500, 4000]), 0, [5, 30]),
+    "behind a prefix, few rows": (dict(seed=40, Hk=2, G=4, D=128, page=16, new=[1, 1, 1], kv=[300, 5, 0], prefix=[700]), 1, [0, 2]),
+    "behind a prefix, many rows": (dict(seed=41, Hk=2, G=4, D=128, page=16, new=[1] * 30 + [30], kv=[40] * 31, prefix=[900]), 0, [4, 45]),
+    "a prompt behind a prefix": (dict(seed=42, Hk=1, G=4, D=128, page=16, new=[130], kv=[500], prefix=[3000]), 0, [100]),
+}
+
+
+@pytest.mark.parametrize("name", NAN_STEPS)
+def test_a_nan_query_gives_nan_and_leaves_its_neighbours(B, name):
+    """However its keys are cut, a head whose query is NaN gives NaN, not the 0 and -inf of a row without keys."""
+    kw, max_new, tokens = NAN_STEPS[name]
+    c = AttnCase(**kw)
+    Hq, D = c.Hk * c.G, c.D
+    o, lse = c.run(B, max_new=max_new)
+    c.check(o, lse, name)
+    clean, clean_lse = o.clone(), lse.clone()
+    hit = torch.zeros(c.T, Hq, dtype=torch.bool, device="cuda")
+    for i, t in enumerate(tokens):
+        h = (5 * i + 2) % Hq
+        hit[t, h] = True
+        c.q[t, h * D:(h + 1) * D] = float("nan")
+    o, lse = c.run(B, max_new=max_new)
+    B.osc_sync_check()
+    o, clean = o.reshape(c.T, Hq, D), clean.reshape(c.T, Hq, D)
+    assert torch.isnan(o[hit].float()).all() and torch.isnan(lse[hit]).all(), f"{name}: NaN was lost"
+    o[hit], lse[hit] = clean[hit], clean_lse[hit]
+    c.check(o.reshape(c.T, Hq * D), lse, f"{name}, neighbours")      # (rows of one tile are rescaled together, so not bit for bit)
+
+
+@pytest.mark.parametrize("new,max_new", [(1, 1), (40, 0)])
+@pytest.mark.parametrize("kv", [60, 3000])
+@pytest.mark.parametrize("prefix", [[], [500]])
+def test_a_nan_key_gives_nan_where_it_is_seen(B, new, max_new, kv, prefix):
+    """One key of one request holds NaN: every row of that request and head gives NaN, in whichever piece the key lies, and nobody else."""
+    for at in (0, kv // 2, kv - new):
+        c = AttnCase(43, 2, 4, 128, 16, [1, new, 1], [70, kv, 20], prefix=prefix)
+        Hq, D = 8, 128
+        o, lse = c.run(B, max_new=max_new)
+        clean, clean_lse = o.clone().reshape(c.T, Hq, D), lse.clone()
+        c.k[int(c.table[1, at // 16]), at % 16, 1, 3] = float("nan")
+        o, lse = c.run(B, max_new=max_new)
+        B.osc_sync_check()
+        o = o.reshape(c.T, Hq, D)
+        hit = torch.zeros(c.T, Hq, dtype=torch.bool, device="cuda")
+        hit[1 + max(at - (kv - new), 0):1 + new, 4:] = True          # token i of the request sees own keys up to kv - new + i
+        assert torch.isnan(o[hit].float()).all() and torch.isnan(lse[hit]).all(), f"key {at}"
+        assert same_bits(o[~hit], clean[~hit]) and torch.equal(lse[~hit], clean_lse[~hit]), f"key {at}"
