@@ -584,8 +584,8 @@ typedef struct {
 
 /* QKV [T, (n_q + 2 n_kv) * head_dim] (the QKV projection's output: query heads, key heads, value heads; n_kv and head_dim
  * from the cache) in one pass: RMSNorm of every query and key head (gamma_q / gamma_k: dev bf16 [head_dim], 16-byte
- * aligned; null = no norm), rotation, one rounding to bf16; queries to Q (dev bf16 [T, ldq]; may be QKV itself, with ldq = ld), keys and values (copied)
- * to the tokens' slots of the cache.
+ * aligned; null = no norm), rotation, one rounding to bf16; queries to Q (dev bf16 [T, ldq]; may be QKV itself, with ldq = ld, and shares no byte
+ * with its T rows otherwise: OSC_ERR_INVALID_ARG), keys and values (copied) to the tokens' slots of the cache, which overlaps neither.
  *   positions: dev int32 [axes][ld_pos];  slots: dev int32 [T], or null: token t at slot t.
  * Tokens with a slot outside 0 .. n_pages * page_size - 1 write nothing to the cache.  Two tokens must not share a
  * slot.  Arithmetic in fp32 (so a head whose sum of squares passes its range, |x| from about 10^18 on, gives zeros where there is

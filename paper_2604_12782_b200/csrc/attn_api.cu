@@ -2,6 +2,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <utility>
 
 #include "../../include/osc.h"
 #include "common.cuh"
@@ -22,6 +23,30 @@ static osc_status check_cache(const osc_kv_cache_t* c) {
     if (c->page_stride % 8 || c->token_stride % 8 || c->head_stride % 8 || !aligned16(c->k) || !aligned16(c->v))
         return fail(OSC_ERR_ALIGN, "cache: k and v must be 16-byte aligned, strides multiples of 8");
     return OSC_OK;
+}
+
+// A matrix in memory: `rows` pieces of `width` bytes, `ld` >= width bytes from one to the next.
+struct ByteRows { __int128 at, rows, ld, width; };
+static ByteRows bytes_of(const void* p, int64_t rows, __int128 ld, int64_t width) {
+    return {(__int128)reinterpret_cast<uintptr_t>(p), rows, ld, width};
+}
+// Whether two matrices share a byte.  Rows of one may lie in the gaps between the other's rows.
+static bool rows_meet(ByteRows a, ByteRows b) {
+    if (a.rows < 1 || b.rows < 1 || a.width < 1 || b.width < 1) return false;
+    if (b.at < a.at) std::swap(a, b);
+    if (b.at >= a.at + (a.rows - 1) * a.ld + a.width) return false;
+    if (a.rows == 1) a.ld = b.ld;
+    if (b.rows == 1) b.ld = a.ld;
+    // The same stride: b's first row begins at byte c of a row of a's grid, and reaches the next one (which is there: b begins before a ends) or not.
+    if (a.ld == b.ld) {
+        const __int128 c = (b.at - a.at) % a.ld;
+        return c < a.width || c + b.width > a.ld;
+    }
+    for (__int128 i = 0; i < b.rows; ++i) {      // a's first row that ends behind the beginning of b's
+        const __int128 from = b.at + i * b.ld - a.at, r = from < a.width ? 0 : (from - a.width) / a.ld + 1;
+        if (r < a.rows && r * a.ld < from + b.width) return true;
+    }
+    return false;
 }
 
 // bf16 tensor map of 3 or 4 dimensions, boxes of 64 channels, 128-byte swizzle, zeros outside.  strides in elements.
@@ -119,7 +144,8 @@ osc_status osc_qk_norm_rope(const void* QKV, int T, int64_t ld, int n_q, const o
                     (long long)n_q * D, (long long)ld_pos);
     if (ld % 8 || ldq % 8 || !aligned16(QKV) || !aligned16(Q) || !aligned16(gamma_q) || !aligned16(gamma_k))
         return fail(OSC_ERR_ALIGN, "QKV, Q, gamma_q and gamma_k must be 16-byte aligned, ld and ldq multiples of 8");
-    if (Q == QKV && T > 1 && ldq != ld) return fail(OSC_ERR_INVALID_ARG, "Q is QKV, but ldq = %lld is not ld = %lld", (long long)ldq, (long long)ld);
+    if (!(Q == QKV && (T == 1 || ldq == ld)) && rows_meet(bytes_of(QKV, T, (__int128)ld * 2, width * 2), bytes_of(Q, T, (__int128)ldq * 2, (int64_t)n_q * D * 2)))
+        return fail(OSC_ERR_INVALID_ARG, "Q overlaps QKV and is not QKV itself with ldq = ld");
     DeviceInfo di;
     if (osc_status s = device_info(&di)) return s;
     QkNormRopeArgs a = {};

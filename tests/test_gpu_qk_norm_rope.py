@@ -140,3 +140,35 @@ def test_more_tokens_than_warps(B, T, inter):
     """About the numbers of tokens (warps on 148 SMs) behind which the rest is spread over several warps a token."""
     run_case(B, T, T, 3, 1, 64, 64, inter=inter)
     run_case(B, T + 1, T, 1, 1, 128, 128 if inter else 48, inter=inter)
+
+
+@pytest.mark.parametrize("where", ["gap", "gap, other stride", "behind", "columns of a wider buffer"])
+def test_queries_beside_qkv_in_one_buffer(B, where):
+    """Queries in the gaps between QKV's rows, or right behind them: the same as in a buffer of their own."""
+    T, Hq, Hk, D = 37, 4, 2, 128
+    w, wq = (Hq + 2 * Hk) * D, Hq * D
+    g = torch.Generator().manual_seed(3)
+    data = torch.randn(T, w, generator=g).to(torch.bfloat16).cuda()
+    pos = torch.arange(T, dtype=torch.int32, device="cuda") * 5
+    rope = B.Rope((1e-4 ** (torch.arange(D // 2) / (D // 2))).cuda())
+    gam = torch.ones(D, dtype=torch.bfloat16, device="cuda")
+
+    def run(x, q):
+        k, v = (torch.zeros(3, 16, Hk, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        B.osc_qk_norm_rope(x, Hq, B.KvCache(k, v), q, pos, rope, gamma_q=gam, gamma_k=gam)
+        torch.cuda.synchronize()
+        return q.clone(), k, v
+    want = run(data, torch.zeros(T, wq, dtype=torch.bfloat16, device="cuda"))
+    big = torch.full((4 * T * (w + wq),), 7.0, dtype=torch.bfloat16, device="cuda")
+    if where == "behind":
+        x, q = big[:T * w].view(T, w), big[T * w:T * (w + wq)].view(T, wq)
+    elif where == "gap":
+        x, q = (v[:, a:b] for v, a, b in ((big[:T * (w + wq)].view(T, -1), 0, w), (big[:T * (w + wq)].view(T, -1), w, w + wq)))
+    elif where == "columns of a wider buffer":
+        wide = big[:T * 2 * (w + wq)].view(T, -1)
+        x, q = wide[:, wq + 8:wq + 8 + w], wide[:, :wq]
+    else:
+        x, q = big[:T * (w + wq)].view(T, -1)[:, :w], big[:2 * T * (w + wq)].view(T, -1)[:, w:w + wq]
+    x.copy_(data)
+    got = run(x, q)
+    assert all(torch.equal(a, b) for a, b in zip(want, got)) and torch.equal(x, data)

@@ -168,3 +168,22 @@ def test_qk_norm_rope_refuses_unaligned_gamma(B):
     for off in (2, 4, 6, 8, 10, 14):
         assert call(0x9000 + off, None) == -4 and call(None, 0x9000 + off) == -4, off
         assert call(0x9000 + off, 0xA000) == -4 and call(0xA000, 0x9000 + off) == -4, off
+
+
+def test_queries_that_overlap_qkv_without_being_it_are_refused(B):
+    """Warps of one token, and steps of one warp, read heads of QKV after others have written queries, so only the same place can be
+    read before it is written."""
+    r = B.RopeStruct(0x800000, None, 128, 1, 0, 1.0)
+    qkv, ld, T = 0x100000, 1024, 4                      # elements of two bytes; 4 query and 2 + 2 other heads of 128 channels
+
+    def call(Q, ldq=512, T=T, ld=ld, qkv=qkv):
+        return B._lib.osc_qk_norm_rope(qkv, T, ld, 4, cache(B), None, None, 1e-6, r, 0x900000, T, None, Q, ldq, None)
+    for off in (16, 256, 512, 1024 - 16, 1024, 1536, 2048, 3 * 2048, 4 * 2048 - 16):     # bytes into QKV's 4 * 2048
+        assert call(qkv + off) == -1 and call(qkv + off, ldq=ld) == -1, off
+    for off in (16, 512, 3 * 1024 + 1008):              # QKV begins inside Q
+        assert call(qkv - off) == -1, off
+    assert call(qkv + 16, T=1) == -1 and call(qkv, ldq=520) == -1
+    # rows of Q in the gaps of QKV's, of the same stride and of another: those that reach into a row
+    assert call(qkv + 2048 + 1040, ldq=2048, ld=2048) == -1 and call(qkv + 2048 - 16, ldq=2048, ld=2048) == -1
+    assert call(qkv + 2048, ldq=3072, ld=2048) == -1 and call(qkv + 2048 + 1040, ldq=4096, ld=2048) == -1
+    assert call(qkv - 1024 + 16, ldq=2048, ld=2048) == -1 and call(qkv - 4096 - 1024, ldq=3072, ld=2048) == -1
