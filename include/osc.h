@@ -603,7 +603,8 @@ osc_status osc_qk_norm_rope(const void* QKV, int T, int64_t ld, int n_q, const o
  *   O = softmax(scale * Q K^T) V per head, dev bf16 [T, ldo]; lse (dev float [T][n_q], or null): natural logarithm of the
  *   sum of exp(scale * q . k).  A row without any key gives 0 and -inf; one that sees a NaN score
  *   (a NaN in its query or in a key that it sees) gives NaN for both.  Rows from row_off[R] on are left as they are.
- * O must not overlap Q.
+ * O, lse and the workspace must not overlap one another, Q, the offsets, the lengths and the tables (OSC_ERR_INVALID_ARG), nor the cache.
+ * (Rows of O may lie in the gaps between the rows of Q.)
  * Sums and the running maximum in fp32, weights in bf16.  page_size: a power of two of at least 16.  Lengths are read on
  * the device: kv_len and prefix_len are cut to what the table's columns hold, a table entry outside 0 .. n_pages - 1 reads as a
  * page of zeros, and nothing behind a length is used, whatever the cache holds there (NaN too).  A key that is masked for a row only by

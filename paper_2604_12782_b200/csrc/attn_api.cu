@@ -27,7 +27,7 @@ static osc_status check_cache(const osc_kv_cache_t* c) {
 
 // A matrix in memory: `rows` pieces of `width` bytes, `ld` >= width bytes from one to the next.
 struct ByteRows { __int128 at, rows, ld, width; };
-static ByteRows bytes_of(const void* p, int64_t rows, __int128 ld, int64_t width) {
+static ByteRows bytes_of(const void* p, int64_t rows, __int128 ld, __int128 width) {
     return {(__int128)reinterpret_cast<uintptr_t>(p), rows, ld, width};
 }
 // Whether two matrices share a byte.  Rows of one may lie in the gaps between the other's rows.
@@ -35,6 +35,7 @@ static bool rows_meet(ByteRows a, ByteRows b) {
     if (a.rows < 1 || b.rows < 1 || a.width < 1 || b.width < 1) return false;
     if (b.at < a.at) std::swap(a, b);
     if (b.at >= a.at + (a.rows - 1) * a.ld + a.width) return false;
+    if (a.rows == 1 && b.rows == 1) return true;
     if (a.rows == 1) a.ld = b.ld;
     if (b.rows == 1) b.ld = a.ld;
     // The same stride: b's first row begins at byte c of a row of a's grid, and reaches the next one (which is there: b begins before a ends) or not.
@@ -202,7 +203,6 @@ osc_status osc_paged_attention(const void* Q, int T, int64_t ldq, int n_q, const
         return fail(OSC_ERR_SHAPE, "ldq = %lld, ldo = %lld < n_q * head_dim = %lld", (long long)ldq, (long long)ldo, (long long)n_q * D);
     if (ldq % 8 || ldo % 8 || !aligned16(Q) || !aligned16(O) || !aligned16(workspace))
         return fail(OSC_ERR_ALIGN, "Q, O and workspace must be 16-byte aligned, ldq and ldo multiples of 8");
-    if (O == Q) return fail(OSC_ERR_INVALID_ARG, "O is Q");
     // Counts of tiles and of rows are ints on the device.  The line cannot hold more than every request's units over all the keys its
     // table names (16 keys and 16 rows to a tile at the least), nor more than that of all rows over the prefix tables.
     const int64_t own_keys = (int64_t)cols * cache->page_size, front_keys = P ? (int64_t)prefix_cols * cache->page_size : 0;
@@ -218,6 +218,18 @@ osc_status osc_paged_attention(const void* Q, int T, int64_t ldq, int n_q, const
         return fail(OSC_ERR_SHAPE, "T = %d, R = %d, P = %d over up to %lld keys: too many tiles", T, R, P, (long long)(own_keys + front_keys));
     const AttnLayout l = attn_layout(T, n_q, D, R, P);
     if (workspace_bytes < l.total) return fail(OSC_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, l.total);
+    // What is written may lie on nothing else: other CTAs still read it.
+    const __int128 row = (__int128)n_q * D * 2;
+    const struct { ByteRows b; const char* name; } buf[10] = {
+        {bytes_of(O, T, (__int128)ldo * 2, row), "O"}, {bytes_of(lse, lse ? 1 : 0, 0, (int64_t)T * n_q * 4), "lse"},
+        {bytes_of(workspace, 1, 0, l.total), "the workspace"}, {bytes_of(Q, T, (__int128)ldq * 2, row), "Q"},
+        {bytes_of(row_off, 1, 0, ((int64_t)R + 1) * 4), "row_off"}, {bytes_of(kv_len, 1, 0, (int64_t)R * 4), "kv_len"},
+        {bytes_of(table, cols ? R : 0, (__int128)ld_table * 4, (int64_t)cols * 4), "table"},
+        {bytes_of(group_off, P ? 1 : 0, 0, ((int64_t)P + 1) * 4), "group_off"}, {bytes_of(prefix_len, P ? 1 : 0, 0, (int64_t)P * 4), "prefix_len"},
+        {bytes_of(prefix_table, P && prefix_cols ? P : 0, (__int128)ld_prefix * 4, (__int128)prefix_cols * 4), "prefix_table"}};
+    for (int i = 0; i < 3; ++i)
+        for (int j = i + 1; j < 10; ++j)
+            if (rows_meet(buf[i].b, buf[j].b)) return fail(OSC_ERR_INVALID_ARG, "%s overlaps %s", buf[i].name, buf[j].name);
     DeviceInfo di;
     if (osc_status s = device_info(&di)) return s;
     uint8_t* ws = static_cast<uint8_t*>(workspace);

@@ -407,3 +407,20 @@ def test_a_nan_key_gives_nan_where_it_is_seen(B, new, max_new, kv, prefix):
         hit[1 + max(at - (kv - new), 0):1 + new, 4:] = True          # token i of the request sees own keys up to kv - new + i
         assert torch.isnan(o[hit].float()).all() and torch.isnan(lse[hit]).all(), f"key {at}"
         assert same_bits(o[~hit], clean[~hit]) and torch.equal(lse[~hit], clean_lse[~hit]), f"key {at}"
+
+
+def test_rows_of_o_in_the_gaps_of_q(B):
+    """Q and O as columns of one buffer, and a single token right behind another: the same as in buffers of their own."""
+    for kw, max_new in ((dict(seed=44, Hk=2, G=4, D=128, page=16, new=[1, 40, 1], kv=[300, 77, 9], prefix=[90]), 0),
+                        (dict(seed=45, Hk=4, G=2, D=64, page=16, new=[1], kv=[500]), 1)):
+        c = AttnCase(**kw)
+        o, lse = c.run(B, max_new=max_new)
+        w, P = c.Hk * c.G * c.D, len(c.prefix)
+        buf = torch.full((c.T, 2 * w), 7.0, dtype=torch.bfloat16, device="cuda")
+        buf[:, :w] = c.q
+        ws = torch.zeros(B.osc_paged_attention_workspace_bytes(c.T, c.Hk * c.G, c.D, len(c.new), P), dtype=torch.uint8, device="cuda")
+        lse2 = torch.full_like(lse, 7.0)
+        B.osc_paged_attention(buf[:, :w], B.KvCache(c.k, c.v), c.row_off, c.kv_len, c.table, buf[:, w:], ws, c.scale, lse=lse2,
+                              group_off=c.group_off, prefix_len=c.prefix_len, prefix_table=c.ptable if P else None, max_new=max_new)
+        B.osc_sync_check()
+        assert same_bits(buf[:, w:], o) and torch.equal(lse, lse2) and same_bits(buf[:, :w], c.q)

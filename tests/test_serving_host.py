@@ -187,3 +187,31 @@ def test_queries_that_overlap_qkv_without_being_it_are_refused(B):
     assert call(qkv + 2048 + 1040, ldq=2048, ld=2048) == -1 and call(qkv + 2048 - 16, ldq=2048, ld=2048) == -1
     assert call(qkv + 2048, ldq=3072, ld=2048) == -1 and call(qkv + 2048 + 1040, ldq=4096, ld=2048) == -1
     assert call(qkv - 1024 + 16, ldq=2048, ld=2048) == -1 and call(qkv - 4096 - 1024, ldq=3072, ld=2048) == -1
+
+
+def test_attention_outputs_that_overlap_anything_are_refused(B):
+    """O, lse and the workspace are written while Q, the offsets and the tables are still read by other CTAs."""
+    T, n_q, R, P, need = 4, 4, 2, 2, B.osc_paged_attention_workspace_bytes(4, 4, 128, 2, 2)
+    base = 1 << 40                                       # (no address below zero where the workspace ends on a table)
+    ok = dict(Q=base, T=T, ldq=512, n_q=n_q, c=cache(B), R=R, row=base + 0x200000, kv=base + 0x210000, table=base + 0x220000, cols=3, ld=3, P=P,
+              goff=base + 0x230000, plen=base + 0x240000, ptab=base + 0x250000, pcols=2, ldp=2, max_new=0, scale=0.1, O=base + 0x300000, ldo=512,
+              lse=base + 0x400000, ws=base + 0x1000000, n=need)
+
+    def call(**kw):
+        return B._lib.osc_paged_attention(*{**ok, **kw}.values(), None)
+    rows = T * 1024
+    for off in (0, 16, 512, 1024, rows - 16, -16, -512, 16 - rows):      # O against Q, rows of the same stride without gaps
+        assert call(O=ok["Q"] + off) == -1, off
+    # rows of Q and O of other strides and with gaps between them
+    assert call(ldq=1024, ldo=1024, O=ok["Q"] + 1040) == -1 and call(ldq=1024, ldo=1024, O=ok["Q"] + 1008) == -1
+    assert call(ldq=1024, ldo=2048, O=ok["Q"] + 1040) == -1 and call(ldq=1024, ldo=1536, O=ok["Q"] + 1024) == -1
+    small = dict(row=4 * (R + 1), kv=4 * R, table=4 * R * 3, goff=4 * (P + 1), plen=4 * P, ptab=4 * P * 2)
+    for name, size in small.items():
+        assert call(O=ok[name] - rows + 16) == -1 and call(O=ok[name]) == -1, name
+        assert call(lse=ok[name]) == -1 and call(lse=ok[name] + size - 4) == -1 and call(lse=ok[name] - 4 * T * n_q + 4) == -1, name
+        assert call(ws=ok[name] - need // 16 * 16 + 16) == -1 and call(ws=ok[name]) == -1, name
+    for name, size in (("Q", rows), ("O", rows)):
+        assert call(lse=ok[name]) == -1 and call(lse=ok[name] + size - 4) == -1 and call(lse=ok[name] - 4 * T * n_q + 4) == -1, name
+        assert call(ws=ok[name]) == -1 and call(ws=ok[name] + size - 16) == -1 and call(ws=ok[name] - need // 16 * 16 + 16) == -1, name
+    assert call(lse=ok["ws"] + need - 4) == -1 and call(lse=ok["ws"]) == -1
+    assert call(table=ok["ws"] + 4096, ld=100) == -1 and call(P=0, table=ok["O"] + 8) == -1
