@@ -559,7 +559,7 @@ typedef struct {
  *                  those of new pages are written, the rest is left as it is
  * Request r takes ceil((cached + fresh) / page_size) - ceil(cached / page_size) pages, requests in order.  Outputs:
  *   row_off: int32 [R + 1]: first row of every request among the step's tokens, row_off[R] = number of tokens
- *   kv_len:  int32 [R]: cached + fresh
+ *   kv_len:  int32 [R]: cached + fresh  (row_off, kv_len and taken stop at 2^31 - 1)
  *   slots, positions: int32 [T]: slot and position of every token; rows from row_off[R] on (a step filled up to a
  *            captured size) get slot -1 and position 0
  *   taken:   int32 [1]: pages taken.  More than n_free: the list ran out; table entries past it and the slots of

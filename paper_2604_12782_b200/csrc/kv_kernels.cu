@@ -14,8 +14,8 @@ namespace osc {
 //   table[r][have + j] = free[first_r + j]
 //   row_off      = exclusive sum of fresh
 //   token i of r : at = cached + i, slot = table[r][at / p] * p + at % p, position = base + at
-// Both sums run over the requests only, so every CTA does them for itself (32-bit halves of one 64-bit value, two
-// shuffle scans) instead of a second launch; tokens and pages are then shared out over the grid, each finding its
+// Both sums run over the requests only, so every CTA does them for itself (32-bit halves of one 64-bit value that stop at
+// 2^31 - 1, shuffle scans) instead of a second launch; tokens and pages are then shared out over the grid, each finding its
 // request by binary search in shared memory.  A page that this call hands out is read from the free list, not
 // from the table, so nothing written by another CTA is read.  What bounds it is latency: lengths -> scan ->
 // search -> page -> store, one after the other.
@@ -45,6 +45,13 @@ __device__ __forceinline__ int search_last(const int* start, int n, int x) {
     return lo;
 }
 
+// Tokens in the low half, pages in the high half.  Lengths are the caller's: a half that has reached 2^31 - 1 stays there (none of the
+// first T tokens, and no page of the list, lies behind it).  Grouping does not matter to a sum that stops, so it can be scanned.
+__device__ __forceinline__ unsigned long long add_counts(unsigned long long a, unsigned long long b) {
+    const unsigned lo = min((unsigned)a + (unsigned)b, 0x7FFFFFFFu), hi = min((unsigned)(a >> 32) + (unsigned)(b >> 32), 0x7FFFFFFFu);
+    return (unsigned long long)lo | (unsigned long long)hi << 32;
+}
+
 // KS_THREADS: 256, or 1024 for more requests than that, so that nearly every step is one chunk of requests
 template <int KS_THREADS>
 __global__ void __launch_bounds__(KS_THREADS) kv_slots_kernel(const KvSlotsArgs a) {
@@ -64,22 +71,22 @@ __global__ void __launch_bounds__(KS_THREADS) kv_slots_kernel(const KvSlotsArgs 
             s_cached[tid] = cached;
             s_base[tid] = a.base ? a.base[r0 + tid] : 0;
         }
-        const unsigned long long own = (unsigned long long)(unsigned)fresh | (unsigned long long)(unsigned)need << 32;
-        unsigned long long inc = own;
+        unsigned long long inc = (unsigned long long)(unsigned)fresh | (unsigned long long)(unsigned)need << 32;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const unsigned long long up = __shfl_up_sync(0xFFFFFFFFu, inc, o);
-            if (lane >= o) inc += up;
+            if (lane >= o) inc = add_counts(inc, up);
         }
         if (lane == 31) s_warp[warp] = inc;
+        unsigned long long exc = __shfl_up_sync(0xFFFFFFFFu, inc, 1);
         __syncthreads();
         unsigned long long before = carry, total = carry;
 #pragma unroll 1
         for (int w = 0; w < KS_THREADS / 32; ++w) {
-            if (w < warp) before += s_warp[w];
-            total += s_warp[w];
+            if (w < warp) before = add_counts(before, s_warp[w]);
+            total = add_counts(total, s_warp[w]);
         }
-        const unsigned long long exc = before + inc - own;
+        exc = lane ? add_counts(before, exc) : before;
         s_row[tid] = (int)(unsigned)exc;
         s_first[tid] = (int)(exc >> 32);
         if (tid == 0) {
@@ -92,10 +99,11 @@ __global__ void __launch_bounds__(KS_THREADS) kv_slots_kernel(const KvSlotsArgs 
         }
         __syncthreads();
         // the chunk's tokens
-        const int t_end = min((int)(unsigned)total, a.T);
-        for (int t = (int)(unsigned)carry + blockIdx.x * KS_THREADS + tid; t >= 0 && t < t_end; t += gridDim.x * KS_THREADS) {
-            const int i = search_last(s_row, nr, t);
-            const int at = s_cached[i] + (t - s_row[i]);
+        const unsigned stride = gridDim.x * KS_THREADS, first = blockIdx.x * KS_THREADS + tid;
+        const unsigned t_end = min((unsigned)total, (unsigned)a.T);
+        for (unsigned t = (unsigned)carry + first; t < t_end; t += stride) {
+            const int i = search_last(s_row, nr, (int)t);
+            const int at = s_cached[i] + ((int)t - s_row[i]);
             const int col = at / a.page, have = (s_cached[i] + a.page - 1) / a.page;
             int page = -1;
             if (at >= 0 && col < a.cols) {
@@ -108,17 +116,22 @@ __global__ void __launch_bounds__(KS_THREADS) kv_slots_kernel(const KvSlotsArgs 
             a.positions[t] = s_base[i] + at;
         }
         // the chunk's new pages
-        const int p_begin = (int)(carry >> 32), p_end = (int)(total >> 32);
-        for (int f = p_begin + blockIdx.x * KS_THREADS + tid; f >= 0 && f < p_end; f += gridDim.x * KS_THREADS) {
-            const int i = search_last(s_first, nr, f);
-            const int col = (s_cached[i] + a.page - 1) / a.page + (f - s_first[i]);
-            if (col >= 0 && col < a.cols) a.table[(int64_t)(r0 + i) * a.ld_table + col] = f < a.n_free ? a.free_pages[f] : -1;
+        const unsigned p_end = (unsigned)(total >> 32);
+        for (unsigned f = (unsigned)(carry >> 32) + first; f < p_end;) {
+            const int i = search_last(s_first, nr, (int)f);
+            const int col = (s_cached[i] + a.page - 1) / a.page + ((int)f - s_first[i]);
+            if (col >= 0 && col < a.cols) {
+                a.table[(int64_t)(r0 + i) * a.ld_table + col] = f < (unsigned)a.n_free ? a.free_pages[f] : -1;
+                f += stride;
+            } else {                   // nor do the request's other pages have a column: on to the next request's
+                f += ((unsigned)s_first[i + 1] - f + stride - 1) / stride * stride;
+            }
         }
         carry = total;
         __syncthreads();   // the shared arrays are filled again for the next chunk
     }
     // rows that only fill the step up have no slot: whatever writes the cache leaves them out
-    for (int t = max((int)(unsigned)carry, 0) + blockIdx.x * KS_THREADS + tid; t >= 0 && t < a.T; t += gridDim.x * KS_THREADS) {
+    for (unsigned t = (unsigned)carry + blockIdx.x * KS_THREADS + tid; t < (unsigned)a.T; t += gridDim.x * KS_THREADS) {
         a.slots[t] = -1;
         a.positions[t] = 0;
     }

@@ -137,3 +137,35 @@ def test_captured_step_follows_the_lengths(B):
         row, kv, tab, slots, pos, taken = serving.kv_slots(c, n, None, 16, np.arange(100, 200), before, 64)
         for got, want in zip(out + [table], (row, kv, slots, pos, [taken], tab)):
             assert np.array_equal(got.cpu().numpy(), np.asarray(want))
+
+
+@pytest.mark.parametrize("page", [1 << 16, 1 << 20])
+def test_lengths_whose_sum_passes_32_bits(B, page):
+    """However long the requests behind them are, the first T tokens get their slots; counts stop at 2^31 - 1."""
+    big = 2 ** 31 - 1
+    for seed, cached, fresh in ((20, [5, 0, 0, 7], [3, big, big, 4]), (21, [0, 9], [big, 2]), (22, [100, 0, 0, 0], [2, 2 ** 30, 2 ** 30, 2 ** 30]),
+                                (23, [0] * 2, [big] * 2), (24, [3] + [0] * 700, [5] + [big] * 700), (25, [0] * 300 + [4], [1] * 300 + [big])):
+        s = Step(seed, np.array(cached), np.array(fresh), page, T=400, n_free=600, cols=40)
+        s_tab = s.table.copy()
+        _, tab, out = s.run(B)
+        torch.cuda.synchronize()
+        c, n = np.array(cached, np.int64), np.array(fresh, np.int64)
+        rows, grown = np.concatenate([[0], np.cumsum(n)]), -(-(c + n) // page) - -(-c // page)
+        first = np.concatenate([[0], np.cumsum(grown)])
+        assert np.array_equal(out["row_off"].cpu().numpy()[:len(c) + 1], np.minimum(rows, big))
+        assert np.array_equal(out["kv_len"].cpu().numpy()[:len(c)], np.minimum(c + n, big))
+        assert out["taken"].tolist()[0] == min(int(first[-1]), big)
+        for r in range(len(c)):
+            for j in range(int(grown[r])):
+                col, f = -(-int(c[r]) // page) + j, int(first[r]) + j
+                if col >= 40:
+                    break
+                s_tab[r, col] = s.free[f] if f < 600 else -1
+        assert np.array_equal(tab.cpu().numpy(), s_tab)
+        slots, pos = np.full(400, -1, np.int64), np.zeros(400, np.int64)
+        for t in range(min(400, int(rows[-1]))):
+            r = int(np.searchsorted(rows, t, side="right")) - 1
+            at = int(c[r]) + t - int(rows[r])
+            p = int(s_tab[r, at // page]) if at // page < 40 else -1
+            slots[t], pos[t] = (p * page + at % page if p >= 0 and p * page + at % page < 2 ** 31 else -1), s.base[r] + at
+        assert np.array_equal(out["slots"].cpu().numpy(), slots) and np.array_equal(out["positions"].cpu().numpy(), pos)
