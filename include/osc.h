@@ -563,7 +563,8 @@ typedef struct {
  *   slots, positions: int32 [T]: slot and position of every token; rows from row_off[R] on (a step filled up to a
  *            captured size) get slot -1 and position 0
  *   taken:   int32 [1]: pages taken.  More than n_free: the list ran out; table entries past it and the slots of
- *            their tokens are -1.  Slots of tokens whose page lies past cols, or whose table entry is negative, are -1 too.
+ *            their tokens are -1.  Slots of tokens whose page lies past cols, whose table entry is negative, or which would pass
+ *            2^31 - 1, are -1 too.
  * More than T tokens: only the first T get slots and positions.  A second call with the same inputs gives the same
  * outputs.  Negative lengths count as 0.  What is written (table included) must not overlap anything else (OSC_ERR_INVALID_ARG). */
 osc_status osc_kv_slots(const int32_t* cached, const int32_t* fresh, const int32_t* base, int R, int page_size,

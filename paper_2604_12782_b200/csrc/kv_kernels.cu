@@ -45,6 +45,9 @@ __device__ __forceinline__ int search_last(const int* start, int n, int x) {
     return lo;
 }
 
+// ceil(n / page) for 0 <= n < 2^31: the sum passes 31 bits, but not 32
+__device__ __forceinline__ int pages_of(int n, int page) { return (int)(((unsigned)n + (unsigned)page - 1u) / (unsigned)page); }
+
 // Tokens in the low half, pages in the high half.  Lengths are the caller's: a half that has reached 2^31 - 1 stays there (none of the
 // first T tokens, and no page of the list, lies behind it).  Grouping does not matter to a sum that stops, so it can be scanned.
 __device__ __forceinline__ unsigned long long add_counts(unsigned long long a, unsigned long long b) {
@@ -104,7 +107,7 @@ __global__ void __launch_bounds__(KS_THREADS) kv_slots_kernel(const KvSlotsArgs 
         for (unsigned t = (unsigned)carry + first; t < t_end; t += stride) {
             const int i = search_last(s_row, nr, (int)t);
             const int at = s_cached[i] + ((int)t - s_row[i]);
-            const int col = at / a.page, have = (s_cached[i] + a.page - 1) / a.page;
+            const int col = at / a.page, have = pages_of(s_cached[i], a.page);
             int page = -1;
             if (at >= 0 && col < a.cols) {
                 const int f = s_first[i] + (col - have);
@@ -119,8 +122,8 @@ __global__ void __launch_bounds__(KS_THREADS) kv_slots_kernel(const KvSlotsArgs 
         const unsigned p_end = (unsigned)(total >> 32);
         for (unsigned f = (unsigned)(carry >> 32) + first; f < p_end;) {
             const int i = search_last(s_first, nr, (int)f);
-            const int col = (s_cached[i] + a.page - 1) / a.page + ((int)f - s_first[i]);
-            if (col >= 0 && col < a.cols) {
+            const unsigned col = pages_of(s_cached[i], a.page) + (f - s_first[i]);
+            if (col < (unsigned)a.cols) {
                 a.table[(int64_t)(r0 + i) * a.ld_table + col] = f < (unsigned)a.n_free ? a.free_pages[f] : -1;
                 f += stride;
             } else {                   // nor do the request's other pages have a column: on to the next request's

@@ -169,3 +169,20 @@ def test_lengths_whose_sum_passes_32_bits(B, page):
             p = int(s_tab[r, at // page]) if at // page < 40 else -1
             slots[t], pos[t] = (p * page + at % page if p >= 0 and p * page + at % page < 2 ** 31 else -1), s.base[r] + at
         assert np.array_equal(out["slots"].cpu().numpy(), slots) and np.array_equal(out["positions"].cpu().numpy(), pos)
+
+
+def test_tokens_at_the_end_of_the_range(B):
+    """A request whose cached tokens end within a page of 2^31."""
+    page, cols = 1 << 20, 2048
+    table = torch.arange(cols, dtype=torch.int32, device="cuda")[None].flip(1).contiguous()
+    for cached, fresh in ((2 ** 31 - 9, 4), (2 ** 31 - page - 3, 6), (2 ** 31 - page, 2)):
+        tab, T = table.clone(), 8
+        held = -(-cached // page)
+        tab[0, held:] = -9
+        out = [dev(np.full(n, 5)) for n in (2, 1, T, T, 1)]
+        B.osc_kv_slots(dev([cached]), dev([fresh]), None, page, dev([17, 18]), tab, *out)
+        torch.cuda.synchronize()
+        row, kv, tab_ref, slots, pos, taken = serving.kv_slots([cached], [fresh], None, page, [17, 18], np.where(np.arange(cols) < held, 2047 - np.arange(cols), -9)[None], T)
+        assert (slots[:fresh] < 2 ** 31).all()
+        for got, want in zip(out + [tab], (row, kv, slots, pos, [taken], tab_ref)):
+            assert np.array_equal(got.cpu().numpy(), np.asarray(want))
