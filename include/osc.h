@@ -541,7 +541,7 @@ osc_status osc_nvfp4_rmsnorm_linear_grouped_gather(const osc_weights* w, const v
 
 /* Keys and values of one layer in pages of page_size tokens.  Dev bf16; channel d of head h of the token at place s
  * of page p is element p * page_stride + s * token_stride + h * head_stride + d, for K and V alike (so both
- * [page][token][head][channel] and [page][head][token][channel] buffers fit, and K and V may lie in one buffer).
+ * [page][token][head][channel] and [page][head][token][channel] buffers fit, and K and V may lie in one buffer, in places of their own).
  * head_dim is 64 or 128; strides are elements, multiples of 8; n_pages * page_size < 2^31.  A "slot" is
  * page * page_size + place.  The struct is host memory, read during the call. */
 typedef struct {

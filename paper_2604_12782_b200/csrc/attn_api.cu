@@ -145,6 +145,7 @@ osc_status osc_qk_norm_rope(const void* QKV, int T, int64_t ld, int n_q, const o
                     (long long)n_q * D, (long long)ld_pos);
     if (ld % 8 || ldq % 8 || !aligned16(QKV) || !aligned16(Q) || !aligned16(gamma_q) || !aligned16(gamma_k))
         return fail(OSC_ERR_ALIGN, "QKV, Q, gamma_q and gamma_k must be 16-byte aligned, ld and ldq multiples of 8");
+    if (cache->n_pages > 0 && cache->k == cache->v) return fail(OSC_ERR_INVALID_ARG, "cache: keys and values would be written to the same place");
     if (!(Q == QKV && (T == 1 || ldq == ld)) && rows_meet(bytes_of(QKV, T, (__int128)ld * 2, width * 2), bytes_of(Q, T, (__int128)ldq * 2, (int64_t)n_q * D * 2)))
         return fail(OSC_ERR_INVALID_ARG, "Q overlaps QKV and is not QKV itself with ldq = ld");
     DeviceInfo di;

@@ -215,3 +215,11 @@ def test_attention_outputs_that_overlap_anything_are_refused(B):
         assert call(ws=ok[name]) == -1 and call(ws=ok[name] + size - 16) == -1 and call(ws=ok[name] - need // 16 * 16 + 16) == -1, name
     assert call(lse=ok["ws"] + need - 4) == -1 and call(lse=ok["ws"]) == -1
     assert call(table=ok["ws"] + 4096, ld=100) == -1 and call(P=0, table=ok["O"] + 8) == -1
+
+
+def test_one_place_for_keys_and_values_is_refused_where_they_are_written(B):
+    r = B.RopeStruct(0x8000, None, 128, 1, 0, 1.0)
+
+    def call(k, v):
+        return B._lib.osc_qk_norm_rope(0x70000, 4, 8 * 128, 4, cache(B, k=k, v=v), None, None, 1e-6, r, 0x5000, 4, None, 0x60000, 512, None)
+    assert call(0x1000, 0x1000) == -1
