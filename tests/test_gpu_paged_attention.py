@@ -424,3 +424,55 @@ def test_rows_of_o_in_the_gaps_of_q(B):
                               group_off=c.group_off, prefix_len=c.prefix_len, prefix_table=c.ptable if P else None, max_new=max_new)
         B.osc_sync_check()
         assert same_bits(buf[:, w:], o) and torch.equal(lse, lse2) and same_bits(buf[:, :w], c.q)
+
+
+class Guarded:
+    """A buffer with 64 KB of marked bytes on either side."""
+    EDGE = 1 << 16
+
+    def __init__(self, nbytes, fill):
+        self.all = torch.full((nbytes + 2 * self.EDGE + 512,), 0xA5, dtype=torch.uint8, device="cuda")
+        self.nbytes = nbytes
+        self.all[self.EDGE:self.EDGE + nbytes] = fill
+
+    def view(self, dtype, *shape):
+        return self.all[self.EDGE:self.EDGE + self.nbytes].view(dtype).view(*shape)
+
+    def intact(self):
+        return bool((self.all[:self.EDGE] == 0xA5).all() and (self.all[self.EDGE + self.nbytes:] == 0xA5).all())
+
+
+@pytest.mark.parametrize("max_new", [0, 1])
+@pytest.mark.parametrize("rows,groups,new,group_rows", [
+    ([0, 10, 4, 1000], [0, 3], None, None), ([40, 30, 20, 10], [2, 1], None, None), ([0, 2, 4, 34], [3, 0], None, None),
+    ([-5, 2, 2, 34], [-2, 9], [2, 0, 32], [0, 3]), ([0, 2, 4, 34], [3, 3], [2, 2, 30], [3, 3]), ([-7, -1, 6, 99], [1, 40], [0, 6, 28], [1, 3])])
+def test_unusual_offsets_inside_marked_buffers(B, max_new, rows, groups, new, group_rows):
+    """Offsets outside [0, T] count as cut to it; where they fall no row is written.  Nothing around O, lse and the workspace changes."""
+    c = AttnCase(16, 2, 4, 128, 16, [2, 2, 30], [20, 20, 40], prefix=[50])
+    T, Hq, D = c.T, 8, 128
+    need = B.osc_paged_attention_workspace_bytes(T, Hq, D, 3, 1)
+    go_, gl, gw = Guarded(T * Hq * D * 2, 0), Guarded(T * Hq * 4, 0), Guarded(need, 0xFF)
+    o, lse = go_.view(torch.bfloat16, T, Hq * D), gl.view(torch.float32, T, Hq)
+    o.fill_(7.0)
+    lse.fill_(7.0)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")      # noqa: E731
+    B.osc_paged_attention(c.q, B.KvCache(c.k, c.v), i32(rows), c.kv_len, c.table, o, gw.view(torch.uint8, need), c.scale, lse=lse,
+                          group_off=i32(groups), prefix_len=c.prefix_len, prefix_table=c.ptable, max_new=max_new)
+    B.osc_sync_check()
+    assert go_.intact() and gl.intact() and gw.intact(), "written outside the buffers"
+    if new is None:
+        assert (o == 7.0).all() and (lse == 7.0).all()
+        return
+    c.new, c.groups, c.rows = new, group_rows, np.concatenate([[0], np.cumsum(new)]).astype(int)
+    c.check(o, lse, f"rows {rows}, groups {groups}")
+
+
+@pytest.mark.parametrize("new,max_new", [([1, 1, 1], 1), ([3, 40, 1], 0)])
+def test_tables_without_columns(B, new, max_new):
+    """Requests that hold no key of their own: the prefix alone, or nothing."""
+    for prefix, groups in (([70], [0, 2]), ([], None)):
+        c = AttnCase(46, 2, 4, 128, 16, new, [0, 0, 0], prefix=prefix, groups=groups)
+        c.table = torch.empty(3, 0, dtype=torch.int32, device="cuda")
+        o, lse = c.run(B, max_new=max_new)
+        B.osc_sync_check()
+        c.check(o, lse, f"prefix {prefix}")

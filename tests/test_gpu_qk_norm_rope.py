@@ -172,3 +172,23 @@ def test_queries_beside_qkv_in_one_buffer(B, where):
     x.copy_(data)
     got = run(x, q)
     assert all(torch.equal(a, b) for a, b in zip(want, got)) and torch.equal(x, data)
+
+
+def test_positions_with_a_stride(B):
+    """Rows of positions further apart than there are tokens, as columns of a table of all steps: the same as side by side."""
+    T, Hq, Hk, D = 45, 4, 2, 128
+    g = torch.Generator().manual_seed(4)
+    x = torch.randn(T, (Hq + 2 * Hk) * D, generator=g).to(torch.bfloat16).cuda()
+    rope = B.Rope((1e-4 ** (torch.arange(D // 2) / (D // 2))).cuda(), (torch.arange(D // 2) % 3).to(torch.uint8).cuda())
+    table = torch.randint(0, 9000, (3, T + 30), generator=g).to(torch.int32).cuda()
+    out = []
+    for pos in (table[:, 11:11 + T], table[:, 11:11 + T].contiguous()):
+        k, v = (torch.zeros(4, 16, Hk, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        q = torch.zeros(T, Hq * D, dtype=torch.bfloat16, device="cuda")
+        B.osc_qk_norm_rope(x, Hq, B.KvCache(k, v), q, pos, rope)
+        out.append((q, k, v))
+    assert all(torch.equal(a, b) for a, b in zip(*out))
+    # and not by chance: other positions give other queries
+    q = torch.zeros_like(q)
+    B.osc_qk_norm_rope(x, Hq, B.KvCache(k, v), q, table[:, :T], rope)
+    assert not torch.equal(q, out[0][0])
