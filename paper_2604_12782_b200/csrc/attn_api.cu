@@ -25,29 +25,43 @@ static osc_status check_cache(const osc_kv_cache_t* c) {
     return OSC_OK;
 }
 
-// A matrix in memory: `rows` pieces of `width` bytes, `ld` >= width bytes from one to the next.
-struct ByteRows { __int128 at, rows, ld, width; };
-static ByteRows bytes_of(const void* p, int64_t rows, __int128 ld, __int128 width) {
-    return {(__int128)reinterpret_cast<uintptr_t>(p), rows, ld, width};
+// A matrix in memory: `rows` pieces of `width` bytes, `ld` >= width bytes from one to the next; it ends in front of `end` (which stops
+// at the end of the address space, as strides are the caller's).
+struct ByteRows {
+    uint64_t at, end;
+    int64_t rows, ld, width;
+};
+static ByteRows bytes_of(const void* p, int64_t rows, int64_t ld, int64_t width, int item) {
+    ByteRows b = {reinterpret_cast<uintptr_t>(p), 0, rows, 0, 0};
+    if (rows < 1 || width < 1) return b;
+    uint64_t span = 0;
+    b.width = width * item;
+    bool over = __builtin_mul_overflow(ld, (int64_t)item, &b.ld);
+    if (over) b.ld = INT64_MAX;
+    over &= rows > 1;
+    over |= rows > 1 && __builtin_mul_overflow((uint64_t)(rows - 1), (uint64_t)b.ld, &span);
+    over |= __builtin_add_overflow(span, (uint64_t)b.width, &span) || __builtin_add_overflow(b.at, span, &b.end);
+    if (over) b.end = ~0ull;
+    return b;
 }
-// Whether two matrices share a byte.  Rows of one may lie in the gaps between the other's rows.
-static bool rows_meet(ByteRows a, ByteRows b) {
-    if (a.rows < 1 || b.rows < 1 || a.width < 1 || b.width < 1) return false;
-    if (b.at < a.at) std::swap(a, b);
-    if (b.at >= a.at + (a.rows - 1) * a.ld + a.width) return false;
+// Whether two matrices that reach into one another share a byte.  Rows of one may lie in the gaps between the other's rows.
+static bool rows_cross(const ByteRows& a, const ByteRows& b) {   // b begins inside a
     if (a.rows == 1 && b.rows == 1) return true;
-    if (a.rows == 1) a.ld = b.ld;
-    if (b.rows == 1) b.ld = a.ld;
-    // The same stride: b's first row begins at byte c of a row of a's grid, and reaches the next one (which is there: b begins before a ends) or not.
-    if (a.ld == b.ld) {
-        const __int128 c = (b.at - a.at) % a.ld;
-        return c < a.width || c + b.width > a.ld;
+    // b's rows as places on a's grid
+    const __int128 ld = a.rows > 1 ? a.ld : b.ld, ldb = b.rows > 1 ? b.ld : ld, from0 = b.at - a.at;
+    if (ld == ldb) {     // b's first row begins at byte c of a row of a's grid, and reaches the next one (which is there: b begins before a ends) or not
+        const __int128 c = from0 % ld;
+        return c < a.width || c + b.width > ld;
     }
     for (__int128 i = 0; i < b.rows; ++i) {      // a's first row that ends behind the beginning of b's
-        const __int128 from = b.at + i * b.ld - a.at, r = from < a.width ? 0 : (from - a.width) / a.ld + 1;
-        if (r < a.rows && r * a.ld < from + b.width) return true;
+        const __int128 from = from0 + i * ldb, r = from < a.width ? 0 : (from - a.width) / ld + 1;
+        if (r < a.rows && r * ld < from + b.width) return true;
     }
     return false;
+}
+static bool rows_meet(const ByteRows& a, const ByteRows& b) {
+    if (a.end <= b.at || b.end <= a.at) return false;       // (also where one is empty: its end is 0)
+    return a.at <= b.at ? rows_cross(a, b) : rows_cross(b, a);
 }
 
 // bf16 tensor map of 3 or 4 dimensions, boxes of 64 channels, 128-byte swizzle, zeros outside.  strides in elements.
@@ -146,7 +160,7 @@ osc_status osc_qk_norm_rope(const void* QKV, int T, int64_t ld, int n_q, const o
     if (ld % 8 || ldq % 8 || !aligned16(QKV) || !aligned16(Q) || !aligned16(gamma_q) || !aligned16(gamma_k))
         return fail(OSC_ERR_ALIGN, "QKV, Q, gamma_q and gamma_k must be 16-byte aligned, ld and ldq multiples of 8");
     if (cache->n_pages > 0 && cache->k == cache->v) return fail(OSC_ERR_INVALID_ARG, "cache: keys and values would be written to the same place");
-    if (!(Q == QKV && (T == 1 || ldq == ld)) && rows_meet(bytes_of(QKV, T, (__int128)ld * 2, width * 2), bytes_of(Q, T, (__int128)ldq * 2, (int64_t)n_q * D * 2)))
+    if (!(Q == QKV && (T == 1 || ldq == ld)) && rows_meet(bytes_of(QKV, T, ld, width, 2), bytes_of(Q, T, ldq, (int64_t)n_q * D, 2)))
         return fail(OSC_ERR_INVALID_ARG, "Q overlaps QKV and is not QKV itself with ldq = ld");
     DeviceInfo di;
     if (osc_status s = device_info(&di)) return s;
@@ -220,14 +234,13 @@ osc_status osc_paged_attention(const void* Q, int T, int64_t ldq, int n_q, const
     const AttnLayout l = attn_layout(T, n_q, D, R, P);
     if (workspace_bytes < l.total) return fail(OSC_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, l.total);
     // What is written may lie on nothing else: other CTAs still read it.
-    const __int128 row = (__int128)n_q * D * 2;
+    const int64_t width = (int64_t)n_q * D;
     const struct { ByteRows b; const char* name; } buf[10] = {
-        {bytes_of(O, T, (__int128)ldo * 2, row), "O"}, {bytes_of(lse, lse ? 1 : 0, 0, (int64_t)T * n_q * 4), "lse"},
-        {bytes_of(workspace, 1, 0, l.total), "the workspace"}, {bytes_of(Q, T, (__int128)ldq * 2, row), "Q"},
-        {bytes_of(row_off, 1, 0, ((int64_t)R + 1) * 4), "row_off"}, {bytes_of(kv_len, 1, 0, (int64_t)R * 4), "kv_len"},
-        {bytes_of(table, cols ? R : 0, (__int128)ld_table * 4, (int64_t)cols * 4), "table"},
-        {bytes_of(group_off, P ? 1 : 0, 0, ((int64_t)P + 1) * 4), "group_off"}, {bytes_of(prefix_len, P ? 1 : 0, 0, (int64_t)P * 4), "prefix_len"},
-        {bytes_of(prefix_table, P && prefix_cols ? P : 0, (__int128)ld_prefix * 4, (__int128)prefix_cols * 4), "prefix_table"}};
+        {bytes_of(O, T, ldo, width, 2), "O"}, {bytes_of(lse, lse ? 1 : 0, 0, (int64_t)T * n_q, 4), "lse"},
+        {bytes_of(workspace, 1, 0, (int64_t)l.total, 1), "the workspace"}, {bytes_of(Q, T, ldq, width, 2), "Q"},
+        {bytes_of(row_off, 1, 0, (int64_t)R + 1, 4), "row_off"}, {bytes_of(kv_len, 1, 0, R, 4), "kv_len"}, {bytes_of(table, R, ld_table, cols, 4), "table"},
+        {bytes_of(group_off, P ? 1 : 0, 0, (int64_t)P + 1, 4), "group_off"}, {bytes_of(prefix_len, P ? 1 : 0, 0, P, 4), "prefix_len"},
+        {bytes_of(prefix_table, P, ld_prefix, prefix_cols, 4), "prefix_table"}};
     for (int i = 0; i < 3; ++i)
         for (int j = i + 1; j < 10; ++j)
             if (rows_meet(buf[i].b, buf[j].b)) return fail(OSC_ERR_INVALID_ARG, "%s overlaps %s", buf[i].name, buf[j].name);

@@ -215,6 +215,9 @@ def test_attention_outputs_that_overlap_anything_are_refused(B):
         assert call(ws=ok[name]) == -1 and call(ws=ok[name] + size - 16) == -1 and call(ws=ok[name] - need // 16 * 16 + 16) == -1, name
     assert call(lse=ok["ws"] + need - 4) == -1 and call(lse=ok["ws"]) == -1
     assert call(table=ok["ws"] + 4096, ld=100) == -1 and call(P=0, table=ok["O"] + 8) == -1
+    for ld in (1 << 40, 1 << 62, (1 << 63) - 8):          # rows so far apart that the last ones have no address
+        assert call(ldq=ld, O=ok["Q"] + 512) == -1 and call(ldo=ld, Q=ok["O"] + 512) == -1 and call(ld=ld, table=ok["ws"]) == -1, ld
+        assert call(ldq=ld, ldo=ld, O=ok["Q"] + 512) == -1 and call(ldp=ld, ptab=ok["lse"]) == -1, ld
 
 
 def test_one_place_for_keys_and_values_is_refused_where_they_are_written(B):
