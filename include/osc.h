@@ -613,8 +613,9 @@ osc_status osc_qk_norm_rope(const void* QKV, int T, int64_t ld, int n_q, const o
  * token reaches the rows of the tokens before it in the same request.
  * max_new: most new tokens of any request if the caller knows (1 in a decoding step), 0 otherwise; a choice of kernel, the
  * result holds whatever it says.  P = 0: group_off, prefix_len and prefix_table are not read.
- * Workspace: osc_paged_attention_workspace_bytes with the same n_q and head_dim and with T, R, P at least the call's; what it
- * holds does not matter.  Two calls under way at once need one each.
+ * Workspace: osc_paged_attention_workspace_bytes with the same n_q and head_dim and with T, R, P at least the call's (at least 78 MB with
+ * 128 channels, 40 MB with 64; with prefixes and long prompts several hundred MB); what it holds does not matter.  Two calls under way at once
+ * need one each.
  * Limits (OSC_ERR_SHAPE): T * n_q <= 2^29; the columns of a table hold at most 2^29 keys; R, P and the tables' widths together
  * stay below 2^31 tiles (a tile is at the least 64 keys of one key/value head, or 16 of four, by 16 rows).
  * The cache's, the offsets' and the tables' contents are the caller's: where row_off or group_off falls, no row is written; whatever they hold,

@@ -18,9 +18,10 @@
 //   warps 9, 11    : MMA issue of S, of P V (warp 9 owns TMEM)
 //   warp 10        : the units of the CTA's share, for everyone else
 //
-// Bound by the tensor pipe: 2560 cycles per 128 keys of both tiles, of which the four products are 2080, and 7000 cycles to end a unit and begin
-// the next one (5000 of them the epilogue; a second Q and a second pair of O to hide it behind have no room).  8001 tokens of
-// prompts behind 2048 keys: 375 us, 1.33 PFLOP/s, in a short run; the power limit takes a sixth of that in a loop of seconds.
+// Bound by the tensor pipe and the exponentials alike (72 % of the cycles each): 2560 cycles per 128 keys of both tiles, of which the four
+// products are 2080 and the exponentials 2048, and 7000 cycles to end a unit and begin the next one (5000 of them the epilogue; a second Q and a second pair of O
+// to hide it behind have no room).  8001 tokens of prompts behind 2048 keys: 375 us from the plan's end on, 1.33 PFLOP/s, replayed from a graph in a short
+// run (402 cold, under the profiler); the power limit takes a sixth of that in a loop of seconds.
 //
 // P V with the weights of the running maximum as it stands: O is rescaled in TMEM only when the maximum has moved by
 // more than 2^8 (see AT_SLACK), by the softmax threads themselves, between the P V before and the one to come.
@@ -475,7 +476,7 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                             p0 = exp2_approx(p0);
                             p1 = exp2_approx(p1);
                             sum[(e / 2) & 1] = add2(sum[(e / 2) & 1], pack2(p0, p1));
-                            pk[j][e / 2] = bf162_bits(__floats2bfloat162_rn(p0, p1));
+                            pk[j][e / 2] = bf162_bits(__floats2bfloat162_rn(p0, p1));      // bf16 as V is: operands of one type
                         }
                     if (i > 0) {      // the P V before has read P, and O is not being written
                         if (!wait_bounded(&pv_done[s], pv_ph, abort_flag, 82)) goto done;

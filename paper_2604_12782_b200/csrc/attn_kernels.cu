@@ -229,16 +229,18 @@ __device__ __forceinline__ int head_span(const AttnArgs& a, const Segment& g) {
 __device__ __forceinline__ int share_tiles(int N, int ctas, int least) { return max((int)(((int64_t)N + ctas - 1) / ctas), least); }
 // Least share of the few-row line.  Where there is less work than CTAs, q tiles to a share take about 0.62 q us, and the t / q pieces of a
 // row whose keys are t tiles 0.85 us for every 16 in the join: the sum is least at q = sqrt(0.086 t).  t is taken as the mean over the
-// segments.  One request of 100 / 300 / 600 / 1500 / 4000 keys, 8 heads: 7.6 / 8.2 / 8.9 / 11.1 / 13.5 us; with four tiles for all
-// 10.7 / 10.9 / 10.9 / 11.5 / 13.7, with one for all 7.6 / 8.1 / 9.1 / 12.3 / 15.4.
+// segments.  One request of 100 / 300 / 600 / 1500 / 4000 keys, 8 heads of 128 channels, from CUDA graphs on three inputs in turn:
+// 10.3 / 10.3 / 11.7 / 14.4 / 16.4 us; with four tiles for all 12.4 / 13.0 / 13.6 / 14.4 / 16.4, with one for all 10.3 / 10.3 / 12.3 / 14.5 / 18.6.
+// (The constants are those of 128 channels; other head sizes and counts were not tuned for.)
 __device__ __forceinline__ int few_min_tiles(const AttnArgs& a, int n) {
     return max((int)(sqrtf(0.086f * (float)n / ((float)(a.P + a.R) * (float)FewUnits::heads(a))) + 0.5f), 1);
 }
 constexpr int AT_WIDE_MIN_TILES = 4;
 // Shares of the two lines of a step that has both (nf, nw tiles).  The tcgen05 kernel is bound by arithmetic, the few-row kernel by
 // memory, and both are resident at once: the first gets as many CTAs as its part of the SMs' time, the second runs on the other
-// SMs.  A tcgen05 tile takes an SM about 1.9 us, a few-row tile 0.65 us (256 requests behind 16384 keys: 150 us like this, 170 us with
-// all SMs on one kernel after the other; 66 tcgen05 CTAs 150, 50 181, 84 157).  How long either takes is only known that roughly, so the
+// SMs.  With 128 channels and the other kernel beside it, a place on the tcgen05 line takes an SM about 1.75 us (1.3, 2560 cycles, where it has
+// the machine to itself), a few-row tile 0.6 us: three to one.  (256 requests behind 16384 keys when this was chosen: 150 us like this, 170 us with
+// all SMs on one kernel after the other; 66 tcgen05 CTAs 150, 50 181, 84 157.  64 channels were not tuned for.)  How long either takes is only known that roughly, so the
 // few-row shares are several rounds of the SMs left over: those that the tcgen05 kernel leaves early take from the last round.
 __device__ __forceinline__ void share_lines(const AttnArgs& a, int nf, int nw, int32_t* share) {
     const int sms = a.wide_ctas;
@@ -589,8 +591,9 @@ struct FewCfg {
 // It needs nothing of the tcgen05 kernel that may be launched in front of it, so it begins (`early`) on every SM that has no
 // tcgen05 CTA or whose CTA has ended.  Its last CTA alone waits for that kernel before it ends: whatever comes behind waits for both,
 // and no SM is held by CTAs that have nothing left to do (32 requests behind 4096 keys: 43 -> 38 us).
-// Without prefixes and prompts, up to FEW_SELF requests, every CTA lays out the line for itself in shared memory (SELF) and
-// no plan kernel runs: the launch and its two trips through L2 would be a third of the smallest calls.
+// Without prefixes and prompts, up to FEW_SELF requests, with a multiple of four key/value heads, every CTA lays out the line for itself in
+// shared memory (SELF) and no plan kernel runs: the launch and its two trips through L2 would be a third of the smallest calls.  (With other
+// head counts the warps' join buffers would come on top: 124 KB for one head of 128 channels, one CTA to an SM instead of two.)
 // The loads run on over the ends of units.  A page number is fetched one tile ahead of the loads that need it.
 template <int D, int HW, bool SELF>
 __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnArgs a, bool early) {
@@ -777,6 +780,8 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
                         for (int j = 0; j < NJ; ++j) { o[j][2 * hlf] *= f; o[j][2 * hlf + 1] *= f; }
                     }
                 }
+                // Weights in bf16 for P V: the tensor cores take both operands in one type, and V is bf16.  Each is off by at most 2^-8 of itself, either
+                // way, as the output is from its own rounding (error of the outputs 0.0023 of their size, 0.0017 with weights in fp32); l sums them unrounded.
                 uint32_t pf[4];
                 float p[2][4];
 #pragma unroll
@@ -882,7 +887,7 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
 
 // ------------------------------------------------------------------------------------------------- join
 // Joins the pieces of rows whose keys were not all in one unit of one share, in the order of the lines (so the result does not depend on
-// which CTA was first), one warp to a row.  Three kinds of blocks, because the rows to be joined are not known on the host and looking at
+// which CTA was first), one warp to a row.  Two kinds of blocks, because the rows to be joined are not known on the host and looking at
 // every row costs more than the joining (262 us for 8001 tokens of prompts against 1 ms of attention, when it was done that way):
 //   units that the end of a share cuts, as the attention kernels told them: blocks for every share of either line;
 //   rows with two sources (prefix and own keys): blocks over the tokens, only launched where there are prefixes.
@@ -963,7 +968,7 @@ struct JoinGrid {
     int few_split;           // few_ctas x few_split: a part of the rows of a cut few-row unit each
 };
 
-constexpr int64_t AT_JOIN_FEW_ROWS = 4096;
+constexpr int64_t AT_JOIN_FEW_ROWS = 4096;     // between 224 and 256032 rows of the two steps above
 template <int D, int FLIGHT>
 __global__ void __launch_bounds__(AT_JOIN_THREADS, FLIGHT > 8 ? 2 : 3) attn_join_kernel(const AttnArgs a, const JoinGrid grid) {
     grid_launch_dependents();

@@ -173,6 +173,8 @@ cudaError_t launch_kv_slots(const KvSlotsArgs& a, int num_sms, cudaStream_t st) 
 // (Batches of eight, or the whole token on its way into shared memory by one bulk copy with eight warps an SM, were
 // slower: 42 and 57 us for 8192 tokens, because the chains of a step want many warps.  Calling a warp's whole part into L2 first changed
 // nothing: HBM, reading and writing, is 85 % busy.)
+// With fewer heads to a token (32 + 2 x 4, three axes, 5001 tokens: 23.1 us, 0.57 of the issue slots, long scoreboard first among the stalls) the
+// chain positions -> angles -> factors in front of the first head's load shows, and key and value steps fill half a batch.
 // The angle is reduced in double (position * frequency passes 2^24 for far positions, where fp32 would lose the
 // turn entirely) to half turns in [-1, 1], whose sine and cosine are taken in fp32: an error of 2^-23 against a
 // rounding step of 2^-8.
@@ -406,9 +408,10 @@ static cudaError_t launch_qk_norm_rope_mode(QkNormRopeArgs a, int num_sms, cudaS
     const int hps = 32 / (D / 8);
     const int steps = (a.Hq + hps - 1) / hps + 2 * ((a.Hk + hps - 1) / hps);
     // A warp per token for as many rounds of the machine's resident warps as are full.  The tokens behind them (all, where there are few) are spread
-    // over more warps while those fill half of the machine: the last round is then as short as its work (5001 tokens, 1.06 rounds: 23.4 us,
-    // 27.0 with a warp per token).  More is worse, every warp works out the angles again: 8192 tokens in 1 / 2 / 4 / 8 warps each
-    // 39.4 / 37.0 / 46.4 / 66.5 us, 5001 tokens 27.8 / 29.9 / 35.8 / 46.8, 256 tokens 10.4 / 6.3 / 6.3 / 6.3.
+    // over more warps while those fill half of the machine: the last round is then as short as its work.  From CUDA graphs on three inputs
+    // in turn, 32 + 2 x 8 heads of 128: 5001 tokens (1.06 rounds) 26.7 us like this; all of them in 1 / 2 / 4 / 8 warps each 30.8 / 28.6 / 32.8 /
+    // 43.1, because every warp works out the angles again; 8192 tokens (1.73 rounds) 37.4 like this, 37.4 / 39.0 / 47.7 / 67.5; 256 tokens
+    // 6.2 like this, 10.3 / 6.2 / 6.2 / 6.2.
     const int resident = num_sms * QR_WARPS * (MODE == ROPE_SPLIT ? QR_CTAS : QR_CTAS - 2);
     a.whole = a.T / resident * resident;
     const int rest = a.T - a.whole;
