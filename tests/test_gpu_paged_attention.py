@@ -476,3 +476,43 @@ def test_tables_without_columns(B, new, max_new):
         o, lse = c.run(B, max_new=max_new)
         B.osc_sync_check()
         c.check(o, lse, f"prefix {prefix}")
+
+
+def test_calls_of_all_kinds_share_a_workspace_one_behind_the_other(B):
+    """Layers and steps of a model back to back on one stream, by every way of planning, with one workspace between them: the same bits as with
+    the device idle between calls."""
+    kinds = [(dict(Hk=4, G=4, D=128, page=16, new=[1] * 7, kv=[900, 3, 40, 2000, 1, 77, 600]), 1),
+             (dict(Hk=2, G=4, D=128, page=16, new=[1] * 30 + [70], kv=[300 + 7 * i for i in range(31)], prefix=[1500]), 0),
+             (dict(Hk=2, G=8, D=64, page=32, new=[1] * 12, kv=[50 * i for i in range(12)], prefix=[700, 90], groups=[0, 5, 11]), 1),
+             (dict(Hk=8, G=4, D=128, page=64, new=[400, 1, 300], kv=[700, 900, 300]), 0),
+             (dict(Hk=1, G=16, D=64, page=16, new=[1] * 3, kv=[4000, 10, 0]), 1),
+             (dict(Hk=2, G=4, D=128, page=16, new=[260, 300], kv=[500, 300], prefix=[333]), 0)]
+    cases = [(AttnCase(50 + i, **kw), max_new) for i, (kw, max_new) in enumerate(kinds * 2)]
+    ws = torch.empty(max(B.osc_paged_attention_workspace_bytes(c.T, c.Hk * c.G, c.D, len(c.new), len(c.prefix)) for c, _ in cases),
+                     dtype=torch.uint8, device="cuda")
+    caches = [B.KvCache(c.k, c.v) for c, _ in cases]
+
+    def outputs():
+        return [(torch.full((c.T, c.Hk * c.G * c.D), 7.0, dtype=torch.bfloat16, device="cuda"), torch.full((c.T, c.Hk * c.G), 7.0, device="cuda"))
+                for c, _ in cases]
+
+    def call(i, out):
+        c, max_new = cases[i]
+        B.osc_paged_attention(c.q, caches[i], c.row_off, c.kv_len, c.table, out[i][0], ws, c.scale, lse=out[i][1], group_off=c.group_off,
+                              prefix_len=c.prefix_len, prefix_table=c.ptable if c.prefix else None, max_new=max_new)
+    alone = outputs()
+    for i, (c, _) in enumerate(cases):
+        ws.fill_(0xFF)
+        call(i, alone)
+        B.osc_sync_check()
+        if i < len(kinds):
+            c.check(*alone[i], f"kind {i}")
+    rng = np.random.default_rng(0)
+    for _ in range(20):
+        out = outputs()
+        torch.cuda.synchronize()
+        for i in rng.permutation(len(cases)):
+            call(int(i), out)
+        B.osc_sync_check()
+        for i, ((o, lse), (ro, rl)) in enumerate(zip(out, alone)):
+            assert same_bits(o, ro) and torch.equal(lse, rl), f"call {i}"
