@@ -185,8 +185,8 @@ def test_queries_that_overlap_qkv_without_being_it_are_refused(B):
     assert call(qkv + 16, T=1) == -1 and call(qkv, ldq=520) == -1
     # rows of Q in the gaps of QKV's, of the same stride and of another: those that reach into a row
     assert call(qkv + 2048 + 1040, ldq=2048, ld=2048) == -1 and call(qkv + 2048 - 16, ldq=2048, ld=2048) == -1
-    assert call(qkv + 2048, ldq=3072, ld=2048) == -1 and call(qkv + 2048 + 1040, ldq=4096, ld=2048) == -1
-    assert call(qkv - 1024 + 16, ldq=2048, ld=2048) == -1 and call(qkv - 4096 - 1024, ldq=3072, ld=2048) == -1
+    assert call(qkv + 2048, ldq=2560, ld=2048) == -1 and call(qkv + 2048 + 1040, ldq=4096, ld=2048) == -1
+    assert call(qkv - 1024 + 16, ldq=2048, ld=2048) == -1 and call(qkv - 4096 - 1024, ldq=2560, ld=2048) == -1
 
 
 def test_attention_outputs_that_overlap_anything_are_refused(B):
