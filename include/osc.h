@@ -54,8 +54,9 @@
  * (RMSNorm + Algorithm 2, SwiGLU + per-token FP8), the grouped form with the MoE dispatch fused behind the
  * quantizer, the MXFP8 form of the fallback, the NVFP4 / G = 16 form of the OSC path, the dynamic-protection
  * control group of Section 4.2 (a measured baseline), offline profiling (Algorithm 1), osc_linear_static
- * (a deployment aid), and what a served layer runs between its QKV projection and o_proj (pages and slots of a
- * key/value cache, norm and rotation of the heads, attention with shared prefixes).
+ * (a deployment aid), what a served layer runs between its QKV projection and o_proj (pages and slots of a
+ * key/value cache, norm and rotation of the heads, attention with shared prefixes), and what a step adds to that in which a
+ * request has more than one continuation (drafted trees, beams).
  *
  * Kernel selection is internal and depends only on the shape.  Few rows (M <= 32; <= 64 for layers with more
  * 128-feature tiles than SMs or a long K loop; <= 256 for long K loops with few tiles) run on a
@@ -626,6 +627,88 @@ osc_status osc_paged_attention(const void* Q, int T, int64_t ldq, int n_q, const
                                int P, const int32_t* group_off, const int32_t* prefix_len, const int32_t* prefix_table,
                                int prefix_cols, int64_t ld_prefix, int max_new, float scale, void* O, int64_t ldo, float* lse,
                                void* workspace, size_t workspace_bytes, void* stream);
+
+/* ----------------------------- requests with more than one continuation: drafted trees, beams */
+
+/* A step that verifies drafted tokens gives every request its whole tree of them as new tokens: osc_kv_slots and osc_qk_norm_rope as for any new
+ * tokens (positions from osc_tree_mask), osc_tree_attention per layer, osc_token_logprobs on the logits, and osc_kv_compact for the tokens that were
+ * accepted (osc_kv_trim for pages that are no longer needed).  A step of a beam search gives the pages of beams that end back (osc_kv_trim), forks
+ * rows of the page table (osc_kv_fork) and copies the pages that are not full (osc_kv_copy_pages). */
+#define OSC_TREE_WORDS 32
+
+/* Ancestors and positions of the tokens of drafted trees (once per step).
+ *   parents: dev int32 [T]: the token's parent as an index among its request's new tokens, smaller than its own; -1: a root (its parent is the last
+ *            token in the cache).  Anything else: the token is not there, nor are its descendants.
+ *   row_off: dev int32 [R + 1], rising from 0, as osc_kv_slots writes it;  base: dev int32 [R] or null (0): position of a root
+ *   mask:    uint32 [T][ld_mask], `words` columns (1 .. OSC_TREE_WORDS): bit m % 32 of word m / 32 of a token's row is set if the request's new token
+ *            m is the token itself or an ancestor of it.  Tokens that are not there, from the request's (32 * words)-th on, or in rows from
+ *            row_off[R] on get an empty row.
+ *   positions: int32 [T] or null: base + number of ancestors; 0 for tokens with an empty row.
+ * Neither output may overlap anything else (OSC_ERR_INVALID_ARG). */
+osc_status osc_tree_mask(const int32_t* parents, const int32_t* row_off, const int32_t* base, int R, int T, uint32_t* mask, int words,
+                         int64_t ld_mask, int32_t* positions, void* stream);
+
+/* osc_paged_attention with a mask among the new tokens instead of their order.  A row sees the keys of its group's prefix, the request's first
+ * kv_len[r] - n own keys, and of the n new tokens those whose bits are set in its row of the mask (dev uint32 [T][ld_mask], 1 .. OSC_TREE_WORDS words:
+ * any bits, as osc_tree_mask writes them or not); new tokens from 32 * words on are seen by nobody.  Where kv_len[r] < n the first n - kv_len[r] new
+ * tokens have no key.  A row that sees nothing gives 0 and -inf, and nothing that a row does not see reaches it, Inf and NaN among the values
+ * included.  Everything else as in osc_paged_attention, the workspace (osc_paged_attention_workspace_bytes) too; the mask must not overlap what is written. */
+osc_status osc_tree_attention(const void* Q, int T, int64_t ldq, int n_q, const osc_kv_cache_t* cache, int R, const int32_t* row_off,
+                              const int32_t* kv_len, const int32_t* table, int cols, int64_t ld_table, int P, const int32_t* group_off,
+                              const int32_t* prefix_len, const int32_t* prefix_table, int prefix_cols, int64_t ld_prefix, const uint32_t* mask,
+                              int words, int64_t ld_mask, int max_new, float scale, void* O, int64_t ldo, float* lse, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
+/* Scores of tokens from rows of logits (dev, OSC_BF16 or OSC_F32 [T, ld], V columns; any ld >= V, aligned to an element), with y = scale * logit:
+ *   logprob: float [T][n_ids]: y[id] - lse for the given ids (dev int32 [T][ld_ids]); -inf for an id outside 0 .. V - 1
+ *   lse:     float [T] or null: ln sum_j exp(y_j)
+ *   entropy: float [T] or null: -sum_j p_j ln p_j with p_j = exp(y_j - lse), in nats
+ *   top_ids, top_logprobs: int32 / float [T][top_k]: the top_k <= 32 largest logits in falling order, the lower index first among equal ones
+ *            (0 and -0 are equal), and their log probabilities; behind the V-th -1 and -inf
+ * n_ids = 0 and top_k = 0 leave those out.  scale (one over the temperature) is positive.  Sums in fp32, relative to the row's maximum.  Logits of
+ * -inf have probability 0; a row of nothing else gives -inf, and 0 for the entropy.  A NaN or +inf in a row makes its lse, entropy and log
+ * probabilities NaN (of ids in range); NaN comes last among the alternatives.  No output may overlap anything else (OSC_ERR_INVALID_ARG). */
+enum { OSC_BF16 = 0, OSC_F32 = 1 };
+osc_status osc_token_logprobs(const void* logits, int dtype, int T, int V, int64_t ld, float scale, const int32_t* ids, int n_ids, int64_t ld_ids,
+                              float* logprob, float* lse, float* entropy, int top_k, int32_t* top_ids, float* top_logprobs, void* stream);
+
+/* Accepted tokens moved together behind the context, keys and values of all layers in one call.  Of request r's n = row_off[r + 1] - row_off[r] new
+ * tokens, the last n of kv_len[r], the one with index keep[r][d] goes to the place of new token d; the indices rise, and the list ends
+ * where it does not (or at an index outside 0 .. n - 1), at n_keep[r] or at keep_cols entries.
+ *   layers: host array of n_layers caches of one shape and strides (k and v of their own each), read during the call
+ *   keep: dev int32 [R][ld_keep];  n_keep: dev int32 [R];  new_len: int32 [R]: kv_len[r] - n + tokens kept (it must not overlap the inputs)
+ * Places whose page is not in the table (entries outside 0 .. n_pages - 1, or past cols) are left out.  Pages of new tokens belong to one
+ * request only.  R <= 2^20. */
+osc_status osc_kv_compact(const osc_kv_cache_t* layers, int n_layers, int R, const int32_t* row_off, const int32_t* kv_len, const int32_t* table,
+                          int cols, int64_t ld_table, const int32_t* keep, int keep_cols, int64_t ld_keep, const int32_t* n_keep,
+                          int32_t* new_len, void* stream);
+
+/* Pages given back: request r shrinks from from_len[r] to to_len[r] tokens (0: it ends), and the pages of columns ceil(to / page_size) ..
+ * ceil(from / page_size) - 1 of its table row leave it; those entries become -1 (entries outside 0 .. n_pages - 1 only do that).
+ *   refs:  dev int32 [n_pages] or null: number of table rows that hold a page; falls by one for every row that gives it back, not below 0.  A
+ *          page is freed when it reaches 0.  null: every page has one holder.
+ *   freed: int32 [n_pages]: the freed pages in rising order, n_freed: int32 [1] of them; the rest is left as it is
+ * A second call with the same inputs finds nothing to give back.  n_pages <= 12 million.  What is written (table and refs included) must not overlap anything
+ * else (OSC_ERR_INVALID_ARG). */
+osc_status osc_kv_trim(const int32_t* from_len, const int32_t* to_len, int R, int page_size, int32_t* table, int cols, int64_t ld_table,
+                       int32_t* refs, int n_pages, int32_t* freed, int32_t* n_freed, void* stream);
+
+/* Forks of requests: table row dst[i] (dev int32 [n], rows of the R of the table) becomes a second holder of the len[src[i]] tokens of row src[i].  Its full
+ * pages are shared: their entries are copied and refs (as in osc_kv_trim, null: not kept) rises by one.  Tokens on a page that is not full get a page of their
+ * own, from free_pages [n_free] in the order of the forks (its count rises by one too), and are to be copied: copy_from[i], copy_to[i] and
+ * copy_used[i] (int32 [n]) are what osc_kv_copy_pages takes, -1, -1 and 0 where there is nothing to copy.  len[dst[i]] = len[src[i]]; entries of the row behind
+ * these pages are left as they are, and what it held before is not given back (osc_kv_trim does that).
+ *   taken: int32 [1]: pages taken; more than n_free: the list ran out, and the entries of forks past it are -1
+ * No row is in dst twice, nor in both src and dst.  Pairs with a row outside 0 .. R - 1, or with src = dst, are left out (copy -1, -1, 0).  What is written
+ * must not overlap anything else (OSC_ERR_INVALID_ARG). */
+osc_status osc_kv_fork(const int32_t* src, const int32_t* dst, int n, int32_t* len, int R, int page_size, const int32_t* free_pages, int n_free,
+                       int32_t* table, int cols, int64_t ld_table, int32_t* refs, int n_pages, int32_t* copy_from, int32_t* copy_to,
+                       int32_t* copy_used, int32_t* taken, void* stream);
+
+/* The first used[i] places (dev int32 [n], null: all) of page from[i] to page to[i], keys and values of all layers (as in osc_kv_compact).  Pairs with a page
+ * outside 0 .. n_pages - 1, or with from = to, are left out.  A page that is copied to appears nowhere else in the lists.  n <= 2^22. */
+osc_status osc_kv_copy_pages(const osc_kv_cache_t* layers, int n_layers, const int32_t* from, const int32_t* to, const int32_t* used, int n,
+                             void* stream);
 
 #ifdef __cplusplus
 }

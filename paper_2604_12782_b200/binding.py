@@ -155,6 +155,14 @@ _SIGS = {
     "osc_paged_attention_workspace_bytes": (_i, [_i, _i, _i, _i, _i, C.POINTER(_sz)]),
     "osc_paged_attention": (_i, [_vp, _i, _i64, _i, C.POINTER(KvCacheStruct), _i, _vp, _vp, _vp, _i, _i64, _i, _vp, _vp, _vp, _i,
                                  _i64, _i, C.c_float, _vp, _i64, _vp, _vp, _sz, _vp]),
+    "osc_tree_mask": (_i, [_vp, _vp, _vp, _i, _i, _vp, _i, _i64, _vp, _vp]),
+    "osc_tree_attention": (_i, [_vp, _i, _i64, _i, C.POINTER(KvCacheStruct), _i, _vp, _vp, _vp, _i, _i64, _i, _vp, _vp, _vp, _i,
+                                _i64, _vp, _i, _i64, _i, C.c_float, _vp, _i64, _vp, _vp, _sz, _vp]),
+    "osc_token_logprobs": (_i, [_vp, _i, _i, _i, _i64, C.c_float, _vp, _i, _i64, _vp, _vp, _vp, _i, _vp, _vp, _vp]),
+    "osc_kv_compact": (_i, [_vp, _i, _i, _vp, _vp, _vp, _i, _i64, _vp, _i, _i64, _vp, _vp, _vp]),
+    "osc_kv_trim": (_i, [_vp, _vp, _i, _i, _vp, _i, _i64, _vp, _i, _vp, _vp, _vp]),
+    "osc_kv_fork": (_i, [_vp, _vp, _i, _vp, _i, _i, _vp, _i, _vp, _i, _i64, _vp, _i, _vp, _vp, _vp, _vp, _vp]),
+    "osc_kv_copy_pages": (_i, [_vp, _i, _vp, _vp, _vp, _i, _vp]),
 }
 for _name, (_res, _args) in _SIGS.items():
     _f = getattr(_lib, _name)
@@ -967,3 +975,152 @@ def osc_paged_attention(Q: torch.Tensor, cache: KvCache, row_off, kv_len, table,
         _check(_lib.osc_paged_attention(Q.data_ptr(), T, ldq, n_q, cache.c, R, row_off.data_ptr(), kv_len.data_ptr(), table.data_ptr(), cols,
                                         table.stride()[0], 0, None, None, None, 0, 0, max_new, scale, O.data_ptr(), ldo, _addr(lse),
                                         workspace.data_ptr(), workspace.numel(), _stream(stream)))
+
+
+class KvLayers:
+    """The caches of a model's layers (KvCache, all of one shape and strides), for calls that move tokens in all of them."""
+
+    def __init__(self, caches):
+        self.caches = list(caches)
+        if not self.caches:
+            raise ValueError("KvLayers: no cache")
+        self.first = self.caches[0]
+        self.device = self.first.device
+        if any(c.device != self.device for c in self.caches):
+            raise ValueError("KvLayers: caches on several devices")
+        self.c = (KvCacheStruct * len(self.caches))(*[c.c for c in self.caches])
+
+    def __len__(self):
+        return len(self.caches)
+
+
+def osc_tree_mask(parents, row_off, base, mask, positions=None, stream=None):
+    """Ancestors (mask [T, words], bits) and positions [T] of drafted tokens from their parents [T]; row_off [R + 1], base [R] or None.  All int32."""
+    dev, i32 = _device_of(parents), torch.int32
+    if _bad(i32, dev, parents, row_off, base, positions) or _bad_rows(i32, dev, mask):
+        _refuse(i32, 1, dev, parents=parents, row_off=row_off, base=base, positions=positions)
+        _refuse(i32, 2, dev, mask=mask)
+        raise ValueError("osc_tree_mask: vectors must be contiguous")
+    T, R = parents.numel(), row_off.numel() - 1
+    rows, words = mask.shape
+    if R < 0 or rows != T or (base is not None and base.numel() < R) or (positions is not None and positions.numel() < T):
+        raise ValueError("osc_tree_mask: lengths do not belong together")
+    _check(_lib.osc_tree_mask(parents.data_ptr(), row_off.data_ptr(), _addr(base), R, T, mask.data_ptr(), words, mask.stride()[0] if T > 1 else words,
+                              _addr(positions), _stream(stream)))
+
+
+def osc_tree_attention(Q: torch.Tensor, cache: KvCache, row_off, kv_len, table, mask, O: torch.Tensor, workspace: torch.Tensor, scale: float,
+                       lse=None, group_off=None, prefix_len=None, prefix_table=None, max_new: int = 0, stream=None):
+    """osc_paged_attention with a mask among the new tokens: int32 [T, words], bit m of a token's row set where it sees its request's new token m."""
+    dev, i32, bf16 = _device_of(Q), torch.int32, torch.bfloat16
+    if (_bad_rows(bf16, dev, Q, O) or _bad(i32, dev, row_off, kv_len, prefix_len, group_off) or _bad_rows(i32, dev, table, prefix_table, mask) or
+            _bad(torch.float32, dev, lse) or _bad(torch.uint8, dev, workspace) or cache.device != dev):
+        _refuse(bf16, 2, dev, Q=Q, O=O)
+        _refuse(i32, 1, dev, row_off=row_off, kv_len=kv_len, prefix_len=prefix_len, group_off=group_off)
+        _refuse(i32, 2, dev, table=table, prefix_table=prefix_table, mask=mask)
+        _refuse(torch.float32, 2, dev, lse=lse)
+        _refuse(torch.uint8, 1, dev, workspace=workspace)
+        raise ValueError(f"osc_tree_attention: vectors and lse must be contiguous, the cache (cuda:{cache.device}) on the device of Q, cuda:{dev}")
+    T, width = Q.shape
+    R, (rows, cols), n_q = kv_len.numel(), table.shape, width // cache.head_dim
+    P = prefix_len.numel() if prefix_len is not None else 0
+    if (width % cache.head_dim or O.shape != Q.shape or row_off.numel() < R + 1 or rows < R or mask.shape[0] != T or
+            (P and (group_off is None or prefix_table is None or group_off.numel() < P + 1 or prefix_table.shape[0] < P)) or
+            (lse is not None and lse.numel() != T * n_q)):
+        raise ValueError("osc_tree_attention: shapes do not belong together")
+    words = mask.shape[1]
+    ldq, ldo, ldm = (Q.stride()[0], O.stride()[0], mask.stride()[0]) if T > 1 else (width, width, words)
+    prefix = (P, group_off.data_ptr(), prefix_len.data_ptr(), prefix_table.data_ptr(), prefix_table.shape[1],
+              prefix_table.stride()[0]) if P else (0, None, None, None, 0, 0)
+    _check(_lib.osc_tree_attention(Q.data_ptr(), T, ldq, n_q, cache.c, R, row_off.data_ptr(), kv_len.data_ptr(), table.data_ptr(), cols,
+                                   table.stride()[0], *prefix, mask.data_ptr(), words, ldm, max_new, scale, O.data_ptr(), ldo, _addr(lse),
+                                   workspace.data_ptr(), workspace.numel(), _stream(stream)))
+
+
+def osc_token_logprobs(logits: torch.Tensor, ids=None, logprob=None, scale: float = 1.0, lse=None, entropy=None, top_ids=None, top_logprobs=None,
+                       stream=None):
+    """Log probabilities (float32 [T, n_ids]) of the given tokens (int32 [T, n_ids]) under logits (bf16 or float32 [T, V]) times scale; lse and
+    entropy float32 [T]; the best alternatives, top_ids int32 [T, k] and top_logprobs float32 [T, k].  What is None is left out."""
+    dev, i32, f32 = _device_of(logits), torch.int32, torch.float32
+    if logits.dtype not in (torch.bfloat16, f32):
+        raise ValueError(f"osc_token_logprobs: logits are {logits.dtype}, must be bfloat16 or float32")
+    if _bad_rows(logits.dtype, dev, logits) or _bad_rows(i32, dev, ids) or _bad(i32, dev, top_ids) or _bad(f32, dev, logprob, lse, entropy, top_logprobs):
+        _refuse(logits.dtype, 2, dev, logits=logits)
+        _refuse(i32, 2, dev, ids=ids, top_ids=top_ids)
+        _refuse(f32, 2, dev, logprob=logprob, top_logprobs=top_logprobs)
+        _refuse(f32, 1, dev, lse=lse, entropy=entropy)
+        raise ValueError("osc_token_logprobs: what is written must be contiguous")
+    T, V = logits.shape
+    n_ids, k = ids.shape[1] if ids is not None else 0, top_ids.shape[1] if top_ids is not None else 0
+    if ((ids is None) != (logprob is None) or (ids is not None and (ids.shape[0] != T or logprob.shape != ids.shape)) or
+            (top_ids is None) != (top_logprobs is None) or (top_ids is not None and (top_ids.shape[0] != T or top_logprobs.shape != top_ids.shape)) or
+            (lse is not None and lse.numel() != T) or (entropy is not None and entropy.numel() != T)):
+        raise ValueError("osc_token_logprobs: shapes do not belong together")
+    ld, ld_ids = (logits.stride()[0], ids.stride()[0] if ids is not None else 0) if T > 1 else (V, n_ids)
+    _check(_lib.osc_token_logprobs(logits.data_ptr(), 1 if logits.dtype is f32 else 0, T, V, ld, scale, _addr(ids), n_ids, ld_ids, _addr(logprob),
+                                   _addr(lse), _addr(entropy), k, _addr(top_ids), _addr(top_logprobs), _stream(stream)))
+
+
+def osc_kv_compact(layers: KvLayers, row_off, kv_len, table, keep, n_keep, new_len, stream=None):
+    """Accepted tokens moved together in all layers: keep [R, most] indices among the new tokens, n_keep [R] of them; new_len [R] is written.  All int32."""
+    dev, i32 = _device_of(kv_len), torch.int32
+    if _bad(i32, dev, row_off, kv_len, n_keep, new_len) or _bad_rows(i32, dev, table, keep) or layers.device != dev:
+        _refuse(i32, 1, dev, row_off=row_off, kv_len=kv_len, n_keep=n_keep, new_len=new_len)
+        _refuse(i32, 2, dev, table=table, keep=keep)
+        raise ValueError(f"osc_kv_compact: vectors must be contiguous, the layers (cuda:{layers.device}) on the device of kv_len, cuda:{dev}")
+    R = kv_len.numel()
+    if row_off.numel() < R + 1 or n_keep.numel() != R or new_len.numel() < R or table.shape[0] < R or keep.shape[0] != R:
+        raise ValueError("osc_kv_compact: lengths do not belong together")
+    _check(_lib.osc_kv_compact(layers.c, len(layers.caches), R, row_off.data_ptr(), kv_len.data_ptr(), table.data_ptr(), table.shape[1], table.stride()[0],
+                               keep.data_ptr(), keep.shape[1], keep.stride()[0], n_keep.data_ptr(), new_len.data_ptr(), _stream(stream)))
+
+
+def osc_kv_trim(from_len, to_len, page_size: int, table, refs, freed, n_freed, n_pages: int = None, stream=None):
+    """Pages given back by requests that shrink from from_len to to_len [R] tokens; table [R, cols] and refs [n_pages] (or None) are updated in place,
+    freed [n_pages] and n_freed [1] are written.  All int32.  n_pages: the length of refs, or of freed without it, if it is not given."""
+    dev, i32 = _device_of(from_len), torch.int32
+    if _bad(i32, dev, from_len, to_len, refs, freed, n_freed) or _bad_rows(i32, dev, table):
+        _refuse(i32, 1, dev, from_len=from_len, to_len=to_len, refs=refs, freed=freed, n_freed=n_freed)
+        _refuse(i32, 2, dev, table=table)
+        raise ValueError("osc_kv_trim: vectors must be contiguous")
+    R, (rows, cols) = from_len.numel(), table.shape
+    if n_pages is None:
+        n_pages = refs.numel() if refs is not None else freed.numel()
+    if to_len.numel() != R or rows < R or (refs is not None and refs.numel() < n_pages) or freed.numel() < n_pages or n_freed.numel() < 1:
+        raise ValueError("osc_kv_trim: lengths do not belong together")
+    _check(_lib.osc_kv_trim(from_len.data_ptr(), to_len.data_ptr(), R, page_size, table.data_ptr(), cols, table.stride()[0], _addr(refs), n_pages,
+                            freed.data_ptr(), n_freed.data_ptr(), _stream(stream)))
+
+
+def osc_kv_fork(src, dst, len_, page_size: int, free_pages, table, refs, copy_from, copy_to, copy_used, taken, n_pages: int = None, stream=None):
+    """Rows dst [n] of table [R, cols] become forks of rows src [n]; len_ [R], table and refs [n_pages] (or None, then n_pages is given) are updated in
+    place, copy_from, copy_to, copy_used [n] (what osc_kv_copy_pages takes) and taken [1] are written.  All int32."""
+    dev, i32 = _device_of(src), torch.int32
+    if _bad(i32, dev, src, dst, len_, free_pages, refs, copy_from, copy_to, copy_used, taken) or _bad_rows(i32, dev, table):
+        _refuse(i32, 1, dev, src=src, dst=dst, len_=len_, free_pages=free_pages, refs=refs, copy_from=copy_from, copy_to=copy_to, copy_used=copy_used,
+                taken=taken)
+        _refuse(i32, 2, dev, table=table)
+        raise ValueError("osc_kv_fork: vectors must be contiguous")
+    n, (R, cols) = src.numel(), table.shape
+    if n_pages is None:
+        if refs is None:
+            raise ValueError("osc_kv_fork: n_pages is needed where there is no refs")
+        n_pages = refs.numel()
+    if (dst.numel() != n or len_.numel() < R or copy_from.numel() < n or copy_to.numel() < n or copy_used.numel() < n or taken.numel() < 1 or
+            (refs is not None and refs.numel() < n_pages)):
+        raise ValueError("osc_kv_fork: lengths do not belong together")
+    _check(_lib.osc_kv_fork(src.data_ptr(), dst.data_ptr(), n, len_.data_ptr(), R, page_size, free_pages.data_ptr(), free_pages.numel(), table.data_ptr(), cols,
+                            table.stride()[0], _addr(refs), n_pages, copy_from.data_ptr(), copy_to.data_ptr(), copy_used.data_ptr(), taken.data_ptr(),
+                            _stream(stream)))
+
+
+def osc_kv_copy_pages(layers: KvLayers, from_pages, to_pages, used=None, stream=None):
+    """The first used[i] places (all without it) of page from_pages[i] to page to_pages[i], in all layers.  All int32 [n]."""
+    dev, i32 = _device_of(from_pages), torch.int32
+    if _bad(i32, dev, from_pages, to_pages, used) or layers.device != dev:
+        _refuse(i32, 1, dev, from_pages=from_pages, to_pages=to_pages, used=used)
+        raise ValueError(f"osc_kv_copy_pages: vectors must be contiguous, the layers (cuda:{layers.device}) on the device of from_pages, cuda:{dev}")
+    n = from_pages.numel()
+    if to_pages.numel() != n or (used is not None and used.numel() != n):
+        raise ValueError("osc_kv_copy_pages: lengths do not belong together")
+    _check(_lib.osc_kv_copy_pages(layers.c, len(layers.caches), from_pages.data_ptr(), to_pages.data_ptr(), _addr(used), n, _stream(stream)))

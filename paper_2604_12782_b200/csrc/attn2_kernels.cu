@@ -125,6 +125,8 @@ struct __align__(16) WideUnit {
     int h, row0;        // head, first row of the unit (token index in Q)
     int tok0, tokens;   // first token of the unit and number of tokens, inside the segment
     int causal;
+    int ctx;            // TREE: first new token among the own keys (a prefix: past all keys)
+    int odd;            // TREE: a value of a new token is an Inf or a NaN; told by the P V warp
     int out;            // bits: OUT_*
 };
 constexpr int OUT_SPLIT = 1, OUT_TWO = 2, OUT_OWN = 4, OUT_LATER = 8;   // OUT_LATER: the share has tiles before this unit
@@ -134,7 +136,9 @@ __device__ __forceinline__ int unit_left(const WideUnit& w, int kt) {
     return kt < w.nf ? w.plen - kt * AT_WIDE_KEYS : w.klen - (kt - w.nf) * AT_WIDE_KEYS;
 }
 
-template <int D>
+// TREE: new tokens are seen by the bits of a mask, looked up only for the tiles that hold some.  An Inf or a NaN among the values of a
+// new token would reach rows that do not see it through a weight of 0: such values are 0 in the product, and the epilogue adds them to the rows that do.
+template <int D, bool TREE>
 __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_constant__ AttnWideArgs args) {
     using C = WideCfg<D>;
     constexpr int STAGES = C::STAGES, NSW = AW_SOFTMAX_WARPS;
@@ -230,6 +234,7 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                     w.h = cur.h;
                     w.row0 = cur.g.t0 + w.tok0;
                     w.causal = cur.g.flags & SEG_OWN ? cur.g.n : 0;
+                    w.ctx = cur.s >= a.P ? cur.g.klen - cur.g.n : 0x7FFFFFFF;
                     w.out = (w.n < cur.nt ? OUT_SPLIT : 0) | (cur.g.flags & SEG_TWO ? OUT_TWO : 0) | (cur.s >= a.P ? OUT_OWN : 0) | (x > x0 ? OUT_LATER : 0);
                 }
                 if (!wait_bounded(&u_empty[b], ph ^ 1u, abort_flag, 76)) break;
@@ -365,7 +370,7 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                     __syncwarp();
                 } else {
                     // tiles of the unit's part that end inside, counted from its first
-                    const int ka = uni(w.ka), nf = uni(w.nf), plen = uni(w.plen), klen = uni(w.klen);
+                    const int ka = uni(w.ka), nf = uni(w.nf), plen = uni(w.plen), klen = uni(w.klen), ctx = TREE ? uni(w.ctx) : 0;
                     const int end_front = plen % AT_WIDE_KEYS ? nf - 1 - ka : -1, end_own = klen % AT_WIDE_KEYS ? nf + klen / AT_WIDE_KEYS - ka : -1;
                     if (!wait_bounded(o_empty, oe_ph, abort_flag, 67)) goto done;      // the epilogue of the unit before has read O
                     oe_ph ^= 1u;
@@ -385,6 +390,31 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                                         *reinterpret_cast<uint4*>(v + hf * C::HALF_BYTES + c * 16) = make_uint4(0u, 0u, 0u, 0u);
                                 fence_proxy_async_smem();
                                 __syncwarp();
+                            }
+                            if (TREE && (x == 0 || !pair || i >= cnt0)) {
+                                const int key0 = (ka + tile - nf) * AT_WIDE_KEYS;
+                                if (ka + tile >= nf && key0 + AT_WIDE_KEYS > ctx) {
+                                    uint8_t* v = smem + 2 * C::QTILE_BYTES + stg * C::TILE_BYTES;
+                                    bool odd = false;
+                                    // 16-byte units of the keys from the first new token to the last one
+                                    const int c0 = max(ctx - key0, 0) * 8, c1 = min(klen - key0, AT_WIDE_KEYS) * 8;
+#pragma unroll 4
+                                    for (int c = c0 + lane; c < c1; c += 32)
+#pragma unroll
+                                        for (int hf = 0; hf < C::HALVES; ++hf) odd |= has_odd(*reinterpret_cast<const uint4*>(v + hf * C::HALF_BYTES + c * 16));
+                                    if (__any_sync(0xFFFFFFFFu, odd)) {
+#pragma unroll 1
+                                        for (int c = c0 + lane; c < c1; c += 32)
+                                            for (int hf = 0; hf < C::HALVES; ++hf) {
+                                                uint4* y = reinterpret_cast<uint4*>(v + hf * C::HALF_BYTES + c * 16);
+                                                *y = drop_odd(*y);
+                                            }
+                                        if (lane == 0) units[b].odd = 1;
+                                        __threadfence_block();       // before the commit that the epilogue waits for
+                                        fence_proxy_async_smem();
+                                        __syncwarp();
+                                    }
+                                }
                             }
                             if (!wait_bounded(&p_full[x], (p_ph >> x) & 1u, abort_flag, 69)) goto done;
                             p_ph ^= 1u << x;
@@ -431,7 +461,15 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                 // own keys that the row sees; a row that is not there sees all
                 const int sees = valid && w.causal ? max(w.klen - w.causal + w.tok0 + tok + 1, 0) : w.klen;
                 int kt = w.pair ? w.ka : w.ka + s;
+                const int ctx = TREE ? w.ctx : 0;
+                const uint32_t* mask = TREE ? a.mask + (valid ? (int64_t)(w.row0 + tok) * a.ld_mask : 0) : nullptr;
                 for (int i = 0; i < cnt; ++i, kt += step) {
+                    uint32_t bits[4];
+                    const bool masked = TREE && kt >= nf && (kt - nf + 1) * AT_WIDE_KEYS > ctx;
+                    if (masked) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) bits[j] = valid ? tree_sees(a, mask, (kt - nf) * AT_WIDE_KEYS + j * 32, ctx, w.klen) : 0xFFFFFFFFu;
+                    }
                     if (!wait_bounded(&s_full[s], s_ph, abort_flag, 70)) goto done;
                     s_ph ^= 1u;
                     tc_fence_after();
@@ -444,7 +482,13 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(s_empty);
-                    if (!whole) {
+                    if (masked) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if (!(bits[j] >> e & 1u)) v[j][e] = 0xFF800000u;
+                    } else if (!whole) {
 #pragma unroll
                         for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -571,6 +615,26 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                 int tok, hq;
                 to[y] = !row_of(x, tok, hq) ? -1 : direct ? tok * a.ldo + hq * D : (int64_t)part_row(x, tok, hq) * D;
             }
+            // Channels c .. c + n of the odd values of the new tokens that this thread's row sees, from the cache: added to o.
+            const bool odd = TREE && w.odd;
+            auto add_odd = [&](int c, int n, float* o) {
+                const int tok = tok0 + (r * a.inv_g >> 16), own0 = max(w.ka - w.nf, 0) * AT_WIDE_KEYS;
+                if ((r * a.inv_g >> 16) >= tpt || tok >= tokens) return;
+                const uint32_t* row = a.mask + (int64_t)(row0 + tok) * a.ld_mask;
+                const int32_t* pages = seg_pages(a, w.seg);
+                const int end = min((w.ka + w.n - w.nf) * AT_WIDE_KEYS, w.klen);
+#pragma unroll 1
+                for (int key = max(own0, w.ctx); key < end; ++key) {
+                    if (!(tree_sees(a, row, key, w.ctx, w.klen) & 1u)) continue;
+                    const int p = pages[key >> a.page_shift];
+                    if (p < 0 || p >= a.n_pages) continue;
+                    const uint16_t* v = a.v + (int64_t)p * a.page_stride + (int64_t)(key & ((1 << a.page_shift) - 1)) * a.token_stride +
+                                        (int64_t)w.h * a.head_stride + c;
+#pragma unroll
+                    for (int y = 0; y < 32; ++y)
+                        if (y < n && (v[y] & 0x7F80u) == 0x7F80u) o[y] += __uint_as_float((uint32_t)v[y] << 16);
+                }
+            };
             uint8_t* tile = out_tiles + warp * 2048;
             const int cols = pair ? D : D / 2, col0 = pair ? 0 : s * cols;
             const int e = lane & 3, wsw = (lane >> 1) & 3, rsw = (lane >> 3) & 3;
@@ -595,6 +659,7 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                             for (int y = 0; y < 32; ++y) o[y] = fmaf(__uint_as_float(x[y]), c1, o[y]);
                         }
                     }
+                    if (odd) add_odd(c, 32, o);
 #pragma unroll
                     for (int y = 0; y < 16; ++y) pk[y] = bf162_bits(__floats2bfloat162_rn(o[2 * y], o[2 * y + 1]));
 #pragma unroll
@@ -631,6 +696,7 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                             for (int y = 0; y < 16; ++y) o[y] = fmaf(__uint_as_float(x[y]), c1, o[y]);
                         }
                     }
+                    if (odd) add_odd(c, 16, o);
 #pragma unroll
                     for (int y = 0; y < 4; ++y)
                         *reinterpret_cast<float4*>(tile + lane * 64 + ((y ^ wsw) * 16)) = make_float4(o[4 * y], o[4 * y + 1], o[4 * y + 2], o[4 * y + 3]);
@@ -673,39 +739,39 @@ done:
 
 // ---------------------------------------------------------------------------------------------- launch
 // plan -> tcgen05 kernel (if any segment can be wide) -> few-row kernel -> join, one behind the other on the stream
-template <int D, int HW, bool SELF>
+template <int D, int HW, bool SELF, bool TREE>
 static cudaError_t launch_attn_few(const AttnArgs& a, bool early, cudaStream_t st) {
     static PerDevice pd;
     constexpr int smem = FewCfg<D, HW, SELF>::SMEM;
-    cudaError_t e = opt_in_shared_memory(pd, attn_few_kernel<D, HW, SELF>, smem);
+    cudaError_t e = opt_in_shared_memory(pd, attn_few_kernel<D, HW, SELF, TREE>, smem);
     if (e != cudaSuccess) return e;
-    return launch_pdl(attn_few_kernel<D, HW, SELF>, dim3(a.few_ctas), dim3(AT_FEW_THREADS), smem, st, a, early);
+    return launch_pdl(attn_few_kernel<D, HW, SELF, TREE>, dim3(a.few_ctas), dim3(AT_FEW_THREADS), smem, st, a, early);
 }
 // The kernel's register split only works out if it was compiled to be launched with AW_REGS_LAUNCH registers a thread.
-template <int D>
+template <int D, bool TREE>
 static cudaError_t prepare_attn_wide() {
     static PerDevice pd;
     const int slot = per_device_slot();
     if (slot >= 0 && pd.done[slot]) return cudaSuccess;
     cudaFuncAttributes fa;
-    cudaError_t e = cudaFuncGetAttributes(&fa, attn_wide_kernel<D>);
+    cudaError_t e = cudaFuncGetAttributes(&fa, attn_wide_kernel<D, TREE>);
     if (e != cudaSuccess) return e;
     if (fa.numRegs != AW_REGS_LAUNCH) return cudaErrorInvalidKernelImage;
-    return opt_in_shared_memory(pd, attn_wide_kernel<D>, WideCfg<D>::SMEM);
+    return opt_in_shared_memory(pd, attn_wide_kernel<D, TREE>, WideCfg<D>::SMEM);
 }
-template <int D>
+template <int D, bool TREE>
 static cudaError_t launch_attn_d(const AttnWideArgs& w, bool wide, cudaStream_t st) {
     const AttnArgs& a = w.a;
-    cudaError_t e = wide ? prepare_attn_wide<D>() : cudaSuccess;
+    cudaError_t e = wide ? prepare_attn_wide<D, TREE>() : cudaSuccess;
     if (e != cudaSuccess) return e;
     if (!wide && a.P == 0 && a.R <= FEW_SELF && a.few_hw == 4) {
-        if ((e = launch_attn_few<D, 4, true>(a, false, st)) != cudaSuccess) return e;
+        if ((e = launch_attn_few<D, 4, true, TREE>(a, false, st)) != cudaSuccess) return e;
     } else {
         const int threads = std::min(1024, std::max(128, (a.P + a.R + 31) / 32 * 32));
         if ((e = launch_pdl(attn_plan_kernel, dim3(1), dim3(threads), 0, st, a)) != cudaSuccess) return e;
-        if (wide && (e = launch_pdl(attn_wide_kernel<D>, dim3(a.wide_ctas), dim3(AW_THREADS), WideCfg<D>::SMEM, st, w)) != cudaSuccess) return e;
-        e = a.few_hw == 4 ? launch_attn_few<D, 4, false>(a, wide, st)
-            : a.few_hw == 2 ? launch_attn_few<D, 2, false>(a, wide, st) : launch_attn_few<D, 1, false>(a, wide, st);
+        if (wide && (e = launch_pdl(attn_wide_kernel<D, TREE>, dim3(a.wide_ctas), dim3(AW_THREADS), WideCfg<D>::SMEM, st, w)) != cudaSuccess) return e;
+        e = a.few_hw == 4 ? launch_attn_few<D, 4, false, TREE>(a, wide, st)
+            : a.few_hw == 2 ? launch_attn_few<D, 2, false, TREE>(a, wide, st) : launch_attn_few<D, 1, false, TREE>(a, wide, st);
         if (e != cudaSuccess) return e;
     }
     JoinGrid g;
@@ -718,7 +784,8 @@ static cudaError_t launch_attn_d(const AttnWideArgs& w, bool wide, cudaStream_t 
 }
 
 cudaError_t launch_attn(const AttnWideArgs& w, int D, bool wide, cudaStream_t st) {
-    return D == 128 ? launch_attn_d<128>(w, wide, st) : launch_attn_d<64>(w, wide, st);
+    if (w.a.mask) return D == 128 ? launch_attn_d<128, true>(w, wide, st) : launch_attn_d<64, true>(w, wide, st);
+    return D == 128 ? launch_attn_d<128, false>(w, wide, st) : launch_attn_d<64, false>(w, wide, st);
 }
 
 }  // namespace osc

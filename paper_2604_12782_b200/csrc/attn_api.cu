@@ -192,11 +192,12 @@ osc_status osc_paged_attention_workspace_bytes(int T, int n_q, int head_dim, int
     return OSC_OK;
 }
 
-osc_status osc_paged_attention(const void* Q, int T, int64_t ldq, int n_q, const osc_kv_cache_t* cache, int R,
-                               const int32_t* row_off, const int32_t* kv_len, const int32_t* table, int cols, int64_t ld_table,
-                               int P, const int32_t* group_off, const int32_t* prefix_len, const int32_t* prefix_table,
-                               int prefix_cols, int64_t ld_prefix, int max_new, float scale, void* O, int64_t ldo, float* lse,
-                               void* workspace, size_t workspace_bytes, void* stream) {
+// Both attention calls; words = 0: without a mask.
+static osc_status attention(const void* Q, int T, int64_t ldq, int n_q, const osc_kv_cache_t* cache, int R, const int32_t* row_off,
+                            const int32_t* kv_len, const int32_t* table, int cols, int64_t ld_table, int P, const int32_t* group_off,
+                            const int32_t* prefix_len, const int32_t* prefix_table, int prefix_cols, int64_t ld_prefix, const uint32_t* mask,
+                            int words, int64_t ld_mask, int max_new, float scale, void* O, int64_t ldo, float* lse, void* workspace,
+                            size_t workspace_bytes, void* stream) {
     if (osc_status s = check_cache(cache)) return s;
     const int D = cache->head_dim;
     if (osc_status s = check_attention_sizes(T, n_q, D, R, P)) return s;
@@ -208,7 +209,7 @@ osc_status osc_paged_attention(const void* Q, int T, int64_t ldq, int n_q, const
         return fail(OSC_ERR_INVALID_ARG, "cols = %d, prefix_cols = %d, max_new = %d", cols, prefix_cols, max_new);
     if (!(scale > 0.0f) || !(scale < INFINITY)) return fail(OSC_ERR_INVALID_ARG, "scale = %g must be positive and finite", (double)scale);
     if (T == 0 || R == 0) return OSC_OK;
-    if (!Q || !O || !row_off || !kv_len || (cols > 0 && !table) || !workspace) return fail(OSC_ERR_INVALID_ARG, "null device pointer");
+    if (!Q || !O || !row_off || !kv_len || (cols > 0 && !table) || !workspace || (words > 0 && !mask)) return fail(OSC_ERR_INVALID_ARG, "null device pointer");
     if (P > 0 && (!group_off || !prefix_len || (prefix_cols > 0 && !prefix_table)))
         return fail(OSC_ERR_INVALID_ARG, "null device pointer of a shared prefix");
     if ((R > 1 && ld_table < cols) || (P > 1 && ld_prefix < prefix_cols))
@@ -235,14 +236,14 @@ osc_status osc_paged_attention(const void* Q, int T, int64_t ldq, int n_q, const
     if (workspace_bytes < l.total) return fail(OSC_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, l.total);
     // What is written may lie on nothing else: other CTAs still read it.
     const int64_t width = (int64_t)n_q * D;
-    const struct { ByteRows b; const char* name; } buf[10] = {
+    const struct { ByteRows b; const char* name; } buf[11] = {
         {bytes_of(O, T, ldo, width, 2), "O"}, {bytes_of(lse, lse ? 1 : 0, 0, (int64_t)T * n_q, 4), "lse"},
         {bytes_of(workspace, 1, 0, (int64_t)l.total, 1), "the workspace"}, {bytes_of(Q, T, ldq, width, 2), "Q"},
         {bytes_of(row_off, 1, 0, (int64_t)R + 1, 4), "row_off"}, {bytes_of(kv_len, 1, 0, R, 4), "kv_len"}, {bytes_of(table, R, ld_table, cols, 4), "table"},
         {bytes_of(group_off, P ? 1 : 0, 0, (int64_t)P + 1, 4), "group_off"}, {bytes_of(prefix_len, P ? 1 : 0, 0, P, 4), "prefix_len"},
-        {bytes_of(prefix_table, P, ld_prefix, prefix_cols, 4), "prefix_table"}};
+        {bytes_of(prefix_table, P, ld_prefix, prefix_cols, 4), "prefix_table"}, {bytes_of(mask, words ? T : 0, ld_mask, words, 4), "mask"}};
     for (int i = 0; i < 3; ++i)
-        for (int j = i + 1; j < 10; ++j)
+        for (int j = i + 1; j < 11; ++j)
             if (rows_meet(buf[i].b, buf[j].b)) return fail(OSC_ERR_INVALID_ARG, "%s overlaps %s", buf[i].name, buf[j].name);
     DeviceInfo di;
     if (osc_status s = device_info(&di)) return s;
@@ -258,6 +259,7 @@ osc_status osc_paged_attention(const void* Q, int T, int64_t ldq, int n_q, const
     a.T = T; a.Hq = n_q; a.Hk = cache->n_heads; a.G = n_q / cache->n_heads; a.tpt = AT_WIDE_TILE / a.G; a.inv_g = (65536 + a.G - 1) / a.G; a.head_dim = D; a.R = R; a.P = P; a.n_pages = cache->n_pages;
     while ((1 << a.page_shift) < cache->page_size) ++a.page_shift;
     a.scale_log2 = scale * 1.44269504088896341f;
+    if (words) { a.mask = mask; a.ld_mask = ld_mask; a.words = words; }
     a.few_hw = hw;
     a.wide_ctas = di.num_sms < AT_WIDE_CTAS ? di.num_sms : AT_WIDE_CTAS;
     // Up to 16 rows per key/value head a request is one unit of the few-row kernel, whatever the rest of the step is.  The tcgen05
@@ -287,6 +289,54 @@ osc_status osc_paged_attention(const void* Q, int T, int64_t ldq, int n_q, const
     cudaError_t e = launch_attn(w, D, wide, static_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) return cuda_fail(e, "attention kernels");
     return OSC_OK;
+}
+
+osc_status osc_paged_attention(const void* Q, int T, int64_t ldq, int n_q, const osc_kv_cache_t* cache, int R,
+                               const int32_t* row_off, const int32_t* kv_len, const int32_t* table, int cols, int64_t ld_table,
+                               int P, const int32_t* group_off, const int32_t* prefix_len, const int32_t* prefix_table,
+                               int prefix_cols, int64_t ld_prefix, int max_new, float scale, void* O, int64_t ldo, float* lse,
+                               void* workspace, size_t workspace_bytes, void* stream) {
+    return attention(Q, T, ldq, n_q, cache, R, row_off, kv_len, table, cols, ld_table, P, group_off, prefix_len, prefix_table, prefix_cols, ld_prefix,
+                     nullptr, 0, 0, max_new, scale, O, ldo, lse, workspace, workspace_bytes, stream);
+}
+
+static osc_status check_words(int words, int64_t ld_mask, int T) {
+    if (words < 1 || words > OSC_TREE_WORDS) return fail(OSC_ERR_SHAPE, "words = %d outside 1..%d", words, OSC_TREE_WORDS);
+    if (T > 1 && ld_mask < words) return fail(OSC_ERR_SHAPE, "ld_mask = %lld < words = %d", (long long)ld_mask, words);
+    return OSC_OK;
+}
+
+osc_status osc_tree_mask(const int32_t* parents, const int32_t* row_off, const int32_t* base, int R, int T, uint32_t* mask, int words,
+                         int64_t ld_mask, int32_t* positions, void* stream) {
+    if (R < 0 || T < 0) return fail(OSC_ERR_INVALID_ARG, "R = %d, T = %d", R, T);
+    if (osc_status s = check_words(words, ld_mask, T)) return s;
+    if (T == 0) return OSC_OK;
+    if (!mask || (R > 0 && (!parents || !row_off))) return fail(OSC_ERR_INVALID_ARG, "null device pointer");
+    const struct { ByteRows b; const char* name; } buf[5] = {
+        {bytes_of(mask, T, ld_mask, words, 4), "mask"}, {bytes_of(positions, positions ? 1 : 0, 0, T, 4), "positions"},
+        {bytes_of(parents, R ? 1 : 0, 0, T, 4), "parents"}, {bytes_of(row_off, R ? 1 : 0, 0, (int64_t)R + 1, 4), "row_off"},
+        {bytes_of(base, base ? 1 : 0, 0, R, 4), "base"}};
+    for (int i = 0; i < 2; ++i)
+        for (int j = i + 1; j < 5; ++j)
+            if (rows_meet(buf[i].b, buf[j].b)) return fail(OSC_ERR_INVALID_ARG, "%s overlaps %s", buf[i].name, buf[j].name);
+    DeviceInfo di;
+    if (osc_status s = device_info(&di)) return s;
+    TreeMaskArgs a = {};
+    a.parents = parents; a.row_off = row_off; a.base = base; a.mask = mask; a.ld_mask = ld_mask; a.positions = positions;
+    a.R = R; a.T = T; a.words = words;
+    cudaError_t e = launch_tree_mask(a, di.num_sms, static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail(e, "tree_mask_kernel");
+    return OSC_OK;
+}
+
+osc_status osc_tree_attention(const void* Q, int T, int64_t ldq, int n_q, const osc_kv_cache_t* cache, int R, const int32_t* row_off,
+                              const int32_t* kv_len, const int32_t* table, int cols, int64_t ld_table, int P, const int32_t* group_off,
+                              const int32_t* prefix_len, const int32_t* prefix_table, int prefix_cols, int64_t ld_prefix, const uint32_t* mask,
+                              int words, int64_t ld_mask, int max_new, float scale, void* O, int64_t ldo, float* lse, void* workspace,
+                              size_t workspace_bytes, void* stream) {
+    if (osc_status s = check_words(words, ld_mask, T)) return s;
+    return attention(Q, T, ldq, n_q, cache, R, row_off, kv_len, table, cols, ld_table, P, group_off, prefix_len, prefix_table, prefix_cols, ld_prefix,
+                     mask, words, ld_mask, max_new, scale, O, ldo, lse, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

@@ -3,7 +3,8 @@
 //   o = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m),  s_j = scale * q . k_j,  lse = m + ln(sum_j exp(s_j - m))
 //
 // over all keys of the group's prefix and the own keys j <= kv_len - n + i of the request (i = index of the token
-// among the request's n new ones).  The softmax is evaluated piecewise: any set of keys gives (m, l, O), two sets
+// among the request's n new ones).  With a mask (trees of drafted tokens) a row sees all own keys before the new tokens, and
+// of those the ones whose bits are set in its row of the mask.  The softmax is evaluated piecewise: any set of keys gives (m, l, O), two sets
 // join as m = max, l = sum l_i 2^(m_i - m), O = sum O_i 2^(m_i - m) (everything in units of log2).
 //
 // The work is a list of segments: every group's prefix with the rows (tokens x query heads of one key/value head)
@@ -44,7 +45,7 @@ struct __align__(16) Segment {
     int flags;
 };
 constexpr int SEG_WIDE = 1;  // on the tcgen05 line
-constexpr int SEG_OWN = 4;   // own keys: token i sees klen - n + i + 1 of them; else a prefix: every token sees klen
+constexpr int SEG_OWN = 4;   // own keys without a mask: token i sees klen - n + i + 1 of them; else every token meets all klen (a prefix, or masked)
 constexpr int SEG_TWO = 2;   // the rows have another source: O goes to the workspace, and the join looks at every row
 
 // A unit that the end of a CTA's share cuts, told by the first CTA that meets it; the join finds its pieces by it.
@@ -89,6 +90,9 @@ struct AttnArgs {
     int few_hw;              // heads of a few-row unit: 4, 2 or 1
     int few_ctas, wide_ctas;
     float scale_log2;        // scale * log2(e)
+    const uint32_t* mask;    // [T][ld_mask], null: tokens see the new tokens before them.  Bit m % 32 of word m / 32: the row sees new token m
+    int64_t ld_mask;
+    int words;               // of a row of the mask
     AttnPlan plan;
     // Partial results, row by row: O [D] in part, (m, l) in ml.  Rows [0, AT_FEW_SLOTS): the first and the last piece of every few-row
     // CTA ([CTA][2][few_hw][16]); then those of the tcgen05 CTAs ([CTA][2][256]); then, where there are prefixes, twice T * Hq rows
@@ -117,6 +121,32 @@ __device__ __forceinline__ const int32_t* seg_pages(const AttnArgs& a, int s) {
 }
 // keys that token i of the segment sees, without the prefix in front
 __device__ __forceinline__ int seg_sees(const Segment& g, int i) { return g.flags & SEG_OWN ? max(g.klen - g.n + i + 1, 0) : g.klen; }
+
+// tokens of a request, its first ones, that see no own key, as far as lengths tell
+__device__ __forceinline__ int seg_blind(const AttnArgs& a, const Segment& g) { return a.mask ? (g.klen > 0 ? 0 : g.n) : max(g.n - g.klen, 0); }
+
+// Which of the 32 own keys from `key` on a row with the given mask row sees: those before the first new token (at ctx, which is
+// negative where the cache holds less than all new tokens), then by the mask's bits, none from klen on.  Words past the row's last read as 0.
+__device__ __forceinline__ uint32_t mask_word(const AttnArgs& a, const uint32_t* row, int w) { return (unsigned)w < (unsigned)a.words ? row[w] : 0u; }
+__device__ __forceinline__ uint32_t tree_sees(const AttnArgs& a, const uint32_t* row, int key, int ctx, int klen) {
+    const int m = key - ctx;
+    uint32_t bits = 0xFFFFFFFFu;
+    if (m > -32) {
+        const int w = m >> 5;            // -1 where the 32 keys begin before the first new token
+        bits = __funnelshift_r(w < 0 ? 0xFFFFFFFFu : mask_word(a, row, w), mask_word(a, row, w + 1), m & 31);
+    }
+    const int left = klen - key;
+    return left >= 32 ? bits : left > 0 ? bits & ((1u << left) - 1u) : 0u;
+}
+
+// bf16 pairs: whether one of the two is an Inf or a NaN, and the pair with those replaced by 0
+__device__ __forceinline__ bool has_odd(uint32_t x) { return (x & 0x7F80u) == 0x7F80u || (x & 0x7F800000u) == 0x7F800000u; }
+__device__ __forceinline__ bool has_odd(const uint4& x) { return has_odd(x.x) || has_odd(x.y) || has_odd(x.z) || has_odd(x.w); }
+__device__ __forceinline__ uint32_t drop_odd(uint32_t x) {
+    if ((x & 0x7F80u) == 0x7F80u) x &= 0xFFFF0000u;
+    return (x & 0x7F800000u) == 0x7F800000u ? x & 0xFFFFu : x;
+}
+__device__ __forceinline__ uint4 drop_odd(const uint4& x) { return make_uint4(drop_odd(x.x), drop_odd(x.y), drop_odd(x.z), drop_odd(x.w)); }
 
 // Rows of a segment (tokens x heads of one key/value head) and of all segments are ints: the host has seen to T * n_q <= 2^29.
 // The two kinds of units.  Few-row: 16 consecutive (token, head) rows of one token list, few_hw heads side by side, tiles
@@ -442,7 +472,7 @@ __global__ void __launch_bounds__(1024) attn_plan_kernel(const AttnArgs a) {
         Segment g;
         if (s < S) {
             g.plen = 0;
-            g.flags = s >= a.P ? SEG_OWN : 0;
+            g.flags = s >= a.P && !a.mask ? SEG_OWN : 0;
             if (s < a.P) {
                 const int r0 = off(s), r1 = max(off(s + 1), r0);
                 falls |= off(s + 1) < r0;
@@ -464,7 +494,7 @@ __global__ void __launch_bounds__(1024) attn_plan_kernel(const AttnArgs a) {
                     else g.plen = len(g.group);
                 }
                 two |= g.n > 0 && (g.flags & SEG_TWO);
-                empty |= g.n > g.klen && g.group < 0;
+                empty |= g.group < 0 && seg_blind(a, g) > 0;
                 if (a.P > 0 && g.n <= 32)          // the tokens' requests; of longer ones and behind the last token further down
                     for (int t = g.t0; t < g.t0 + g.n; ++t) a.plan.tok_req[t] = g.flags & SEG_TWO ? r : -1;
                 longer |= a.P > 0 && g.n > 32;
@@ -509,7 +539,7 @@ __global__ void __launch_bounds__(1024) attn_plan_kernel(const AttnArgs a) {
     if (empty) {
         for (int r = tid >> 5; r < a.R; r += threads / 32) {
             const Segment& g = a.plan.seg[a.P + r];
-            if (g.group < 0 && g.n > g.klen) clear_rows(a, g.t0, g.n - g.klen);
+            if (g.group < 0) clear_rows(a, g.t0, seg_blind(a, g));
             if (two && g.n > 32)
                 for (int t = g.t0 + (tid & 31); t < g.t0 + g.n; t += 32) a.plan.tok_req[t] = g.flags & SEG_TWO ? r : -1;
         }
@@ -595,7 +625,8 @@ struct FewCfg {
 // shared memory (SELF) and no plan kernel runs: the launch and its two trips through L2 would be a third of the smallest calls.  (With other
 // head counts the warps' join buffers would come on top: 124 KB for one head of 128 channels, one CTA to an SM instead of two.)
 // The loads run on over the ends of units.  A page number is fetched one tile ahead of the loads that need it.
-template <int D, int HW, bool SELF>
+// TREE: new tokens are seen by the bits of a mask, looked up only for the tiles that hold some.
+template <int D, int HW, bool SELF, bool TREE>
 __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnArgs a, bool early) {
     using C = FewCfg<D, HW, SELF>;
     constexpr int NJ = D / 8;          // 8-channel column blocks of O
@@ -621,7 +652,7 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
             if (s < S) {
                 Segment g;
                 g.plen = 0;
-                g.flags = SEG_OWN;
+                g.flags = TREE ? 0 : SEG_OWN;
                 g.group = -1;
                 g.t0 = attn_row(a, s);
                 g.n = attn_row(a, s + 1) - g.t0;
@@ -632,7 +663,7 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
                 own = g.tiles * FewUnits::heads(a);
                 inc[0] = own;
                 seg[s] = g;
-                empty |= g.n > g.klen;
+                empty |= seg_blind(a, g) > 0;
             }
             block_scan2(inc, total, s_warp, AT_FEW_THREADS / 32);
             if (s < S) start[s] = seg[s].start = carry + inc[0] - own;
@@ -649,7 +680,7 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
         src.start = start;
         if (empty)
             for (int r = blockIdx.x * 4 + warp; r < S; r += gridDim.x * 4)
-                if (seg[r].n > seg[r].klen) clear_rows(a, seg[r].t0, seg[r].n - seg[r].klen);
+                clear_rows(a, seg[r].t0, seg_blind(a, seg[r]));
     } else {
         N = load_plan(a.plan.few_start + S);
         q = load_plan(a.plan.share);
@@ -715,12 +746,15 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
         const int head = cur.h * HW + hw;
         uint32_t qf[KS][4];
         int sees[2];
+        const uint32_t* mask[2];
+        const int ctx = TREE && cur.s >= a.P ? cur.g.klen - cur.g.n : 0x7FFFFFFF;      // first new token among the keys
 #pragma unroll
         for (int hlf = 0; hlf < 2; ++hlf) {
             const int r = r0 + hlf * 8;
             const int tok = (row0 + r) / a.G, hd = (row0 + r) % a.G;
             const bool ok = r < nrows;
             sees[hlf] = ok ? seg_sees(cur.g, tok) : 0;
+            if (TREE) mask[hlf] = a.mask + (ok ? (int64_t)(cur.g.t0 + tok) * a.ld_mask : 0);
             const uint16_t* qp = a.q + (ok ? (int64_t)(cur.g.t0 + tok) * a.ldq + (int64_t)(head * a.G + hd) * D : 0) + cq * 2;
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
@@ -754,14 +788,28 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
                     }
                 }
                 float mx[2] = {-INFINITY, -INFINITY};
+                const bool masked = TREE && key0 + 16 > ctx;
+                uint32_t bits[2];
+                if (!masked) {
 #pragma unroll
-                for (int n8 = 0; n8 < 2; ++n8)
+                    for (int n8 = 0; n8 < 2; ++n8)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int key = key0 + n8 * 8 + cq * 2 + (e & 1);
-                        sc[n8][e] = key < sees[e >> 1] ? sc[n8][e] * a.scale_log2 : -INFINITY;
-                        mx[e >> 1] = fmaxf(mx[e >> 1], sc[n8][e]);
-                    }
+                        for (int e = 0; e < 4; ++e) {
+                            const int key = key0 + n8 * 8 + cq * 2 + (e & 1);
+                            sc[n8][e] = key < sees[e >> 1] ? sc[n8][e] * a.scale_log2 : -INFINITY;
+                            mx[e >> 1] = fmaxf(mx[e >> 1], sc[n8][e]);
+                        }
+                } else {
+#pragma unroll
+                    for (int hlf = 0; hlf < 2; ++hlf) bits[hlf] = tree_sees(a, mask[hlf], key0, ctx, sees[hlf]);      // sees: all keys, or none
+#pragma unroll
+                    for (int n8 = 0; n8 < 2; ++n8)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            sc[n8][e] = bits[e >> 1] >> (n8 * 8 + cq * 2 + (e & 1)) & 1u ? sc[n8][e] * a.scale_log2 : -INFINITY;
+                            mx[e >> 1] = fmaxf(mx[e >> 1], sc[n8][e]);
+                        }
+                }
                 bool move = false;
 #pragma unroll
                 for (int hlf = 0; hlf < 2; ++hlf) {
@@ -778,6 +826,35 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
                         l[hlf] *= f;
 #pragma unroll
                         for (int j = 0; j < NJ; ++j) { o[j][2 * hlf] *= f; o[j][2 * hlf + 1] *= f; }
+                    }
+                }
+                if (masked) {
+                    // An Inf or a NaN among the values of a token would reach the rows that do not see it, through a weight of 0.  It is added
+                    // here to the rows that do (any positive weight gives the same), behind the correction of O, and is 0 in the product.
+                    bool odd = false;
+#pragma unroll 1
+                    for (int i = lane; i < 16 * CHUNKS; i += 32) odd |= has_odd(*reinterpret_cast<const uint4*>(at_smem + (vb - smem_u32(at_smem)) + i * 16));
+                    if (__any_sync(0xFFFFFFFFu, odd)) {
+                        uint8_t* v = at_smem + (vb - smem_u32(at_smem));
+#pragma unroll 1
+                        for (int k = 0; k < 16; ++k)
+#pragma unroll
+                            for (int j = 0; j < NJ; ++j) {
+                                const uint32_t x = *reinterpret_cast<const uint32_t*>(v + k * (D * 2) + ((j ^ (k & 7)) * 16) + cq * 4);
+                                const uint32_t y = x & ~drop_odd(x);       // the odd ones alone, others 0
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    const uint32_t z = e & 1 ? y & 0xFFFF0000u : y << 16;
+                                    if ((z & 0x7F800000u) == 0x7F800000u && (bits[e >> 1] >> k & 1u)) o[j][e] += __uint_as_float(z);
+                                }
+                            }
+                        __syncwarp();
+#pragma unroll 1
+                        for (int i = lane; i < 16 * CHUNKS; i += 32) {
+                            uint4* x = reinterpret_cast<uint4*>(v + i * 16);
+                            *x = drop_odd(*x);
+                        }
+                        __syncwarp();
                     }
                 }
                 // Weights in bf16 for P V: the tensor cores take both operands in one type, and V is bf16.  Each is off by at most 2^-8 of itself, either
