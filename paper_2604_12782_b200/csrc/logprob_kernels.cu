@@ -6,14 +6,17 @@
 // ln l and -S are never negative, so nothing cancels where a row is sure of one token.  A thread keeps its own (max, l, S) and joins a
 // chunk of 16-byte vectors at a time: the chunk's maximum first, one correction of (l, S) if it is a new one, then the chunk's terms
 // (l' = l f, S' = f (S + l (m - m')), f = exp(scale (m - m'))).  A row is one block's, or with few rows a cluster's, whose blocks take
-// consecutive parts and are joined through distributed shared memory, so there is one launch and no workspace.
+// consecutive parts and are joined through distributed shared memory, so there is one launch and no workspace.  Every thread copies its own
+// vectors into a ring in shared memory (cp.async), two chunks ahead; nobody else reads them, so the ring needs no barrier.
 //
-// Alternatives: the order is value, then lower index, as one key: the value's bits made monotone (NaN below -inf) and the index.  The chunk is in
-// registers, and a thread's largest value is known from the maximum above.  First chunk: the k-th largest of the threads' largest values bounds
-// the k-th best value of the row from below, and few other values pass it (with 256 threads and k = 20 less than one more), so the values
-// at or above it go to a list in shared memory.  Later chunks: only values above the bound, a handful a chunk; a chunk without any costs one
-// barrier that counts.  Where too many values pass (equal logits, rows in rising order) the chunk's best are taken one by one instead, k rounds of a
-// maximum over the block.
+// Alternatives: the order is value, then lower index, as one key: the value's bits made monotone (NaN below -inf) and the index.  A thread's
+// largest value of a chunk is known from the maximum above.  First chunk: the largest 16-bit key prefix that k threads' largest values reach bounds
+// the k-th best value of the row from below (found by halving, a barrier that counts a step), and few other values pass it, so the values at
+// or above it go to a list in shared memory.  Later chunks: only values above the bound, without a barrier; the list is joined with the k best so far,
+// which raises the bound, behind chunks 1, 2, 4, 8, ... and the last: some k candidates each time.  Where a thread has some, its warp looks at its values
+// of the chunk in shared memory, one lane each.  (By the thread itself, in registers one by one, that cost more than the sums: 600 us for 3001 rows of
+// 152064; in shared memory 394.)  Where too many values pass (equal logits, rows in rising order) the chunks since the last rank are read again, each with a bound of its
+// own, and where that does not help (ties) its best are taken one by one, k rounds of a maximum over the block.
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -24,9 +27,12 @@
 namespace osc {
 
 constexpr int LP_THREADS = 256, LP_WARPS = LP_THREADS / 32;
-constexpr int LP_VECS = 8;               // 16-byte vectors of a chunk, per thread
+constexpr int LP_VECS = 4;               // 16-byte vectors of a chunk, per thread
+static_assert(LP_VECS * 8 <= 32, "a lane for every value of a thread");
+constexpr int LP_STAGES = 3;             // chunks in the ring
+constexpr int LP_RING = LP_STAGES * LP_THREADS * LP_VECS * 16;
 constexpr int LP_MAX_TOP = 32;
-constexpr int LP_LIST = 1024;            // candidates that wait to be ranked
+constexpr int LP_LIST = 512;            // candidates that wait to be ranked
 constexpr int LP_MAX_CLUSTER = 8;
 
 struct LogprobArgs {
@@ -49,6 +55,7 @@ __device__ __forceinline__ uint32_t lp_key(float x) {
     const uint32_t b = __float_as_uint(x + 0.0f);
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
+constexpr uint32_t LP_KEY_LOW = 0x007FFFFFu;      // -inf
 __device__ __forceinline__ float lp_value(uint32_t key) {
     if (key <= 1u) return __uint_as_float(0x7FC00000u);
     return __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key);
@@ -73,86 +80,159 @@ struct LpVec {
         return __uint_as_float(F32 ? w : e & 1 ? w & 0xFFFF0000u : w << 16);
     }
 };
+
 template <bool F32, bool TOP>
-__global__ void __launch_bounds__(LP_THREADS, 3) token_logprobs_kernel(const LogprobArgs a, int cluster) {
+__global__ void __launch_bounds__(LP_THREADS, 4) token_logprobs_kernel(const LogprobArgs a, int cluster) {
     using Vec = LpVec<F32>;
-    constexpr int E = Vec::E, U = LP_VECS;
-    __shared__ unsigned long long s_list[TOP ? LP_LIST + LP_MAX_TOP : 1];    // candidates, the ranked ones first
-    __shared__ unsigned long long s_best[TOP ? LP_MAX_TOP : 1];
-    __shared__ uint32_t s_key[TOP ? LP_THREADS : 1];
+    using Elem = typename Vec::Elem;
+    constexpr int E = Vec::E, U = LP_VECS, CHUNK = LP_THREADS * U;
+    extern __shared__ __align__(16) uint8_t lp_ring[];       // [LP_STAGES][CHUNK] vectors
+    __shared__ unsigned long long s_list[TOP ? LP_LIST : 1];             // candidates since the last rank
+    __shared__ unsigned long long s_kept[2][TOP ? LP_MAX_TOP : 1];       // the k best, in order (0: none); the one of two that `which` says
     __shared__ unsigned long long s_warp[LP_WARPS];
     __shared__ float s_red[3][LP_WARPS];
     __shared__ float s_part[3];                      // (max, l, S) of the block
-    __shared__ int s_n;
-    __shared__ uint32_t s_bound;
+    __shared__ int s_which;
+    __shared__ int s_n, s_over;                      // candidates; whether some found no place
     grid_launch_dependents();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rank = cluster > 1 ? (int)cluster_ctarank() : 0;
     const int64_t row = blockIdx.x / cluster;
     const float scale2 = a.scale * 1.44269504088896341f;
     const int k = TOP ? a.k : 0;
-    if (TOP && tid == 0) s_n = 0;
+    if (TOP) {
+        if (tid == 0) s_n = s_over = 0;
+        if (tid < 2 * LP_MAX_TOP) s_kept[tid / LP_MAX_TOP][tid % LP_MAX_TOP] = 0;
+    }
     grid_dependency_wait();
 
-    // Rows begin at any element: vectors are counted from the 16-byte boundary at or before the row, `lead` elements of the first one are not the row's.
-    const typename Vec::Elem* xr = static_cast<const typename Vec::Elem*>(a.x) + row * a.ld;
-    const int lead = (int)((reinterpret_cast<uintptr_t>(xr) & 15u) / sizeof(typename Vec::Elem));
+    // Rows begin at any element: vectors are counted from the 16-byte boundary at or before the row, whose first `lead` elements are not the row's.
+    // Vectors [full0, full1) are the row's as a whole, [v0, v1) of them this block's; the few elements in front and behind come last.
+    const Elem* xr = static_cast<const Elem*>(a.x) + row * a.ld;
+    const int lead = (int)((reinterpret_cast<uintptr_t>(xr) & 15u) / sizeof(Elem));
     const uint4* xv = reinterpret_cast<const uint4*>(xr - lead);
-    const int nvec = (int)(((int64_t)lead + a.V + E - 1) / E);
-    const int v0 = (int)((int64_t)nvec * rank / cluster), v1 = (int)((int64_t)nvec * (rank + 1) / cluster);
-    const int full0 = lead ? 1 : 0, full1 = (int)(((int64_t)lead + a.V) / E);      // vectors [full0, full1) are the row's as a whole
+    const int full0 = lead ? 1 : 0, full1 = max((int)(((int64_t)lead + a.V) / E), full0);
+    const int v0 = full0 + (int)((int64_t)(full1 - full0) * rank / cluster), v1 = full0 + (int)((int64_t)(full1 - full0) * (rank + 1) / cluster);
 
-    float m = -INFINITY, l = 0.0f, S = 0.0f;
-    uint32_t bound = 0;          // values above it are candidates
-    bool bounded = false;
-    if (TOP) __syncthreads();
-
-    // Ranks the candidates and keeps the k best, in order; `bound` is then the last one's key.
-    auto rank_list = [&]() {
-        __syncthreads();
-        const int n = s_n;
-        for (int i = tid; i < n; i += LP_THREADS) {
-            const unsigned long long mine = s_list[i];
-            int better = 0;
-            for (int j = 0; j < n; ++j) better += s_list[j] > mine;
-            if (better < k) s_best[better] = mine;
-        }
-        __syncthreads();
-        const int kept = min(n, k);
-        if (tid < kept) s_list[tid] = s_best[tid];
-        if (tid == 0) s_n = kept;
-        __syncthreads();
-        if (kept == k) bound = (uint32_t)(s_list[k - 1] >> 32);
-    };
-
-#pragma unroll 1
-    for (int base = v0; base < v1; base += LP_THREADS * U) {
-        uint4 v[U];
+    uint4* mine = reinterpret_cast<uint4*>(lp_ring) + tid;       // the thread's vectors of a stage: mine[u * LP_THREADS]
+    const uint64_t policy = l2_policy_evict_first();             // read once
+    auto load = [&](int base, int stage) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int i = base + u * LP_THREADS + tid;
-            if (i >= full0 && i < full1 && i < v1) {
-                v[u] = __ldcs(xv + i);
-            } else {
-                // the row's first or last vector, of which some elements are not the row's, or none at all: those read as -inf
-                uint32_t w[4];
+            if (i < v1) cp_async_16(smem_u32(mine + stage * CHUNK + u * LP_THREADS), xv + i, true, policy);
+        }
+        cp_async_commit();
+    };
 #pragma unroll
-                for (int e = 0; e < 4; ++e) w[e] = F32 ? 0xFF800000u : 0xFF80FF80u;
-                if (i < v1) {
+    for (int i = 0; i < LP_STAGES - 1; ++i) load(v0 + i * CHUNK, i);
+
+    float m = -INFINITY, l = 0.0f, S = 0.0f;
+    uint32_t bound = 0;          // values with a key above it are candidates
+    float value = 0.0f;          // the value it stands for, from -inf on
+    int which = 0;
+    auto set_bound = [&](uint32_t b) {
+        bound = b;
+        value = b == 0x7FFFFFFFu ? __uint_as_float(0x80000001u) : lp_value(max(b, LP_KEY_LOW));      // (no value has that key: -0 counts as 0)
+    };
+    if (TOP) __syncthreads();
+
+    // Joins the candidates with the k best; `bound` becomes the last one's key.  All threads have passed a barrier since the last candidate came.
+    auto rank_list = [&]() {
+        const int n = min(s_n, LP_LIST);
+        unsigned long long* to = s_kept[which ^ 1];
+        const unsigned long long* from = s_kept[which];
+#pragma unroll 1
+        for (int i = tid; i < n + k; i += LP_THREADS) {
+            const unsigned long long x = i < k ? from[i] : s_list[i - k];
+            if (x == 0) continue;
+            int better = 0;
+#pragma unroll 4
+            for (int j = 0; j < k; ++j) better += from[j] > x;
+#pragma unroll 4
+            for (int j = 0; j < n; ++j) better += s_list[j] > x;
+            if (better < k) to[better] = x;
+        }
+        __syncthreads();
+        which ^= 1;
+        set_bound((uint32_t)(s_kept[which][k - 1] >> 32));
+        if (tid < k) s_kept[which ^ 1][tid] = 0;
+        if (tid == 0) s_n = s_over = 0;
+        __syncthreads();
+    };
+    auto add = [&](uint32_t key, int j) {
+        const int n = atomicAdd(&s_n, 1);
+        if (n < LP_LIST) s_list[n] = lp_rank(key, j);
+        else s_over = 1;
+    };
+    // every value of the thread in a chunk, which lies at `at` (LP_THREADS vectors apart): f(key, index)
+    auto each = [&](const uint4* at, int base, auto f) {
+#pragma unroll 1
+        for (int u = 0; u < U && base + u * LP_THREADS + tid < v1; ++u) {
+            const uint4 x = at[u * LP_THREADS];
+            const int j = (base + u * LP_THREADS + tid) * E - lead;
 #pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        const int j = i * E + e - lead;
-                        if (j >= 0 && j < a.V) {
-                            if (F32) w[e & 3] = __float_as_uint(Vec::value(xr[j]));
-                            else {
-                                const uint32_t b = __float_as_uint(Vec::value(xr[j]));
-                                w[e / 2 & 3] = e & 1 ? (w[e / 2 & 3] & 0xFFFFu) | b : (w[e / 2 & 3] & 0xFFFF0000u) | b >> 16;
-                            }
-                        }
-                    }
-                }
-                v[u] = make_uint4(w[0], w[1], w[2], w[3]);
-            }
+            for (int e = 0; e < E; ++e) f(lp_key(Vec::get(x, e)), j + e);
+        }
+    };
+    // a key that at least k of the threads' largest values reach, or 0
+    auto reached = [&](uint32_t best) -> uint32_t {
+        uint32_t t = 0;
+#pragma unroll 1
+        for (int bit = 15; bit >= 0; --bit)
+            if (__syncthreads_count(best >> 16 >= (t | 1u << bit)) >= k) t |= 1u << bit;
+        return t << 16;
+    };
+    // a chunk with many values above the bound, read once more
+    auto again = [&](int base) {
+        const uint4* at = xv + base + tid;
+        uint32_t best = 0;
+        each(at, base, [&](uint32_t key, int) { best = max(best, key); });
+        const uint32_t t = reached(best);
+        if (t) set_bound(max(bound, t - 1));
+        each(at, base, [&](uint32_t key, int j) { if (key > bound) add(key, j); });
+        __syncthreads();
+        if (!s_over) return rank_list();
+        __syncthreads();
+        if (tid == 0) s_n = 0;
+        __syncthreads();
+        set_bound((uint32_t)(s_kept[which][k - 1] >> 32));
+        unsigned long long last = ~0ull;
+#pragma unroll 1
+        for (int i = 0; i < k; ++i) {
+            unsigned long long next = 0;
+            each(at, base, [&](uint32_t key, int j) {
+                const unsigned long long c = lp_rank(key, j);
+                if (c < last && c > next) next = c;
+            });
+#pragma unroll
+            for (int o = 16; o; o >>= 1) next = max(next, __shfl_xor_sync(0xFFFFFFFFu, next, o));
+            if (lane == 0) s_warp[warp] = next;
+            __syncthreads();
+            last = s_warp[0];
+#pragma unroll
+            for (int w = 1; w < LP_WARPS; ++w) last = max(last, s_warp[w]);
+            __syncthreads();
+            if ((uint32_t)(last >> 32) <= bound) break;      // 0, or no better than the k of the chunks before
+            if (tid == 0) s_list[s_n++] = last;
+        }
+        __syncthreads();
+        rank_list();
+    };
+
+    int stage = 0, chunk = 0, since = v0;        // since: first vector of the chunks that are not ranked
+#pragma unroll 1
+    for (int base = v0; base < v1; base += CHUNK, ++chunk) {
+        // into the stage of the chunk before, whose vectors are done with
+        load(base + (LP_STAGES - 1) * CHUNK, stage == 0 ? LP_STAGES - 1 : stage - 1);
+        cp_async_wait<LP_STAGES - 1>();
+        const uint4* at = mine + stage * CHUNK;
+        stage = stage + 1 == LP_STAGES ? 0 : stage + 1;
+        uint4 v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            v[u].x = v[u].y = v[u].z = v[u].w = F32 ? 0xFF800000u : 0xFF80FF80u;      // past the end: -inf
+            if (base + u * LP_THREADS + tid < v1) v[u] = at[u * LP_THREADS];
         }
         // ---- the chunk's maximum (a NaN leaves it alone)
         float top;
@@ -165,8 +245,8 @@ __global__ void __launch_bounds__(LP_THREADS, 3) token_logprobs_kernel(const Log
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) t = __hmax2(t, *reinterpret_cast<const __nv_bfloat162*>(&w[e]));
+                const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(w);
+                t = __hmax2(t, __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3])));
             }
             top = fmaxf(__low2float(t), __high2float(t));
         }
@@ -203,108 +283,87 @@ __global__ void __launch_bounds__(LP_THREADS, 3) token_logprobs_kernel(const Log
             float sum = s0 + s1;
             if (sum != sum) {        // 0 * -inf: -inf among the logits (or a NaN, or +inf, which l shows)
                 sum = 0.0f;
-#pragma unroll
-                for (int u = 0; u < U; ++u)
+#pragma unroll 1
+                for (int u = 0; u < U && base + u * LP_THREADS + tid < v1; ++u) {
+                    const uint4 x = at[u * LP_THREADS];
 #pragma unroll
                     for (int e = 0; e < E; ++e) {
-                        const float d = Vec::get(v[u], e) + ref, p = lp_exp2(d * scale2);
+                        const float d = Vec::get(x, e) + ref, p = lp_exp2(d * scale2);
                         sum += p == 0.0f ? 0.0f : p * d;
                     }
+                }
             }
             l += l0 + l1;
             S += sum;
         }
         // ---- candidates
         if (TOP) {
-            // a NaN is a value too: a thread that holds nothing else has it as its largest
-            uint32_t best = lp_key(top);
-            const bool any = base + tid < v1;
-            if (top == -INFINITY) {
-                best = 0;
-                if (any) {
-#pragma unroll
-                    for (int u = 0; u < U; ++u)
-#pragma unroll
-                        for (int e = 0; e < E; ++e) {
-                            const int j = (base + u * LP_THREADS + tid) * E + e - lead;
-                            if (base + u * LP_THREADS + tid < v1 && j >= 0 && j < a.V) best = max(best, lp_key(Vec::get(v[u], e)));
-                        }
+            if (chunk == 0) {
+                uint32_t best = lp_key(top);
+                if (top == -INFINITY) {              // a NaN is a value too
+                    best = 0;
+                    each(at, base, [&](uint32_t key, int) { best = max(best, key); });
                 }
+                const uint32_t t = reached(best);
+                set_bound(t ? t - 1 : 0);            // values at t are candidates themselves
             }
-            const int before = s_n;
-            uint32_t raised = 0;
-            bool add;
-            if (!bounded) {
-                // k-th largest of the threads' largest values; ties by the thread
-                s_key[tid] = best;
-                __syncthreads();
-                int better = 0;
-#pragma unroll 8
-                for (int j = 0; j < LP_THREADS; ++j) better += s_key[j] > best || (s_key[j] == best && j < tid);
-                if (better == k - 1) s_bound = best;
-                __syncthreads();
-                raised = s_bound;
-                bound = raised ? raised - 1 : 0;     // values at the bound are candidates themselves
-                add = best > bound;
-                bounded = true;
-            } else {
-                if (!__syncthreads_or(best > bound)) continue;
-                add = best > bound;
-            }
-            if (add) {
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-#pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        const uint32_t key = lp_key(Vec::get(v[u], e));
-                        if (key > bound) {
-                            const int i = base + u * LP_THREADS + tid, j = i * E + e - lead;
-                            if (i < v1 && j >= 0 && j < a.V) {
-                                const int at = atomicAdd(&s_n, 1);
-                                if (at < LP_LIST) s_list[at] = lp_rank(key, j);
-                            }
-                        }
-                    }
-            }
-            if (raised) bound = raised;          // of the chunks behind this one only values above it count: indices rise
-            __syncthreads();
-            if (s_n > LP_LIST) {
-                // too many: the chunk's best one by one
-                __syncthreads();
-                if (tid == 0) s_n = before;
-                bound = 0;
-                rank_list();
-                unsigned long long last = ~0ull;
+            __syncwarp();                            // the lanes' copies, for one another
+            uint32_t lanes = __ballot_sync(0xFFFFFFFFu, bound < LP_KEY_LOW ? base + tid < v1 : top > value);
 #pragma unroll 1
-                for (int i = 0; i < k; ++i) {
-                    unsigned long long mine = 0;
-#pragma unroll
-                    for (int u = 0; u < U; ++u)
-#pragma unroll
-                        for (int e = 0; e < E; ++e) {
-                            const int q = base + u * LP_THREADS + tid, j = q * E + e - lead;
-                            if (q < v1 && j >= 0 && j < a.V) {
-                                const unsigned long long c = lp_rank(lp_key(Vec::get(v[u], e)), j);
-                                if (c < last && c > mine) mine = c;
-                            }
-                        }
-#pragma unroll
-                    for (int o = 16; o; o >>= 1) mine = max(mine, __shfl_xor_sync(0xFFFFFFFFu, mine, o));
-                    if (lane == 0) s_warp[warp] = mine;
-                    __syncthreads();
-                    unsigned long long best_of = s_warp[0];
-#pragma unroll
-                    for (int w = 1; w < LP_WARPS; ++w) best_of = max(best_of, s_warp[w]);
-                    __syncthreads();
-                    last = best_of;
-                    if ((uint32_t)(last >> 32) <= bound) break;      // 0, or no better than the k of the chunks before
-                    if (tid == 0) s_list[s_n++] = last;
+            for (; lanes; lanes &= lanes - 1) {
+                const int of = tid - lane + __ffs((int)lanes) - 1, u = lane / E, e = lane % E, i = base + u * LP_THREADS + of;
+                uint32_t key = 0;
+                if (lane < U * E && i < v1) key = lp_key(Vec::value(reinterpret_cast<const Elem*>(at - tid + u * LP_THREADS + of)[e]));
+                const uint32_t found = __ballot_sync(0xFFFFFFFFu, key > bound);
+                if (found == 0) continue;
+                int n = 0;
+                if (lane == 0) n = atomicAdd(&s_n, __popc(found));
+                n = __shfl_sync(0xFFFFFFFFu, n, 0) + __popc(found & ((1u << lane) - 1u));
+                if (key > bound) {
+                    if (n < LP_LIST) s_list[n] = lp_rank(key, i * E + e - lead);
+                    else s_over = 1;
                 }
-                rank_list();
-            } else if (s_n > LP_LIST / 2) {
-                rank_list();
             }
+            if ((chunk & (chunk + 1)) == 0 || base + CHUNK >= v1) {
+                __syncthreads();
+                if (!s_over) {
+                    rank_list();
+                } else {
+                    __syncthreads();
+                    if (tid == 0) s_n = s_over = 0;
+                    set_bound((uint32_t)(s_kept[which][k - 1] >> 32));
+                    __syncthreads();
+#pragma unroll 1
+                    for (int b = since; b < min(base + CHUNK, v1); b += CHUNK) again(b);
+                }
+                since = base + CHUNK;
+            }
+        }
+    }
+    cp_async_wait<0>();
+
+    // ---- the elements in front of the row's first whole vector and behind its last one
+    {
+        const int head = min(full0 * E - lead, a.V), tail = max(full1 * E - lead, head);      // [0, head), [tail, V)
+        const int j = rank == 0 && tid < head ? tid : rank == cluster - 1 && tid >= 32 && tid - 32 < a.V - tail ? tail + tid - 32 : -1;
+        if (j >= 0) {
+            const float x = Vec::value(xr[j]);
+            if (x > m) {
+                const float d = m - x, f = m > -INFINITY ? lp_exp2(d * scale2) : 0.0f;
+                S = f == 0.0f ? 0.0f : f * (S + l * d);
+                l = f == 0.0f && l == l ? 0.0f : l * f;
+                m = x;
+            }
+            if (x != -INFINITY) {
+                const float d = x - (m == -INFINITY ? 0.0f : m), p = lp_exp2(d * scale2);
+                l += p;
+                if (p != 0.0f) S += p * d;
+            }
+            if (TOP) add(lp_key(x), j);
+        }
+        if (TOP && (head > 0 || tail < a.V)) {
             __syncthreads();
+            rank_list();
         }
     }
 
@@ -348,13 +407,12 @@ __global__ void __launch_bounds__(LP_THREADS, 3) token_logprobs_kernel(const Log
             s_part[2] = S;
         }
     }
-    if (TOP) rank_list();
-
     // ---- the cluster's: every block joins the sums in rank order, rank 0 the candidates and the rest
     if (cluster > 1) {
+        if (TOP && tid == 0) s_which = which;
         cluster_sync_all();
         if (rank == 0) {
-            const uint32_t part = smem_u32(s_part), list = smem_u32(s_list), count = smem_u32(&s_n);
+            const uint32_t part = smem_u32(s_part);
             auto ld32 = [](uint32_t addr) {
                 uint32_t r;
                 asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(r) : "r"(addr) : "memory");
@@ -380,18 +438,15 @@ __global__ void __launch_bounds__(LP_THREADS, 3) token_logprobs_kernel(const Log
                     l += pl[c] * f;
                     S += f * (ps[c] + pl[c] * d);
                 }
-            if (TOP) {
-                // the others' lists behind this block's: at most 8 * 32 candidates
-                for (int c = 1; c < cluster; ++c) {
-                    const int n = (int)ld32(map_to_cta(count, c)), at = s_n;
-                    __syncthreads();
-                    if (tid < n) {
-                        const uint32_t p = map_to_cta(list, c) + tid * 8;
-                        s_list[at + tid] = (unsigned long long)ld32(p + 4) << 32 | ld32(p);
-                    }
-                    if (tid == 0) s_n = at + n;
-                    __syncthreads();
+            if constexpr (TOP) {
+                // the others' k best as candidates; which of the two buffers holds them depends on how often a block has ranked
+                for (int i = tid; i < (cluster - 1) * k; i += LP_THREADS) {
+                    const int c = 1 + i / k;
+                    const uint32_t p = map_to_cta(smem_u32(s_kept[ld32(map_to_cta(smem_u32(&s_which), c))] + i % k), c);
+                    s_list[i] = (unsigned long long)ld32(p + 4) << 32 | ld32(p);
                 }
+                if (tid == 0) s_n = (cluster - 1) * k;
+                __syncthreads();
                 rank_list();
             }
         }
@@ -412,8 +467,8 @@ __global__ void __launch_bounds__(LP_THREADS, 3) token_logprobs_kernel(const Log
     }
     if (TOP) {
         for (int i = tid; i < k; i += LP_THREADS) {
-            const bool there = i < s_n;
-            const unsigned long long c = s_list[there ? i : 0];
+            const unsigned long long c = s_kept[which][i];
+            const bool there = c != 0;
             a.top_ids[row * k + i] = there ? (int)~(uint32_t)c : -1;
             a.top_logprob[row * k + i] = there ? logprob(lp_value((uint32_t)(c >> 32))) : -INFINITY;
         }
@@ -422,9 +477,12 @@ __global__ void __launch_bounds__(LP_THREADS, 3) token_logprobs_kernel(const Log
 
 template <bool F32, bool TOP>
 static cudaError_t launch_logprobs_t(const LogprobArgs& a, int cluster, cudaStream_t st) {
+    static PerDevice pd;
+    if (cudaError_t e = opt_in_shared_memory(pd, token_logprobs_kernel<F32, TOP>, LP_RING)) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((int64_t)a.T * cluster));
     cfg.blockDim = dim3(LP_THREADS);
+    cfg.dynamicSmemBytes = LP_RING;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
