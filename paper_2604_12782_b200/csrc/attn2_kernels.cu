@@ -55,6 +55,8 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return r;
 }
 
+constexpr int WIDE_SELF = 256;         // requests whose line every CTA lays out for itself
+
 template <int D>
 struct WideCfg {
     static constexpr int HALVES = D / 64;                        // 128-byte swizzle rows hold 64 channels
@@ -66,7 +68,8 @@ struct WideCfg {
     static constexpr int OUT_BYTES = AW_SOFTMAX_WARPS * 2048;    // every softmax warp's 32 rows x 64 bytes of O on the way out
     static constexpr int ROW_FLOATS = 2 * 2 * 2 * 128;           // [parity][stream][128] maxima and sums of a unit
     static constexpr int BAR_BYTES = 320;
-    static constexpr int SMEM = 2 * QTILE_BYTES + 2 * STAGES * TILE_BYTES + OUT_BYTES + ROW_FLOATS * 4 + BAR_BYTES + 2 * 64 + 1024;
+    static constexpr int PLAN = 2 * QTILE_BYTES + 2 * STAGES * TILE_BYTES + OUT_BYTES + ROW_FLOATS * 4 + BAR_BYTES + 2 * 80 + 32;      // where a line laid out here lies
+    static constexpr int SMEM = PLAN + WIDE_SELF * ((int)sizeof(Segment) + 4) + 1024;
     static constexpr int TM_S = 0;         // TMEM columns: S (128), P0, P1 (64 each), O0, O1 (D each)
     static constexpr int TM_P = 128;
     static constexpr int TM_O = 256;
@@ -191,6 +194,43 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
     const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, *tmem_slot, 0);
     grid_dependency_wait();
     grid_launch_dependents();   // not before: the few-row kernel counts on the plan being there when it begins
+    const int S = a.P + a.R;
+    Segment* self_seg = reinterpret_cast<Segment*>(smem + C::PLAN);
+    int* self_start = reinterpret_cast<int*>(self_seg + WIDE_SELF);
+    int self_N = 0;
+    if (TREE && a.self) {       // as in the few-row kernel: no plan kernel runs, every segment is a request's own keys
+        __shared__ int s_scan[2][32];
+        bool empty = false, falls = false;
+        const int s = threadIdx.x;           // at most WIDE_SELF of them
+        int inc[2] = {0, 0}, total[2], own = 0;
+        Segment g;
+        if (s < S) {
+            g.plen = 0;
+            g.flags = SEG_WIDE;
+            g.group = -1;
+            g.t0 = attn_row(a, s);
+            g.n = attn_row(a, s + 1) - g.t0;
+            falls = g.n < 0;
+            g.n = max(g.n, 0);
+            g.klen = attn_keys(a.kv_len[s], a.cols, a.page_shift);
+            g.tiles = head_span<WideUnits>(a, g);
+            inc[0] = own = g.tiles * WideUnits::heads(a);
+            empty = seg_blind(a, g) > 0;
+        }
+        block_scan2(inc, total, s_scan, AW_THREADS / 32);
+        if (s < S) {
+            g.start = self_start[s] = inc[0] - own;
+            self_seg[s] = g;
+        }
+        self_N = total[0];
+        empty = __syncthreads_or(empty || falls);
+        if (empty && __syncthreads_or(falls)) {
+            empty = false;
+            self_N = 0;
+        }
+        if (empty)
+            for (int r = blockIdx.x * (AW_THREADS / 32) + warp; r < S; r += gridDim.x * (AW_THREADS / 32)) clear_rows(a, self_seg[r].t0, seg_blind(a, self_seg[r]));
+    }
     const int tpt = a.tpt;
     const uint32_t ring0 = smem_u32(ring);
 
@@ -198,59 +238,69 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
         regs_dec<AW_REGS_OTHER>();
         if (warp == NSW + 2) {
             // ------------------------------------------------------------------------------------- units
-            const int S = a.P + a.R;
-            const int N = a.plan.wide_start[S], q = a.plan.share[1];
-            const int x0 = (int)min((int64_t)q * blockIdx.x, (int64_t)N), x1 = (int)min((int64_t)x0 + q, (int64_t)N);
-            Cursor<WideUnits> cur;
-            const LineSource<false> src = {a.plan.seg, a.plan.wide_start};
-            if (lane == 0) a.plan.cut[1][blockIdx.x].tiles = 0;
-            int b = 0, x = x0;
-            uint32_t ph = 0;
-            if (x0 < x1) {
-                cur.seek(a, src, S, x0);
-                if (cur.kt < 0) { x -= cur.kt; cur.kt = 0; }         // in front of the unit's tiles
-            }
-            while (true) {
-                WideUnit w = {};
-                if (x < x1) {
-                    w.ka = cur.kt;
-                    w.n = min(cur.nt - cur.kt, x1 - x);
-                    w.tok0 = cur.u * 2 * tpt;
-                    w.tokens = min(cur.g.n - w.tok0, 2 * tpt);
-                    w.pair = w.tokens > tpt;
-                    w.nf = front_tiles<WideUnits>(a, cur.g);
-                    if (w.pair) {
-                        const int nt0 = w.nf + (seg_sees(cur.g, w.tok0 + tpt - 1) + AT_WIDE_KEYS - 1) / AT_WIDE_KEYS;
-                        w.cnt[0] = max(min(w.ka + w.n, nt0) - w.ka, 0);
-                        w.cnt[1] = w.n;
-                    } else {
-                        w.cnt[0] = (w.n + 1) / 2;
-                        w.cnt[1] = w.n / 2;
+            auto walk = [&](auto& cur, const auto& src, int N, int q) {
+                const int x0 = (int)min((int64_t)q * blockIdx.x, (int64_t)N), x1 = (int)min((int64_t)x0 + q, (int64_t)N);
+                if (lane == 0) a.plan.cut[1][blockIdx.x].tiles = 0;
+                int b = 0, x = x0;           // (last) place of the tile to come
+                uint32_t ph = 0;
+                bool first = true;
+                if (x0 < x1) {
+                    cur.seek(a, src, S, x0);
+                    if (cur.kt < 0) cur.kt = 0;      // in front of the unit's tiles
+                    x = unit_begin<WideUnits>(a, cur.g, cur.h, cur.u) + cur.kt * WideUnits::weight(a, cur.g, cur.u);
+                }
+                while (true) {
+                    WideUnit w = {};
+                    const int weight = x < x1 ? WideUnits::weight(a, cur.g, cur.u) : 1, begin = x - cur.kt * weight;
+                    if (x < x1) {
+                        w.ka = cur.kt;
+                        w.n = min(cur.nt - cur.kt, (x1 - x + weight - 1) / weight);
+                        w.tok0 = cur.u * 2 * tpt;
+                        w.tokens = min(cur.g.n - w.tok0, 2 * tpt);
+                        w.pair = w.tokens > tpt;
+                        w.nf = front_tiles<WideUnits>(a, cur.g);
+                        if (w.pair) {
+                            const int nt0 = w.nf + (seg_sees(cur.g, w.tok0 + tpt - 1) + AT_WIDE_KEYS - 1) / AT_WIDE_KEYS;
+                            w.cnt[0] = max(min(w.ka + w.n, nt0) - w.ka, 0);
+                            w.cnt[1] = w.n;
+                        } else {
+                            w.cnt[0] = (w.n + 1) / 2;
+                            w.cnt[1] = w.n / 2;
+                        }
+                        w.plen = cur.g.plen;
+                        w.klen = cur.g.klen;
+                        w.front = cur.g.group;
+                        w.seg = cur.s;
+                        w.h = cur.h;
+                        w.row0 = cur.g.t0 + w.tok0;
+                        w.causal = cur.g.flags & SEG_OWN ? cur.g.n : 0;
+                        w.ctx = cur.s >= a.P ? cur.g.klen - cur.g.n : 0x7FFFFFFF;
+                        w.out = (w.n < cur.nt ? OUT_SPLIT : 0) | (cur.g.flags & SEG_TWO ? OUT_TWO : 0) | (cur.s >= a.P ? OUT_OWN : 0) |
+                                (!first || (cur.kt == 0 && begin > x0) ? OUT_LATER : 0);
+                        first = false;
                     }
-                    w.plen = cur.g.plen;
-                    w.klen = cur.g.klen;
-                    w.front = cur.g.group;
-                    w.seg = cur.s;
-                    w.h = cur.h;
-                    w.row0 = cur.g.t0 + w.tok0;
-                    w.causal = cur.g.flags & SEG_OWN ? cur.g.n : 0;
-                    w.ctx = cur.s >= a.P ? cur.g.klen - cur.g.n : 0x7FFFFFFF;
-                    w.out = (w.n < cur.nt ? OUT_SPLIT : 0) | (cur.g.flags & SEG_TWO ? OUT_TWO : 0) | (cur.s >= a.P ? OUT_OWN : 0) | (x > x0 ? OUT_LATER : 0);
+                    if (!wait_bounded(&u_empty[b], ph ^ 1u, abort_flag, 76)) break;
+                    if (lane == 0) {
+                        units[b] = w;
+                        mbar_arrive(&u_full[b]);
+                    }
+                    if (++b == 2) { b = 0; ph ^= 1u; }
+                    if (w.n == 0) break;
+                    x += w.n * weight;
+                    if (x >= x1 && lane == 0) tell_cut(a.plan.cut[1] + blockIdx.x, begin, cur.nt, weight, x0, x1, q, cur.h, cur.u, cur.g);
+                    if (x < x1) {
+                        // the next unit begins where this one ends, behind its empty places
+                        cur.next_unit(a, src, SEG_WIDE);
+                        x += (WideUnits::LEAD + 1) * WideUnits::weight(a, cur.g, cur.u) - weight;
+                    }
                 }
-                if (!wait_bounded(&u_empty[b], ph ^ 1u, abort_flag, 76)) break;
-                if (lane == 0) {
-                    units[b] = w;
-                    mbar_arrive(&u_full[b]);
-                }
-                if (++b == 2) { b = 0; ph ^= 1u; }
-                if (w.n == 0) break;
-                if (x + w.n == x1 && lane == 0)
-                    tell_cut(a.plan.cut[1] + blockIdx.x, x - w.ka, x - w.ka + cur.nt, x0, x1, q, cur.h, cur.u, cur.g);
-                x += w.n;
-                if (x < x1) {
-                    cur.next_unit(a, src, SEG_WIDE);
-                    x += WideUnits::LEAD;
-                }
+            };
+            if (TREE && a.self) {
+                Cursor<WideUnits, true> cur;
+                walk(cur, LineSource<true>{self_seg, self_start}, self_N, wide_share(a, self_N, a.wide_ctas));
+            } else {
+                Cursor<WideUnits> cur;
+                walk(cur, LineSource<false>{a.plan.seg, a.plan.wide_start}, a.plan.wide_start[S], a.plan.share[1]);
             }
         } else if (warp == NSW) {
             // --------------------------------------------------------------------------------------- TMA
@@ -764,23 +814,26 @@ static cudaError_t launch_attn_d(const AttnWideArgs& w, bool wide, cudaStream_t 
     const AttnArgs& a = w.a;
     cudaError_t e = wide ? prepare_attn_wide<D, TREE>() : cudaSuccess;
     if (e != cudaSuccess) return e;
-    if (!wide && a.P == 0 && a.R <= FEW_SELF && a.few_hw == 4) {
+    const bool few = !wide || a.wide_min_rows > 1;       // some segments may be the few-row kernel's
+    if (TREE && a.self) {
+        if ((e = launch_pdl(attn_wide_kernel<D, TREE>, dim3(a.wide_ctas), dim3(AW_THREADS), WideCfg<D>::SMEM, st, w)) != cudaSuccess) return e;
+    } else if (!wide && a.P == 0 && a.R <= FEW_SELF && a.few_hw == 4) {
         if ((e = launch_attn_few<D, 4, true, TREE>(a, false, st)) != cudaSuccess) return e;
     } else {
         const int threads = std::min(1024, std::max(128, (a.P + a.R + 31) / 32 * 32));
         if ((e = launch_pdl(attn_plan_kernel, dim3(1), dim3(threads), 0, st, a)) != cudaSuccess) return e;
         if (wide && (e = launch_pdl(attn_wide_kernel<D, TREE>, dim3(a.wide_ctas), dim3(AW_THREADS), WideCfg<D>::SMEM, st, w)) != cudaSuccess) return e;
-        e = a.few_hw == 4 ? launch_attn_few<D, 4, false, TREE>(a, wide, st)
+        if (few) e = a.few_hw == 4 ? launch_attn_few<D, 4, false, TREE>(a, wide, st)
             : a.few_hw == 2 ? launch_attn_few<D, 2, false, TREE>(a, wide, st) : launch_attn_few<D, 1, false, TREE>(a, wide, st);
         if (e != cudaSuccess) return e;
     }
     JoinGrid g;
-    g.wide_split = (int64_t)a.T * a.G >= 2048 ? 8 : 1;      // with few rows nearly all of them have two sources
+    g.wide_split = (int64_t)a.T * a.G >= 2048 ? 8 : a.P ? 1 : 16;      // with few rows and prefixes nearly all of them have two sources
     g.few_split = wide ? 1 : a.few_hw;
     g.wide_blocks = wide ? a.wide_ctas * g.wide_split : 0;
     g.row_blocks = a.P ? (int)std::min<int64_t>(3 * AT_MAX_SMS, ((int64_t)a.T * a.Hq + AT_JOIN_WARPS - 1) / AT_JOIN_WARPS) : 0;
     return launch_pdl((int64_t)a.T * a.Hq <= AT_JOIN_FEW_ROWS ? attn_join_kernel<D, 16> : attn_join_kernel<D, 8>,
-                      dim3(g.row_blocks + g.wide_blocks + a.few_ctas * g.few_split), dim3(AT_JOIN_THREADS), 0, st, a, g);
+                      dim3(std::max(1, g.row_blocks + g.wide_blocks + (few ? a.few_ctas * g.few_split : 0))), dim3(AT_JOIN_THREADS), 0, st, a, g);
 }
 
 cudaError_t launch_attn(const AttnWideArgs& w, int D, bool wide, cudaStream_t st) {

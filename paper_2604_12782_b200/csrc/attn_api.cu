@@ -226,7 +226,7 @@ static osc_status attention(const void* Q, int T, int64_t ldq, int n_q, const os
     const int64_t wide_units = few_units / 8 + (int64_t)R + P;
     const int hw = cache->n_heads % 4 == 0 ? 4 : cache->n_heads % 2 == 0 ? 2 : 1;
     const double most_few = (double)few_units * (cache->n_heads / hw) * (std::max(own_keys, front_keys) / (64.0 / hw) + 1.0);
-    const double most_wide = (double)wide_units * cache->n_heads * ((own_keys + front_keys) / 128.0 + 2.0 + WideUnits::LEAD);
+    const double most_wide = (double)wide_units * cache->n_heads * ((own_keys + front_keys) / 128.0 + 2.0 + WideUnits::LEAD) * (words ? 3.0 : 1.0);      // (places of a tile)
     const double most_request = ((double)R + P) * (cache->n_heads / hw) * (std::max(own_keys, front_keys) / (64.0 / hw) + 1.0);
     if (own_keys > 0x20000000 || front_keys > 0x20000000)
         return fail(OSC_ERR_SHAPE, "table columns hold %lld / %lld keys, at most 2^29 are supported", (long long)own_keys, (long long)front_keys);
@@ -268,6 +268,12 @@ static osc_status attention(const void* Q, int T, int64_t ldq, int n_q, const os
     const bool wide = a.n_pages > 0 && (P > 0 || max_new == 0 || (int64_t)max_new * a.G > AT_FEW_ROWS || most_few >= 2147483648.0);
     a.few_ctas = std::min(di.num_sms * (wide ? 4 : 2), AT_FEW_CTAS);
     a.wide_min_rows = wide ? AT_FEW_ROWS + 1 : 0x7FFFFFFF;
+    // Trees: where requests have more rows than that on average, all go to the tcgen05 kernel (HBM bounds its units with few rows as it does the few-row
+    // kernel), and without prefixes that kernel lays out its line itself: two launches instead of four.
+    if (wide && words && (int64_t)T * a.G > (int64_t)R * AT_FEW_ROWS) {
+        a.wide_min_rows = 1;
+        a.self = P == 0 && R <= WIDE_SELF;
+    }
     if (wide) {
         const int64_t qd[3] = {D, n_q, T}, qs[3] = {1, D, ldq};
         const int qb[3] = {64, a.G, a.tpt};

@@ -50,11 +50,11 @@ constexpr int SEG_TWO = 2;   // the rows have another source: O goes to the work
 
 // A unit that the end of a CTA's share cuts, told by the first CTA that meets it; the join finds its pieces by it.
 struct __align__(16) CutUnit {
-    int begin, share;        // its first tile, and the tiles of a share
+    int begin, share;        // (last) place of its first tile, and the places of a share
     int tiles;               // 0: the share ends with a unit, or the unit's rows have two sources, or it was cut before
     int h, u;                // head (group) and row unit
     int t0, n;               // rows of the segment
-    int pad;
+    int weight;              // places of a tile
 };
 
 struct AttnPlan {            // filled by attn_plan_kernel
@@ -89,6 +89,7 @@ struct AttnArgs {
     int tpt;                 // whole tokens that fit the 128 rows of a tcgen05 tile
     int few_hw;              // heads of a few-row unit: 4, 2 or 1
     int few_ctas, wide_ctas;
+    int self;                // no plan kernel in front of the tcgen05 kernel (masked calls only)
     float scale_log2;        // scale * log2(e)
     const uint32_t* mask;    // [T][ld_mask], null: tokens see the new tokens before them.  Bit m % 32 of word m / 32: the row sees new token m
     int64_t ld_mask;
@@ -152,7 +153,8 @@ __device__ __forceinline__ uint4 drop_odd(const uint4& x) { return make_uint4(dr
 // The two kinds of units.  Few-row: 16 consecutive (token, head) rows of one token list, few_hw heads side by side, tiles
 // of 64 / few_hw keys.  Wide: two tiles of as many whole tokens as fit 128 rows, one head.
 struct FewUnits {
-    static constexpr int LEAD = 0;     // places on the line in front of a unit's tiles
+    static constexpr int LEAD = 0;     // tiles' places on the line in front of a unit's tiles
+    __device__ static int weight(const AttnArgs&, const Segment&, int) { return 1; }     // places of a tile
     __device__ static int key_shift(const AttnArgs& a) { return a.few_hw == 4 ? 4 : a.few_hw == 2 ? 5 : 6; }
     __device__ static int heads(const AttnArgs& a) { return a.Hk / a.few_hw; }
     __device__ static int count(const AttnArgs& a, const Segment& g) { return (g.n * a.G + AT_FEW_ROWS - 1) / AT_FEW_ROWS; }
@@ -171,6 +173,10 @@ struct FewUnits {
 };
 struct WideUnits {
     static constexpr int LEAD = 4;     // a unit costs about that many tiles beside its own: Q, an empty and a filling pipeline, O
+    // Requests with a tree each are units with one row tile or with two, in any mixture.  A key tile takes 1.1 to 1.25 us with one and 1.6 to 1.7 with two
+    // (five requests of 40000 keys, and 24 of 4200, HBM saturated): two places to three.  With the same place for all the CTAs of the five requests ended between
+    // 147 and 227 us.  Prompts without a mask fill both row tiles nearly always.
+    __device__ static int weight(const AttnArgs& a, const Segment& g, int u) { return !a.mask ? 1 : g.n - u * tokens(a) > a.tpt ? 3 : 2; }
     __device__ static constexpr int key_shift(const AttnArgs&) { return 7; }
     __device__ static int heads(const AttnArgs& a) { return a.Hk; }
     __device__ static int tokens(const AttnArgs& a) { return 2 * a.tpt; }
@@ -197,7 +203,7 @@ __device__ __forceinline__ int unit_tiles(const AttnArgs& a, const Segment& g, i
     return front_tiles<U>(a, g) + ((seg_sees(g, U::last_token(a, g, u)) + (1 << U::key_shift(a)) - 1) >> U::key_shift(a));
 }
 template <class U>
-__device__ __forceinline__ int unit_span(int tiles) { return tiles ? tiles + U::LEAD : 0; }
+__device__ __forceinline__ int unit_span(int tiles, int weight) { return tiles ? (tiles + U::LEAD) * weight : 0; }
 // sum over i < n of floor((a i + b) / m), for a, b >= 0 and m > 0, as in Euclid's algorithm
 __device__ __forceinline__ int64_t floor_sum(int64_t n, int64_t m, int64_t a, int64_t b) {
     int64_t sum = 0;
@@ -220,7 +226,10 @@ constexpr int AT_LOOP_UNITS = 64;
 template <class U>
 __device__ __forceinline__ int span_before(const AttnArgs& a, const Segment& g, int nu, int u) {
     if (u == 0) return 0;
-    if (!(g.flags & SEG_OWN)) return u * unit_span<U>(unit_tiles<U>(a, g, 0));
+    if (!(g.flags & SEG_OWN)) {              // all units but the last have the same weight
+        const int tiles = unit_tiles<U>(a, g, 0), all = u == nu ? 1 : 0;
+        return (u - all) * unit_span<U>(tiles, U::weight(a, g, 0)) + all * unit_span<U>(tiles, U::weight(a, g, nu - 1));
+    }
     const int front = front_tiles<U>(a, g);
     int sum = u * front, some = front ? u : 0;   // tiles, and units that have any
     if (g.klen > 0) {
@@ -266,6 +275,7 @@ __device__ __forceinline__ int few_min_tiles(const AttnArgs& a, int n) {
     return max((int)(sqrtf(0.086f * (float)n / ((float)(a.P + a.R) * (float)FewUnits::heads(a))) + 0.5f), 1);
 }
 constexpr int AT_WIDE_MIN_TILES = 4;
+__device__ __forceinline__ int wide_share(const AttnArgs& a, int N, int ctas) { return share_tiles(N, ctas, AT_WIDE_MIN_TILES * (a.mask ? 2 : 1)); }
 // Shares of the two lines of a step that has both (nf, nw tiles).  The tcgen05 kernel is bound by arithmetic, the few-row kernel by
 // memory, and both are resident at once: the first gets as many CTAs as its part of the SMs' time, the second runs on the other
 // SMs.  With 128 channels and the other kernel beside it, a place on the tcgen05 line takes an SM about 1.75 us (1.3, 2560 cycles, where it has
@@ -275,8 +285,9 @@ constexpr int AT_WIDE_MIN_TILES = 4;
 __device__ __forceinline__ void share_lines(const AttnArgs& a, int nf, int nw, int32_t* share) {
     const int sms = a.wide_ctas;
     int wide = sms, few = min(a.few_ctas, 2 * sms);
-    if (nf > 0 && nw > 0) wide = max((int)(sms * (3.0f * nw) / (3.0f * nw + nf) + 0.5f), 1);
-    const int q = share_tiles(nw, wide, AT_WIDE_MIN_TILES);
+    const float tiles = a.mask ? 0.4f * nw : (float)nw;
+    if (nf > 0 && nw > 0) wide = max((int)(sms * (3.0f * tiles) / (3.0f * tiles + nf) + 0.5f), 1);
+    const int q = wide_share(a, nw, wide);
     const int left = 2 * (sms - (nw + q - 1) / q);
     if (nw > 0 && left > 0 && left <= a.few_ctas) few = a.few_ctas / left * left;
     share[0] = share_tiles(nf, few, few_min_tiles(a, nf));
@@ -323,13 +334,15 @@ struct Cursor {
         y -= h * g.tiles;
         if (!(g.flags & SEG_OWN)) {
             nt = unit_tiles<U>(a, g, 0);
-            u = y / unit_span<U>(nt);
-            kt = y - u * unit_span<U>(nt) - U::LEAD;
+            const int span = unit_span<U>(nt, U::weight(a, g, 0));
+            u = min(y / span, nu - 1);
+            const int w = U::weight(a, g, u);
+            kt = (y - u * span) / w - U::LEAD;               // a tile counts where its last place is
         } else if (nu <= AT_LOOP_UNITS) {
             u = 0;
             nt = unit_tiles<U>(a, g, 0);
-            while (y >= unit_span<U>(nt)) {
-                y -= unit_span<U>(nt);
+            while (y >= unit_span<U>(nt, 1)) {
+                y -= unit_span<U>(nt, 1);
                 nt = unit_tiles<U>(a, g, ++u);
             }
             kt = y - U::LEAD;
@@ -361,21 +374,23 @@ struct Cursor {
     }
 };
 
-// first tile of unit u of head h of a segment
+// (last) place of the first tile of unit u of head h of a segment
 template <class U>
 __device__ __forceinline__ int unit_begin(const AttnArgs& a, const Segment& g, int h, int u) {
-    return g.start + h * g.tiles + span_before<U>(a, g, U::count(a, g), u) + U::LEAD;
+    return g.start + h * g.tiles + span_before<U>(a, g, U::count(a, g), u) + (U::LEAD + 1) * U::weight(a, g, u) - 1;
 }
 
-__device__ __forceinline__ void tell_cut(CutUnit* c, int unit_x0, int unit_x1, int x0, int x1, int q, int h, int u,
+// unit_x0: (last) place of the unit's first tile
+__device__ __forceinline__ void tell_cut(CutUnit* c, int unit_x0, int tiles, int weight, int x0, int x1, int q, int h, int u,
                                          const Segment& g) {
     c->begin = unit_x0;
+    c->weight = weight;
     c->share = q;
     c->h = h;
     c->u = u;
     c->t0 = g.t0;
     c->n = g.n;
-    c->tiles = unit_x1 > x1 && unit_x0 >= x0 && !(g.flags & SEG_TWO) ? unit_x1 - unit_x0 : 0;
+    c->tiles = unit_x0 + (tiles - 1) * weight >= x1 && unit_x0 >= x0 && !(g.flags & SEG_TWO) ? tiles : 0;
 }
 
 // ------------------------------------------------------------------------------------------------ the plan
@@ -551,11 +566,11 @@ struct PieceList {           // pieces of one row from one unit
     int count;               // 0: none; 1: the whole unit
     int first, rest, stride; // rows of the partial results: `first` for piece 0, rest + i * stride for the others
 };
-// A unit of `tiles` tiles from `begin` on, cut into shares of q; `base`: row of the line's slots; stride: rows between two
+// A unit of `tiles` tiles of `weight` places from `begin` on, cut into shares of q (each of which has a tile at least); `base`: row of the line's slots; stride: rows between two
 // slots of a CTA; row: row in a slot; whole: row of the dense results
-__device__ __forceinline__ PieceList list_pieces(int begin, int tiles, int q, int base, int stride, int row, int whole) {
+__device__ __forceinline__ PieceList list_pieces(int begin, int tiles, int weight, int q, int base, int stride, int row, int whole) {
     PieceList p;
-    const int c0 = begin / q, c1 = (begin + tiles - 1) / q;
+    const int c0 = begin / q, c1 = (begin + (tiles - 1) * weight) / q;
     p.count = c1 - c0 + 1;
     p.stride = 2 * stride;
     p.rest = base + c0 * 2 * stride + row;
@@ -956,7 +971,7 @@ __global__ void __launch_bounds__(AT_FEW_THREADS, 2) attn_few_kernel(const AttnA
             }
         }
         if (x < x1) cur.next_unit(a, src, 0);
-        else if (threadIdx.x == 0) tell_cut(a.plan.cut[0] + blockIdx.x, unit_x0, unit_x1, x0, x1, q, cur.h, cur.u, cur.g);
+        else if (threadIdx.x == 0) tell_cut(a.plan.cut[0] + blockIdx.x, unit_x0, unit_x1 - unit_x0, 1, x0, x1, q, cur.h, cur.u, cur.g);
     }
     cp_async_wait<0>();
     if (early && blockIdx.x == gridDim.x - 1) grid_dependency_wait();
@@ -1067,7 +1082,7 @@ __global__ void __launch_bounds__(AT_JOIN_THREADS, FLIGHT > 8 ? 2 : 3) attn_join
             const int row = part * rows + i, r = wide ? row % AT_WIDE_TILE : cut.u * AT_FEW_ROWS + row % AT_FEW_ROWS;
             const int tok = r / a.G + (wide ? (cut.u * 2 + row / AT_WIDE_TILE) * a.tpt : 0);
             if ((wide && r >= a.tpt * a.G) || tok >= cut.n) continue;
-            p[1] = list_pieces(cut.begin, cut.tiles, cut.share, wide ? AT_FEW_SLOTS : 0, slot_rows, row, 0);
+            p[1] = list_pieces(cut.begin, cut.tiles, cut.weight, cut.share, wide ? AT_FEW_SLOTS : 0, slot_rows, row, 0);
             join_row<D, FLIGHT>(a, p, cut.t0 + tok, (wide ? cut.h : cut.h * a.few_hw + row / AT_FEW_ROWS) * a.G + r % a.G);
         }
         return;
@@ -1095,7 +1110,7 @@ __global__ void __launch_bounds__(AT_JOIN_THREADS, FLIGHT > 8 ? 2 : 3) attn_join
             const int row = w ? (in >= tpt ? AT_WIDE_TILE + (in - tpt) * a.G : in * a.G) + g : (h & (a.few_hw - 1)) * AT_FEW_ROWS + fr % AT_FEW_ROWS;
             const int nt = w ? unit_tiles<WideUnits>(a, sg, u) : unit_tiles<FewUnits>(a, sg, u);
             const int begin = w ? unit_begin<WideUnits>(a, sg, h, u) : unit_begin<FewUnits>(a, sg, h >> hs, u);
-            if (nt) x = list_pieces(begin, nt, w ? nw : nf, w ? AT_FEW_SLOTS : 0, w ? 2 * AT_WIDE_TILE : a.few_hw * AT_FEW_ROWS, row, dense_row(a, which, i));
+            if (nt) x = list_pieces(begin, nt, w ? WideUnits::weight(a, sg, u) : 1, w ? nw : nf, w ? AT_FEW_SLOTS : 0, w ? 2 * AT_WIDE_TILE : a.few_hw * AT_FEW_ROWS, row, dense_row(a, which, i));
         }
         __syncwarp();
 #pragma unroll

@@ -10,9 +10,8 @@
 // vectors into a ring in shared memory (cp.async), two chunks ahead; nobody else reads them, so the ring needs no barrier.
 //
 // Alternatives: the order is value, then lower index, as one key: the value's bits made monotone (NaN below -inf) and the index.  A thread's
-// largest value of a chunk is known from the maximum above.  First chunk: the largest 16-bit key prefix that k threads' largest values reach bounds
-// the k-th best value of the row from below (found by halving, a barrier that counts a step), and few other values pass it, so the values at
-// or above it go to a list in shared memory.  Later chunks: only values above the bound, without a barrier; the list is joined with the k best so far,
+// largest value of a chunk is known from the maximum above.  First chunk: the k-th of the warps' four largest such values bounds the k-th best
+// value of the row from below, and few other values pass it, so the values at or above it go to a list in shared memory.  Later chunks: only values above the bound, without a barrier; the list is joined with the k best so far,
 // which raises the bound, behind chunks 1, 2, 4, 8, ... and the last: some k candidates each time.  Where a thread has some, its warp looks at its values
 // of the chunk in shared memory, one lane each.  (By the thread itself, in registers one by one, that cost more than the sums: 600 us for 3001 rows of
 // 152064; in shared memory 394.)  Where too many values pass (equal logits, rows in rising order) the chunks since the last rank are read again, each with a bound of its
@@ -26,11 +25,10 @@
 
 namespace osc {
 
-constexpr int LP_THREADS = 256, LP_WARPS = LP_THREADS / 32;
 constexpr int LP_VECS = 4;               // 16-byte vectors of a chunk, per thread
 static_assert(LP_VECS * 8 <= 32, "a lane for every value of a thread");
 constexpr int LP_STAGES = 3;             // chunks in the ring
-constexpr int LP_RING = LP_STAGES * LP_THREADS * LP_VECS * 16;
+constexpr int LP_SHORT_BYTES = 16384;    // rows up to here
 constexpr int LP_MAX_TOP = 32;
 constexpr int LP_LIST = 512;            // candidates that wait to be ranked
 constexpr int LP_MAX_CLUSTER = 8;
@@ -81,20 +79,22 @@ struct LpVec {
     }
 };
 
-template <bool F32, bool TOP>
-__global__ void __launch_bounds__(LP_THREADS, 4) token_logprobs_kernel(const LogprobArgs a, int cluster) {
+template <bool F32, bool TOP, int NT>
+__global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const LogprobArgs a, int cluster) {
     using Vec = LpVec<F32>;
     using Elem = typename Vec::Elem;
-    constexpr int E = Vec::E, U = LP_VECS, CHUNK = LP_THREADS * U;
+    constexpr int E = Vec::E, U = LP_VECS, CHUNK = NT * U, WARPS = NT / 32;
     extern __shared__ __align__(16) uint8_t lp_ring[];       // [LP_STAGES][CHUNK] vectors
     __shared__ unsigned long long s_list[TOP ? LP_LIST : 1];             // candidates since the last rank
     __shared__ unsigned long long s_kept[2][TOP ? LP_MAX_TOP : 1];       // the k best, in order (0: none); the one of two that `which` says
-    __shared__ unsigned long long s_warp[LP_WARPS];
-    __shared__ float s_red[3][LP_WARPS];
-    __shared__ float s_part[3];                      // (max, l, S) of the block
-    __shared__ int s_which;
+    __shared__ unsigned long long s_warp[WARPS];
+    __shared__ float s_red[3][WARPS];
+    __shared__ unsigned long long s_in[TOP ? LP_MAX_CLUSTER * LP_MAX_TOP : 1];     // the k best of the cluster's other blocks, in the one of rank 0
+    __shared__ float s_part[LP_MAX_CLUSTER][3];      // (max, l, S) of the cluster's blocks, likewise
+    __shared__ __align__(16) uint32_t s_largest[32];
     __shared__ int s_n, s_over;                      // candidates; whether some found no place
     grid_launch_dependents();
+    if (cluster > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");      // every block is there before anyone writes to rank 0
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rank = cluster > 1 ? (int)cluster_ctarank() : 0;
     const int64_t row = blockIdx.x / cluster;
@@ -114,13 +114,13 @@ __global__ void __launch_bounds__(LP_THREADS, 4) token_logprobs_kernel(const Log
     const int full0 = lead ? 1 : 0, full1 = max((int)(((int64_t)lead + a.V) / E), full0);
     const int v0 = full0 + (int)((int64_t)(full1 - full0) * rank / cluster), v1 = full0 + (int)((int64_t)(full1 - full0) * (rank + 1) / cluster);
 
-    uint4* mine = reinterpret_cast<uint4*>(lp_ring) + tid;       // the thread's vectors of a stage: mine[u * LP_THREADS]
+    uint4* mine = reinterpret_cast<uint4*>(lp_ring) + tid;       // the thread's vectors of a stage: mine[u * NT]
     const uint64_t policy = l2_policy_evict_first();             // read once
     auto load = [&](int base, int stage) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int i = base + u * LP_THREADS + tid;
-            if (i < v1) cp_async_16(smem_u32(mine + stage * CHUNK + u * LP_THREADS), xv + i, true, policy);
+            const int i = base + u * NT + tid;
+            if (i < v1) cp_async_16(smem_u32(mine + stage * CHUNK + u * NT), xv + i, true, policy);
         }
         cp_async_commit();
     };
@@ -138,20 +138,22 @@ __global__ void __launch_bounds__(LP_THREADS, 4) token_logprobs_kernel(const Log
     if (TOP) __syncthreads();
 
     // Joins the candidates with the k best; `bound` becomes the last one's key.  All threads have passed a barrier since the last candidate came.
-    auto rank_list = [&]() {
-        const int n = min(s_n, LP_LIST);
+    auto rank_list = [&](const unsigned long long* list, int n) {
         unsigned long long* to = s_kept[which ^ 1];
         const unsigned long long* from = s_kept[which];
+        // four lanes to an entry, which share out the others
 #pragma unroll 1
-        for (int i = tid; i < n + k; i += LP_THREADS) {
-            const unsigned long long x = i < k ? from[i] : s_list[i - k];
-            if (x == 0) continue;
+        for (int i0 = 0; i0 < n + k; i0 += NT / 4) {
+            const int i = i0 + tid / 4;
+            const unsigned long long x = i < k ? from[i] : i < n + k ? list[i - k] : 0;
             int better = 0;
+#pragma unroll 2
+            for (int j = tid & 3; j < k; j += 4) better += from[j] > x;
 #pragma unroll 4
-            for (int j = 0; j < k; ++j) better += from[j] > x;
-#pragma unroll 4
-            for (int j = 0; j < n; ++j) better += s_list[j] > x;
-            if (better < k) to[better] = x;
+            for (int j = tid & 3; j < n; j += 4) better += list[j] > x;
+            better += __shfl_xor_sync(0xFFFFFFFFu, better, 1);
+            better += __shfl_xor_sync(0xFFFFFFFFu, better, 2);
+            if (x != 0 && better < k) to[better] = x;
         }
         __syncthreads();
         which ^= 1;
@@ -165,34 +167,59 @@ __global__ void __launch_bounds__(LP_THREADS, 4) token_logprobs_kernel(const Log
         if (n < LP_LIST) s_list[n] = lp_rank(key, j);
         else s_over = 1;
     };
-    // every value of the thread in a chunk, which lies at `at` (LP_THREADS vectors apart): f(key, index)
+    // every value of the thread in a chunk, which lies at `at` (NT vectors apart): f(key, index)
     auto each = [&](const uint4* at, int base, auto f) {
 #pragma unroll 1
-        for (int u = 0; u < U && base + u * LP_THREADS + tid < v1; ++u) {
-            const uint4 x = at[u * LP_THREADS];
-            const int j = (base + u * LP_THREADS + tid) * E - lead;
+        for (int u = 0; u < U && base + u * NT + tid < v1; ++u) {
+            const uint4 x = at[u * NT];
+            const int j = (base + u * NT + tid) * E - lead;
 #pragma unroll
             for (int e = 0; e < E; ++e) f(lp_key(Vec::get(x, e)), j + e);
         }
     };
-    // a key that at least k of the threads' largest values reach, or 0
-    auto reached = [&](uint32_t best) -> uint32_t {
-        uint32_t t = 0;
+    // A key that at least k of the threads' largest values reach, or 0: the k-th of the largest few of every warp that has some, 2^n warps and 32 values at
+    // the most.
+    auto reached = [&](uint32_t best, int base) -> uint32_t {
+        const int active = min(WARPS, (v1 - base + 31) / 32), warps = 1 << (31 - __clz(active)), each_has = min(32 / warps, 2 * ((k + warps - 1) / warps));
+        if (warp < warps) {
+            uint32_t keep = 0;
 #pragma unroll 1
-        for (int bit = 15; bit >= 0; --bit)
-            if (__syncthreads_count(best >> 16 >= (t | 1u << bit)) >= k) t |= 1u << bit;
-        return t << 16;
+            for (int i = 0; i < each_has; ++i) {         // of equal ones the first lane's
+                const uint32_t t = __reduce_max_sync(0xFFFFFFFFu, best);
+                if (lane == i) keep = t;
+                if (lane == __ffs((int)__ballot_sync(0xFFFFFFFFu, best == t)) - 1) best = 0;
+            }
+            if (lane < each_has) s_largest[warp * each_has + lane] = keep;
+        }
+        __syncthreads();
+        const int have = warps * each_has;
+        const uint32_t mine = lane < have ? s_largest[lane] : 0;
+        int better = 0;
+#pragma unroll
+        for (int j = 0; j < 32; j += 4) {
+            const uint4 x = *reinterpret_cast<const uint4*>(s_largest + j);      // (broadcasts: 32 shuffles a warp took 1000 cycles with four blocks on the SM)
+            better += j < have && (x.x > mine || (x.x == mine && j < lane));
+            better += j + 1 < have && (x.y > mine || (x.y == mine && j + 1 < lane));
+            better += j + 2 < have && (x.z > mine || (x.z == mine && j + 2 < lane));
+            better += j + 3 < have && (x.w > mine || (x.w == mine && j + 3 < lane));
+        }
+        const uint32_t at = __ballot_sync(0xFFFFFFFFu, lane < have && better == k - 1);
+        return at ? __shfl_sync(0xFFFFFFFFu, mine, __ffs((int)at) - 1) : 0;
     };
     // a chunk with many values above the bound, read once more
     auto again = [&](int base) {
         const uint4* at = xv + base + tid;
         uint32_t best = 0;
         each(at, base, [&](uint32_t key, int) { best = max(best, key); });
-        const uint32_t t = reached(best);
-        if (t) set_bound(max(bound, t - 1));
+        // the largest 16-bit prefix of a key that k threads' largest values reach
+        uint32_t t = 0;
+#pragma unroll 1
+        for (int bit = 15; bit >= 0; --bit)
+            if (__syncthreads_count(best >> 16 >= (t | 1u << bit)) >= k) t |= 1u << bit;
+        if (t) set_bound(max(bound, (t << 16) - 1));
         each(at, base, [&](uint32_t key, int j) { if (key > bound) add(key, j); });
         __syncthreads();
-        if (!s_over) return rank_list();
+        if (!s_over) return rank_list(s_list, s_n);
         __syncthreads();
         if (tid == 0) s_n = 0;
         __syncthreads();
@@ -211,14 +238,30 @@ __global__ void __launch_bounds__(LP_THREADS, 4) token_logprobs_kernel(const Log
             __syncthreads();
             last = s_warp[0];
 #pragma unroll
-            for (int w = 1; w < LP_WARPS; ++w) last = max(last, s_warp[w]);
+            for (int w = 1; w < WARPS; ++w) last = max(last, s_warp[w]);
             __syncthreads();
             if ((uint32_t)(last >> 32) <= bound) break;      // 0, or no better than the k of the chunks before
             if (tid == 0) s_list[s_n++] = last;
         }
         __syncthreads();
-        rank_list();
+        rank_list(s_list, s_n);
     };
+
+    // ---- the elements in front of the row's first whole vector and behind its last one
+    const int head = min(full0 * E - lead, a.V), tail = max(full1 * E - lead, head);          // [0, head), [tail, V)
+    const int edge = rank == 0 && tid < head ? tid : rank == cluster - 1 && tid >= 32 && tid - 32 < a.V - tail ? tail + tid - 32 : -1;
+    if (edge >= 0) {
+        const float x = Vec::value(xr[edge]);
+        if (x != -INFINITY) {
+            m = x != x ? -INFINITY : x;
+            l = lp_exp2((x - x) * scale2);           // 1, or NaN
+        }
+        if (TOP) add(lp_key(x), edge);
+    }
+    if (TOP && v0 >= v1) {
+        __syncthreads();
+        rank_list(s_list, s_n);
+    }
 
     int stage = 0, chunk = 0, since = v0;        // since: first vector of the chunks that are not ranked
 #pragma unroll 1
@@ -232,7 +275,7 @@ __global__ void __launch_bounds__(LP_THREADS, 4) token_logprobs_kernel(const Log
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             v[u].x = v[u].y = v[u].z = v[u].w = F32 ? 0xFF800000u : 0xFF80FF80u;      // past the end: -inf
-            if (base + u * LP_THREADS + tid < v1) v[u] = at[u * LP_THREADS];
+            if (base + u * NT + tid < v1) v[u] = at[u * NT];
         }
         // ---- the chunk's maximum (a NaN leaves it alone)
         float top;
@@ -266,7 +309,7 @@ __global__ void __launch_bounds__(LP_THREADS, 4) token_logprobs_kernel(const Log
             uint64_t lc = 0, sc = 0;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                if (base + u * LP_THREADS + tid >= v1) break;
+                if (base + u * NT + tid >= v1) break;
 #pragma unroll
                 for (int e = 0; e < E; e += 2) {
                     const uint64_t d = add2(pack2(Vec::get(v[u], e), Vec::get(v[u], e + 1)), ref2);
@@ -284,8 +327,8 @@ __global__ void __launch_bounds__(LP_THREADS, 4) token_logprobs_kernel(const Log
             if (sum != sum) {        // 0 * -inf: -inf among the logits (or a NaN, or +inf, which l shows)
                 sum = 0.0f;
 #pragma unroll 1
-                for (int u = 0; u < U && base + u * LP_THREADS + tid < v1; ++u) {
-                    const uint4 x = at[u * LP_THREADS];
+                for (int u = 0; u < U && base + u * NT + tid < v1; ++u) {
+                    const uint4 x = at[u * NT];
 #pragma unroll
                     for (int e = 0; e < E; ++e) {
                         const float d = Vec::get(x, e) + ref, p = lp_exp2(d * scale2);
@@ -304,16 +347,16 @@ __global__ void __launch_bounds__(LP_THREADS, 4) token_logprobs_kernel(const Log
                     best = 0;
                     each(at, base, [&](uint32_t key, int) { best = max(best, key); });
                 }
-                const uint32_t t = reached(best);
+                const uint32_t t = reached(best, base);
                 set_bound(t ? t - 1 : 0);            // values at t are candidates themselves
             }
             __syncwarp();                            // the lanes' copies, for one another
             uint32_t lanes = __ballot_sync(0xFFFFFFFFu, bound < LP_KEY_LOW ? base + tid < v1 : top > value);
 #pragma unroll 1
             for (; lanes; lanes &= lanes - 1) {
-                const int of = tid - lane + __ffs((int)lanes) - 1, u = lane / E, e = lane % E, i = base + u * LP_THREADS + of;
+                const int of = tid - lane + __ffs((int)lanes) - 1, u = lane / E, e = lane % E, i = base + u * NT + of;
                 uint32_t key = 0;
-                if (lane < U * E && i < v1) key = lp_key(Vec::value(reinterpret_cast<const Elem*>(at - tid + u * LP_THREADS + of)[e]));
+                if (lane < U * E && i < v1) key = lp_key(Vec::value(reinterpret_cast<const Elem*>(at - tid + u * NT + of)[e]));
                 const uint32_t found = __ballot_sync(0xFFFFFFFFu, key > bound);
                 if (found == 0) continue;
                 int n = 0;
@@ -327,12 +370,13 @@ __global__ void __launch_bounds__(LP_THREADS, 4) token_logprobs_kernel(const Log
             if ((chunk & (chunk + 1)) == 0 || base + CHUNK >= v1) {
                 __syncthreads();
                 if (!s_over) {
-                    rank_list();
+                    rank_list(s_list, s_n);
                 } else {
                     __syncthreads();
                     if (tid == 0) s_n = s_over = 0;
                     set_bound((uint32_t)(s_kept[which][k - 1] >> 32));
                     __syncthreads();
+                    if (since == v0 && edge >= 0) add(lp_key(Vec::value(xr[edge])), edge);
 #pragma unroll 1
                     for (int b = since; b < min(base + CHUNK, v1); b += CHUNK) again(b);
                 }
@@ -341,31 +385,6 @@ __global__ void __launch_bounds__(LP_THREADS, 4) token_logprobs_kernel(const Log
         }
     }
     cp_async_wait<0>();
-
-    // ---- the elements in front of the row's first whole vector and behind its last one
-    {
-        const int head = min(full0 * E - lead, a.V), tail = max(full1 * E - lead, head);      // [0, head), [tail, V)
-        const int j = rank == 0 && tid < head ? tid : rank == cluster - 1 && tid >= 32 && tid - 32 < a.V - tail ? tail + tid - 32 : -1;
-        if (j >= 0) {
-            const float x = Vec::value(xr[j]);
-            if (x > m) {
-                const float d = m - x, f = m > -INFINITY ? lp_exp2(d * scale2) : 0.0f;
-                S = f == 0.0f ? 0.0f : f * (S + l * d);
-                l = f == 0.0f && l == l ? 0.0f : l * f;
-                m = x;
-            }
-            if (x != -INFINITY) {
-                const float d = x - (m == -INFINITY ? 0.0f : m), p = lp_exp2(d * scale2);
-                l += p;
-                if (p != 0.0f) S += p * d;
-            }
-            if (TOP) add(lp_key(x), j);
-        }
-        if (TOP && (head > 0 || tail < a.V)) {
-            __syncthreads();
-            rank_list();
-        }
-    }
 
     // ---- the block's (max, l, S)
     {
@@ -376,7 +395,7 @@ __global__ void __launch_bounds__(LP_THREADS, 4) token_logprobs_kernel(const Log
         __syncthreads();
         M = s_red[0][0];
 #pragma unroll
-        for (int w = 1; w < LP_WARPS; ++w) M = fmaxf(M, s_red[0][w]);
+        for (int w = 1; w < WARPS; ++w) M = fmaxf(M, s_red[0][w]);
         float f = 1.0f, d = 0.0f;
         if (m != -INFINITY || l != 0.0f) {           // l without a maximum: a NaN
             d = m == -INFINITY ? 0.0f : m - M;
@@ -397,61 +416,40 @@ __global__ void __launch_bounds__(LP_THREADS, 4) token_logprobs_kernel(const Log
         m = M;
         l = S = 0.0f;
 #pragma unroll
-        for (int w = 0; w < LP_WARPS; ++w) {
+        for (int w = 0; w < WARPS; ++w) {
             l += s_red[1][w];
             S += s_red[2][w];
         }
-        if (tid == 0) {
-            s_part[0] = m;
-            s_part[1] = l;
-            s_part[2] = S;
-        }
     }
-    // ---- the cluster's: every block joins the sums in rank order, rank 0 the candidates and the rest
+
+    // ---- the cluster's: the others hand their sums and their k best to rank 0, which joins them in rank order
     if (cluster > 1) {
-        if (TOP && tid == 0) s_which = which;
-        cluster_sync_all();
-        if (rank == 0) {
-            const uint32_t part = smem_u32(s_part);
-            auto ld32 = [](uint32_t addr) {
-                uint32_t r;
-                asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(r) : "r"(addr) : "memory");
-                return r;
-            };
-            float pm[LP_MAX_CLUSTER], pl[LP_MAX_CLUSTER], ps[LP_MAX_CLUSTER];
-            m = -INFINITY;
-#pragma unroll
-            for (int c = 0; c < LP_MAX_CLUSTER; ++c)
-                if (c < cluster) {
-                    const uint32_t p = map_to_cta(part, c);
-                    pm[c] = __uint_as_float(ld32(p));
-                    pl[c] = __uint_as_float(ld32(p + 4));
-                    ps[c] = __uint_as_float(ld32(p + 8));
-                    m = fmaxf(m, pm[c]);
-                }
-            l = S = 0.0f;
-#pragma unroll
-            for (int c = 0; c < LP_MAX_CLUSTER; ++c)
-                if (c < cluster && pl[c] != 0.0f) {
-                    const float d = pm[c] == -INFINITY ? 0.0f : pm[c] - m, f = lp_exp2(d * scale2);
-                    if (f == 0.0f && pl[c] == pl[c]) continue;
-                    l += pl[c] * f;
-                    S += f * (ps[c] + pl[c] * d);
-                }
-            if constexpr (TOP) {
-                // the others' k best as candidates; which of the two buffers holds them depends on how often a block has ranked
-                for (int i = tid; i < (cluster - 1) * k; i += LP_THREADS) {
-                    const int c = 1 + i / k;
-                    const uint32_t p = map_to_cta(smem_u32(s_kept[ld32(map_to_cta(smem_u32(&s_which), c))] + i % k), c);
-                    s_list[i] = (unsigned long long)ld32(p + 4) << 32 | ld32(p);
-                }
-                if (tid == 0) s_n = (cluster - 1) * k;
-                __syncthreads();
-                rank_list();
+        asm volatile("barrier.cluster.wait;" ::: "memory");
+        if (rank) {
+            if (TOP && tid < k) {
+                const unsigned long long x = s_kept[which][tid];
+                const uint32_t to = map_to_cta(smem_u32(s_in + (rank - 1) * k + tid), 0);
+                st_cluster(to, (uint32_t)x);
+                st_cluster(to + 4, (uint32_t)(x >> 32));
             }
+            if (tid < 3) st_cluster(map_to_cta(smem_u32(&s_part[rank][tid]), 0), __float_as_uint(tid == 0 ? m : tid == 1 ? l : S));
+        } else if (tid < 3) {
+            s_part[0][tid] = tid == 0 ? m : tid == 1 ? l : S;
         }
-        cluster_sync_all();      // nobody leaves while its shared memory is read
+        asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
         if (rank) return;
+        m = -INFINITY;
+        for (int c = 0; c < cluster; ++c) m = fmaxf(m, s_part[c][0]);
+        l = S = 0.0f;
+        for (int c = 0; c < cluster; ++c) {
+            const float pl = s_part[c][1];
+            if (pl == 0.0f) continue;
+            const float d = s_part[c][0] == -INFINITY ? 0.0f : s_part[c][0] - m, f = lp_exp2(d * scale2);
+            if (f == 0.0f && pl == pl) continue;
+            l += pl * f;
+            S += f * (s_part[c][2] + pl * d);
+        }
+        if (TOP) rank_list(s_in, (cluster - 1) * k);
     }
     const float ln = logf(l), nan = __uint_as_float(0x7FC00000u);
     const bool empty = l == 0.0f;        // no logit above -inf
@@ -461,12 +459,12 @@ __global__ void __launch_bounds__(LP_THREADS, 4) token_logprobs_kernel(const Log
         if (a.lse) a.lse[row] = bad ? nan : empty ? -INFINITY : a.scale * m + ln;
         if (a.entropy) a.entropy[row] = bad ? nan : empty ? 0.0f : ln - a.scale * S / l;
     }
-    for (int i = tid; i < a.n_ids; i += LP_THREADS) {
+    for (int i = tid; i < a.n_ids; i += NT) {
         const int id = a.ids[row * a.ld_ids + i];
         a.logprob[row * a.n_ids + i] = id >= 0 && id < a.V ? logprob(Vec::value(xr[id])) : -INFINITY;
     }
     if (TOP) {
-        for (int i = tid; i < k; i += LP_THREADS) {
+        for (int i = tid; i < k; i += NT) {
             const unsigned long long c = s_kept[which][i];
             const bool there = c != 0;
             a.top_ids[row * k + i] = there ? (int)~(uint32_t)c : -1;
@@ -475,14 +473,15 @@ __global__ void __launch_bounds__(LP_THREADS, 4) token_logprobs_kernel(const Log
     }
 }
 
-template <bool F32, bool TOP>
+template <bool F32, bool TOP, int NT>
 static cudaError_t launch_logprobs_t(const LogprobArgs& a, int cluster, cudaStream_t st) {
     static PerDevice pd;
-    if (cudaError_t e = opt_in_shared_memory(pd, token_logprobs_kernel<F32, TOP>, LP_RING)) return e;
+    constexpr int RING = LP_STAGES * NT * LP_VECS * 16;
+    if (cudaError_t e = opt_in_shared_memory(pd, token_logprobs_kernel<F32, TOP, NT>, RING)) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((int64_t)a.T * cluster));
-    cfg.blockDim = dim3(LP_THREADS);
-    cfg.dynamicSmemBytes = LP_RING;
+    cfg.blockDim = dim3(NT);
+    cfg.dynamicSmemBytes = RING;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -493,16 +492,22 @@ static cudaError_t launch_logprobs_t(const LogprobArgs& a, int cluster, cudaStre
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = cluster > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, token_logprobs_kernel<F32, TOP>, a, cluster);
+    return cudaLaunchKernelEx(&cfg, token_logprobs_kernel<F32, TOP, NT>, a, cluster);
+}
+template <bool F32, bool TOP>
+static cudaError_t launch_logprobs(const LogprobArgs& a, int num_sms, cudaStream_t st) {
+    // Short rows, many of them: blocks of two warps, of which 16 are on an SM at a time.
+    if ((int64_t)a.V * (F32 ? 4 : 2) <= LP_SHORT_BYTES) return launch_logprobs_t<F32, TOP, 64>(a, 1, st);
+    // A cluster where the rows alone do not fill the machine, as long as every block of it has a chunk's work.
+    const int64_t chunk = 256ll * LP_VECS * (F32 ? 4 : 8);
+    int cluster = 1;
+    while (cluster < LP_MAX_CLUSTER && (int64_t)a.T * cluster * 2 <= 3 * num_sms && (int64_t)a.V > chunk / 2 * cluster) cluster *= 2;
+    return launch_logprobs_t<F32, TOP, 256>(a, cluster, st);
 }
 
 cudaError_t launch_token_logprobs(const LogprobArgs& a, bool f32, int num_sms, cudaStream_t st) {
-    // A cluster where the rows alone do not fill the machine, as long as every block of it has a chunk's work.
-    const int64_t chunk = (int64_t)LP_THREADS * LP_VECS * (f32 ? 4 : 8);
-    int cluster = 1;
-    while (cluster < LP_MAX_CLUSTER && (int64_t)a.T * cluster * 2 <= 6 * num_sms && (int64_t)a.V > chunk / 2 * cluster) cluster *= 2;
-    if (a.k) return f32 ? launch_logprobs_t<true, true>(a, cluster, st) : launch_logprobs_t<false, true>(a, cluster, st);
-    return f32 ? launch_logprobs_t<true, false>(a, cluster, st) : launch_logprobs_t<false, false>(a, cluster, st);
+    if (a.k) return f32 ? launch_logprobs<true, true>(a, num_sms, st) : launch_logprobs<false, true>(a, num_sms, st);
+    return f32 ? launch_logprobs<true, false>(a, num_sms, st) : launch_logprobs<false, false>(a, num_sms, st);
 }
 
 }  // namespace osc
