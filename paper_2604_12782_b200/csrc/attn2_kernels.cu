@@ -16,7 +16,9 @@
 //   warps 0-3, 4-7 : softmax of stream 0, 1, and their epilogue
 //   warp 8         : TMA (a key tile is loaded page by page; a page that is not there reads as zeros)
 //   warps 9, 11    : MMA issue of S, of P V (warp 9 owns TMEM)
-//   warp 10        : the units of the CTA's share, for everyone else
+//   warp 10        : the units of the CTA's share, for everyone else, one ahead; with small pages also the TMA of V.  (In pages of 16 tokens the issue of
+//                    2 x 16 copies a tile was what bounded it, 2.3 us: 40 trees behind 4100 keys 117 -> 102 us with the copies in two warps.  With larger
+//                    pages one warp keeps K and V in step, and where HBM is the limit that matters: five contexts of 40000 keys 237 us with one, 253 with two.)
 //
 // Bound by the tensor pipe and the exponentials alike (72 % of the cycles each): 2560 cycles per 128 keys of both tiles, of which the four
 // products are 2080 and the exponentials 2048, and 7000 cycles to end a unit and begin the next one (5000 of them the epilogue; a second Q and a second pair of O
@@ -55,6 +57,7 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return r;
 }
 
+constexpr int AW_UNITS = 4;            // units in shared memory
 constexpr int WIDE_SELF = 256;         // requests whose line every CTA lays out for itself
 
 template <int D>
@@ -67,8 +70,8 @@ struct WideCfg {
     static constexpr int STAGES = D == 128 ? 2 : 4;              // K tiles, and as many V tiles
     static constexpr int OUT_BYTES = AW_SOFTMAX_WARPS * 2048;    // every softmax warp's 32 rows x 64 bytes of O on the way out
     static constexpr int ROW_FLOATS = 2 * 2 * 2 * 128;           // [parity][stream][128] maxima and sums of a unit
-    static constexpr int BAR_BYTES = 320;
-    static constexpr int PLAN = 2 * QTILE_BYTES + 2 * STAGES * TILE_BYTES + OUT_BYTES + ROW_FLOATS * 4 + BAR_BYTES + 2 * 80 + 32;      // where a line laid out here lies
+    static constexpr int BAR_BYTES = 384;
+    static constexpr int PLAN = 2 * QTILE_BYTES + 2 * STAGES * TILE_BYTES + OUT_BYTES + ROW_FLOATS * 4 + BAR_BYTES + AW_UNITS * 80;      // where a line laid out here lies
     static constexpr int SMEM = PLAN + WIDE_SELF * ((int)sizeof(Segment) + 4) + 1024;
     static constexpr int TM_S = 0;         // TMEM columns: S (128), P0, P1 (64 each), O0, O1 (D each)
     static constexpr int TM_P = 128;
@@ -159,14 +162,15 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
     uint64_t* s_full = q_full + 2;       // [2]
     uint64_t* p_full = q_full + 4;       // [2]
     uint64_t* pv_done = q_full + 6;      // [2]
-    uint64_t* u_full = q_full + 8;       // [2]
-    uint64_t* u_empty = q_full + 10;     // [2]
-    uint64_t* s_empty = q_full + 12;
-    uint64_t* o_empty = q_full + 13;
-    uint64_t* e_full = q_full + 14;
-    uint64_t* drain_bar = q_full + 15;
-    constexpr int BARS = 4 * STAGES + 16;
-    WideUnit* units = reinterpret_cast<WideUnit*>(reinterpret_cast<uint8_t*>(bars) + C::BAR_BYTES);   // [2]
+    uint64_t* u_full = q_full + 8;       // [AW_UNITS]
+    uint64_t* u_empty = q_full + 12;     // [AW_UNITS]
+    uint64_t* s_empty = q_full + 16;
+    uint64_t* o_empty = q_full + 17;
+    uint64_t* e_full = q_full + 18;
+    uint64_t* drain_bar = q_full + 19;
+    constexpr int BARS = 4 * STAGES + 20;
+    WideUnit* units = reinterpret_cast<WideUnit*>(reinterpret_cast<uint8_t*>(bars) + C::BAR_BYTES);   // [AW_UNITS]
+    static_assert(sizeof(WideUnit) == 80 && AW_UNITS == 4, "layout of shared memory");
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + BARS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     static_assert(BARS * 8 + 8 <= C::BAR_BYTES, "barriers");
@@ -176,7 +180,7 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
     if (threadIdx.x == 0) {
         for (int i = 0; i < BARS; ++i) {
             const int b = i - 4 * STAGES;      // all barriers take one arrival but these
-            mbar_init(&bars[i], b == 4 || b == 5 || b == 12 ? NSW / 2 : b == 10 || b == 11 ? NSW + 3 : b == 13 || b == 14 ? NSW : b == 15 ? 2 : 1);
+            mbar_init(&bars[i], b == 4 || b == 5 || b == 16 ? NSW / 2 : b >= 12 && b < 16 ? NSW + 3 : b == 17 || b == 18 ? NSW : b == 19 ? 2 : 1);
         }
         *abort_flag = 0;
         fence_barrier_init();
@@ -236,22 +240,71 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
 
     if (warp >= NSW) {
         regs_dec<AW_REGS_OTHER>();
+        // The unit's tiles of K (from = to = 0), of V (1, 1) or of both (0, 1: K one tile ahead of V, as a K slot is free again long before the V slot of the
+        // same tile), page by page, one box to a lane; `count`: loads of K and of V so far, tile n in slot n % STAGES, phase n / STAGES.  A page number is on its
+        // way while the tile before waits for its slot.
+        const int bt = min(1 << a.page_shift, AT_WIDE_KEYS);     // tokens of a box
+        const int boxes = AT_WIDE_KEYS / bt * C::HALVES;         // of a tile: at most 16, one lane each
+        const bool two_warps = bt < 64;
+        auto load_tiles = [&](const WideUnit& w, int from, int to, uint32_t (&count)[2], auto behind_first) -> bool {
+            const int mine = lane / C::HALVES, half = lane % C::HALVES, ka = w.ka, n = w.n, nf = w.nf, h = w.h, lag = to - from;
+            const int32_t* own_pages = seg_pages(a, w.seg);
+            const int32_t* front_pages = nf ? seg_pages(a, w.front) : own_pages;
+            auto look_up = [&](int kt, int& page, int& place) {
+                page = a.n_pages;          // a box past the last page is filled with zeros
+                place = 0;
+                if (lane < boxes && mine * bt < unit_left(w, kt)) {              // a length is within the list's columns
+                    const int key = (kt < nf ? kt : kt - nf) * AT_WIDE_KEYS + mine * bt;
+                    const int p = (kt < nf ? front_pages : own_pages)[key >> a.page_shift];
+                    if (p >= 0 && p < a.n_pages) page = p;
+                    place = key & ((1 << a.page_shift) - 1);
+                }
+            };
+            int next_page, next_place, page = 0, place = 0;
+            look_up(ka, next_page, next_place);
+            for (int i = 0; i < n + lag; ++i) {
+                const int last_page = page, last_place = place;
+                page = next_page;
+                place = next_place;
+                if (i + 1 < n) look_up(ka + i + 1, next_page, next_place);
+#pragma unroll 1
+                for (int v = from; v <= to; ++v) {
+                    const bool behind = v && lag;
+                    if (behind ? i == 0 : i == n) continue;
+                    const uint32_t t = count[v], st = v * STAGES + t % STAGES;
+                    if (!wait_bounded(&empty[st], (t / STAGES + 1) & 1u, abort_flag, 62)) return false;
+                    if (lane == 0) mbar_arrive_expect_tx(&full[st], C::TILE_BYTES);
+                    __syncwarp();
+                    if (lane < boxes)
+                        tma_load_4d(ring0 + st * C::TILE_BYTES + half * C::HALF_BYTES + mine * bt * 128, v ? &args.tm_v : &args.tm_k, &full[st], half * 64,
+                                    behind ? last_place : place, h, behind ? last_page : page);
+                    ++count[v];
+                }
+                if (i == 0 && !behind_first()) return false;
+            }
+            return true;
+        };
+        auto drain_tiles = [&](int v, uint32_t count) {
+            int dummy = 0;
+            volatile int* never = &dummy;
+            for (uint32_t i = count > STAGES ? count - STAGES : 0; i < count; ++i) wait_bounded(&full[v * STAGES + i % STAGES], (i / STAGES) & 1u, never, 63);
+        };
         if (warp == NSW + 2) {
             // ------------------------------------------------------------------------------------- units
             auto walk = [&](auto& cur, const auto& src, int N, int q) {
                 const int x0 = (int)min((int64_t)q * blockIdx.x, (int64_t)N), x1 = (int)min((int64_t)x0 + q, (int64_t)N);
                 if (lane == 0) a.plan.cut[1][blockIdx.x].tiles = 0;
-                int b = 0, x = x0;           // (last) place of the tile to come
-                uint32_t ph = 0;
-                bool first = true;
+                int x = x0;                  // (last) place of the tile to come
+                uint32_t made = 0, count[2] = {0, 0};        // units so far; loads of V so far
+                bool first = true, more = true;
                 if (x0 < x1) {
                     cur.seek(a, src, S, x0);
                     if (cur.kt < 0) cur.kt = 0;      // in front of the unit's tiles
                     x = unit_begin<WideUnits>(a, cur.g, cur.h, cur.u) + cur.kt * WideUnits::weight(a, cur.g, cur.u);
                 }
-                while (true) {
+                auto make = [&]() -> bool {
                     WideUnit w = {};
-                    const int weight = x < x1 ? WideUnits::weight(a, cur.g, cur.u) : 1, begin = x - cur.kt * weight;
+                    const int b = made % AW_UNITS, weight = x < x1 ? WideUnits::weight(a, cur.g, cur.u) : 1, begin = x - cur.kt * weight;
                     if (x < x1) {
                         w.ka = cur.kt;
                         w.n = min(cur.nt - cur.kt, (x1 - x + weight - 1) / weight);
@@ -279,13 +332,15 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                                 (!first || (cur.kt == 0 && begin > x0) ? OUT_LATER : 0);
                         first = false;
                     }
-                    if (!wait_bounded(&u_empty[b], ph ^ 1u, abort_flag, 76)) break;
+                    if (!wait_bounded(&u_empty[b], (made / AW_UNITS + 1) & 1u, abort_flag, 76)) return false;
                     if (lane == 0) {
                         units[b] = w;
                         mbar_arrive(&u_full[b]);
                     }
-                    if (++b == 2) { b = 0; ph ^= 1u; }
-                    if (w.n == 0) break;
+                    __syncwarp();
+                    ++made;
+                    more = w.n != 0;
+                    if (!more) return true;
                     x += w.n * weight;
                     if (x >= x1 && lane == 0) tell_cut(a.plan.cut[1] + blockIdx.x, begin, cur.nt, weight, x0, x1, q, cur.h, cur.u, cur.g);
                     if (x < x1) {
@@ -293,7 +348,15 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                         cur.next_unit(a, src, SEG_WIDE);
                         x += (WideUnits::LEAD + 1) * WideUnits::weight(a, cur.g, cur.u) - weight;
                     }
+                    return true;
+                };
+                bool fine = make();
+                for (uint32_t k = 0; fine && units[k % AW_UNITS].n; ++k) {
+                    fine = make() && (!two_warps || load_tiles(units[k % AW_UNITS], 1, 1, count, []() { return true; }));
+                    if (!more && k + 2 == made) break;       // that was the last one in front of the end
                 }
+                __syncwarp();
+                if (*abort_flag) drain_tiles(1, count[1]);
             };
             if (TREE && a.self) {
                 Cursor<WideUnits, true> cur;
@@ -304,72 +367,35 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
             }
         } else if (warp == NSW) {
             // --------------------------------------------------------------------------------------- TMA
-            const int bt = min(1 << a.page_shift, AT_WIDE_KEYS);     // tokens of a box
-            const int boxes = AT_WIDE_KEYS / bt * C::HALVES;         // of a K or V tile: at most 16, one lane each
-            const int mine = lane / C::HALVES, half = lane % C::HALVES;
-            uint32_t n_k = 0, n_v = 0;      // K and V loads so far: tile n in slot n % STAGES, phase n / STAGES
+            uint32_t count[2] = {0, 0};
             int b = 0;
             uint32_t q_ph = 0, u_ph = 0;
             while (true) {
-                if (!wait_bounded(&u_full[b], u_ph, abort_flag, 60)) goto stop_loads;
+                if (!wait_bounded(&u_full[b], u_ph, abort_flag, 60)) break;
                 const WideUnit& w = units[b];
-                const int ka = w.ka, n = w.n, nf = w.nf, h = w.h;
-                if (n == 0) break;
-                const int32_t* own_pages = seg_pages(a, w.seg);
-                const int32_t* front_pages = nf ? seg_pages(a, w.front) : own_pages;
-                int page = 0, place = 0;
-                // K one tile ahead of V: a K slot is free again long before the V slot of the same tile
-                for (int i = 0; i <= n; ++i) {
-                    const int v_page = page, v_place = place;
-                    if (i < n) {
-                        const int kt = ka + i;
-                        page = a.n_pages;      // a box past the last page is filled with zeros
-                        place = 0;
-                        if (lane < boxes) {
-                            const int key = (kt < nf ? kt : kt - nf) * AT_WIDE_KEYS + mine * bt;
-                            if (mine * bt < unit_left(w, kt)) {          // a length is within the list's columns
-                                const int p = (kt < nf ? front_pages : own_pages)[key >> a.page_shift];
-                                if (p >= 0 && p < a.n_pages) page = p;
-                                place = key & ((1 << a.page_shift) - 1);
-                            }
-                        }
-                    }
-#pragma unroll 1
-                    for (int v = 0; v < 2; ++v) {
-                        if (v ? i == 0 : i == n) continue;
-                        const uint32_t t = v ? n_v : n_k, st = v * STAGES + t % STAGES;
-                        if (!wait_bounded(&empty[st], (t / STAGES + 1) & 1u, abort_flag, 62)) goto stop_loads;
-                        if (lane == 0) mbar_arrive_expect_tx(&full[st], C::TILE_BYTES);
-                        __syncwarp();
-                        if (lane < boxes)
-                            tma_load_4d(ring0 + st * C::TILE_BYTES + half * C::HALF_BYTES + mine * bt * 128, v ? &args.tm_v : &args.tm_k, &full[st],
-                                        half * 64, v ? v_place : place, h, v ? v_page : page);
-                        if (v) ++n_v; else ++n_k;
-                    }
-                    if (i == 0) {      // behind the first K: Q, whose place is free when the unit before has no more S to come
-                        if (!wait_bounded(q_empty, q_ph ^ 1u, abort_flag, 61)) goto stop_loads;
+                if (w.n == 0) break;
+                if (!load_tiles(w, 0, two_warps ? 0 : 1, count, [&]() -> bool {      // behind the first K: Q, whose place is free when the unit before has no more S to come
+                        if (!wait_bounded(q_empty, q_ph ^ 1u, abort_flag, 61)) return false;
                         q_ph ^= 1u;
                         const int tiles = w.pair ? 2 : 1;
                         if (lane == 0) mbar_arrive_expect_tx(q_full, (uint32_t)(tiles * C::HALVES * tpt * a.G * 128));
                         __syncwarp();
                         if (lane < tiles * C::HALVES)
-                            tma_load_3d(smem_u32(smem + mine * C::QTILE_BYTES + half * C::QHALF_BYTES), &args.tm_q, q_full, half * 64, h * a.G,
-                                        w.row0 + mine * tpt);
-                    }
-                }
+                            tma_load_3d(smem_u32(smem + (lane / C::HALVES) * C::QTILE_BYTES + (lane % C::HALVES) * C::QHALF_BYTES), &args.tm_q, q_full,
+                                        lane % C::HALVES * 64, w.h * a.G, w.row0 + lane / C::HALVES * tpt);
+                        return true;
+                    }))
+                    break;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&u_empty[b]);
-                if (++b == 2) { b = 0; u_ph ^= 1u; }
+                if (++b == AW_UNITS) { b = 0; u_ph ^= 1u; }
             }
-        stop_loads:
             __syncwarp();
             if (*abort_flag) {      // gave up somewhere: the copies under way land before the CTA's memory goes away
+                drain_tiles(0, count[0]);
+                drain_tiles(1, count[1]);
                 int dummy = 0;
                 volatile int* never = &dummy;
-                for (int v = 0; v < 2; ++v) {
-                    const uint32_t t = v ? n_v : n_k;
-                    for (uint32_t i = t > STAGES ? t - STAGES : 0; i < t; ++i) wait_bounded(&full[v * STAGES + i % STAGES], (i / STAGES) & 1u, never, 63);
-                }
                 wait_bounded(q_full, q_ph ^ 1u, never, 64);
             }
         } else {
@@ -484,7 +510,7 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                 }
                 base += n;
                 if (lane == 0) mbar_arrive(&u_empty[b]);
-                if (++b == 2) { b = 0; u_ph ^= 1u; }
+                if (++b == AW_UNITS) { b = 0; u_ph ^= 1u; }
             }
         }
     } else {
@@ -765,7 +791,7 @@ __global__ void __launch_bounds__(AW_THREADS, 1) attn_wide_kernel(const __grid_c
                 mbar_arrive(o_empty);
                 mbar_arrive(&u_empty[b]);
             }
-            if (++b == 2) { b = 0; u_ph ^= 1u; }
+            if (++b == AW_UNITS) { b = 0; u_ph ^= 1u; }
         }
     }
 
