@@ -9,13 +9,13 @@
 // consecutive parts and are joined through distributed shared memory, so there is one launch and no workspace.  Every thread copies its own
 // vectors into a ring in shared memory (cp.async), two chunks ahead; nobody else reads them, so the ring needs no barrier.
 //
-// Alternatives: the order is value, then lower index, as one key: the value's bits made monotone (NaN below -inf) and the index.  A thread's
-// largest value of a chunk is known from the maximum above.  First chunk: the k-th of the warps' four largest such values bounds the k-th best
-// value of the row from below, and few other values pass it, so the values at or above it go to a list in shared memory.  Later chunks: only values above the bound, without a barrier; the list is joined with the k best so far,
-// which raises the bound, behind chunks 1, 2, 4, 8, ... and the last: some k candidates each time.  Where a thread has some, its warp looks at its values
-// of the chunk in shared memory, one lane each.  (By the thread itself, in registers one by one, that cost more than the sums: 600 us for 3001 rows of
-// 152064; in shared memory 394.)  Where too many values pass (equal logits, rows in rising order) the chunks since the last rank are read again, each with a bound of its
-// own, and where that does not help (ties) its best are taken one by one, k rounds of a maximum over the block.
+// Alternatives: the order is value, then lower index, as one key: the value's bits made monotone (NaN below -inf) and the index.  The loop over the
+// chunks keeps nothing but the largest key of every warp's part of a chunk (1024 values).  Behind it, the k-th largest of those bounds the k-th best value
+// of the row from below, so the best are in the parts that reach it, about k of them: these are read again (from L2 mostly) and their values at or
+// above the bound, a few more than k, are ranked.  No barrier runs in the loop, and it takes 10 instructions a part.  (Candidates picked out of every chunk as
+// it passed, with a bound that rose, took 60 more: 240 us for 3001 rows of 152064 bf16 logits.)  Where too many values reach the bound (equal logits), or too
+// few parts have any (short rows, masks), the chunks are read again in order, each with a bound of its own; chunks whose largest value is not above the k-th
+// so far are passed over, and where ties alone fill the list a chunk's best are taken one by one, k rounds of a maximum over the block.
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -29,8 +29,9 @@ constexpr int LP_VECS = 4;               // 16-byte vectors of a chunk, per thre
 static_assert(LP_VECS * 8 <= 32, "a lane for every value of a thread");
 constexpr int LP_STAGES = 3;             // chunks in the ring
 constexpr int LP_SHORT_BYTES = 16384;    // rows up to here
+constexpr int LP_GROUPS = 32;            // groups of chunks of a block
 constexpr int LP_MAX_TOP = 32;
-constexpr int LP_LIST = 512;            // candidates that wait to be ranked
+constexpr int LP_LIST = 448;            // candidates that wait to be ranked
 constexpr int LP_MAX_CLUSTER = 8;
 
 struct LogprobArgs {
@@ -91,7 +92,9 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
     __shared__ float s_red[3][WARPS];
     __shared__ unsigned long long s_in[TOP ? LP_MAX_CLUSTER * LP_MAX_TOP : 1];     // the k best of the cluster's other blocks, in the one of rank 0
     __shared__ float s_part[LP_MAX_CLUSTER][3];      // (max, l, S) of the cluster's blocks, likewise
-    __shared__ __align__(16) uint32_t s_largest[32];
+    __shared__ uint32_t s_most[TOP ? LP_GROUPS * WARPS : 1];              // largest key above -inf of every warp's part of a chunk (of a group of chunks)
+    __shared__ uint16_t s_part_of[TOP ? LP_GROUPS * WARPS : 1];           // the parts that reach the bound
+    __shared__ int s_parts;
     __shared__ int s_n, s_over;                      // candidates; whether some found no place
     grid_launch_dependents();
     if (cluster > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");      // every block is there before anyone writes to rank 0
@@ -101,7 +104,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
     const float scale2 = a.scale * 1.44269504088896341f;
     const int k = TOP ? a.k : 0;
     if (TOP) {
-        if (tid == 0) s_n = s_over = 0;
+        if (tid == 0) s_n = s_over = s_parts = 0;
         if (tid < 2 * LP_MAX_TOP) s_kept[tid / LP_MAX_TOP][tid % LP_MAX_TOP] = 0;
     }
     grid_dependency_wait();
@@ -129,12 +132,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
 
     float m = -INFINITY, l = 0.0f, S = 0.0f;
     uint32_t bound = 0;          // values with a key above it are candidates
-    float value = 0.0f;          // the value it stands for, from -inf on
     int which = 0;
-    auto set_bound = [&](uint32_t b) {
-        bound = b;
-        value = b == 0x7FFFFFFFu ? __uint_as_float(0x80000001u) : lp_value(max(b, LP_KEY_LOW));      // (no value has that key: -0 counts as 0)
-    };
     if (TOP) __syncthreads();
 
     // Joins the candidates with the k best; `bound` becomes the last one's key.  All threads have passed a barrier since the last candidate came.
@@ -157,7 +155,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
         }
         __syncthreads();
         which ^= 1;
-        set_bound((uint32_t)(s_kept[which][k - 1] >> 32));
+        bound = (uint32_t)(s_kept[which][k - 1] >> 32);
         if (tid < k) s_kept[which ^ 1][tid] = 0;
         if (tid == 0) s_n = s_over = 0;
         __syncthreads();
@@ -177,53 +175,28 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
             for (int e = 0; e < E; ++e) f(lp_key(Vec::get(x, e)), j + e);
         }
     };
-    // A key that at least k of the threads' largest values reach, or 0: the k-th of the largest few of every warp that has some, 2^n warps and 32 values at
-    // the most.
-    auto reached = [&](uint32_t best, int base) -> uint32_t {
-        const int active = min(WARPS, (v1 - base + 31) / 32), warps = 1 << (31 - __clz(active)), each_has = min(32 / warps, 2 * ((k + warps - 1) / warps));
-        if (warp < warps) {
-            uint32_t keep = 0;
-#pragma unroll 1
-            for (int i = 0; i < each_has; ++i) {         // of equal ones the first lane's
-                const uint32_t t = __reduce_max_sync(0xFFFFFFFFu, best);
-                if (lane == i) keep = t;
-                if (lane == __ffs((int)__ballot_sync(0xFFFFFFFFu, best == t)) - 1) best = 0;
-            }
-            if (lane < each_has) s_largest[warp * each_has + lane] = keep;
-        }
-        __syncthreads();
-        const int have = warps * each_has;
-        const uint32_t mine = lane < have ? s_largest[lane] : 0;
-        int better = 0;
-#pragma unroll
-        for (int j = 0; j < 32; j += 4) {
-            const uint4 x = *reinterpret_cast<const uint4*>(s_largest + j);      // (broadcasts: 32 shuffles a warp took 1000 cycles with four blocks on the SM)
-            better += j < have && (x.x > mine || (x.x == mine && j < lane));
-            better += j + 1 < have && (x.y > mine || (x.y == mine && j + 1 < lane));
-            better += j + 2 < have && (x.z > mine || (x.z == mine && j + 2 < lane));
-            better += j + 3 < have && (x.w > mine || (x.w == mine && j + 3 < lane));
-        }
-        const uint32_t at = __ballot_sync(0xFFFFFFFFu, lane < have && better == k - 1);
-        return at ? __shfl_sync(0xFFFFFFFFu, mine, __ffs((int)at) - 1) : 0;
-    };
-    // a chunk with many values above the bound, read once more
-    auto again = [&](int base) {
-        const uint4* at = xv + base + tid;
-        uint32_t best = 0;
-        each(at, base, [&](uint32_t key, int) { best = max(best, key); });
-        // the largest 16-bit prefix of a key that k threads' largest values reach
+    // the largest 16-bit prefix of a key that k threads' largest ones reach; 0: fewer have any
+    auto reached = [&](uint32_t best) -> uint32_t {
         uint32_t t = 0;
 #pragma unroll 1
         for (int bit = 15; bit >= 0; --bit)
             if (__syncthreads_count(best >> 16 >= (t | 1u << bit)) >= k) t |= 1u << bit;
-        if (t) set_bound(max(bound, (t << 16) - 1));
+        return t << 16;
+    };
+    // the values of a chunk above the bound, joined with the k best
+    auto again = [&](int base) {
+        const uint4* at = xv + base + tid;
+        uint32_t best = 0;
+        each(at, base, [&](uint32_t key, int) { best = max(best, key); });
+        const uint32_t t = reached(best);
+        if (t) bound = max(bound, t - 1);
         each(at, base, [&](uint32_t key, int j) { if (key > bound) add(key, j); });
         __syncthreads();
         if (!s_over) return rank_list(s_list, s_n);
         __syncthreads();
         if (tid == 0) s_n = 0;
         __syncthreads();
-        set_bound((uint32_t)(s_kept[which][k - 1] >> 32));
+        bound = (uint32_t)(s_kept[which][k - 1] >> 32);
         unsigned long long last = ~0ull;
 #pragma unroll 1
         for (int i = 0; i < k; ++i) {
@@ -256,14 +229,12 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
             m = x != x ? -INFINITY : x;
             l = lp_exp2((x - x) * scale2);           // 1, or NaN
         }
-        if (TOP) add(lp_key(x), edge);
-    }
-    if (TOP && v0 >= v1) {
-        __syncthreads();
-        rank_list(s_list, s_n);
     }
 
-    int stage = 0, chunk = 0, since = v0;        // since: first vector of the chunks that are not ranked
+    int stage = 0, chunk = 0;
+    const int chunks = (v1 - v0 + CHUNK - 1) / CHUNK;
+    int shift = 0;               // of chunks to the groups that s_most keeps apart
+    while (chunks >> shift >= LP_GROUPS) ++shift;
 #pragma unroll 1
     for (int base = v0; base < v1; base += CHUNK, ++chunk) {
         // into the stage of the chunk before, whose vectors are done with
@@ -339,52 +310,72 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
             l += l0 + l1;
             S += sum;
         }
-        // ---- candidates
         if (TOP) {
-            if (chunk == 0) {
-                uint32_t best = lp_key(top);
-                if (top == -INFINITY) {              // a NaN is a value too
-                    best = 0;
-                    each(at, base, [&](uint32_t key, int) { best = max(best, key); });
-                }
-                const uint32_t t = reached(best, base);
-                set_bound(t ? t - 1 : 0);            // values at t are candidates themselves
-            }
-            __syncwarp();                            // the lanes' copies, for one another
-            uint32_t lanes = __ballot_sync(0xFFFFFFFFu, bound < LP_KEY_LOW ? base + tid < v1 : top > value);
-#pragma unroll 1
-            for (; lanes; lanes &= lanes - 1) {
-                const int of = tid - lane + __ffs((int)lanes) - 1, u = lane / E, e = lane % E, i = base + u * NT + of;
-                uint32_t key = 0;
-                if (lane < U * E && i < v1) key = lp_key(Vec::value(reinterpret_cast<const Elem*>(at - tid + u * NT + of)[e]));
-                const uint32_t found = __ballot_sync(0xFFFFFFFFu, key > bound);
-                if (found == 0) continue;
-                int n = 0;
-                if (lane == 0) n = atomicAdd(&s_n, __popc(found));
-                n = __shfl_sync(0xFFFFFFFFu, n, 0) + __popc(found & ((1u << lane) - 1u));
-                if (key > bound) {
-                    if (n < LP_LIST) s_list[n] = lp_rank(key, i * E + e - lead);
-                    else s_over = 1;
-                }
-            }
-            if ((chunk & (chunk + 1)) == 0 || base + CHUNK >= v1) {
-                __syncthreads();
-                if (!s_over) {
-                    rank_list(s_list, s_n);
-                } else {
-                    __syncthreads();
-                    if (tid == 0) s_n = s_over = 0;
-                    set_bound((uint32_t)(s_kept[which][k - 1] >> 32));
-                    __syncthreads();
-                    if (since == v0 && edge >= 0) add(lp_key(Vec::value(xr[edge])), edge);
-#pragma unroll 1
-                    for (int b = since; b < min(base + CHUNK, v1); b += CHUNK) again(b);
-                }
-                since = base + CHUNK;
+            const uint32_t most = __reduce_max_sync(0xFFFFFFFFu, top > -INFINITY ? lp_key(top) : 0u);
+            if (lane == 0) {
+                uint32_t* to = &s_most[(chunk >> shift) * WARPS + warp];
+                *to = chunk & ((1 << shift) - 1) ? max(*to, most) : most;
             }
         }
     }
     cp_async_wait<0>();
+
+    // ---- the k best of the block's part
+    if (TOP) {
+        const int parts = chunks > 0 ? ((chunks - 1 >> shift) + 1) * WARPS : 0;
+        __syncthreads();
+        uint32_t best = 0;
+        for (int i = tid; i < parts; i += NT) best = max(best, s_most[i]);
+        const uint32_t t = reached(best);
+        bool done = false;
+        if (t) {
+            for (int i = tid; i < parts; i += NT)
+                if (s_most[i] >= t) s_part_of[atomicAdd(&s_parts, 1)] = (uint16_t)i;
+            __syncthreads();
+            const int n = s_parts;
+#pragma unroll 1
+            for (int i = warp; i < n; i += WARPS) {
+                const int part = s_part_of[i], c0 = part / WARPS << shift, first = v0 + part % WARPS * 32 + lane;
+#pragma unroll 1
+                for (int c = c0; c < min(c0 + (1 << shift), chunks); ++c) {
+                    const int at = first + c * CHUNK;
+                    uint4 x[U];
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        x[u].x = x[u].y = x[u].z = x[u].w = F32 ? 0xFF800000u : 0xFF80FF80u;
+                        if (at + u * NT < v1) x[u] = xv[at + u * NT];
+                    }
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+#pragma unroll
+                        for (int e = 0; e < E; ++e) {
+                            const uint32_t key = lp_key(Vec::get(x[u], e));
+                            if (key >= t) add(key, (at + u * NT) * E + e - lead);      // (t is above the -inf of what is not there)
+                        }
+                }
+            }
+            if (edge >= 0) add(lp_key(Vec::value(xr[edge])), edge);
+            __syncthreads();
+            done = !s_over;
+            if (done) rank_list(s_list, s_n);
+        }
+        if (!done) {
+            __syncthreads();
+            if (tid == 0) s_n = s_over = 0;
+            __syncthreads();
+#pragma unroll 1
+            for (int c = 0; c < chunks; ++c) {
+                uint32_t most = 0;
+                for (int w = 0; w < WARPS; ++w) most = max(most, s_most[(c >> shift) * WARPS + w]);
+                if (bound < LP_KEY_LOW || most > bound) again(v0 + c * CHUNK);
+            }
+            if (head > 0 || tail < a.V) {
+                if (edge >= 0) add(lp_key(Vec::value(xr[edge])), edge);
+                __syncthreads();
+                rank_list(s_list, s_n);
+            }
+        }
+    }
 
     // ---- the block's (max, l, S)
     {
