@@ -10,7 +10,7 @@
 // vectors into a ring in shared memory (cp.async), two chunks ahead; nobody else reads them, so the ring needs no barrier.
 //
 // Alternatives: the order is value, then lower index, as one key: the value's bits made monotone (NaN below -inf) and the index.  The loop over the
-// chunks keeps nothing but the largest key of every warp's part of a chunk (1024 values).  Behind it, the k-th largest of those bounds the k-th best value
+// chunks keeps nothing but the largest key of every warp's part of a chunk (1024 values), in short rows of every thread's (32).  Behind it, the k-th largest of those bounds the k-th best value
 // of the row from below, so the best are in the parts that reach it, about k of them: these are read again (from L2 mostly) and their values at or
 // above the bound, a few more than k, are ranked.  No barrier runs in the loop, and it takes 10 instructions a part.  (Candidates picked out of every chunk as
 // it passed, with a bound that rose, took 60 more: 240 us for 3001 rows of 152064 bf16 logits.)  Where too many values reach the bound (equal logits), or too
@@ -29,9 +29,9 @@ constexpr int LP_VECS = 4;               // 16-byte vectors of a chunk, per thre
 static_assert(LP_VECS * 8 <= 32, "a lane for every value of a thread");
 constexpr int LP_STAGES = 3;             // chunks in the ring
 constexpr int LP_SHORT_BYTES = 16384;    // rows up to here
-constexpr int LP_GROUPS = 32;            // groups of chunks of a block
+constexpr int LP_PARTS = 1024;           // parts of a block's row
 constexpr int LP_MAX_TOP = 32;
-constexpr int LP_LIST = 448;            // candidates that wait to be ranked
+constexpr int LP_LIST = 512;            // candidates that wait to be ranked
 constexpr int LP_MAX_CLUSTER = 8;
 
 struct LogprobArgs {
@@ -86,14 +86,15 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
     using Elem = typename Vec::Elem;
     constexpr int E = Vec::E, U = LP_VECS, CHUNK = NT * U, WARPS = NT / 32;
     extern __shared__ __align__(16) uint8_t lp_ring[];       // [LP_STAGES][CHUNK] vectors
-    __shared__ unsigned long long s_list[TOP ? LP_LIST : 1];             // candidates since the last rank
     __shared__ unsigned long long s_kept[2][TOP ? LP_MAX_TOP : 1];       // the k best, in order (0: none); the one of two that `which` says
     __shared__ unsigned long long s_warp[WARPS];
     __shared__ float s_red[3][WARPS];
     __shared__ unsigned long long s_in[TOP ? LP_MAX_CLUSTER * LP_MAX_TOP : 1];     // the k best of the cluster's other blocks, in the one of rank 0
     __shared__ float s_part[LP_MAX_CLUSTER][3];      // (max, l, S) of the cluster's blocks, likewise
-    __shared__ uint32_t s_most[TOP ? LP_GROUPS * WARPS : 1];              // largest key above -inf of every warp's part of a chunk (of a group of chunks)
-    __shared__ uint16_t s_part_of[TOP ? LP_GROUPS * WARPS : 1];           // the parts that reach the bound
+    __shared__ uint32_t s_most[TOP ? LP_PARTS : 1];                       // largest key above -inf of every part
+    // behind the loop the ring holds
+    unsigned long long* s_list = reinterpret_cast<unsigned long long*>(lp_ring);       // candidates
+    uint16_t* s_part_of = reinterpret_cast<uint16_t*>(s_list + LP_LIST);               // [LP_PARTS] the parts that reach the bound
     __shared__ int s_parts;
     __shared__ int s_n, s_over;                      // candidates; whether some found no place
     grid_launch_dependents();
@@ -233,8 +234,9 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
 
     int stage = 0, chunk = 0;
     const int chunks = (v1 - v0 + CHUNK - 1) / CHUNK;
-    int shift = 0;               // of chunks to the groups that s_most keeps apart
-    while (chunks >> shift >= LP_GROUPS) ++shift;
+    int shift = 0;               // of chunks to the groups of them whose parts are one
+    while (chunks >> shift >= LP_PARTS / WARPS) ++shift;
+    const bool fine = chunks * NT <= LP_PARTS;       // a part is a thread's
 #pragma unroll 1
     for (int base = v0; base < v1; base += CHUNK, ++chunk) {
         // into the stage of the chunk before, whose vectors are done with
@@ -311,10 +313,15 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
             S += sum;
         }
         if (TOP) {
-            const uint32_t most = __reduce_max_sync(0xFFFFFFFFu, top > -INFINITY ? lp_key(top) : 0u);
-            if (lane == 0) {
-                uint32_t* to = &s_most[(chunk >> shift) * WARPS + warp];
-                *to = chunk & ((1 << shift) - 1) ? max(*to, most) : most;
+            const uint32_t key = top > -INFINITY ? lp_key(top) : 0u;
+            if (fine) {
+                s_most[chunk * NT + tid] = key;
+            } else {
+                const uint32_t most = __reduce_max_sync(0xFFFFFFFFu, key);
+                if (lane == 0) {
+                    uint32_t* to = &s_most[(chunk >> shift) * WARPS + warp];
+                    *to = chunk & ((1 << shift) - 1) ? max(*to, most) : most;
+                }
             }
         }
     }
@@ -322,7 +329,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
 
     // ---- the k best of the block's part
     if (TOP) {
-        const int parts = chunks > 0 ? ((chunks - 1 >> shift) + 1) * WARPS : 0;
+        const int parts = fine ? chunks * NT : (((chunks - 1) >> shift) + 1) * WARPS;
         __syncthreads();
         uint32_t best = 0;
         for (int i = tid; i < parts; i += NT) best = max(best, s_most[i]);
@@ -333,8 +340,26 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
                 if (s_most[i] >= t) s_part_of[atomicAdd(&s_parts, 1)] = (uint16_t)i;
             __syncthreads();
             const int n = s_parts;
+            constexpr int FLIGHT = 4;        // parts whose values are on their way
 #pragma unroll 1
-            for (int i = warp; i < n; i += WARPS) {
+            for (int i0 = warp; fine && i0 < n; i0 += FLIGHT * WARPS) {       // a lane for every value
+                Elem x[FLIGHT];
+                int j[FLIGHT];
+#pragma unroll
+                for (int f = 0; f < FLIGHT; ++f) {
+                    const int i = i0 + f * WARPS, part = s_part_of[min(i, n - 1)], u = lane / E;
+                    const int at = v0 + part / NT * CHUNK + u * NT + part % NT;
+                    j[f] = i < n && u < U && at < v1 ? at * E + lane % E - lead : -1;
+                    x[f] = j[f] >= 0 ? xr[j[f]] : Elem(0);
+                }
+#pragma unroll
+                for (int f = 0; f < FLIGHT; ++f) {
+                    const uint32_t key = lp_key(Vec::value(x[f]));
+                    if (j[f] >= 0 && key >= t) add(key, j[f]);
+                }
+            }
+#pragma unroll 1
+            for (int i = warp; !fine && i < n; i += WARPS) {
                 const int part = s_part_of[i], c0 = part / WARPS << shift, first = v0 + part % WARPS * 32 + lane;
 #pragma unroll 1
                 for (int c = c0; c < min(c0 + (1 << shift), chunks); ++c) {
@@ -366,7 +391,12 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
 #pragma unroll 1
             for (int c = 0; c < chunks; ++c) {
                 uint32_t most = 0;
-                for (int w = 0; w < WARPS; ++w) most = max(most, s_most[(c >> shift) * WARPS + w]);
+                if (fine) {
+                    const uint32_t key = s_most[c * NT + tid];
+                    most = __syncthreads_or(key > bound) ? 0xFFFFFFFFu : 0u;
+                } else {
+                    for (int w = 0; w < WARPS; ++w) most = max(most, s_most[(c >> shift) * WARPS + w]);
+                }
                 if (bound < LP_KEY_LOW || most > bound) again(v0 + c * CHUNK);
             }
             if (head > 0 || tail < a.V) {
