@@ -10,9 +10,9 @@
 // vectors into a ring in shared memory (cp.async), two chunks ahead; nobody else reads them, so the ring needs no barrier.
 //
 // Alternatives: the order is value, then lower index, as one key: the value's bits made monotone (NaN below -inf) and the index.  The loop over the
-// chunks keeps nothing but the largest key of every warp's part of a chunk (1024 values), in short rows of every thread's (32).  Behind it, the k-th largest of those bounds the k-th best value
+// chunks keeps nothing but the largest key of every eight threads' part of a chunk (256 values), in short rows of every thread's (32).  Behind it, the k-th largest of those bounds the k-th best value
 // of the row from below, so the best are in the parts that reach it, about k of them: these are read again (from L2 mostly) and their values at or
-// above the bound, a few more than k, are ranked.  No barrier runs in the loop, and it takes 10 instructions a part.  (Candidates picked out of every chunk as
+// above the bound, a few more than k, are ranked.  No barrier runs in the loop, and the maxima take 15 instructions of a warp and chunk.  (Candidates picked out of every chunk as
 // it passed, with a bound that rose, took 60 more: 240 us for 3001 rows of 152064 bf16 logits.)  Where too many values reach the bound (equal logits), or too
 // few parts have any (short rows, masks), the chunks are read again in order, each with a bound of its own; chunks whose largest value is not above the k-th
 // so far are passed over, and where ties alone fill the list a chunk's best are taken one by one, k rounds of a maximum over the block.
@@ -235,7 +235,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
     int stage = 0, chunk = 0;
     const int chunks = (v1 - v0 + CHUNK - 1) / CHUNK;
     int shift = 0;               // of chunks to the groups of them whose parts are one
-    while (chunks >> shift >= LP_PARTS / WARPS) ++shift;
+    while (chunks >> shift >= LP_PARTS / (NT / 8)) ++shift;
     const bool fine = chunks * NT <= LP_PARTS;       // a part is a thread's
 #pragma unroll 1
     for (int base = v0; base < v1; base += CHUNK, ++chunk) {
@@ -317,9 +317,11 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
             if (fine) {
                 s_most[chunk * NT + tid] = key;
             } else {
-                const uint32_t most = __reduce_max_sync(0xFFFFFFFFu, key);
-                if (lane == 0) {
-                    uint32_t* to = &s_most[(chunk >> shift) * WARPS + warp];
+                uint32_t most = key;
+#pragma unroll
+                for (int o = 1; o < 8; o <<= 1) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
+                if ((lane & 7) == 0) {
+                    uint32_t* to = &s_most[(chunk >> shift) * (NT / 8) + tid / 8];
                     *to = chunk & ((1 << shift) - 1) ? max(*to, most) : most;
                 }
             }
@@ -329,7 +331,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
 
     // ---- the k best of the block's part
     if (TOP) {
-        const int parts = fine ? chunks * NT : (((chunks - 1) >> shift) + 1) * WARPS;
+        const int parts = fine ? chunks * NT : (((chunks - 1) >> shift) + 1) * (NT / 8);
         __syncthreads();
         uint32_t best = 0;
         for (int i = tid; i < parts; i += NT) best = max(best, s_most[i]);
@@ -358,26 +360,28 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
                     if (j[f] >= 0 && key >= t) add(key, j[f]);
                 }
             }
+            const float least = lp_value(t);         // (t is above the -inf of what is not there, and a NaN is not at or above anything)
+            const int per = 8 * U << shift, total = fine ? 0 : n * per;          // vectors of a part, of all
+            constexpr int VECS = 3;
 #pragma unroll 1
-            for (int i = warp; !fine && i < n; i += WARPS) {
-                const int part = s_part_of[i], c0 = part / WARPS << shift, first = v0 + part % WARPS * 32 + lane;
-#pragma unroll 1
-                for (int c = c0; c < min(c0 + (1 << shift), chunks); ++c) {
-                    const int at = first + c * CHUNK;
-                    uint4 x[U];
+            for (int i0 = tid; i0 < total; i0 += VECS * NT) {
+                uint4 x[VECS];
+                int at[VECS];
 #pragma unroll
-                    for (int u = 0; u < U; ++u) {
-                        x[u].x = x[u].y = x[u].z = x[u].w = F32 ? 0xFF800000u : 0xFF80FF80u;
-                        if (at + u * NT < v1) x[u] = xv[at + u * NT];
-                    }
-#pragma unroll
-                    for (int u = 0; u < U; ++u)
-#pragma unroll
-                        for (int e = 0; e < E; ++e) {
-                            const uint32_t key = lp_key(Vec::get(x[u], e));
-                            if (key >= t) add(key, (at + u * NT) * E + e - lead);      // (t is above the -inf of what is not there)
-                        }
+                for (int f = 0; f < VECS; ++f) {
+                    const int i = i0 + f * NT, part = s_part_of[min(i, total - 1) / per], r = i % per;
+                    const int c = (part / (NT / 8) << shift) + r / (8 * U);
+                    at[f] = v0 + c * CHUNK + r / 8 % U * NT + part % (NT / 8) * 8 + r % 8;
+                    x[f].x = x[f].y = x[f].z = x[f].w = F32 ? 0xFF800000u : 0xFF80FF80u;
+                    if (i < total && at[f] < v1) x[f] = xv[at[f]];
                 }
+#pragma unroll
+                for (int f = 0; f < VECS; ++f)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        const float y = Vec::get(x[f], e);
+                        if (y >= least) add(lp_key(y), at[f] * E + e - lead);
+                    }
             }
             if (edge >= 0) add(lp_key(Vec::value(xr[edge])), edge);
             __syncthreads();
@@ -395,7 +399,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
                     const uint32_t key = s_most[c * NT + tid];
                     most = __syncthreads_or(key > bound) ? 0xFFFFFFFFu : 0u;
                 } else {
-                    for (int w = 0; w < WARPS; ++w) most = max(most, s_most[(c >> shift) * WARPS + w]);
+                    for (int i = 0; i < NT / 8; ++i) most = max(most, s_most[(c >> shift) * (NT / 8) + i]);
                 }
                 if (bound < LP_KEY_LOW || most > bound) again(v0 + c * CHUNK);
             }
