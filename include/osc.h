@@ -652,7 +652,8 @@ osc_status osc_tree_mask(const int32_t* parents, const int32_t* row_off, const i
  * kv_len[r] - n own keys, and of the n new tokens those whose bits are set in its row of the mask (dev uint32 [T][ld_mask], 1 .. OSC_TREE_WORDS words:
  * any bits, as osc_tree_mask writes them or not); new tokens from 32 * words on are seen by nobody.  Where kv_len[r] < n the first n - kv_len[r] new
  * tokens have no key.  A row that sees nothing gives 0 and -inf, and nothing that a row does not see reaches it, Inf and NaN among the values
- * included.  Everything else as in osc_paged_attention, the workspace (osc_paged_attention_workspace_bytes) too; the mask must not overlap what is written. */
+ * included.  Everything else as in osc_paged_attention, the workspace (osc_paged_attention_workspace_bytes) too (of the limits, a tile counts three times); the
+ * mask must not overlap what is written. */
 osc_status osc_tree_attention(const void* Q, int T, int64_t ldq, int n_q, const osc_kv_cache_t* cache, int R, const int32_t* row_off,
                               const int32_t* kv_len, const int32_t* table, int cols, int64_t ld_table, int P, const int32_t* group_off,
                               const int32_t* prefix_len, const int32_t* prefix_table, int prefix_cols, int64_t ld_prefix, const uint32_t* mask,
@@ -665,7 +666,7 @@ osc_status osc_tree_attention(const void* Q, int T, int64_t ldq, int n_q, const 
  *   entropy: float [T] or null: -sum_j p_j ln p_j with p_j = exp(y_j - lse), in nats
  *   top_ids, top_logprobs: int32 / float [T][top_k]: the top_k <= 32 largest logits in falling order, the lower index first among equal ones
  *            (0 and -0 are equal), and their log probabilities; behind the V-th -1 and -inf
- * n_ids = 0 and top_k = 0 leave those out.  scale (one over the temperature) is positive.  Sums in fp32, relative to the row's maximum.  Logits of
+ * n_ids = 0 and top_k = 0 leave those out.  scale (one over the temperature) is positive and below 10^30.  Sums in fp32, relative to the row's maximum.  Logits of
  * -inf have probability 0; a row of nothing else gives -inf, and 0 for the entropy.  A NaN or +inf in a row makes its lse, entropy and log
  * probabilities NaN (of ids in range); NaN comes last among the alternatives.  No output may overlap anything else (OSC_ERR_INVALID_ARG). */
 enum { OSC_BF16 = 0, OSC_F32 = 1 };

@@ -160,7 +160,7 @@ osc_status osc_token_logprobs(const void* logits, int dtype, int T, int V, int64
     if (T < 0 || V < 1 || n_ids < 0 || top_k < 0) return fail(OSC_ERR_INVALID_ARG, "T = %d, V = %d, n_ids = %d, top_k = %d", T, V, n_ids, top_k);
     if (top_k > LP_MAX_TOP) return fail(OSC_ERR_SHAPE, "top_k = %d: at most %d", top_k, LP_MAX_TOP);
     if (V > 0x40000000) return fail(OSC_ERR_SHAPE, "V = %d: at most 2^30", V);
-    if (!(scale > 0.0f) || !(scale < INFINITY)) return fail(OSC_ERR_INVALID_ARG, "scale = %g must be positive and finite", (double)scale);
+    if (!(scale > 0.0f) || !(scale < 1e30f)) return fail(OSC_ERR_INVALID_ARG, "scale = %g must be positive and below 1e30", (double)scale);
     if (T == 0) return OSC_OK;
     if (!logits || (n_ids > 0 && (!ids || !logprob)) || (top_k > 0 && (!top_ids || !top_logprobs))) return fail(OSC_ERR_INVALID_ARG, "null device pointer");
     if (T > 1 && (ld < V || ld_ids < n_ids)) return fail(OSC_ERR_SHAPE, "ld = %lld < V = %d or ld_ids = %lld < n_ids = %d", (long long)ld, V, (long long)ld_ids, n_ids);

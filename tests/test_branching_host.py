@@ -67,7 +67,7 @@ def test_token_logprobs_refusals(B):
         assert call(**{k: None}) == -1, k
     assert call(T=0) == 0 and call(T=0, x=None) == 0
     assert call(dtype=2) == -1 and call(dtype=-1) == -1 and call(T=-1) == -1 and call(V=0) == -1 and call(n_ids=-1) == -1 and call(k=-1) == -1
-    for s in (0.0, -1.0, math.inf, math.nan):
+    for s in (0.0, -1.0, math.inf, math.nan, 2e30):
         assert call(scale=s) == -1, s
     assert call(k=33) == -2 and call(ld=99) == -2 and call(ld_ids=1) == -2 and call(x=0x100001) == -4 and call(x=0x100002, dtype=1) == -4
     for out in ("lp", "lse", "ent", "tid", "tlp"):

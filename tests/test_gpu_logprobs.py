@@ -170,6 +170,27 @@ def test_sure_rows_keep_their_digits(B):
         assert abs(got["entropy"][0] - ent) <= 17 * 2.0 ** -24 + 1e-5 * ent
 
 
+@pytest.mark.parametrize("dtype", DTYPES, ids=["bf16", "f32"])
+@pytest.mark.parametrize("V", [3000, 70000, 300000])
+def test_few_tokens_allowed(B, dtype, V):
+    """All but a few logits masked, fewer than the alternatives asked for: the masked ones follow by index."""
+    rng = np.random.default_rng(V)
+    for n in (1, 5, 19, 40, 600):
+        x = torch.full((2, V), -float("inf"), dtype=dtype, device="cuda")
+        at = rng.choice(V, n, replace=False)
+        x[0, at] = torch.randn(n, generator=torch.Generator().manual_seed(n)).to(dtype).cuda()
+        x[1, at] = 0.5
+        got = call(B, x, [[int(at[0]), 7]] * 2, k=20)
+        for r in range(2):
+            v = x[r].double().cpu().numpy()
+            order = np.lexsort((np.arange(V), -v))[:20]
+            assert got["top_ids"][r].tolist() == order.tolist()
+            lse = np.log(np.exp(v[at]).sum())
+            there = np.isfinite(v[order])
+            assert abs(got["lse"][r] - lse) < 1e-5 and np.abs(got["top_logprobs"][r][there] - v[order][there] + lse).max() < 1e-5
+            assert (got["top_logprobs"][r][~there] == -np.inf).all()
+
+
 def test_ids_outside_and_parts_left_out(B):
     x = rows(3, 500, torch.float32, 4)
     got = call(B, x, [[-1, 500, 2 ** 31 - 1], [0, 499, -2 ** 31], [7, 7, 7]])

@@ -244,6 +244,23 @@ def test_another_stream_and_a_captured_graph(B):
         x.check(o, lse)
 
 
+@pytest.mark.parametrize("new", [[3, 2], [40, 9]])
+def test_a_cache_without_pages(B, new):
+    """Every key reads as zero: equal weights, O = 0, lse = ln of the number of keys that a row sees."""
+    c = TreeCase(91, 4, 4, 128, 16, new, [n + 20 for n in new])
+    want = np.concatenate([np.log(c.sees(r).sum(1)) for r in range(2)])
+    c.k, c.v = (torch.zeros(0, 16, 4, 128, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    o, lse = c.run(B)
+    torch.cuda.synchronize()
+    assert (o == 0).all() and np.abs(lse.cpu().numpy() - want[:, None]).max() < 1e-5
+    # pages that are not there, in a cache that has some
+    c = TreeCase(91, 4, 4, 128, 16, new, [n + 20 for n in new])
+    c.table[:] = torch.where(torch.arange(c.table.shape[1], device="cuda") % 2 == 0, -1, 10 ** 9).int()
+    o, lse = c.run(B)
+    torch.cuda.synchronize()
+    assert (o == 0).all() and np.abs(lse.cpu().numpy() - want[:, None]).max() < 1e-5
+
+
 def test_offsets_that_fall_write_no_row_twice(B):
     """Contents are the caller's; whatever they hold nothing outside the buffers is touched."""
     c = TreeCase(81, 4, 4, 128, 16, [9, 30], [40, 60])
