@@ -3,7 +3,9 @@
 //   d_j = x_j - max x,  l = sum_j exp(scale d_j),  S = sum_j d_j exp(scale d_j)
 //   lse = scale max x + ln l,   log p_j = scale d_j - ln l,   entropy = ln l - scale S / l
 //
-// ln l and -S are never negative, so nothing cancels where a row is sure of one token.  A thread keeps its own (max, l, S) and joins a
+// ln l and -S are never negative, so nothing cancels where a row is sure of one token.  But l is then just above 1, and every addition to a sum that holds the
+// 1 rounds what is above it to 2^-24.  Where l comes out below 1.25, the warp whose thread has the maximum goes over that thread's values (1 / 256 of the
+// row) once more without it, and what is above 1 is summed by itself; ln l is then log1p of that.  A thread keeps its own (max, l, S) and joins a
 // chunk of 16-byte vectors at a time: the chunk's maximum first, one correction of (l, S) if it is a new one, then the chunk's terms
 // (l' = l f, S' = f (S + l (m - m')), f = exp(scale (m - m'))).  A row is one block's, or with few rows a cluster's, whose blocks take
 // consecutive parts and are joined through distributed shared memory, so there is one launch and no workspace.  Every thread copies its own
@@ -90,7 +92,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
     __shared__ unsigned long long s_warp[WARPS];
     __shared__ float s_red[3][WARPS];
     __shared__ unsigned long long s_in[TOP ? LP_MAX_CLUSTER * LP_MAX_TOP : 1];     // the k best of the cluster's other blocks, in the one of rank 0
-    __shared__ float s_part[LP_MAX_CLUSTER][3];      // (max, l, S) of the cluster's blocks, likewise
+    __shared__ float s_part[LP_MAX_CLUSTER][4];      // (max, l, S, l - 1) of the cluster's blocks, likewise
     __shared__ uint32_t s_most[TOP ? LP_PARTS : 1];                       // largest key above -inf of every part
     // behind the loop the ring holds
     unsigned long long* s_list = reinterpret_cast<unsigned long long*>(lp_ring);       // candidates
@@ -411,7 +413,8 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
         }
     }
 
-    // ---- the block's (max, l, S)
+    // ---- the block's (max, l, S), and l - 1 where that is small
+    float above = 0.0f;
     {
         float M = m;
 #pragma unroll
@@ -438,13 +441,55 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
             s_red[2][warp] = ss;
         }
         __syncthreads();
-        m = M;
-        l = S = 0.0f;
+        float sum = 0.0f, sum_S = 0.0f;
 #pragma unroll
         for (int w = 0; w < WARPS; ++w) {
-            l += s_red[1][w];
-            S += s_red[2][w];
+            sum += s_red[1][w];
+            sum_S += s_red[2][w];
         }
+        if (sum < 1.25f && M > -INFINITY) {          // the same for all threads
+            float part = m == M ? 0.0f : l * f;
+            int count = 0;
+            uint32_t owners = __ballot_sync(0xFFFFFFFFu, m == M);
+#pragma unroll 1
+            for (; owners; owners &= owners - 1) {
+                const int of = __ffs((int)owners) - 1;
+                const int its_edge = __shfl_sync(0xFFFFFFFFu, edge, of);
+                auto take = [&](float x) {
+                    if (x == M) ++count;
+                    else part += lp_exp2((x - M) * scale2);
+                };
+                if (lane == 0 && its_edge >= 0) take(Vec::value(xr[its_edge]));
+#pragma unroll 1
+                for (int i = lane; i < chunks * U; i += 32) {
+                    const int at = v0 + i * NT + warp * 32 + of;
+                    if (at >= v1) continue;
+                    const uint4 x = xv[at];
+#pragma unroll
+                    for (int e = 0; e < E; ++e) take(Vec::get(x, e));
+                }
+            }
+#pragma unroll
+            for (int o = 16; o; o >>= 1) {
+                part += __shfl_xor_sync(0xFFFFFFFFu, part, o);
+                count += __shfl_xor_sync(0xFFFFFFFFu, count, o);
+            }
+            __syncthreads();             // the sums have been read
+            if (lane == 0) {
+                s_red[0][warp] = part;
+                s_red[1][warp] = (float)count;
+            }
+            __syncthreads();
+            float times = -1.0f;
+            for (int w = 0; w < WARPS; ++w) {
+                above += s_red[0][w];
+                times += s_red[1][w];
+            }
+            above += times;              // 0, but for several maxima
+        }
+        m = M;
+        l = sum;
+        S = sum_S;
     }
 
     // ---- the cluster's: the others hand their sums and their k best to rank 0, which joins them in rank order
@@ -457,15 +502,16 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
                 st_cluster(to, (uint32_t)x);
                 st_cluster(to + 4, (uint32_t)(x >> 32));
             }
-            if (tid < 3) st_cluster(map_to_cta(smem_u32(&s_part[rank][tid]), 0), __float_as_uint(tid == 0 ? m : tid == 1 ? l : S));
-        } else if (tid < 3) {
-            s_part[0][tid] = tid == 0 ? m : tid == 1 ? l : S;
+            if (tid < 4) st_cluster(map_to_cta(smem_u32(&s_part[rank][tid]), 0), __float_as_uint(tid == 0 ? m : tid == 1 ? l : tid == 2 ? S : above));
+        } else if (tid < 4) {
+            s_part[0][tid] = tid == 0 ? m : tid == 1 ? l : tid == 2 ? S : above;
         }
         asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
         if (rank) return;
         m = -INFINITY;
         for (int c = 0; c < cluster; ++c) m = fmaxf(m, s_part[c][0]);
         l = S = 0.0f;
+        above = 0.0f;
         for (int c = 0; c < cluster; ++c) {
             const float pl = s_part[c][1];
             if (pl == 0.0f) continue;
@@ -473,10 +519,11 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
             if (f == 0.0f && pl == pl) continue;
             l += pl * f;
             S += f * (s_part[c][2] + pl * d);
+            above += s_part[c][0] == m ? s_part[c][3] : pl * f;      // (two blocks with the maximum: l is 2 at least)
         }
         if (TOP) rank_list(s_in, (cluster - 1) * k);
     }
-    const float ln = logf(l), nan = __uint_as_float(0x7FC00000u);
+    const float ln = l < 1.25f ? log1pf(above) : logf(l), nan = __uint_as_float(0x7FC00000u);
     const bool empty = l == 0.0f;        // no logit above -inf
     const bool bad = m == INFINITY;
     auto logprob = [&](float x) { return bad ? nan : empty ? -INFINITY : a.scale * (x - m) - ln; };

@@ -191,6 +191,29 @@ def test_few_tokens_allowed(B, dtype, V):
             assert (got["top_logprobs"][r][~there] == -np.inf).all()
 
 
+@pytest.mark.parametrize("dtype", DTYPES, ids=["bf16", "f32"])
+@pytest.mark.parametrize("V", [7, 300, 4001, 33000, 152064])
+def test_very_sure_rows(B, dtype, V):
+    """Where one token has nearly all of the probability, ln l = ln(1 + r), and r is summed without the 1.  Relative to its own size r is off as any sum of
+    exponentials is (e_l in `tolerances`, here with |scale d| up to 60), and so are the log probability and the entropy, r (1 + lead) and less."""
+    for lead in (9.0, 14.0, 25.0, 40.0):
+        x = rows(4, V, dtype, V, mul=1.0, ld=V + 3, at=1)
+        best = np.array([0, V - 1, V // 2, V // 3])
+        x[torch.arange(4), torch.from_numpy(best)] = lead + np.log(V)
+        got = call(B, x, best[:, None], k=2)
+        xd = x.double().cpu().numpy()
+        d = xd - xd[np.arange(4), best][:, None]
+        d[np.arange(4), best] = -np.inf
+        with np.errstate(invalid="ignore"):
+            r = np.exp(d).sum(1)
+            s = np.where(np.isfinite(d), np.exp(d) * d, 0).sum(1)
+        rel = 4 * 60 * 2.0 ** -24 + 2.0 ** -21 + (V / 512 + 60) * 2.0 ** -24
+        assert np.array_equal(got["top_ids"][:, 0], best)
+        assert (np.abs(got["logprob"][:, 0] + np.log1p(r)) <= rel * np.log1p(r)).all(), (got["logprob"][:, 0], -np.log1p(r))
+        ent = np.log1p(r) - s / (1 + r)
+        assert (np.abs(got["entropy"] - ent) <= 2 * rel * ent).all(), (got["entropy"], ent)
+
+
 def test_ids_outside_and_parts_left_out(B):
     x = rows(3, 500, torch.float32, 4)
     got = call(B, x, [[-1, 500, 2 ** 31 - 1], [0, 499, -2 ** 31], [7, 7, 7]])
