@@ -4,7 +4,7 @@
 //   lse = scale max x + ln l,   log p_j = scale d_j - ln l,   entropy = ln l - scale S / l
 //
 // ln l and -S are never negative, so nothing cancels where a row is sure of one token.  But l is then just above 1, and every addition to a sum that holds the
-// 1 rounds what is above it to 2^-24.  Where l comes out below 1.25, the warp whose thread has the maximum goes over that thread's values (1 / 256 of the
+// 1 rounds what is above it to 2^-24.  Where l comes out below 1 + 2^-7, the warp whose thread has the maximum goes over that thread's values (1 / 256 of the
 // row) once more without it, and what is above 1 is summed by itself; ln l is then log1p of that.  A thread keeps its own (max, l, S) and joins a
 // chunk of 16-byte vectors at a time: the chunk's maximum first, one correction of (l, S) if it is a new one, then the chunk's terms
 // (l' = l f, S' = f (S + l (m - m')), f = exp(scale (m - m'))).  A row is one block's, or with few rows a cluster's, whose blocks take
@@ -32,6 +32,7 @@ static_assert(LP_VECS * 8 <= 32, "a lane for every value of a thread");
 constexpr int LP_STAGES = 3;             // chunks in the ring
 constexpr int LP_SHORT_BYTES = 16384;    // rows up to here
 constexpr int LP_PARTS = 1024;           // parts of a block's row
+constexpr float LP_SURE = 1.0f + 1.0f / 128;
 constexpr int LP_MAX_TOP = 32;
 constexpr int LP_LIST = 512;            // candidates that wait to be ranked
 constexpr int LP_MAX_CLUSTER = 8;
@@ -447,7 +448,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
             sum += s_red[1][w];
             sum_S += s_red[2][w];
         }
-        if (sum < 1.25f && M > -INFINITY) {          // the same for all threads
+        if (sum < LP_SURE && M > -INFINITY) {          // the same for all threads
             float part = m == M ? 0.0f : l * f;
             int count = 0;
             uint32_t owners = __ballot_sync(0xFFFFFFFFu, m == M);
@@ -461,12 +462,18 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
                 };
                 if (lane == 0 && its_edge >= 0) take(Vec::value(xr[its_edge]));
 #pragma unroll 1
-                for (int i = lane; i < chunks * U; i += 32) {
-                    const int at = v0 + i * NT + warp * 32 + of;
-                    if (at >= v1) continue;
-                    const uint4 x = xv[at];
+                for (int i = lane; i < chunks * U; i += 3 * 32) {
+                    uint4 x[3];
 #pragma unroll
-                    for (int e = 0; e < E; ++e) take(Vec::get(x, e));
+                    for (int f = 0; f < 3; ++f) {
+                        const int at = v0 + (i + f * 32) * NT + warp * 32 + of;
+                        x[f].x = x[f].y = x[f].z = x[f].w = F32 ? 0xFF800000u : 0xFF80FF80u;
+                        if (i + f * 32 < chunks * U && at < v1) x[f] = xv[at];
+                    }
+#pragma unroll
+                    for (int f = 0; f < 3; ++f)
+#pragma unroll
+                        for (int e = 0; e < E; ++e) take(Vec::get(x[f], e));
                 }
             }
 #pragma unroll
@@ -523,7 +530,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
         }
         if (TOP) rank_list(s_in, (cluster - 1) * k);
     }
-    const float ln = l < 1.25f ? log1pf(above) : logf(l), nan = __uint_as_float(0x7FC00000u);
+    const float ln = l < LP_SURE ? log1pf(above) : logf(l), nan = __uint_as_float(0x7FC00000u);
     const bool empty = l == 0.0f;        // no logit above -inf
     const bool bad = m == INFINITY;
     auto logprob = [&](float x) { return bad ? nan : empty ? -INFINITY : a.scale * (x - m) - ln; };
