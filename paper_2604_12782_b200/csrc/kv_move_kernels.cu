@@ -148,7 +148,7 @@ struct KvCompactArgs {
 
 __global__ void __launch_bounds__(KC_THREADS) kv_compact_kernel(const __grid_constant__ KvCompactArgs a, bool write_len) {
     __shared__ int64_t s_from[KC_LIST], s_to[KC_LIST];
-    __shared__ int s_stop;
+    __shared__ int s_stop, s_moved;      // first entry that ends the list, first one that moves
     grid_launch_dependents();
     grid_dependency_wait();
     const KvPlanes& l = a.l;
@@ -165,24 +165,25 @@ __global__ void __launch_bounds__(KC_THREADS) kv_compact_kernel(const __grid_con
         return p >= 0 && p < l.n_pages ? p * l.page_stride + (at - col * l.page) * l.token_stride : -1;
     };
     int done = 0;
-    while (done < count) {       // KC_LIST entries at a time
-        if (threadIdx.x == 0) s_stop = KC_LIST;
-        __syncthreads();
+    while (true) {               // KC_LIST entries at a time
+        // The list is read next to the lengths, and the pages of all its entries next to the check of their order: two trips to memory in front of the rows.
         const int d = done + threadIdx.x;
-        int k = -1;
-        if (d < count) {
+        int k = -1, last = -1;
+        if (d < a.keep_cols) {
             k = keep[d];
-            if (k >= n || k <= (d ? keep[d - 1] : -1)) atomicMin(&s_stop, (int)threadIdx.x);
+            if (d) last = keep[d - 1];
         }
+        if (threadIdx.x == 0) s_stop = s_moved = KC_LIST;
         __syncthreads();
-        const int good = min(s_stop, count - done);
-        // entries that stay where they are come first (an index above its place leaves all behind it above theirs)
-        const int still = __syncthreads_count((int)threadIdx.x < good && k == d);
-        if ((int)threadIdx.x < good) {
+        if (d < count) {
+            if (k >= n || k <= last) atomicMin(&s_stop, (int)threadIdx.x);
+            if (k != d) atomicMin(&s_moved, (int)threadIdx.x);
             s_from[threadIdx.x] = place(ctx + k);
             s_to[threadIdx.x] = place(ctx + d);
         }
         __syncthreads();
+        // entries that stay where they are come first (an index above its place leaves all behind it above theirs)
+        const int good = min(s_stop, min(count - done, KC_LIST)), still = min(s_moved, good);
         if (still < good)
             for (int x = split * KC_THREADS + threadIdx.x; x < l.planes * l.row; x += a.splits * KC_THREADS) {
                 const int plane = x / l.row;
