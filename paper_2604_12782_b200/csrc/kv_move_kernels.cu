@@ -49,7 +49,8 @@ __device__ __forceinline__ int search_last(const long long* start, int n, long l
 // on), gets no bits and position 0.
 // A request's parents go through shared memory; a thread walks up from its token.  Parents come before their children, so the
 // walk meets falling indices and a row's words are finished one after the other, without an array.  Latency bounds it: offsets -> parents ->
-// walk -> stores, each step of a walk one shared-memory load (a chain of 1024 tokens is the longest).
+// walk -> stores, each step of a walk one shared-memory load (a chain of 1024 tokens is the longest).  26 tokens of one request 4.2 us from a CUDA graph, an empty
+// launch's time; 16201 tokens of 500 requests 7.6 us, where the bytes would take 0.1.  A block for every request, not one for several, as the chain is the time.
 constexpr int TREE_THREADS = 128;
 
 struct TreeMaskArgs {
@@ -130,7 +131,10 @@ __device__ __forceinline__ int64_t unit_offset(const KvPlanes& l, int u) {
 // goes to place ctx + d.  An index is at least its place in the list, so walking the list in order never overwrites what is still to be
 // read, and neither does reading several entries ahead: a thread takes one 16-byte column of one plane (keys or values of a layer) and
 // moves it for all entries, KC_FLIGHT loads at a time.  Every byte is read and written once: HBM bounds it once there is enough of it, the
-// chain offsets -> list -> pages -> rows in front of the first load before that.
+// chain offsets -> list -> pages -> rows in front of the first load before that.  96 requests, 36 layers, 86 MB read and written: 22.3 us from a CUDA graph, 17 to 18 of
+// them in the kernel, where the copy rate gives 13.1; one request 4.2 us.  What is left of the 96 is that chain, three trips to memory before a block's
+// rows, twice over (the blocks are 1.5 rounds of those resident).  Three columns to a thread (26.7 us), eight entries under way (23.6) and two or four times the blocks (22.5) were
+// no better: a request accepts about three tokens, so there is little to keep under way.
 constexpr int KC_THREADS = 256, KC_LIST = 256, KC_FLIGHT = 4;
 
 struct KvCompactArgs {
@@ -206,7 +210,8 @@ __global__ void __launch_bounds__(KC_THREADS) kv_compact_kernel(const __grid_con
 }
 
 // kv_copy_pages: the first `used` places of page from[i] to page to[i], in every plane.  A block takes a part of one page of one plane; its threads
-// walk over 16-byte units, KP_FLIGHT loads at a time.
+// walk over 16-byte units, KP_FLIGHT loads at a time.  HBM: 1505 tokens of 90 forks in 36 layers, 444 MB read and written, in 65 us, the copy rate; the planes of a page are neighbours
+// on the grid because their pages are the same, so that a block's three trips (pages, count, rows) overlap with its neighbours' rows.
 constexpr int KP_THREADS = 256, KP_FLIGHT = 8;
 
 struct KvCopyArgs {
@@ -272,7 +277,8 @@ cudaError_t launch_kv_copy_pages(const KvCopyArgs& args, int num_sms, cudaStream
 // One cluster: the rows' columns are flattened (a scan over the requests, which every block does for itself) and shared out over all
 // its threads; the bitmap of freed pages is spread over the blocks' shared memories (remote atomics), so nothing has to be cleared or kept in
 // global memory; then every block lists its part behind those of lower rank.  The decrement that takes a count from 1 to 0 happens once,
-// so does its bit.  (A count that was 0 or less is put back: it never reaches 1 on the way.)
+// so does its bit.  (A count that was 0 or less is put back: it never reaches 1 on the way.)  Latency bounds it: 7 to 8 us for 192 rows.  One launch of one
+// cluster instead of three of a grid (clear, mark, list): the bitmap is small, and a launch costs as much as the whole call.
 constexpr int TRIM_CLUSTER = 8, TRIM_THREADS = 512;
 constexpr int TRIM_MAX_WORDS = 48 * 1024;     // of a block's part of the bitmap: 12.5 million pages in all
 
@@ -381,7 +387,8 @@ cudaError_t launch_kv_trim(const KvTrimArgs& args, cudaStream_t st) {
 // ------------------------------------------------------------------------------------------------ kv_fork
 // Row dst[i] of the table becomes a fork of row src[i], which holds `len` tokens: the full pages are shared (their counts of holders
 // rise by one), and for tokens on a page that is not full the fork takes a page of its own from the free list, forks in order, and asks for a
-// copy of those tokens.  (No row is both forked and a fork, so the lengths that block 0 writes are read by nobody.)  As in kv_slots every block scans the forks for itself; table entries are then shared out over the grid.
+// copy of those tokens.  (No row is both forked and a fork, so the lengths that block 0 writes are read by nobody.)  As in kv_slots every block scans the
+// forks for itself; table entries are then shared out over the grid.  Latency: lengths -> scan -> search -> entry -> store, 5 to 6 us for 90 forks.
 constexpr int FORK_THREADS = 256;
 
 struct KvForkArgs {
