@@ -854,7 +854,9 @@ static cudaError_t launch_attn_d(const AttnWideArgs& w, bool wide, cudaStream_t 
         if (e != cudaSuccess) return e;
     }
     JoinGrid g;
-    g.wide_split = (int64_t)a.T * a.G >= 2048 ? 8 : a.P ? 1 : 16;      // with few rows and prefixes nearly all of them have two sources
+    // Blocks to a CTA's cut unit.  With few rows and prefixes nearly all of them have two sources, which the blocks by rows join; without prefixes few units are all
+    // there is, in many pieces (one tree of 26 tokens 41.2 us with 1, 31.4 with 4, 24.6 with 16, five contexts of 40000 keys 275, 266, 255).
+    g.wide_split = (int64_t)a.T * a.G >= 2048 ? 8 : a.P ? 1 : 16;
     g.few_split = wide ? 1 : a.few_hw;
     g.wide_blocks = wide ? a.wide_ctas * g.wide_split : 0;
     g.row_blocks = a.P ? (int)std::min<int64_t>(3 * AT_MAX_SMS, ((int64_t)a.T * a.Hq + AT_JOIN_WARPS - 1) / AT_JOIN_WARPS) : 0;

@@ -269,8 +269,8 @@ static osc_status attention(const void* Q, int T, int64_t ldq, int n_q, const os
     a.few_ctas = std::min(di.num_sms * (wide ? 4 : 2), AT_FEW_CTAS);
     a.wide_min_rows = wide ? AT_FEW_ROWS + 1 : 0x7FFFFFFF;
     // Trees: where requests have more rows than that on average, all go to the tcgen05 kernel (HBM bounds its units with few rows as it does the few-row
-    // kernel), and without prefixes that kernel lays out its line itself: two launches instead of four.  With the few-row kernel beside it for
-    // requests of up to 16 rows 24 trees behind 4200 keys each took 142 us, with the tcgen05 kernel alone 130; one tree of 26 tokens 41.6 and 26.7.
+    // kernel), and without prefixes that kernel lays out its line itself: two launches instead of four.  24 trees behind 4200 keys each take 137 us with
+    // the few-row kernel beside it, 136 without it but with the plan kernel, 130 so; one tree of 26 tokens behind 900 keys 28.9, 26.9 and 24.6.
     if (wide && words && (int64_t)T * a.G > (int64_t)R * AT_FEW_ROWS) {
         a.wide_min_rows = 1;
         a.self = P == 0 && R <= WIDE_SELF;

@@ -22,8 +22,9 @@
 // Bound: without alternatives HBM (3001 rows of 152064 bf16 logits 150 us, 0.93 of the copy rate), with 20 of them the issue of instructions (189 us, 0.73: 3.1 of 4 slots a
 // cycle, of which the exponentials' conversions, products and sums are most); 1500 such rows of fp32, half as many values to a byte, 149 us, 0.93.  Few rows:
 // latency, 26 rows of 128000 in fp32 12.4 us, 2.0 at the copy rate.  Two rules on sizes.  Rows of up to 16 KB are on blocks of two warps: a block of
-// eight has less than a chunk of them, and the steps behind the loop, which cost a block the same whatever the row, bound them (20000 rows of 4096 in bf16
-// 117 us with eight warps, 92 with two).  Rows that do not fill the machine are split over clusters of up to eight (one row of 151936 in fp32 12.6 us).
+// eight has less than a chunk of them, and the steps behind the loop, which cost a block the same whatever the row, bound them (with 20 alternatives 20000 rows of
+// 4096 in bf16 234 us with eight warps, 131 with two, of 8192, the longest that count as short, 250 and 161).  Rows that do not fill the machine are split over
+// clusters of up to eight (one row of 151936 in fp32 26.8 us without, 12.6 with; 220 of them in bf16, the most that still are, 26.9 and 24.8).
 #include <cuda_bf16.h>
 
 #include <algorithm>
