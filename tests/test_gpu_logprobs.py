@@ -82,6 +82,13 @@ def test_shapes(B, dtype, T, V, k):
 
 
 @pytest.mark.parametrize("dtype", DTYPES, ids=["bf16", "f32"])
+@pytest.mark.parametrize("T,V,k", [(2, 262144, 32), (17, 200001, 1), (30, 151937, 20), (60, 131073, 0), (120, 99999, 8), (250, 65537, 5)])
+def test_rows_over_clusters(B, dtype, T, V, k):
+    """Rows of several chunks to a block, on clusters of eight, four, two and one."""
+    check(B, rows(T, V, dtype, V), np.random.default_rng(V).integers(0, V, (T, 2)), k=k)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=["bf16", "f32"])
 @pytest.mark.parametrize("at,pad", [(0, 1), (1, 0), (3, 5), (7, 2), (5, 8), (2, 3)])
 def test_rows_at_any_element(B, dtype, at, pad):
     for V in (5, 100, 20000):
