@@ -131,10 +131,10 @@ __device__ __forceinline__ int64_t unit_offset(const KvPlanes& l, int u) {
 // goes to place ctx + d.  An index is at least its place in the list, so walking the list in order never overwrites what is still to be
 // read, and neither does reading several entries ahead: a thread takes one 16-byte column of one plane (keys or values of a layer) and
 // moves it for all entries, KC_FLIGHT loads at a time.  Every byte is read and written once: HBM bounds it once there is enough of it, the
-// chain offsets -> list -> pages -> rows in front of the first load before that.  96 requests, 36 layers, 86 MB read and written: 22.3 us from a CUDA graph, 17 to 18 of
+// chain offsets -> list -> pages -> rows in front of the first load before that.  96 requests, 36 layers, 86 MB read and written: 21.6 us from a CUDA graph, 17 to 18 of
 // them in the kernel, where the copy rate gives 13.1; one request 4.2 us.  What is left of the 96 is that chain, three trips to memory before a block's
-// rows, twice over (the blocks are 1.5 rounds of those resident).  Three columns to a thread (26.7 us), eight entries under way (23.6) and two or four times the blocks (22.5) were
-// no better: a request accepts about three tokens, so there is little to keep under way.
+// rows.  Three columns to a thread (26.7 us) and eight entries under way (23.6) were no better: a request accepts about three tokens, so there is little to keep under way, and
+// other blocks are what hides the chain.
 constexpr int KC_THREADS = 256, KC_LIST = 256, KC_FLIGHT = 4;
 
 struct KvCompactArgs {
@@ -254,9 +254,10 @@ __global__ void __launch_bounds__(KP_THREADS) kv_copy_pages_kernel(const __grid_
 
 cudaError_t launch_kv_compact(const KvCompactArgs& args, bool write_len, int num_sms, cudaStream_t st) {
     KvCompactArgs a = args;
-    // a block for every KC_THREADS columns, as long as all of them are resident at once
+    // A block for every KC_THREADS columns, as long as that is no more than 16 to an SM, two to three rounds of those resident (96 / 250 / 600 requests, 86 / 207 / 160 MB: 24.4 / 54.9 / - us
+    // with 6, 22.3 / 49.6 / 49.3 with 8, 21.6 / 44.4 / 36.8 with 16, 21.9 / 41.5 / 35.1 with 32, where other sizes take 6-8 % longer than with 16).
     const int most = (a.l.planes * a.l.row + KC_THREADS - 1) / KC_THREADS;
-    a.splits = std::max(1, std::min(most, num_sms * 8 / std::max(a.R, 1)));
+    a.splits = std::max(1, std::min(most, num_sms * 16 / std::max(a.R, 1)));
     return launch_pdl(kv_compact_kernel, dim3(a.R * a.splits), dim3(KC_THREADS), 0, st, a, write_len);
 }
 
