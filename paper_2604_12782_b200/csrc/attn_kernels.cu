@@ -1055,13 +1055,14 @@ __device__ __forceinline__ void join_row(const AttnArgs& a, const PieceList (&p)
 // Blocks in this order: those with the longest chains come first, the many that mostly find nothing to do last.
 struct JoinGrid {
     int row_blocks;          // over the tokens' rows
-    int wide_blocks;         // wide_ctas x wide_split: a part of the 256 rows of a cut wide unit each
+    int wide_blocks;         // over the wide_ctas << wide_split parts of the 256 rows of a cut wide unit: one to a block, or (WALK) up to 32
     int wide_split;
-    int few_split;           // few_ctas x few_split: a part of the rows of a cut few-row unit each
+    int few_split;           // few_ctas << few_split blocks: a part of the rows of a cut few-row unit each
 };
 
 constexpr int64_t AT_JOIN_FEW_ROWS = 4096;     // between 224 and 256032 rows of the two steps above
-template <int D, int FLIGHT>
+// WALK: blocks look at several parts of cut wide units each.
+template <int D, int FLIGHT, bool WALK>
 __global__ void __launch_bounds__(AT_JOIN_THREADS, FLIGHT > 8 ? 2 : 3) attn_join_kernel(const AttnArgs a, const JoinGrid grid) {
     grid_launch_dependents();
     grid_dependency_wait();
@@ -1074,16 +1075,30 @@ __global__ void __launch_bounds__(AT_JOIN_THREADS, FLIGHT > 8 ? 2 : 3) attn_join
         const bool wide = b < grid.wide_blocks;
         if (!wide) b -= grid.wide_blocks;
         const int split = wide ? grid.wide_split : grid.few_split;
-        const CutUnit cut = a.plan.cut[wide][b / split];
-        if (cut.tiles == 0) return;
-        const int slot_rows = wide ? 2 * AT_WIDE_TILE : a.few_hw * AT_FEW_ROWS, rows = slot_rows / split, part = b % split;
+        const int slot_rows = wide ? 2 * AT_WIDE_TILE : a.few_hw * AT_FEW_ROWS, rows = slot_rows >> split;
+        uint32_t has = 1;        // which of its parts have something to join: lane i looks at the i-th
+        const int parts = a.wide_ctas << split;
+        if (WALK && wide && grid.wide_blocks < parts) {
+            const int at = b + (threadIdx.x & 31) * grid.wide_blocks;
+            has = __ballot_sync(0xFFFFFFFFu, at < parts && a.plan.cut[1][at >> split].tiles != 0);
+        }
 #pragma unroll 1
-        for (int i = warp; i < rows; i += AT_JOIN_WARPS) {
-            const int row = part * rows + i, r = wide ? row % AT_WIDE_TILE : cut.u * AT_FEW_ROWS + row % AT_FEW_ROWS;
-            const int tok = r / a.G + (wide ? (cut.u * 2 + row / AT_WIDE_TILE) * a.tpt : 0);
-            if ((wide && r >= a.tpt * a.G) || tok >= cut.n) continue;
-            p[1] = list_pieces(cut.begin, cut.tiles, cut.weight, cut.share, wide ? AT_FEW_SLOTS : 0, slot_rows, row, 0);
-            join_row<D, FLIGHT>(a, p, cut.t0 + tok, (wide ? cut.h : cut.h * a.few_hw + row / AT_FEW_ROWS) * a.G + r % a.G);
+        for (; has; has &= has - 1) {
+            const int at = WALK ? b + (__ffs((int)has) - 1) * grid.wide_blocks : b;
+            const CutUnit cut = a.plan.cut[wide][at >> split];
+            if (cut.tiles == 0) return;
+            const int row0 = (at & ((1 << split) - 1)) * rows;
+            const PieceList list = list_pieces(cut.begin, cut.tiles, cut.weight, cut.share, wide ? AT_FEW_SLOTS : 0, slot_rows, 0, 0);      // two pieces at least
+#pragma unroll 1
+            for (int i = warp; i < rows; i += AT_JOIN_WARPS) {
+                const int row = row0 + i, r = wide ? row % AT_WIDE_TILE : cut.u * AT_FEW_ROWS + row % AT_FEW_ROWS;
+                const int tok = r / a.G + (wide ? (cut.u * 2 + row / AT_WIDE_TILE) * a.tpt : 0);
+                if ((wide && r >= a.tpt * a.G) || tok >= cut.n) continue;
+                p[1] = list;
+                p[1].first += row;
+                p[1].rest += row;
+                join_row<D, FLIGHT>(a, p, cut.t0 + tok, (wide ? cut.h : cut.h * a.few_hw + row / AT_FEW_ROWS) * a.G + r % a.G);
+            }
         }
         return;
     }
