@@ -857,7 +857,7 @@ static cudaError_t launch_attn_d(const AttnWideArgs& w, bool wide, cudaStream_t 
     // Parts of a CTA's cut unit.  With few rows and prefixes nearly all of them have two sources, which the blocks by rows join; without prefixes few units are all
     // there is, in many pieces (one tree of 26 tokens 41.2 us with 1, 31.4 with 4, 24.6 with 16, five contexts of 40000 keys 275, 266, 255; a prompt of 100 tokens
     // behind 1900 keys 60, 40.8 and 34.9).  Sixteen parts go to two blocks a CTA, eight parts each: with a block to a part steps without any cut unit pay for the launch
-    // of 2368 blocks (one decoding request of 600 keys whose caller does not say so 25.3 us, 21.1 with 296, 20.1 with 148, where the tree takes 26.8)  Masked steps of many
+    // of 2368 blocks (one decoding request of 600 keys whose caller does not say so 25.3 us, 21.1 with 296, 20.1 with 148, where the tree takes 26.8).  Masked steps of many
     // rows, whose units are cut nearly always, keep a block to a part (five contexts of 40000 keys 265 us, 274 with 296 blocks).
     g.wide_split = (int64_t)a.T * a.G >= 2048 ? 3 : a.P ? 0 : 4;
     g.few_split = wide || a.few_hw == 1 ? 0 : a.few_hw == 2 ? 1 : 2;

@@ -108,7 +108,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
     __shared__ int s_parts;
     __shared__ int s_n, s_over;                      // candidates; whether some found no place
     grid_launch_dependents();
-    if (cluster > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");      // every block is there before anyone writes to rank 0
+    if (cluster > 1) cluster_meet();                 // every block is there before anyone writes to rank 0
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rank = cluster > 1 ? (int)cluster_ctarank() : 0;
     const int64_t row = blockIdx.x / cluster;
@@ -508,7 +508,6 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
 
     // ---- the cluster's: the others hand their sums and their k best to rank 0, which joins them in rank order
     if (cluster > 1) {
-        asm volatile("barrier.cluster.wait;" ::: "memory");
         if (rank) {
             if (TOP && tid < k) {
                 const unsigned long long x = s_kept[which][tid];
@@ -520,7 +519,8 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
         } else if (tid < 4) {
             s_part[0][tid] = tid == 0 ? m : tid == 1 ? l : tid == 2 ? S : above;
         }
-        asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+        __syncwarp();
+        cluster_sync_all();
         if (rank) return;
         m = -INFINITY;
         for (int c = 0; c < cluster; ++c) m = fmaxf(m, s_part[c][0]);
