@@ -311,6 +311,7 @@ __global__ void __launch_bounds__(TRIM_THREADS) kv_trim_kernel(const KvTrimArgs 
     for (int w = tid; w < a.part; w += TRIM_THREADS) s_bits[w] = 0;
     const uint32_t bits = smem_u32(s_bits), counts = smem_u32(s_count);
     grid_dependency_wait();
+    __syncwarp();
     cluster_sync_all();      // all parts are clear
     for (int r0 = 0; r0 < a.R; r0 += TRIM_THREADS) {
         const int nr = min(TRIM_THREADS, a.R - r0);
@@ -344,6 +345,7 @@ __global__ void __launch_bounds__(TRIM_THREADS) kv_trim_kernel(const KvTrimArgs 
     for (int w = tid; w < a.part; w += TRIM_THREADS) mine += __popc(s_bits[w]);
     block_scan(mine, total, s_warp, TRIM_THREADS / 32);
     if (tid < TRIM_CLUSTER) st_cluster(map_to_cta(counts + rank * 4, tid), (uint32_t)total);
+    __syncwarp();
     cluster_sync_all();
     int at = 0, all = 0;
     for (int b = 0; b < TRIM_CLUSTER; ++b) {
