@@ -3,6 +3,9 @@
 //   d_j = x_j - max x,  l = sum_j exp(scale d_j),  S = sum_j d_j exp(scale d_j)
 //   lse = scale max x + ln l,   log p_j = scale d_j - ln l,   entropy = ln l - scale S / l
 //
+// For a scale so small that logits near the end of fp32's range still count (below 10^-20: no difference that has a weight passes 10^22 otherwise, nor does a sum
+// of 2^30 of them end the range) differences and S are held in units of 2^40 (SMALL: kernels of their own, whose loop takes values one by one).
+//
 // ln l and -S are never negative, so nothing cancels where a row is sure of one token.  But l is then just above 1, and every addition to a sum that holds the
 // 1 rounds what is above it to 2^-24.  Where l comes out below 1 + 2^-7, the warp whose thread has the maximum goes over that thread's values (1 / 256 of the
 // row) once more without it, and what is above 1 is summed by itself; ln l is then log1p of that.  A thread keeps its own (max, l, S) and joins a
@@ -90,7 +93,7 @@ struct LpVec {
     }
 };
 
-template <bool F32, bool TOP, int NT>
+template <bool F32, bool TOP, int NT, bool SMALL>
 __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const LogprobArgs a, int cluster) {
     using Vec = LpVec<F32>;
     using Elem = typename Vec::Elem;
@@ -112,7 +115,9 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rank = cluster > 1 ? (int)cluster_ctarank() : 0;
     const int64_t row = blockIdx.x / cluster;
-    const float scale2 = a.scale * 1.44269504088896341f;
+    constexpr float UNIT = SMALL ? 0x1p-40f : 1.0f;              // differences are held as x UNIT - max UNIT
+    const float rate = SMALL ? a.scale * 0x1p40f : a.scale, scale2 = rate * 1.44269504088896341f;
+    auto diff = [&](float x, float from) { return SMALL ? x * UNIT - from * UNIT : x - from; };
     const int k = TOP ? a.k : 0;
     if (TOP) {
         if (tid == 0) s_n = s_over = s_parts = 0;
@@ -279,7 +284,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
         // ---- (max, l, S)
         if (top > m) {
             if (m > -INFINITY) {
-                const float d = m - top, f = lp_exp2(d * scale2);
+                const float d = diff(m, top), f = lp_exp2(d * scale2);
                 S = f == 0.0f ? 0.0f : f * (S + l * d);      // d may be -inf
                 l *= f;
             }
@@ -287,39 +292,45 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
         }
         {
             // A thread without a value above -inf has nothing to add; but a NaN has to reach the sums.
-            const float ref = m == -INFINITY ? 0.0f : -m;
-            const uint64_t ref2 = pack2(ref, ref), sc2 = pack2(scale2, scale2);
-            uint64_t lc = 0, sc = 0;
+            const float ref = m == -INFINITY ? 0.0f : -(m * UNIT);
+            float sum = 0.0f;
+            if (!SMALL) {
+                const uint64_t ref2 = pack2(ref, ref), sc2 = pack2(scale2, scale2);
+                uint64_t lc = 0, sc = 0;
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (base + u * NT + tid >= v1) break;
+                for (int u = 0; u < U; ++u) {
+                    if (base + u * NT + tid >= v1) break;
 #pragma unroll
-                for (int e = 0; e < E; e += 2) {
-                    const uint64_t d = add2(pack2(Vec::get(v[u], e), Vec::get(v[u], e + 1)), ref2);
-                    float t0, t1;
-                    unpack2(mul2(d, sc2), t0, t1);
-                    const uint64_t p = pack2(lp_exp2(t0), lp_exp2(t1));
-                    lc = add2(lc, p);
-                    sc = fma2(p, d, sc);
+                    for (int e = 0; e < E; e += 2) {
+                        const uint64_t d = add2(pack2(Vec::get(v[u], e), Vec::get(v[u], e + 1)), ref2);
+                        float t0, t1;
+                        unpack2(mul2(d, sc2), t0, t1);
+                        const uint64_t p = pack2(lp_exp2(t0), lp_exp2(t1));
+                        lc = add2(lc, p);
+                        sc = fma2(p, d, sc);
+                    }
                 }
+                float l0, l1, s0, s1;
+                unpack2(lc, l0, l1);
+                unpack2(sc, s0, s1);
+                l += l0 + l1;
+                sum = s0 + s1;
             }
-            float l0, l1, s0, s1;
-            unpack2(lc, l0, l1);
-            unpack2(sc, s0, s1);
-            float sum = s0 + s1;
-            if (sum != sum) {        // 0 * -inf: -inf among the logits (or a NaN, or +inf, which l shows)
+            if (SMALL || sum != sum) {        // 0 * -inf: -inf among the logits (or a NaN, or +inf, which l shows)
+                float more = 0.0f;
                 sum = 0.0f;
 #pragma unroll 1
                 for (int u = 0; u < U && base + u * NT + tid < v1; ++u) {
                     const uint4 x = at[u * NT];
 #pragma unroll
                     for (int e = 0; e < E; ++e) {
-                        const float d = Vec::get(x, e) + ref, p = lp_exp2(d * scale2);
+                        const float d = Vec::get(x, e) * UNIT + ref, p = lp_exp2(d * scale2);
+                        more += p;
                         sum += p == 0.0f ? 0.0f : p * d;
                     }
                 }
+                if (SMALL) l += more;
             }
-            l += l0 + l1;
             S += sum;
         }
         if (TOP) {
@@ -434,7 +445,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
         for (int w = 1; w < WARPS; ++w) M = fmaxf(M, s_red[0][w]);
         float f = 1.0f, d = 0.0f;
         if (m != -INFINITY || l != 0.0f) {           // l without a maximum: a NaN
-            d = m == -INFINITY ? 0.0f : m - M;
+            d = m == -INFINITY ? 0.0f : diff(m, M);
             f = lp_exp2(d * scale2);
         }
         float ls = l * f, ss = l != 0.0f ? f * (S + l * d) : 0.0f;
@@ -465,7 +476,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
                 const int its_edge = __shfl_sync(0xFFFFFFFFu, edge, of);
                 auto take = [&](float x) {
                     if (x == M) ++count;
-                    else part += lp_exp2((x - M) * scale2);
+                    else part += lp_exp2(diff(x, M) * scale2);
                 };
                 if (lane == 0 && its_edge >= 0) take(Vec::value(xr[its_edge]));
 #pragma unroll 1
@@ -529,7 +540,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
         for (int c = 0; c < cluster; ++c) {
             const float pl = s_part[c][1];
             if (pl == 0.0f) continue;
-            const float d = s_part[c][0] == -INFINITY ? 0.0f : s_part[c][0] - m, f = lp_exp2(d * scale2);
+            const float d = s_part[c][0] == -INFINITY ? 0.0f : diff(s_part[c][0], m), f = lp_exp2(d * scale2);
             if (f == 0.0f && pl == pl) continue;
             l += pl * f;
             S += f * (s_part[c][2] + pl * d);
@@ -540,10 +551,10 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
     const float ln = l < LP_SURE ? log1pf(above) : logf(l), nan = __uint_as_float(0x7FC00000u);
     const bool empty = l == 0.0f;        // no logit above -inf
     const bool bad = m == INFINITY;
-    auto logprob = [&](float x) { return bad ? nan : empty ? -INFINITY : a.scale * (x - m) - ln; };
+    auto logprob = [&](float x) { return bad ? nan : empty ? -INFINITY : 2.0f * rate * (0.5f * UNIT * x - 0.5f * UNIT * m) - ln; };      // (halves: x - m may pass the range)
     if (tid == 0) {
         if (a.lse) a.lse[row] = bad ? nan : empty ? -INFINITY : a.scale * m + ln;
-        if (a.entropy) a.entropy[row] = bad ? nan : empty ? 0.0f : ln - a.scale * S / l;
+        if (a.entropy) a.entropy[row] = bad ? nan : empty ? 0.0f : ln - rate * S / l;
     }
     for (int i = tid; i < a.n_ids; i += NT) {
         const int id = a.ids[row * a.ld_ids + i];
@@ -559,11 +570,11 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprobs_kernel(const Log
     }
 }
 
-template <bool F32, bool TOP, int NT>
+template <bool F32, bool TOP, int NT, bool SMALL = false>
 static cudaError_t launch_logprobs_t(const LogprobArgs& a, int cluster, cudaStream_t st) {
     static PerDevice pd;
     constexpr int RING = LP_STAGES * NT * LP_VECS * 16;
-    if (cudaError_t e = opt_in_shared_memory(pd, token_logprobs_kernel<F32, TOP, NT>, RING)) return e;
+    if (cudaError_t e = opt_in_shared_memory(pd, token_logprobs_kernel<F32, TOP, NT, SMALL>, RING)) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((int64_t)a.T * cluster));
     cfg.blockDim = dim3(NT);
@@ -578,10 +589,11 @@ static cudaError_t launch_logprobs_t(const LogprobArgs& a, int cluster, cudaStre
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = cluster > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, token_logprobs_kernel<F32, TOP, NT>, a, cluster);
+    return cudaLaunchKernelEx(&cfg, token_logprobs_kernel<F32, TOP, NT, SMALL>, a, cluster);
 }
 template <bool F32, bool TOP>
 static cudaError_t launch_logprobs(const LogprobArgs& a, int num_sms, cudaStream_t st) {
+    if (a.scale < 1e-20f) return launch_logprobs_t<F32, TOP, 256, true>(a, 1, st);
     // Short rows, many of them: blocks of two warps, of which 16 are on an SM at a time.
     if ((int64_t)a.V * (F32 ? 4 : 2) <= LP_SHORT_BYTES) return launch_logprobs_t<F32, TOP, 64>(a, 1, st);
     // A cluster where the rows alone do not fill the machine, as long as every block of it has a chunk's work.
