@@ -676,7 +676,7 @@ osc_status osc_token_logprobs(const void* logits, int dtype, int T, int V, int64
 /* Accepted tokens moved together behind the context, keys and values of all layers in one call.  Of request r's n = row_off[r + 1] - row_off[r] new
  * tokens, the last n of kv_len[r], the one with index keep[r][d] goes to the place of new token d; the indices rise, and the list ends
  * where it does not (or at an index outside 0 .. n - 1), at n_keep[r] or at keep_cols entries.
- *   layers: host array of n_layers caches of one shape and strides (k and v of their own each), read during the call
+ *   layers: host array of n_layers caches of one shape and strides, read during the call; k and v of their own each (the same address twice: OSC_ERR_INVALID_ARG)
  *   keep: dev int32 [R][ld_keep];  n_keep: dev int32 [R];  new_len: int32 [R]: kv_len[r] - n + tokens kept (it must not overlap the inputs)
  * Places whose page is not in the table (entries outside 0 .. n_pages - 1, or past cols) are left out.  Pages of new tokens belong to one
  * request only.  R <= 2^20. */

