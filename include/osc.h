@@ -633,7 +633,11 @@ osc_status osc_paged_attention(const void* Q, int T, int64_t ldq, int n_q, const
 /* A step that verifies drafted tokens gives every request its whole tree of them as new tokens: osc_kv_slots and osc_qk_norm_rope as for any new
  * tokens (positions from osc_tree_mask), osc_tree_attention per layer, osc_token_logprobs on the logits, and osc_kv_compact for the tokens that were
  * accepted (osc_kv_trim for pages that are no longer needed).  A step of a beam search gives the pages of beams that end back (osc_kv_trim), forks
- * rows of the page table (osc_kv_fork) and copies the pages that are not full (osc_kv_copy_pages). */
+ * rows of the page table (osc_kv_fork) and copies the pages that are not full (osc_kv_copy_pages).
+ * The pool of free pages is the caller's, and so is the count of the pages that osc_kv_slots takes, which knows of none: where counts are kept
+ * (refs below), the caller raises those of free_pages[0] .. free_pages[taken - 1] by one after that call.  A page that nobody has counted is not freed
+ * when it is given back, and a fork of it would be its only holder that counts.  Either can be kept on the device, with a list that is filled up with -1 behind
+ * its pages (-1 is no page: what would have been placed on it has no slot, or no copy), so that a step is captured as a whole. */
 #define OSC_TREE_WORDS 32
 
 /* Ancestors and positions of the tokens of drafted trees (once per step).
@@ -686,8 +690,8 @@ osc_status osc_kv_compact(const osc_kv_cache_t* layers, int n_layers, int R, con
 
 /* Pages given back: request r shrinks from from_len[r] to to_len[r] tokens (0: it ends), and the pages of columns ceil(to / page_size) ..
  * ceil(from / page_size) - 1 of its table row leave it; those entries become -1 (entries outside 0 .. n_pages - 1 only do that).
- *   refs:  dev int32 [n_pages] or null: number of table rows that hold a page; falls by one for every row that gives it back, not below 0.  A
- *          page is freed when it reaches 0.  null: every page has one holder.
+ *   refs:  dev int32 [n_pages] or null: number of table rows that hold a page (for pages from osc_kv_slots the caller's to raise, see above); falls by one for
+ *          every row that gives it back, not below 0.  A page is freed when it reaches 0 from 1.  null: every page has one holder.
  *   freed: int32 [n_pages]: the freed pages in rising order, n_freed: int32 [1] of them; the rest is left as it is
  * A second call with the same inputs finds nothing to give back.  n_pages <= 12 million.  What is written (table and refs included) must not overlap anything
  * else (OSC_ERR_INVALID_ARG). */

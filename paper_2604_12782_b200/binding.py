@@ -1077,7 +1077,8 @@ def osc_kv_compact(layers: KvLayers, row_off, kv_len, table, keep, n_keep, new_l
 
 def osc_kv_trim(from_len, to_len, page_size: int, table, refs, freed, n_freed, n_pages: int = None, stream=None):
     """Pages given back by requests that shrink from from_len to to_len [R] tokens; table [R, cols] and refs [n_pages] (or None) are updated in place,
-    freed [n_pages] and n_freed [1] are written.  All int32.  n_pages: the length of refs, or of freed without it, if it is not given."""
+    freed [n_pages] and n_freed [1] are written.  All int32.  n_pages: the length of refs, or of freed without it, if it is not given.  (refs of pages that
+    osc_kv_slots took are the caller's to raise.)"""
     dev, i32 = _device_of(from_len), torch.int32
     if _bad(i32, dev, from_len, to_len, refs, freed, n_freed) or _bad_rows(i32, dev, table):
         _refuse(i32, 1, dev, from_len=from_len, to_len=to_len, refs=refs, freed=freed, n_freed=n_freed)
