@@ -120,7 +120,7 @@ __device__ __forceinline__ uint64_t smem_desc_sw128_mn(uint32_t saddr, uint32_t 
 constexpr uint32_t IDESC_B_MN = 1u << 16;   // B operand with its N extent contiguous
 
 // What the roles need to know of a unit, or of the part of it that the CTA's share has: key tiles [ka, ka + n).  The units
-// warp walks over the line and keeps two of these ahead in shared memory.
+// warp walks over the line and keeps one of these ahead, in a ring of AW_UNITS in shared memory.
 struct __align__(16) WideUnit {
     int ka, n;          // n = 0: the share is done
     int cnt[2];         // key tiles of stream 0 and 1

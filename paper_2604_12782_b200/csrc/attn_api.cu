@@ -270,7 +270,11 @@ static osc_status attention(const void* Q, int T, int64_t ldq, int n_q, const os
     a.wide_min_rows = wide ? AT_FEW_ROWS + 1 : 0x7FFFFFFF;
     // Trees: where requests have more rows than that on average, all go to the tcgen05 kernel (HBM bounds its units with few rows as it does the few-row
     // kernel), and without prefixes that kernel lays out its line itself: two launches instead of four.  24 trees behind 4200 keys each take 137 us with
-    // the few-row kernel beside it, 136 without it but with the plan kernel, 130 so; one tree of 26 tokens behind 900 keys 28.9, 26.9 and 24.6.
+    // the few-row kernel beside it, 136 without it but with the plan kernel, 130 so; one tree of 26 tokens behind 900 keys 28.9, 26.9 and 24.6.  The host knows no
+    // lengths but T and R (rows that fill a step up count too), so this goes by the mean.  Requests of one size gain from just above it on (24 of 5 tokens, 20
+    // rows, behind 2000 keys 67 us, 74 with the few-row kernel; 96 of 5 behind 1000 106 and 114); steps whose mean a few large trees lift above it
+    // lose, as single tokens then pay a unit's beginning and end (90 single tokens beside 6 trees of 64, 20 rows on average, all behind 1000 keys 110 and 98, behind
+    // 4000 335 and 275; 200 beside 20 trees 234 and 171; 20 beside 4 trees of 40 66 and 69).
     if (wide && words && (int64_t)T * a.G > (int64_t)R * AT_FEW_ROWS) {
         a.wide_min_rows = 1;
         a.self = P == 0 && R <= WIDE_SELF;

@@ -285,6 +285,9 @@ __device__ __forceinline__ int wide_share(const AttnArgs& a, int N, int ctas) { 
 __device__ __forceinline__ void share_lines(const AttnArgs& a, int nf, int nw, int32_t* share) {
     const int sms = a.wide_ctas;
     int wide = sms, few = min(a.few_ctas, 2 * sms);
+    // With a mask a tile has two places, or three with both row tiles: 0.4 of a tile to a place.  (Small drafts behind a prefix, 0.25 / 0.4 / 0.65 / 1: 64 of 2
+    // tokens behind 16000 + 1000 keys 106 / 96 / 103 / 105 us, 200 of 3 behind 2000 + 800 174 / 155 / 152 / 181, 96 of 3 behind 4000 + 500 88 / 86 / 87 / 92,
+    // 32 of 3 behind 4000 + 300 47 / 50 / 50 / 50.)
     const float tiles = a.mask ? 0.4f * nw : (float)nw;
     if (nf > 0 && nw > 0) wide = max((int)(sms * (3.0f * tiles) / (3.0f * tiles + nf) + 0.5f), 1);
     const int q = wide_share(a, nw, wide);

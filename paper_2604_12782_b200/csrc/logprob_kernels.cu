@@ -7,8 +7,8 @@
 // of 2^30 of them end the range) differences and S are held in units of 2^40 (SMALL: kernels of their own, whose loop takes values one by one).
 //
 // ln l and -S are never negative, so nothing cancels where a row is sure of one token.  But l is then just above 1, and every addition to a sum that holds the
-// 1 rounds what is above it to 2^-24.  Where l comes out below 1 + 2^-7, the warp whose thread has the maximum goes over that thread's values (1 / 256 of the
-// row) once more without it, and what is above 1 is summed by itself; ln l is then log1p of that.  A thread keeps its own (max, l, S) and joins a
+// 1 rounds what is above it to 2^-24.  Where l comes out below 1 + 2^-7, the warp whose thread has the maximum goes over that thread's values (one part of
+// as many as the row has threads) once more without it, and what is above 1 is summed by itself; ln l is then log1p of that.  A thread keeps its own (max, l, S) and joins a
 // chunk of 16-byte vectors at a time: the chunk's maximum first, one correction of (l, S) if it is a new one, then the chunk's terms
 // (l' = l f, S' = f (S + l (m - m')), f = exp(scale (m - m'))).  A row is one block's, or with few rows a cluster's, whose blocks take
 // consecutive parts and are joined through distributed shared memory, so there is one launch and no workspace.  Every thread copies its own
@@ -594,7 +594,7 @@ static cudaError_t launch_logprobs_t(const LogprobArgs& a, int cluster, cudaStre
 template <bool F32, bool TOP>
 static cudaError_t launch_logprobs(const LogprobArgs& a, int num_sms, cudaStream_t st) {
     if (a.scale < 1e-20f) return launch_logprobs_t<F32, TOP, 256, true>(a, 1, st);
-    // Short rows, many of them: blocks of two warps, of which 16 are on an SM at a time.
+    // Short rows, many of them: blocks of two warps, of which 16 are on an SM at a time, 11 with alternatives (shared memory).
     if ((int64_t)a.V * (F32 ? 4 : 2) <= LP_SHORT_BYTES) return launch_logprobs_t<F32, TOP, 64>(a, 1, st);
     // A cluster where the rows alone do not fill the machine, as long as every block of it has a chunk's work.
     const int64_t chunk = 256ll * LP_VECS * (F32 ? 4 : 8);
