@@ -42,3 +42,25 @@ def test_sure_rows_relative_to_their_size(B, V, lead):       # noqa: F811
     one = 2 * (V / 64 + 40) * 2.0 ** -24 if rest >= 1 / 128 else 0.0
     assert rest < 1 and abs(got["logprob"][0, 0] - lp) <= rel * abs(lp) + one and abs(got["top_logprobs"][0, 0] - lp) <= rel * abs(lp) + one
     assert abs(got["entropy"][0] - ent) <= 2 * rel * ent + one * (1 + lead)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=["bf16", "f32"])
+def test_a_very_long_row(B, dtype):                          # noqa: F811
+    """2^27 logits: several thousand chunks to a block, parts of many chunks.  On its way into l a term goes through one addition for every chunk of its block
+    (4096 values of fp32, an eighth of the row: V / 32768) and less than 100 others, each off by 2^-24; exponents and exp2 as in `tolerances`."""
+    V = 2 ** 27 + 5
+    x = torch.randn(1, V, device="cuda", generator=torch.Generator(device="cuda").manual_seed(3)).mul_(3.0).to(dtype)
+    got = call(B, x, [[0, V - 1, V // 3]], k=20)
+    y = x[0].double()
+    top = y.max()
+    l = (y - top).exp().sum()
+    lse = (top + l.log()).item()
+    e_l = 120 * 2.0 ** -24 + 2.0 ** -22 + (V / 32768 + 100) * 2.0 ** -24
+    assert abs(got["lse"][0] - lse) <= e_l + 2.0 ** -20
+    assert np.abs(got["logprob"][0] - (y[torch.tensor([0, V - 1, V // 3], device="cuda")] - lse).cpu().numpy()).max() <= e_l + 2.0 ** -19
+    ent = (l.log() - ((y - top).exp() * (y - top)).sum() / l).item()
+    assert abs(got["entropy"][0] - ent) <= 3 * e_l * 20 + 2.0 ** -18
+    best = x[0].float().topk(4000).values[19]
+    at = torch.nonzero(x[0] >= best.to(dtype))[:, 0]
+    order = at[torch.argsort(x[0, at].float(), descending=True, stable=True)][:20]
+    assert got["top_ids"][0].tolist() == order.tolist()
