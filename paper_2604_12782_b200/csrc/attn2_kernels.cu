@@ -855,14 +855,15 @@ static cudaError_t launch_attn_d(const AttnWideArgs& w, bool wide, cudaStream_t 
     }
     JoinGrid g;
     // Parts of a CTA's cut unit.  With few rows and prefixes nearly all of them have two sources, which the blocks by rows join; without prefixes few units are all
-    // there is, in many pieces (one tree of 26 tokens 41.2 us with 1, 31.4 with 4, 24.6 with 16, five contexts of 40000 keys 275, 266, 255; a prompt of 100 tokens
-    // behind 1900 keys 60, 40.8 and 34.9).  Sixteen parts go to two blocks a CTA, eight parts each: with a block to a part steps without any cut unit pay for the launch
-    // of 2368 blocks (one decoding request of 600 keys whose caller does not say so 25.3 us, 21.1 with 296, 20.1 with 148, where the tree takes 26.8).  Masked steps of many
-    // rows, whose units are cut nearly always, keep a block to a part (five contexts of 40000 keys 265 us, 274 with 296 blocks).
+    // there is, in many pieces (one tree of 26 tokens 41.2 us with 1, 31.4 with 4, 23.8 with 16, five contexts of 40000 keys 275, 266, 255; a prompt of 100 tokens
+    // behind 1900 keys 60, 40.8 and 30.9).  Sixteen parts are shared out over two or six blocks a CTA: with a block for every part that there can be, steps without
+    // any cut unit pay for the launch of 2368 (one decoding request of 600 keys whose caller does not say so 25.0 us, 21.2 with 296, 20.3 with 148, where the
+    // prompt takes 34.8; 256 requests of 512 keys 105.7, 104.4 with 888, 103.9 with 592, where 20 prompts of 20 tokens take 54.1 instead of 52.4), and blocks
+    // with fixed parts of their own have several where others have none (a prompt of 64 tokens behind 30000 keys 86 us, shared out 58).
     g.wide_split = (int64_t)a.T * a.G >= 2048 ? 3 : a.P ? 0 : 4;
     g.few_split = wide || a.few_hw == 1 ? 0 : a.few_hw == 2 ? 1 : 2;
-    const bool flight = (int64_t)a.T * a.Hq <= AT_JOIN_FEW_ROWS, walk = wide && g.wide_split == 4 && (flight || !a.mask);
-    g.wide_blocks = wide ? a.wide_ctas << (walk ? 1 : g.wide_split) : 0;
+    const bool flight = (int64_t)a.T * a.Hq <= AT_JOIN_FEW_ROWS, walk = wide && g.wide_split == 4;
+    g.wide_blocks = !wide ? 0 : walk ? a.wide_ctas * (flight ? 2 : 6) : a.wide_ctas << g.wide_split;
     g.row_blocks = a.P ? (int)std::min<int64_t>(3 * AT_MAX_SMS, ((int64_t)a.T * a.Hq + AT_JOIN_WARPS - 1) / AT_JOIN_WARPS) : 0;
     const auto kernel = flight ? (walk ? attn_join_kernel<D, 16, true> : attn_join_kernel<D, 16, false>)
         : walk ? attn_join_kernel<D, 8, true> : attn_join_kernel<D, 8, false>;

@@ -1058,13 +1058,13 @@ __device__ __forceinline__ void join_row(const AttnArgs& a, const PieceList (&p)
 // Blocks in this order: those with the longest chains come first, the many that mostly find nothing to do last.
 struct JoinGrid {
     int row_blocks;          // over the tokens' rows
-    int wide_blocks;         // over the wide_ctas << wide_split parts of the 256 rows of a cut wide unit: one to a block, or (WALK) up to 32
+    int wide_blocks;         // over the parts, 1 << wide_split of them, of the 256 rows of a cut wide unit: a block for every part that there can be, or
+                             // (WALK) fewer, that share out the parts that there are
     int wide_split;
     int few_split;           // few_ctas << few_split blocks: a part of the rows of a cut few-row unit each
 };
 
 constexpr int64_t AT_JOIN_FEW_ROWS = 4096;     // between 224 and 256032 rows of the two steps above
-// WALK: blocks look at several parts of cut wide units each.
 template <int D, int FLIGHT, bool WALK>
 __global__ void __launch_bounds__(AT_JOIN_THREADS, FLIGHT > 8 ? 2 : 3) attn_join_kernel(const AttnArgs a, const JoinGrid grid) {
     grid_launch_dependents();
@@ -1079,18 +1079,33 @@ __global__ void __launch_bounds__(AT_JOIN_THREADS, FLIGHT > 8 ? 2 : 3) attn_join
         if (!wide) b -= grid.wide_blocks;
         const int split = wide ? grid.wide_split : grid.few_split;
         const int slot_rows = wide ? 2 * AT_WIDE_TILE : a.few_hw * AT_FEW_ROWS, rows = slot_rows >> split;
-        uint32_t has = 1;        // which of its parts have something to join: lane i looks at the i-th
-        const int parts = a.wide_ctas << split;
-        if (WALK && wide && grid.wide_blocks < parts) {
-            const int at = b + (threadIdx.x & 31) * grid.wide_blocks;
-            has = __ballot_sync(0xFFFFFFFFu, at < parts && a.plan.cut[1][at >> split].tiles != 0);
-        }
 #pragma unroll 1
-        for (; has; has &= has - 1) {
-            const int at = WALK ? b + (__ffs((int)has) - 1) * grid.wide_blocks : b;
-            const CutUnit cut = a.plan.cut[wide][at >> split];
+        for (int part = b;; part += grid.wide_blocks) {
+            int c = part >> split;               // CTA that told the unit
+            if (WALK && wide) {                  // the (part >> split)-th of those that told one
+                constexpr int WORDS = (AT_WIDE_CTAS + 31) / 32;
+                int tiles[WORDS], n = c;
+                c = -1;
+#pragma unroll
+                for (int i = 0; i < WORDS; ++i) {
+                    const int at = i * 32 + (threadIdx.x & 31);
+                    tiles[i] = at < a.wide_ctas ? a.plan.cut[1][at].tiles : 0;
+                }
+#pragma unroll
+                for (int i = 0; i < WORDS; ++i) {
+                    uint32_t told = __ballot_sync(0xFFFFFFFFu, tiles[i] != 0);
+                    const int k = __popc(told);
+                    if (c < 0 && n < k) {
+                        for (; n > 0; --n) told &= told - 1;
+                        c = i * 32 + __ffs((int)told) - 1;
+                    }
+                    n -= k;
+                }
+                if (c < 0) return;
+            }
+            const CutUnit cut = a.plan.cut[wide][c];
             if (cut.tiles == 0) return;
-            const int row0 = (at & ((1 << split) - 1)) * rows;
+            const int row0 = (part & ((1 << split) - 1)) * rows;
             const PieceList list = list_pieces(cut.begin, cut.tiles, cut.weight, cut.share, wide ? AT_FEW_SLOTS : 0, slot_rows, 0, 0);      // two pieces at least
 #pragma unroll 1
             for (int i = warp; i < rows; i += AT_JOIN_WARPS) {
@@ -1102,8 +1117,8 @@ __global__ void __launch_bounds__(AT_JOIN_THREADS, FLIGHT > 8 ? 2 : 3) attn_join
                 p[1].rest += row;
                 join_row<D, FLIGHT>(a, p, cut.t0 + tok, (wide ? cut.h : cut.h * a.few_hw + row / AT_FEW_ROWS) * a.G + r % a.G);
             }
+            if (!WALK || !wide) return;
         }
-        return;
     }
     // rows that have a prefix and own keys
     const int two = a.plan.share[2], nf = a.plan.share[0], nw = a.plan.share[1], rows = a.T * a.Hq;

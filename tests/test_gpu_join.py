@@ -3,6 +3,7 @@ while the caller has not said so (max_new = 0): what joins the pieces looks at a
 import pytest
 import torch
 
+from branching_inputs import TreeCase
 from serving_inputs import AttnCase
 
 pytestmark = pytest.mark.gpu
@@ -24,6 +25,9 @@ def B():
     (2, 8, 128, 64, [33], [9000]),
     (1, 1, 64, 16, [700], [700]),
     (3, 7, 128, 16, [60], [3001]),
+    (8, 4, 128, 16, [130], [3000]),
+    (8, 4, 128, 64, [1] * 30 + [200, 1, 70], [40] * 30 + [1500, 2, 900]),
+    (4, 2, 64, 16, [64, 3, 90], [6000, 3, 500]),
 ])
 def test_few_units_in_many_pieces(B, Hk, G, D, page, new, kv):
     assert sum(new) * G < 2048
@@ -36,3 +40,9 @@ def test_few_units_in_many_pieces(B, Hk, G, D, page, new, kv):
 def test_decoding_steps_that_are_not_announced(B, Hk, G, D, R, kv):
     c = AttnCase(4, Hk, G, D, 16, [1] * R, [kv + 13 * r for r in range(R)], tail_rows=1)
     c.check(*c.run(B))
+
+
+@pytest.mark.parametrize("Hk,G,D,page,new,kv", [(8, 4, 128, 16, [140], [2500]), (2, 4, 64, 16, [60, 1, 33], [5000, 800, 33])])
+def test_trees_in_many_pieces(B, Hk, G, D, page, new, kv):
+    c = TreeCase(5, Hk, G, D, page, new, kv, tail_rows=1)
+    c.check(*c.run(B, max_new=max(new)))
