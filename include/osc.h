@@ -655,9 +655,10 @@ osc_status osc_tree_mask(const int32_t* parents, const int32_t* row_off, const i
 /* osc_paged_attention with a mask among the new tokens instead of their order.  A row sees the keys of its group's prefix, the request's first
  * kv_len[r] - n own keys, and of the n new tokens those whose bits are set in its row of the mask (dev uint32 [T][ld_mask], 1 .. OSC_TREE_WORDS words:
  * any bits, as osc_tree_mask writes them or not); new tokens from 32 * words on are seen by nobody.  Where kv_len[r] < n the first n - kv_len[r] new
- * tokens have no key.  A row that sees nothing gives 0 and -inf, and nothing that a row does not see reaches it, Inf and NaN among the values
- * included.  Everything else as in osc_paged_attention, the workspace (osc_paged_attention_workspace_bytes) too (of the limits, a tile counts three times); the
- * mask must not overlap what is written. */
+ * tokens have no key.  (A kv_len that passes what the table's columns hold is cut to that here too, and the new tokens are the last n keys of what is left, not
+ * those that osc_kv_slots placed: drafts end where the table does.)  A row that sees nothing gives 0 and -inf, and nothing that a row does not see reaches it,
+ * Inf and NaN among the values included.  Everything else as in osc_paged_attention, the workspace (osc_paged_attention_workspace_bytes) too (of the
+ * limits, a tile counts three times); the mask must not overlap what is written. */
 osc_status osc_tree_attention(const void* Q, int T, int64_t ldq, int n_q, const osc_kv_cache_t* cache, int R, const int32_t* row_off,
                               const int32_t* kv_len, const int32_t* table, int cols, int64_t ld_table, int P, const int32_t* group_off,
                               const int32_t* prefix_len, const int32_t* prefix_table, int prefix_cols, int64_t ld_prefix, const uint32_t* mask,

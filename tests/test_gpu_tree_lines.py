@@ -103,3 +103,15 @@ def test_calls_repeat_themselves(B, new, kv, prefix):
             junk.normal_()
         o2, lse2 = c.run(B)
         assert torch.equal(o.view(torch.int16), o2.view(torch.int16)) and torch.equal(lse.view(torch.int32), lse2.view(torch.int32)), i
+
+
+@pytest.mark.parametrize("new,kv", [([3, 20], 96), ([2, 1, 1], 64)])
+def test_lengths_past_the_table_are_cut(B, new, kv):
+    """To what the columns hold, the new tokens being the last keys of that."""
+    c = TreeCase(15, 4, 4, 128, 16, new, [kv] * len(new), prefix=[32])
+    o, lse = c.run(B)
+    c.kv_len.fill_(100000)
+    c.prefix_len.fill_(2 ** 31 - 1)
+    c.table, c.ptable = c.table[:, :kv // 16].contiguous(), c.ptable[:, :2].contiguous()
+    o2, lse2 = c.run(B)
+    assert torch.equal(o, o2) and torch.equal(lse, lse2)
