@@ -635,7 +635,7 @@ osc_status osc_paged_attention(const void* Q, int T, int64_t ldq, int n_q, const
  * accepted (osc_kv_trim for pages that are no longer needed).  A step of a beam search gives the pages of beams that end back (osc_kv_trim), forks
  * rows of the page table (osc_kv_fork) and copies the pages that are not full (osc_kv_copy_pages).
  * The pool of free pages is the caller's, and so is the count of the pages that osc_kv_slots takes, which knows of none: where counts are kept
- * (refs below), the caller raises those of free_pages[0] .. free_pages[taken - 1] by one after that call.  A page that nobody has counted is not freed
+ * (refs below), the caller raises those of free_pages[0] .. free_pages[min(taken, n_free) - 1] by one after that call.  A page that nobody has counted is not freed
  * when it is given back, and a fork of it would be its only holder that counts.  Either can be kept on the device, with a list that is filled up with -1 behind
  * its pages (-1 is no page: what would have been placed on it has no slot, or no copy), so that a step is captured as a whole. */
 #define OSC_TREE_WORDS 32
